@@ -49,9 +49,10 @@ typedef enum {
     SSBA_ERR_CUDA = 3,        /* a CUDA runtime/driver call or launch failed               */
     SSBA_ERR_TIMEOUT = 4,     /* (device status) a bounded wait inside a kernel ran out    */
     SSBA_ERR_WORKSPACE = 5,   /* workspace missing or smaller than ssba_mask_workspace_bytes */
-    SSBA_ERR_CHECK = 6        /* (device status, checked build only) an index list broke its
-                                 invariants: a label outside [0, Tb), not ascending, or a
-                                 count other than keep                                      */
+    SSBA_ERR_CHECK = 6        /* (device status) checked build only: an index list broke its
+                                 invariants (a label outside [0, Tb), not ascending, or a
+                                 count other than keep); every build: a page table, length,
+                                 row range or list of the paged cache was out of range       */
 } ssba_status;
 
 typedef enum { SSBA_BF16 = 0, SSBA_FP32 = 1 } ssba_dtype;
@@ -375,8 +376,105 @@ SSBA_API int ssba_test_backward_late(const ssba_desc* desc, const void* Q, const
                                      const int32_t* kv_cnt, float* dQ, float* dK, float* dV, void* workspace,
                                      size_t ws_bytes, uint64_t budget_ns, void* stream);
 
-/* Reads and clears the device status word of the current device (SSBA_OK or
- * SSBA_ERR_TIMEOUT). Synchronous: call after the caller's stream sync. Returns
+/* ------------------------------------------------------------------ paged 8-bit K/V cache
+ * The gate and the attention of Sec. 2.2 for a model that is served token by token: K and V live in
+ * a pool of 64-token pages in 8 bits, each query selects pages by their mean keys, and attention reads
+ * those alone (or everything). The paper has no counterpart to these calls; its gate, taken from
+ * block attention over sequences (Sec. 2.2), is the same.
+ *
+ * Shapes and rules shared by the calls below
+ *   Pool       ssba_cache: K, V e4m3 [pages][kv_heads][64][head_dim], k_scale, v_scale fp32
+ *              [pages][kv_heads] (value = e4m3 value * scale), k_mean fp32 [pages][kv_heads][head_dim]
+ *              (mean key of every full page). Device memory of the caller's; needs no initial contents.
+ *   Batch      B sequences and T rows. Rows [cu[b], cu[b + 1]) are the new tokens of sequence b (cu int32
+ *              [B + 1], ascending, none may be negative or above T); rows from cu[B] on belong to none and
+ *              are neither read nor written. table int32 [B][width]: page table[b][j] holds tokens 64 j ..
+ *              64 j + 63; entries behind a sequence's last page may hold anything. lens int32 [B]: tokens
+ *              that sequence b holds when the call runs, for ssba_cache_append those in front of the new
+ *              ones, for the others all of them, the new ones its last. A sequence may have no rows or
+ *              no tokens.
+ *   Checks     table, lens, cu and lists are device memory and are checked on the device: lengths and
+ *              rows are clamped to what the buffers hold, a page outside [0, pages) or a listed label
+ *              outside the row's pages is left out, and the status word reads SSBA_ERR_CHECK (in
+ *              every build). No such value reaches memory out of range.
+ *   Errors     as above; B = 0 or T = 0 is no work and succeeds. */
+#define SSBA_CACHE_PAGE 64
+#define SSBA_CACHE_MAX_HEADS 16384   /* heads */
+#define SSBA_CACHE_MAX_ROWS (1 << 24) /* T and B */
+#define SSBA_CACHE_MAX_WIDTH 32768   /* pages of a selection's sequences, and keep */
+
+/* heads        query heads, a multiple of kv_heads; query heads [g * heads / kv_heads, (g + 1) * ...) share
+ *              K/V head g.
+ * head_dim     64 or 128.
+ * pages        pages of the pool.
+ * dtype        ssba_dtype of k, v, q and O.
+ * softmax_scale  scale of q.k inside the softmax; 0 selects 1/sqrt(head_dim). */
+typedef struct {
+    int32_t heads, kv_heads, head_dim, pages;
+    int32_t dtype;
+    float softmax_scale;
+} ssba_cache_desc;
+
+typedef struct {
+    void *K, *V;               /* 128-byte aligned */
+    float *k_scale, *v_scale;
+    float *k_mean;             /* 16-byte aligned */
+} ssba_cache;
+
+/* Writes new tokens into their sequences' pages.
+ *   k, v        device, [T][kv_heads][head_dim] of desc->dtype.
+ * Token i of sequence b goes to position lens[b] + i. Of each page and head that takes new tokens, the
+ * scale becomes the smallest power of two (at least 2^-126; 0 when all are zero) under which no new finite
+ * value passes 448, or stays as it is where that is larger and the page held tokens before; a new value
+ * is held as e4m3(x / scale), rounded to nearest; where the scale has grown the page's older tokens are
+ * rounded again under the new one. NaN and infinities are held as NaN and have no part in the scale. The rest
+ * of a page stays as it was. A page whose 64th token is among the new ones gets its k_mean, the mean of
+ * its held keys. Tokens behind the table's last page are left out and flagged.
+ * No two sequences may append to one page in one call. lens is not changed. */
+SSBA_API int ssba_cache_append(const ssba_cache_desc* desc, const ssba_cache* cache, const void* k, const void* v,
+                               int32_t T, const int32_t* table, int32_t width, const int32_t* lens,
+                               const int32_t* cu, int32_t B, void* stream);
+
+/* Selects the pages that each row attends to.
+ *   q           device, [T][heads][head_dim] of desc->dtype.
+ *   keep, first pages kept a row, and how many of a sequence's first pages are always among them;
+ *               0 <= first < keep.
+ *   idx, cnt    device out, int32 [T][kv_heads][keep] and [T][kv_heads]: labels of the kept pages (label j
+ *               holds tokens 64 j ..) in ascending order, -1 behind the last, and how many they are.
+ * The i-th of n new tokens of a sequence that holds L sees tokens [0, L - n + i + 1), in P pages: page P - 1 and
+ * the first `first` are kept, and of the others those with the highest max over the K/V head's query heads
+ * of q . k_mean (fp32 sums), ties to the lower label, NaN lowest, until min(keep, P) are. */
+SSBA_API int ssba_cache_select(const ssba_cache_desc* desc, const ssba_cache* cache, const void* q, int32_t T,
+                               const int32_t* table, int32_t width, const int32_t* lens, const int32_t* cu,
+                               int32_t B, int32_t keep, int32_t first, int32_t* idx, int32_t* cnt, void* stream);
+
+/* Bytes of device workspace ssba_cache_attend needs on the current device, the same for every
+ * valid descriptor. Returns 0 for an invalid one. */
+SSBA_API size_t ssba_cache_attend_workspace_bytes(const ssba_cache_desc* desc);
+
+/* Softmax attention of each row over the tokens that it sees.
+ *   q           device, [T][heads][head_dim] of desc->dtype.
+ *   idx, cnt    NULL: all pages of the row's sequence. Else the lists of ssba_cache_select ([T][kv_heads][keep]
+ *               and [T][kv_heads]): the pages listed, in any order; one listed twice counts twice.
+ *   O, lse      device out, [T][heads][head_dim] of desc->dtype and fp32 [T][heads], the natural log of the row's
+ *               sum of exp(scale * q.k). A row that sees no token: O = 0, lse = -inf.
+ *   workspace   device scratch of at least ssba_cache_attend_workspace_bytes(desc), 16-byte aligned.
+ *               Calls that may overlap on the GPU need workspaces of their own.
+ * Tokens that a row does not see have no part in it, whatever their K and V hold. Products and sums are
+ * fp32 (bf16 calls form products of 8-bit values exactly and round the weights to 8 bits of significand
+ * before they meet V). */
+SSBA_API int ssba_cache_attend(const ssba_cache_desc* desc, const ssba_cache* cache, const void* q, int32_t T,
+                               const int32_t* table, int32_t width, const int32_t* lens, const int32_t* cu,
+                               int32_t B, const int32_t* idx, const int32_t* cnt, int32_t keep, void* O, float* lse,
+                               void* workspace, size_t ws_bytes, void* stream);
+
+/* Copies whole pages of the pool: page src[i] to page dst[i] (device, int32 [n]), with scales and mean
+ * keys. No page may be among dst twice, or both among src and dst. */
+SSBA_API int ssba_cache_copy(const ssba_cache_desc* desc, const ssba_cache* cache, const int32_t* src,
+                             const int32_t* dst, int32_t n, void* stream);
+
+/* Reads and clears the device status word of the current device (SSBA_OK,
+ * SSBA_ERR_TIMEOUT or SSBA_ERR_CHECK). Synchronous: call after the caller's stream sync. Returns
  * SSBA_OK, or SSBA_ERR_CUDA if the read failed. */
 SSBA_API int ssba_get_status(int32_t* device_status_out);
 

@@ -33,7 +33,8 @@ EXPORTED = ("ssba_keep_count", "ssba_mask_workspace_bytes", "ssba_build_mask", "
             "ssba_test_backward_late", "ssba_backward", "ssba_backward_workspace_bytes", "ssba_haar_dwt",
             "ssba_haar_iwt", "ssba_haar_dwt_pyramid", "ssba_haar_iwt_pyramid", "ssba_qkv_rope_pool",
             "ssba_select_mask", "ssba_pool_blocks", "ssba_forward_select", "ssba_forward_fused",
-            "ssba_get_status", "ssba_last_error", "ssba_timeline_read")
+            "ssba_cache_append", "ssba_cache_select", "ssba_cache_attend_workspace_bytes", "ssba_cache_attend",
+            "ssba_cache_copy", "ssba_get_status", "ssba_last_error", "ssba_timeline_read")
 
 
 class SsbaError(RuntimeError):
@@ -47,6 +48,15 @@ class _Desc(ctypes.Structure):
                 ("W_tok", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("block", ctypes.c_int32),
                 ("shift_r", ctypes.c_int32), ("shift_c", ctypes.c_int32), ("rho", ctypes.c_double),
                 ("dtype", ctypes.c_int32), ("softmax_scale", ctypes.c_float)]
+
+
+class _CacheDesc(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("pages", ctypes.c_int32), ("dtype", ctypes.c_int32), ("softmax_scale", ctypes.c_float)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("K", "V", "k_scale", "v_scale", "k_mean")]
 
 
 @dataclass
@@ -152,6 +162,16 @@ def load_library(path: str | None = None):
         lib.ssba_haar_dwt_pyramid.restype = ctypes.c_int
         lib.ssba_haar_iwt_pyramid.argtypes = [PP, P, I, I, I, I, I, I, I, P]
         lib.ssba_haar_iwt_pyramid.restype = ctypes.c_int
+        CP = ctypes.POINTER(_CacheDesc)
+        batch = [P, I, P, P, I]  # table, width, lens, cu, B
+        lib.ssba_cache_append.argtypes = [CP, P, P, P, I, *batch, P]
+        lib.ssba_cache_select.argtypes = [CP, P, P, I, *batch, I, I, P, P, P]
+        lib.ssba_cache_attend.argtypes = [CP, P, P, I, *batch, P, P, I, P, P, P, ctypes.c_size_t, P]
+        lib.ssba_cache_copy.argtypes = [CP, P, P, P, I, P]
+        for fn in ("append", "select", "attend", "copy"):
+            getattr(lib, "ssba_cache_" + fn).restype = ctypes.c_int
+        lib.ssba_cache_attend_workspace_bytes.argtypes = [CP]
+        lib.ssba_cache_attend_workspace_bytes.restype = ctypes.c_size_t
         lib.ssba_get_status.argtypes = [ctypes.POINTER(ctypes.c_int32)]
         lib.ssba_get_status.restype = ctypes.c_int
         lib.ssba_last_error.argtypes = []

@@ -1,0 +1,238 @@
+"""Binding of the paged 8-bit K/V cache (``ssba_cache_*`` in include/ssba.h), and the host's side of it:
+which pages hold which sequence.
+
+``cache_append``, ``cache_select``, ``cache_attend`` and ``cache_copy`` marshal arguments as api.py does
+(device, dtype, shape, contiguity; the current stream unless ``stream`` is given). ``PagedCache`` owns a
+pool, keeps a page table with reference counts, and makes those calls for sequences by their ids: append,
+attend, fork with copy on write, free, compact. It holds integers only; every byte of the cache is moved by
+the library's kernels.
+"""
+from __future__ import annotations
+
+import ctypes
+from dataclasses import dataclass
+
+import torch
+
+from . import api
+from .api import (SSBA_BF16, SSBA_ERR_INVALID, SSBA_ERR_WORKSPACE, SSBA_FP32, SsbaError, _check, _empty, _lock, _out,
+                  _raise_on, _side, _stream_ptr, load_library)
+
+PAGE = 64
+_E4M3 = torch.float8_e4m3fn
+
+
+@dataclass
+class CacheDesc:
+    """Python mirror of ``ssba_cache_desc``."""
+    heads: int
+    kv_heads: int
+    head_dim: int
+    pages: int
+    dtype: torch.dtype = torch.bfloat16
+    softmax_scale: float = 0.0
+
+    def c(self) -> api._CacheDesc:
+        if self.dtype == torch.bfloat16:
+            dt = SSBA_BF16
+        elif self.dtype == torch.float32:
+            dt = SSBA_FP32
+        else:
+            raise SsbaError(SSBA_ERR_INVALID, f"unsupported dtype {self.dtype}")
+        return api._CacheDesc(self.heads, self.kv_heads, self.head_dim, self.pages, dt, float(self.softmax_scale))
+
+
+@dataclass
+class Cache:
+    """The pool's tensors: K, V float8_e4m3fn [pages, kv_heads, 64, head_dim]; k_scale, v_scale fp32
+    [pages, kv_heads]; k_mean fp32 [pages, kv_heads, head_dim]."""
+    K: torch.Tensor
+    V: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    k_mean: torch.Tensor
+
+
+class _Plan:
+    """What the calls derive from a descriptor's values alone: the C struct and the pool's shapes."""
+    __slots__ = ("c", "ref", "dtype", "heads", "kv", "d", "pages", "tiles", "scales", "means")
+
+    def __init__(self, desc: CacheDesc, c):
+        self.c, self.ref, self.dtype = c, ctypes.byref(c), desc.dtype
+        self.heads, self.kv, self.d, self.pages = desc.heads, desc.kv_heads, desc.head_dim, desc.pages
+        self.tiles = torch.Size((desc.pages, desc.kv_heads, PAGE, desc.head_dim))
+        self.scales = self.tiles[:2]
+        self.means = torch.Size((desc.pages, desc.kv_heads, desc.head_dim))
+
+
+_plans: dict = {}
+
+
+def _plan(desc: CacheDesc) -> _Plan:
+    """The plan of a descriptor, kept by its C struct and its sizes as given (the struct keeps 32 bits of them)."""
+    c = desc.c()
+    key = (bytes(c), desc.heads, desc.kv_heads, desc.head_dim, desc.pages)
+    pl = _plans.get(key)
+    if pl is None:
+        if min(key[1:]) <= 0 or max(key[1:]) > 2 ** 31 - 1:
+            raise SsbaError(SSBA_ERR_INVALID, f"sizes must be positive and below 2^31: {desc}")
+        pl = _Plan(desc, c)
+        if len(_plans) >= api._PLAN_CAP:
+            _plans.clear()
+        _plans[key] = pl
+    return pl
+
+
+def _pool(pl: _Plan, cache: Cache):
+    """The C struct of a checked pool, and its device, which has to be the current one."""
+    _check(cache.K, "cache.K", pl.tiles, _E4M3)
+    _check(cache.V, "cache.V", pl.tiles, _E4M3)
+    _check(cache.k_scale, "cache.k_scale", pl.scales, torch.float32)
+    _check(cache.v_scale, "cache.v_scale", pl.scales, torch.float32)
+    _check(cache.k_mean, "cache.k_mean", pl.means, torch.float32)
+    return api._Cache(cache.K.data_ptr(), cache.V.data_ptr(), cache.k_scale.data_ptr(), cache.v_scale.data_ptr(),
+                      cache.k_mean.data_ptr()), cache.K.device
+
+
+def _same_device(dev, cache: Cache, *tensors) -> None:
+    """Kernels run on the current device: everything has to be there."""
+    for t in (cache.V, cache.k_scale, cache.v_scale, cache.k_mean, *tensors):
+        if t is not None and t.device != dev:
+            raise SsbaError(SSBA_ERR_INVALID, f"tensors on {dev} and {t.device} in one call")
+    if dev.index != torch.cuda.current_device():
+        raise SsbaError(SSBA_ERR_INVALID, f"the cache is on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _rows(x, name: str, heads: int, pl: _Plan) -> int:
+    """Rows of a [T, heads, head_dim] tensor."""
+    T = int(x.shape[0]) if isinstance(x, torch.Tensor) and x.dim() == 3 else -1
+    _check(x, name, (max(T, 0), heads, pl.d), pl.dtype)
+    return T
+
+
+def _batch(table, lens, cu):
+    """(table, width, lens, cu, B) as the C calls take them."""
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise SsbaError(SSBA_ERR_INVALID, "table must be a 2-D tensor [B, width]")
+    B, width = table.shape
+    _check(table, "table", (B, width), torch.int32)
+    _check(lens, "lens", (B,), torch.int32)
+    _check(cu, "cu", (B + 1,), torch.int32)
+    return table.data_ptr(), width, lens.data_ptr(), cu.data_ptr(), B
+
+
+def cache_alloc(desc: CacheDesc, device="cuda") -> Cache:
+    """A pool of desc.pages pages (contents undefined: an append writes what later calls read)."""
+    pl = _plan(desc)
+    kv = [torch.empty(pl.tiles, dtype=_E4M3, device=device) for _ in range(2)]
+    scales = [torch.empty(pl.scales, dtype=torch.float32, device=device) for _ in range(2)]
+    return Cache(*kv, *scales, torch.empty(pl.means, dtype=torch.float32, device=device))
+
+
+def cache_append(desc: CacheDesc, cache: Cache, k, v, table, lens, cu, stream=None) -> Cache:
+    """ssba_cache_append: k, v [T, kv_heads, head_dim] into the pages of their sequences; table [B, width],
+    lens [B] (tokens held before), cu [B + 1], all int32. Returns the cache."""
+    lib = load_library()
+    pl = _plan(desc)
+    pool, dev = _pool(pl, cache)
+    T = _rows(k, "k", pl.kv, pl)
+    _check(v, "v", k.shape, pl.dtype)
+    batch = _batch(table, lens, cu)
+    _same_device(dev, cache, k, v, table, lens, cu)
+    _raise_on(lib.ssba_cache_append(pl.ref, ctypes.byref(pool), k.data_ptr(), v.data_ptr(), T, *batch,
+                                    _stream_ptr(stream)))
+    return cache
+
+
+def cache_select(desc: CacheDesc, cache: Cache, q, table, lens, cu, keep: int, first: int = 1, idx=None, cnt=None,
+                 stream=None):
+    """ssba_cache_select: q [T, heads, head_dim] -> (idx [T, kv_heads, keep], cnt [T, kv_heads]) int32.
+    lens: tokens held, the rows of q among them."""
+    lib = load_library()
+    pl = _plan(desc)
+    pool, dev = _pool(pl, cache)
+    T = _rows(q, "q", pl.heads, pl)
+    batch = _batch(table, lens, cu)
+    if not 0 <= first < keep:
+        raise SsbaError(SSBA_ERR_INVALID, f"keep={keep} must be more than first={first}, first >= 0")
+    _same_device(dev, cache, q, table, lens, cu, idx, cnt)
+    side = _side(stream, dev)
+    idx = _out(idx, "idx", (T, pl.kv, keep), torch.int32, dev, side)
+    cnt = _out(cnt, "cnt", (T, pl.kv), torch.int32, dev, side)
+    _raise_on(lib.ssba_cache_select(pl.ref, ctypes.byref(pool), q.data_ptr(), T, *batch, keep, first, idx.data_ptr(),
+                                    cnt.data_ptr(), _stream_ptr(stream)))
+    return idx, cnt
+
+
+def cache_attend_workspace_bytes(desc: CacheDesc) -> int:
+    lib = load_library()
+    n = int(lib.ssba_cache_attend_workspace_bytes(_plan(desc).ref))
+    if n == 0:
+        _raise_on(SSBA_ERR_INVALID)
+    return n
+
+
+_ws: dict = {}
+
+
+def _default_workspace(pl: _Plan, lib, dev, stream):
+    """A workspace kept per (device, stream): the calls of one stream run in order and can share it. A capture
+    gets one of its own, so that no two graphs, and no graph and an eager call, meet in one."""
+    need = int(lib.ssba_cache_attend_workspace_bytes(pl.ref))
+    if need == 0:
+        _raise_on(SSBA_ERR_INVALID)
+    side = _side(stream, dev)
+    with torch.cuda.stream(stream if side is not None else None):
+        if torch.cuda.is_current_stream_capturing():
+            return torch.empty(need, dtype=torch.uint8, device=dev)
+        key = (dev.index, _stream_ptr(stream))
+        with _lock:
+            ws = _ws.get(key)
+            if ws is None or ws.numel() < need:
+                ws = _ws[key] = torch.empty(need, dtype=torch.uint8, device=dev)
+    return ws
+
+
+def cache_attend(desc: CacheDesc, cache: Cache, q, table, lens, cu, idx=None, cnt=None, O=None, lse=None,
+                 workspace="default", stream=None):
+    """ssba_cache_attend: q [T, heads, head_dim] -> (O [T, heads, head_dim], lse [T, heads] fp32), over every
+    page of the rows' sequences, or over the lists (idx, cnt) of cache_select."""
+    lib = load_library()
+    pl = _plan(desc)
+    pool, dev = _pool(pl, cache)
+    T = _rows(q, "q", pl.heads, pl)
+    batch = _batch(table, lens, cu)
+    keep = 0
+    if (idx is None) != (cnt is None):
+        raise SsbaError(SSBA_ERR_INVALID, "idx and cnt come together")
+    if idx is not None:
+        keep = int(idx.shape[2]) if isinstance(idx, torch.Tensor) and idx.dim() == 3 else 0
+        _check(idx, "idx", (T, pl.kv, keep), torch.int32)
+        _check(cnt, "cnt", (T, pl.kv), torch.int32)
+    _same_device(dev, cache, q, table, lens, cu, idx, cnt, O, lse)
+    side = _side(stream, dev)
+    O = _out(O, "O", q.shape, pl.dtype, dev, side)
+    lse = _out(lse, "lse", (T, pl.heads), torch.float32, dev, side)
+    if isinstance(workspace, str):
+        workspace = _default_workspace(pl, lib, dev, stream)
+    elif workspace is None:
+        raise SsbaError(SSBA_ERR_WORKSPACE, "cache_attend needs a workspace")
+    wp, wn = api._ws_args(workspace)
+    _raise_on(lib.ssba_cache_attend(pl.ref, ctypes.byref(pool), q.data_ptr(), T, *batch,
+                                    idx.data_ptr() if idx is not None else None,
+                                    cnt.data_ptr() if cnt is not None else None, keep, O.data_ptr(), lse.data_ptr(),
+                                    wp, wn, _stream_ptr(stream)))
+    return O, lse
+
+
+def cache_copy(desc: CacheDesc, cache: Cache, src, dst, stream=None) -> Cache:
+    """ssba_cache_copy: pages src[i] -> dst[i], int32 CUDA tensors [n]. Returns the cache."""
+    lib = load_library()
+    pl = _plan(desc)
+    pool, dev = _pool(pl, cache)
+    n = src.numel() if isinstance(src, torch.Tensor) else -1
+    _check(src, "src", (max(n, 0),), torch.int32)
+    _check(dst, "dst", (max(n, 0),), torch.int32)
+    _same_device(dev, cache, src, dst)
+    _raise_on(lib.ssba_cache_copy(pl.ref, ctypes.byref(pool), src.data_ptr(), dst.data_ptr(), n, _stream_ptr(stream)))
+    return cache

@@ -1,0 +1,257 @@
+// cache_attend_simt.cu -- attention over the paged 8-bit cache on the CUDA cores, in fp32.
+//
+//   s = scale * k_scale * (q . byte values of k),  O = sum softmax(s) * v_scale * byte values of v
+// over the tokens that a row sees, in all pages of its sequence or in listed ones.
+#include <algorithm>
+#include <cmath>
+
+#include "cache.cuh"
+
+namespace ssba {
+namespace cache {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr int kHeads = 8;      // query heads that a CTA takes together
+constexpr int kMaxParts = 608;  // CTAs that write partial results at most: four an SM
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void store(float* p, float x) { *p = x; }
+__device__ __forceinline__ void store(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// One CTA: row t, up to 8 heads of one group, and one of `parts` shares of its pages. A warp takes whole
+// pages: a lane scores two tokens (their K rows in 16-byte loads, q broadcast from shared memory), then owns D / 32
+// channels of O over the page's V rows. The warps' results are joined at the end; shares through the workspace.
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
+    const Pool pl, const Batch bt, const T* q, const int32_t* idx, const int32_t* cnt, int keep, float scale_log2,
+    T* O, float* lse, float* ws, int parts, int chunks)
+{
+    constexpr int kC = D / 32;  // channels of a lane
+    __shared__ float qs[kHeads][D];
+    __shared__ float ps[kWarps][kPage][kHeads];
+    __shared__ float ms[kWarps][kHeads], ls[kWarps][kHeads];
+    const int t = blockIdx.x, part = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int h = blockIdx.y / chunks, chunk = blockIdx.y % chunks;
+    const int b = find_seq(bt, t, lane);
+    if (b < 0) return;
+    const int G = pl.heads / pl.kv_heads, g0 = chunk * kHeads, ng = min(kHeads, G - g0);
+    const size_t head0 = (size_t)t * pl.heads + h * G + g0;
+    const Seq s = load_seq(bt, b, pl.status);
+    const int L = visible(s, t, pl.status);
+    const int P = (L + kPage - 1) / kPage;
+    const size_t row = (size_t)t * pl.kv_heads + h;
+    int n = P;
+    if (idx) {
+        n = __ldg(cnt + row);
+        if (n < 0 || n > keep) {
+            flag(pl.status);
+            n = min(max(n, 0), keep);
+        }
+    }
+    for (int i = tid; i < kHeads * D; i += kThreads)
+        qs[i / D][i % D] = i / D < ng ? to_float(q[head0 * D + i]) : 0.f;
+    __syncthreads();
+    float m[kHeads], l[kHeads], o[kHeads][kC];
+#pragma unroll
+    for (int g = 0; g < kHeads; ++g) {
+        m[g] = -INFINITY;
+        l[g] = 0.f;
+#pragma unroll
+        for (int c = 0; c < kC; ++c) o[g][c] = 0.f;
+    }
+    for (int i = part * kWarps + warp; i < n; i += parts * kWarps) {
+        int j = i;
+        if (idx) {
+            j = __ldg(idx + row * keep + i);
+            if (j < 0 || j >= P) {
+                flag(pl.status);
+                continue;
+            }
+        }
+        const int page = page_of(bt, pl, b, j);
+        if (page < 0) continue;
+        const int nt = min(kPage, L - j * kPage);  // tokens of the page that the row sees
+        const size_t unit = (size_t)page * pl.kv_heads + h;
+        const float ks = __ldg(pl.k_scale + unit) * scale_log2, vs = __ldg(pl.v_scale + unit);
+        const uint8_t* K = pl.K + unit * kPage * D;
+        const uint8_t* V = pl.V + unit * kPage * D;
+        float a[2][kHeads] = {};
+#pragma unroll 1
+        for (int c = 0; c < D; c += 16) {
+            uint4 kk[2];
+            kk[0] = __ldg(reinterpret_cast<const uint4*>(K + lane * D + c));
+            kk[1] = __ldg(reinterpret_cast<const uint4*>(K + (lane + 32) * D + c));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float f[2][4];
+                from_e4m3x4((&kk[0].x)[e], f[0]);
+                from_e4m3x4((&kk[1].x)[e], f[1]);
+#pragma unroll
+                for (int g = 0; g < kHeads; ++g) {
+                    const float4 x = *reinterpret_cast<const float4*>(&qs[g][c + 4 * e]);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+                        a[u][g] = fmaf(x.w, f[u][3], fmaf(x.z, f[u][2], fmaf(x.y, f[u][1], fmaf(x.x, f[u][0], a[u][g]))));
+                }
+            }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int g = 0; g < kHeads; ++g) {
+            const float s0 = lane < nt ? a[0][g] * ks : -INFINITY, s1 = lane + 32 < nt ? a[1][g] * ks : -INFINITY;
+            float top = fmaxf(s0, s1);
+#pragma unroll
+            for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const float mn = fmaxf(m[g], top), ref = mn == -INFINITY ? 0.f : mn;
+            const float f = exp2f(m[g] - ref);
+            m[g] = mn;
+            const float p0 = lane < nt ? exp2f(s0 - ref) : 0.f, p1 = lane + 32 < nt ? exp2f(s1 - ref) : 0.f;
+            l[g] = l[g] * f + (p0 + p1);
+#pragma unroll
+            for (int c = 0; c < kC; ++c) o[g][c] *= f;
+            ps[warp][lane][g] = p0 * vs;
+            ps[warp][lane + 32][g] = p1 * vs;
+        }
+        __syncwarp();
+#pragma unroll 4
+        for (int r = 0; r < nt; ++r) {
+            float f[4];
+            if (kC == 4) {
+                from_e4m3x4(__ldg(reinterpret_cast<const uint32_t*>(V + r * D) + lane), f);
+            } else {
+                const float2 y = from_e4m3x2(__ldg(reinterpret_cast<const uint16_t*>(V + r * D) + lane));
+                f[0] = y.x;
+                f[1] = y.y;
+            }
+#pragma unroll
+            for (int g = 0; g < kHeads; g += 4) {
+                const float4 x = *reinterpret_cast<const float4*>(&ps[warp][r][g]);
+#pragma unroll
+                for (int c = 0; c < kC; ++c) {
+                    o[g][c] = fmaf(x.x, f[c], o[g][c]);
+                    o[g + 1][c] = fmaf(x.y, f[c], o[g + 1][c]);
+                    o[g + 2][c] = fmaf(x.z, f[c], o[g + 2][c]);
+                    o[g + 3][c] = fmaf(x.w, f[c], o[g + 3][c]);
+                }
+            }
+        }
+    }
+    // join the warps, one head after another through shared memory (ps is free: 64 x 8 floats a warp hold D)
+#pragma unroll
+    for (int g = 0; g < kHeads; ++g) {
+        float lg = l[g];
+#pragma unroll
+        for (int d = 16; d; d >>= 1) lg += __shfl_xor_sync(0xffffffffu, lg, d);
+        if (lane == 0) {
+            ms[warp][g] = m[g];
+            ls[warp][g] = lg;
+        }
+    }
+    __syncthreads();
+    float* po = &ps[0][0][0];  // [kWarps][2][D] at a time
+#pragma unroll
+    for (int gp = 0; gp < kHeads; gp += 2) {
+#pragma unroll
+        for (int g = gp; g < gp + 2; ++g)
+#pragma unroll
+            for (int c = 0; c < kC; ++c) po[(warp * 2 + g - gp) * D + lane * kC + c] = o[g][c];
+        __syncthreads();
+        for (int i = tid; i < 2 * D; i += kThreads) {
+            const int g = gp + i / D, c = i % D;
+            if (g < ng) {
+                float top = -INFINITY, lt = 0.f, ot = 0.f;
+                for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ms[w][g]);
+                const float ref = top == -INFINITY ? 0.f : top;
+                for (int w = 0; w < kWarps; ++w) {
+                    const float f = exp2f(ms[w][g] - ref);
+                    lt += ls[w][g] * f;
+                    ot += po[(w * 2 + g - gp) * D + c] * f;
+                }
+                if (parts == 1) {
+                    store(O + (head0 + g) * D + c, lt != 0.f ? ot / lt : 0.f);
+                    if (c == 0) lse[head0 + g] = (ref + log2f(lt)) * kLn2;
+                } else {
+                    float* w = ws + (((size_t)blockIdx.x * gridDim.y + blockIdx.y) * parts + part) * kHeads * (D + 2) + g * (D + 2);
+                    w[c] = ot;
+                    if (c == 0) {
+                        w[D] = top;
+                        w[D + 1] = lt;
+                    }
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Joins the shares of one head of one row, in order.
+template <typename T, int D>
+__global__ void __launch_bounds__(D) ssba_cache_join_kernel(const Pool pl, const Batch bt, const float* ws, T* O,
+                                                            float* lse, int parts, int chunks)
+{
+    const int t = blockIdx.x, h = blockIdx.y / chunks, chunk = blockIdx.y % chunks, g = blockIdx.z, c = threadIdx.x;
+    const int G = pl.heads / pl.kv_heads, gg = chunk * kHeads + g;
+    if (gg >= G || find_seq(bt, t, c & 31) < 0) return;
+    const float* w = ws + ((size_t)blockIdx.x * gridDim.y + blockIdx.y) * parts * kHeads * (D + 2) + g * (D + 2);
+    const size_t step = (size_t)kHeads * (D + 2);
+    float top = -INFINITY, l = 0.f, o = 0.f;
+    for (int i = 0; i < parts; ++i) top = fmaxf(top, w[i * step + D]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    for (int i = 0; i < parts; ++i) {
+        const float f = exp2f(w[i * step + D] - ref);
+        l += w[i * step + D + 1] * f;
+        o += w[i * step + c] * f;
+    }
+    const size_t head = (size_t)t * pl.heads + h * G + gg;
+    store(O + head * D + c, l != 0.f ? o / l : 0.f);
+    if (c == 0) lse[head] = (ref + log2f(l)) * kLn2;
+}
+
+template <typename T, int D>
+int attend_as(const Pool& pl, const Batch& bt, float scale, const void* q, const int32_t* idx, const int32_t* cnt,
+              int keep, void* O, float* lse, void* ws, cudaStream_t st)
+{
+    const int G = pl.heads / pl.kv_heads, chunks = (G + kHeads - 1) / kHeads;
+    const long long items = (long long)bt.T * pl.kv_heads * chunks;
+    const int pages = idx ? keep : bt.width;
+    // shares: as many as give the SMs work, none of fewer than a page a warp
+    const int parts = (int)std::max<long long>(1, std::min<long long>(kMaxParts / std::max<long long>(items, 1), (pages + kWarps - 1) / kWarps));
+    const dim3 grid(bt.T, pl.kv_heads * chunks, parts);
+    ssba_cache_attend_simt_kernel<T, D><<<grid, kThreads, 0, st>>>(pl, bt, static_cast<const T*>(q), idx, cnt, keep,
+                                                                  scale * kLog2e, static_cast<T*>(O), lse,
+                                                                  static_cast<float*>(ws), parts, chunks);
+    if (parts > 1)
+        ssba_cache_join_kernel<T, D><<<dim3(bt.T, pl.kv_heads * chunks, kHeads), D, 0, st>>>(
+            pl, bt, static_cast<const float*>(ws), static_cast<T*>(O), lse, parts, chunks);
+    const cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) return SSBA_OK;
+    set_error("ssba_cache_attend: %s", cudaGetErrorString(e));
+    return SSBA_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace cache
+
+size_t cache_attend_simt_workspace(int head_dim)
+{
+    return (size_t)cache::kMaxParts * cache::kHeads * (head_dim + 2) * sizeof(float);
+}
+
+int launch_cache_attend_simt(const cache::Pool& pl, const cache::Batch& bt, int head_dim, int dtype, float scale,
+                             const void* q, const int32_t* idx, const int32_t* cnt, int keep, void* O, float* lse,
+                             void* ws, cudaStream_t st)
+{
+    if (dtype == SSBA_BF16)
+        return head_dim == 64
+                   ? cache::attend_as<__nv_bfloat16, 64>(pl, bt, scale, q, idx, cnt, keep, O, lse, ws, st)
+                   : cache::attend_as<__nv_bfloat16, 128>(pl, bt, scale, q, idx, cnt, keep, O, lse, ws, st);
+    return head_dim == 64 ? cache::attend_as<float, 64>(pl, bt, scale, q, idx, cnt, keep, O, lse, ws, st)
+                          : cache::attend_as<float, 128>(pl, bt, scale, q, idx, cnt, keep, O, lse, ws, st);
+}
+
+}  // namespace ssba

@@ -1,0 +1,143 @@
+"""Host-side checks of the paged cache's entry points (no compute call is made) and of the reference that
+the GPU tests compare with."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import cache_ref as ref
+from paper_2605_15684_gb300 import api, build
+from paper_2605_15684_gb300 import cache as pc
+
+FAKE = 0x100000  # a 128-byte aligned, never dereferenced address
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return api.load_library()
+
+
+def desc(**kw):
+    base = dict(heads=8, kv_heads=2, head_dim=128, pages=10, dtype=api.SSBA_BF16, softmax_scale=0.0)
+    base.update(kw)
+    return ctypes.byref(api._CacheDesc(**base))
+
+
+def pool(**kw):
+    base = dict(K=FAKE, V=FAKE, k_scale=FAKE, v_scale=FAKE, k_mean=FAKE)
+    base.update(kw)
+    return ctypes.byref(api._Cache(**base))
+
+
+BATCH = (FAKE, 4, FAKE, FAKE, 2)  # table, width, lens, cu, B
+
+
+def calls(lib, d, c, T=3, batch=BATCH):
+    return (lib.ssba_cache_append(d, c, FAKE, FAKE, T, *batch, None),
+            lib.ssba_cache_select(d, c, FAKE, T, *batch, 4, 1, FAKE, FAKE, None),
+            lib.ssba_cache_attend(d, c, FAKE, T, *batch, None, None, 0, FAKE, FAKE, FAKE, 0, None))
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(heads=0), 1), (dict(kv_heads=0), 1), (dict(heads=7), 1), (dict(pages=0), 1), (dict(dtype=5), 1),
+    (dict(softmax_scale=-1.0), 1), (dict(softmax_scale=float("nan")), 1), (dict(softmax_scale=float("inf")), 1),
+    (dict(head_dim=0), 1), (dict(head_dim=96), 2), (dict(head_dim=256), 2), (dict(heads=32768, kv_heads=8), 2),
+    (dict(pages=2 ** 30, kv_heads=8), 2)])
+def test_descriptors(lib, bad, code):
+    assert set(calls(lib, desc(**bad), pool())) == {code}
+    assert lib.ssba_cache_copy(desc(**bad), pool(), FAKE, FAKE, 1, None) == code
+    assert lib.ssba_cache_attend_workspace_bytes(desc(**bad)) == 0
+    assert lib.ssba_last_error()
+
+
+@pytest.mark.parametrize("bad", [dict(K=None), dict(V=None), dict(k_scale=None), dict(v_scale=None), dict(k_mean=None),
+                                 dict(K=FAKE + 16), dict(V=FAKE + 64), dict(k_scale=FAKE + 2), dict(k_mean=FAKE + 8)])
+def test_pools(lib, bad):
+    assert set(calls(lib, desc(), pool(**bad))) == {api.SSBA_ERR_INVALID}
+    assert lib.ssba_cache_copy(desc(), pool(**bad), FAKE, FAKE, 1, None) == api.SSBA_ERR_INVALID
+    assert set(calls(lib, desc(), None)) == {api.SSBA_ERR_INVALID}
+    assert set(calls(lib, None, pool())) == {api.SSBA_ERR_INVALID}
+
+
+@pytest.mark.parametrize("T,batch,code", [
+    (-1, BATCH, 1), (3, (FAKE, 0, FAKE, FAKE, 2), 1), (3, (FAKE, 4, FAKE, FAKE, -1), 1), (3, (None, 4, FAKE, FAKE, 2), 1),
+    (3, (FAKE, 4, None, FAKE, 2), 1), (3, (FAKE, 4, FAKE, None, 2), 1), (3, (FAKE + 2, 4, FAKE, FAKE, 2), 1),
+    (2 ** 24 + 1, BATCH, 2), (3, (FAKE, 2 ** 25, FAKE, FAKE, 2), 2), (3, (FAKE, 4, FAKE, FAKE, 2 ** 24 + 1), 2)])
+def test_batches(lib, T, batch, code):
+    assert set(calls(lib, desc(), pool(), T, batch)) == {code}
+
+
+def test_no_work_succeeds_without_a_device(lib):
+    assert set(calls(lib, desc(), pool(), 0)) == {api.SSBA_OK}
+    assert set(calls(lib, desc(), pool(), 3, (None, 4, None, None, 0))) == {api.SSBA_OK}
+    assert lib.ssba_cache_copy(desc(), pool(), None, None, 0, None) == api.SSBA_OK
+
+
+def test_outputs_lists_and_workspaces(lib):
+    d, c = desc(), pool()
+    sel = lambda q=FAKE, keep=4, first=1, idx=FAKE, cnt=FAKE, batch=BATCH: lib.ssba_cache_select(
+        d, c, q, 3, *batch, keep, first, idx, cnt, None)
+    for kw in (dict(q=None), dict(q=FAKE + 8), dict(keep=0, first=0), dict(keep=2, first=2), dict(first=-1), dict(idx=None),
+               dict(cnt=None), dict(idx=FAKE + 1), dict(keep=32769)):
+        assert sel(**kw) == api.SSBA_ERR_INVALID, kw
+    assert sel(batch=(FAKE, 32769, FAKE, FAKE, 2)) == api.SSBA_ERR_UNSUPPORTED
+    need = lib.ssba_cache_attend_workspace_bytes(d)
+    assert need > 0
+    att = lambda q=FAKE, idx=None, cnt=None, keep=0, O=FAKE, lse=FAKE, ws=FAKE, n=need: lib.ssba_cache_attend(
+        d, c, q, 3, *BATCH, idx, cnt, keep, O, lse, ws, n, None)
+    for kw in (dict(q=None), dict(O=None), dict(lse=None), dict(O=FAKE + 8), dict(idx=FAKE, keep=4), dict(cnt=FAKE, keep=4),
+               dict(idx=FAKE, cnt=FAKE, keep=0), dict(idx=FAKE + 2, cnt=FAKE, keep=4)):
+        assert att(**kw) == api.SSBA_ERR_INVALID, kw
+    for kw in (dict(ws=None), dict(n=need - 1), dict(ws=FAKE + 8)):
+        assert att(**kw) == api.SSBA_ERR_WORKSPACE, kw
+    assert lib.ssba_cache_append(d, c, None, FAKE, 3, *BATCH, None) == api.SSBA_ERR_INVALID
+    assert lib.ssba_cache_append(d, c, FAKE, FAKE + 4, 3, *BATCH, None) == api.SSBA_ERR_INVALID
+    assert lib.ssba_cache_copy(d, c, None, FAKE, 1, None) == api.SSBA_ERR_INVALID
+    assert lib.ssba_cache_copy(d, c, FAKE, FAKE, -1, None) == api.SSBA_ERR_INVALID
+
+
+def test_binding_refuses_before_it_calls(lib):
+    d = pc.CacheDesc(8, 2, 128, 4)
+    c = pc.cache_alloc(d, "cpu")
+    q, t = torch.zeros(3, 8, 128, dtype=torch.bfloat16), torch.zeros(1, 4, dtype=torch.int32)
+    with pytest.raises(api.SsbaError, match="CUDA tensor"):
+        pc.cache_attend(d, c, q, t, t[0, :1], t[0, :2])
+    with pytest.raises(api.SsbaError, match="dtype"):
+        pc.cache_alloc(pc.CacheDesc(8, 2, 128, 4, torch.float16), "cpu")
+    with pytest.raises(api.SsbaError, match="2\\^31"):
+        pc.cache_alloc(pc.CacheDesc(2 ** 32 + 8, 2, 128, 4), "cpu")
+
+
+# ----------------------------------------------------------------------------- the reference itself
+def test_reference_bytes_and_rounding():
+    """The table of values and the rounding equal torch's own e4m3."""
+    b = torch.arange(256, dtype=torch.uint8)
+    assert np.array_equal(ref.VALUES, b.view(ref.E4M3).double().numpy(), equal_nan=True)
+    x = torch.cat([torch.randn(20000) * s for s in (100, 1, 0.01, 0.001)]).clamp(-448, 448)
+    x = torch.cat([x, torch.arange(-448, 449) / 1.0, torch.arange(-1000, 1000) * 2.0 ** -11])
+    assert np.array_equal(ref.round_e4m3(x.double().numpy()), x.to(ref.E4M3).double().numpy())
+
+
+@pytest.mark.parametrize("a,s", [(0.0, 0.0), (448.0, 1.0), (448.001, 2.0), (224.0, 0.5), (1.0, 2.0 ** -8), (3.5, 2.0 ** -7),
+                                 (3.6, 2.0 ** -6), (1e-45, 2.0 ** -126), (3e38, 2.0 ** 120)])
+def test_reference_scale(a, s):
+    assert ref.scale_for(a) == s
+
+
+def test_reference_attention_is_a_softmax():
+    """Against a dense softmax over contiguous values."""
+    g = np.random.default_rng(0)
+    p = ref.Pool.__new__(ref.Pool)
+    p.K, p.V = g.normal(size=(3, 1, 64, 8)), g.normal(size=(3, 1, 64, 8))
+    p.k_scale, p.v_scale, p.k_mean = np.full((3, 1), 0.5), np.full((3, 1), 2.0), None
+    q = g.normal(size=(2, 2, 8))
+    table = np.array([[2, 0]])
+    O, lse, A, S = ref.attend(p, q, table, [100], [0, 2], 0.3)
+    K = np.concatenate([p.K[2, 0], p.K[0, 0]]) * 0.5
+    V = np.concatenate([p.V[2, 0], p.V[0, 0]]) * 2
+    for i, L in ((0, 99), (1, 100)):
+        a = 0.3 * q[i] @ K[:L].T
+        w = np.exp(a) / np.exp(a).sum(1, keepdims=True)
+        assert np.allclose(O[i], w @ V[:L], atol=1e-13) and np.allclose(lse[i], np.log(np.exp(a).sum(1)), atol=1e-13)
