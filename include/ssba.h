@@ -402,6 +402,7 @@ SSBA_API int ssba_test_backward_late(const ssba_desc* desc, const void* Q, const
 #define SSBA_CACHE_MAX_HEADS 16384   /* heads */
 #define SSBA_CACHE_MAX_ROWS (1 << 24) /* T and B */
 #define SSBA_CACHE_MAX_WIDTH 32768   /* pages of a selection's sequences, and keep */
+#define SSBA_CACHE_TICKET_BYTES 4096 /* of the attention's workspace: zero before its first call */
 
 /* heads        query heads, a multiple of kv_heads; query heads [g * heads / kv_heads, (g + 1) * ...) share
  *              K/V head g.
@@ -459,7 +460,9 @@ SSBA_API size_t ssba_cache_attend_workspace_bytes(const ssba_cache_desc* desc);
  *   O, lse      device out, [T][heads][head_dim] of desc->dtype and fp32 [T][heads], the natural log of the row's
  *               sum of exp(scale * q.k). A row that sees no token: O = 0, lse = -inf.
  *   workspace   device scratch of at least ssba_cache_attend_workspace_bytes(desc), 16-byte aligned.
- *               Calls that may overlap on the GPU need workspaces of their own.
+ *               Its first SSBA_CACHE_TICKET_BYTES are zero-filled once; a call leaves them zero (after
+ *               SSBA_ERR_TIMEOUT they have to be zeroed again). Calls that may overlap on the GPU need
+ *               workspaces of their own.
  * Tokens that a row does not see have no part in it, whatever their K and V hold. Products and sums are
  * fp32 (bf16 calls form products of 8-bit values exactly and round the weights to 8 bits of significand
  * before they meet V). */

@@ -19,6 +19,7 @@ from .api import (SSBA_BF16, SSBA_ERR_INVALID, SSBA_ERR_WORKSPACE, SSBA_FP32, Ss
                   _raise_on, _side, _stream_ptr, load_library)
 
 PAGE = 64
+_TICKET_BYTES = 4096  # of the attention's workspace, zero between calls (SSBA_CACHE_TICKET_BYTES)
 _E4M3 = torch.float8_e4m3fn
 
 
@@ -184,12 +185,15 @@ def _default_workspace(pl: _Plan, lib, dev, stream):
     side = _side(stream, dev)
     with torch.cuda.stream(stream if side is not None else None):
         if torch.cuda.is_current_stream_capturing():
-            return torch.empty(need, dtype=torch.uint8, device=dev)
+            # the fill is a node of the graph, so no later call may count on it
+            ws = torch.empty(need, dtype=torch.uint8, device=dev)
+            ws[:_TICKET_BYTES].zero_()
+            return ws
         key = (dev.index, _stream_ptr(stream))
         with _lock:
             ws = _ws.get(key)
             if ws is None or ws.numel() < need:
-                ws = _ws[key] = torch.empty(need, dtype=torch.uint8, device=dev)
+                ws = _ws[key] = torch.zeros(need, dtype=torch.uint8, device=dev)
     return ws
 
 

@@ -132,6 +132,10 @@ int launch_cache_select(const cache::Pool& pl, const cache::Batch& bt, int head_
 int launch_cache_attend_simt(const cache::Pool& pl, const cache::Batch& bt, int head_dim, int dtype, float scale,
                              const void* q, const int32_t* idx, const int32_t* cnt, int keep, void* O, float* lse,
                              void* ws, cudaStream_t st);
-size_t cache_attend_simt_workspace(int head_dim);
+size_t cache_attend_simt_workspace();
+int launch_cache_attend_tc(const cache::Pool& pl, const cache::Batch& bt, int head_dim, float scale, const void* q,
+                           const int32_t* idx, const int32_t* cnt, int keep, void* O, float* lse, void* ws,
+                           cudaStream_t st);
+size_t cache_attend_tc_workspace();
 
 }  // namespace ssba

@@ -1,5 +1,6 @@
 // cache_api.cu -- the entry points of the paged 8-bit cache (include/ssba.h): argument validation on the
 // host and kernel launches on the caller's stream.
+#include <algorithm>
 #include <climits>
 #include <cmath>
 
@@ -153,7 +154,7 @@ int ssba_cache_select(const ssba_cache_desc* desc, const ssba_cache* cache, cons
 size_t ssba_cache_attend_workspace_bytes(const ssba_cache_desc* desc)
 {
     if (check_cache_desc(desc, "ssba_cache_attend_workspace_bytes") != SSBA_OK) return 0;
-    return (cache_attend_simt_workspace(desc->head_dim) + 255) & ~(size_t)255;
+    return (std::max(cache_attend_simt_workspace(), cache_attend_tc_workspace()) + 255) & ~(size_t)255;
 }
 
 int ssba_cache_attend(const ssba_cache_desc* desc, const ssba_cache* cache, const void* q, int32_t T,
@@ -185,8 +186,11 @@ int ssba_cache_attend(const ssba_cache_desc* desc, const ssba_cache* cache, cons
     cache::Pool p;
     if (!make_pool(desc, cache, who, &p)) return SSBA_ERR_CUDA;
     const float scale = desc->softmax_scale > 0.f ? desc->softmax_scale : 1.0f / std::sqrt((float)desc->head_dim);
-    return launch_cache_attend_simt(p, cache::Batch{table, lens, cu, B, width, T}, desc->head_dim, desc->dtype, scale,
-                                    q, idx, cnt, keep, O, lse, workspace, static_cast<cudaStream_t>(stream));
+    const cache::Batch bt{table, lens, cu, B, width, T};
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (desc->dtype == SSBA_BF16)
+        return launch_cache_attend_tc(p, bt, desc->head_dim, scale, q, idx, cnt, keep, O, lse, workspace, st);
+    return launch_cache_attend_simt(p, bt, desc->head_dim, desc->dtype, scale, q, idx, cnt, keep, O, lse, workspace, st);
 }
 
 int ssba_cache_copy(const ssba_cache_desc* desc, const ssba_cache* cache, const int32_t* src, const int32_t* dst,

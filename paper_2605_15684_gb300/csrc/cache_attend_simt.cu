@@ -217,6 +217,7 @@ int attend_as(const Pool& pl, const Batch& bt, float scale, const void* q, const
               int keep, void* O, float* lse, void* ws, cudaStream_t st)
 {
     const int G = pl.heads / pl.kv_heads, chunks = (G + kHeads - 1) / kHeads;
+    float* parts_at = reinterpret_cast<float*>(static_cast<char*>(ws) + SSBA_CACHE_TICKET_BYTES);
     const long long items = (long long)bt.T * pl.kv_heads * chunks;
     const int pages = idx ? keep : bt.width;
     // shares: as many as give the SMs work, none of fewer than a page a warp
@@ -224,10 +225,10 @@ int attend_as(const Pool& pl, const Batch& bt, float scale, const void* q, const
     const dim3 grid(bt.T, pl.kv_heads * chunks, parts);
     ssba_cache_attend_simt_kernel<T, D><<<grid, kThreads, 0, st>>>(pl, bt, static_cast<const T*>(q), idx, cnt, keep,
                                                                   scale * kLog2e, static_cast<T*>(O), lse,
-                                                                  static_cast<float*>(ws), parts, chunks);
+                                                                  parts_at, parts, chunks);
     if (parts > 1)
         ssba_cache_join_kernel<T, D><<<dim3(bt.T, pl.kv_heads * chunks, kHeads), D, 0, st>>>(
-            pl, bt, static_cast<const float*>(ws), static_cast<T*>(O), lse, parts, chunks);
+            pl, bt, parts_at, static_cast<T*>(O), lse, parts, chunks);
     const cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess) return SSBA_OK;
     set_error("ssba_cache_attend: %s", cudaGetErrorString(e));
@@ -237,9 +238,9 @@ int attend_as(const Pool& pl, const Batch& bt, float scale, const void* q, const
 }  // namespace
 }  // namespace cache
 
-size_t cache_attend_simt_workspace(int head_dim)
+size_t cache_attend_simt_workspace()
 {
-    return (size_t)cache::kMaxParts * cache::kHeads * (head_dim + 2) * sizeof(float);
+    return SSBA_CACHE_TICKET_BYTES + (size_t)cache::kMaxParts * cache::kHeads * (128 + 2) * sizeof(float);
 }
 
 int launch_cache_attend_simt(const cache::Pool& pl, const cache::Batch& bt, int head_dim, int dtype, float scale,
