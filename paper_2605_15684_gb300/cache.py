@@ -43,41 +43,59 @@ class CacheDesc:
         return api._CacheDesc(self.heads, self.kv_heads, self.head_dim, self.pages, dt, float(self.softmax_scale))
 
 
-@dataclass
 class Cache:
     """The pool's tensors: K, V float8_e4m3fn [pages, kv_heads, 64, head_dim]; k_scale, v_scale fp32
-    [pages, kv_heads]; k_mean fp32 [pages, kv_heads, head_dim]."""
-    K: torch.Tensor
-    V: torch.Tensor
-    k_scale: torch.Tensor
-    v_scale: torch.Tensor
-    k_mean: torch.Tensor
+    [pages, kv_heads]; k_mean fp32 [pages, kv_heads, head_dim]. They are checked here, once, and are the pool's
+    for good: a tensor may not be resized or given other memory while the calls use it."""
+    __slots__ = ("K", "V", "k_scale", "v_scale", "k_mean", "_shape", "_dev", "_ref", "_c")
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                 k_mean: torch.Tensor):
+        if not isinstance(K, torch.Tensor) or K.dim() != 4 or K.shape[2] != PAGE:
+            raise SsbaError(SSBA_ERR_INVALID, f"K must be a tensor [pages, kv_heads, {PAGE}, head_dim]")
+        pages, kv, _, d = K.shape
+        tensors = (K, V, k_scale, v_scale, k_mean)
+        for t, n, shape, dtype in ((K, "K", K.shape, _E4M3), (V, "V", K.shape, _E4M3),
+                                   (k_scale, "k_scale", (pages, kv), torch.float32),
+                                   (v_scale, "v_scale", (pages, kv), torch.float32),
+                                   (k_mean, "k_mean", (pages, kv, d), torch.float32)):
+            _check(t, "cache." + n, shape, dtype)
+            if t.device != K.device:
+                raise SsbaError(SSBA_ERR_INVALID, f"cache.{n} is on {t.device}, K on {K.device}")
+        put = object.__setattr__
+        for n, t in zip(Cache.__slots__, tensors):
+            put(self, n, t)
+        put(self, "_shape", (pages, kv, d))
+        put(self, "_dev", K.device)
+        c = api._Cache(*(t.data_ptr() for t in tensors))
+        put(self, "_c", c)
+        put(self, "_ref", ctypes.byref(c))
+
+    def __setattr__(self, name, value):
+        raise AttributeError("a cache's tensors are given when it is made")
 
 
 class _Plan:
-    """What the calls derive from a descriptor's values alone: the C struct and the pool's shapes."""
-    __slots__ = ("c", "ref", "dtype", "heads", "kv", "d", "pages", "tiles", "scales", "means")
+    """What the calls derive from a descriptor's values alone: the C struct and the sizes."""
+    __slots__ = ("c", "ref", "dtype", "heads", "kv", "d", "shape")
 
     def __init__(self, desc: CacheDesc, c):
         self.c, self.ref, self.dtype = c, ctypes.byref(c), desc.dtype
-        self.heads, self.kv, self.d, self.pages = desc.heads, desc.kv_heads, desc.head_dim, desc.pages
-        self.tiles = torch.Size((desc.pages, desc.kv_heads, PAGE, desc.head_dim))
-        self.scales = self.tiles[:2]
-        self.means = torch.Size((desc.pages, desc.kv_heads, desc.head_dim))
+        self.heads, self.kv, self.d = desc.heads, desc.kv_heads, desc.head_dim
+        self.shape = (desc.pages, desc.kv_heads, desc.head_dim)
 
 
 _plans: dict = {}
 
 
 def _plan(desc: CacheDesc) -> _Plan:
-    """The plan of a descriptor, kept by its C struct and its sizes as given (the struct keeps 32 bits of them)."""
-    c = desc.c()
-    key = (bytes(c), desc.heads, desc.kv_heads, desc.head_dim, desc.pages)
+    """The plan of a descriptor, kept by its values."""
+    key = (desc.heads, desc.kv_heads, desc.head_dim, desc.pages, desc.dtype, desc.softmax_scale)
     pl = _plans.get(key)
     if pl is None:
-        if min(key[1:]) <= 0 or max(key[1:]) > 2 ** 31 - 1:
+        if min(key[:4]) <= 0 or max(key[:4]) > 2 ** 31 - 1:  # the struct keeps 32 bits
             raise SsbaError(SSBA_ERR_INVALID, f"sizes must be positive and below 2^31: {desc}")
-        pl = _Plan(desc, c)
+        pl = _Plan(desc, desc.c())
         if len(_plans) >= api._PLAN_CAP:
             _plans.clear()
         _plans[key] = pl
@@ -85,23 +103,22 @@ def _plan(desc: CacheDesc) -> _Plan:
 
 
 def _pool(pl: _Plan, cache: Cache):
-    """The C struct of a checked pool, and its device, which has to be the current one."""
-    _check(cache.K, "cache.K", pl.tiles, _E4M3)
-    _check(cache.V, "cache.V", pl.tiles, _E4M3)
-    _check(cache.k_scale, "cache.k_scale", pl.scales, torch.float32)
-    _check(cache.v_scale, "cache.v_scale", pl.scales, torch.float32)
-    _check(cache.k_mean, "cache.k_mean", pl.means, torch.float32)
-    return api._Cache(cache.K.data_ptr(), cache.V.data_ptr(), cache.k_scale.data_ptr(), cache.v_scale.data_ptr(),
-                      cache.k_mean.data_ptr()), cache.K.device
-
-
-def _same_device(dev, cache: Cache, *tensors) -> None:
-    """Kernels run on the current device: everything has to be there."""
-    for t in (cache.V, cache.k_scale, cache.v_scale, cache.k_mean, *tensors):
-        if t is not None and t.device != dev:
-            raise SsbaError(SSBA_ERR_INVALID, f"tensors on {dev} and {t.device} in one call")
-    if dev.index != torch.cuda.current_device():
+    """The device of a pool of the plan's sizes; it has to be the current one, where kernels run."""
+    if not isinstance(cache, Cache):
+        raise SsbaError(SSBA_ERR_INVALID, "cache must be a Cache")
+    if cache._shape != pl.shape:
+        raise SsbaError(SSBA_ERR_INVALID, f"cache of (pages, kv_heads, head_dim) {cache._shape}, expected {pl.shape}")
+    dev = cache._dev
+    if dev.index != torch._C._cuda_getDevice():
         raise SsbaError(SSBA_ERR_INVALID, f"the cache is on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+    return dev
+
+
+def _same_device(dev, *tensors) -> None:
+    index = dev.index
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            raise SsbaError(SSBA_ERR_INVALID, f"tensors on {dev} and {t.device} in one call")
 
 
 def _rows(x, name: str, heads: int, pl: _Plan) -> int:
@@ -124,10 +141,10 @@ def _batch(table, lens, cu):
 
 def cache_alloc(desc: CacheDesc, device="cuda") -> Cache:
     """A pool of desc.pages pages (contents undefined: an append writes what later calls read)."""
-    pl = _plan(desc)
-    kv = [torch.empty(pl.tiles, dtype=_E4M3, device=device) for _ in range(2)]
-    scales = [torch.empty(pl.scales, dtype=torch.float32, device=device) for _ in range(2)]
-    return Cache(*kv, *scales, torch.empty(pl.means, dtype=torch.float32, device=device))
+    pages, kv, d = _plan(desc).shape
+    kw = dict(device=device, dtype=torch.float32)
+    return Cache(*(torch.empty((pages, kv, PAGE, d), device=device, dtype=_E4M3) for _ in range(2)),
+                 *(torch.empty((pages, kv), **kw) for _ in range(2)), torch.empty((pages, kv, d), **kw))
 
 
 def cache_append(desc: CacheDesc, cache: Cache, k, v, table, lens, cu, stream=None) -> Cache:
@@ -135,12 +152,12 @@ def cache_append(desc: CacheDesc, cache: Cache, k, v, table, lens, cu, stream=No
     lens [B] (tokens held before), cu [B + 1], all int32. Returns the cache."""
     lib = load_library()
     pl = _plan(desc)
-    pool, dev = _pool(pl, cache)
+    dev = _pool(pl, cache)
     T = _rows(k, "k", pl.kv, pl)
     _check(v, "v", k.shape, pl.dtype)
     batch = _batch(table, lens, cu)
-    _same_device(dev, cache, k, v, table, lens, cu)
-    _raise_on(lib.ssba_cache_append(pl.ref, ctypes.byref(pool), k.data_ptr(), v.data_ptr(), T, *batch,
+    _same_device(dev, k, v, table, lens, cu)
+    _raise_on(lib.ssba_cache_append(pl.ref, cache._ref, k.data_ptr(), v.data_ptr(), T, *batch,
                                     _stream_ptr(stream)))
     return cache
 
@@ -151,16 +168,16 @@ def cache_select(desc: CacheDesc, cache: Cache, q, table, lens, cu, keep: int, f
     lens: tokens held, the rows of q among them."""
     lib = load_library()
     pl = _plan(desc)
-    pool, dev = _pool(pl, cache)
+    dev = _pool(pl, cache)
     T = _rows(q, "q", pl.heads, pl)
     batch = _batch(table, lens, cu)
     if not 0 <= first < keep:
         raise SsbaError(SSBA_ERR_INVALID, f"keep={keep} must be more than first={first}, first >= 0")
-    _same_device(dev, cache, q, table, lens, cu, idx, cnt)
+    _same_device(dev, q, table, lens, cu, idx, cnt)
     side = _side(stream, dev)
     idx = _out(idx, "idx", (T, pl.kv, keep), torch.int32, dev, side)
     cnt = _out(cnt, "cnt", (T, pl.kv), torch.int32, dev, side)
-    _raise_on(lib.ssba_cache_select(pl.ref, ctypes.byref(pool), q.data_ptr(), T, *batch, keep, first, idx.data_ptr(),
+    _raise_on(lib.ssba_cache_select(pl.ref, cache._ref, q.data_ptr(), T, *batch, keep, first, idx.data_ptr(),
                                     cnt.data_ptr(), _stream_ptr(stream)))
     return idx, cnt
 
@@ -174,25 +191,33 @@ def cache_attend_workspace_bytes(desc: CacheDesc) -> int:
 
 
 _ws: dict = {}
+_ws_need: dict = {}  # per device: the same for every descriptor
 
 
-def _default_workspace(pl: _Plan, lib, dev, stream):
+def _default_workspace(pl: _Plan, lib, dev, stream, side):
     """A workspace kept per (device, stream): the calls of one stream run in order and can share it. A capture
     gets one of its own, so that no two graphs, and no graph and an eager call, meet in one."""
-    need = int(lib.ssba_cache_attend_workspace_bytes(pl.ref))
-    if need == 0:
-        _raise_on(SSBA_ERR_INVALID)
-    side = _side(stream, dev)
-    with torch.cuda.stream(stream if side is not None else None):
+    need = _ws_need.get(dev.index)
+    if need is None:
+        need = int(lib.ssba_cache_attend_workspace_bytes(pl.ref))
+        if need == 0:
+            _raise_on(SSBA_ERR_INVALID)
+        _ws_need[dev.index] = need
+    if side is None and not torch.cuda.is_current_stream_capturing():
+        key = (dev.index, torch._C._cuda_getCurrentRawStream(dev.index))
+        ws = _ws.get(key)
+        if ws is not None:
+            return ws
+    with torch.cuda.stream(side):  # allocated and filled on the stream that uses it
         if torch.cuda.is_current_stream_capturing():
             # the fill is a node of the graph, so no later call may count on it
             ws = torch.empty(need, dtype=torch.uint8, device=dev)
             ws[:_TICKET_BYTES].zero_()
             return ws
-        key = (dev.index, _stream_ptr(stream))
+        key = (dev.index, torch._C._cuda_getCurrentRawStream(dev.index))
         with _lock:
             ws = _ws.get(key)
-            if ws is None or ws.numel() < need:
+            if ws is None:
                 ws = _ws[key] = torch.zeros(need, dtype=torch.uint8, device=dev)
     return ws
 
@@ -203,7 +228,7 @@ def cache_attend(desc: CacheDesc, cache: Cache, q, table, lens, cu, idx=None, cn
     page of the rows' sequences, or over the lists (idx, cnt) of cache_select."""
     lib = load_library()
     pl = _plan(desc)
-    pool, dev = _pool(pl, cache)
+    dev = _pool(pl, cache)
     T = _rows(q, "q", pl.heads, pl)
     batch = _batch(table, lens, cu)
     keep = 0
@@ -213,16 +238,16 @@ def cache_attend(desc: CacheDesc, cache: Cache, q, table, lens, cu, idx=None, cn
         keep = int(idx.shape[2]) if isinstance(idx, torch.Tensor) and idx.dim() == 3 else 0
         _check(idx, "idx", (T, pl.kv, keep), torch.int32)
         _check(cnt, "cnt", (T, pl.kv), torch.int32)
-    _same_device(dev, cache, q, table, lens, cu, idx, cnt, O, lse)
+    _same_device(dev, q, table, lens, cu, idx, cnt, O, lse)
     side = _side(stream, dev)
     O = _out(O, "O", q.shape, pl.dtype, dev, side)
     lse = _out(lse, "lse", (T, pl.heads), torch.float32, dev, side)
     if isinstance(workspace, str):
-        workspace = _default_workspace(pl, lib, dev, stream)
+        workspace = _default_workspace(pl, lib, dev, stream, side)
     elif workspace is None:
         raise SsbaError(SSBA_ERR_WORKSPACE, "cache_attend needs a workspace")
     wp, wn = api._ws_args(workspace)
-    _raise_on(lib.ssba_cache_attend(pl.ref, ctypes.byref(pool), q.data_ptr(), T, *batch,
+    _raise_on(lib.ssba_cache_attend(pl.ref, cache._ref, q.data_ptr(), T, *batch,
                                     idx.data_ptr() if idx is not None else None,
                                     cnt.data_ptr() if cnt is not None else None, keep, O.data_ptr(), lse.data_ptr(),
                                     wp, wn, _stream_ptr(stream)))
@@ -233,10 +258,10 @@ def cache_copy(desc: CacheDesc, cache: Cache, src, dst, stream=None) -> Cache:
     """ssba_cache_copy: pages src[i] -> dst[i], int32 CUDA tensors [n]. Returns the cache."""
     lib = load_library()
     pl = _plan(desc)
-    pool, dev = _pool(pl, cache)
+    dev = _pool(pl, cache)
     n = src.numel() if isinstance(src, torch.Tensor) else -1
     _check(src, "src", (max(n, 0),), torch.int32)
     _check(dst, "dst", (max(n, 0),), torch.int32)
-    _same_device(dev, cache, src, dst)
-    _raise_on(lib.ssba_cache_copy(pl.ref, ctypes.byref(pool), src.data_ptr(), dst.data_ptr(), n, _stream_ptr(stream)))
+    _same_device(dev, src, dst)
+    _raise_on(lib.ssba_cache_copy(pl.ref, cache._ref, src.data_ptr(), dst.data_ptr(), n, _stream_ptr(stream)))
     return cache

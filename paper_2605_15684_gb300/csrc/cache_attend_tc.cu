@@ -159,23 +159,24 @@ struct Blocks {
 
     __device__ __forceinline__ Blocks(const Seq& s, int tq_) : a(s.len - s.n), n(s.n), len(s.len), tq(tq_)
     {
-        count = (n + tq - 1) / tq;
+        count = (n + tq - 1) >> shift();
     }
+    __device__ __forceinline__ int shift() const { return 31 - __clz(tq); }
     __device__ __forceinline__ int tiles(int t) const
     {
         const int seen = t + 1 < count ? a + (t + 1) * tq : len;
         return max(1, (seen + kTile - 1) / kTile);
     }
-    static __device__ __forceinline__ long long upto(long long k, int m)  // sum of max(1, ceil(j / m)), j = 1 .. k
+    static __device__ __forceinline__ long long upto(int k, int m)  // sum of max(1, ceil(j / m)), j = 1 .. k
     {
         if (k <= 0) return k;
-        const long long d = k / m, r = k - d * m;
-        return m * (d * (d + 1) / 2) + r * (d + 1);
+        const int d = k >> (31 - __clz(m)), r = k & (m - 1);  // m is a power of two
+        return (long long)m * d * (d + 1) / 2 + (long long)r * (d + 1);
     }
     __device__ __forceinline__ long long before(int t) const  // tiles of blocks 0 .. t - 1, t < count
     {
-        const int u = a >= 0 ? (a + tq - 1) / tq : -(-a / tq), m = kTile / tq;
-        return upto((long long)u + t, m) - upto(u, m);
+        const int u = (a + tq - 1) >> shift(), m = kTile >> shift();
+        return upto(u + t, m) - upto(u, m);
     }
     __device__ __forceinline__ long long sum() const { return count ? before(count - 1) + tiles(count - 1) : 0; }
 };
@@ -304,32 +305,48 @@ __device__ void make_share(const Params& p, S& sm)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int heads = p.pl.kv_heads * p.chunks;
     __shared__ long long wsum[kThreads / 32];
-    if (kList) {
-        if (tid == 0) {
-            const int r0 = max(0, min(__ldg(p.bt.cu), p.bt.T)), r1 = max(r0, min(__ldg(p.bt.cu + p.bt.B), p.bt.T));
-            sm.total = (long long)(r1 - r0) * heads * ((p.keep + 1) / 2);
-        }
-        __syncthreads();
-    } else {
-        long long mine = 0;
-        for (int b = tid; b < p.bt.B; b += kThreads) mine += Blocks(load_seq(p.bt, b, p.pl.status), p.tq).sum();
+    // tiles of thread tid's sequence of those from b0 on, all heads: sum over the CTA, or that in front of the thread
+    auto scan = [&](int b0, long long mine, long long& front) {
+        long long inc = mine;
 #pragma unroll
-        for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-        if (lane == 0) wsum[warp] = mine;
-        __syncthreads();
-        if (tid == 0) {
-            long long t = 0;
-            for (int w = 0; w < kThreads / 32; ++w) t += wsum[w];
-            sm.total = t * heads;
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long x = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += x;
         }
         __syncthreads();
+        if (lane == 31) wsum[warp] = inc;
+        __syncthreads();
+        long long sum = 0;
+        front = inc - mine;
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) {
+            if (w < warp) front += wsum[w];
+            sum += wsum[w];
+        }
+        return sum;
+    };
+    auto tiles_of = [&](int b) {
+        return b < p.bt.B ? Blocks(load_seq(p.bt, b, p.pl.status), p.tq).sum() * heads : 0LL;
+    };
+    long long W = 0, mine = 0, front = 0;
+    if (kList) {
+        const int r0 = max(0, min(__ldg(p.bt.cu), p.bt.T)), r1 = max(r0, min(__ldg(p.bt.cu + p.bt.B), p.bt.T));
+        W = (long long)(r1 - r0) * heads * ((p.keep + 1) / 2);
+    } else {
+        for (int b0 = 0; b0 < p.bt.B; b0 += kThreads) {
+            mine = tiles_of(b0 + tid);
+            W += scan(b0, mine, front);
+        }
     }
-    const long long W = sm.total;
-    const int C = (int)min((long long)gridDim.x, max(W, 1LL));
-    const long long w0 = (int)blockIdx.x < C ? W * blockIdx.x / C : W, w1 = (int)blockIdx.x < C ? W * (blockIdx.x + 1) / C : W;
+    const int C = (int)min((long long)gridDim.x, max(W, 1LL)), c = blockIdx.x;
+    // (32-bit division where it does)
+    const bool small = W < INT_MAX / kMaxGrid;
+    const long long w0 = c >= C ? W : small ? (int)W * c / C : W * c / C;
+    const long long w1 = c >= C ? W : small ? (int)W * (c + 1) / C : W * (c + 1) / C;
     if (tid == 0) {
         sm.w0 = w0;
         sm.w1 = w1;
+        sm.total = W;
         sm.ctas = C;
         sm.first_b = 0;
         sm.first_at = 0;
@@ -337,38 +354,93 @@ __device__ void make_share(const Params& p, S& sm)
     __syncthreads();
     if (!kList && w0 < w1) {
         long long base = 0;  // tiles of the sequences in front, all heads
-        for (int b0 = 0; b0 < p.bt.B; b0 += kThreads) {
-            const int b = b0 + tid;
-            const long long mine = b < p.bt.B ? Blocks(load_seq(p.bt, b, p.pl.status), p.tq).sum() * heads : 0;
-            long long inc = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long x = __shfl_up_sync(0xffffffffu, inc, o);
-                if (lane >= o) inc += x;
+        for (int b0 = 0; b0 < p.bt.B && base <= w0; b0 += kThreads) {
+            long long sum = W;
+            if (p.bt.B > kThreads) {  // else the sum's own scan
+                mine = tiles_of(b0 + tid);
+                sum = scan(b0, mine, front);
             }
-            __syncthreads();
-            if (lane == 31) wsum[warp] = inc;
-            __syncthreads();
-            long long at = base + inc - mine, sum = 0;
-#pragma unroll
-            for (int w = 0; w < kThreads / 32; ++w) {
-                if (w < warp) at += wsum[w];
-                sum += wsum[w];
-            }
+            const long long at = base + front;
             if (w0 >= at && w0 < at + mine) {
-                sm.first_b = b;
+                sm.first_b = b0 + tid;
                 sm.first_at = w0 - at;
             }
             base += sum;
-            if (base > w0) break;
         }
     }
     __syncthreads();
 }
 
+// Joins the np parts of an item that begins in CTA c0, in order, and writes its rows: a softmax warp takes every
+// fourth row, two at a time, a lane four channels, with four parts' loads in flight.
+template <int R, int D, class W>
+__device__ __noinline__ void join(const Params& p, const W& it, int c0, int np, int quad, int lane)
+{
+    constexpr int kAhead = 4;
+#pragma unroll 1
+    for (int r0 = quad; r0 < R; r0 += 8) {
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {}, o[2][4] = {};
+        int row[2], head[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) row[u] = it.row_of(r0 + 4 * u, head[u]);
+#pragma unroll 1
+        for (int k0 = 0; k0 < np; k0 += kAhead) {
+            float2 ml[2][kAhead];
+            float4 v[2][kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                // part 0 is slot 1 of CTA c0, part k slot 0 of CTA c0 + k
+                const float* at = p.parts + ((size_t)(c0 + k0 + k) * 2 + (k0 + k == 0)) * R * (D + 2);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    ml[u][k] = make_float2(-INFINITY, 0.f);
+                    v[u][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (k0 + k < np && row[u] >= 0) {
+                        ml[u][k] = __ldcg(reinterpret_cast<const float2*>(at + R * D) + r0 + 4 * u);
+                        if (lane < D / 4) v[u][k] = __ldcg(reinterpret_cast<const float4*>(at + (r0 + 4 * u) * D) + lane);
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                float top = m[u];
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) top = fmaxf(top, ml[u][k].x);
+                const float at0 = top == -INFINITY ? 0.f : top, f = fast_exp2(m[u] - at0);
+                m[u] = top;
+                l[u] *= f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[u][e] *= f;
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    const float fk = fast_exp2(ml[u][k].x - at0);
+                    l[u] = fmaf(ml[u][k].y, fk, l[u]);
+                    o[u][0] = fmaf(v[u][k].x, fk, o[u][0]);
+                    o[u][1] = fmaf(v[u][k].y, fk, o[u][1]);
+                    o[u][2] = fmaf(v[u][k].z, fk, o[u][2]);
+                    o[u][3] = fmaf(v[u][k].w, fk, o[u][3]);
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if (row[u] < 0) continue;
+            const size_t at = (size_t)row[u] * p.pl.heads + head[u];
+            const float inv = l[u] != 0.f ? 1.f / l[u] : 0.f;
+            if (lane < D / 4) {
+                __nv_bfloat162 a = __floats2bfloat162_rn(o[u][0] * inv, o[u][1] * inv);
+                __nv_bfloat162 b = __floats2bfloat162_rn(o[u][2] * inv, o[u][3] * inv);
+                *reinterpret_cast<uint2*>(p.O + at * D + lane * 4) =
+                    make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
+            }
+            if (lane == 0) p.lse[at] = l[u] != 0.f ? (m[u] + log2f(l[u])) * kLn2 : -INFINITY;
+        }
+    }
+}
+
 template <int R, int D, bool kList>
 __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_tc_kernel(const __grid_constant__ Maps maps,
-                                                                                          const Params p)
+                                                                                          const __grid_constant__ Params p)
 {
     using C = Cfg<R, D>;
     constexpr int N = C::N;
@@ -406,6 +478,9 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
         for (int i = threadIdx.x - kSoft; i < D; i += kSoft) sm.nan_at[i] = INT_MAX;
     }
     tc_fence_before();
+    // everything above reads no input (programmatic dependent launch: it may run beside the last grid's end)
+    grid_dep_wait();
+    grid_dep_launch();
     make_share<kList>(p, sm);  // ends in a barrier
     tc_fence_after();
     const uint32_t tbase = sm.tmem_base;
@@ -768,7 +843,6 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sm.q_empty[st]));
             const bool whole = it.tb == 0 && it.te == it.tiles;
-            bool out = whole;
             if (!whole) {
                 // parts: slot 1 of the CTA that the item starts in, slot 0 of the others
                 float* part = p.parts + ((size_t)blockIdx.x * 2 + (it.tb == 0)) * R * (D + 2);
@@ -778,10 +852,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
                 }
 #pragma unroll
                 for (int r = 0; r < R; ++r)
-                    if (tok == r) {
-                        part[R * D + r] = ref;
-                        part[R * D + R + r] = l[r];
-                    }
+                    if (tok == r) reinterpret_cast<float2*>(part + R * D)[r] = make_float2(ref, l[r]);
                 __threadfence();
                 soft_sync();
                 const int c0 = (int)(((it.start + 1) * sm.ctas - 1) / sm.total);
@@ -793,33 +864,11 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
                     __threadfence();
                 }
                 soft_sync();
-                out = sm.last != 0;
-                if (out) {
-                    const float* first = p.parts + ((size_t)c0 * 2 + 1) * R * (D + 2);
-                    const float* rest = p.parts + (size_t)c0 * 2 * R * (D + 2);  // CTA c0 + k: + k * 2 parts
-                    const size_t step = (size_t)2 * R * (D + 2);
-                    const int np = c1 - c0;
-#pragma unroll
-                    for (int r = 0; r < R; ++r) {
-                        float m = __ldcg(first + R * D + r);
-                        for (int k = 1; k <= np; ++k) m = fmaxf(m, __ldcg(rest + k * step + R * D + r));
-                        const float mm = m == -INFINITY ? 0.f : m;
-                        float f = fast_exp2(__ldcg(first + R * D + r) - mm);
-                        float lt = __ldcg(first + R * D + R + r) * f;
-                        float ot = tok < D ? __ldcg(first + r * D + tok) * f : 0.f;
-#pragma unroll 4
-                        for (int k = 1; k <= np; ++k) {
-                            f = fast_exp2(__ldcg(rest + k * step + R * D + r) - mm);
-                            lt += __ldcg(rest + k * step + R * D + R + r) * f;
-                            if (tok < D) ot += __ldcg(rest + k * step + r * D + tok) * f;
-                        }
-                        if (tok == r) ref = m;
-                        l[r] = lt;
-                        o[r] = ot;
-                    }
+                if (sm.last) {
+                    const Walk<kList> at = it;  // (a copy, so that the walk itself stays in registers)
+                    join<R, D>(p, at, c0, c1 - c0 + 1, quad, lane);
                 }
-            }
-            if (out) {
+            } else {
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     int head;
@@ -877,8 +926,18 @@ int launch(const Maps& maps, const Params& p, cudaStream_t st)
     });
     const int most = kMaxGrid / (R <= 16 ? 1 : 2);
     const int grid = std::min(device_sm_count() * C::kCtas, most);
-    ssba_cache_attend_tc_kernel<R, D, kList><<<grid, kThreads, smem, st>>>(maps, p);
-    const cudaError_t e = cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid, 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, ssba_cache_attend_tc_kernel<R, D, kList>, maps, p);
+    if (e == cudaSuccess) e = cudaGetLastError();
     if (e == cudaSuccess) return SSBA_OK;
     set_error("ssba_cache_attend: %s", cudaGetErrorString(e));
     return SSBA_ERR_CUDA;

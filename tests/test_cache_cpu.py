@@ -100,10 +100,11 @@ def test_outputs_lists_and_workspaces(lib):
 
 def test_binding_refuses_before_it_calls(lib):
     d = pc.CacheDesc(8, 2, 128, 4)
-    c = pc.cache_alloc(d, "cpu")
     q, t = torch.zeros(3, 8, 128, dtype=torch.bfloat16), torch.zeros(1, 4, dtype=torch.int32)
     with pytest.raises(api.SsbaError, match="CUDA tensor"):
-        pc.cache_attend(d, c, q, t, t[0, :1], t[0, :2])
+        pc.cache_alloc(d, "cpu")
+    with pytest.raises(api.SsbaError, match="must be a Cache"):
+        pc.cache_attend(d, None, q, t, t[0, :1], t[0, :2])
     with pytest.raises(api.SsbaError, match="dtype"):
         pc.cache_alloc(pc.CacheDesc(8, 2, 128, 4, torch.float16), "cpu")
     with pytest.raises(api.SsbaError, match="2\\^31"):
