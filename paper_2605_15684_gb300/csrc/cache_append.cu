@@ -16,8 +16,10 @@ namespace ssba {
 namespace cache {
 namespace {
 
-constexpr int kThreads = 256;  // half of them K, half V
-constexpr int kHalf = kThreads / 2;
+constexpr int kThreads = 128;
+constexpr int kWarps = kThreads / 32;
+constexpr int kSeqs = 1024;  // sequences whose pages are counted at a time
+constexpr int kStages = 2;
 
 template <typename T>
 struct Chunk;  // 16 bytes of input
@@ -46,166 +48,207 @@ struct Chunk<float> {
     }
 };
 
-// The unit-th (sequence, page label) that the batch touches, pages of a sequence in order; false if
-// there are fewer. Called by the whole CTA.
-__device__ bool find_unit(const Batch& bt, int unit, int* status, int& b_out, int& j_out, Seq& s_out)
+// Touched pages of sequences [b0, b0 + kSeqs): ends[i] is how many those up to b0 + i have; returns their sum.
+__device__ int count_pages(const Batch& bt, int b0, int* status, int* ends, int* buf)
 {
-    __shared__ int wsum[kThreads / 32];
-    __shared__ int found[2];
-    __shared__ Seq fseq;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid == 0) found[0] = -1;
-    int base = 0;
-    for (int b0 = 0; b0 < bt.B; b0 += kThreads) {
-        const int b = b0 + tid;
-        int cnt = 0;
-        Seq s{0, 0, 0};
+    constexpr int kEach = kSeqs / kThreads;
+    int cnt[kEach], sum = 0;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        const int b = b0 + tid * kEach + e;
+        cnt[e] = 0;
         if (b < bt.B) {
-            s = load_seq(bt, b, status);
-            const int end = s.len + min(s.n, bt.width * kPage - s.len);
-            if (end < s.len + s.n) flag(status);  // no room in the table: the rest is left out
-            s.n = end - s.len;
-            cnt = s.n > 0 ? (end - 1) / kPage - s.len / kPage + 1 : 0;
+            const Seq s = load_seq(bt, b, status);
+            const int room = bt.width * kPage - s.len;
+            if (s.n > room) flag(status);  // the rest has no place in the table and is left out
+            const int n = min(s.n, room);
+            cnt[e] = n > 0 ? (s.len + n - 1) / kPage - s.len / kPage + 1 : 0;
         }
-        int inc = cnt;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int x = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += x;
-        }
-        if (lane == 31) wsum[warp] = inc;
-        __syncthreads();
-        int before = base, total = 0;
-#pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w) {
-            if (w < warp) before += wsum[w];
-            total += wsum[w];
-        }
-        const int from = before + inc - cnt;
-        if (unit >= from && unit < from + cnt) {
-            found[0] = b;
-            found[1] = s.len / kPage + (unit - from);
-            fseq = s;
-        }
-        base += total;
-        __syncthreads();
-        if (found[0] >= 0 || unit < base) break;
+        sum += cnt[e];
     }
-    b_out = found[0];
-    j_out = found[1];
-    s_out = fseq;
-    return b_out >= 0;
+    int inc = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += x;
+    }
+    __syncthreads();
+    if (lane == 31) buf[warp] = inc;
+    __syncthreads();
+    int at = inc - sum, total = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) at += buf[w];
+        total += buf[w];
+    }
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) ends[tid * kEach + e] = at += cnt[e];
+    __syncthreads();
+    return total;
 }
 
-// One CTA per (touched page, head); threads [0, 128) take K, the others V. A thread keeps its chunks of
-// 16 input bytes in registers between the maximum and the rounding, so that inputs are read once.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool real)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+
+// A unit is a touched page, a head, and K or V. CTAs take units in turn; the inputs of the next one are under way
+// (each thread copies to shared memory what it will read itself) while one is worked on.
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) ssba_cache_append_kernel(const Pool pl, const Batch bt, const T* k,
                                                                      const T* v)
 {
-    constexpr int kN = Chunk<T>::n, kRowChunks = D / kN, kRows = kHalf / kRowChunks, kPass = kPage / kRows;
-    __shared__ float red[2][kHalf / 32];
-    __shared__ float sums[kRows][D];
-    int b, j;
-    Seq s;
-    if (!find_unit(bt, blockIdx.x, pl.status, b, j, s)) return;
-    const int page = page_of(bt, pl, b, j);
-    if (page < 0) return;
-    const int h = blockIdx.y, half = threadIdx.x / kHalf, tid = threadIdx.x % kHalf;
+    constexpr int kN = Chunk<T>::n, kRowChunks = D / kN, kRows = kThreads / kRowChunks, kPass = kPage / kRows;
+    extern __shared__ uint4 stage[];  // [kStages][kPass][kThreads]
+    __shared__ int ends[kSeqs];
+    __shared__ int buf[kWarps];
+    __shared__ float red[2][kWarps];
+    __shared__ float sums[kWarps][D];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int row0 = tid / kRowChunks, c = tid % kRowChunks;
-    const int s0 = max(s.len - j * kPage, 0), s1 = min(s.len + s.n - j * kPage, kPage);  // new slots
-    const T* x = half ? v : k;
-    const T* src = x + ((size_t)(s.row + j * kPage - s.len) * pl.kv_heads + h) * D + c * kN;
-    uint8_t* dst = (half ? pl.V : pl.K) + ((size_t)page * pl.kv_heads + h) * kPage * D + c * kN;
-    float* scale_at = (half ? pl.v_scale : pl.k_scale) + (size_t)page * pl.kv_heads + h;
 
-    uint4 in[kPass];
-    float amax = 0.f;
+    struct Unit {
+        int s0, s1;       // new slots
+        size_t tile;      // page * kv_heads + head
+        bool v, real;
+        float was;
+    };
+    int turn = 0, phase = 0;
+    for (int b0 = 0; b0 < bt.B; b0 += kSeqs) {
+        const int pages = count_pages(bt, b0, pl.status, ends, buf);
+        const long long units = (long long)pages * pl.kv_heads * 2;
+        // unit u of this pass, its copies under way into stage st
+        auto begin = [&](long long u, int st) {
+            Unit x{0, 0, 0, false, false, 0.f};
+            if (u < units) {
+                const int pg = (int)(u / (2 * pl.kv_heads)), hv = (int)(u - (long long)pg * 2 * pl.kv_heads);
+                const int h = hv >> 1;
+                x.v = hv & 1;
+                int lo = 0, hi = kSeqs - 1;  // the first sequence with ends > pg
+                while (lo < hi) {
+                    const int mid = (lo + hi) / 2;
+                    if (ends[mid] > pg) hi = mid;
+                    else lo = mid + 1;
+                }
+                const int b = b0 + lo;
+                const Seq s = load_seq(bt, b, pl.status);
+                const int j = s.len / kPage + pg - (lo ? ends[lo - 1] : 0);
+                const int page = page_of(bt, pl, b, j);
+                if (page >= 0) {
+                    const int n = min(s.n, bt.width * kPage - s.len);
+                    x.real = true;
+                    x.s0 = max(s.len - j * kPage, 0);
+                    x.s1 = min(s.len + n - j * kPage, kPage);
+                    x.tile = (size_t)page * pl.kv_heads + h;
+                    if (x.s0 > 0) x.was = (x.v ? pl.v_scale : pl.k_scale)[x.tile];
+                    const T* src = (x.v ? v : k) + ((ptrdiff_t)(s.row + j * kPage - s.len) * pl.kv_heads + h) * D + c * kN;
 #pragma unroll
-    for (int i = 0; i < kPass; ++i) {
-        const int slot = row0 + i * kRows;
-        in[i] = make_uint4(0, 0, 0, 0);
-        if (slot >= s0 && slot < s1) in[i] = __ldg(reinterpret_cast<const uint4*>(src + (size_t)slot * pl.kv_heads * D));
-    }
-    const float was = s0 > 0 ? *scale_at : 0.f;
-#pragma unroll
-    for (int i = 0; i < kPass; ++i) {
-        float f[kN];
-        Chunk<T>::get(in[i], f);
-#pragma unroll
-        for (int e = 0; e < kN; ++e) {
-            const float a = fabsf(f[e]);
-            if (a < INFINITY) amax = fmaxf(amax, a);
-        }
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-    if ((tid & 31) == 0) red[half][tid >> 5] = amax;
-    __syncthreads();
-    amax = fmaxf(fmaxf(red[half][0], red[half][1]), fmaxf(red[half][2], red[half][3]));
-    const float scale = fmaxf(was, scale_for(amax));
-    const float inv = scale > 0.f ? 1.f / scale : 1.f;
-    const float shrink = was < scale ? was * inv : 1.f;  // of the older bytes
-    const bool full = !half && s1 == kPage;
-    float sum[kN] = {};
-#pragma unroll
-    for (int i = 0; i < kPass; ++i) {
-        const int slot = row0 + i * kRows;
-        uint8_t* at = dst + (size_t)slot * D;
-        if (slot >= s0 && slot < s1) {
-            float f[kN];
-            Chunk<T>::get(in[i], f);
-            uint32_t w[kN / 4];
-#pragma unroll
-            for (int e = 0; e < kN; e += 4) {
-                float y[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) y[r] = fabsf(f[e + r]) < INFINITY ? f[e + r] * inv : NAN;
-                w[e / 4] = to_e4m3x2(y[0], y[1]) | (to_e4m3x2(y[2], y[3]) << 16);
+                    for (int i = 0; i < kPass; ++i) {
+                        const int slot = row0 + i * kRows;
+                        const bool in = slot >= x.s0 && slot < x.s1;
+                        copy16(static_cast<uint32_t>(__cvta_generic_to_shared(stage + (st * kPass + i) * kThreads + tid)),
+                               in ? src + (ptrdiff_t)slot * pl.kv_heads * D : k, in);
+                    }
+                }
             }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            return x;
+        };
+        Unit next = begin(blockIdx.x, turn % kStages);
+        for (long long u = blockIdx.x; u < units; u += gridDim.x, ++turn) {
+            const Unit x = next;
+            next = begin(u + gridDim.x, (turn + 1) % kStages);
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            if (!x.real) continue;
+            phase ^= 1;
+            const uint4* in = stage + (turn % kStages) * kPass * kThreads + tid;
+            float amax = 0.f;
 #pragma unroll
-            for (int e = 0; e < kN / 4; ++e) reinterpret_cast<uint32_t*>(at)[e] = w[e];
+            for (int i = 0; i < kPass; ++i) {
+                float f[kN];
+                Chunk<T>::get(in[i * kThreads], f);
+#pragma unroll
+                for (int e = 0; e < kN; ++e) {
+                    const float a = fabsf(f[e]);
+                    if (a < INFINITY) amax = fmaxf(amax, a);
+                }
+            }
+            amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
+            if (lane == 0) red[phase][warp] = amax;
+            __syncthreads();
+            amax = fmaxf(fmaxf(red[phase][0], red[phase][1]), fmaxf(red[phase][2], red[phase][3]));
+            const float scale = fmaxf(x.was, scale_for(amax));
+            const float inv = scale > 0.f ? 1.f / scale : 1.f;
+            const float shrink = x.was < scale ? x.was * inv : 1.f;  // of the older bytes
+            const bool full = !x.v && x.s1 == kPage;
+            uint8_t* dst = (x.v ? pl.V : pl.K) + x.tile * kPage * D + c * kN;
+            float sum[kN] = {};
+#pragma unroll
+            for (int i = 0; i < kPass; ++i) {
+                const int slot = row0 + i * kRows;
+                uint32_t* at = reinterpret_cast<uint32_t*>(dst + slot * D);
+                uint32_t w[kN / 4];
+                if (slot >= x.s0 && slot < x.s1) {
+                    float f[kN];
+                    Chunk<T>::get(in[i * kThreads], f);
+#pragma unroll
+                    for (int e = 0; e < kN; e += 4) {
+                        float y[4];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) y[r] = fabsf(f[e + r]) < INFINITY ? f[e + r] * inv : NAN;
+                        w[e / 4] = to_e4m3x2(y[0], y[1]) | (to_e4m3x2(y[2], y[3]) << 16);
+                    }
+                } else if (slot < x.s0 && (full || shrink != 1.f)) {
+#pragma unroll
+                    for (int e = 0; e < kN / 4; ++e) {
+                        w[e] = at[e];
+                        float y[4];
+                        from_e4m3x4(w[e], y);
+                        if (shrink != 1.f)
+                            w[e] = to_e4m3x2(y[0] * shrink, y[1] * shrink) | (to_e4m3x2(y[2] * shrink, y[3] * shrink) << 16);
+                    }
+                } else {
+                    continue;
+                }
+                if (kN == 8) *reinterpret_cast<uint2*>(at) = make_uint2(w[0], w[kN / 4 - 1]);
+                else at[0] = w[0];
+                if (full) {
+#pragma unroll
+                    for (int e = 0; e < kN; e += 4) {
+                        float y[4];
+                        from_e4m3x4(w[e / 4], y);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) sum[e + r] += y[r];
+                    }
+                }
+            }
+            if (tid == 0) (x.v ? pl.v_scale : pl.k_scale)[x.tile] = scale;
             if (full) {
+                // rows of a warp by shuffles (where it holds several), the warps through shared memory
 #pragma unroll
-                for (int e = 0; e < kN; e += 4) {
-                    float y[4];
-                    from_e4m3x4(w[e / 4], y);
+                for (int e = 0; e < kN; ++e) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) sum[e + r] += y[r];
+                    for (int o = 16; o >= kRowChunks; o >>= 1) sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], o);
+                    if (lane < kRowChunks) sums[warp][c * kN + e] = sum[e];
                 }
-            }
-        } else if (slot < s0 && (full || shrink != 1.f)) {
-#pragma unroll
-            for (int e = 0; e < kN; e += 4) {
-                uint32_t w = reinterpret_cast<uint32_t*>(at)[e / 4];
-                float y[4];
-                from_e4m3x4(w, y);
-                if (shrink != 1.f) {
-                    w = to_e4m3x2(y[0] * shrink, y[1] * shrink) | (to_e4m3x2(y[2] * shrink, y[3] * shrink) << 16);
-                    reinterpret_cast<uint32_t*>(at)[e / 4] = w;
-                    from_e4m3x4(w, y);
+                __syncthreads();
+                if (tid < D) {
+                    const float m = (sums[0][tid] + sums[1][tid]) + (sums[2][tid] + sums[3][tid]);
+                    pl.k_mean[x.tile * D + tid] = m * (scale * (1.f / kPage));
                 }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) sum[e + r] += y[r];
+                __syncthreads();
             }
         }
-    }
-    if (full) {
-#pragma unroll
-        for (int e = 0; e < kN; ++e) sums[row0][c * kN + e] = sum[e];
-    }
-    __syncthreads();
-    if (tid == 0) *scale_at = scale;
-    if (full && tid < D) {
-        float m = 0.f;
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) m += sums[r][tid];
-        pl.k_mean[((size_t)page * pl.kv_heads + h) * D + tid] = m * (scale * (1.f / kPage));
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();
     }
 }
 
 // Pages src[i] -> dst[i]; the kv_heads * 64 * D bytes of a page are contiguous in K and in V.
-__global__ void __launch_bounds__(kThreads) ssba_cache_copy_kernel(const Pool pl, int D, const int32_t* src,
+constexpr int kCopyThreads = 256;
+
+__global__ void __launch_bounds__(kCopyThreads) ssba_cache_copy_kernel(const Pool pl, int D, const int32_t* src,
                                                                    const int32_t* dst)
 {
     const int i = blockIdx.x, h = blockIdx.y;
@@ -221,7 +264,7 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_copy_kernel(const Pool pl
     uint4 kr[2], vr[2];  // D <= 128: at most 512 chunks a tensor
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        const int at = threadIdx.x + u * kThreads;
+        const int at = threadIdx.x + u * kCopyThreads;
         if (at < n16) {
             kr[u] = __ldcs(ks + at);
             vr[u] = __ldcs(vs + at);
@@ -232,7 +275,7 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_copy_kernel(const Pool pl
     if (threadIdx.x == 32) pl.v_scale[to] = pl.v_scale[from];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        const int at = threadIdx.x + u * kThreads;
+        const int at = threadIdx.x + u * kCopyThreads;
         if (at < n16) {
             __stcs(kd + at, kr[u]);
             __stcs(vd + at, vr[u]);
@@ -251,9 +294,15 @@ int launched(const char* who)
 template <typename T, int D>
 int append_as(const Pool& pl, const Batch& bt, const void* k, const void* v, cudaStream_t st)
 {
+    const size_t smem = (size_t)kStages * kPage * D * sizeof(T);
+    static PerDeviceOnce once;
+    once.run([smem] {
+        cudaFuncSetAttribute(ssba_cache_append_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    });
     // every touched page takes a new token, and a run of n tokens touches at most n / 64 + 2 pages
-    const long long units = std::min<long long>(bt.T, bt.T / kPage + 2LL * bt.B);
-    ssba_cache_append_kernel<T, D><<<dim3((unsigned)units, pl.kv_heads), kThreads, 0, st>>>(
+    const long long units = std::min<long long>(bt.T, bt.T / kPage + 2LL * bt.B) * pl.kv_heads * 2;
+    const int fit = (int)std::min<size_t>(8, (size_t)200 * 1024 / (smem + 8192));  // CTAs of an SM
+    ssba_cache_append_kernel<T, D><<<(int)std::min<long long>(units, (long long)fit * device_sm_count()), kThreads, smem, st>>>(
         pl, bt, static_cast<const T*>(k), static_cast<const T*>(v));
     return launched("ssba_cache_append");
 }
@@ -274,7 +323,7 @@ int launch_cache_append(const cache::Pool& pl, const cache::Batch& bt, int head_
 int launch_cache_copy(const cache::Pool& pl, int head_dim, const int32_t* src, const int32_t* dst, int n,
                       cudaStream_t st)
 {
-    cache::ssba_cache_copy_kernel<<<dim3(n, pl.kv_heads), cache::kThreads, 0, st>>>(pl, head_dim, src, dst);
+    cache::ssba_cache_copy_kernel<<<dim3(n, pl.kv_heads), cache::kCopyThreads, 0, st>>>(pl, head_dim, src, dst);
     return cache::launched("ssba_cache_copy");
 }
 
