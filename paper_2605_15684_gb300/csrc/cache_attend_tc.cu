@@ -68,6 +68,19 @@ struct Params {
     uint64_t budget_ns;
 };
 
+// The rows of an item: tokens [row, row + n) of the batch, each with the heads of chunk hv.
+struct Rows {
+    int hv, row, n;
+
+    // Row r of the item: its row of the batch (-1: none) and head.
+    __device__ __forceinline__ int of(const Params& p, int r, int& head) const
+    {
+        const int i = r / p.gc, g = (hv % p.chunks) * p.gc + r - i * p.gc;
+        head = (hv / p.chunks) * p.G + g;
+        return g < p.G && i < n ? row + i : -1;
+    }
+};
+
 struct Maps {
     CUtensorMap k, v;
 };
@@ -107,7 +120,8 @@ struct __align__(1024) Smem {
     int first_b, ctas;
     long long first_at;
     uint32_t tmem_base;
-    int abort_flag, last;
+    Rows rows[2];          // of the items that are shared with other CTAs
+    int abort_flag, last[2], last_c0[2];
 };
 
 __device__ __forceinline__ float fast_exp2(float x)
@@ -200,9 +214,9 @@ struct Walk {
         if (w >= w1) return;
         if (kList) {
             tiles = (p.keep + 1) / 2;
-            const long long item = w / tiles;
+            const long long item = sm.total < INT_MAX ? (int)w / tiles : w / tiles;
             start = item * tiles;
-            t = (int)(item / heads);
+            t = (int)(sm.total < INT_MAX ? (int)item / heads : item / heads);
             hv = (int)(item - (long long)t * heads);
             t += max(0, min(__ldg(p.bt.cu), p.bt.T));
             locate();
@@ -212,7 +226,7 @@ struct Walk {
             const Blocks bl(s, p.tq);
             const long long one = max(bl.sum(), 1LL);
             long long at = sm.first_at;
-            hv = (int)min(at / one, (long long)heads - 1);
+            hv = (int)min(sm.total < INT_MAX ? (int)at / (int)one : at / one, (long long)heads - 1);
             at -= (long long)hv * one;
             int lo = 0, hi = bl.count - 1;  // the last block with before(t) <= at
             while (lo < hi) {
@@ -265,16 +279,12 @@ struct Walk {
         }
         share();
     }
-    // Row r of the item: its row of the batch (-1: none) and head.
-    __device__ __forceinline__ int row_of(int r, int& head) const
+    __device__ __forceinline__ Rows rows() const
     {
-        const int i = r / p.gc, g = (hv % p.chunks) * p.gc + r - i * p.gc;
-        head = (hv / p.chunks) * p.G + g;
-        if (g >= p.G) return -1;
-        if (kList) return i == 0 && b >= 0 ? t : -1;
-        const int k = t * p.tq + i;
-        return i < p.tq && k < s.n ? s.row + k : -1;
+        if (kList) return Rows{hv, t, b >= 0 ? 1 : 0};
+        return Rows{hv, s.row + t * p.tq, min(s.n - t * p.tq, p.tq)};
     }
+    __device__ __forceinline__ int row_of(int r, int& head) const { return rows().of(p, r, head); }
     __device__ __forceinline__ int limit(int row) const { return min(max(s.len - s.n + row - s.row + 1, 0), s.len); }
     // Label of the item's k-th page, or -1: no such page, or (flagged) a listed label that the row does not see.
     __device__ __forceinline__ int label(int k) const
@@ -371,18 +381,26 @@ __device__ void make_share(const Params& p, S& sm)
     __syncthreads();
 }
 
-// Joins the np parts of an item that begins in CTA c0, in order, and writes its rows: a softmax warp takes every
-// fourth row, two at a time, a lane four channels, with four parts' loads in flight.
-template <int R, int D, class W>
-__device__ __noinline__ void join(const Params& p, const W& it, int c0, int np, int quad, int lane)
+// The CTA whose share tile w lies in: the last c with W c / C <= w.
+template <class S>
+__device__ __forceinline__ int cta_of(long long w, const S& sm)
 {
-    constexpr int kAhead = 4;
+    if (sm.total < INT_MAX / kMaxGrid - 1) return (int)(((int)w + 1) * sm.ctas - 1) / (int)sm.total;
+    return (int)(((w + 1) * sm.ctas - 1) / sm.total);
+}
+
+// Joins the np parts of an item that begins in CTA c0, in order, and writes its rows: a softmax warp takes every
+// fourth row, two at a time, a lane four channels, with eight parts' loads in flight.
+template <int R, int D>
+__device__ __noinline__ void join(const Params& p, const Rows rows, int c0, int np, int quad, int lane)
+{
+    constexpr int kAhead = 8;
 #pragma unroll 1
     for (int r0 = quad; r0 < R; r0 += 8) {
         float m[2] = {-INFINITY, -INFINITY}, l[2] = {}, o[2][4] = {};
         int row[2], head[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) row[u] = it.row_of(r0 + 4 * u, head[u]);
+        for (int u = 0; u < 2; ++u) row[u] = rows.of(p, r0 + 4 * u, head[u]);
 #pragma unroll 1
         for (int k0 = 0; k0 < np; k0 += kAhead) {
             float2 ml[2][kAhead];
@@ -684,8 +702,11 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
             }
             pending = false;
         };
+        // items shared with other CTAs: one that began before the share, one that goes on behind it
+        long long start0 = 0, start1 = 0;
+        int tiles0 = 0, tiles1 = 0;
         // (the four warps meet in barriers, so they give up together)
-        for (; it.more() && !soft_any(*abortf != 0); it.next(), ++seg) {
+        for (; it.more() && !soft_any(*abortf != 0); ++seg) {
             const int st = seg & 1;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -853,21 +874,15 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
 #pragma unroll
                 for (int r = 0; r < R; ++r)
                     if (tok == r) reinterpret_cast<float2*>(part + R * D)[r] = make_float2(ref, l[r]);
-                __threadfence();
-                soft_sync();
-                const int c0 = (int)(((it.start + 1) * sm.ctas - 1) / sm.total);
-                const int c1 = (int)(((it.start + it.tiles) * sm.ctas - 1) / sm.total);
-                if (tok == 0) {
-                    const unsigned seen = atomicAdd(p.tickets + c0, 1u);
-                    sm.last = seen == (unsigned)(c1 - c0);
-                    if (sm.last) p.tickets[c0] = 0;
-                    __threadfence();
+                const int which = it.tb == 0;
+                if (which) {
+                    start1 = it.start;
+                    tiles1 = it.tiles;
+                } else {
+                    start0 = it.start;
+                    tiles0 = it.tiles;
                 }
-                soft_sync();
-                if (sm.last) {
-                    const Walk<kList> at = it;  // (a copy, so that the walk itself stays in registers)
-                    join<R, D>(p, at, c0, c1 - c0 + 1, quad, lane);
-                }
+                if (tok == 0) sm.rows[which] = it.rows();
             } else {
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
@@ -880,6 +895,31 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
                     }
                 }
             }
+            if (it.start + it.te >= it.w1) break;  // (the walk stays at its last item)
+            it.next();
+        }
+        // The items that are shared with other CTAs, counted off once all is written: a fence beside the loads of
+        // every CTA takes 10 us and more, in which this one would issue none (16 sequences of up to 8000 tokens:
+        // 43 us with a fence behind each item, 40 like this).
+        if (tiles0 + tiles1 > 0 && !soft_any(*abortf != 0)) {
+            if (tok < 2) {  // (everyone's stores lie before the barrier, and with it before the counting)
+                const long long start = tok ? start1 : start0;
+                const int tiles = tok ? tiles1 : tiles0;
+                int c0 = 0, np = 0;
+                if (tiles > 0) {
+                    c0 = cta_of(start, sm);
+                    np = cta_of(start + tiles - 1, sm) - c0 + 1;
+                    unsigned seen;
+                    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(seen) : "l"(p.tickets + c0) : "memory");
+                    if (seen == (unsigned)(np - 1)) p.tickets[c0] = 0;
+                    else np = 0;
+                }
+                sm.last_c0[tok] = c0;
+                sm.last[tok] = np;
+            }
+            soft_sync();
+            for (int i = 0; i < 2; ++i)
+                if (sm.last[i]) join<R, D>(p, sm.rows[i], sm.last_c0[i], sm.last[i], quad, lane);
         }
         dead = *abortf != 0;
     }
