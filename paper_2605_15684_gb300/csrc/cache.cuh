@@ -137,5 +137,8 @@ int launch_cache_attend_tc(const cache::Pool& pl, const cache::Batch& bt, int he
                            const int32_t* idx, const int32_t* cnt, int keep, void* O, float* lse, void* ws,
                            cudaStream_t st);
 size_t cache_attend_tc_workspace();
+int launch_cache_attend_rows(const cache::Pool& pl, const cache::Batch& bt, int head_dim, float scale, const void* q,
+                             void* O, float* lse, void* ws, cudaStream_t st);
+size_t cache_attend_rows_workspace();
 
 }  // namespace ssba

@@ -154,7 +154,8 @@ int ssba_cache_select(const ssba_cache_desc* desc, const ssba_cache* cache, cons
 size_t ssba_cache_attend_workspace_bytes(const ssba_cache_desc* desc)
 {
     if (check_cache_desc(desc, "ssba_cache_attend_workspace_bytes") != SSBA_OK) return 0;
-    return (std::max(cache_attend_simt_workspace(), cache_attend_tc_workspace()) + 255) & ~(size_t)255;
+    const size_t n = std::max(cache_attend_simt_workspace(), cache_attend_tc_workspace());
+    return (std::max(n, cache_attend_rows_workspace()) + 255) & ~(size_t)255;
 }
 
 int ssba_cache_attend(const ssba_cache_desc* desc, const ssba_cache* cache, const void* q, int32_t T,
@@ -188,8 +189,12 @@ int ssba_cache_attend(const ssba_cache_desc* desc, const ssba_cache* cache, cons
     const float scale = desc->softmax_scale > 0.f ? desc->softmax_scale : 1.0f / std::sqrt((float)desc->head_dim);
     const cache::Batch bt{table, lens, cu, B, width, T};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (desc->dtype == SSBA_BF16)
+    if (desc->dtype == SSBA_BF16) {
+        // rows that share a K/V head's tokens, on average over the batch's sequences
+        const long long rows = ((long long)T + B - 1) / B * (desc->heads / desc->kv_heads);
+        if (!idx && rows > 32) return launch_cache_attend_rows(p, bt, desc->head_dim, scale, q, O, lse, workspace, st);
         return launch_cache_attend_tc(p, bt, desc->head_dim, scale, q, idx, cnt, keep, O, lse, workspace, st);
+    }
     return launch_cache_attend_simt(p, bt, desc->head_dim, desc->dtype, scale, q, idx, cnt, keep, O, lse, workspace, st);
 }
 

@@ -31,59 +31,19 @@
 #include <cmath>
 #include <cstring>
 
-#include "cache.cuh"
-#include "ptx.cuh"
+#include "cache_items.cuh"
 
 namespace ssba {
 namespace cache {
 namespace {
 
-using namespace ptx;
-
-constexpr int kTile = 128;           // tokens of a tile: two pages
 constexpr int kThreads = 256;
 constexpr int kSoft = 128;           // softmax threads
 constexpr int kMeta = 32;            // pages of a meta chunk
 constexpr float kTop = 8.f;          // log2 of a tile's largest P: 2^8 < 448
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kNowhere = 1 << 30;    // token position of a page that is not there
 enum Role { kLoad = 0, kIssue = 1, kLoadQ = 2, kLoadMeta = 3 };
 
-constexpr int kMaxGrid = 608;        // CTAs of a launch at most (two an SM of up to 304)
-static_assert(kMaxGrid * sizeof(unsigned) <= SSBA_CACHE_TICKET_BYTES, "a counter a CTA");
 constexpr size_t kPartFloats = (size_t)16 * 130 * 2 * kMaxGrid;  // two parts a CTA of 16 rows (half as many CTAs of 32)
-
-struct Params {
-    Pool pl;
-    Batch bt;
-    const __nv_bfloat16* q;
-    const int32_t *idx, *cnt;  // null: all pages
-    int keep;
-    float scale_log2;
-    __nv_bfloat16* O;
-    float* lse;
-    float* parts;
-    unsigned* tickets;
-    int G, gc, chunks, tq;  // group size; heads and tokens of an item; chunks of a group
-    uint64_t budget_ns;
-};
-
-// The rows of an item: tokens [row, row + n) of the batch, each with the heads of chunk hv.
-struct Rows {
-    int hv, row, n;
-
-    // Row r of the item: its row of the batch (-1: none) and head.
-    __device__ __forceinline__ int of(const Params& p, int r, int& head) const
-    {
-        const int i = r / p.gc, g = (hv % p.chunks) * p.gc + r - i * p.gc;
-        head = (hv / p.chunks) * p.G + g;
-        return g < p.G && i < n ? row + i : -1;
-    }
-};
-
-struct Maps {
-    CUtensorMap k, v;
-};
 
 template <int R, int D>
 struct Cfg {
@@ -124,21 +84,6 @@ struct __align__(1024) Smem {
     int abort_flag, last[2], last_c0[2];
 };
 
-__device__ __forceinline__ float fast_exp2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-__device__ __forceinline__ bool wait_raw(uint32_t bar, uint32_t parity, uint64_t budget_ns)
-{
-    const uint64_t t0 = globaltimer_ns();
-    while (!mbar_try_wait(bar, parity))
-        if (globaltimer_ns() - t0 > budget_ns) return false;
-    return true;
-}
-
 __device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
 // Largest of the warp's values (NaN are passed over).
@@ -163,230 +108,6 @@ __device__ __forceinline__ bool soft_any(bool x)
         : "r"(x ? 1u : 0u)
         : "memory");
     return r != 0;
-}
-
-// Tiles of the row blocks of a sequence. Block t of tq tokens (tq a power of two up to 128) sees
-// a + (t + 1) tq tokens, a = len - n, the last one len; a block takes max(1, ceil(seen / 128)) tiles. With u =
-// ceil(a / tq) and m = 128 / tq that is max(1, ceil((u + t + 1) / m)), so sums over blocks have a closed form.
-struct Blocks {
-    int a, n, len, tq, count;
-
-    __device__ __forceinline__ Blocks(const Seq& s, int tq_) : a(s.len - s.n), n(s.n), len(s.len), tq(tq_)
-    {
-        count = (n + tq - 1) >> shift();
-    }
-    __device__ __forceinline__ int shift() const { return 31 - __clz(tq); }
-    __device__ __forceinline__ int tiles(int t) const
-    {
-        const int seen = t + 1 < count ? a + (t + 1) * tq : len;
-        return max(1, (seen + kTile - 1) / kTile);
-    }
-    static __device__ __forceinline__ long long upto(int k, int m)  // sum of max(1, ceil(j / m)), j = 1 .. k
-    {
-        if (k <= 0) return k;
-        const int d = k >> (31 - __clz(m)), r = k & (m - 1);  // m is a power of two
-        return (long long)m * d * (d + 1) / 2 + (long long)r * (d + 1);
-    }
-    __device__ __forceinline__ long long before(int t) const  // tiles of blocks 0 .. t - 1, t < count
-    {
-        const int u = (a + tq - 1) >> shift(), m = kTile >> shift();
-        return upto(u + t, m) - upto(u, m);
-    }
-    __device__ __forceinline__ long long sum() const { return count ? before(count - 1) + tiles(count - 1) : 0; }
-};
-
-// The items of a CTA's share, in order: sequence, K/V head (and chunk of its group), block of rows. With lists an
-// item is one row and K/V head, of equally many tiles for all.
-template <bool kList>
-struct Walk {
-    const Params& p;
-    long long w, w1;   // next tile of the share, its end
-    long long start;   // first tile of the item, in the batch's order
-    int heads;         // K/V heads times chunks
-    int b, hv, t;      // t: row block of the sequence, or the row with lists
-    Seq s;
-    int tiles, tb, te;  // tiles of the item; those of this CTA
-
-    template <class S>
-    __device__ __forceinline__ Walk(const Params& p_, const S& sm) : p(p_), w(sm.w0), w1(sm.w1)
-    {
-        heads = p.pl.kv_heads * p.chunks;
-        if (w >= w1) return;
-        if (kList) {
-            tiles = (p.keep + 1) / 2;
-            const long long item = sm.total < INT_MAX ? (int)w / tiles : w / tiles;
-            start = item * tiles;
-            t = (int)(sm.total < INT_MAX ? (int)item / heads : item / heads);
-            hv = (int)(item - (long long)t * heads);
-            t += max(0, min(__ldg(p.bt.cu), p.bt.T));
-            locate();
-        } else {
-            b = sm.first_b;
-            s = load_seq(p.bt, b, p.pl.status);
-            const Blocks bl(s, p.tq);
-            const long long one = max(bl.sum(), 1LL);
-            long long at = sm.first_at;
-            hv = (int)min(sm.total < INT_MAX ? (int)at / (int)one : at / one, (long long)heads - 1);
-            at -= (long long)hv * one;
-            int lo = 0, hi = bl.count - 1;  // the last block with before(t) <= at
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) / 2;
-                if (bl.before(mid) <= at) lo = mid;
-                else hi = mid - 1;
-            }
-            t = lo;
-            tiles = bl.tiles(t);
-            start = w - (at - bl.before(t));
-        }
-        share();
-    }
-    __device__ __forceinline__ void locate()  // (lists) the sequence of row t
-    {
-        b = find_seq(p.bt, t, threadIdx.x & 31);
-        s = b >= 0 ? load_seq(p.bt, b, p.pl.status) : Seq{0, 0, 0};
-    }
-    __device__ __forceinline__ void share()
-    {
-        tb = (int)(w - start);
-        te = (int)min((long long)tiles, tb + (w1 - w));
-    }
-    __device__ __forceinline__ bool more() const { return w < w1; }
-    __device__ __forceinline__ void next()
-    {
-        w = start + te;
-        if (w >= w1) return;
-        start += tiles;
-        if (kList) {
-            if (++hv == heads) {
-                hv = 0;
-                ++t;
-                locate();
-            }
-        } else {
-            Blocks bl(s, p.tq);
-            if (++t >= bl.count) {
-                t = 0;
-                if (++hv == heads) {
-                    hv = 0;
-                    do {
-                        ++b;
-                        s = load_seq(p.bt, min(b, p.bt.B - 1), p.pl.status);
-                    } while (s.n == 0 && b < p.bt.B - 1);
-                }
-                bl = Blocks(s, p.tq);
-            }
-            tiles = bl.tiles(t);
-        }
-        share();
-    }
-    __device__ __forceinline__ Rows rows() const
-    {
-        if (kList) return Rows{hv, t, b >= 0 ? 1 : 0};
-        return Rows{hv, s.row + t * p.tq, min(s.n - t * p.tq, p.tq)};
-    }
-    __device__ __forceinline__ int row_of(int r, int& head) const { return rows().of(p, r, head); }
-    __device__ __forceinline__ int limit(int row) const { return min(max(s.len - s.n + row - s.row + 1, 0), s.len); }
-    // Label of the item's k-th page, or -1: no such page, or (flagged) a listed label that the row does not see.
-    __device__ __forceinline__ int label(int k) const
-    {
-        if (!kList) return (long long)k * kPage < s.len ? k : -1;
-        if (b < 0) return -1;
-        const size_t at = (size_t)t * p.pl.kv_heads + hv / p.chunks;
-        int n = __ldg(p.cnt + at);
-        if (n < 0 || n > p.keep) flag(p.pl.status);
-        if (k >= min(n, p.keep)) return -1;
-        const int j = __ldg(p.idx + at * p.keep + k);
-        if (j >= 0 && (long long)j * kPage < limit(t)) return j;
-        flag(p.pl.status);
-        return -1;
-    }
-    __device__ __forceinline__ int page(int k, int& j) const
-    {
-        j = label(k);
-        if (j < 0) return -1;
-        return page_of(p.bt, p.pl, b, j);
-    }
-};
-
-// The CTA's share [w0, w1) of the batch's tiles and where it starts. All threads.
-template <bool kList, class S>
-__device__ void make_share(const Params& p, S& sm)
-{
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int heads = p.pl.kv_heads * p.chunks;
-    __shared__ long long wsum[kThreads / 32];
-    // tiles of thread tid's sequence of those from b0 on, all heads: sum over the CTA, or that in front of the thread
-    auto scan = [&](int b0, long long mine, long long& front) {
-        long long inc = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long x = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += x;
-        }
-        __syncthreads();
-        if (lane == 31) wsum[warp] = inc;
-        __syncthreads();
-        long long sum = 0;
-        front = inc - mine;
-#pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w) {
-            if (w < warp) front += wsum[w];
-            sum += wsum[w];
-        }
-        return sum;
-    };
-    auto tiles_of = [&](int b) {
-        return b < p.bt.B ? Blocks(load_seq(p.bt, b, p.pl.status), p.tq).sum() * heads : 0LL;
-    };
-    long long W = 0, mine = 0, front = 0;
-    if (kList) {
-        const int r0 = max(0, min(__ldg(p.bt.cu), p.bt.T)), r1 = max(r0, min(__ldg(p.bt.cu + p.bt.B), p.bt.T));
-        W = (long long)(r1 - r0) * heads * ((p.keep + 1) / 2);
-    } else {
-        for (int b0 = 0; b0 < p.bt.B; b0 += kThreads) {
-            mine = tiles_of(b0 + tid);
-            W += scan(b0, mine, front);
-        }
-    }
-    const int C = (int)min((long long)gridDim.x, max(W, 1LL)), c = blockIdx.x;
-    // (32-bit division where it does)
-    const bool small = W < INT_MAX / kMaxGrid;
-    const long long w0 = c >= C ? W : small ? (int)W * c / C : W * c / C;
-    const long long w1 = c >= C ? W : small ? (int)W * (c + 1) / C : W * (c + 1) / C;
-    if (tid == 0) {
-        sm.w0 = w0;
-        sm.w1 = w1;
-        sm.total = W;
-        sm.ctas = C;
-        sm.first_b = 0;
-        sm.first_at = 0;
-    }
-    __syncthreads();
-    if (!kList && w0 < w1) {
-        long long base = 0;  // tiles of the sequences in front, all heads
-        for (int b0 = 0; b0 < p.bt.B && base <= w0; b0 += kThreads) {
-            long long sum = W;
-            if (p.bt.B > kThreads) {  // else the sum's own scan
-                mine = tiles_of(b0 + tid);
-                sum = scan(b0, mine, front);
-            }
-            const long long at = base + front;
-            if (w0 >= at && w0 < at + mine) {
-                sm.first_b = b0 + tid;
-                sm.first_at = w0 - at;
-            }
-            base += sum;
-        }
-    }
-    __syncthreads();
-}
-
-// The CTA whose share tile w lies in: the last c with W c / C <= w.
-template <class S>
-__device__ __forceinline__ int cta_of(long long w, const S& sm)
-{
-    if (sm.total < INT_MAX / kMaxGrid - 1) return (int)(((int)w + 1) * sm.ctas - 1) / (int)sm.total;
-    return (int)(((w + 1) * sm.ctas - 1) / sm.total);
 }
 
 // Joins the np parts of an item that begins in CTA c0, in order, and writes its rows: a softmax warp takes every
@@ -499,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
     // everything above reads no input (programmatic dependent launch: it may run beside the last grid's end)
     grid_dep_wait();
     grid_dep_launch();
-    make_share<kList>(p, sm);  // ends in a barrier
+    make_share<kList, kThreads>(p, sm);  // ends in a barrier
     tc_fence_after();
     const uint32_t tbase = sm.tmem_base;
     volatile int* abortf = &sm.abort_flag;
@@ -940,20 +661,6 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
     if (warp == kIssue) tmem_dealloc(tbase, C::kTmemCols);
 }
 
-// [pages * kv_heads][64][D] bytes, a box a page and head.
-bool encode_page_map(CUtensorMap* m, const void* base, long long tiles, int D)
-{
-    EncodeTiledFn fn = tensor_map_encoder();
-    if (!fn) return false;
-    cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)kPage, (cuuint64_t)tiles};
-    cuuint64_t strides[2] = {(cuuint64_t)D, (cuuint64_t)kPage * D};
-    cuuint32_t box[3] = {(cuuint32_t)D, (cuuint32_t)kPage, 1};
-    cuuint32_t es[3] = {1, 1, 1};
-    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, es,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int R, int D, bool kList>
 int launch(const Maps& maps, const Params& p, cudaStream_t st)
 {
@@ -1003,7 +710,8 @@ int launch_cache_attend_tc(const cache::Pool& pl, const cache::Batch& bt, int he
     Maps maps;
     memset(&maps, 0, sizeof(maps));
     const long long tiles = (long long)pl.pages * pl.kv_heads;
-    if (!encode_page_map(&maps.k, pl.K, tiles, head_dim) || !encode_page_map(&maps.v, pl.V, tiles, head_dim)) {
+    const CUtensorMapSwizzle swizzle = head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
+    if (!encode_page_map(&maps.k, pl.K, tiles, head_dim, swizzle) || !encode_page_map(&maps.v, pl.V, tiles, head_dim, swizzle)) {
         set_error("ssba_cache_attend: cuTensorMapEncodeTiled failed");
         return SSBA_ERR_CUDA;
     }
