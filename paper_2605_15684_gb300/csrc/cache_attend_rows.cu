@@ -12,11 +12,11 @@
 // power of two; their 8 bits of significand are exact in fp16 down to 2^-25 of the row's largest. P is rounded to fp16's
 // 11 bits; m is 8 below the largest exponent, so P's smallest step is 2^-32 of the largest weight.
 //
-// One CTA an SM, 12 warps: a producer (TMA of the pages' bytes), an issuer, two converters (a page each: bytes to
-// fp16 in the swizzled layout of the products), and a softmax warpgroup for each row tile (a thread is a row). P
-// overwrites the upper half of its S, so of one row tile PV_g comes before QK_{g + 1}; while one row tile
-// is with the tensor cores the other is with its softmax. Against a reference maximum that is raised only
-// where a tile's sum passes 2^14 (O is then rescaled in tensor memory), as in the other kernels of this library.
+// One CTA an SM, 16 warps: a producer (TMA of the pages' bytes), an issuer, four converters (half a page each: bytes
+// to fp16 in the swizzled layout of the products), and a softmax warpgroup for each row tile (a thread is a row).
+// P overwrites the lower half of its S, so of one row tile PV_g comes before QK_{g + 1}; while one row tile
+// is with the tensor cores the other is with its softmax. A tile's maximum is taken first, but the row's reference is
+// raised (and O rescaled in tensor memory) only where P would pass 2^14.
 // Work is shared out and joined as in cache_attend_tc.cu.
 #include <algorithm>
 #include <climits>
@@ -29,17 +29,28 @@ namespace ssba {
 namespace cache {
 namespace {
 
-constexpr int kThreads = 384;
+constexpr int kThreads = 512;
 constexpr int kRowTile = 128;
 constexpr int kItemRows = 2 * kRowTile;
 constexpr int kCv = 3, kRaw = 3, kMetas = 8;
 constexpr float kTop = 8.f;         // log2 of the largest P against a new reference
-constexpr float kMost = 16384.f;    // row sum of a tile above which the reference is raised (fp16 ends at 65504)
+constexpr float kMost = 14.f;       // log2 of the largest P that is let stand (fp16 ends at 65504)
+constexpr int kConverters = 4;
 constexpr float kSpan = 100.f;      // log2 of V scales, relative to the first page's
-enum Role { kLoad = 0, kIssue = 1, kConvert = 2, kSoftmax = 4 };
+enum Role { kLoad = 0, kIssue = 1, kConvert = 2, kItems = 6, kSoftmax = 8 };
 constexpr uint32_t kTmemCols = 512;
 
 constexpr uint32_t idesc_f16_f32(int M, int N, bool b_mn_major) { return idesc_e4m3_f32(M, N, false, b_mn_major); }
+
+constexpr int kItemRing = 4;
+
+// An item's share as the softmax warps get it, which have no registers for the walk.
+struct Item {
+    Rows rows;
+    Seq s;
+    int tb, te, tiles, two;
+    long long start;
+};
 
 struct Meta {
     float ks, lv, inv;  // K scale; log2 of the V scale (relative); 2^-lv
@@ -51,8 +62,11 @@ struct __align__(1024) Smem {
     uint8_t q[2][D / 64][kRowTile][128];   // fp16, 64 channels a 128-byte row, 128-byte swizzle
     uint8_t cv[kCv][D / 64][kTile][128];
     uint8_t raw[kRaw][kTile * D];
-    int nan_at[2][2][D];  // by item parity and converter: first token whose V is NaN, of those that not every row sees
-    int nan_any[2][2];
+    // by item parity and converter: first token whose V is NaN, of those that not every row sees
+    int nan_at[2][kConverters][D];
+    int nan_any[2][kConverters];
+    float qf[2][kRowTile];  // scale of a row's scores
+    float first_lv[2];      // by item parity: log2 of the V scale that the item's are relative to
     Meta meta[kMetas][2];
     uint64_t raw_full[kRaw], raw_empty[kRaw], cv_full[kCv], cv_empty[kCv], m_full[kMetas];
     uint64_t q_full[2], s_full[2], p_full[2], o_full[2], n_full[2], n_empty[2], drain;
@@ -60,8 +74,13 @@ struct __align__(1024) Smem {
     int first_b, ctas;
     long long first_at;
     uint32_t tmem_base;
+    Item item[kItemRing];  // te = 0: no more
+    uint64_t i_full[kItemRing], i_empty[kItemRing];
+    // of the items that are shared with other CTAs: one that began before the share, one that goes on behind it
     Rows rows[2];
     float base[2];
+    long long start[2];
+    int tiles[2];
     int abort_flag, last[2], last_c0[2];
 };
 
@@ -94,62 +113,66 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi)
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// log2 of the V scale that an item's P is relative to: its sequence's first page's.
-template <class W>
-__device__ __forceinline__ float base_of(const Params& p, const W& it)
-{
-    int j;
-    const int page = it.page(0, j);
-    const float vs = page >= 0 ? __ldg(p.pl.v_scale + (size_t)page * p.pl.kv_heads + it.hv / p.chunks) : 0.f;
-    return vs > 0.f && vs < INFINITY ? log2f(vs) : 0.f;
-}
-
-// Joins the np parts of an item that begins in CTA c0, in order, and writes its rows: a softmax warp takes every
-// eighth row, a lane D / 32 channels, with eight parts' loads in flight.
+// Joins the np parts of an item that begins in CTA c0, in order, and writes its rows: a warp takes every sixteenth
+// row, four at a time, a lane four channels, with two parts' loads in flight.
 template <int D>
 __device__ __noinline__ void join(const Params& p, const Rows rows, float base, int c0, int np, int w, int lane)
 {
-    constexpr int kAhead = 8, kE = D / 32;
+    constexpr int kAhead = 2, kR = 4, kWarps = kThreads / 32;
     const size_t size = (size_t)kItemRows * (D + 2);
+    const float scale = exp2f(base);
 #pragma unroll 1
-    for (int r = w; r < kItemRows; r += 8) {
-        int head;
-        const int row = rows.of(p, r, head);
-        if (row < 0) continue;
-        float m = -INFINITY, l = 0.f, o[kE] = {};
+    for (int r0 = w; r0 < min(kItemRows, rows.n * p.gc); r0 += kR * kWarps) {
+        float m[kR], l[kR];
+        float4 o[kR];
+#pragma unroll
+        for (int u = 0; u < kR; ++u) {
+            m[u] = -INFINITY;
+            l[u] = 0.f;
+            o[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
 #pragma unroll 1
         for (int k0 = 0; k0 < np; k0 += kAhead) {
-            float2 ml[kAhead];
-            float v[kAhead][kE];
+            float2 ml[kAhead][kR];
+            float4 v[kAhead][kR];
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
+                // part 0 is slot 1 of CTA c0, part k slot 0 of CTA c0 + k
                 const float* at = p.parts + ((size_t)(c0 + k0 + k) * 2 + (k0 + k == 0)) * size;
-                const bool real = k0 + k < np;
-                ml[k] = real ? __ldcg(reinterpret_cast<const float2*>(at + kItemRows * D) + r) : make_float2(-INFINITY, 0.f);
 #pragma unroll
-                for (int e = 0; e < kE; ++e) v[k][e] = real ? __ldcg(at + (size_t)r * D + e * 32 + lane) : 0.f;
+                for (int u = 0; u < kR; ++u) {
+                    const int r = r0 + u * kWarps;
+                    const bool real = k0 + k < np && r < rows.n * p.gc;
+                    ml[k][u] = real ? __ldcg(reinterpret_cast<const float2*>(at + kItemRows * D) + r) : make_float2(-INFINITY, 0.f);
+                    v[k][u] = real && lane < D / 4 ? __ldcg(reinterpret_cast<const float4*>(at + (size_t)r * D) + lane)
+                                                   : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
             }
-            float top = m;
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) top = fmaxf(top, ml[k].x);
-            const float at0 = top == -INFINITY ? 0.f : top, f = fast_exp2(m - at0);
-            m = top;
-            l *= f;
-#pragma unroll
-            for (int e = 0; e < kE; ++e) o[e] *= f;
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                const float fk = fast_exp2(ml[k].x - at0);
-                l = fmaf(ml[k].y, fk, l);
-#pragma unroll
-                for (int e = 0; e < kE; ++e) o[e] = fmaf(v[k][e], fk, o[e]);
+            for (int u = 0; u < kR; ++u) {
+                const float top = fmaxf(fmaxf(m[u], ml[0][u].x), ml[1][u].x), at0 = top == -INFINITY ? 0.f : top;
+                const float f = fast_exp2(m[u] - at0), f0 = fast_exp2(ml[0][u].x - at0), f1 = fast_exp2(ml[1][u].x - at0);
+                m[u] = top;
+                l[u] = fmaf(ml[1][u].y, f1, fmaf(ml[0][u].y, f0, l[u] * f));
+                o[u].x = fmaf(v[1][u].x, f1, fmaf(v[0][u].x, f0, o[u].x * f));
+                o[u].y = fmaf(v[1][u].y, f1, fmaf(v[0][u].y, f0, o[u].y * f));
+                o[u].z = fmaf(v[1][u].z, f1, fmaf(v[0][u].z, f0, o[u].z * f));
+                o[u].w = fmaf(v[1][u].w, f1, fmaf(v[0][u].w, f0, o[u].w * f));
             }
         }
-        const size_t at = (size_t)row * p.pl.heads + head;
-        const float inv = l != 0.f ? exp2f(base) / l : 0.f;
 #pragma unroll
-        for (int e = 0; e < kE; ++e) p.O[at * D + e * 32 + lane] = __float2bfloat16_rn(o[e] * inv);
-        if (lane == 0) p.lse[at] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+        for (int u = 0; u < kR; ++u) {
+            int head;
+            const int row = rows.of(p, r0 + u * kWarps, head);
+            if (row < 0) continue;
+            const size_t at = (size_t)row * p.pl.heads + head;
+            const float inv = l[u] != 0.f ? scale / l[u] : 0.f;
+            if (lane < D / 4) {
+                const __nv_bfloat162 a = __floats2bfloat162_rn(o[u].x * inv, o[u].y * inv), b = __floats2bfloat162_rn(o[u].z * inv, o[u].w * inv);
+                *reinterpret_cast<uint2*>(p.O + at * D + lane * 4) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+            }
+            if (lane == 0) p.lse[at] = l[u] != 0.f ? (m[u] + log2f(l[u])) * kLn2 : -INFINITY;
+        }
     }
 }
 
@@ -161,13 +184,17 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
     Smem<D>& sm = *reinterpret_cast<Smem<D>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        sm.abort_flag = 0;
+        sm.abort_flag = sm.last[0] = sm.last[1] = sm.tiles[0] = sm.tiles[1] = 0;
+        for (int i = 0; i < kItemRing; ++i) {
+            mbar_init(smem_u32(&sm.i_full[i]), 1);
+            mbar_init(smem_u32(&sm.i_empty[i]), 8);
+        }
         for (int i = 0; i < kRaw; ++i) {
             mbar_init(smem_u32(&sm.raw_full[i]), 1);
-            mbar_init(smem_u32(&sm.raw_empty[i]), 2);
+            mbar_init(smem_u32(&sm.raw_empty[i]), kConverters);
         }
         for (int i = 0; i < kCv; ++i) {
-            mbar_init(smem_u32(&sm.cv_full[i]), 2);
+            mbar_init(smem_u32(&sm.cv_full[i]), kConverters);
             mbar_init(smem_u32(&sm.cv_empty[i]), 1);
         }
         for (int i = 0; i < kMetas; ++i) mbar_init(smem_u32(&sm.m_full[i]), 2);
@@ -176,7 +203,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
             mbar_init(smem_u32(&sm.s_full[i]), 1);
             mbar_init(smem_u32(&sm.p_full[i]), 4);
             mbar_init(smem_u32(&sm.o_full[i]), 1);
-            mbar_init(smem_u32(&sm.n_full[i]), 2);
+            mbar_init(smem_u32(&sm.n_full[i]), kConverters);
             mbar_init(smem_u32(&sm.n_empty[i]), 8);
         }
         mbar_init(smem_u32(&sm.drain), 1);
@@ -203,12 +230,12 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
     const uint32_t cfull0 = smem_u32(&sm.cv_full[0]), cempty0 = smem_u32(&sm.cv_empty[0]);
     bool dead = false;
     uint32_t loads = 0;  // of the producer
-    Walk<false> it(p, sm);
     // an item of up to 128 rows has no second row tile
     auto both = [&](const Walk<false>& w) { return w.rows().n * p.gc > kRowTile; };
 
     if (warp == kLoad) {
         // ------------------------------------------------------------ producer: K_0, V_0, K_1, ...
+        Walk<false> it(p, sm);
         for (; it.more() && !dead; it.next()) {
             const int h = it.hv / p.chunks;
             for (int c0 = 2 * it.tb; c0 < 2 * it.te && !dead; c0 += 32) {  // 32 pages at a time
@@ -240,6 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
         __syncwarp();
     } else if (warp == kIssue) {
         // ------------------------------------------------------------ issuer
+        Walk<false> it(p, sm);
         uint32_t cnt[2] = {0, 0}, qs[2] = {0, 0};  // tiles, items of each row tile
         bool pend[2] = {false, false}, p_first[2] = {}, p_last[2] = {};  // PV still to come: first, last tile of its item's share
         uint32_t vslot = 0;
@@ -252,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 const uint64_t b = sdesc_sw128(smem_u32(&sm.cv[vslot % kCv][0][0][0]), kTile * 128, 1024);
 #pragma unroll
                 for (int k = 0; k < kTile / 16; ++k)
-                    mma_ts(tbase + 256 + u * D, tbase + u * 128 + 64 + k * 8, b + (uint64_t)(k * 128),
+                    mma_ts(tbase + 256 + u * D, tbase + u * 128 + k * 8, b + (uint64_t)(k * 128),
                            idesc_f16_f32(128, D, true), (!p_first[u] || k > 0) ? 1u : 0u);
                 if (p_last[u]) mma_commit(smem_u32(&sm.o_full[u]));
                 if (u == 1 || !pend[1]) mma_commit(cempty0 + 8 * (vslot % kCv));
@@ -299,29 +327,59 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 if (pend[u]) pv(u);
         }
         dead = *abortf != 0;
+    } else if (warp >= kItems && warp < kSoftmax) {
+        // ------------------------------------------------------------ items for the softmax warps
+        if (warp == kItems) {
+            Walk<false> it(p, sm);
+            for (int seg = 0;; ++seg) {
+                const int k = seg % kItemRing;
+                wait_phase(smem_u32(&sm.i_empty[k]), ((seg / kItemRing) & 1) ^ 1, abort_at, p.budget_ns);
+                const bool more = it.more();
+                if (lane == 0) {
+                    sm.item[k].te = 0;
+                    if (more) sm.item[k] = Item{it.rows(), it.s, it.tb, it.te, it.tiles, both(it) ? 1 : 0, it.start};
+                    mbar_arrive(smem_u32(&sm.i_full[k]));
+                }
+                if (!more) break;
+                it.next();
+            }
+        }
+        dead = *abortf != 0;
     } else if (warp < kSoftmax) {
-        // ------------------------------------------------------------ converters: page `w` of every tile
-        constexpr int kLanes = D / 16, kRows = 32 / kLanes;  // lanes of a row (16 bytes each), rows at a time
-        const int w = warp - kConvert, c = lane % kLanes;
+        // ------------------------------------------------------------ converters: half a page of every tile
+        constexpr int kLanes = D / 16, kRows = 32 / kLanes, kIts = 32 / kRows;  // lanes of a row (16 bytes each), rows at a time
+        const int w = warp - kConvert, c = lane % kLanes, row0 = w * 32 + lane / kLanes;
         uint32_t use = 0, g = 0;
         int seg = 0;
+        Walk<false> it(p, sm);
         for (; it.more(); it.next(), ++seg) {
             const int h = it.hv / p.chunks;
             const Rows rows = it.rows();
             const int lo_lim = it.limit(rows.row), hi_lim = it.limit(rows.row + max(rows.n, 1) - 1);
-            const float base = base_of(p, it);
-            wait_phase(smem_u32(&sm.n_empty[seg & 1]), ((seg >> 1) & 1) ^ 1, abort_at, p.budget_ns);
-            for (int i = lane; i < D; i += 32) sm.nan_at[seg & 1][w][i] = INT_MAX;
-            if (lane == 0) sm.nan_any[seg & 1][w] = 0;
-            __syncwarp();
+            float base = 0.f;
             for (int c0 = it.tb; c0 < it.te; c0 += 32) {  // 32 tiles' pages at a time
-                int j, page = -1;
-                if (c0 + lane < it.te) page = it.page(2 * (c0 + lane) + w, j);
-                float my_ks = 0.f, my_lv = 0.f;
+                int j, j0, page = -1;
+                const int page0 = it.page(0, j0);
+                if (c0 + lane < it.te) page = it.page(2 * (c0 + lane) + w / 2, j);
+                float my_ks = 0.f, my_lv = 0.f, vs = 0.f;
+                const float vs0 = page0 >= 0 ? __ldg(p.pl.v_scale + (size_t)page0 * p.pl.kv_heads + h) : 0.f;
                 if (page >= 0) {
                     const size_t unit = (size_t)page * p.pl.kv_heads + h;
                     my_ks = __ldg(p.pl.k_scale + unit);
-                    const float vs = __ldg(p.pl.v_scale + unit);
+                    vs = __ldg(p.pl.v_scale + unit);
+                }
+                if (c0 == it.tb) {
+                    // V scales are taken relative to the sequence's first page's
+                    base = vs0 > 0.f && vs0 < INFINITY ? log2f(vs0) : 0.f;
+                    wait_phase(smem_u32(&sm.n_empty[seg & 1]), ((seg >> 1) & 1) ^ 1, abort_at, p.budget_ns);
+                    for (int i = lane; i < D; i += 32) sm.nan_at[seg & 1][w][i] = INT_MAX;
+                    if (lane == 0) {
+                        sm.nan_any[seg & 1][w] = 0;
+                        sm.first_lv[seg & 1] = base;
+                    }
+                    __syncwarp();
+                }
+                if (page >= 0) {
                     my_lv = vs > 0.f ? fminf(fmaxf(log2f(vs) - base, -kSpan), kSpan) : isnan(vs) ? vs : 0.f;
                 }
                 const int my_pos = page >= 0 ? j * kPage : kNowhere;
@@ -329,55 +387,58 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 for (int i = 0; i < n; ++i, ++g) {
                     const int pos = __shfl_sync(0xffffffffu, my_pos, i);
                     const float ks = __shfl_sync(0xffffffffu, my_ks, i), lv = __shfl_sync(0xffffffffu, my_lv, i);
-#pragma unroll
+#pragma unroll 1
                     for (int v = 0; v < 2; ++v, ++use) {
                         const uint32_t rs = use % kRaw, cs = use % kCv;
                         wait_phase(rfull0 + 8 * rs, (use / kRaw) & 1, abort_at, p.budget_ns);
-                        wait_phase(cempty0 + 8 * cs, ((use / kCv) & 1) ^ 1, abort_at, p.budget_ns);
-                        const uint8_t* from = &sm.raw[rs][w * kPage * D];
-                        if (pos != kNowhere || v) {
-#pragma unroll 4
-                            for (int r0 = 0; r0 < kPage; r0 += kRows) {
-                                const int r = r0 + lane / kLanes, row = w * kPage + r;
-                                uint4 x = *reinterpret_cast<const uint4*>(from + r * D + c * 16);
-                                if (v && pos + r >= lo_lim) {
-                                    // tokens that no row sees: their V is whatever the page holds, and 0 * NaN would
-                                    // reach every row; tokens that some rows see: a NaN is taken out and kept for those
-                                    if (pos + r >= hi_lim) {
-                                        x = make_uint4(0, 0, 0, 0);
-                                    } else {
-                                        uint32_t word[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                                        for (int k = 0; k < 4; ++k) {
-                                            const uint32_t m = word[k] & 0x7f7f7f7fu;
-                                            if (((m + 0x01010101u) & 0x80808080u) == 0) continue;  // no byte of 0x7f
-                                            for (int e = 0; e < 4; ++e)
-                                                if (((word[k] >> (8 * e)) & 0x7f) == 0x7f) {
-                                                    atomicMin(&sm.nan_at[seg & 1][w][c * 16 + k * 4 + e], pos + r);
-                                                    sm.nan_any[seg & 1][w] = 1;
-                                                    word[k] &= ~(0xffu << (8 * e));
-                                                }
-                                        }
-                                        x = make_uint4(word[0], word[1], word[2], word[3]);
+                        const int first = pos + (w & 1) * 32;  // token of the half page's first row
+                        if (v && first + 31 >= lo_lim) {
+                            // tokens that no row sees: their V is whatever the page holds, and 0 * NaN would reach
+                            // every row; tokens that some rows see: a NaN is taken out and kept for those rows
+#pragma unroll 1
+                            for (int k = 0; k < kIts; ++k) {
+                                uint32_t* word = reinterpret_cast<uint32_t*>(&sm.raw[rs][(row0 + k * kRows) * D + c * 16]);
+                                const int at = first + lane / kLanes + k * kRows;
+#pragma unroll 1
+                                for (int m = 0; m < 4 && at >= lo_lim; ++m) {
+                                    uint32_t x = at >= hi_lim ? 0u : word[m];
+                                    if ((((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0) {  // a byte of 0x7f
+                                        for (int e = 0; e < 4; ++e)
+                                            if (((x >> (8 * e)) & 0x7f) == 0x7f) {
+                                                atomicMin(&sm.nan_at[seg & 1][w][c * 16 + m * 4 + e], at);
+                                                sm.nan_any[seg & 1][w] = 1;
+                                                x &= ~(0xffu << (8 * e));
+                                            }
                                     }
+                                    word[m] = x;
                                 }
-                                const uint4 a = make_uint4(half2_of(x.x & 0xffff), half2_of(x.x >> 16), half2_of(x.y & 0xffff), half2_of(x.y >> 16));
-                                const uint4 b = make_uint4(half2_of(x.z & 0xffff), half2_of(x.z >> 16), half2_of(x.w & 0xffff), half2_of(x.w >> 16));
-                                uint8_t* to = &sm.cv[cs][c / 4][row][0];
-                                const int k = (c % 4) * 2;
-                                // lanes of the second 64 channels write their second half first: no bank conflicts
-                                const bool turn = c / 4;
-                                *reinterpret_cast<uint4*>(to + ((k + turn) ^ (row & 7)) * 16) = turn ? b : a;
-                                *reinterpret_cast<uint4*>(to + ((k + !turn) ^ (row & 7)) * 16) = turn ? a : b;
                             }
                         }
-                        if (!v && lane == 0) sm.meta[g % kMetas][w] = Meta{ks, lv, exp2f(-lv), pos};
+                        uint4 x[kIts];
+#pragma unroll
+                        for (int k = 0; k < kIts; ++k)
+                            x[k] = *reinterpret_cast<const uint4*>(&sm.raw[rs][(row0 + k * kRows) * D + c * 16]);
+                        wait_phase(cempty0 + 8 * cs, ((use / kCv) & 1) ^ 1, abort_at, p.budget_ns);
+#pragma unroll
+                        for (int k = 0; k < kIts; ++k) {
+                            const int row = row0 + k * kRows;
+                            const uint4 a = make_uint4(half2_of(x[k].x & 0xffff), half2_of(x[k].x >> 16), half2_of(x[k].y & 0xffff), half2_of(x[k].y >> 16));
+                            const uint4 b = make_uint4(half2_of(x[k].z & 0xffff), half2_of(x[k].z >> 16), half2_of(x[k].w & 0xffff), half2_of(x[k].w >> 16));
+                            uint8_t* to = &sm.cv[cs][c / 4][row][0];
+                            const int q = (c % 4) * 2;
+                            // lanes of the second 64 channels write their second half first: no bank conflicts
+                            const bool turn = c / 4;
+                            *reinterpret_cast<uint4*>(to + ((q + turn) ^ (row & 7)) * 16) = turn ? b : a;
+                            *reinterpret_cast<uint4*>(to + ((q + !turn) ^ (row & 7)) * 16) = turn ? a : b;
+                        }
+                        const bool meta = !v && (w & 1) == 0 && lane == 0;
+                        if (meta) sm.meta[g % kMetas][w / 2] = Meta{ks, lv, exp2f(-lv), pos};
                         fence_proxy_async_smem();
                         __syncwarp();
                         if (lane == 0) {
                             mbar_arrive(rempty0 + 8 * rs);
                             mbar_arrive(cfull0 + 8 * cs);
-                            if (!v) mbar_arrive(smem_u32(&sm.m_full[g % kMetas]));
+                            if (meta) mbar_arrive(smem_u32(&sm.m_full[g % kMetas]));
                         }
                     }
                 }
@@ -389,179 +450,192 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
         // ------------------------------------------------------------ softmax and output: a thread is a row
         const int u = (warp - kSoftmax) / 4, quad = warp & 3, r = quad * 32 + lane;
         const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
-        const uint32_t scol = tbase + u * 128 + lanes, pcol = scol + 64, ocol = tbase + 256 + u * D + lanes;
-        long long start0 = 0, start1 = 0;
-        int tiles0 = 0, tiles1 = 0;
+        const uint32_t scol = tbase + u * 128 + lanes, ocol = tbase + 256 + u * D + lanes;
         uint32_t cnt = 0, items = 0, g = 0;  // tiles and items of this row tile; tiles of the CTA
         int seg = 0;
-        // the row's query to shared memory; its row of the batch, head, tokens it sees and factor of scores
-        int row = -1, head = 0, lim = 0;
-        float qf = 0.f, base = 0.f;
-        auto load_q = [&](const Walk<false>& w) {
-            base = base_of(p, w);
-            row = w.rows().of(p, u * kRowTile + r, head);
-            lim = row >= 0 ? w.limit(row) : 0;
-            uint4 in[D / 8];
-            float amax = 0.f;
-#pragma unroll
-            for (int c = 0; c < D / 8; ++c)
-                in[c] = row >= 0 ? __ldg(reinterpret_cast<const uint4*>(p.q + ((size_t)row * p.pl.heads + head) * D) + c)
-                                 : make_uint4(0, 0, 0, 0);
-#pragma unroll
-            for (int c = 0; c < D / 8; ++c) {
-                const uint32_t x[4] = {in[c].x, in[c].y, in[c].z, in[c].w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float a = fabsf(__uint_as_float(x[e] << 16)), b = fabsf(__uint_as_float(x[e] & 0xffff0000u));
-                    if (a < INFINITY) amax = fmaxf(amax, a);
-                    if (b < INFINITY) amax = fmaxf(amax, b);
-                }
+        int lim = 0;     // tokens that the thread's row sees
+        float qf = 0.f;  // scale of its scores
+        auto limit = [&](const Item& w, int row) {
+            return row >= 0 ? min(max(w.s.len - w.s.n + row - w.s.row + 1, 0), w.s.len) : 0;
+        };
+        // the warp's 32 rows of Q to shared memory
+        // (small loops: code that runs once an item is read from memory, and unrolled sixteen times it took 20 us)
+        auto load_q = [&](const Item& w) {
+            constexpr int kLanes = D / 8, kRows = 32 / kLanes;  // lanes of a row (8 values each), rows at a time
+            const int c = lane % kLanes;
+            const Rows rows = w.rows;
+            auto at = [&](int k) { return quad * 32 + k * kRows + lane / kLanes; };
+            auto to = [&](int x) { return &sm.q[u][c / 8][x][((c % 8) ^ (x & 7)) * 16]; };
+#pragma unroll 2
+            for (int k = 0; k < 32 / kRows; ++k) {  // as it is, to where it will be
+                int hd;
+                const int rr = rows.of(p, u * kRowTile + at(k), hd);
+                const __nv_bfloat16* src = p.q + ((size_t)max(rr, 0) * p.pl.heads + (rr >= 0 ? hd : 0)) * D + c * 8;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to(at(k)))), "l"(src), "r"(rr >= 0 ? 16 : 0)
+                             : "memory");
             }
-            const float scale = scale_for(amax), inv = scale > 0.f ? 1.f / scale : 1.f;
-            qf = scale * p.scale_log2;
+            asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll 1
+            for (int k = 0; k < 32 / kRows; ++k) {
+                uint4* mine = reinterpret_cast<uint4*>(to(at(k)));
+                const uint4 in = *mine;
+                const uint32_t x[4] = {in.x, in.y, in.z, in.w};
+                float f[8], amax = 0.f;
 #pragma unroll
-            for (int c = 0; c < D / 8; ++c) {
-                const uint32_t x[4] = {in[c].x, in[c].y, in[c].z, in[c].w};
+                for (int e = 0; e < 8; ++e) {
+                    f[e] = __uint_as_float(e & 1 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16);
+                    const float a = fabsf(f[e]);
+                    if (a < INFINITY) amax = fmaxf(amax, a);
+                }
+#pragma unroll
+                for (int o = kLanes / 2; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+                const float scale = scale_for(amax), inv = scale > 0.f ? 1.f / scale : 1.f;
                 uint32_t y[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    // an infinity makes its row's scores NaN, as it would a softmax's
-                    const float a = __uint_as_float(x[e] << 16), b = __uint_as_float(x[e] & 0xffff0000u);
-                    y[e] = pack_half(fabsf(a) < INFINITY ? a * inv : NAN, fabsf(b) < INFINITY ? b * inv : NAN);
-                }
-                *reinterpret_cast<uint4*>(&sm.q[u][c / 8][r][((c % 8) ^ (r & 7)) * 16]) = make_uint4(y[0], y[1], y[2], y[3]);
+                for (int e = 0; e < 4; ++e)  // an infinity makes its row's scores NaN, as it would a softmax's
+                    y[e] = pack_half(fabsf(f[2 * e]) < INFINITY ? f[2 * e] * inv : NAN,
+                                     fabsf(f[2 * e + 1]) < INFINITY ? f[2 * e + 1] * inv : NAN);
+                *mine = make_uint4(y[0], y[1], y[2], y[3]);
+                if (c == 0) sm.qf[u][at(k)] = scale * p.scale_log2;
             }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sm.q_full[u]));
+            int head;
+            lim = limit(w, rows.of(p, u * kRowTile + r, head));
+            qf = sm.qf[u][r];
+            __syncwarp();
         };
-        if (it.more() && (u == 0 || both(it))) load_q(it);
-        while (it.more() && !*abortf) {
-            const bool active = u == 0 || both(it);
+        // the next item, its rows of Q under way
+        auto begin = [&](int k) -> bool {
+            wait_phase(smem_u32(&sm.i_full[k % kItemRing]), (k / kItemRing) & 1, abort_at, p.budget_ns);
+            const Item& w = sm.item[k % kItemRing];
+            if (w.te == 0) return false;
+            if (u == 0 || w.two) load_q(w);
+            return true;
+        };
+        bool more = begin(0);
+        while (more && !*abortf) {
+            const Item& it = sm.item[seg % kItemRing];
+            const int nt = it.te - it.tb;
+            const bool active = u == 0 || it.two;
             float m = -INFINITY, l = 0.f;
-            for (int i = it.tb; i < it.te && active; ++i, ++cnt) {
-                const uint32_t gt = g + (i - it.tb);
+            for (int i = 0; i < nt && active; ++i, ++cnt) {
+                const uint32_t gt = g + i;
                 wait_phase(smem_u32(&sm.m_full[gt % kMetas]), (gt / kMetas) & 1, abort_at, p.budget_ns);
                 const Meta ma = sm.meta[gt % kMetas][0], mb = sm.meta[gt % kMetas][1];
-                const float ca = ma.ks * qf, cb = mb.ks * qf;
+                // (a factor of 0 would make a masked score NaN)
+                const float fa = ma.ks * qf, fb = mb.ks * qf, ca = fa == 0.f ? 1e-30f : fa, cb = fb == 0.f ? 1e-30f : fb;
                 const int la = min(max(lim - ma.pos, 0), kPage), lb = min(max(lim - mb.pos, 0), kPage);
                 const bool cut = __any_sync(0xffffffffu, la < kPage || lb < kPage);
                 wait_phase(smem_u32(&sm.s_full[u]), cnt & 1, abort_at, p.budget_ns);
                 tc_fence_after();
-                uint32_t pk[64];
-                float sa = 0.f, sb = 0.f;
-                bool raise = __any_sync(0xffffffffu, m == -INFINITY && la + lb > 0);
-#pragma unroll 1
-                for (bool again = true; again;) {
-                    if (raise) {
-                        float mx = -INFINITY;
-#pragma unroll
-                        for (int ch = 0; ch < 4; ++ch) {
-                            uint32_t x[32];
-                            tmem_ld_32x32b_x32(scol + 32 * ch, x);
-                            tmem_wait_ld();
-                            const float cc = ch < 2 ? ca : cb, lv = ch < 2 ? ma.lv : mb.lv;
-                            const int left = (ch < 2 ? la : lb) - (ch & 1) * 32;
-#pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                if (e < left) mx = fmaxf(mx, fmaf(__uint_as_float(x[e]), cc, lv));
-                        }
-                        const float now = mx == -INFINITY ? m : fmaxf(m, mx - kTop);
-                        const float f = m == -INFINITY ? 0.f : fast_exp2(m - now);
-                        l *= f;
-                        m = now;
-                        if (i > it.tb) {  // O holds the tiles so far: QK of this one was issued behind their PV
-#pragma unroll
-                            for (int c = 0; c < D; c += 16) {
-                                uint32_t o[16];
-                                tmem_ld_32x32b_x16(ocol + c, o);
-                                tmem_wait_ld();
-#pragma unroll
-                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                                tmem_st_32x32b_x16(ocol + c, o);
-                            }
-                            tmem_wait_st();
-                        }
-                    }
-                    const float ref = m == -INFINITY ? 0.f : m;
-                    sa = sb = 0.f;
-#pragma unroll
-                    for (int ch = 0; ch < 4; ++ch) {
-                        uint32_t x[32];
-                        tmem_ld_32x32b_x32(scol + 32 * ch, x);
-                        tmem_wait_ld();
-                        const float cc = ch < 2 ? ca : cb, off = (ch < 2 ? ma.lv : mb.lv) - ref;
+                uint32_t x[32];
+                auto get = [&](int ch) {  // chunk ch of the scores, what the row does not see at -inf
+                    tmem_ld_32x32b_x32(scol + 32 * ch, x);
+                    tmem_wait_ld();
+                    if (cut) {
                         const int left = (ch < 2 ? la : lb) - (ch & 1) * 32;
-                        const float2 c2 = make_float2(cc, cc), o2 = make_float2(off, off);
-                        float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            float2 y = __ffma2_rn(make_float2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), c2, o2);
-                            if (cut) {
-                                if (2 * e >= left) y.x = -INFINITY;
-                                if (2 * e + 1 >= left) y.y = -INFINITY;
-                            }
-                            y = make_float2(fast_exp2(y.x), fast_exp2(y.y));
-                            sum = __fadd2_rn(sum, y);
-                            pk[16 * ch + e] = pack_half(y.x, y.y);
-                        }
-                        if (ch < 2) sa += sum.x + sum.y;
-                        else sb += sum.x + sum.y;
+                        for (int e = 0; e < 32; ++e)
+                            if (e >= left) x[e] = 0xff800000u;
                     }
-                    again = !raise && __any_sync(0xffffffffu, sa + sb > kMost);
-                    raise = again;
-                }
-                l += sa * ma.inv + sb * mb.inv;
+                };
+                // the tile's largest exponent: factors of scores are not negative
+                float mx = -INFINITY;
+#pragma unroll 1
+                for (int ch = 0; ch < 4; ++ch) {
+                    get(ch);
+                    float top = __uint_as_float(x[0]);
 #pragma unroll
-                for (int ch = 0; ch < 4; ++ch) tmem_st_32x32b_x16(pcol + 16 * ch, *reinterpret_cast<uint32_t(*)[16]>(&pk[16 * ch]));
+                    for (int e = 1; e < 31; e += 2) top = max3(top, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+                    top = fmaxf(top, __uint_as_float(x[31]));
+                    mx = fmaxf(mx, fmaf(top, ch < 2 ? ca : cb, ch < 2 ? ma.lv : mb.lv));
+                }
+                const bool up = m == -INFINITY ? mx > -INFINITY : mx > m + kMost;
+                if (__any_sync(0xffffffffu, up)) {
+                    const float now = up ? mx - kTop : m, f = up ? fast_exp2(m - now) : 1.f;
+                    l *= f;
+                    m = now;
+                    if (i > 0) {  // O holds the tiles so far: QK of this one was issued behind their PV
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 16) {
+                            uint32_t o[16];
+                            tmem_ld_32x32b_x16(ocol + c, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            tmem_st_32x32b_x16(ocol + c, o);
+                        }
+                    }
+                }
+                const float ref = m == -INFINITY ? 0.f : m;
+                // P of a chunk goes over scores that have been read
+#pragma unroll 1
+                for (int ch = 0; ch < 4; ++ch) {
+                    get(ch);
+                    const float cc = ch < 2 ? ca : cb, off = (ch < 2 ? ma.lv : mb.lv) - ref;
+                    const float2 c2 = make_float2(cc, cc), o2 = make_float2(off, off);
+                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float2 y = __ffma2_rn(make_float2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), c2, o2);
+                        y = make_float2(fast_exp2(y.x), fast_exp2(y.y));
+                        sum[e & 1] = __fadd2_rn(sum[e & 1], y);
+                        pk[e] = pack_half(y.x, y.y);
+                    }
+                    tmem_st_32x32b_x16(scol + 16 * ch, pk);
+                    l = fmaf((sum[0].x + sum[1].x) + (sum[0].y + sum[1].y), ch < 2 ? ma.inv : mb.inv, l);
+                }
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&sm.p_full[u]));
             }
-            g += it.te - it.tb;
-            // the next item's rows first: its QK can run beside this one's output (no wait is under way on Q's memory:
-            // the last S has come)
-            const int row0 = row, head0 = head, lim0 = lim;
-            const float base0 = base;
+            g += nt;
+            // the next item's rows first: its QK can run beside this one's output (nothing reads Q's memory any more: the
+            // last S has come)
+            const int lim0 = lim;
+            more = begin(seg + 1);
             const bool whole = it.tb == 0 && it.te == it.tiles, head_part = it.tb == 0;
-            if (!whole) {
-                if (head_part) {
-                    start1 = it.start;
-                    tiles1 = it.tiles;
-                } else {
-                    start0 = it.start;
-                    tiles0 = it.tiles;
-                }
-                if (threadIdx.x == kSoftmax * 32) {
-                    sm.rows[head_part] = it.rows();
-                    sm.base[head_part] = base0;
-                }
-            }
-            it.next();
-            if (it.more() && (u == 0 || both(it))) load_q(it);
             wait_phase(smem_u32(&sm.n_full[seg & 1]), (seg >> 1) & 1, abort_at, p.budget_ns);
+            const float base = sm.first_lv[seg & 1];
+            if (!whole && threadIdx.x == kSoftmax * 32) {
+                sm.rows[head_part] = it.rows;
+                sm.base[head_part] = base;
+                sm.start[head_part] = it.start;
+                sm.tiles[head_part] = it.tiles;
+            }
             if (active) {
                 wait_phase(smem_u32(&sm.o_full[u]), items & 1, abort_at, p.budget_ns);
                 ++items;
                 tc_fence_after();
-                const bool nan = sm.nan_any[seg & 1][0] || sm.nan_any[seg & 1][1];
-                float* part = p.parts + ((size_t)blockIdx.x * 2 + head_part) * kItemRows * (D + 2);
-                const float inv = l != 0.f ? exp2f(base0) / l : 0.f;
-                const size_t at = (size_t)max(row0, 0) * p.pl.heads + head0;
+                bool nan = false;
 #pragma unroll
+                for (int k = 0; k < kConverters; ++k) nan |= sm.nan_any[seg & 1][k] != 0;
+                float* part = p.parts + ((size_t)blockIdx.x * 2 + head_part) * kItemRows * (D + 2);
+                const float inv = l != 0.f ? exp2f(base) / l : 0.f;
+                int head0;
+                const int row0 = it.rows.of(p, u * kRowTile + r, head0);
+                const size_t at = (size_t)max(row0, 0) * p.pl.heads + head0;
+#pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
                     uint32_t o[32];
                     tmem_ld_32x32b_x32(ocol + c, o);
                     tmem_wait_ld();
                     if (nan) {
 #pragma unroll 1
-                        for (int e = 0; e < 32; ++e)
-                            if (min(sm.nan_at[seg & 1][0][c + e], sm.nan_at[seg & 1][1][c + e]) < lim0) {
+                        for (int e = 0; e < 32; ++e) {
+                            int at = INT_MAX;
+#pragma unroll
+                            for (int k = 0; k < kConverters; ++k) at = min(at, sm.nan_at[seg & 1][k][c + e]);
+                            if (at < lim0) {
 #pragma unroll
                                 for (int k = 0; k < 32; ++k)
                                     if (k == e) o[k] = 0x7fc00000u;
                             }
+                        }
                     }
                     if (whole && row0 >= 0) {
 #pragma unroll
@@ -585,16 +659,19 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 tc_fence_before();
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sm.n_empty[seg & 1]));
+            if (lane == 0) {
+                mbar_arrive(smem_u32(&sm.n_empty[seg & 1]));
+                mbar_arrive(smem_u32(&sm.i_empty[seg % kItemRing]));
+            }
             ++seg;
         }
         // the items that are shared with other CTAs, counted off once all is written (see cache_attend_tc.cu)
         const bool bad = soft_any(*abortf != 0);  // (else every warp has been through every item)
-        if (tiles0 + tiles1 > 0 && !bad) {
+        if (!bad) {
             const int tid = threadIdx.x - kSoftmax * 32;
             if (tid < 2) {
-                const long long start = tid ? start1 : start0;
-                const int tiles = tid ? tiles1 : tiles0;
+                const long long start = sm.start[tid];
+                const int tiles = sm.tiles[tid];
                 int c0 = 0, np = 0;
                 if (tiles > 0) {
                     c0 = cta_of(start, sm);
@@ -607,9 +684,6 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 sm.last_c0[tid] = c0;
                 sm.last[tid] = np;
             }
-            soft_any(false);
-            for (int i = 0; i < 2; ++i)
-                if (sm.last[i]) join<D>(p, sm.rows[i], sm.base[i], sm.last_c0[i], sm.last[i], warp - kSoftmax, lane);
         }
         dead = *abortf != 0;
     }
@@ -623,6 +697,9 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
             wait_raw(smem_u32(&sm.drain), 0, p.budget_ns);
         }
         if (threadIdx.x == 0) atomicExch(p.pl.status, SSBA_ERR_TIMEOUT);
+    } else {
+        for (int i = 0; i < 2; ++i)
+            if (sm.last[i]) join<D>(p, sm.rows[i], sm.base[i], sm.last_c0[i], sm.last[i], warp, lane);
     }
     tc_fence_before();
     __syncthreads();
@@ -691,6 +768,7 @@ int launch_cache_attend_rows(const cache::Pool& pl, const cache::Batch& bt, int 
     p.budget_ns = kWaitBudgetNs;
     p.chunks = (p.G + kItemRows - 1) / kItemRows;
     p.gc = (p.G + p.chunks - 1) / p.chunks;
+    p.gc_inv = (65536 + p.gc - 1) / p.gc;
     p.tq = 1;
     while (2 * p.tq * p.gc <= kItemRows) p.tq *= 2;
     return head_dim == 64 ? launch<64>(maps, p, st) : launch<128>(maps, p, st);

@@ -736,6 +736,7 @@ int launch_cache_attend_tc(const cache::Pool& pl, const cache::Batch& bt, int he
     const int R = want <= 8 ? 8 : want <= 16 ? 16 : 32;
     p.chunks = (p.G + R - 1) / R;
     p.gc = (p.G + p.chunks - 1) / p.chunks;
+    p.gc_inv = (65536 + p.gc - 1) / p.gc;
     p.tq = 1;
     while (!idx && 2 * p.tq * p.gc <= R) p.tq *= 2;
     return R == 8 ? launch_rows<8>(maps, p, head_dim, st)

@@ -31,6 +31,7 @@ struct Params {
     float* parts;
     unsigned* tickets;
     int G, gc, chunks, tq;  // group size; heads and tokens of an item; chunks of a group
+    int gc_inv;             // ceil(2^16 / gc): r / gc for r < 256
     uint64_t budget_ns;
 };
 
@@ -41,8 +42,9 @@ struct Rows {
     // Row r of the item: its row of the batch (-1: none) and head.
     __device__ __forceinline__ int of(const Params& p, int r, int& head) const
     {
-        const int i = r / p.gc, g = (hv % p.chunks) * p.gc + r - i * p.gc;
-        head = (hv / p.chunks) * p.G + g;
+        const int i = r * p.gc_inv >> 16, chunk = p.chunks == 1 ? 0 : hv % p.chunks;  // r < 256
+        const int g = chunk * p.gc + r - i * p.gc;
+        head = (p.chunks == 1 ? hv : hv / p.chunks) * p.G + g;
         return g < p.G && i < n ? row + i : -1;
     }
 };
