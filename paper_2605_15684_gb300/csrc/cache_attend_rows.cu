@@ -3,20 +3,23 @@
 //
 // An item is up to 256 rows (tokens times the group's heads) of one sequence and K/V head, in two tiles of 128
 // rows; it visits its sequence's tiles of 128 tokens (two pages):
-//   S_u = Q_u K^T   tcgen05.mma kind::f16, M = 128, N = 128, K = D   (fp16 operands, K-major)
-//   O_u += P_u V    M = 128, N = D, K = 128                          (P from tensor memory, V MN-major)
+//   S_u = Q_u K^T   tcgen05.mma kind::f16, M = 128, N = 128, K = D   (fp16, K-major)
+//   O_u += P_u V    M = 128, N = D, K = 128                          (fp16, P from tensor memory, V MN-major)
 // An e4m3 value is an fp16 value, so K and V are converted without rounding, once for both row tiles, and their
 // page's scale stays out of the products: K's multiplies the scores, V's is added to their exponent,
 //   P = 2^(s + log2 v_scale - m),   l = sum P / v_scale,   O = sum P (bytes of V) / l,
 // v_scale relative to the sequence's first page (within 2^+-100 of it). Rows of Q are brought below 448 by a
 // power of two; their 8 bits of significand are exact in fp16 down to 2^-25 of the row's largest. P is rounded to fp16's
-// 11 bits; m is 8 below the largest exponent, so P's smallest step is 2^-32 of the largest weight.
+// 11 bits; m begins 8 below the largest exponent, so P's smallest step is 2^-32 of the largest weight.
 //
-// One CTA an SM, 16 warps: a producer (TMA of the pages' bytes), an issuer, four converters (half a page each: bytes
-// to fp16 in the swizzled layout of the products), and a softmax warpgroup for each row tile (a thread is a row).
+// One CTA an SM, 16 warps: a producer (TMA of the pages' bytes), an issuer, four converters (half a page each: bytes to
+// fp16 in the swizzled layout of the products), one that walks the items for the softmax, and a softmax warpgroup for each row tile (a thread is a row).
 // P overwrites the lower half of its S, so of one row tile PV_g comes before QK_{g + 1}; while one row tile
 // is with the tensor cores the other is with its softmax. A tile's maximum is taken first, but the row's reference is
-// raised (and O rescaled in tensor memory) only where P would pass 2^14.
+// raised (and O rescaled in tensor memory) only where P would pass 2^14. The softmax's code is loops over 32 scores: it
+// has to stay in the SM's instruction cache beside the other roles' (unrolled, a tile takes 2.5 us instead of 2.3).
+// What bounds it: of one row tile, S to P takes 1.2 us (one warp a scheduler, so latencies show) and PV and QK
+// of 128 x 128 x 128 another 1.1 beside the other tile's; the tensor pipe is busy 1.35 of a tile's 2.3 us.
 // Work is shared out and joined as in cache_attend_tc.cu.
 #include <algorithm>
 #include <climits>
@@ -40,7 +43,7 @@ constexpr float kSpan = 100.f;      // log2 of V scales, relative to the first p
 enum Role { kLoad = 0, kIssue = 1, kConvert = 2, kItems = 6, kSoftmax = 8 };
 constexpr uint32_t kTmemCols = 512;
 
-constexpr uint32_t idesc_f16_f32(int M, int N, bool b_mn_major) { return idesc_e4m3_f32(M, N, false, b_mn_major); }
+constexpr uint32_t idesc_f16_f32(int M, int N, bool b_mn_major) { return idesc_e4m3_f32(M, N, false, b_mn_major); }  // formats 0: fp16
 
 constexpr int kItemRing = 4;
 
@@ -422,8 +425,9 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
 #pragma unroll
                         for (int k = 0; k < kIts; ++k) {
                             const int row = row0 + k * kRows;
-                            const uint4 a = make_uint4(half2_of(x[k].x & 0xffff), half2_of(x[k].x >> 16), half2_of(x[k].y & 0xffff), half2_of(x[k].y >> 16));
-                            const uint4 b = make_uint4(half2_of(x[k].z & 0xffff), half2_of(x[k].z >> 16), half2_of(x[k].w & 0xffff), half2_of(x[k].w >> 16));
+                            uint32_t y[8] = {half2_of(x[k].x & 0xffff), half2_of(x[k].x >> 16), half2_of(x[k].y & 0xffff), half2_of(x[k].y >> 16),
+                                             half2_of(x[k].z & 0xffff), half2_of(x[k].z >> 16), half2_of(x[k].w & 0xffff), half2_of(x[k].w >> 16)};
+                            const uint4 a = make_uint4(y[0], y[1], y[2], y[3]), b = make_uint4(y[4], y[5], y[6], y[7]);
                             uint8_t* to = &sm.cv[cs][c / 4][row][0];
                             const int q = (c % 4) * 2;
                             // lanes of the second 64 channels write their second half first: no bank conflicts
@@ -459,44 +463,68 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
             return row >= 0 ? min(max(w.s.len - w.s.n + row - w.s.row + 1, 0), w.s.len) : 0;
         };
         // the warp's 32 rows of Q to shared memory
-        // (small loops: code that runs once an item is read from memory, and unrolled sixteen times it took 20 us)
         auto load_q = [&](const Item& w) {
             constexpr int kLanes = D / 8, kRows = 32 / kLanes;  // lanes of a row (8 values each), rows at a time
             const int c = lane % kLanes;
             const Rows rows = w.rows;
-            auto at = [&](int k) { return quad * 32 + k * kRows + lane / kLanes; };
-            auto to = [&](int x) { return &sm.q[u][c / 8][x][((c % 8) ^ (x & 7)) * 16]; };
 #pragma unroll 2
-            for (int k = 0; k < 32 / kRows; ++k) {  // as it is, to where it will be
+            for (int k = 0; k < 32 / kRows; ++k) {
+                const int at = quad * 32 + k * kRows + lane / kLanes;
                 int hd;
-                const int rr = rows.of(p, u * kRowTile + at(k), hd);
+                const int rr = rows.of(p, u * kRowTile + at, hd);
                 const __nv_bfloat16* src = p.q + ((size_t)max(rr, 0) * p.pl.heads + (rr >= 0 ? hd : 0)) * D + c * 8;
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to(at(k)))), "l"(src), "r"(rr >= 0 ? 16 : 0)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                                 smem_u32(&sm.q[u][c / 8][at][((c % 8) ^ (at & 7)) * 16])),
+                             "l"(src), "r"(rr >= 0 ? 16 : 0)
                              : "memory");
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
+            // each lane what it has copied itself: 8 values of a row, which is scaled by a power of two
+            // (four rows at a time, their shuffles side by side)
+            constexpr int kB = 4;
 #pragma unroll 1
-            for (int k = 0; k < 32 / kRows; ++k) {
-                uint4* mine = reinterpret_cast<uint4*>(to(at(k)));
-                const uint4 in = *mine;
-                const uint32_t x[4] = {in.x, in.y, in.z, in.w};
-                float f[8], amax = 0.f;
+            for (int k0 = 0; k0 < 32 / kRows; k0 += kB) {
+                uint4 w[kB];
+                uint32_t top[kB];
+                auto at = [&](int k) { return quad * 32 + (k0 + k) * kRows + lane / kLanes; };
+                auto mine = [&](int k) { return reinterpret_cast<uint4*>(&sm.q[u][c / 8][at(k)][((c % 8) ^ (at(k) & 7)) * 16]); };
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    f[e] = __uint_as_float(e & 1 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16);
-                    const float a = fabsf(f[e]);
-                    if (a < INFINITY) amax = fmaxf(amax, a);
+                for (int k = 0; k < kB; ++k) w[k] = *mine(k);
+#pragma unroll
+                for (int k = 0; k < kB; ++k) {
+                    const uint32_t a = 0x7fff7fffu;
+                    top[k] = __vmaxu2(__vmaxu2(w[k].x & a, w[k].y & a), __vmaxu2(w[k].z & a, w[k].w & a));
+                    if (__vcmpgeu2(top[k], 0x7f807f80u)) {  // an infinity or NaN: the finite ones' largest
+                        const uint32_t v[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+                        top[k] = 0;
+#pragma unroll 1
+                        for (int e = 0; e < 8; ++e) {
+                            const uint32_t b = ((e < 4 ? (e < 2 ? v[0] : v[1]) : (e < 6 ? v[2] : v[3])) >> (16 * (e & 1))) & 0x7fffu;
+                            if (b < 0x7f80u) top[k] = max(top[k], b);
+                        }
+                    }
+                    top[k] = max(top[k] & 0xffffu, top[k] >> 16);
                 }
 #pragma unroll
-                for (int o = kLanes / 2; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-                const float scale = scale_for(amax), inv = scale > 0.f ? 1.f / scale : 1.f;
-                uint32_t y[4];
+                for (int o = kLanes / 2; o; o >>= 1) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)  // an infinity makes its row's scores NaN, as it would a softmax's
-                    y[e] = pack_half(fabsf(f[2 * e]) < INFINITY ? f[2 * e] * inv : NAN,
-                                     fabsf(f[2 * e + 1]) < INFINITY ? f[2 * e + 1] * inv : NAN);
-                *mine = make_uint4(y[0], y[1], y[2], y[3]);
-                if (c == 0) sm.qf[u][at(k)] = scale * p.scale_log2;
+                    for (int k = 0; k < kB; ++k) top[k] = max(top[k], __shfl_xor_sync(0xffffffffu, top[k], o));
+                }
+#pragma unroll
+                for (int k = 0; k < kB; ++k) {
+                    const float scale = scale_for(__uint_as_float(top[k] << 16));
+                    // (a power of two from 2^-126 to 2^120: its inverse by its exponent)
+                    const float inv = scale > 0.f ? __uint_as_float(0x7f000000u - __float_as_uint(scale)) : 1.f;
+                    const uint32_t v[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+                    uint32_t y[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {  // (an infinity times 0 is NaN: it makes its row's scores NaN, as it would a softmax's)
+                        const float a = __uint_as_float(v[e] << 16), b = __uint_as_float(v[e] & 0xffff0000u);
+                        y[e] = pack_half(fmaf(a, 0.f, a * inv), fmaf(b, 0.f, b * inv));
+                    }
+                    *mine(k) = make_uint4(y[0], y[1], y[2], y[3]);
+                    if (c == 0) sm.qf[u][at(k)] = scale * p.scale_log2;
+                }
             }
             fence_proxy_async_smem();
             __syncwarp();

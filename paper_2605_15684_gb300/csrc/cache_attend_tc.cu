@@ -565,16 +565,26 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
             }
             add_o();
             tc_fence_before();
-            // the sums over tokens, to every thread
+            // The sums over tokens: lanes halve what they hold with every exchange, so that row r ends in lane r * 32 / R.
+            // Lane r then works out row r's factor and place. (All of this runs once an item, when the code has to
+            // come from memory: as short as can be.)
+            constexpr int kEach = 32 / R;
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
+            for (int n = R / 2, d = 16; d; d >>= 1) {
+                if (n) {
 #pragma unroll
-                for (int d = 16; d; d >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
-                if (lane == 0) sm.red[quad][r] = l[r];
+                    for (int r = 0; r < R / 2; ++r)
+                        if (r < n) {
+                            const float keep = lane & d ? l[r + n] : l[r], send = lane & d ? l[r] : l[r + n];
+                            l[r] = keep + __shfl_xor_sync(0xffffffffu, send, d);
+                        }
+                    n /= 2;
+                } else {
+                    l[0] += __shfl_xor_sync(0xffffffffu, l[0], d);
+                }
             }
+            if (lane % kEach == 0) sm.red[quad][lane / kEach] = l[0];
             soft_sync();
-#pragma unroll
-            for (int r = 0; r < R; ++r) l[r] = (sm.red[0][r] + sm.red[1][r]) + (sm.red[2][r] + sm.red[3][r]);
             const int nan_at = tok < D ? sm.nan_at[tok] : INT_MAX;
             if (nan_at != INT_MAX) {
                 sm.nan_at[tok] = INT_MAX;
@@ -585,16 +595,32 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sm.q_empty[st]));
             const bool whole = it.tb == 0 && it.te == it.tiles;
-            if (!whole) {
-                // parts: slot 1 of the CTA that the item starts in, slot 0 of the others
-                float* part = p.parts + ((size_t)blockIdx.x * 2 + (it.tb == 0)) * R * (D + 2);
-                if (tok < D) {
-#pragma unroll
-                    for (int r = 0; r < R; ++r) part[r * D + tok] = o[r];
+            // parts: slot 1 of the CTA that the item starts in, slot 0 of the others
+            float* part = p.parts + ((size_t)blockIdx.x * 2 + (it.tb == 0)) * R * (D + 2);
+            if (lane < R) {
+                const float sum = (sm.red[0][lane] + sm.red[1][lane]) + (sm.red[2][lane] + sm.red[3][lane]);
+                int head;
+                const int row = it.row_of(lane, head);
+                const long long at = row >= 0 ? (long long)row * p.pl.heads + head : -1;
+                sm.row[quad][0][lane] = make_float4(sum != 0.f ? 1.f / sum : 0.f, 0.f, __int_as_float((int)at), __int_as_float((int)(at >> 32)));
+                if (quad == 0) {
+                    if (!whole) reinterpret_cast<float2*>(part + R * D)[lane] = make_float2(ref, sum);
+                    else if (row >= 0) p.lse[at] = sum != 0.f ? (ref + log2f(sum)) * kLn2 : -INFINITY;
                 }
+            }
+            __syncwarp();
+            if (tok < D) {
 #pragma unroll
-                for (int r = 0; r < R; ++r)
-                    if (tok == r) reinterpret_cast<float2*>(part + R * D)[r] = make_float2(ref, l[r]);
+                for (int r = 0; r < R; ++r) {
+                    const float4 w = sm.row[quad][0][r];
+                    const int hi = __float_as_int(w.w);
+                    const size_t at = ((size_t)(uint32_t)hi << 32) | (uint32_t)__float_as_int(w.z);
+                    if (!whole) part[r * D + tok] = o[r];
+                    else if (hi >= 0) p.O[at * D + tok] = __float2bfloat16_rn(o[r] * w.x);
+                }
+            }
+            __syncwarp();
+            if (!whole) {
                 const int which = it.tb == 0;
                 if (which) {
                     start1 = it.start;
@@ -604,17 +630,6 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
                     tiles0 = it.tiles;
                 }
                 if (tok == 0) sm.rows[which] = it.rows();
-            } else {
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    int head;
-                    const int row = it.row_of(r, head);
-                    if (row >= 0) {
-                        const size_t at = (size_t)row * p.pl.heads + head;
-                        if (tok < D) p.O[at * D + tok] = __float2bfloat16_rn(l[r] != 0.f ? o[r] / l[r] : 0.f);
-                        if (tok == r) p.lse[at] = l[r] != 0.f ? (ref + log2f(l[r])) * kLn2 : -INFINITY;
-                    }
-                }
             }
             if (it.start + it.te >= it.w1) break;  // (the walk stays at its last item)
             it.next();

@@ -16,6 +16,7 @@ constexpr int kTile = 128;           // tokens of a tile: two pages
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kNowhere = 1 << 30;    // token position of a page that is not there
 
+constexpr int kLeast = 4;            // tiles of a share at least: below, joining costs more than the tiles
 constexpr int kMaxGrid = 608;        // CTAs of a launch at most (two an SM of up to 304)
 static_assert(kMaxGrid * sizeof(unsigned) <= SSBA_CACHE_TICKET_BYTES, "a counter a CTA");
 
@@ -256,7 +257,7 @@ __device__ void make_share(const Params& p, S& sm)
             W += scan(b0, mine, front);
         }
     }
-    const int C = (int)min((long long)gridDim.x, max(W, 1LL)), c = blockIdx.x;
+    const int C = (int)min((long long)gridDim.x, max(W / kLeast, 1LL)), c = blockIdx.x;
     // (32-bit division where it does)
     const bool small = W < INT_MAX / kMaxGrid;
     const long long w0 = c >= C ? W : small ? (int)W * c / C : W * c / C;
