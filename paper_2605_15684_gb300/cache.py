@@ -15,7 +15,7 @@ from dataclasses import dataclass
 import torch
 
 from . import api
-from .api import (SSBA_BF16, SSBA_ERR_INVALID, SSBA_ERR_WORKSPACE, SSBA_FP32, SsbaError, _check, _empty, _lock, _out,
+from .api import (SSBA_BF16, SSBA_ERR_INVALID, SSBA_ERR_WORKSPACE, SSBA_FP32, SsbaError, _check, _empty, _lock,
                   _raise_on, _side, _stream_ptr, load_library)
 
 PAGE = 64
@@ -114,29 +114,40 @@ def _pool(pl: _Plan, cache: Cache):
     return dev
 
 
-def _same_device(dev, *tensors) -> None:
-    index = dev.index
-    for t in tensors:
-        if t is not None and t.get_device() != index:
-            raise SsbaError(SSBA_ERR_INVALID, f"tensors on {dev} and {t.device} in one call")
+def _on(t, name: str, shape, dtype, dev) -> None:
+    """_check, and that the tensor is on the call's device."""
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == dev.index
+            and t.is_contiguous()):
+        return
+    _check(t, name, shape, dtype)
+    raise SsbaError(SSBA_ERR_INVALID, f"{name} is on {t.device}, the cache on {dev}")
 
 
-def _rows(x, name: str, heads: int, pl: _Plan) -> int:
+def _rows(x, name: str, heads: int, pl: _Plan, dev) -> int:
     """Rows of a [T, heads, head_dim] tensor."""
-    T = int(x.shape[0]) if isinstance(x, torch.Tensor) and x.dim() == 3 else -1
-    _check(x, name, (max(T, 0), heads, pl.d), pl.dtype)
+    T = x.shape[0] if isinstance(x, torch.Tensor) and x.dim() == 3 else 0
+    _on(x, name, (T, heads, pl.d), pl.dtype, dev)
     return T
 
 
-def _batch(table, lens, cu):
+def _batch(table, lens, cu, dev):
     """(table, width, lens, cu, B) as the C calls take them."""
     if not isinstance(table, torch.Tensor) or table.dim() != 2:
         raise SsbaError(SSBA_ERR_INVALID, "table must be a 2-D tensor [B, width]")
-    B, width = table.shape
-    _check(table, "table", (B, width), torch.int32)
-    _check(lens, "lens", (B,), torch.int32)
-    _check(cu, "cu", (B + 1,), torch.int32)
+    shape = table.shape
+    B, width = shape
+    _on(table, "table", shape, torch.int32, dev)
+    _on(lens, "lens", (B,), torch.int32, dev)
+    _on(cu, "cu", (B + 1,), torch.int32, dev)
     return table.data_ptr(), width, lens.data_ptr(), cu.data_ptr(), B
+
+
+def _result(t, name: str, shape, dtype, dev, side):
+    """An output: allocated when the caller gave none, else checked."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=dev) if side is None else _empty(shape, dtype, dev, side)
+    _on(t, name, shape, dtype, dev)
+    return t
 
 
 def cache_alloc(desc: CacheDesc, device="cuda") -> Cache:
@@ -150,13 +161,12 @@ def cache_alloc(desc: CacheDesc, device="cuda") -> Cache:
 def cache_append(desc: CacheDesc, cache: Cache, k, v, table, lens, cu, stream=None) -> Cache:
     """ssba_cache_append: k, v [T, kv_heads, head_dim] into the pages of their sequences; table [B, width],
     lens [B] (tokens held before), cu [B + 1], all int32. Returns the cache."""
-    lib = load_library()
+    lib = api._lib or load_library()
     pl = _plan(desc)
     dev = _pool(pl, cache)
-    T = _rows(k, "k", pl.kv, pl)
-    _check(v, "v", k.shape, pl.dtype)
-    batch = _batch(table, lens, cu)
-    _same_device(dev, k, v, table, lens, cu)
+    T = _rows(k, "k", pl.kv, pl, dev)
+    _on(v, "v", k.shape, pl.dtype, dev)
+    batch = _batch(table, lens, cu, dev)
     _raise_on(lib.ssba_cache_append(pl.ref, cache._ref, k.data_ptr(), v.data_ptr(), T, *batch,
                                     _stream_ptr(stream)))
     return cache
@@ -166,17 +176,16 @@ def cache_select(desc: CacheDesc, cache: Cache, q, table, lens, cu, keep: int, f
                  stream=None):
     """ssba_cache_select: q [T, heads, head_dim] -> (idx [T, kv_heads, keep], cnt [T, kv_heads]) int32.
     lens: tokens held, the rows of q among them."""
-    lib = load_library()
+    lib = api._lib or load_library()
     pl = _plan(desc)
     dev = _pool(pl, cache)
-    T = _rows(q, "q", pl.heads, pl)
-    batch = _batch(table, lens, cu)
+    T = _rows(q, "q", pl.heads, pl, dev)
+    batch = _batch(table, lens, cu, dev)
     if not 0 <= first < keep:
         raise SsbaError(SSBA_ERR_INVALID, f"keep={keep} must be more than first={first}, first >= 0")
-    _same_device(dev, q, table, lens, cu, idx, cnt)
     side = _side(stream, dev)
-    idx = _out(idx, "idx", (T, pl.kv, keep), torch.int32, dev, side)
-    cnt = _out(cnt, "cnt", (T, pl.kv), torch.int32, dev, side)
+    idx = _result(idx, "idx", (T, pl.kv, keep), torch.int32, dev, side)
+    cnt = _result(cnt, "cnt", (T, pl.kv), torch.int32, dev, side)
     _raise_on(lib.ssba_cache_select(pl.ref, cache._ref, q.data_ptr(), T, *batch, keep, first, idx.data_ptr(),
                                     cnt.data_ptr(), _stream_ptr(stream)))
     return idx, cnt
@@ -226,22 +235,21 @@ def cache_attend(desc: CacheDesc, cache: Cache, q, table, lens, cu, idx=None, cn
                  workspace="default", stream=None):
     """ssba_cache_attend: q [T, heads, head_dim] -> (O [T, heads, head_dim], lse [T, heads] fp32), over every
     page of the rows' sequences, or over the lists (idx, cnt) of cache_select."""
-    lib = load_library()
+    lib = api._lib or load_library()
     pl = _plan(desc)
     dev = _pool(pl, cache)
-    T = _rows(q, "q", pl.heads, pl)
-    batch = _batch(table, lens, cu)
+    T = _rows(q, "q", pl.heads, pl, dev)
+    batch = _batch(table, lens, cu, dev)
     keep = 0
     if (idx is None) != (cnt is None):
         raise SsbaError(SSBA_ERR_INVALID, "idx and cnt come together")
     if idx is not None:
         keep = int(idx.shape[2]) if isinstance(idx, torch.Tensor) and idx.dim() == 3 else 0
-        _check(idx, "idx", (T, pl.kv, keep), torch.int32)
-        _check(cnt, "cnt", (T, pl.kv), torch.int32)
-    _same_device(dev, q, table, lens, cu, idx, cnt, O, lse)
+        _on(idx, "idx", (T, pl.kv, keep), torch.int32, dev)
+        _on(cnt, "cnt", (T, pl.kv), torch.int32, dev)
     side = _side(stream, dev)
-    O = _out(O, "O", q.shape, pl.dtype, dev, side)
-    lse = _out(lse, "lse", (T, pl.heads), torch.float32, dev, side)
+    O = _result(O, "O", q.shape, pl.dtype, dev, side)
+    lse = _result(lse, "lse", (T, pl.heads), torch.float32, dev, side)
     if isinstance(workspace, str):
         workspace = _default_workspace(pl, lib, dev, stream, side)
     elif workspace is None:
@@ -256,12 +264,11 @@ def cache_attend(desc: CacheDesc, cache: Cache, q, table, lens, cu, idx=None, cn
 
 def cache_copy(desc: CacheDesc, cache: Cache, src, dst, stream=None) -> Cache:
     """ssba_cache_copy: pages src[i] -> dst[i], int32 CUDA tensors [n]. Returns the cache."""
-    lib = load_library()
+    lib = api._lib or load_library()
     pl = _plan(desc)
     dev = _pool(pl, cache)
     n = src.numel() if isinstance(src, torch.Tensor) else -1
-    _check(src, "src", (max(n, 0),), torch.int32)
-    _check(dst, "dst", (max(n, 0),), torch.int32)
-    _same_device(dev, src, dst)
+    _on(src, "src", (max(n, 0),), torch.int32, dev)
+    _on(dst, "dst", (max(n, 0),), torch.int32, dev)
     _raise_on(lib.ssba_cache_copy(pl.ref, cache._ref, src.data_ptr(), dst.data_ptr(), n, _stream_ptr(stream)))
     return cache

@@ -8,6 +8,7 @@
 // A page that becomes full gets its mean key, s * (sum of the 64 bytes' values) / 64: at most 64 * 448 in
 // steps of 2^-9 are 24 bits, so that sum is exact in any order.
 #include <algorithm>
+#include <climits>
 #include <cmath>
 
 #include "cache.cuh"
@@ -21,30 +22,65 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kSeqs = 1024;  // sequences whose pages are counted at a time
 constexpr int kStages = 2;
 
+// 16 bytes of input: running largest magnitude of finite values (as bits that are ordered like them), and e4m3
+// bytes of the values times a power of two (an infinity times 0 is NaN, so it is held as NaN).
 template <typename T>
-struct Chunk;  // 16 bytes of input
+struct Chunk;
 template <>
 struct Chunk<__nv_bfloat16> {
     static constexpr int n = 8;
-    static __device__ __forceinline__ void get(const uint4& u, float* f)
+    static __device__ __forceinline__ uint32_t largest(const uint4& u, uint32_t top, bool& odd)
     {
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        const uint32_t m = 0x7fff7fffu, a[4] = {u.x & m, u.y & m, u.z & m, u.w & m};
+        const uint32_t t = __vmaxu2(__vmaxu2(a[0], a[1]), __vmaxu2(a[2], a[3]));
+        if (__vcmpgeu2(t, 0x7f807f80u) == 0) return __vmaxu2(top, t);
+        odd = true;
+#pragma unroll 1
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t b = ((e < 4 ? (e < 2 ? a[0] : a[1]) : (e < 6 ? a[2] : a[3])) >> (16 * (e & 1))) & 0x7fffu;
+            if (b < 0x7f80u) top = __vmaxu2(top, b);
+        }
+        return top;
+    }
+    static __device__ __forceinline__ float value(uint32_t top) { return __uint_as_float(max(top & 0xffffu, top >> 16) << 16); }
+    template <bool kOdd>
+    static __device__ __forceinline__ void round(const uint4& u, float inv, uint32_t* w)
+    {
+        const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+        const __nv_bfloat162 s = __float2bfloat162_rn(inv), zero = __float2bfloat162_rn(0.f);  // a power of two: exact
+        uint32_t r[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            f[2 * i] = __uint_as_float(w[i] << 16);
-            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(&x[i]);
+            const __nv_bfloat162 y = kOdd ? __hfma2(v, zero, __hmul2(v, s)) : __hmul2(v, s);
+            const uint32_t b = *reinterpret_cast<const uint32_t*>(&y);
+            r[i] = to_e4m3x2(__uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u));
         }
+        w[0] = r[0] | (r[1] << 16);
+        w[1] = r[2] | (r[3] << 16);
     }
 };
 template <>
 struct Chunk<float> {
     static constexpr int n = 4;
-    static __device__ __forceinline__ void get(const uint4& u, float* f)
+    static __device__ __forceinline__ uint32_t largest(const uint4& u, uint32_t top, bool& odd)
     {
-        f[0] = __uint_as_float(u.x);
-        f[1] = __uint_as_float(u.y);
-        f[2] = __uint_as_float(u.z);
-        f[3] = __uint_as_float(u.w);
+        const uint32_t a[4] = {u.x & 0x7fffffffu, u.y & 0x7fffffffu, u.z & 0x7fffffffu, u.w & 0x7fffffffu};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (a[i] < 0x7f800000u) top = max(top, a[i]);
+            else odd = true;
+        }
+        return top;
+    }
+    static __device__ __forceinline__ float value(uint32_t top) { return __uint_as_float(top); }
+    template <bool kOdd>
+    static __device__ __forceinline__ void round(const uint4& u, float inv, uint32_t* w)
+    {
+        float y[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = kOdd ? fmaf(y[i], 0.f, y[i] * inv) : y[i] * inv;
+        w[0] = to_e4m3x2(y[0], y[1]) | (to_e4m3x2(y[2], y[3]) << 16);
     }
 };
 
@@ -93,17 +129,18 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool real)
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
 }
 
-// A unit is a touched page, a head, and K or V. CTAs take units in turn; the inputs of the next one are under way
-// (each thread copies to shared memory what it will read itself) while one is worked on.
+// A unit is a touched page, a head, and K or V. A CTA takes consecutive ones, so that it seldom has to look for a page;
+// the inputs of the next one are under way (each thread copies to shared memory what it will read itself) while
+// one is worked on.
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) ssba_cache_append_kernel(const Pool pl, const Batch bt, const T* k,
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 2) ssba_cache_append_kernel(const Pool pl, const Batch bt, const T* k,
                                                                      const T* v)
 {
     constexpr int kN = Chunk<T>::n, kRowChunks = D / kN, kRows = kThreads / kRowChunks, kPass = kPage / kRows;
     extern __shared__ uint4 stage[];  // [kStages][kPass][kThreads]
     __shared__ int ends[kSeqs];
     __shared__ int buf[kWarps];
-    __shared__ float red[2][kWarps];
+    __shared__ uint32_t red[2][kWarps];
     __shared__ float sums[kWarps][D];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int row0 = tid / kRowChunks, c = tid % kRowChunks;
@@ -116,101 +153,86 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_append_kernel(const Pool 
     };
     int turn = 0, phase = 0;
     for (int b0 = 0; b0 < bt.B; b0 += kSeqs) {
-        const int pages = count_pages(bt, b0, pl.status, ends, buf);
-        const long long units = (long long)pages * pl.kv_heads * 2;
-        // unit u of this pass, its copies under way into stage st
-        auto begin = [&](long long u, int st) {
+        const int pages = count_pages(bt, b0, pl.status, ends, buf), each = 2 * pl.kv_heads;
+        const long long units = (long long)pages * each;
+        const bool small = units < INT_MAX / 65536;  // (32-bit division where it does)
+        long long u = small ? (int)units * (int)blockIdx.x / (int)gridDim.x : units * blockIdx.x / gridDim.x;
+        const long long u_end = small ? (int)units * (int)(blockIdx.x + 1) / (int)gridDim.x : units * (blockIdx.x + 1) / gridDim.x;
+        // the touched page that the next unit lies in, its sequence, and the unit's place among the page's
+        int pg = small ? (int)u / each : (int)(u / each), hv = (int)(u - (long long)pg * each), b = 0, page = -1, s0 = 0, s1 = 0;
+        ptrdiff_t first = 0;  // row of the page's slot 0
+        bool found = false;
+        {
+            int hi = kSeqs - 1;  // the first sequence with ends > pg
+            while (b < hi) {
+                const int mid = (b + hi) / 2;
+                if (ends[mid] > pg) hi = mid;
+                else b = mid + 1;
+            }
+        }
+        // the next unit, its copies under way into stage st
+        auto begin = [&](long long i, int st) {
             Unit x{0, 0, 0, false, false, 0.f};
-            if (u < units) {
-                const int pg = (int)(u / (2 * pl.kv_heads)), hv = (int)(u - (long long)pg * 2 * pl.kv_heads);
-                const int h = hv >> 1;
-                x.v = hv & 1;
-                int lo = 0, hi = kSeqs - 1;  // the first sequence with ends > pg
-                while (lo < hi) {
-                    const int mid = (lo + hi) / 2;
-                    if (ends[mid] > pg) hi = mid;
-                    else lo = mid + 1;
+            if (i < u_end) {
+                if (!found) {
+                    while (ends[b] <= pg) ++b;
+                    const Seq s = load_seq(bt, b0 + b, pl.status);
+                    const int j = s.len / kPage + pg - (b ? ends[b - 1] : 0), n = min(s.n, bt.width * kPage - s.len);
+                    page = page_of(bt, pl, b0 + b, j);
+                    s0 = max(s.len - j * kPage, 0);
+                    s1 = min(s.len + n - j * kPage, kPage);
+                    first = (ptrdiff_t)s.row + j * kPage - s.len;
+                    found = true;
                 }
-                const int b = b0 + lo;
-                const Seq s = load_seq(bt, b, pl.status);
-                const int j = s.len / kPage + pg - (lo ? ends[lo - 1] : 0);
-                const int page = page_of(bt, pl, b, j);
                 if (page >= 0) {
-                    const int n = min(s.n, bt.width * kPage - s.len);
+                    const int h = hv >> 1;
                     x.real = true;
-                    x.s0 = max(s.len - j * kPage, 0);
-                    x.s1 = min(s.len + n - j * kPage, kPage);
+                    x.v = hv & 1;
+                    x.s0 = s0;
+                    x.s1 = s1;
                     x.tile = (size_t)page * pl.kv_heads + h;
-                    if (x.s0 > 0) x.was = (x.v ? pl.v_scale : pl.k_scale)[x.tile];
-                    const T* src = (x.v ? v : k) + ((ptrdiff_t)(s.row + j * kPage - s.len) * pl.kv_heads + h) * D + c * kN;
+                    if (s0 > 0) x.was = (x.v ? pl.v_scale : pl.k_scale)[x.tile];
+                    const T* src = (x.v ? v : k) + (first * pl.kv_heads + h) * D + c * kN;
 #pragma unroll
                     for (int i = 0; i < kPass; ++i) {
                         const int slot = row0 + i * kRows;
-                        const bool in = slot >= x.s0 && slot < x.s1;
+                        const bool in = slot >= s0 && slot < s1;
                         copy16(static_cast<uint32_t>(__cvta_generic_to_shared(stage + (st * kPass + i) * kThreads + tid)),
                                in ? src + (ptrdiff_t)slot * pl.kv_heads * D : k, in);
                     }
+                }
+                if (++hv == each) {
+                    hv = 0;
+                    ++pg;
+                    found = false;
                 }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
             return x;
         };
-        Unit next = begin(blockIdx.x, turn % kStages);
-        for (long long u = blockIdx.x; u < units; u += gridDim.x, ++turn) {
+        Unit next = begin(u, turn % kStages);
+        for (; u < u_end; ++u, ++turn) {
             const Unit x = next;
-            next = begin(u + gridDim.x, (turn + 1) % kStages);
+            next = begin(u + 1, (turn + 1) % kStages);
             asm volatile("cp.async.wait_group 1;" ::: "memory");
             if (!x.real) continue;
             phase ^= 1;
             const uint4* in = stage + (turn % kStages) * kPass * kThreads + tid;
-            float amax = 0.f;
+            uint32_t top = 0;
+            bool odd = false;
 #pragma unroll
-            for (int i = 0; i < kPass; ++i) {
-                float f[kN];
-                Chunk<T>::get(in[i * kThreads], f);
-#pragma unroll
-                for (int e = 0; e < kN; ++e) {
-                    const float a = fabsf(f[e]);
-                    if (a < INFINITY) amax = fmaxf(amax, a);
-                }
-            }
-            amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
-            if (lane == 0) red[phase][warp] = amax;
+            for (int i = 0; i < kPass; ++i) top = Chunk<T>::largest(in[i * kThreads], top, odd);
+            const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(Chunk<T>::value(top)));
+            if (lane == 0) red[phase][warp] = most;
             __syncthreads();
-            amax = fmaxf(fmaxf(red[phase][0], red[phase][1]), fmaxf(red[phase][2], red[phase][3]));
+            const float amax = __uint_as_float(max(max(red[phase][0], red[phase][1]), max(red[phase][2], red[phase][3])));
             const float scale = fmaxf(x.was, scale_for(amax));
             const float inv = scale > 0.f ? 1.f / scale : 1.f;
             const float shrink = x.was < scale ? x.was * inv : 1.f;  // of the older bytes
             const bool full = !x.v && x.s1 == kPage;
             uint8_t* dst = (x.v ? pl.V : pl.K) + x.tile * kPage * D + c * kN;
             float sum[kN] = {};
-#pragma unroll
-            for (int i = 0; i < kPass; ++i) {
-                const int slot = row0 + i * kRows;
-                uint32_t* at = reinterpret_cast<uint32_t*>(dst + slot * D);
-                uint32_t w[kN / 4];
-                if (slot >= x.s0 && slot < x.s1) {
-                    float f[kN];
-                    Chunk<T>::get(in[i * kThreads], f);
-#pragma unroll
-                    for (int e = 0; e < kN; e += 4) {
-                        float y[4];
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) y[r] = fabsf(f[e + r]) < INFINITY ? f[e + r] * inv : NAN;
-                        w[e / 4] = to_e4m3x2(y[0], y[1]) | (to_e4m3x2(y[2], y[3]) << 16);
-                    }
-                } else if (slot < x.s0 && (full || shrink != 1.f)) {
-#pragma unroll
-                    for (int e = 0; e < kN / 4; ++e) {
-                        w[e] = at[e];
-                        float y[4];
-                        from_e4m3x4(w[e], y);
-                        if (shrink != 1.f)
-                            w[e] = to_e4m3x2(y[0] * shrink, y[1] * shrink) | (to_e4m3x2(y[2] * shrink, y[3] * shrink) << 16);
-                    }
-                } else {
-                    continue;
-                }
+            auto put = [&](uint32_t* at, const uint32_t* w) {
                 if (kN == 8) *reinterpret_cast<uint2*>(at) = make_uint2(w[0], w[kN / 4 - 1]);
                 else at[0] = w[0];
                 if (full) {
@@ -221,6 +243,46 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_append_kernel(const Pool 
 #pragma unroll
                         for (int r = 0; r < 4; ++r) sum[e + r] += y[r];
                     }
+                }
+            };
+            if (x.s0 == 0 && x.s1 == kPage && !odd) {  // a whole page, as most of a prompt's are
+#pragma unroll
+                for (int i = 0; i < kPass; ++i) {
+                    uint32_t w[kN / 4];
+                    Chunk<T>::template round<false>(in[i * kThreads], inv, w);
+                    put(reinterpret_cast<uint32_t*>(dst + (row0 + i * kRows) * D), w);
+                }
+            } else {
+                // older bytes, where they are needed, all under way at once
+                const bool older = full || shrink != 1.f;
+                uint32_t w[kPass][kN / 4];
+#pragma unroll
+                for (int i = 0; i < kPass; ++i) {
+                    const int slot = row0 + i * kRows;
+                    const uint32_t* at = reinterpret_cast<const uint32_t*>(dst + slot * D);
+                    if (older && slot < x.s0) {
+#pragma unroll
+                        for (int e = 0; e < kN / 4; ++e) w[i][e] = at[e];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < kPass; ++i) {
+                    const int slot = row0 + i * kRows;
+                    if (slot >= x.s0 && slot < x.s1) {
+                        Chunk<T>::template round<true>(in[i * kThreads], inv, w[i]);
+                    } else if (older && slot < x.s0) {
+                        if (shrink != 1.f) {
+#pragma unroll
+                            for (int e = 0; e < kN / 4; ++e) {
+                                float y[4];
+                                from_e4m3x4(w[i][e], y);
+                                w[i][e] = to_e4m3x2(y[0] * shrink, y[1] * shrink) | (to_e4m3x2(y[2] * shrink, y[3] * shrink) << 16);
+                            }
+                        }
+                    } else {
+                        continue;
+                    }
+                    put(reinterpret_cast<uint32_t*>(dst + slot * D), w[i]);
                 }
             }
             if (tid == 0) (x.v ? pl.v_scale : pl.k_scale)[x.tile] = scale;

@@ -320,10 +320,10 @@ int select_as(const Pool& pl, const Batch& bt, const void* q, int keep, int firs
     once.run([&] {
         cudaFuncSetAttribute(ssba_cache_select_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSelectSmem);
     });
-    // CTAs a row: enough rows in flight to fill the SMs, and no share of fewer than 32 pages
+    // CTAs a row: as many as run at once (four an SM), and no share of fewer than 32 pages
     const long long rows = (long long)bt.T * pl.kv_heads;
     int ranks = 1;
-    while (ranks < 8 && rows * ranks < 4LL * device_sm_count() && bt.width > 64 * ranks) ranks *= 2;
+    while (ranks < 8 && 2 * rows * ranks <= 4LL * device_sm_count() && bt.width > 64 * ranks) ranks *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(bt.T * ranks, pl.kv_heads, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
