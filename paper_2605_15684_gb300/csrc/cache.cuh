@@ -61,6 +61,10 @@ __device__ __forceinline__ int visible(const Seq& s, int t, int* status)
 // Called by whole warps: 32 entries are compared at a time, so that a batch of 1024 takes two rounds.
 __device__ __forceinline__ int find_seq(const Batch& bt, int t, int lane)
 {
+    if (t < bt.B) {  // most batches have one row a sequence: then this is it
+        const int c0 = __ldg(bt.cu + t), c1 = __ldg(bt.cu + t + 1);
+        if (c0 <= t && t < c1) return t;
+    }
     if (t < __ldg(bt.cu) || t >= __ldg(bt.cu + bt.B)) return -1;
     int lo = 0, n = bt.B;  // the answer lies in [lo, lo + n)
     while (n > 1) {
@@ -129,9 +133,9 @@ int launch_cache_copy(const cache::Pool& pl, int head_dim, const int32_t* src, c
 int launch_cache_select(const cache::Pool& pl, const cache::Batch& bt, int head_dim, int dtype, const void* q,
                         int keep, int first, int32_t* idx, int32_t* cnt, cudaStream_t st);
 // idx null: every page of the sequence; else [T][kv_heads][keep] with cnt [T][kv_heads].
-int launch_cache_attend_simt(const cache::Pool& pl, const cache::Batch& bt, int head_dim, int dtype, float scale,
-                             const void* q, const int32_t* idx, const int32_t* cnt, int keep, void* O, float* lse,
-                             void* ws, cudaStream_t st);
+int launch_cache_attend_simt(const cache::Pool& pl, const cache::Batch& bt, int head_dim, float scale, const void* q,
+                             const int32_t* idx, const int32_t* cnt, int keep, void* O, float* lse, void* ws,
+                             cudaStream_t st);
 size_t cache_attend_simt_workspace();
 int launch_cache_attend_tc(const cache::Pool& pl, const cache::Batch& bt, int head_dim, float scale, const void* q,
                            const int32_t* idx, const int32_t* cnt, int keep, void* O, float* lse, void* ws,

@@ -195,7 +195,7 @@ int ssba_cache_attend(const ssba_cache_desc* desc, const ssba_cache* cache, cons
         if (!idx && rows > 32) return launch_cache_attend_rows(p, bt, desc->head_dim, scale, q, O, lse, workspace, st);
         return launch_cache_attend_tc(p, bt, desc->head_dim, scale, q, idx, cnt, keep, O, lse, workspace, st);
     }
-    return launch_cache_attend_simt(p, bt, desc->head_dim, desc->dtype, scale, q, idx, cnt, keep, O, lse, workspace, st);
+    return launch_cache_attend_simt(p, bt, desc->head_dim, scale, q, idx, cnt, keep, O, lse, workspace, st);
 }
 
 int ssba_cache_copy(const ssba_cache_desc* desc, const ssba_cache* cache, const int32_t* src, const int32_t* dst,

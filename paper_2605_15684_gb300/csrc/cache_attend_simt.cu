@@ -1,4 +1,4 @@
-// cache_attend_simt.cu -- attention over the paged 8-bit cache on the CUDA cores, in fp32.
+// cache_attend_simt.cu -- attention over the paged 8-bit cache on the CUDA cores, for fp32 queries.
 //
 //   s = scale * k_scale * (q . byte values of k),  O = sum softmax(s) * v_scale * byte values of v
 // over the tokens that a row sees, in all pages of its sequence or in listed ones.
@@ -13,33 +13,29 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kHeads = 8;      // query heads that a CTA takes together
+constexpr int kHeads = 8;      // query heads that a CTA takes together at most
 constexpr int kMaxParts = 608;  // CTAs that write partial results at most: four an SM
-
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ void store(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// One CTA: row t, up to 8 heads of one group, and one of `parts` shares of its pages. A warp takes whole
+// One CTA: row t, up to H heads of one group (1, 2, 4 or 8, by the group's size: a head costs 2 D multiply-adds a
+// token whether it is there or not), and one of `parts` shares of its pages. A warp takes whole
 // pages: a lane scores two tokens (their K rows in 16-byte loads, q broadcast from shared memory), then owns D / 32
 // channels of O over the page's V rows. The warps' results are joined at the end; shares through the workspace.
-template <typename T, int D>
+template <int D, int H>
 __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
-    const Pool pl, const Batch bt, const T* q, const int32_t* idx, const int32_t* cnt, int keep, float scale_log2,
-    T* O, float* lse, float* ws, int parts, int chunks)
+    const Pool pl, const Batch bt, const float* q, const int32_t* idx, const int32_t* cnt, int keep, float scale_log2,
+    float* O, float* lse, float* ws, int parts, int chunks)
 {
     constexpr int kC = D / 32;  // channels of a lane
-    __shared__ float qs[kHeads][D];
-    __shared__ float ps[kWarps][kPage][kHeads];
-    __shared__ float ms[kWarps][kHeads], ls[kWarps][kHeads];
+    __shared__ __align__(16) float qs[H][D];
+    __shared__ __align__(16) float ps[kWarps][kPage][H];
+    __shared__ float ms[kWarps][H], ls[kWarps][H];
     const int t = blockIdx.x, part = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int h = blockIdx.y / chunks, chunk = blockIdx.y % chunks;
     const int b = find_seq(bt, t, lane);
     if (b < 0) return;
-    const int G = pl.heads / pl.kv_heads, g0 = chunk * kHeads, ng = min(kHeads, G - g0);
+    const int G = pl.heads / pl.kv_heads, g0 = chunk * H, ng = min(H, G - g0);
     const size_t head0 = (size_t)t * pl.heads + h * G + g0;
     const Seq s = load_seq(bt, b, pl.status);
     const int L = visible(s, t, pl.status);
@@ -53,12 +49,12 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
             n = min(max(n, 0), keep);
         }
     }
-    for (int i = tid; i < kHeads * D; i += kThreads)
-        qs[i / D][i % D] = i / D < ng ? to_float(q[head0 * D + i]) : 0.f;
+    for (int i = tid; i < H * D; i += kThreads)
+        qs[i / D][i % D] = i / D < ng ? q[head0 * D + i] : 0.f;
     __syncthreads();
-    float m[kHeads], l[kHeads], o[kHeads][kC];
+    float m[H], l[H], o[H][kC];
 #pragma unroll
-    for (int g = 0; g < kHeads; ++g) {
+    for (int g = 0; g < H; ++g) {
         m[g] = -INFINITY;
         l[g] = 0.f;
 #pragma unroll
@@ -80,7 +76,7 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
         const float ks = __ldg(pl.k_scale + unit) * scale_log2, vs = __ldg(pl.v_scale + unit);
         const uint8_t* K = pl.K + unit * kPage * D;
         const uint8_t* V = pl.V + unit * kPage * D;
-        float a[2][kHeads] = {};
+        float a[2][H] = {};
 #pragma unroll 1
         for (int c = 0; c < D; c += 16) {
             uint4 kk[2];
@@ -92,7 +88,7 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
                 from_e4m3x4((&kk[0].x)[e], f[0]);
                 from_e4m3x4((&kk[1].x)[e], f[1]);
 #pragma unroll
-                for (int g = 0; g < kHeads; ++g) {
+                for (int g = 0; g < H; ++g) {
                     const float4 x = *reinterpret_cast<const float4*>(&qs[g][c + 4 * e]);
 #pragma unroll
                     for (int u = 0; u < 2; ++u)
@@ -102,7 +98,7 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
         }
         __syncwarp();
 #pragma unroll
-        for (int g = 0; g < kHeads; ++g) {
+        for (int g = 0; g < H; ++g) {
             const float s0 = lane < nt ? a[0][g] * ks : -INFINITY, s1 = lane + 32 < nt ? a[1][g] * ks : -INFINITY;
             float top = fmaxf(s0, s1);
 #pragma unroll
@@ -129,21 +125,16 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
                 f[1] = y.y;
             }
 #pragma unroll
-            for (int g = 0; g < kHeads; g += 4) {
-                const float4 x = *reinterpret_cast<const float4*>(&ps[warp][r][g]);
+            for (int g = 0; g < H; ++g) {
+                const float x = ps[warp][r][g];
 #pragma unroll
-                for (int c = 0; c < kC; ++c) {
-                    o[g][c] = fmaf(x.x, f[c], o[g][c]);
-                    o[g + 1][c] = fmaf(x.y, f[c], o[g + 1][c]);
-                    o[g + 2][c] = fmaf(x.z, f[c], o[g + 2][c]);
-                    o[g + 3][c] = fmaf(x.w, f[c], o[g + 3][c]);
-                }
+                for (int c = 0; c < kC; ++c) o[g][c] = fmaf(x, f[c], o[g][c]);
             }
         }
     }
-    // join the warps, one head after another through shared memory (ps is free: 64 x 8 floats a warp hold D)
+    // join the warps, two heads at a time through shared memory
 #pragma unroll
-    for (int g = 0; g < kHeads; ++g) {
+    for (int g = 0; g < H; ++g) {
         float lg = l[g];
 #pragma unroll
         for (int d = 16; d; d >>= 1) lg += __shfl_xor_sync(0xffffffffu, lg, d);
@@ -153,15 +144,16 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
         }
     }
     __syncthreads();
-    float* po = &ps[0][0][0];  // [kWarps][2][D] at a time
+    constexpr int kP = H < 2 ? 1 : 2;
+    __shared__ float po[kWarps * kP * D];  // heads gp .. gp + kP - 1 of the warps
 #pragma unroll
-    for (int gp = 0; gp < kHeads; gp += 2) {
+    for (int gp = 0; gp < H; gp += kP) {
 #pragma unroll
-        for (int g = gp; g < gp + 2; ++g)
+        for (int g = gp; g < gp + kP; ++g)
 #pragma unroll
-            for (int c = 0; c < kC; ++c) po[(warp * 2 + g - gp) * D + lane * kC + c] = o[g][c];
+            for (int c = 0; c < kC; ++c) po[(warp * kP + g - gp) * D + lane * kC + c] = o[g][c];
         __syncthreads();
-        for (int i = tid; i < 2 * D; i += kThreads) {
+        for (int i = tid; i < kP * D; i += kThreads) {
             const int g = gp + i / D, c = i % D;
             if (g < ng) {
                 float top = -INFINITY, lt = 0.f, ot = 0.f;
@@ -170,13 +162,13 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
                 for (int w = 0; w < kWarps; ++w) {
                     const float f = exp2f(ms[w][g] - ref);
                     lt += ls[w][g] * f;
-                    ot += po[(w * 2 + g - gp) * D + c] * f;
+                    ot += po[(w * kP + g - gp) * D + c] * f;
                 }
                 if (parts == 1) {
-                    store(O + (head0 + g) * D + c, lt != 0.f ? ot / lt : 0.f);
+                    O[(head0 + g) * D + c] = lt != 0.f ? ot / lt : 0.f;
                     if (c == 0) lse[head0 + g] = (ref + log2f(lt)) * kLn2;
                 } else {
-                    float* w = ws + (((size_t)blockIdx.x * gridDim.y + blockIdx.y) * parts + part) * kHeads * (D + 2) + g * (D + 2);
+                    float* w = ws + (((size_t)blockIdx.x * gridDim.y + blockIdx.y) * parts + part) * H * (D + 2) + g * (D + 2);
                     w[c] = ot;
                     if (c == 0) {
                         w[D] = top;
@@ -190,15 +182,15 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
 }
 
 // Joins the shares of one head of one row, in order.
-template <typename T, int D>
-__global__ void __launch_bounds__(D) ssba_cache_join_kernel(const Pool pl, const Batch bt, const float* ws, T* O,
-                                                            float* lse, int parts, int chunks)
+template <int D>
+__global__ void __launch_bounds__(D) ssba_cache_join_kernel(const Pool pl, const Batch bt, const float* ws, float* O,
+                                                            float* lse, int parts, int chunks, int H)
 {
     const int t = blockIdx.x, h = blockIdx.y / chunks, chunk = blockIdx.y % chunks, g = blockIdx.z, c = threadIdx.x;
-    const int G = pl.heads / pl.kv_heads, gg = chunk * kHeads + g;
+    const int G = pl.heads / pl.kv_heads, gg = chunk * H + g;
     if (gg >= G || find_seq(bt, t, c & 31) < 0) return;
-    const float* w = ws + ((size_t)blockIdx.x * gridDim.y + blockIdx.y) * parts * kHeads * (D + 2) + g * (D + 2);
-    const size_t step = (size_t)kHeads * (D + 2);
+    const float* w = ws + ((size_t)blockIdx.x * gridDim.y + blockIdx.y) * parts * H * (D + 2) + g * (D + 2);
+    const size_t step = (size_t)H * (D + 2);
     float top = -INFINITY, l = 0.f, o = 0.f;
     for (int i = 0; i < parts; ++i) top = fmaxf(top, w[i * step + D]);
     const float ref = top == -INFINITY ? 0.f : top;
@@ -208,31 +200,41 @@ __global__ void __launch_bounds__(D) ssba_cache_join_kernel(const Pool pl, const
         o += w[i * step + c] * f;
     }
     const size_t head = (size_t)t * pl.heads + h * G + gg;
-    store(O + head * D + c, l != 0.f ? o / l : 0.f);
+    O[head * D + c] = l != 0.f ? o / l : 0.f;
     if (c == 0) lse[head] = (ref + log2f(l)) * kLn2;
 }
 
-template <typename T, int D>
+template <int D, int H>
 int attend_as(const Pool& pl, const Batch& bt, float scale, const void* q, const int32_t* idx, const int32_t* cnt,
               int keep, void* O, float* lse, void* ws, cudaStream_t st)
 {
-    const int G = pl.heads / pl.kv_heads, chunks = (G + kHeads - 1) / kHeads;
+    const int G = pl.heads / pl.kv_heads, chunks = (G + H - 1) / H;
     float* parts_at = reinterpret_cast<float*>(static_cast<char*>(ws) + SSBA_CACHE_TICKET_BYTES);
     const long long items = (long long)bt.T * pl.kv_heads * chunks;
     const int pages = idx ? keep : bt.width;
     // shares: as many as give the SMs work, none of fewer than a page a warp
     const int parts = (int)std::max<long long>(1, std::min<long long>(kMaxParts / std::max<long long>(items, 1), (pages + kWarps - 1) / kWarps));
     const dim3 grid(bt.T, pl.kv_heads * chunks, parts);
-    ssba_cache_attend_simt_kernel<T, D><<<grid, kThreads, 0, st>>>(pl, bt, static_cast<const T*>(q), idx, cnt, keep,
-                                                                  scale * kLog2e, static_cast<T*>(O), lse,
-                                                                  parts_at, parts, chunks);
+    ssba_cache_attend_simt_kernel<D, H><<<grid, kThreads, 0, st>>>(pl, bt, static_cast<const float*>(q), idx, cnt, keep,
+                                                                     scale * kLog2e, static_cast<float*>(O), lse, parts_at,
+                                                                     parts, chunks);
     if (parts > 1)
-        ssba_cache_join_kernel<T, D><<<dim3(bt.T, pl.kv_heads * chunks, kHeads), D, 0, st>>>(
-            pl, bt, parts_at, static_cast<T*>(O), lse, parts, chunks);
+        ssba_cache_join_kernel<D><<<dim3(bt.T, pl.kv_heads * chunks, H), D, 0, st>>>(pl, bt, parts_at, static_cast<float*>(O),
+                                                                                       lse, parts, chunks, H);
     const cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess) return SSBA_OK;
     set_error("ssba_cache_attend: %s", cudaGetErrorString(e));
     return SSBA_ERR_CUDA;
+}
+
+template <int D, class... A>
+int attend_heads(const Pool& pl, A... a)
+{
+    const int G = pl.heads / pl.kv_heads;
+    if (G == 1) return attend_as<D, 1>(pl, a...);
+    if (G == 2) return attend_as<D, 2>(pl, a...);
+    if (G <= 4) return attend_as<D, 4>(pl, a...);
+    return attend_as<D, 8>(pl, a...);
 }
 
 }  // namespace
@@ -243,16 +245,12 @@ size_t cache_attend_simt_workspace()
     return SSBA_CACHE_TICKET_BYTES + (size_t)cache::kMaxParts * cache::kHeads * (128 + 2) * sizeof(float);
 }
 
-int launch_cache_attend_simt(const cache::Pool& pl, const cache::Batch& bt, int head_dim, int dtype, float scale,
-                             const void* q, const int32_t* idx, const int32_t* cnt, int keep, void* O, float* lse,
-                             void* ws, cudaStream_t st)
+int launch_cache_attend_simt(const cache::Pool& pl, const cache::Batch& bt, int head_dim, float scale, const void* q,
+                             const int32_t* idx, const int32_t* cnt, int keep, void* O, float* lse, void* ws,
+                             cudaStream_t st)
 {
-    if (dtype == SSBA_BF16)
-        return head_dim == 64
-                   ? cache::attend_as<__nv_bfloat16, 64>(pl, bt, scale, q, idx, cnt, keep, O, lse, ws, st)
-                   : cache::attend_as<__nv_bfloat16, 128>(pl, bt, scale, q, idx, cnt, keep, O, lse, ws, st);
-    return head_dim == 64 ? cache::attend_as<float, 64>(pl, bt, scale, q, idx, cnt, keep, O, lse, ws, st)
-                          : cache::attend_as<float, 128>(pl, bt, scale, q, idx, cnt, keep, O, lse, ws, st);
+    return head_dim == 64 ? cache::attend_heads<64>(pl, bt, scale, q, idx, cnt, keep, O, lse, ws, st)
+                          : cache::attend_heads<128>(pl, bt, scale, q, idx, cnt, keep, O, lse, ws, st);
 }
 
 }  // namespace ssba
