@@ -17,7 +17,7 @@ namespace ssba {
 namespace cache {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
 
 __device__ __forceinline__ float to_float(float x) { return x; }
@@ -48,7 +48,7 @@ __device__ __forceinline__ int block_prefix(int v, int* buf, int& total)
     return before;
 }
 
-constexpr int kBins = 1024, kCand = 256, kSlice = 512;
+constexpr int kBins = 1024, kCand = kThreads, kSlice = 512;
 
 struct Scratch {
     int hist[kBins];
@@ -77,10 +77,16 @@ __device__ void select_radix(const float* score, int n, int want, int first, int
         }
         __syncthreads();
         int total;
-        const int c = sc.hist[255 - tid], over = block_prefix(c, sc.buf, total);  // keys of higher digits
-        if (over < left && over + c >= left) {
-            sc.pick[0] = 255 - tid;
-            sc.pick[1] = left - over;
+        const int c1 = sc.hist[255 - 2 * tid], c0 = sc.hist[254 - 2 * tid];
+        int over = block_prefix(c1 + c0, sc.buf, total);  // keys of higher digits
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int c = e ? c0 : c1;
+            if (over < left && over + c >= left) {
+                sc.pick[0] = 255 - 2 * tid - e;
+                sc.pick[1] = left - over;
+            }
+            over += c;
         }
         __syncthreads();
         prefix |= static_cast<uint32_t>(sc.pick[0]) << shift;
@@ -320,10 +326,10 @@ int select_as(const Pool& pl, const Batch& bt, const void* q, int keep, int firs
     once.run([&] {
         cudaFuncSetAttribute(ssba_cache_select_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSelectSmem);
     });
-    // CTAs a row: as many as run at once (four an SM), and no share of fewer than 32 pages
+    // CTAs a row: as many as run at once (eight an SM), and no share of fewer than 32 pages
     const long long rows = (long long)bt.T * pl.kv_heads;
     int ranks = 1;
-    while (ranks < 8 && 2 * rows * ranks <= 4LL * device_sm_count() && bt.width > 64 * ranks) ranks *= 2;
+    while (ranks < 8 && 2 * rows * ranks <= 8LL * device_sm_count() && bt.width > 64 * ranks) ranks *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(bt.T * ranks, pl.kv_heads, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
