@@ -43,17 +43,15 @@ constexpr int kMeta = 32;            // pages of a meta chunk
 constexpr float kTop = 8.f;          // log2 of a tile's largest P: 2^8 < 448
 enum Role { kLoad = 0, kIssue = 1, kLoadQ = 2, kLoadMeta = 3 };
 
-constexpr size_t kPartFloats = (size_t)16 * 130 * 2 * kMaxGrid;  // two parts a CTA of 16 rows (half as many CTAs of 32)
+constexpr size_t kPartFloats = (size_t)16 * (128 + 2) * 2 * kMaxGrid;  // two parts a CTA of up to 16 rows
 
 template <int R, int D>
 struct Cfg {
     static constexpr int N = 2 * R;
-    static constexpr int kCtas = R <= 16 ? 2 : 1;  // of an SM
+    static constexpr int kCtas = 2;  // of an SM
     static constexpr uint32_t kSlotBytes = kTile * D;
-    static constexpr int kSlots = (R == 8 ? 96 : R == 16 ? 80 : 160) * 1024 / kSlotBytes > 12
-                                      ? 12
-                                      : (R == 8 ? 96 : R == 16 ? 80 : 160) * 1024 / kSlotBytes;
-    static constexpr uint32_t kTmemCols = 4 * N < 32 ? 32 : 4 * N;
+    static constexpr int kRing = (R == 8 ? 96 : 80) * 1024 / kSlotBytes, kSlots = kRing < 12 ? kRing : 12;
+    static constexpr uint32_t kTmemCols = 4 * N;
     static constexpr uint32_t kColS = 0, kColO = 2 * N;  // two buffers of N each
     static constexpr uint32_t kIdescQK = idesc_e4m3_f32(128, N, false, false);
     static constexpr uint32_t kIdescPV = idesc_e4m3_f32(128, N, true, true);
@@ -686,8 +684,7 @@ int launch(const Maps& maps, const Params& p, cudaStream_t st)
     once.run([smem] {
         cudaFuncSetAttribute(ssba_cache_attend_tc_kernel<R, D, kList>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     });
-    const int most = kMaxGrid / (R <= 16 ? 1 : 2);
-    const int grid = std::min(device_sm_count() * C::kCtas, most);
+    const int grid = std::min(device_sm_count() * C::kCtas, kMaxGrid);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid, 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
@@ -744,18 +741,16 @@ int launch_cache_attend_tc(const cache::Pool& pl, const cache::Batch& bt, int he
     p.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + SSBA_CACHE_TICKET_BYTES);
     p.G = pl.heads / pl.kv_heads;
     p.budget_ns = kWaitBudgetNs;
-    // rows of an item: a group's heads, of several tokens where the sequences have them
-    const int most = 32;
+    // rows of an item: a group's heads, of several tokens where the sequences have them (16 rows cost the
+    // softmax warps twice what 8 do: 16 sequences of up to 8000 tokens 37 us with 8 rows, 62 with 16)
     const long long each = idx ? 1 : ((long long)bt.T + bt.B - 1) / bt.B;  // rows of a sequence, on average
-    const long long want = std::min<long long>((long long)p.G * each, most);
-    const int R = want <= 8 ? 8 : want <= 16 ? 16 : 32;
+    const int R = (long long)p.G * each <= 8 ? 8 : 16;
     p.chunks = (p.G + R - 1) / R;
     p.gc = (p.G + p.chunks - 1) / p.chunks;
     p.gc_inv = (65536 + p.gc - 1) / p.gc;
     p.tq = 1;
     while (!idx && 2 * p.tq * p.gc <= R) p.tq *= 2;
-    return R == 8 ? launch_rows<8>(maps, p, head_dim, st)
-                  : R == 16 ? launch_rows<16>(maps, p, head_dim, st) : launch_rows<32>(maps, p, head_dim, st);
+    return R == 8 ? launch_rows<8>(maps, p, head_dim, st) : launch_rows<16>(maps, p, head_dim, st);
 }
 
 }  // namespace ssba
