@@ -384,7 +384,8 @@ SSBA_API int ssba_test_backward_late(const ssba_desc* desc, const void* Q, const
  *
  * Shapes and rules shared by the calls below
  *   Pool       ssba_cache: K, V e4m3 [pages][kv_heads][64][head_dim], k_scale, v_scale fp32
- *              [pages][kv_heads] (value = e4m3 value * scale), k_mean fp32 [pages][kv_heads][head_dim]
+ *              [pages][kv_heads] (value = e4m3 value * scale; powers of two or 0, as
+ *              ssba_cache_append writes them), k_mean fp32 [pages][kv_heads][head_dim]
  *              (mean key of every full page). Device memory of the caller's; needs no initial contents.
  *   Batch      B sequences and T rows. Rows [cu[b], cu[b + 1]) are the new tokens of sequence b (cu int32
  *              [B + 1], ascending, none may be negative or above T); rows from cu[B] on belong to none and
@@ -470,6 +471,18 @@ SSBA_API int ssba_cache_attend(const ssba_cache_desc* desc, const ssba_cache* ca
                                const int32_t* table, int32_t width, const int32_t* lens, const int32_t* cu,
                                int32_t B, const int32_t* idx, const int32_t* cnt, int32_t keep, void* O, float* lse,
                                void* workspace, size_t ws_bytes, void* stream);
+
+/* Test hook for failure detection in the cache's attention: runs ssba_cache_attend over all pages (bf16) with every wait
+ * limited to budget_ns of wall time (clamped to [1 ms, 2 s]) and CTA 0 announcing its first tile's copies without
+ * issuing them, so that the waits on them run out. That CTA stops all its roles, waits (bounded) for its own
+ * copies and MMAs in flight, frees its tensor memory and returns; the others finish their shares. The device
+ * status word reads SSBA_ERR_TIMEOUT (ssba_get_status, after a synchronize), O and lse are undefined, the workspace's
+ * first SSBA_CACHE_TICKET_BYTES have to be zeroed again, and the context stays usable. No fault, trap or endless
+ * wait is involved. Arguments as ssba_cache_attend; bf16 only, and at least one row with a page. */
+SSBA_API int ssba_test_cache_timeout(const ssba_cache_desc* desc, const ssba_cache* cache, const void* q, int32_t T,
+                                     const int32_t* table, int32_t width, const int32_t* lens, const int32_t* cu,
+                                     int32_t B, void* O, float* lse, void* workspace, size_t ws_bytes,
+                                     uint64_t budget_ns, void* stream);
 
 /* Copies whole pages of the pool: page src[i] to page dst[i] (device, int32 [n]), with scales and mean
  * keys. No page may be among dst twice, or both among src and dst. */

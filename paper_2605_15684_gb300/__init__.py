@@ -13,7 +13,8 @@ from .api import (  # noqa: F401
     select_mask,
 )
 from .cache import (  # noqa: F401
-    Cache, CacheDesc, cache_alloc, cache_append, cache_attend, cache_attend_workspace_bytes, cache_copy, cache_select,
+    Cache, CacheDesc, CacheStep, PagedCache, PageTable, cache_alloc, cache_append, cache_attend,
+    cache_attend_workspace_bytes, cache_copy, cache_select,
 )
 
 __all__ = [
@@ -22,6 +23,6 @@ __all__ = [
     "forward_joint", "forward_select", "forward_workspace_bytes", "get_status", "haar_dwt", "haar_dwt_pyramid",
     "haar_iwt", "haar_iwt_pyramid", "keep_count", "library_path", "load_library", "mask_workspace_bytes",
     "pool_blocks", "qkv_rope_pool", "realized_sparsity", "select_mask",
-    "Cache", "CacheDesc", "cache_alloc", "cache_append", "cache_attend", "cache_attend_workspace_bytes",
+    "Cache", "CacheDesc", "CacheStep", "PagedCache", "PageTable", "cache_alloc", "cache_append", "cache_attend", "cache_attend_workspace_bytes",
     "cache_copy", "cache_select",
 ]

@@ -34,7 +34,7 @@ EXPORTED = ("ssba_keep_count", "ssba_mask_workspace_bytes", "ssba_build_mask", "
             "ssba_haar_iwt", "ssba_haar_dwt_pyramid", "ssba_haar_iwt_pyramid", "ssba_qkv_rope_pool",
             "ssba_select_mask", "ssba_pool_blocks", "ssba_forward_select", "ssba_forward_fused",
             "ssba_cache_append", "ssba_cache_select", "ssba_cache_attend_workspace_bytes", "ssba_cache_attend",
-            "ssba_cache_copy", "ssba_get_status", "ssba_last_error", "ssba_timeline_read")
+            "ssba_cache_copy", "ssba_test_cache_timeout", "ssba_get_status", "ssba_last_error", "ssba_timeline_read")
 
 
 class SsbaError(RuntimeError):
@@ -168,8 +168,9 @@ def load_library(path: str | None = None):
         lib.ssba_cache_select.argtypes = [CP, P, P, I, *batch, I, I, P, P, P]
         lib.ssba_cache_attend.argtypes = [CP, P, P, I, *batch, P, P, I, P, P, P, ctypes.c_size_t, P]
         lib.ssba_cache_copy.argtypes = [CP, P, P, P, I, P]
-        for fn in ("append", "select", "attend", "copy"):
-            getattr(lib, "ssba_cache_" + fn).restype = ctypes.c_int
+        lib.ssba_test_cache_timeout.argtypes = [CP, P, P, I, *batch, P, P, P, ctypes.c_size_t, ctypes.c_uint64, P]
+        for fn in ("cache_append", "cache_select", "cache_attend", "cache_copy", "test_cache_timeout"):
+            getattr(lib, "ssba_" + fn).restype = ctypes.c_int
         lib.ssba_cache_attend_workspace_bytes.argtypes = [CP]
         lib.ssba_cache_attend_workspace_bytes.restype = ctypes.c_size_t
         lib.ssba_get_status.argtypes = [ctypes.POINTER(ctypes.c_int32)]
@@ -732,11 +733,17 @@ def haar_iwt_pyramid(ys, C: int, nb: int = 4, x=None, stream=None) -> torch.Tens
     return x
 
 
+_timed_out: list = []  # called when a timeout has been read: what a launch that gave up leaves unusable
+
+
 def get_status() -> int:
     """ssba_get_status: read-and-clear the device status word (call after a sync)."""
     lib = load_library()
     v = ctypes.c_int32(0)
     _raise_on(lib.ssba_get_status(ctypes.byref(v)))
+    if v.value == SSBA_ERR_TIMEOUT:
+        for drop in _timed_out:
+            drop()
     return int(v.value)
 
 

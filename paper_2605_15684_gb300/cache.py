@@ -200,6 +200,7 @@ def cache_attend_workspace_bytes(desc: CacheDesc) -> int:
 
 
 _ws: dict = {}
+api._timed_out.append(_ws.clear)  # counters that a timeout has left set
 _ws_need: dict = {}  # per device: the same for every descriptor
 
 
@@ -262,6 +263,21 @@ def cache_attend(desc: CacheDesc, cache: Cache, q, table, lens, cu, idx=None, cn
     return O, lse
 
 
+def test_cache_timeout(desc: CacheDesc, cache: Cache, q, table, lens, cu, O, lse, workspace, budget_ns: int = 2_000_000,
+                       stream=None) -> None:
+    """ssba_test_cache_timeout: the attention's failure-detection test hook (include/ssba.h)."""
+    lib = load_library()
+    pl = _plan(desc)
+    dev = _pool(pl, cache)
+    T = _rows(q, "q", pl.heads, pl, dev)
+    batch = _batch(table, lens, cu, dev)
+    _on(O, "O", q.shape, pl.dtype, dev)
+    _on(lse, "lse", (T, pl.heads), torch.float32, dev)
+    wp, wn = api._ws_args(workspace)
+    _raise_on(lib.ssba_test_cache_timeout(pl.ref, cache._ref, q.data_ptr(), T, *batch, O.data_ptr(), lse.data_ptr(), wp,
+                                          wn, int(budget_ns), _stream_ptr(stream)))
+
+
 def cache_copy(desc: CacheDesc, cache: Cache, src, dst, stream=None) -> Cache:
     """ssba_cache_copy: pages src[i] -> dst[i], int32 CUDA tensors [n]. Returns the cache."""
     lib = api._lib or load_library()
@@ -272,3 +288,211 @@ def cache_copy(desc: CacheDesc, cache: Cache, src, dst, stream=None) -> Cache:
     _on(dst, "dst", (max(n, 0),), torch.int32, dev)
     _raise_on(lib.ssba_cache_copy(pl.ref, cache._ref, src.data_ptr(), dst.data_ptr(), n, _stream_ptr(stream)))
     return cache
+
+
+class PageTable:
+    """Which pages hold which sequence: the host's bookkeeping of one pool, without any tensor. A page belongs to one
+    sequence or is shared by the forks of one; a shared page is copied before one of them writes to it."""
+
+    def __init__(self, pages: int):
+        if pages <= 0:
+            raise SsbaError(SSBA_ERR_INVALID, f"pages={pages} must be positive")
+        self.pages = pages
+        self._free = list(range(pages - 1, -1, -1))  # taken from the end: low pages first
+        self._users = [0] * pages
+        self._seqs: dict = {}  # id -> [pages, tokens]
+        self._next = 0
+
+    @property
+    def free_pages(self) -> int:
+        return len(self._free)
+
+    @property
+    def sequences(self):
+        return list(self._seqs)
+
+    def _seq(self, seq: int):
+        if seq not in self._seqs:
+            raise SsbaError(SSBA_ERR_INVALID, f"no sequence {seq}")
+        return self._seqs[seq]
+
+    def length(self, seq: int) -> int:
+        """Tokens of a sequence."""
+        return self._seq(seq)[1]
+
+    def pages_of(self, seq: int):
+        return list(self._seq(seq)[0])
+
+    def new(self) -> int:
+        """An empty sequence's id."""
+        self._seqs[self._next] = [[], 0]
+        self._next += 1
+        return self._next - 1
+
+    def fork(self, seq: int) -> int:
+        """A sequence that begins with all of another's tokens, on the same pages."""
+        pages, n = self._seq(seq)
+        new = self.new()
+        self._seqs[new] = [list(pages), n]
+        for p in pages:
+            self._users[p] += 1
+        return new
+
+    def _drop(self, pages) -> None:
+        for p in pages:
+            self._users[p] -= 1
+            if self._users[p] == 0:
+                self._free.append(p)
+
+    def free(self, seq: int) -> None:
+        """Ends a sequence; its pages that nobody else uses are free."""
+        self._drop(self._seq(seq)[0])
+        del self._seqs[seq]
+
+    def truncate(self, seq: int, tokens: int) -> None:
+        """Keeps the first tokens of a sequence (a rejected draft)."""
+        s = self._seq(seq)
+        if not 0 <= tokens <= s[1]:
+            raise SsbaError(SSBA_ERR_INVALID, f"sequence {seq} has {s[1]} tokens, not {tokens}")
+        keep = -(-tokens // PAGE)
+        self._drop(s[0][keep:])
+        s[0], s[1] = s[0][:keep], tokens
+
+    def grow(self, seqs, counts):
+        """Room for counts[i] more tokens of each sequence. Returns the copies (src, dst) that have to be made before they are
+        written: of last pages that others use too. Changes nothing when pages do not suffice."""
+        if len(set(seqs)) != len(seqs) or len(seqs) != len(counts) or any(n < 0 for n in counts):
+            raise SsbaError(SSBA_ERR_INVALID, "sequences come once each, with a count >= 0")
+        plan, need, left = [], 0, {}
+        for seq, n in zip(seqs, counts):
+            pages, held = self._seq(seq)
+            more = -(-(held + n) // PAGE) - len(pages)
+            shared = False
+            if n > 0 and held % PAGE:  # (of the forks that write to one page here, the last one left keeps it)
+                users = left.get(pages[-1], self._users[pages[-1]])
+                shared = users > 1
+                left[pages[-1]] = users - shared
+            plan.append((more, shared))
+            need += more + shared
+        if need > len(self._free):
+            raise SsbaError(SSBA_ERR_WORKSPACE, f"{need} pages are needed, {len(self._free)} are free")
+        copies = []
+        for seq, n, (more, shared) in zip(seqs, counts, plan):
+            s = self._seqs[seq]
+            if shared:
+                p = self._take()
+                copies.append((s[0][-1], p))
+                self._users[s[0][-1]] -= 1
+                s[0][-1] = p
+            s[0].extend(self._take() for _ in range(more))
+            s[1] += n
+        return copies
+
+    def _take(self) -> int:
+        p = self._free.pop()
+        self._users[p] = 1
+        return p
+
+    def compact(self):
+        """Live pages to the front of the pool. Returns the moves (src, dst); no page is in both."""
+        live = sum(u > 0 for u in self._users)
+        to = [p for p in range(live) if self._users[p] == 0]
+        moves = dict(zip((p for p in range(live, self.pages) if self._users[p] > 0), to))
+        for s in self._seqs.values():
+            s[0] = [moves.get(p, p) for p in s[0]]
+        for a, b in moves.items():
+            self._users[b], self._users[a] = self._users[a], 0
+        self._free = list(range(self.pages - 1, live - 1, -1))
+        return list(moves.items())
+
+
+@dataclass
+class CacheStep:
+    """The new tokens of some sequences, as the calls of every layer take them: table [B, width], held [B] tokens before
+    the step, lens [B] with it, cu [B + 1] rows; int32 on the device."""
+    table: torch.Tensor
+    held: torch.Tensor
+    lens: torch.Tensor
+    cu: torch.Tensor
+    rows: int
+
+
+class PagedCache:
+    """The K/V cache of a model's layers: a pool a layer, and one page table for all of them.
+
+        cache = PagedCache(CacheDesc(heads, kv_heads, head_dim, pages), layers)
+        a = cache.new()
+        step = cache.step([a], [k.shape[0]])            # pages for the new tokens
+        for layer in range(layers):
+            cache.append(step, layer, k, v)
+            O, lse = cache.attend(step, layer, q)       # keep=64: only the 64 pages selected for each query
+        b = cache.fork(a)                               # shares a's pages
+
+    All its calls belong on one stream: pages are reused in the order of that stream."""
+
+    def __init__(self, desc: CacheDesc, layers: int = 1, device="cuda"):
+        self.desc = desc
+        self.table = PageTable(desc.pages)
+        self.pools = [cache_alloc(desc, device) for _ in range(layers)]
+        self.device = self.pools[0].K.device
+
+    def new(self) -> int:
+        return self.table.new()
+
+    def fork(self, seq: int) -> int:
+        return self.table.fork(seq)
+
+    def free(self, seq: int) -> None:
+        self.table.free(seq)
+
+    def truncate(self, seq: int, tokens: int) -> None:
+        self.table.truncate(seq, tokens)
+
+    def length(self, seq: int) -> int:
+        return self.table.length(seq)
+
+    @property
+    def free_pages(self) -> int:
+        return self.table.free_pages
+
+    def _ints(self, x) -> torch.Tensor:
+        return torch.tensor(x, dtype=torch.int32).to(self.device, non_blocking=True)
+
+    def _copy(self, pairs) -> None:
+        if pairs:
+            src, dst = (self._ints(x) for x in zip(*pairs))
+            for pool in self.pools:
+                cache_copy(self.desc, pool, src, dst)
+
+    def compact(self) -> int:
+        """Moves the live pages to the front of the pools; returns how many moved."""
+        moves = self.table.compact()
+        self._copy(moves)
+        return len(moves)
+
+    def step(self, seqs, counts) -> CacheStep:
+        """Makes room for counts[i] new tokens of sequence seqs[i], whose rows follow one another in k, v and q. Their
+        K and V are to be appended, in every layer, before anything reads them."""
+        seqs, counts = list(seqs), [int(n) for n in counts]
+        self._copy(self.table.grow(seqs, counts))
+        pages = [self.table.pages_of(s) for s in seqs]
+        width = max(max(map(len, pages), default=0), 1)
+        lens = [self.table.length(s) for s in seqs]
+        cu = [0]
+        for n in counts:
+            cu.append(cu[-1] + n)
+        table = torch.tensor([p + [-1] * (width - len(p)) for p in pages], dtype=torch.int32).reshape(len(seqs), width)
+        return CacheStep(table.to(self.device, non_blocking=True), self._ints([a - n for a, n in zip(lens, counts)]),
+                         self._ints(lens), self._ints(cu), cu[-1])
+
+    def append(self, step: CacheStep, layer: int, k, v) -> None:
+        """The step's K and V [rows, kv_heads, head_dim] into a layer's pool."""
+        cache_append(self.desc, self.pools[layer], k, v, step.table, step.held, step.cu)
+
+    def attend(self, step: CacheStep, layer: int, q, keep: int | None = None, first: int = 1):
+        """Attention of the step's queries [rows, heads, head_dim] over a layer's pool; with keep, over the pages that
+        cache_select picks for each of them. Returns (O, lse)."""
+        lists = (None, None)
+        if keep is not None:
+            lists = cache_select(self.desc, self.pools[layer], q, step.table, step.lens, step.cu, keep, first)
+        return cache_attend(self.desc, self.pools[layer], q, step.table, step.lens, step.cu, *lists)

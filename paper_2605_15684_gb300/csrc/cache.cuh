@@ -139,10 +139,11 @@ int launch_cache_attend_simt(const cache::Pool& pl, const cache::Batch& bt, int 
 size_t cache_attend_simt_workspace();
 int launch_cache_attend_tc(const cache::Pool& pl, const cache::Batch& bt, int head_dim, float scale, const void* q,
                            const int32_t* idx, const int32_t* cnt, int keep, void* O, float* lse, void* ws,
-                           cudaStream_t st);
+                           cudaStream_t st, uint64_t budget_ns = kWaitBudgetNs, int withhold = 0);
 size_t cache_attend_tc_workspace();
 int launch_cache_attend_rows(const cache::Pool& pl, const cache::Batch& bt, int head_dim, float scale, const void* q,
-                             void* O, float* lse, void* ws, cudaStream_t st);
+                             void* O, float* lse, void* ws, cudaStream_t st, uint64_t budget_ns = kWaitBudgetNs,
+                             int withhold = 0);
 size_t cache_attend_rows_workspace();
 
 }  // namespace ssba

@@ -93,6 +93,48 @@ bool make_pool(const ssba_cache_desc* d, const ssba_cache* c, const char* who, c
     return p->status != nullptr;
 }
 
+// ssba_cache_attend, and its test hook with a limit of its own and copies that never come.
+int attend(const char* who, const ssba_cache_desc* desc, const ssba_cache* cache, const void* q, int32_t T,
+           const int32_t* table, int32_t width, const int32_t* lens, const int32_t* cu, int32_t B, const int32_t* idx,
+           const int32_t* cnt, int32_t keep, void* O, float* lse, void* workspace, size_t ws_bytes, void* stream,
+           uint64_t budget_ns, int withhold)
+{
+    int rc = check_cache_desc(desc, who);
+    if (rc == SSBA_OK) rc = check_cache(cache, who);
+    if (rc == SSBA_OK) rc = check_batch(T, table, width, lens, cu, B, who);
+    if (rc != SSBA_OK) return rc;
+    if ((idx != nullptr) != (cnt != nullptr) || (idx && (keep <= 0 || keep > SSBA_CACHE_MAX_WIDTH)) ||
+        !aligned(idx, 4) || !aligned(cnt, 4)) {
+        set_error("%s: idx and cnt come together, 4-byte aligned, with 0 < keep <= %d", who, SSBA_CACHE_MAX_WIDTH);
+        return SSBA_ERR_INVALID;
+    }
+    if (T == 0 || B == 0) return SSBA_OK;
+    if (!q || !O || !lse || !aligned(q, 16) || !aligned(O, 16) || !aligned(lse, 4)) {
+        set_error("%s: q, O and lse must be non-null, q and O 16-byte aligned", who);
+        return SSBA_ERR_INVALID;
+    }
+    const size_t need = ssba_cache_attend_workspace_bytes(desc);
+    if (!workspace || ws_bytes < need || !aligned(workspace, 16)) {
+        set_error("%s: workspace of %zu bytes (16-byte aligned) required, got %zu", who, need, ws_bytes);
+        return SSBA_ERR_WORKSPACE;
+    }
+    cache::Pool p;
+    if (!make_pool(desc, cache, who, &p)) return SSBA_ERR_CUDA;
+    const float scale = desc->softmax_scale > 0.f ? desc->softmax_scale : 1.0f / std::sqrt((float)desc->head_dim);
+    const cache::Batch bt{table, lens, cu, B, width, T};
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (desc->dtype == SSBA_BF16) {
+        // Rows that share a K/V head's tokens, on average over the batch's sequences: up to 16 as columns of products
+        // over the bytes, bound by HBM; more as rows of fp16 products. (16 sequences of up to 8000 tokens, 8 K/V
+        // heads: 16 rows 62 us against 113, 32 rows 129 against 115, 64 rows 198 against 118.)
+        const long long rows = ((long long)T + B - 1) / B * (desc->heads / desc->kv_heads);
+        if (!idx && rows > 16) 
+            return launch_cache_attend_rows(p, bt, desc->head_dim, scale, q, O, lse, workspace, st, budget_ns, withhold);
+        return launch_cache_attend_tc(p, bt, desc->head_dim, scale, q, idx, cnt, keep, O, lse, workspace, st, budget_ns, withhold);
+    }
+    return launch_cache_attend_simt(p, bt, desc->head_dim, scale, q, idx, cnt, keep, O, lse, workspace, st);
+}
+
 }  // namespace
 }  // namespace ssba
 
@@ -164,40 +206,22 @@ int ssba_cache_attend(const ssba_cache_desc* desc, const ssba_cache* cache, cons
                       size_t ws_bytes, void* stream)
 {
     SSBA_NVTX_RANGE("ssba_cache_attend");
-    const char* who = "ssba_cache_attend";
-    int rc = check_cache_desc(desc, who);
-    if (rc == SSBA_OK) rc = check_cache(cache, who);
-    if (rc == SSBA_OK) rc = check_batch(T, table, width, lens, cu, B, who);
-    if (rc != SSBA_OK) return rc;
-    if ((idx != nullptr) != (cnt != nullptr) || (idx && (keep <= 0 || keep > SSBA_CACHE_MAX_WIDTH)) ||
-        !aligned(idx, 4) || !aligned(cnt, 4)) {
-        set_error("%s: idx and cnt come together, 4-byte aligned, with 0 < keep <= %d", who, SSBA_CACHE_MAX_WIDTH);
-        return SSBA_ERR_INVALID;
+    return attend("ssba_cache_attend", desc, cache, q, T, table, width, lens, cu, B, idx, cnt, keep, O, lse, workspace,
+                  ws_bytes, stream, kWaitBudgetNs, 0);
+}
+
+int ssba_test_cache_timeout(const ssba_cache_desc* desc, const ssba_cache* cache, const void* q, int32_t T,
+                            const int32_t* table, int32_t width, const int32_t* lens, const int32_t* cu, int32_t B,
+                            void* O, float* lse, void* workspace, size_t ws_bytes, uint64_t budget_ns, void* stream)
+{
+    SSBA_NVTX_RANGE("ssba_test_cache_timeout");
+    if (desc && desc->dtype != SSBA_BF16) {
+        set_error("ssba_test_cache_timeout: bf16 only");
+        return SSBA_ERR_UNSUPPORTED;
     }
-    if (T == 0 || B == 0) return SSBA_OK;
-    if (!q || !O || !lse || !aligned(q, 16) || !aligned(O, 16) || !aligned(lse, 4)) {
-        set_error("%s: q, O and lse must be non-null, q and O 16-byte aligned", who);
-        return SSBA_ERR_INVALID;
-    }
-    const size_t need = ssba_cache_attend_workspace_bytes(desc);
-    if (!workspace || ws_bytes < need || !aligned(workspace, 16)) {
-        set_error("%s: workspace of %zu bytes (16-byte aligned) required, got %zu", who, need, ws_bytes);
-        return SSBA_ERR_WORKSPACE;
-    }
-    cache::Pool p;
-    if (!make_pool(desc, cache, who, &p)) return SSBA_ERR_CUDA;
-    const float scale = desc->softmax_scale > 0.f ? desc->softmax_scale : 1.0f / std::sqrt((float)desc->head_dim);
-    const cache::Batch bt{table, lens, cu, B, width, T};
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (desc->dtype == SSBA_BF16) {
-        // Rows that share a K/V head's tokens, on average over the batch's sequences: up to 16 as columns of products
-        // over the bytes, bound by HBM; more as rows of fp16 products. (16 sequences of up to 8000 tokens, 8 K/V
-        // heads: 16 rows 62 us against 113, 32 rows 129 against 115, 64 rows 198 against 118.)
-        const long long rows = ((long long)T + B - 1) / B * (desc->heads / desc->kv_heads);
-        if (!idx && rows > 16) return launch_cache_attend_rows(p, bt, desc->head_dim, scale, q, O, lse, workspace, st);
-        return launch_cache_attend_tc(p, bt, desc->head_dim, scale, q, idx, cnt, keep, O, lse, workspace, st);
-    }
-    return launch_cache_attend_simt(p, bt, desc->head_dim, scale, q, idx, cnt, keep, O, lse, workspace, st);
+    const uint64_t limit = std::min<uint64_t>(std::max<uint64_t>(budget_ns, 1000000ull), kWaitBudgetNs);
+    return attend("ssba_test_cache_timeout", desc, cache, q, T, table, width, lens, cu, B, nullptr, nullptr, 0, O, lse,
+                  workspace, ws_bytes, stream, limit, 1);
 }
 
 int ssba_cache_copy(const ssba_cache_desc* desc, const ssba_cache* cache, const int32_t* src, const int32_t* dst,

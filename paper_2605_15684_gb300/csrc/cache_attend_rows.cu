@@ -258,6 +258,10 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                             const uint32_t bar = rfull0 + 8 * slot, to = smem_u32(&sm.raw[slot][0]);
                             const CUtensorMap* map = v ? &maps.v : &maps.k;
                             mbar_arrive_expect_tx(bar, ((p0 >= 0) + (p1 >= 0)) * (uint32_t)(kPage * D));
+                            if (p.withhold && blockIdx.x == 0) {
+                                dead = true;
+                                break;
+                            }
                             if (p0 >= 0) tma_load_3d(to, map, bar, 0, 0, p0);
                             if (p1 >= 0) tma_load_3d(to + kPage * D, map, bar, 0, 0, p1);
                             ++loads;
@@ -771,7 +775,7 @@ size_t cache_attend_rows_workspace()
 }
 
 int launch_cache_attend_rows(const cache::Pool& pl, const cache::Batch& bt, int head_dim, float scale, const void* q,
-                             void* O, float* lse, void* ws, cudaStream_t st)
+                             void* O, float* lse, void* ws, cudaStream_t st, uint64_t budget_ns, int withhold)
 {
     using namespace cache;
     Maps maps;
@@ -793,7 +797,8 @@ int launch_cache_attend_rows(const cache::Pool& pl, const cache::Batch& bt, int 
     p.tickets = static_cast<unsigned*>(ws);
     p.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + SSBA_CACHE_TICKET_BYTES);
     p.G = pl.heads / pl.kv_heads;
-    p.budget_ns = kWaitBudgetNs;
+    p.budget_ns = budget_ns;
+    p.withhold = withhold;
     p.chunks = (p.G + kItemRows - 1) / kItemRows;
     p.gc = (p.G + p.chunks - 1) / p.chunks;
     p.gc_inv = (65536 + p.gc - 1) / p.gc;

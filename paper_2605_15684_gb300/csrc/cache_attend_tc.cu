@@ -241,6 +241,10 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
             }
             const uint32_t bar = full0 + 8 * slot, to = ring0 + slot * C::kSlotBytes;
             mbar_arrive_expect_tx(bar, ((p0 >= 0) + (p1 >= 0)) * (uint32_t)(kPage * D));
+            if (p.withhold && blockIdx.x == 0) {
+                dead = true;
+                return;
+            }
             if (p0 >= 0) tma_load_3d(to, map, bar, 0, 0, p0);
             if (p1 >= 0) tma_load_3d(to + kPage * D, map, bar, 0, 0, p1);
             ++loads;
@@ -716,7 +720,7 @@ size_t cache_attend_tc_workspace() { return SSBA_CACHE_TICKET_BYTES + cache::kPa
 
 int launch_cache_attend_tc(const cache::Pool& pl, const cache::Batch& bt, int head_dim, float scale, const void* q,
                            const int32_t* idx, const int32_t* cnt, int keep, void* O, float* lse, void* ws,
-                           cudaStream_t st)
+                           cudaStream_t st, uint64_t budget_ns, int withhold)
 {
     using namespace cache;
     Maps maps;
@@ -740,7 +744,8 @@ int launch_cache_attend_tc(const cache::Pool& pl, const cache::Batch& bt, int he
     p.tickets = static_cast<unsigned*>(ws);
     p.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + SSBA_CACHE_TICKET_BYTES);
     p.G = pl.heads / pl.kv_heads;
-    p.budget_ns = kWaitBudgetNs;
+    p.budget_ns = budget_ns;
+    p.withhold = withhold;
     // rows of an item: a group's heads, of several tokens where the sequences have them (16 rows cost the
     // softmax warps twice what 8 do: 16 sequences of up to 8000 tokens 37 us with 8 rows, 62 with 16)
     const long long each = idx ? 1 : ((long long)bt.T + bt.B - 1) / bt.B;  // rows of a sequence, on average

@@ -33,7 +33,8 @@ struct Params {
     unsigned* tickets;
     int G, gc, chunks, tq;  // group size; heads and tokens of an item; chunks of a group
     int gc_inv;             // ceil(2^16 / gc): r / gc for r < 256
-    uint64_t budget_ns;
+    uint64_t budget_ns;     // of every wait
+    int withhold;           // (test hook) CTA 0 announces its first copies and issues none
 };
 
 // The rows of an item: tokens [row, row + n) of the batch, each with the heads of chunk hv.

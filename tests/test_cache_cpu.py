@@ -142,3 +142,98 @@ def test_reference_attention_is_a_softmax():
         a = 0.3 * q[i] @ K[:L].T
         w = np.exp(a) / np.exp(a).sum(1, keepdims=True)
         assert np.allclose(O[i], w @ V[:L], atol=1e-13) and np.allclose(lse[i], np.log(np.exp(a).sum(1)), atol=1e-13)
+
+
+# ----------------------------------------------------------------------------- the host's page table
+def check_table(t):
+    """Every page is free or used by as many sequences as hold it."""
+    users = [0] * t.pages
+    for s in t.sequences:
+        pages = t.pages_of(s)
+        assert len(pages) == -(-t.length(s) // 64) and len(set(pages)) == len(pages)
+        for p in pages:
+            users[p] += 1
+    assert users == t._users
+    assert sorted(t._free) == [p for p in range(t.pages) if users[p] == 0]
+
+
+def test_page_table_against_the_tokens_it_stands_for():
+    """Random growing, forking, truncating, freeing and compacting: following the copies, every sequence reads its own tokens."""
+    import random
+    r = random.Random(3)
+    for _ in range(30):
+        t = pc.PageTable(r.randint(3, 40))
+        mem = [[None] * 64 for _ in range(t.pages)]
+        own, stamp = {}, 0
+        for _ in range(120):
+            what = r.random()
+            if what < 0.15 or not own:
+                own[t.new()] = []
+            elif what < 0.3:
+                s = r.choice(list(own))
+                own[t.fork(s)] = list(own[s])
+            elif what < 0.4:
+                s = r.choice(list(own))
+                t.free(s)
+                del own[s]
+            elif what < 0.5:
+                s = r.choice(list(own))
+                n = r.randint(0, len(own[s]))
+                t.truncate(s, n)
+                own[s] = own[s][:n]
+            elif what < 0.55:
+                moves = t.compact()
+                assert not {a for a, _ in moves} & {b for _, b in moves}
+                for a, b in moves:
+                    mem[b] = list(mem[a])
+                    mem[a] = [None] * 64
+                assert t._free == list(range(t.pages - 1, t.pages - 1 - len(t._free), -1))
+            else:
+                some = [s for s in own if r.random() < 0.6]
+                counts = [r.choice([0, 1, 1, 3, 64, 100]) for _ in some]
+                before = (t.free_pages, {s: t.pages_of(s) for s in own})
+                try:
+                    copies = t.grow(some, counts)
+                except api.SsbaError as e:
+                    assert "free" in str(e)
+                    assert before == (t.free_pages, {s: t.pages_of(s) for s in own})
+                    continue
+                for a, b in copies:
+                    mem[b] = list(mem[a])
+                for s, n in zip(some, counts):
+                    for _ in range(n):
+                        stamp += 1
+                        at = len(own[s])
+                        mem[t.pages_of(s)[at // 64]][at % 64] = stamp
+                        own[s].append(stamp)
+            check_table(t)
+            for s, tokens in own.items():
+                pages = t.pages_of(s)
+                assert [mem[pages[i // 64]][i % 64] for i in range(len(tokens))] == tokens
+
+
+def test_page_table_refusals():
+    t = pc.PageTable(2)
+    a, b = t.new(), t.new()
+    for bad in (lambda: t.grow([a, a], [1, 1]), lambda: t.grow([a], [1, 2]), lambda: t.grow([a], [-1]), lambda: t.grow([9], [1]),
+                lambda: t.grow([a, b], [64, 65]), lambda: t.truncate(a, 1), lambda: t.free(7), lambda: t.fork(7),
+                lambda: pc.PageTable(0)):
+        with pytest.raises(api.SsbaError):
+            bad()
+    check_table(t)
+    assert t.grow([a, b], [64, 64]) == [] and t.free_pages == 0
+    # two forks of one half-filled page: one copies, the other keeps it
+    t = pc.PageTable(2)
+    a = t.new()
+    t.grow([a], [10])
+    b = t.fork(a)
+    assert len(t.grow([a, b], [1, 1])) == 1
+    check_table(t)
+
+
+def test_timeout_hook_validation(lib):
+    need = lib.ssba_cache_attend_workspace_bytes(desc())
+    call = lambda d, q=FAKE, ws=FAKE, n=need: lib.ssba_test_cache_timeout(d, pool(), q, 3, *BATCH, FAKE, FAKE, ws, n, 0, None)
+    assert call(desc(dtype=api.SSBA_FP32)) == api.SSBA_ERR_UNSUPPORTED
+    assert call(desc(), q=None) == api.SSBA_ERR_INVALID
+    assert call(desc(), n=need - 1) == api.SSBA_ERR_WORKSPACE

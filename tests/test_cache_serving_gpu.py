@@ -1,0 +1,304 @@
+"""The cache's calls together, as a server makes them: growing, forked, truncated and compacted sequences over several layers,
+on other streams, in graphs, and with a wait that runs out."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import cache_ref as ref
+from paper_2605_15684_gb300 import api, build
+from paper_2605_15684_gb300 import cache as pc
+from test_cache_gpu import BF16, FP32, Batch, hold, ints, queries, shares
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    build.build()
+    api.load_library()
+
+
+@pytest.fixture(autouse=True)
+def _status():
+    torch.cuda.synchronize()
+    api.get_status()
+    yield
+    torch.cuda.synchronize()
+
+
+class Model:
+    """What a PagedCache is to hold: every sequence's own K and V, in a reference pool of its own pages."""
+
+    def __init__(self, kv, d, layers):
+        self.kv, self.d, self.layers, self.seqs = kv, d, layers, {}
+
+    def _pool(self, pages):
+        p = ref.Pool.__new__(ref.Pool)
+        shape = (pages, self.kv, 64, self.d)
+        p.K, p.V = np.zeros(shape), np.zeros(shape)
+        p.k_scale, p.v_scale, p.k_mean = np.zeros(shape[:2]), np.zeros(shape[:2]), np.zeros((pages, self.kv, self.d))
+        return p
+
+    def new(self, s):
+        self.seqs[s] = [0, [self._pool(16) for _ in range(self.layers)]]
+
+    def fork(self, a, b):
+        n, pools = self.seqs[a]
+        copies = []
+        for p in pools:
+            q = ref.Pool.__new__(ref.Pool)
+            q.__dict__ = {k: v.copy() for k, v in p.__dict__.items()}
+            copies.append(q)
+        self.seqs[b] = [n, copies]
+
+    def append(self, s, layer, k, v):
+        n, pools = self.seqs[s]
+        ref.append(pools[layer], k, v, np.arange(16)[None], [n], [0, k.shape[0]])
+
+    def attend(self, s, layer, q, n_after, lists=None):
+        return ref.attend(self.seqs[s][1][layer], q, np.arange(16)[None], [n_after], [0, q.shape[0]], self.d ** -0.5, lists)
+
+
+@pytest.mark.parametrize("dtype,d,heads,kv", [(BF16, 128, 8, 2), (BF16, 64, 3, 3), (FP32, 64, 4, 1)])
+def test_server(dtype, d, heads, kv):
+    """Random steps of several sequences in two layers: prompts, single tokens, drafts, forks, rejected drafts, ends, and
+    compaction; every output against the reference's own copy of the sequence."""
+    layers, rng = 2, np.random.default_rng(5)
+    g = torch.Generator().manual_seed(7)
+    cache, model = pc.PagedCache(pc.CacheDesc(heads, kv, d, 40, dtype), layers), Model(kv, d, layers)
+    live = []
+    for turn in range(30):
+        if len(live) < 3 or rng.random() < 0.15:
+            s = cache.new()
+            model.new(s)
+            live.append(s)
+        elif rng.random() < 0.25:
+            a = live[rng.integers(len(live))]
+            s = cache.fork(a)
+            model.fork(a, s)
+            live.append(s)
+        if len(live) > 5:
+            s = live.pop(rng.integers(len(live)))
+            cache.free(s)
+            del model.seqs[s]
+        if rng.random() < 0.2:
+            s = live[rng.integers(len(live))]
+            n = int(rng.integers(model.seqs[s][0] + 1))
+            cache.truncate(s, n)
+            model.seqs[s][0] = n
+        if turn % 7 == 6:
+            cache.compact()
+            assert cache.table.free_pages == 40 - (max((p for s in live for p in cache.table.pages_of(s)), default=-1) + 1)
+        some = [s for s in live if rng.random() < 0.8 and model.seqs[s][0] < 500]
+        counts = [int(rng.choice([1, 1, 1, 5, 70])) for _ in some]
+        if not some:
+            continue
+        step = cache.step(some, counts)
+        cu = shares(counts)
+        for layer in range(layers):
+            k, v = (torch.randn((cu[-1], kv, d), generator=g).to(dtype) for _ in range(2))
+            q = (torch.randn((cu[-1], heads, d), generator=g) * 1.5).to(dtype)
+            cache.append(step, layer, k.cuda(), v.cuda())
+            O, lse = cache.attend(step, layer, q.cuda())
+            keep = 3
+            lists = pc.cache_select(cache.desc, cache.pools[layer], q.cuda(), step.table, step.lens, step.cu, keep)
+            O2, lse2 = cache.attend(step, layer, q.cuda(), keep=keep)
+            torch.cuda.synchronize()
+            assert api.get_status() == api.SSBA_OK
+            for i, s in enumerate(some):
+                r = slice(cu[i], cu[i + 1])
+                model.append(s, layer, k[r].double().numpy(), v[r].double().numpy())
+                n = model.seqs[s][0] + counts[i]
+                for got, gl, li in ((O, lse, None), (O2, lse2, lists[0][r].cpu().numpy())):
+                    want, wl, A, S = model.attend(s, layer, q[r].double().numpy(), n, li)
+                    bO, bl = ref.bounds(want, A, S, d, n, dtype == BF16)
+                    hold(got[r], want, bO, (turn, s, "O"))
+                    hold(gl[r], wl, bl, (turn, s, "lse"))
+        for s, n in zip(some, counts):
+            model.seqs[s][0] += n
+            assert cache.length(s) == model.seqs[s][0]
+
+
+def args(bt, n, heads, seed=1):
+    cu = shares(n)
+    return bt.desc(heads), bt.cache, queries(cu[-1], heads, bt.d, BF16, seed), bt.gpu_table(), ints(bt.lens), ints(cu)
+
+
+def test_other_streams():
+    """Calls on another stream while the current one is busy, with outputs and workspaces of the binding's."""
+    bts = [Batch([3000, 500], 2, 128, 1), Batch([900, 70], 2, 128, 2)]
+    calls = [args(bts[0], [1, 1], 8), args(bts[1], [40, 9], 8)]
+    want = [(pc.cache_attend(*a), pc.cache_select(*a, 5)) for a in calls]
+    torch.cuda.synchronize()
+    busy = torch.randn(8192, 8192, device="cuda").bfloat16()
+    for _ in range(3):
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        for _ in range(10):
+            busy @ busy
+        got = []
+        for a in calls:
+            got.append((pc.cache_attend(*a, stream=s), pc.cache_select(*a, 5, stream=s)))
+            junk = [torch.full((1 << 20,), -1, dtype=torch.int32, device="cuda") for _ in range(8)]
+        torch.cuda.current_stream().wait_stream(s)
+        torch.cuda.synchronize()
+        assert api.get_status() == api.SSBA_OK
+        for x, y in zip(got, want):
+            for p, q in zip(x, y):
+                assert all(torch.equal(a, b) for a, b in zip(p, q))
+    del junk
+
+
+def test_results_do_not_depend_on_the_order_of_ctas():
+    """Items that many CTAs share: the same bits every time, and beside other work."""
+    for lens, n in (([9000, 31, 2500], [1, 1, 1]), ([2500, 700], [60, 33])):
+        a = args(Batch(lens, 1, 128), n, 8)
+        want = pc.cache_attend(*a)
+        busy = torch.randn(2048, 2048, device="cuda").bfloat16()
+        s = torch.cuda.Stream()
+        for _ in range(20):
+            with torch.cuda.stream(s):
+                busy @ busy
+            got = pc.cache_attend(*a)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        torch.cuda.synchronize()
+
+
+def test_two_graphs_side_by_side():
+    """Two graphs of the same calls, captured before any other and replayed at once: neither's workspace is the other's, nor
+    that of calls outside."""
+    pc._ws.clear()
+    a = args(Batch([5000, 2000], 1, 128), [1, 1], 8)
+    b = args(Batch([1500, 600], 1, 64), [90, 20], 6, 2)
+    graphs = []
+    for x in (a, b, a):
+        s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            out = [pc.cache_attend(*x) for _ in range(3)]
+        graphs.append((s, g, out, x))
+    want = {id(x): pc.cache_attend(*x) for x in (a, b)}
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, g, _, _ in graphs:
+            with torch.cuda.stream(s):
+                g.replay()
+        outside = pc.cache_attend(*a)
+        torch.cuda.synchronize()
+        assert api.get_status() == api.SSBA_OK
+        for _, _, out, x in graphs:
+            for O, lse in out:
+                assert torch.equal(O, want[id(x)][0]) and torch.equal(lse, want[id(x)][1])
+        assert torch.equal(outside[0], want[id(a)][0])
+
+
+def test_a_captured_step_with_new_lengths():
+    """A decoding step in a graph: append, select and attend; lens, tokens and rows change between replays."""
+    bt = Batch([0, 0, 0], 2, 128, pool_lens=[400, 200, 130])
+    pool = bt.pool()
+    lens = [70, 0, 129]
+    k0 = torch.randn((sum(lens), 2, 128)).bfloat16()
+    cu = shares(lens)
+    pc.cache_append(bt.desc(8), bt.cache, k0.cuda(), k0.flip(0).contiguous().cuda(), bt.gpu_table(), ints([0, 0, 0]), ints(cu))
+    ref.append(pool, k0.double().numpy(), k0.flip(0).double().numpy(), bt.table, [0, 0, 0], cu)
+    T = 3
+    k, v, q = (torch.zeros((T, h, 128), dtype=BF16, device="cuda") for h in (2, 2, 8))
+    table, held, now, cud = bt.gpu_table(), ints([0, 0, 0]), ints([1, 1, 1]), ints([0, 1, 2, 3])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        pc.cache_append(bt.desc(8), bt.cache, k, v, table, held, cud)
+        idx, cnt = pc.cache_select(bt.desc(8), bt.cache, q, table, now, cud, 2)
+        O, lse = pc.cache_attend(bt.desc(8), bt.cache, q, table, now, cud)
+        O2, lse2 = pc.cache_attend(bt.desc(8), bt.cache, q, table, now, cud, idx, cnt)
+    for turn in range(12):
+        rows = shares([1, 1, 1] if turn % 3 else [1, 0, 1])  # a padded batch: the last row belongs to none
+        n = [b - a for a, b in zip(rows, rows[1:])]
+        gen = torch.Generator().manual_seed(turn)
+        kn, vn, qn = (torch.randn((T, h, 128), generator=gen).bfloat16() for h in (2, 2, 8))
+        k.copy_(kn), v.copy_(vn), q.copy_(qn)
+        held.copy_(ints(lens)), now.copy_(ints([a + b for a, b in zip(lens, n)])), cud.copy_(ints(rows))
+        g.replay()
+        torch.cuda.synchronize()
+        assert api.get_status() == api.SSBA_OK
+        ref.append(pool, kn.double().numpy(), vn.double().numpy(), bt.table, lens, rows)
+        lens = [a + b for a, b in zip(lens, n)]
+        e = rows[-1]
+        for got, gl, li in ((O, lse, None), (O2, lse2, idx.cpu().numpy())):
+            want, wl, A, S = ref.attend(pool, qn.double().numpy()[:e], bt.table, lens, rows, 128 ** -0.5, li)
+            bO, bl = ref.bounds(want, A, S, 128, max(lens), True)
+            hold(got[:e], want, bO, "O")
+            hold(gl[:e], wl, bl, "lse")
+
+
+@pytest.mark.parametrize("lens,n,d", [([3000, 100], [1, 1], 128), ([3000, 100], [1, 1], 64), ([900, 300], [60, 50], 128),
+                                      ([900, 300], [60, 50], 64)])
+def test_a_wait_that_runs_out(lens, n, d):
+    """Copies that are announced and never come: the call ends with SSBA_ERR_TIMEOUT, the context and the binding's next
+    call are well."""
+    a = args(Batch(lens, 2, d), n, 8)
+    want = pc.cache_attend(*a)
+    torch.cuda.synchronize()
+    assert api.get_status() == api.SSBA_OK
+    ws = torch.zeros(pc.cache_attend_workspace_bytes(a[0]), dtype=torch.uint8, device="cuda")
+    pc.test_cache_timeout(*a, torch.empty_like(want[0]), torch.empty_like(want[1]), ws)
+    torch.cuda.synchronize()
+    assert api.get_status() == api.SSBA_ERR_TIMEOUT
+    got = pc.cache_attend(*a)
+    torch.cuda.synchronize()
+    assert api.get_status() == api.SSBA_OK
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_a_workspace_is_left_as_it_was_found():
+    """The counters are zero after a call, so that a caller's workspace serves call after call of any shape."""
+    ws = torch.zeros(pc.cache_attend_workspace_bytes(Batch([64], 1, 64).desc(1)), dtype=torch.uint8, device="cuda")
+    for lens, n, heads, kv, d in (([9000], [1], 8, 1, 128), ([2000, 900], [50, 60], 4, 1, 64), ([9000, 3], [2, 1], 8, 2, 64)):
+        a = args(Batch(lens, kv, d), n, heads)
+        want = pc.cache_attend(*a)
+        got = pc.cache_attend(*a, workspace=ws)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        assert not ws[:4096].any()
+
+
+def test_scores_of_every_size():
+    """Rows whose weights span many powers of two: one dominating key far from the others, and scores that fall and rise
+    along the sequence, so that references are raised again and again."""
+    for d, n in ((128, 1), (64, 1), (128, 40), (64, 40)):
+        bt = Batch([900], 1, d)
+        # keys grow along the sequence: scales of pages from 2^-12 to 2^-2
+        for j in range(15):
+            bt.cache.k_scale[bt.table[0][j]] = 2.0 ** (-12 + (j * 7) % 11)
+            bt.cache.v_scale[bt.table[0][j]] = 2.0 ** (-9 + (j * 5) % 13)
+        q = queries(n, 4, d, BF16, 3)
+        O, lse = pc.cache_attend(bt.desc(4), bt.cache, q, bt.gpu_table(), ints([900]), ints([0, n]))
+        torch.cuda.synchronize()
+        want, wl, A, S = ref.attend(bt.pool(), q.double().cpu().numpy(), bt.table, [900], [0, n], d ** -0.5)
+        bO, bl = ref.bounds(want, A, S, d, 900, True)
+        hold(O, want, bO, (d, n, "O"))
+        hold(lse, wl, bl, (d, n, "lse"))
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_one_token_that_dominates_many_small_ones(n):
+    """An attention sink: the first token's weight is 2^13 times any other's, and the others together are most of O."""
+    d, L = 64, 20000
+    bt = Batch([L], 1, d)
+    K, V = bt.cache.K.view(torch.uint8), bt.cache.V.view(torch.uint8)
+    K.fill_(0)
+    V.fill_(0x38)  # 1.0
+    bt.cache.k_scale.fill_(1.0)
+    bt.cache.v_scale.fill_(1.0)
+    p0 = bt.table[0][0]
+    K[p0, :, 0] = 0x38
+    V[p0, :, 0] = 0
+    q = torch.full((n, 2, d), 13 * math.log(2) / d ** 0.5, device="cuda").bfloat16()
+    O, lse = pc.cache_attend(bt.desc(2), bt.cache, q, bt.gpu_table(), ints([L]), ints([0, n]))
+    torch.cuda.synchronize()
+    want, wl, A, S = ref.attend(bt.pool(), q.double().cpu().numpy(), bt.table, [L], [0, n], d ** -0.5)
+    bO, bl = ref.bounds(want, A, S, d, L, True)
+    assert 0.6 < want.min() <= want.max() < 0.8
+    hold(O, want, bO, "O")
+    hold(lse, wl, bl, "lse")
