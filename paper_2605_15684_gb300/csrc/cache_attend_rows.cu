@@ -69,10 +69,11 @@ struct __align__(1024) Smem {
     int nan_at[2][kConverters][D];
     int nan_any[2][kConverters];
     float qf[2][kRowTile];  // scale of a row's scores
+    float2 ml[kRowTile];    // (tiles in turn) reference and sum of the second pipeline's rows
     float first_lv[2];      // by item parity: log2 of the V scale that the item's are relative to
     Meta meta[kMetas][2];
     uint64_t raw_full[kRaw], raw_empty[kRaw], cv_full[kCv], cv_empty[kCv], m_full[kMetas];
-    uint64_t q_full[2], s_full[2], p_full[2], o_full[2], n_full[2], n_empty[2], drain;
+    uint64_t q_full[2], s_full[2], p_full[2], o_full[2], n_full[2], n_empty[2], x_full, x_empty, drain;
     long long w0, w1, total;
     int first_b, ctas;
     long long first_at;
@@ -209,6 +210,8 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
             mbar_init(smem_u32(&sm.n_full[i]), kConverters);
             mbar_init(smem_u32(&sm.n_empty[i]), 8);
         }
+        mbar_init(smem_u32(&sm.x_full), 4);
+        mbar_init(smem_u32(&sm.x_empty), 4);
         mbar_init(smem_u32(&sm.drain), 1);
         fence_mbar_init();
     }
@@ -233,14 +236,32 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
     const uint32_t cfull0 = smem_u32(&sm.cv_full[0]), cempty0 = smem_u32(&sm.cv_empty[0]);
     bool dead = false;
     uint32_t loads = 0;  // of the producer
-    // an item of up to 128 rows has no second row tile
+    // an item of up to 128 rows has no second row tile: both pipelines take its rows, and its tiles in turn
     auto both = [&](const Walk<false>& w) { return w.rows().n * p.gc > kRowTile; };
 
     if (warp == kLoad) {
-        // ------------------------------------------------------------ producer: K_0, V_0, K_1, ...
+        // ------------------------------------------------------------ producer
         Walk<false> it(p, sm);
+        auto copy = [&](const CUtensorMap* map, int p0, int p1) {
+            const uint32_t slot = loads % kRaw;
+            if (!mbar_wait(rempty0 + 8 * slot, ((loads / kRaw) & 1) ^ 1, abortf, p.budget_ns)) {
+                dead = true;
+                return;
+            }
+            const uint32_t bar = rfull0 + 8 * slot, to = smem_u32(&sm.raw[slot][0]);
+            mbar_arrive_expect_tx(bar, ((p0 >= 0) + (p1 >= 0)) * (uint32_t)(kPage * D));
+            if (p.withhold && blockIdx.x == 0) {
+                dead = true;
+                return;
+            }
+            if (p0 >= 0) tma_load_3d(to, map, bar, 0, 0, p0);
+            if (p1 >= 0) tma_load_3d(to + kPage * D, map, bar, 0, 0, p1);
+            ++loads;
+        };
         for (; it.more() && !dead; it.next()) {
             const int h = it.hv / p.chunks;
+            const bool two = both(it);
+            int v0 = -1, v1 = -1;  // the last tile's pages
             for (int c0 = 2 * it.tb; c0 < 2 * it.te && !dead; c0 += 32) {  // 32 pages at a time
                 int j, page = -1;
                 if (c0 + lane < 2 * it.te) page = it.page(c0 + lane, j);
@@ -249,89 +270,80 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 for (int i = 0; i < n && !dead; ++i) {
                     const int p0 = __shfl_sync(0xffffffffu, unit, 2 * i), p1 = __shfl_sync(0xffffffffu, unit, 2 * i + 1);
                     if (lane == 0) {
-                        for (int v = 0; v < 2; ++v) {
-                            const uint32_t slot = loads % kRaw;
-                            if (!mbar_wait(rempty0 + 8 * slot, ((loads / kRaw) & 1) ^ 1, abortf, p.budget_ns)) {
-                                dead = true;
-                                break;
-                            }
-                            const uint32_t bar = rfull0 + 8 * slot, to = smem_u32(&sm.raw[slot][0]);
-                            const CUtensorMap* map = v ? &maps.v : &maps.k;
-                            mbar_arrive_expect_tx(bar, ((p0 >= 0) + (p1 >= 0)) * (uint32_t)(kPage * D));
-                            if (p.withhold && blockIdx.x == 0) {
-                                dead = true;
-                                break;
-                            }
-                            if (p0 >= 0) tma_load_3d(to, map, bar, 0, 0, p0);
-                            if (p1 >= 0) tma_load_3d(to + kPage * D, map, bar, 0, 0, p1);
-                            ++loads;
-                        }
+                        copy(&maps.k, p0, p1);
+                        if (two && !dead) copy(&maps.v, p0, p1);
+                        if (!two && !dead && c0 / 2 + i > it.tb) copy(&maps.v, v0, v1);
                     }
+                    v0 = p0;
+                    v1 = p1;
                     dead = __shfl_sync(0xffffffffu, (int)dead, 0) != 0;
                 }
+            }
+            if (!two && !dead) {
+                if (lane == 0) copy(&maps.v, v0, v1);
+                dead = __shfl_sync(0xffffffffu, (int)dead, 0) != 0;
             }
         }
         __syncwarp();
     } else if (warp == kIssue) {
         // ------------------------------------------------------------ issuer
         Walk<false> it(p, sm);
-        uint32_t cnt[2] = {0, 0}, qs[2] = {0, 0};  // tiles, items of each row tile
-        bool pend[2] = {false, false}, p_first[2] = {}, p_last[2] = {};  // PV still to come: first, last tile of its item's share
-        uint32_t vslot = 0;
+        uint32_t cnt[2] = {0, 0}, q0 = 0, q1 = 0, base = 0;  // tiles and items of each pipeline; ring slots used before the item
         auto slot_full = [&](uint32_t x) { wait_phase(cfull0 + 8 * (x % kCv), (x / kCv) & 1, abort_at, p.budget_ns); };
-        auto pv = [&](int u) {
-            wait_phase(smem_u32(&sm.p_full[u]), (cnt[u] - 1) & 1, abort_at, p.budget_ns);
-            slot_full(vslot);
+        auto qk = [&](int u, uint32_t slot, bool release) {
+            slot_full(slot);
             tc_fence_after();
             if (elect_one_sync()) {
-                const uint64_t b = sdesc_sw128(smem_u32(&sm.cv[vslot % kCv][0][0][0]), kTile * 128, 1024);
+                const uint64_t a = sdesc_sw128(smem_u32(&sm.q[u][0][0][0]), 16, 1024);
+                const uint64_t b = sdesc_sw128(smem_u32(&sm.cv[slot % kCv][0][0][0]), 16, 1024);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint64_t at = (uint64_t)((k / 4) * (kTile * 128 / 16) + (k % 4) * 2);
+                    mma_ss(tbase + u * 128, a + at, b + at, idesc_f16_f32(128, 128, false), k > 0 ? 1u : 0u);
+                }
+                mma_commit(smem_u32(&sm.s_full[u]));
+                if (release) mma_commit(cempty0 + 8 * (slot % kCv));
+            }
+            __syncwarp();
+            ++cnt[u];
+        };
+        auto pv = [&](int u, uint32_t slot, bool first, bool last, bool release) {
+            wait_phase(smem_u32(&sm.p_full[u]), (cnt[u] - 1) & 1, abort_at, p.budget_ns);
+            slot_full(slot);
+            tc_fence_after();
+            if (elect_one_sync()) {
+                const uint64_t b = sdesc_sw128(smem_u32(&sm.cv[slot % kCv][0][0][0]), kTile * 128, 1024);
 #pragma unroll
                 for (int k = 0; k < kTile / 16; ++k)
-                    mma_ts(tbase + 256 + u * D, tbase + u * 128 + k * 8, b + (uint64_t)(k * 128),
-                           idesc_f16_f32(128, D, true), (!p_first[u] || k > 0) ? 1u : 0u);
-                if (p_last[u]) mma_commit(smem_u32(&sm.o_full[u]));
-                if (u == 1 || !pend[1]) mma_commit(cempty0 + 8 * (vslot % kCv));
+                    mma_ts(tbase + 256 + u * D, tbase + u * 128 + k * 8, b + (uint64_t)(k * 128), idesc_f16_f32(128, D, true),
+                           (!first || k > 0) ? 1u : 0u);
+                if (last) mma_commit(smem_u32(&sm.o_full[u]));
+                if (release) mma_commit(cempty0 + 8 * (slot % kCv));
             }
             __syncwarp();
         };
-        uint32_t g = 0;
         for (; it.more(); it.next()) {
+            const int n = it.te - it.tb;
             const bool two = both(it);
-            for (int i = it.tb; i < it.te; ++i, ++g) {
-                const uint32_t kslot = 2 * g;
-                vslot = 2 * g - 1;
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    if (pend[u]) pv(u);
-                    if (u == 1 && !two) continue;
-                    if (i == it.tb) wait_phase(smem_u32(&sm.q_full[u]), qs[u]++ & 1, abort_at, p.budget_ns);
-                    slot_full(kslot);
-                    tc_fence_after();
-                    if (elect_one_sync()) {
-                        const uint64_t a = sdesc_sw128(smem_u32(&sm.q[u][0][0][0]), 16, 1024);
-                        const uint64_t b = sdesc_sw128(smem_u32(&sm.cv[kslot % kCv][0][0][0]), 16, 1024);
-#pragma unroll
-                        for (int k = 0; k < D / 16; ++k) {
-                            const uint64_t at = (uint64_t)((k / 4) * (kTile * 128 / 16) + (k % 4) * 2);
-                            mma_ss(tbase + u * 128, a + at, b + at, idesc_f16_f32(128, 128, false), k > 0 ? 1u : 0u);
-                        }
-                        mma_commit(smem_u32(&sm.s_full[u]));
-                        if (u == 1 || !two) mma_commit(cempty0 + 8 * (kslot % kCv));
-                    }
-                    __syncwarp();
-                    ++cnt[u];
+            // steps i = 0 .. n; a pipeline's PV of a tile before its next QK. One loop, one copy of the products' code.
+#pragma unroll 1
+            for (int i = 0; i <= n; ++i) {
+                if (i == 0) {
+                    wait_phase(smem_u32(&sm.q_full[0]), q0++ & 1, abort_at, p.budget_ns);
+                    if (two || n > 1) wait_phase(smem_u32(&sm.q_full[1]), q1++ & 1, abort_at, p.budget_ns);
                 }
-                pend[0] = true;
-                pend[1] = two;
-                p_first[0] = p_first[1] = i == it.tb;
-                p_last[0] = p_last[1] = i == it.te - 1;
+#pragma unroll 1
+                for (int h = 0; h < 2; ++h) {
+                    if (two) {  // K_0 V_0 K_1 V_1 ...; both row tiles at every step
+                        if (i > 0) pv(h, base + 2 * i - 1, i == 1, i == n, h == 1);
+                        if (i < n) qk(h, base + 2 * i, h == 1);
+                    } else {  // K_0 K_1 V_0 K_2 V_1 ... V_{n - 1}; tiles in turn
+                        if (h == 0 && i < n) qk(i & 1, base + max(2 * i - 1, 0), true);
+                        if (h == 1 && i > 0) pv((i - 1) & 1, base + (i < n ? 2 * i : 2 * n - 1), i <= 2, i >= n - 1, true);
+                    }
+                }
             }
-        }
-        if (g > 0) {
-            vslot = 2 * g - 1;
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-                if (pend[u]) pv(u);
+            base += 2 * n;
         }
         dead = *abortf != 0;
     } else if (warp >= kItems && warp < kSoftmax) {
@@ -362,6 +374,8 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
         for (; it.more(); it.next(), ++seg) {
             const int h = it.hv / p.chunks;
             const Rows rows = it.rows();
+            const bool two = both(it);
+            int last_pos = kNowhere;  // of the last tile's page
             const int lo_lim = it.limit(rows.row), hi_lim = it.limit(rows.row + max(rows.n, 1) - 1);
             float base = 0.f;
             for (int c0 = it.tb; c0 < it.te; c0 += 32) {  // 32 tiles' pages at a time
@@ -394,11 +408,15 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 for (int i = 0; i < n; ++i, ++g) {
                     const int pos = __shfl_sync(0xffffffffu, my_pos, i);
                     const float ks = __shfl_sync(0xffffffffu, my_ks, i), lv = __shfl_sync(0xffffffffu, my_lv, i);
+                    // K of the tile, and V of it (two row tiles) or of the one before (tiles in turn; the last tile's own too)
+                    const bool head = c0 + i == it.tb, tail = c0 + i == it.te - 1;
+                    const int steps = two ? 2 : 1 + !head + tail;
 #pragma unroll 1
-                    for (int v = 0; v < 2; ++v, ++use) {
+                    for (int x = 0; x < steps; ++x, ++use) {
+                        const bool v = x > 0;
                         const uint32_t rs = use % kRaw, cs = use % kCv;
                         wait_phase(rfull0 + 8 * rs, (use / kRaw) & 1, abort_at, p.budget_ns);
-                        const int first = pos + (w & 1) * 32;  // token of the half page's first row
+                        const int first = (two || x != 1 || head ? pos : last_pos) + (w & 1) * 32;  // token of the half page's first row
                         if (v && first + 31 >= lo_lim) {
                             // tokens that no row sees: their V is whatever the page holds, and 0 * NaN would reach
                             // every row; tokens that some rows see: a NaN is taken out and kept for those rows
@@ -408,29 +426,29 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                                 const int at = first + lane / kLanes + k * kRows;
 #pragma unroll 1
                                 for (int m = 0; m < 4 && at >= lo_lim; ++m) {
-                                    uint32_t x = at >= hi_lim ? 0u : word[m];
-                                    if ((((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0) {  // a byte of 0x7f
+                                    uint32_t b = at >= hi_lim ? 0u : word[m];
+                                    if ((((b & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0) {  // a byte of 0x7f
                                         for (int e = 0; e < 4; ++e)
-                                            if (((x >> (8 * e)) & 0x7f) == 0x7f) {
+                                            if (((b >> (8 * e)) & 0x7f) == 0x7f) {
                                                 atomicMin(&sm.nan_at[seg & 1][w][c * 16 + m * 4 + e], at);
                                                 sm.nan_any[seg & 1][w] = 1;
-                                                x &= ~(0xffu << (8 * e));
+                                                b &= ~(0xffu << (8 * e));
                                             }
                                     }
-                                    word[m] = x;
+                                    word[m] = b;
                                 }
                             }
                         }
-                        uint4 x[kIts];
+                        uint4 in[kIts];
 #pragma unroll
                         for (int k = 0; k < kIts; ++k)
-                            x[k] = *reinterpret_cast<const uint4*>(&sm.raw[rs][(row0 + k * kRows) * D + c * 16]);
+                            in[k] = *reinterpret_cast<const uint4*>(&sm.raw[rs][(row0 + k * kRows) * D + c * 16]);
                         wait_phase(cempty0 + 8 * cs, ((use / kCv) & 1) ^ 1, abort_at, p.budget_ns);
 #pragma unroll
                         for (int k = 0; k < kIts; ++k) {
                             const int row = row0 + k * kRows;
-                            uint32_t y[8] = {half2_of(x[k].x & 0xffff), half2_of(x[k].x >> 16), half2_of(x[k].y & 0xffff), half2_of(x[k].y >> 16),
-                                             half2_of(x[k].z & 0xffff), half2_of(x[k].z >> 16), half2_of(x[k].w & 0xffff), half2_of(x[k].w >> 16)};
+                            uint32_t y[8] = {half2_of(in[k].x & 0xffff), half2_of(in[k].x >> 16), half2_of(in[k].y & 0xffff), half2_of(in[k].y >> 16),
+                                             half2_of(in[k].z & 0xffff), half2_of(in[k].z >> 16), half2_of(in[k].w & 0xffff), half2_of(in[k].w >> 16)};
                             const uint4 a = make_uint4(y[0], y[1], y[2], y[3]), b = make_uint4(y[4], y[5], y[6], y[7]);
                             uint8_t* to = &sm.cv[cs][c / 4][row][0];
                             const int q = (c % 4) * 2;
@@ -449,6 +467,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                             if (meta) mbar_arrive(smem_u32(&sm.m_full[g % kMetas]));
                         }
                     }
+                    last_pos = pos;
                 }
             }
             if (lane == 0) mbar_arrive(smem_u32(&sm.n_full[seg & 1]));
@@ -459,7 +478,9 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
         const int u = (warp - kSoftmax) / 4, quad = warp & 3, r = quad * 32 + lane;
         const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
         const uint32_t scol = tbase + u * 128 + lanes, ocol = tbase + 256 + u * D + lanes;
-        uint32_t cnt = 0, items = 0, g = 0;  // tiles and items of this row tile; tiles of the CTA
+        uint32_t cnt = 0, g = 0;        // tiles of this pipeline, of the CTA
+        uint32_t outs0 = 0, outs1 = 0;  // results of both pipelines so far
+        uint32_t handed = 0;            // of them, second ones that went through the first
         int seg = 0;
         int lim = 0;     // tokens that the thread's row sees
         float qf = 0.f;  // scale of its scores
@@ -469,13 +490,13 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
         // the warp's 32 rows of Q to shared memory
         auto load_q = [&](const Item& w) {
             constexpr int kLanes = D / 8, kRows = 32 / kLanes;  // lanes of a row (8 values each), rows at a time
-            const int c = lane % kLanes;
+            const int c = lane % kLanes, top = w.two ? u * kRowTile : 0;
             const Rows rows = w.rows;
 #pragma unroll 2
             for (int k = 0; k < 32 / kRows; ++k) {
                 const int at = quad * 32 + k * kRows + lane / kLanes;
                 int hd;
-                const int rr = rows.of(p, u * kRowTile + at, hd);
+                const int rr = rows.of(p, top + at, hd);
                 const __nv_bfloat16* src = p.q + ((size_t)max(rr, 0) * p.pl.heads + (rr >= 0 ? hd : 0)) * D + c * 8;
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
                                  smem_u32(&sm.q[u][c / 8][at][((c % 8) ^ (at & 7)) * 16])),
@@ -489,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
 #pragma unroll 1
             for (int k0 = 0; k0 < 32 / kRows; k0 += kB) {
                 uint4 w[kB];
-                uint32_t top[kB];
+                uint32_t big[kB];
                 auto at = [&](int k) { return quad * 32 + (k0 + k) * kRows + lane / kLanes; };
                 auto mine = [&](int k) { return reinterpret_cast<uint4*>(&sm.q[u][c / 8][at(k)][((c % 8) ^ (at(k) & 7)) * 16]); };
 #pragma unroll
@@ -497,26 +518,26 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
 #pragma unroll
                 for (int k = 0; k < kB; ++k) {
                     const uint32_t a = 0x7fff7fffu;
-                    top[k] = __vmaxu2(__vmaxu2(w[k].x & a, w[k].y & a), __vmaxu2(w[k].z & a, w[k].w & a));
-                    if (__vcmpgeu2(top[k], 0x7f807f80u)) {  // an infinity or NaN: the finite ones' largest
+                    big[k] = __vmaxu2(__vmaxu2(w[k].x & a, w[k].y & a), __vmaxu2(w[k].z & a, w[k].w & a));
+                    if (__vcmpgeu2(big[k], 0x7f807f80u)) {  // an infinity or NaN: the finite ones' largest
                         const uint32_t v[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
-                        top[k] = 0;
+                        big[k] = 0;
 #pragma unroll 1
                         for (int e = 0; e < 8; ++e) {
                             const uint32_t b = ((e < 4 ? (e < 2 ? v[0] : v[1]) : (e < 6 ? v[2] : v[3])) >> (16 * (e & 1))) & 0x7fffu;
-                            if (b < 0x7f80u) top[k] = max(top[k], b);
+                            if (b < 0x7f80u) big[k] = max(big[k], b);
                         }
                     }
-                    top[k] = max(top[k] & 0xffffu, top[k] >> 16);
+                    big[k] = max(big[k] & 0xffffu, big[k] >> 16);
                 }
 #pragma unroll
                 for (int o = kLanes / 2; o; o >>= 1) {
 #pragma unroll
-                    for (int k = 0; k < kB; ++k) top[k] = max(top[k], __shfl_xor_sync(0xffffffffu, top[k], o));
+                    for (int k = 0; k < kB; ++k) big[k] = max(big[k], __shfl_xor_sync(0xffffffffu, big[k], o));
                 }
 #pragma unroll
                 for (int k = 0; k < kB; ++k) {
-                    const float scale = scale_for(__uint_as_float(top[k] << 16));
+                    const float scale = scale_for(__uint_as_float(big[k] << 16));
                     // (a power of two from 2^-126 to 2^120: its inverse by its exponent)
                     const float inv = scale > 0.f ? __uint_as_float(0x7f000000u - __float_as_uint(scale)) : 1.f;
                     const uint32_t v[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
@@ -534,7 +555,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sm.q_full[u]));
             int head;
-            lim = limit(w, rows.of(p, u * kRowTile + r, head));
+            lim = limit(w, rows.of(p, top + r, head));
             qf = sm.qf[u][r];
             __syncwarp();
         };
@@ -543,16 +564,20 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
             wait_phase(smem_u32(&sm.i_full[k % kItemRing]), (k / kItemRing) & 1, abort_at, p.budget_ns);
             const Item& w = sm.item[k % kItemRing];
             if (w.te == 0) return false;
-            if (u == 0 || w.two) load_q(w);
+            if (u == 0 || w.two || w.te - w.tb > 1) load_q(w);  // (the second pipeline has nothing of a single tile)
             return true;
         };
         bool more = begin(0);
         while (more && !*abortf) {
             const Item& it = sm.item[seg % kItemRing];
             const int nt = it.te - it.tb;
-            const bool active = u == 0 || it.two;
+            // two row tiles: each pipeline has its rows and every tile; else both have the same rows, and tiles in turn
+            const int two = it.two, own = two ? 0 : u, step = two ? 1 : 2;
             float m = -INFINITY, l = 0.f;
-            for (int i = 0; i < nt && active; ++i, ++cnt) {
+            if (u == 1 && handed) {  // (what the first pipeline takes over is this one's O, which the next P replaces)
+                wait_phase(smem_u32(&sm.x_empty), (handed - 1) & 1, abort_at, p.budget_ns);
+            }
+            for (int i = own; i < nt; i += step, ++cnt) {
                 const uint32_t gt = g + i;
                 wait_phase(smem_u32(&sm.m_full[gt % kMetas]), (gt / kMetas) & 1, abort_at, p.budget_ns);
                 const Meta ma = sm.meta[gt % kMetas][0], mb = sm.meta[gt % kMetas][1];
@@ -589,7 +614,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                     const float now = up ? mx - kTop : m, f = up ? fast_exp2(m - now) : 1.f;
                     l *= f;
                     m = now;
-                    if (i > 0) {  // O holds the tiles so far: QK of this one was issued behind their PV
+                    if (i > own) {  // O holds the tiles so far: QK of this one was issued behind their PV
 #pragma unroll 1
                         for (int c = 0; c < D; c += 16) {
                             uint32_t o[16];
@@ -639,9 +664,25 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 sm.start[head_part] = it.start;
                 sm.tiles[head_part] = it.tiles;
             }
-            if (active) {
-                wait_phase(smem_u32(&sm.o_full[u]), items & 1, abort_at, p.budget_ns);
-                ++items;
+            const bool hand = !two && nt > 1;  // the second pipeline's result goes to the first
+            if (hand && u == 1) {
+                sm.ml[r] = make_float2(m, l);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sm.x_full));
+            }
+            if (two || u == 0) {
+                wait_phase(smem_u32(&sm.o_full[u]), (u ? outs1 : outs0) & 1, abort_at, p.budget_ns);
+                float f = 1.f, f1 = 0.f;  // factors of the two pipelines' O
+                if (hand) {
+                    wait_phase(smem_u32(&sm.o_full[1]), outs1 & 1, abort_at, p.budget_ns);
+                    wait_phase(smem_u32(&sm.x_full), handed & 1, abort_at, p.budget_ns);
+                    const float2 other = sm.ml[r];
+                    const float top = fmaxf(m, other.x), at0 = top == -INFINITY ? 0.f : top;
+                    f = fast_exp2(m - at0);
+                    f1 = fast_exp2(other.x - at0);
+                    m = top;
+                    l = fmaf(l, f, other.y * f1);
+                }
                 tc_fence_after();
                 bool nan = false;
 #pragma unroll
@@ -649,13 +690,24 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 float* part = p.parts + ((size_t)blockIdx.x * 2 + head_part) * kItemRows * (D + 2);
                 const float inv = l != 0.f ? exp2f(base) / l : 0.f;
                 int head0;
-                const int row0 = it.rows.of(p, u * kRowTile + r, head0);
+                const int row0 = it.rows.of(p, (two ? u * kRowTile : 0) + r, head0);
                 const size_t at = (size_t)max(row0, 0) * p.pl.heads + head0;
 #pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
                     uint32_t o[32];
                     tmem_ld_32x32b_x32(ocol + c, o);
                     tmem_wait_ld();
+                    if (hand) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 16) {
+                            uint32_t x[16];
+                            tmem_ld_32x32b_x16(ocol + D + c + e, x);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int k = 0; k < 16; ++k)
+                                o[e + k] = __float_as_uint(fmaf(__uint_as_float(o[e + k]), f, __uint_as_float(x[k]) * f1));
+                        }
+                    }
                     if (nan) {
 #pragma unroll 1
                         for (int e = 0; e < 32; ++e) {
@@ -691,6 +743,10 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 tc_fence_before();
             }
             __syncwarp();
+            if (hand && u == 0 && lane == 0) mbar_arrive(smem_u32(&sm.x_empty));
+            outs0 += 1;
+            outs1 += two || hand;
+            handed += hand;
             if (lane == 0) {
                 mbar_arrive(smem_u32(&sm.n_empty[seg & 1]));
                 mbar_arrive(smem_u32(&sm.i_empty[seg % kItemRing]));
