@@ -3,6 +3,8 @@
 Each .cu file under csrc/ is compiled by nvcc in parallel and linked into one shared
 object with the CUDA runtime linked statically, so the library loads on a machine
 without a GPU driver (the driver is only needed once a call reaches the device).
+csrc/host/cache_call.cpp becomes _cache_call.so, the Python extension through which cache.py
+makes its calls (g++, against the installed torch).
 
 Variants (built only on request, each in a folder and a library of its own, so that the
 default libssba.so is never affected):
@@ -20,6 +22,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -33,6 +36,32 @@ VARIANTS = {"": [], "timeline": ["-DSSBA_TIMELINE=2"], "phases": ["-DSSBA_TIMELI
 
 def library_file(variant: str = "") -> str:
     return LIB if not variant else os.path.join(HERE, f"libssba_{variant}.so")
+
+
+def call_file() -> str:
+    return os.path.join(HERE, "_cache_call.so")
+
+
+def build_call(force: bool = False) -> str:
+    """Compiles the Python extension of the cache's calls; returns its path."""
+    import torch
+
+    src, out = os.path.join(CSRC, "host", "cache_call.cpp"), call_file()
+    home = os.path.dirname(torch.__file__)
+    if force or _stale(out, [src, os.path.join(INCLUDE, "ssba.h"), os.path.join(home, "version.py")]):
+        cuda = os.path.dirname(os.path.dirname(os.path.realpath(_nvcc())))
+        tmp = out + f".tmp{os.getpid()}"
+        cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", src, "-o", tmp, "-I", INCLUDE]
+        for inc in (os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"),
+                    os.path.join(cuda, "include"), sysconfig.get_paths()["include"]):
+            cmd += ["-isystem", inc]
+        cmd += [f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-L", os.path.join(home, "lib"),
+                "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"g++ failed for {src}:\n{r.stdout}\n{r.stderr}")
+        os.replace(tmp, out)
+    return out
 
 
 def _nvcc() -> str:
@@ -86,10 +115,12 @@ def build(force: bool = False, verbose: bool = False, extra_flags=(), variant: s
         os.replace(obj + ".tmp", obj)
         return r.stderr
 
-    with cf.ThreadPoolExecutor(max_workers=max(1, min(len(jobs), os.cpu_count() or 4))) as ex:
+    with cf.ThreadPoolExecutor(max_workers=max(1, min(len(jobs) + 1, os.cpu_count() or 4))) as ex:
+        call = ex.submit(build_call, force)
         for out in ex.map(compile_one, jobs):
             if verbose and out:
                 print(out, file=sys.stderr)
+        call.result()
     objs = [os.path.join(objdir, os.path.basename(s)[:-3] + ".o") for s in sources()]
     if force or jobs or _stale(lib, objs):
         tmp = lib + f".tmp{os.getpid()}"

@@ -10,11 +10,13 @@ the library's kernels.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
+import os
 from dataclasses import dataclass
 
 import torch
 
-from . import api
+from . import api, build
 from .api import (SSBA_BF16, SSBA_ERR_INVALID, SSBA_ERR_WORKSPACE, SSBA_FP32, SsbaError, _check, _empty, _lock,
                   _raise_on, _side, _stream_ptr, load_library)
 
@@ -47,7 +49,7 @@ class Cache:
     """The pool's tensors: K, V float8_e4m3fn [pages, kv_heads, 64, head_dim]; k_scale, v_scale fp32
     [pages, kv_heads]; k_mean fp32 [pages, kv_heads, head_dim]. They are checked here, once, and are the pool's
     for good: a tensor may not be resized or given other memory while the calls use it."""
-    __slots__ = ("K", "V", "k_scale", "v_scale", "k_mean", "_shape", "_dev", "_ref", "_c")
+    __slots__ = ("K", "V", "k_scale", "v_scale", "k_mean", "_shape", "_dev", "_ref", "_c", "_calls")
 
     def __init__(self, K: torch.Tensor, V: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
                  k_mean: torch.Tensor):
@@ -70,6 +72,7 @@ class Cache:
         c = api._Cache(*(t.data_ptr() for t in tensors))
         put(self, "_c", c)
         put(self, "_ref", ctypes.byref(c))
+        put(self, "_calls", {})
 
     def __setattr__(self, name, value):
         raise AttributeError("a cache's tensors are given when it is made")
@@ -112,6 +115,38 @@ def _pool(pl: _Plan, cache: Cache):
     if dev.index != torch._C._cuda_getDevice():
         raise SsbaError(SSBA_ERR_INVALID, f"the cache is on {dev}, the current device is cuda:{torch.cuda.current_device()}")
     return dev
+
+
+_ext = None
+
+
+def _extension():
+    """The native short way into the calls (csrc/host/cache_call.cpp), made by build() beside the library."""
+    global _ext
+    with _lock:
+        if _ext is None:
+            path = build.call_file()
+            if not os.path.exists(path):
+                raise SsbaError(api.SSBA_ERR_CUDA, f"{path} is missing: run paper_2605_15684_gb300.build.build()")
+            spec = importlib.util.spec_from_file_location("_cache_call", path)
+            ext = importlib.util.module_from_spec(spec)
+            spec.loader.exec_module(ext)
+            _ext = ext
+    return _ext
+
+
+def _call(pl: _Plan, cache: Cache):
+    """What the native calls take for this descriptor and pool; None where the pool is not the descriptor's."""
+    if cache.__class__ is not Cache or cache._shape != pl.shape:
+        return None
+    call = cache._calls.get(pl)
+    if call is None:
+        lib, ext = load_library(), _extension()
+        fns = [ctypes.cast(getattr(lib, "ssba_cache_" + n), ctypes.c_void_p).value for n in ("append", "select", "attend", "copy")]
+        call = ext.bind(*fns, ctypes.addressof(pl.c), ctypes.addressof(cache._c), cache._dev.index,
+                        pl.dtype is torch.bfloat16)
+        cache._calls[pl] = call
+    return call
 
 
 def _on(t, name: str, shape, dtype, dev) -> None:
@@ -161,8 +196,15 @@ def cache_alloc(desc: CacheDesc, device="cuda") -> Cache:
 def cache_append(desc: CacheDesc, cache: Cache, k, v, table, lens, cu, stream=None) -> Cache:
     """ssba_cache_append: k, v [T, kv_heads, head_dim] into the pages of their sequences; table [B, width],
     lens [B] (tokens held before), cu [B + 1], all int32. Returns the cache."""
-    lib = api._lib or load_library()
     pl = _plan(desc)
+    if stream is None:
+        call = _call(pl, cache)
+        rc = _ext.append(call, k, v, table, lens, cu) if call is not None else None
+        if rc == 0:
+            return cache
+        if rc is not None:
+            _raise_on(rc)
+    lib = load_library()
     dev = _pool(pl, cache)
     T = _rows(k, "k", pl.kv, pl, dev)
     _on(v, "v", k.shape, pl.dtype, dev)
@@ -176,8 +218,15 @@ def cache_select(desc: CacheDesc, cache: Cache, q, table, lens, cu, keep: int, f
                  stream=None):
     """ssba_cache_select: q [T, heads, head_dim] -> (idx [T, kv_heads, keep], cnt [T, kv_heads]) int32.
     lens: tokens held, the rows of q among them."""
-    lib = api._lib or load_library()
     pl = _plan(desc)
+    if stream is None and idx is None and cnt is None:
+        call = _call(pl, cache)
+        out = _ext.select(call, q, table, lens, cu, keep, first) if call is not None else None
+        if out.__class__ is tuple:
+            return out
+        if out is not None:
+            _raise_on(out)
+    lib = load_library()
     dev = _pool(pl, cache)
     T = _rows(q, "q", pl.heads, pl, dev)
     batch = _batch(table, lens, cu, dev)
@@ -236,8 +285,16 @@ def cache_attend(desc: CacheDesc, cache: Cache, q, table, lens, cu, idx=None, cn
                  workspace="default", stream=None):
     """ssba_cache_attend: q [T, heads, head_dim] -> (O [T, heads, head_dim], lse [T, heads] fp32), over every
     page of the rows' sequences, or over the lists (idx, cnt) of cache_select."""
-    lib = api._lib or load_library()
     pl = _plan(desc)
+    if stream is None and O is None and lse is None and workspace.__class__ is str:
+        call = _call(pl, cache)
+        if call is not None and cache._dev.index == torch._C._cuda_getDevice():
+            out = _ext.attend(call, q, table, lens, cu, idx, cnt, _default_workspace(pl, api._lib, cache._dev, None, None))
+            if out.__class__ is tuple:
+                return out
+            if out is not None:
+                _raise_on(out)
+    lib = load_library()
     dev = _pool(pl, cache)
     T = _rows(q, "q", pl.heads, pl, dev)
     batch = _batch(table, lens, cu, dev)
@@ -280,8 +337,15 @@ def test_cache_timeout(desc: CacheDesc, cache: Cache, q, table, lens, cu, O, lse
 
 def cache_copy(desc: CacheDesc, cache: Cache, src, dst, stream=None) -> Cache:
     """ssba_cache_copy: pages src[i] -> dst[i], int32 CUDA tensors [n]. Returns the cache."""
-    lib = api._lib or load_library()
     pl = _plan(desc)
+    if stream is None:
+        call = _call(pl, cache)
+        rc = _ext.copy(call, src, dst) if call is not None else None
+        if rc == 0:
+            return cache
+        if rc is not None:
+            _raise_on(rc)
+    lib = load_library()
     dev = _pool(pl, cache)
     n = src.numel() if isinstance(src, torch.Tensor) else -1
     _on(src, "src", (max(n, 0),), torch.int32, dev)
