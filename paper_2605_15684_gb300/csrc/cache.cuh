@@ -36,11 +36,19 @@ struct Seq {
     int row, n, len;  // rows [row, row + n) of the batch; tokens held
 };
 
+// A load of what an earlier grid may have written. Not the read-only path (__ldg): these kernels may start beside that
+// grid's end, so what it writes is not constant for their whole time.
+template <typename T>
+__device__ __forceinline__ T ld(const T* p)
+{
+    return *p;
+}
+
 __device__ __forceinline__ void flag(int* status) { *status = SSBA_ERR_CHECK; }
 
 __device__ __forceinline__ Seq load_seq(const Batch& bt, int b, int* status)
 {
-    const int c0 = __ldg(bt.cu + b), c1 = __ldg(bt.cu + b + 1), l = __ldg(bt.lens + b);
+    const int c0 = ld(bt.cu + b), c1 = ld(bt.cu + b + 1), l = ld(bt.lens + b);
     Seq s;
     s.row = min(max(c0, 0), bt.T);
     const int end = min(max(c1, s.row), bt.T);
@@ -62,14 +70,14 @@ __device__ __forceinline__ int visible(const Seq& s, int t, int* status)
 __device__ __forceinline__ int find_seq(const Batch& bt, int t, int lane)
 {
     if (t < bt.B) {  // most batches have one row a sequence: then this is it
-        const int c0 = __ldg(bt.cu + t), c1 = __ldg(bt.cu + t + 1);
+        const int c0 = ld(bt.cu + t), c1 = ld(bt.cu + t + 1);
         if (c0 <= t && t < c1) return t;
     }
-    if (t < __ldg(bt.cu) || t >= __ldg(bt.cu + bt.B)) return -1;
+    if (t < ld(bt.cu) || t >= ld(bt.cu + bt.B)) return -1;
     int lo = 0, n = bt.B;  // the answer lies in [lo, lo + n)
     while (n > 1) {
         const int step = (n + 31) / 32, at = lo + lane * step;
-        const bool le = lane * step < n && __ldg(bt.cu + at) <= t;
+        const bool le = lane * step < n && ld(bt.cu + at) <= t;
         const unsigned m = __ballot_sync(0xffffffffu, le);
         const int k = m ? 31 - __clz(m) : 0;
         n = min(step, n - k * step);
@@ -81,7 +89,7 @@ __device__ __forceinline__ int find_seq(const Batch& bt, int t, int lane)
 // Page of label j of sequence b, or -1 (flagged) when the table holds none of the pool's.
 __device__ __forceinline__ int page_of(const Batch& bt, const Pool& pl, int b, int j)
 {
-    const int p = __ldg(bt.table + (size_t)b * bt.width + j);
+    const int p = ld(bt.table + (size_t)b * bt.width + j);
     if (p >= 0 && p < pl.pages) return p;
     flag(pl.status);
     return -1;
@@ -122,6 +130,26 @@ __device__ __forceinline__ float scale_for(float amax)
     const uint32_t u = __float_as_uint(amax);
     const int k = static_cast<int>(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
     return __uint_as_float(static_cast<uint32_t>(max(k, -126) + 127) << 23);
+}
+
+// Launch in the stream's order, but allowed to start beside the last grid's end: the kernels wait for that grid before
+// they touch memory that it may have written (griddepcontrol).
+template <class... P, class... A>
+cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, A... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+    if (e == cudaSuccess) e = cudaGetLastError();
+    return e;
 }
 
 }  // namespace cache

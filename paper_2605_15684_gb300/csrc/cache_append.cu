@@ -12,6 +12,7 @@
 #include <cmath>
 
 #include "cache.cuh"
+#include "ptx.cuh"
 
 namespace ssba {
 namespace cache {
@@ -19,7 +20,6 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
-constexpr int kSeqs = 1024;  // sequences whose pages are counted at a time
 constexpr int kStages = 2;
 
 // 16 bytes of input: running largest magnitude of finite values (as bits that are ordered like them), and e4m3
@@ -84,11 +84,11 @@ struct Chunk<float> {
     }
 };
 
-// Touched pages of sequences [b0, b0 + kSeqs): ends[i] is how many those up to b0 + i have; returns their sum.
+// Touched pages of sequences [b0, b0 + kEach * kThreads): ends[i] is how many those up to b0 + i have; returns their sum.
+template <int kEach>
 __device__ int count_pages(const Batch& bt, int b0, int* status, int* ends, int* buf)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    constexpr int kEach = kSeqs / kThreads;
     int cnt[kEach], sum = 0;
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
@@ -132,11 +132,13 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool real)
 // A unit is a touched page, a head, and K or V. A CTA takes consecutive ones, so that it seldom has to look for a page;
 // the inputs of the next one are under way (each thread copies to shared memory what it will read itself) while
 // one is worked on.
-template <typename T, int D>
+// kEach: sequences that a thread counts, 1 for batches of up to 128.
+template <typename T, int D, int kEach>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 2) ssba_cache_append_kernel(const Pool pl, const Batch bt, const T* k,
                                                                      const T* v)
 {
     constexpr int kN = Chunk<T>::n, kRowChunks = D / kN, kRows = kThreads / kRowChunks, kPass = kPage / kRows;
+    constexpr int kSeqs = kEach * kThreads;
     extern __shared__ uint4 stage[];  // [kStages][kPass][kThreads]
     __shared__ int ends[kSeqs];
     __shared__ int buf[kWarps];
@@ -151,9 +153,11 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 2) ssba_cache_a
         bool v, real;
         float was;
     };
+    ptx::grid_dep_wait();
+    ptx::grid_dep_launch();
     int turn = 0, phase = 0;
     for (int b0 = 0; b0 < bt.B; b0 += kSeqs) {
-        const int pages = count_pages(bt, b0, pl.status, ends, buf), each = 2 * pl.kv_heads;
+        const int pages = count_pages<kEach>(bt, b0, pl.status, ends, buf), each = 2 * pl.kv_heads;
         const long long units = (long long)pages * each;
         const bool small = units < INT_MAX / 65536;  // (32-bit division where it does)
         long long u = small ? (int)units * (int)blockIdx.x / (int)gridDim.x : units * blockIdx.x / gridDim.x;
@@ -313,8 +317,10 @@ constexpr int kCopyThreads = 256;
 __global__ void __launch_bounds__(kCopyThreads) ssba_cache_copy_kernel(const Pool pl, int D, const int32_t* src,
                                                                    const int32_t* dst)
 {
+    ptx::grid_dep_wait();
+    ptx::grid_dep_launch();
     const int i = blockIdx.x, h = blockIdx.y;
-    const int a = __ldg(src + i), b = __ldg(dst + i);
+    const int a = ld(src + i), b = ld(dst + i);
     if (a < 0 || a >= pl.pages || b < 0 || b >= pl.pages) {
         if (threadIdx.x == 0) flag(pl.status);
         return;
@@ -345,28 +351,33 @@ __global__ void __launch_bounds__(kCopyThreads) ssba_cache_copy_kernel(const Poo
     }
 }
 
-int launched(const char* who)
+int launched(const char* who, cudaError_t e)
 {
-    const cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess) return SSBA_OK;
     set_error("%s: %s", who, cudaGetErrorString(e));
     return SSBA_ERR_CUDA;
 }
 
-template <typename T, int D>
+template <typename T, int D, int kEach>
 int append_as(const Pool& pl, const Batch& bt, const void* k, const void* v, cudaStream_t st)
 {
     const size_t smem = (size_t)kStages * kPage * D * sizeof(T);
     static PerDeviceOnce once;
     once.run([smem] {
-        cudaFuncSetAttribute(ssba_cache_append_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        cudaFuncSetAttribute(ssba_cache_append_kernel<T, D, kEach>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     });
     // every touched page takes a new token, and a run of n tokens touches at most n / 64 + 2 pages
     const long long units = std::min<long long>(bt.T, bt.T / kPage + 2LL * bt.B) * pl.kv_heads * 2;
     const int fit = (int)std::min<size_t>(8, (size_t)200 * 1024 / (smem + 8192));  // CTAs of an SM
-    ssba_cache_append_kernel<T, D><<<(int)std::min<long long>(units, (long long)fit * device_sm_count()), kThreads, smem, st>>>(
-        pl, bt, static_cast<const T*>(k), static_cast<const T*>(v));
-    return launched("ssba_cache_append");
+    const dim3 grid((unsigned)std::min<long long>(units, (long long)fit * device_sm_count()));
+    return launched("ssba_cache_append", launch_dependent(ssba_cache_append_kernel<T, D, kEach>, grid, kThreads, smem, st, pl, bt,
+                                                          static_cast<const T*>(k), static_cast<const T*>(v)));
+}
+
+template <typename T, int D>
+int append_any(const Pool& pl, const Batch& bt, const void* k, const void* v, cudaStream_t st)
+{
+    return bt.B <= kThreads ? append_as<T, D, 1>(pl, bt, k, v, st) : append_as<T, D, 8>(pl, bt, k, v, st);
 }
 
 }  // namespace
@@ -376,17 +387,17 @@ int launch_cache_append(const cache::Pool& pl, const cache::Batch& bt, int head_
                         const void* v, cudaStream_t st)
 {
     if (dtype == SSBA_BF16)
-        return head_dim == 64 ? cache::append_as<__nv_bfloat16, 64>(pl, bt, k, v, st)
-                              : cache::append_as<__nv_bfloat16, 128>(pl, bt, k, v, st);
-    return head_dim == 64 ? cache::append_as<float, 64>(pl, bt, k, v, st)
-                          : cache::append_as<float, 128>(pl, bt, k, v, st);
+        return head_dim == 64 ? cache::append_any<__nv_bfloat16, 64>(pl, bt, k, v, st)
+                              : cache::append_any<__nv_bfloat16, 128>(pl, bt, k, v, st);
+    return head_dim == 64 ? cache::append_any<float, 64>(pl, bt, k, v, st)
+                          : cache::append_any<float, 128>(pl, bt, k, v, st);
 }
 
 int launch_cache_copy(const cache::Pool& pl, int head_dim, const int32_t* src, const int32_t* dst, int n,
                       cudaStream_t st)
 {
-    cache::ssba_cache_copy_kernel<<<dim3(n, pl.kv_heads), cache::kCopyThreads, 0, st>>>(pl, head_dim, src, dst);
-    return cache::launched("ssba_cache_copy");
+    return cache::launched("ssba_cache_copy", cache::launch_dependent(cache::ssba_cache_copy_kernel, dim3(n, pl.kv_heads),
+                                                                      cache::kCopyThreads, 0, st, pl, head_dim, src, dst));
 }
 
 }  // namespace ssba

@@ -383,11 +383,11 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 const int page0 = it.page(0, j0);
                 if (c0 + lane < it.te) page = it.page(2 * (c0 + lane) + w / 2, j);
                 float my_ks = 0.f, my_lv = 0.f, vs = 0.f;
-                const float vs0 = page0 >= 0 ? __ldg(p.pl.v_scale + (size_t)page0 * p.pl.kv_heads + h) : 0.f;
+                const float vs0 = page0 >= 0 ? ld(p.pl.v_scale + (size_t)page0 * p.pl.kv_heads + h) : 0.f;
                 if (page >= 0) {
                     const size_t unit = (size_t)page * p.pl.kv_heads + h;
-                    my_ks = __ldg(p.pl.k_scale + unit);
-                    vs = __ldg(p.pl.v_scale + unit);
+                    my_ks = ld(p.pl.k_scale + unit);
+                    vs = ld(p.pl.v_scale + unit);
                 }
                 if (c0 == it.tb) {
                     // V scales are taken relative to the sequence's first page's
@@ -804,18 +804,7 @@ int launch(const Maps& maps, const Params& p, cudaStream_t st)
     once.run([smem] {
         cudaFuncSetAttribute(ssba_cache_attend_rows_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     });
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(std::min(device_sm_count(), kMaxGrid), 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, ssba_cache_attend_rows_kernel<D>, maps, p);
-    if (e == cudaSuccess) e = cudaGetLastError();
+    const cudaError_t e = launch_dependent(ssba_cache_attend_rows_kernel<D>, dim3(std::min(device_sm_count(), kMaxGrid)), kThreads, smem, st, maps, p);
     if (e == cudaSuccess) return SSBA_OK;
     set_error("ssba_cache_attend: %s", cudaGetErrorString(e));
     return SSBA_ERR_CUDA;

@@ -6,6 +6,7 @@
 #include <cmath>
 
 #include "cache.cuh"
+#include "ptx.cuh"
 
 namespace ssba {
 namespace cache {
@@ -31,6 +32,8 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
     __shared__ __align__(16) float qs[H][D];
     __shared__ __align__(16) float ps[kWarps][kPage][H];
     __shared__ float ms[kWarps][H], ls[kWarps][H];
+    ptx::grid_dep_wait();
+    ptx::grid_dep_launch();
     const int t = blockIdx.x, part = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int h = blockIdx.y / chunks, chunk = blockIdx.y % chunks;
     const int b = find_seq(bt, t, lane);
@@ -43,7 +46,7 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
     const size_t row = (size_t)t * pl.kv_heads + h;
     int n = P;
     if (idx) {
-        n = __ldg(cnt + row);
+        n = ld(cnt + row);
         if (n < 0 || n > keep) {
             flag(pl.status);
             n = min(max(n, 0), keep);
@@ -63,7 +66,7 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
     for (int i = part * kWarps + warp; i < n; i += parts * kWarps) {
         int j = i;
         if (idx) {
-            j = __ldg(idx + row * keep + i);
+            j = ld(idx + row * keep + i);
             if (j < 0 || j >= P) {
                 flag(pl.status);
                 continue;
@@ -73,15 +76,15 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
         if (page < 0) continue;
         const int nt = min(kPage, L - j * kPage);  // tokens of the page that the row sees
         const size_t unit = (size_t)page * pl.kv_heads + h;
-        const float ks = __ldg(pl.k_scale + unit) * scale_log2, vs = __ldg(pl.v_scale + unit);
+        const float ks = ld(pl.k_scale + unit) * scale_log2, vs = ld(pl.v_scale + unit);
         const uint8_t* K = pl.K + unit * kPage * D;
         const uint8_t* V = pl.V + unit * kPage * D;
         float a[2][H] = {};
 #pragma unroll 1
         for (int c = 0; c < D; c += 16) {
             uint4 kk[2];
-            kk[0] = __ldg(reinterpret_cast<const uint4*>(K + lane * D + c));
-            kk[1] = __ldg(reinterpret_cast<const uint4*>(K + (lane + 32) * D + c));
+            kk[0] = ld(reinterpret_cast<const uint4*>(K + lane * D + c));
+            kk[1] = ld(reinterpret_cast<const uint4*>(K + (lane + 32) * D + c));
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float f[2][4];
@@ -118,9 +121,9 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
         for (int r = 0; r < nt; ++r) {
             float f[4];
             if (kC == 4) {
-                from_e4m3x4(__ldg(reinterpret_cast<const uint32_t*>(V + r * D) + lane), f);
+                from_e4m3x4(ld(reinterpret_cast<const uint32_t*>(V + r * D) + lane), f);
             } else {
-                const float2 y = from_e4m3x2(__ldg(reinterpret_cast<const uint16_t*>(V + r * D) + lane));
+                const float2 y = from_e4m3x2(ld(reinterpret_cast<const uint16_t*>(V + r * D) + lane));
                 f[0] = y.x;
                 f[1] = y.y;
             }
@@ -186,6 +189,8 @@ template <int D>
 __global__ void __launch_bounds__(D) ssba_cache_join_kernel(const Pool pl, const Batch bt, const float* ws, float* O,
                                                             float* lse, int parts, int chunks, int H)
 {
+    ptx::grid_dep_wait();
+    ptx::grid_dep_launch();
     const int t = blockIdx.x, h = blockIdx.y / chunks, chunk = blockIdx.y % chunks, g = blockIdx.z, c = threadIdx.x;
     const int G = pl.heads / pl.kv_heads, gg = chunk * H + g;
     if (gg >= G || find_seq(bt, t, c & 31) < 0) return;
@@ -215,13 +220,11 @@ int attend_as(const Pool& pl, const Batch& bt, float scale, const void* q, const
     // shares: as many as give the SMs work, none of fewer than a page a warp
     const int parts = (int)std::max<long long>(1, std::min<long long>(kMaxParts / std::max<long long>(items, 1), (pages + kWarps - 1) / kWarps));
     const dim3 grid(bt.T, pl.kv_heads * chunks, parts);
-    ssba_cache_attend_simt_kernel<D, H><<<grid, kThreads, 0, st>>>(pl, bt, static_cast<const float*>(q), idx, cnt, keep,
-                                                                     scale * kLog2e, static_cast<float*>(O), lse, parts_at,
-                                                                     parts, chunks);
-    if (parts > 1)
-        ssba_cache_join_kernel<D><<<dim3(bt.T, pl.kv_heads * chunks, H), D, 0, st>>>(pl, bt, parts_at, static_cast<float*>(O),
-                                                                                       lse, parts, chunks, H);
-    const cudaError_t e = cudaGetLastError();
+    cudaError_t e = launch_dependent(ssba_cache_attend_simt_kernel<D, H>, grid, kThreads, 0, st, pl, bt, static_cast<const float*>(q),
+                                     idx, cnt, keep, scale * kLog2e, static_cast<float*>(O), lse, parts_at, parts, chunks);
+    if (e == cudaSuccess && parts > 1)
+        e = launch_dependent(ssba_cache_join_kernel<D>, dim3(bt.T, pl.kv_heads * chunks, H), D, 0, st, pl, bt, parts_at,
+                             static_cast<float*>(O), lse, parts, chunks, H);
     if (e == cudaSuccess) return SSBA_OK;
     set_error("ssba_cache_attend: %s", cudaGetErrorString(e));
     return SSBA_ERR_CUDA;

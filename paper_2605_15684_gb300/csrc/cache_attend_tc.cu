@@ -334,7 +334,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
                     const int r = r0 + u * kRows + lane / kLanes;
                     int head;
                     row[u] = r < R ? it.row_of(r, head) : -1;
-                    in[u] = row[u] >= 0 ? __ldg(reinterpret_cast<const uint4*>(p.q + ((size_t)row[u] * p.pl.heads + head) * D) + c)
+                    in[u] = row[u] >= 0 ? ld(reinterpret_cast<const uint4*>(p.q + ((size_t)row[u] * p.pl.heads + head) * D) + c)
                                         : make_uint4(0, 0, 0, 0);
                 }
 #pragma unroll
@@ -387,8 +387,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
                 float ks = 0.f, vs = 0.f;
                 if (page >= 0) {
                     const size_t unit = (size_t)page * p.pl.kv_heads + h;
-                    ks = __ldg(p.pl.k_scale + unit);
-                    vs = __ldg(p.pl.v_scale + unit);
+                    ks = ld(p.pl.k_scale + unit);
+                    vs = ld(p.pl.v_scale + unit);
                 }
                 wait_phase(smem_u32(&sm.m_empty[ch & 1]), ((ch >> 1) & 1) ^ 1, abort_at, p.budget_ns);
                 sm.ks[ch & 1][lane] = ks;
@@ -688,19 +688,7 @@ int launch(const Maps& maps, const Params& p, cudaStream_t st)
     once.run([smem] {
         cudaFuncSetAttribute(ssba_cache_attend_tc_kernel<R, D, kList>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     });
-    const int grid = std::min(device_sm_count() * C::kCtas, kMaxGrid);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid, 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, ssba_cache_attend_tc_kernel<R, D, kList>, maps, p);
-    if (e == cudaSuccess) e = cudaGetLastError();
+    const cudaError_t e = launch_dependent(ssba_cache_attend_tc_kernel<R, D, kList>, dim3(std::min(device_sm_count() * C::kCtas, kMaxGrid)), kThreads, smem, st, maps, p);
     if (e == cudaSuccess) return SSBA_OK;
     set_error("ssba_cache_attend: %s", cudaGetErrorString(e));
     return SSBA_ERR_CUDA;

@@ -128,7 +128,7 @@ struct Walk {
             start = item * tiles;
             t = (int)(sm.total < INT_MAX ? (int)item / heads : item / heads);
             hv = (int)(item - (long long)t * heads);
-            t += max(0, min(__ldg(p.bt.cu), p.bt.T));
+            t += max(0, min(ld(p.bt.cu), p.bt.T));
             locate();
         } else {
             b = sm.first_b;
@@ -202,10 +202,10 @@ struct Walk {
         if (!kList) return (long long)k * kPage < s.len ? k : -1;
         if (b < 0) return -1;
         const size_t at = (size_t)t * p.pl.kv_heads + hv / p.chunks;
-        int n = __ldg(p.cnt + at);
+        int n = ld(p.cnt + at);
         if (n < 0 || n > p.keep) flag(p.pl.status);
         if (k >= min(n, p.keep)) return -1;
-        const int j = __ldg(p.idx + at * p.keep + k);
+        const int j = ld(p.idx + at * p.keep + k);
         if (j >= 0 && (long long)j * kPage < limit(t)) return j;
         flag(p.pl.status);
         return -1;
@@ -250,7 +250,7 @@ __device__ void make_share(const Params& p, S& sm)
     };
     long long W = 0, mine = 0, front = 0;
     if (kList) {
-        const int r0 = max(0, min(__ldg(p.bt.cu), p.bt.T)), r1 = max(r0, min(__ldg(p.bt.cu + p.bt.B), p.bt.T));
+        const int r0 = max(0, min(ld(p.bt.cu), p.bt.T)), r1 = max(r0, min(ld(p.bt.cu + p.bt.B), p.bt.T));
         W = (long long)(r1 - r0) * heads * ((p.keep + 1) / 2);
     } else {
         for (int b0 = 0; b0 < p.bt.B; b0 += kThreads) {

@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_select_kernel(const Pool 
                 const int i = i0 + 4 * u + (lane >> 3), page = i < ns ? sc.pages[i] : -1;
                 const float4* at = reinterpret_cast<const float4*>(pl.k_mean + ((size_t)max(page, 0) * pl.kv_heads + h) * D) + sub;
 #pragma unroll
-                for (int c = 0; c < kC; ++c) km[u][c] = page >= 0 ? __ldg(at + c * 8) : make_float4(NAN, NAN, NAN, NAN);
+                for (int c = 0; c < kC; ++c) km[u][c] = page >= 0 ? ld(at + c * 8) : make_float4(NAN, NAN, NAN, NAN);
             }
             float best[kU];
             bool nan[kU];
