@@ -12,6 +12,34 @@ namespace {
 
 using namespace ptx;
 
+// Shared-memory matrix descriptor with any layout code (0 none, 2 128-byte, 4 64-byte swizzle); see sdesc_sw128.
+__device__ __forceinline__ uint64_t sdesc(uint32_t saddr, uint32_t lbo_bytes, uint32_t sbo_bytes, uint32_t layout)
+{
+    return (sdesc_sw128(saddr, lbo_bytes, sbo_bytes) & ~(7ull << 61)) | (static_cast<uint64_t>(layout) << 61);
+}
+
+// Instruction descriptor for kind::f8f6f4 with e4m3 A and B (formats 0), and for kind::f16 with fp16 ones (also 0),
+// with an fp32 accumulator; the other fields as in idesc_bf16_f32.
+__host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N, bool a_mn_major, bool b_mn_major)
+{
+    return (1u << 4) | ((a_mn_major ? 1u : 0u) << 15) | ((b_mn_major ? 1u : 0u) << 16) |
+           (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
+}
+
+// D[tmem] (+)= A[smem] * B[smem]^T of 8-bit values, K = 32, issued by one thread.
+__device__ __forceinline__ void mma_f8_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                          uint32_t accumulate)
+{
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n"
+        "}\n" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
 constexpr int kTile = 128;           // tokens of a tile: two pages
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kNowhere = 1 << 30;    // token position of a page that is not there
