@@ -237,3 +237,23 @@ def test_timeout_hook_validation(lib):
     assert call(desc(dtype=api.SSBA_FP32)) == api.SSBA_ERR_UNSUPPORTED
     assert call(desc(), q=None) == api.SSBA_ERR_INVALID
     assert call(desc(), n=need - 1) == api.SSBA_ERR_WORKSPACE
+
+
+def test_native_calls_leave_what_is_not_in_order_to_the_long_way(lib):
+    """The extension loads without a GPU, and gives None for tensors that are not the call's; its errors are Python's."""
+    ext = pc._extension()
+    d = pc.CacheDesc(8, 2, 128, 10)
+    pool_c = api._Cache(FAKE, FAKE, FAKE, FAKE, FAKE)
+    call = ext.bind(FAKE, FAKE, FAKE, FAKE, ctypes.addressof(pc._plan(d).c), ctypes.addressof(pool_c), 0, True)
+    q, t = torch.zeros(3, 8, 128, dtype=torch.bfloat16), torch.zeros(1, 4, dtype=torch.int32)
+    if not torch.cuda.is_available():
+        # (which device is current needs a driver: without one every call is left to the long way)
+        assert ext.append(call, q, q, t, t, t) is None
+        assert ext.select(call, q, t, t, t, 4, 1) is None
+        assert ext.attend(call, q, t, t, t, None, None, t) is None
+        assert ext.copy(call, t, t) is None
+    assert ext.select(call, q, t, t, t, "x", 1) is None
+    with pytest.raises(TypeError):
+        ext.attend(call, q)
+    with pytest.raises(ValueError):
+        ext.append(None, q, q, t, t, t)

@@ -302,3 +302,115 @@ def test_one_token_that_dominates_many_small_ones(n):
     assert 0.6 < want.min() <= want.max() < 0.8
     hold(O, want, bO, "O")
     hold(lse, wl, bl, "lse")
+
+
+def test_short_and_long_way_into_a_call():
+    """Outputs given or not, a stream given or not: the same results; and what is out of order is named either way."""
+    bt = Batch([700, 90], 2, 128)
+    desc, cache, q, table, lens, cu = a = args(bt, [1, 1], 8)
+    short = (*pc.cache_select(*a, 4), *pc.cache_attend(*a))
+    s = torch.cuda.current_stream()
+    long = (*pc.cache_select(*a, 4, stream=s), *pc.cache_attend(*a, stream=s))
+    torch.cuda.synchronize()
+    for x, y in zip(short, long):
+        assert x.shape == y.shape and x.dtype == y.dtype and torch.equal(x, y)
+    O, lse = pc.cache_attend(*a, short[0], short[1])
+    O2, lse2 = pc.cache_attend(*a, short[0], short[1], stream=s)
+    assert torch.equal(O, O2) and torch.equal(lse, lse2)
+    bad = [(dict(q=q.float()), "dtype"), (dict(q=q[:, :4].contiguous()), "shape"), (dict(q=q.cpu()), "CUDA tensor"),
+           (dict(q=q.repeat(1, 1, 2)[:, :, ::2]), "contiguous"), (dict(table=table.long()), "dtype"), (dict(lens=lens[:1]), "shape"),
+           (dict(cu=cu[:2]), "shape"), (dict(idx=short[0]), "together"), (dict(idx=short[0], cnt=short[1][:1]), "shape"),
+           (dict(cache=pc.cache_alloc(pc.CacheDesc(8, 2, 128, 3))), "expected"), (dict(desc=pc.CacheDesc(8, 1, 128, 3)), "expected")]
+    for kw, what in bad:
+        call = dict(desc=desc, cache=cache, q=q, table=table, lens=lens, cu=cu, idx=None, cnt=None)
+        call.update(kw)
+        for more in (dict(), dict(stream=s)):
+            with pytest.raises(api.SsbaError, match=what):
+                pc.cache_attend(**call, **more)
+    with pytest.raises(api.SsbaError, match="more than first"):
+        pc.cache_select(*a, 1)
+    with pytest.raises(api.SsbaError, match="workspace"):
+        pc.cache_attend(*a, workspace=torch.zeros(16, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(api.SsbaError, match="workspace"):
+        pc.cache_attend(*a, workspace=None)
+    with pytest.raises(AttributeError):
+        cache.K = cache.V
+    k = torch.zeros((2, 2, 128), dtype=BF16, device="cuda")
+    for kw, what in ((dict(k=k.float(), v=k), "dtype"), (dict(k=k, v=k[:1]), "shape"), (dict(k=k[:, :1].contiguous(), v=k), "shape")):
+        with pytest.raises(api.SsbaError, match=what):
+            pc.cache_append(desc, cache, kw["k"], kw["v"], table, lens, cu)
+    with pytest.raises(api.SsbaError, match="dtype"):
+        pc.cache_copy(desc, cache, cu.long(), cu.long())
+    # nothing to do
+    none = ints([0])
+    O, lse = pc.cache_attend(desc, cache, q[:0], table[:0], lens[:0], none)
+    idx, cnt = pc.cache_select(desc, cache, q[:0], table[:0], lens[:0], none, 4)
+    pc.cache_append(desc, cache, k[:0], k[:0], table[:0], lens[:0], none)
+    assert O.shape == (0, 8, 128) and lse.shape == (0, 8) and idx.shape == (0, 2, 4) and cnt.shape == (0, 2)
+    torch.cuda.synchronize()
+    assert api.get_status() == api.SSBA_OK
+
+
+@pytest.mark.parametrize("B", [129, 1500])
+def test_large_batches(B):
+    """More sequences than a CTA has threads, and than one pass counts: append, select, attend."""
+    lens = [(37 * b) % 200 + (b % 3 > 0) for b in range(B)]
+    bt = Batch([0] * B, 1, 64, pool_lens=[n + 70 for n in lens], width=5)
+    pool = bt.pool()
+    g = torch.Generator().manual_seed(1)
+    cu = shares(lens)
+    k, v = (torch.randn((cu[-1], 1, 64), generator=g).bfloat16() for _ in range(2))
+    zero = [0] * B
+    pc.cache_append(bt.desc(2), bt.cache, k.cuda(), v.cuda(), bt.gpu_table(), ints(zero), ints(cu))
+    n = [1 if b % 5 else 3 for b in range(B)]
+    cu1 = shares(n)
+    k1, v1 = (torch.randn((cu1[-1], 1, 64), generator=g).bfloat16() for _ in range(2))
+    pc.cache_append(bt.desc(2), bt.cache, k1.cuda(), v1.cuda(), bt.gpu_table(), ints(lens), ints(cu1))
+    torch.cuda.synchronize()
+    ref.append(pool, k.double().numpy(), v.double().numpy(), bt.table, zero, cu)
+    ref.append(pool, k1.double().numpy(), v1.double().numpy(), bt.table, lens, cu1)
+    got = bt.pool()
+    for name in ("K", "V", "k_scale", "v_scale", "k_mean"):
+        assert np.array_equal(getattr(got, name), getattr(pool, name), equal_nan=True), name
+    now = [a + b for a, b in zip(lens, n)]
+    q = queries(cu1[-1], 2, 64, BF16, 4)
+    idx, cnt = pc.cache_select(bt.desc(2), bt.cache, q, bt.gpu_table(), ints(now), ints(cu1), 2)
+    for li in (None, idx):
+        O, lse = pc.cache_attend(bt.desc(2), bt.cache, q, bt.gpu_table(), ints(now), ints(cu1), li, None if li is None else cnt)
+        torch.cuda.synchronize()
+        assert api.get_status() == api.SSBA_OK
+        want, wl, A, S = ref.attend(pool, q.double().cpu().numpy(), bt.table, now, cu1, 0.125, None if li is None else li.cpu().numpy())
+        bO, bl = ref.bounds(want, A, S, 64, max(now), True)
+        hold(O, want, bO, "O")
+        hold(lse, wl, bl, "lse")
+
+
+def test_a_pool_past_32_bits():
+    """Pages whose bytes lie behind 2^31 and 2^32 of K and V: appended, copied, selected and read."""
+    kv, d, pages = 8, 128, 70000  # 4.6 GB a tensor
+    desc = pc.CacheDesc(16, kv, d, pages)
+    cache = pc.cache_alloc(desc)
+    far = [pages - 1, 33000, 65600, 3, 40000]
+    table = ints([far[:3]])
+    k, v = (torch.randn((150, kv, d), device="cuda").bfloat16() for _ in range(2))
+    pc.cache_append(desc, cache, k, v, table, ints([0]), ints([0, 150]))
+    pc.cache_copy(desc, cache, ints([far[1]]), ints([far[4]]))
+    table = ints([[far[0], far[4], far[2]]])
+    small = Batch([0], kv, d, pool_lens=[150])
+    sd = small.desc(16)
+    pc.cache_append(sd, small.cache, k, v, small.gpu_table(), ints([0]), ints([0, 150]))
+    for n in (1, 30):
+        q = queries(n, 16, d, BF16)
+        want = pc.cache_attend(sd, small.cache, q, small.gpu_table()[:, :3].contiguous(), ints([150]), ints([0, n]))
+        got = pc.cache_attend(desc, cache, q, table, ints([150]), ints([0, n]))
+        lists = pc.cache_select(desc, cache, q, table, ints([150]), ints([0, n]), 2)
+        ref_l = pc.cache_select(sd, small.cache, q, small.gpu_table()[:, :3].contiguous(), ints([150]), ints([0, n]), 2)
+        torch.cuda.synchronize()
+        assert api.get_status() == api.SSBA_OK
+        for x, y in zip((*got, *lists), (*want, *ref_l)):
+            assert torch.equal(x, y)
+    qf = queries(2, 16, d, FP32)
+    df = pc.CacheDesc(16, kv, d, pages, FP32)
+    got = pc.cache_attend(df, cache, qf, table, ints([150]), ints([0, 2]))
+    want = pc.cache_attend(small.desc(16, FP32), small.cache, qf, small.gpu_table()[:, :3].contiguous(), ints([150]), ints([0, 2]))
+    assert torch.equal(got[0], want[0])
