@@ -117,67 +117,71 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi)
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Joins the np parts of an item that begins in CTA c0, in order, and writes its rows: a warp takes every sixteenth
-// row, four at a time, a lane four channels, with two parts' loads in flight.
+// A part of a shared item: O as [D / 4][256 rows] of four channels, so that a warp, whose threads are rows, writes and reads
+// 512 bytes in a row; behind it the rows' references and sums.
 template <int D>
-__device__ __noinline__ void join(const Params& p, const Rows rows, float base, int c0, int np, int w, int lane)
+struct Part {
+    float4 o[D / 4][kItemRows];
+    float2 ml[kItemRows];
+};
+
+// Joins the np parts of an item that begins in CTA c0, in order, and writes its rows: two threads a row, half of the
+// channels each, 32 at a time with two parts' loads in flight.
+template <int D>
+__device__ __noinline__ void join(const Params& p, const Rows rows, float base, int c0, int np)
 {
-    constexpr int kAhead = 2, kR = 4, kWarps = kThreads / 32;
-    const size_t size = (size_t)kItemRows * (D + 2);
-    const float scale = exp2f(base);
+    constexpr int kAhead = 2, kN = 8;
+    const int r = threadIdx.x % kItemRows, half = threadIdx.x / kItemRows;
+    int head;
+    const int row = rows.of(p, r, head);
+    if (row < 0) return;
+    // part 0 is slot 1 of CTA c0, part k slot 0 of CTA c0 + k
+    auto part = [&](int k) { return reinterpret_cast<const Part<D>*>(p.parts) + (size_t)(c0 + k) * 2 + (k == 0); };
+    float m = -INFINITY, l = 0.f;
+#pragma unroll 2
+    for (int k = 0; k < np; ++k) {
+        const float2 ml = __ldcg(&part(k)->ml[r]);
+        const float top = fmaxf(m, ml.x), at0 = top == -INFINITY ? 0.f : top;
+        l = fmaf(ml.y, fast_exp2(ml.x - at0), l * fast_exp2(m - at0));
+        m = top;
+    }
+    const float at0 = m == -INFINITY ? 0.f : m, inv = l != 0.f ? exp2f(base) / l : 0.f;
+    const size_t at = (size_t)row * p.pl.heads + head;
 #pragma unroll 1
-    for (int r0 = w; r0 < min(kItemRows, rows.n * p.gc); r0 += kR * kWarps) {
-        float m[kR], l[kR];
-        float4 o[kR];
+    for (int c = half * (D / 8); c < (half + 1) * (D / 8); c += kN) {
+        float4 o[kN];
 #pragma unroll
-        for (int u = 0; u < kR; ++u) {
-            m[u] = -INFINITY;
-            l[u] = 0.f;
-            o[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-        }
+        for (int i = 0; i < kN; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
         for (int k0 = 0; k0 < np; k0 += kAhead) {
-            float2 ml[kAhead][kR];
-            float4 v[kAhead][kR];
+            float4 v[kAhead][kN];
+            float f[kAhead];
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
-                // part 0 is slot 1 of CTA c0, part k slot 0 of CTA c0 + k
-                const float* at = p.parts + ((size_t)(c0 + k0 + k) * 2 + (k0 + k == 0)) * size;
+                const Part<D>* src = part(min(k0 + k, np - 1));
+                f[k] = k0 + k < np ? fast_exp2(__ldcg(&src->ml[r]).x - at0) : 0.f;
 #pragma unroll
-                for (int u = 0; u < kR; ++u) {
-                    const int r = r0 + u * kWarps;
-                    const bool real = k0 + k < np && r < rows.n * p.gc;
-                    ml[k][u] = real ? __ldcg(reinterpret_cast<const float2*>(at + kItemRows * D) + r) : make_float2(-INFINITY, 0.f);
-                    v[k][u] = real && lane < D / 4 ? __ldcg(reinterpret_cast<const float4*>(at + (size_t)r * D) + lane)
-                                                   : make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int i = 0; i < kN; ++i) v[k][i] = k0 + k < np ? __ldcg(&src->o[c + i][r]) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+                for (int i = 0; i < kN; ++i) {
+                    o[i].x = fmaf(v[k][i].x, f[k], o[i].x);
+                    o[i].y = fmaf(v[k][i].y, f[k], o[i].y);
+                    o[i].z = fmaf(v[k][i].z, f[k], o[i].z);
+                    o[i].w = fmaf(v[k][i].w, f[k], o[i].w);
                 }
-            }
-#pragma unroll
-            for (int u = 0; u < kR; ++u) {
-                const float top = fmaxf(fmaxf(m[u], ml[0][u].x), ml[1][u].x), at0 = top == -INFINITY ? 0.f : top;
-                const float f = fast_exp2(m[u] - at0), f0 = fast_exp2(ml[0][u].x - at0), f1 = fast_exp2(ml[1][u].x - at0);
-                m[u] = top;
-                l[u] = fmaf(ml[1][u].y, f1, fmaf(ml[0][u].y, f0, l[u] * f));
-                o[u].x = fmaf(v[1][u].x, f1, fmaf(v[0][u].x, f0, o[u].x * f));
-                o[u].y = fmaf(v[1][u].y, f1, fmaf(v[0][u].y, f0, o[u].y * f));
-                o[u].z = fmaf(v[1][u].z, f1, fmaf(v[0][u].z, f0, o[u].z * f));
-                o[u].w = fmaf(v[1][u].w, f1, fmaf(v[0][u].w, f0, o[u].w * f));
-            }
         }
 #pragma unroll
-        for (int u = 0; u < kR; ++u) {
-            int head;
-            const int row = rows.of(p, r0 + u * kWarps, head);
-            if (row < 0) continue;
-            const size_t at = (size_t)row * p.pl.heads + head;
-            const float inv = l[u] != 0.f ? scale / l[u] : 0.f;
-            if (lane < D / 4) {
-                const __nv_bfloat162 a = __floats2bfloat162_rn(o[u].x * inv, o[u].y * inv), b = __floats2bfloat162_rn(o[u].z * inv, o[u].w * inv);
-                *reinterpret_cast<uint2*>(p.O + at * D + lane * 4) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
-            }
-            if (lane == 0) p.lse[at] = l[u] != 0.f ? (m[u] + log2f(l[u])) * kLn2 : -INFINITY;
+        for (int i = 0; i < kN; i += 2) {
+            const __nv_bfloat162 y[4] = {__floats2bfloat162_rn(o[i].x * inv, o[i].y * inv), __floats2bfloat162_rn(o[i].z * inv, o[i].w * inv),
+                                         __floats2bfloat162_rn(o[i + 1].x * inv, o[i + 1].y * inv),
+                                         __floats2bfloat162_rn(o[i + 1].z * inv, o[i + 1].w * inv)};
+            *reinterpret_cast<uint4*>(p.O + at * D + (c + i) * 4) = *reinterpret_cast<const uint4*>(y);
         }
     }
+    if (half == 0) p.lse[at] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
 template <int D>
@@ -687,7 +691,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 bool nan = false;
 #pragma unroll
                 for (int k = 0; k < kConverters; ++k) nan |= sm.nan_any[seg & 1][k] != 0;
-                float* part = p.parts + ((size_t)blockIdx.x * 2 + head_part) * kItemRows * (D + 2);
+                Part<D>* part = reinterpret_cast<Part<D>*>(p.parts) + (size_t)blockIdx.x * 2 + head_part;
                 const float inv = l != 0.f ? exp2f(base) / l : 0.f;
                 int head0;
                 const int row0 = it.rows.of(p, (two ? u * kRowTile : 0) + r, head0);
@@ -735,11 +739,11 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                     } else if (!whole) {
 #pragma unroll
                         for (int e = 0; e < 32; e += 4)
-                            *reinterpret_cast<uint4*>(part + (size_t)(u * kRowTile + r) * D + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                            *reinterpret_cast<uint4*>(&part->o[(c + e) / 4][u * kRowTile + r]) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                     }
                 }
                 if (whole && row0 >= 0) p.lse[at] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
-                if (!whole) reinterpret_cast<float2*>(part + kItemRows * D)[u * kRowTile + r] = make_float2(m, l);
+                if (!whole) part->ml[u * kRowTile + r] = make_float2(m, l);
                 tc_fence_before();
             }
             __syncwarp();
@@ -787,7 +791,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
         if (threadIdx.x == 0) atomicExch(p.pl.status, SSBA_ERR_TIMEOUT);
     } else {
         for (int i = 0; i < 2; ++i)
-            if (sm.last[i]) join<D>(p, sm.rows[i], sm.base[i], sm.last_c0[i], sm.last[i], warp, lane);
+            if (sm.last[i]) join<D>(p, sm.rows[i], sm.base[i], sm.last_c0[i], sm.last[i]);
     }
     tc_fence_before();
     __syncthreads();
