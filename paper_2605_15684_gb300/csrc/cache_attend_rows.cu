@@ -24,6 +24,7 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
+#include <cstddef>
 #include <cstring>
 
 #include "cache_items.cuh"
@@ -86,6 +87,8 @@ struct __align__(1024) Smem {
     long long start[2];
     int tiles[2];
     int abort_flag, last[2], last_c0[2];
+    uint64_t t_full, d_full;  // the first item's part is written; the last item's products are done and `direct` is set
+    int direct;               // the last item's other parts were there already: the CTA's own stays in shared memory
 };
 
 __device__ __forceinline__ bool soft_any(bool x)  // over the softmax warps
@@ -126,20 +129,23 @@ struct Part {
 };
 
 // Joins the np parts of an item that begins in CTA c0, in order, and writes its rows: two threads a row, half of the
-// channels each, 32 at a time with two parts' loads in flight.
+// channels each, 32 at a time. The first part may be the CTA's own, in shared memory: an SM gets some 36 bytes a
+// nanosecond from L2, so a part of 256 rows of 128 channels that has to be read takes 3.5 us.
 template <int D>
-__device__ __noinline__ void join(const Params& p, const Rows rows, float base, int c0, int np)
+__device__ __noinline__ void join(const Params& p, const Rows rows, float base, int c0, int np, const Part<D>* own)
 {
-    constexpr int kAhead = 2, kN = 8;
+    constexpr int kN = 8;
     const int r = threadIdx.x % kItemRows, half = threadIdx.x / kItemRows;
     int head;
     const int row = rows.of(p, r, head);
     if (row < 0) return;
     // part 0 is slot 1 of CTA c0, part k slot 0 of CTA c0 + k
     auto part = [&](int k) { return reinterpret_cast<const Part<D>*>(p.parts) + (size_t)(c0 + k) * 2 + (k == 0); };
-    float m = -INFINITY, l = 0.f;
+    const int first = own ? 1 : 0;
+    const float2 mine = own ? own->ml[r] : make_float2(-INFINITY, 0.f);
+    float m = mine.x, l = mine.y;
 #pragma unroll 2
-    for (int k = 0; k < np; ++k) {
+    for (int k = first; k < np; ++k) {
         const float2 ml = __ldcg(&part(k)->ml[r]);
         const float top = fmaxf(m, ml.x), at0 = top == -INFINITY ? 0.f : top;
         l = fmaf(ml.y, fast_exp2(ml.x - at0), l * fast_exp2(m - at0));
@@ -150,28 +156,36 @@ __device__ __noinline__ void join(const Params& p, const Rows rows, float base, 
 #pragma unroll 1
     for (int c = half * (D / 8); c < (half + 1) * (D / 8); c += kN) {
         float4 o[kN];
+        auto load = [&](int k, float4 (&v)[kN]) {  // part k's factor and channels
 #pragma unroll
-        for (int i = 0; i < kN; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int i = 0; i < kN; ++i) v[i] = k < np ? __ldcg(&part(k)->o[c + i][r]) : make_float4(0.f, 0.f, 0.f, 0.f);
+            return k < np ? fast_exp2(__ldcg(&part(k)->ml[r]).x - at0) : 0.f;
+        };
+        float4 v[2][kN];
+        float f[2];
+        f[0] = load(first, v[0]);
+        f[1] = load(first + 1, v[1]);
+        const float f_own = fast_exp2(mine.x - at0);
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            o[i] = own ? own->o[c + i][r] : make_float4(0.f, 0.f, 0.f, 0.f);
+            o[i] = make_float4(fmaf(o[i].x, f_own, 0.f), fmaf(o[i].y, f_own, 0.f), fmaf(o[i].z, f_own, 0.f), fmaf(o[i].w, f_own, 0.f));
+        }
 #pragma unroll 1
-        for (int k0 = 0; k0 < np; k0 += kAhead) {
-            float4 v[kAhead][kN];
-            float f[kAhead];
+        for (int k = first;;) {
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                const Part<D>* src = part(min(k0 + k, np - 1));
-                f[k] = k0 + k < np ? fast_exp2(__ldcg(&src->ml[r]).x - at0) : 0.f;
-#pragma unroll
-                for (int i = 0; i < kN; ++i) v[k][i] = k0 + k < np ? __ldcg(&src->o[c + i][r]) : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k)
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int i = 0; i < kN; ++i) {
-                    o[i].x = fmaf(v[k][i].x, f[k], o[i].x);
-                    o[i].y = fmaf(v[k][i].y, f[k], o[i].y);
-                    o[i].z = fmaf(v[k][i].z, f[k], o[i].z);
-                    o[i].w = fmaf(v[k][i].w, f[k], o[i].w);
+                    o[i].x = fmaf(v[j][i].x, f[j], o[i].x);
+                    o[i].y = fmaf(v[j][i].y, f[j], o[i].y);
+                    o[i].z = fmaf(v[j][i].z, f[j], o[i].z);
+                    o[i].w = fmaf(v[j][i].w, f[j], o[i].w);
                 }
+            k += 2;
+            if (k >= np) break;
+            f[0] = load(k, v[0]);
+            f[1] = load(k + 1, v[1]);
         }
 #pragma unroll
         for (int i = 0; i < kN; i += 2) {
@@ -192,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
     Smem<D>& sm = *reinterpret_cast<Smem<D>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        sm.abort_flag = sm.last[0] = sm.last[1] = sm.tiles[0] = sm.tiles[1] = 0;
+        sm.abort_flag = sm.direct = sm.last[0] = sm.last[1] = sm.tiles[0] = sm.tiles[1] = 0;
         for (int i = 0; i < kItemRing; ++i) {
             mbar_init(smem_u32(&sm.i_full[i]), 1);
             mbar_init(smem_u32(&sm.i_empty[i]), 8);
@@ -217,6 +231,8 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
         mbar_init(smem_u32(&sm.x_full), 4);
         mbar_init(smem_u32(&sm.x_empty), 4);
         mbar_init(smem_u32(&sm.drain), 1);
+        mbar_init(smem_u32(&sm.t_full), 8);
+        mbar_init(smem_u32(&sm.d_full), 8);
         fence_mbar_init();
     }
     if (warp == kIssue) {
@@ -365,6 +381,20 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 }
                 if (!more) break;
                 it.next();
+            }
+        } else {
+            // counts the part of an item that began in an earlier CTA as soon as it is written, beside the next items: the fence
+            // takes microseconds, and the earlier CTA, which ends with that item, finds the part there and need not write its own
+            wait_phase(smem_u32(&sm.t_full), 0, abort_at, p.budget_ns);
+            if (lane == 0 && !*abortf && sm.tiles[0] > 0) {
+                const int c0 = cta_of(sm.start[0], sm), np = cta_of(sm.start[0] + sm.tiles[0] - 1, sm) - c0 + 1;
+                unsigned seen;
+                asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(seen) : "l"(p.tickets + c0) : "memory");
+                if (seen == (unsigned)(np - 1)) {
+                    p.tickets[c0] = 0;
+                    sm.last_c0[0] = c0;
+                    sm.last[0] = np;
+                }
             }
         }
         dead = *abortf != 0;
@@ -669,6 +699,18 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 sm.tiles[head_part] = it.tiles;
             }
             const bool hand = !two && nt > 1;  // the second pipeline's result goes to the first
+            const bool shared = head_part && !whole;  // (with later CTAs: the share's last item)
+            if (shared && threadIdx.x == kSoftmax * 32) {
+                const int c0 = blockIdx.x, np = cta_of(it.start + it.tiles - 1, sm) - c0 + 1;
+                unsigned seen;
+                asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(p.tickets + c0) : "memory");
+                if (seen == (unsigned)(np - 1)) {
+                    p.tickets[c0] = 0;
+                    sm.direct = 1;
+                    sm.last_c0[1] = c0;
+                    sm.last[1] = np;
+                }
+            }
             if (hand && u == 1) {
                 sm.ml[r] = make_float2(m, l);
                 __syncwarp();
@@ -676,9 +718,16 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
             }
             if (two || u == 0) {
                 wait_phase(smem_u32(&sm.o_full[u]), (u ? outs1 : outs0) & 1, abort_at, p.budget_ns);
+                if (hand) wait_phase(smem_u32(&sm.o_full[1]), outs1 & 1, abort_at, p.budget_ns);
+            }
+            if (shared) {  // a part in shared memory takes the place of Q, K and V: no product may be left that reads them
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sm.d_full));
+                wait_phase(smem_u32(&sm.d_full), 0, abort_at, p.budget_ns);
+            }
+            if (two || u == 0) {
                 float f = 1.f, f1 = 0.f;  // factors of the two pipelines' O
                 if (hand) {
-                    wait_phase(smem_u32(&sm.o_full[1]), outs1 & 1, abort_at, p.budget_ns);
                     wait_phase(smem_u32(&sm.x_full), handed & 1, abort_at, p.budget_ns);
                     const float2 other = sm.ml[r];
                     const float top = fmaxf(m, other.x), at0 = top == -INFINITY ? 0.f : top;
@@ -691,7 +740,8 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 bool nan = false;
 #pragma unroll
                 for (int k = 0; k < kConverters; ++k) nan |= sm.nan_any[seg & 1][k] != 0;
-                Part<D>* part = reinterpret_cast<Part<D>*>(p.parts) + (size_t)blockIdx.x * 2 + head_part;
+                Part<D>* part = shared && sm.direct ? reinterpret_cast<Part<D>*>(sm.q)
+                                                    : reinterpret_cast<Part<D>*>(p.parts) + (size_t)blockIdx.x * 2 + head_part;
                 const float inv = l != 0.f ? exp2f(base) / l : 0.f;
                 int head0;
                 const int row0 = it.rows.of(p, (two ? u * kRowTile : 0) + r, head0);
@@ -755,26 +805,20 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 mbar_arrive(smem_u32(&sm.n_empty[seg & 1]));
                 mbar_arrive(smem_u32(&sm.i_empty[seg % kItemRing]));
             }
+            if (seg == 0 && lane == 0) mbar_arrive(smem_u32(&sm.t_full));
             ++seg;
         }
-        // the items that are shared with other CTAs, counted off once all is written (see cache_attend_tc.cu)
+        if (seg == 0 && lane == 0) mbar_arrive(smem_u32(&sm.t_full));
+        // the part of the last item, where it was written for another CTA
         const bool bad = soft_any(*abortf != 0);  // (else every warp has been through every item)
-        if (!bad) {
-            const int tid = threadIdx.x - kSoftmax * 32;
-            if (tid < 2) {
-                const long long start = sm.start[tid];
-                const int tiles = sm.tiles[tid];
-                int c0 = 0, np = 0;
-                if (tiles > 0) {
-                    c0 = cta_of(start, sm);
-                    np = cta_of(start + tiles - 1, sm) - c0 + 1;
-                    unsigned seen;
-                    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(seen) : "l"(p.tickets + c0) : "memory");
-                    if (seen == (unsigned)(np - 1)) p.tickets[c0] = 0;
-                    else np = 0;
-                }
-                sm.last_c0[tid] = c0;
-                sm.last[tid] = np;
+        if (!bad && threadIdx.x == kSoftmax * 32 && sm.tiles[1] > 0 && !sm.direct) {
+            const int c0 = cta_of(sm.start[1], sm), np = cta_of(sm.start[1] + sm.tiles[1] - 1, sm) - c0 + 1;
+            unsigned seen;
+            asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(seen) : "l"(p.tickets + c0) : "memory");
+            if (seen == (unsigned)(np - 1)) {
+                p.tickets[c0] = 0;
+                sm.last_c0[1] = c0;
+                sm.last[1] = np;
             }
         }
         dead = *abortf != 0;
@@ -791,7 +835,9 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
         if (threadIdx.x == 0) atomicExch(p.pl.status, SSBA_ERR_TIMEOUT);
     } else {
         for (int i = 0; i < 2; ++i)
-            if (sm.last[i]) join<D>(p, sm.rows[i], sm.base[i], sm.last_c0[i], sm.last[i]);
+            if (sm.last[i])
+                join<D>(p, sm.rows[i], sm.base[i], sm.last_c0[i], sm.last[i],
+                        i && sm.direct ? reinterpret_cast<const Part<D>*>(sm.q) : nullptr);
     }
     tc_fence_before();
     __syncthreads();
@@ -803,6 +849,7 @@ template <int D>
 int launch(const Maps& maps, const Params& p, cudaStream_t st)
 {
     const size_t smem = sizeof(Smem<D>) + 1024;
+    static_assert(offsetof(Smem<D>, raw) >= sizeof(Part<D>), "a part in the place of Q, K and V");
     static_assert(sizeof(Smem<D>) + 1024 + 128 <= 232448, "shared memory of one CTA (227 KB opt-in limit)");
     static PerDeviceOnce once;
     once.run([smem] {
