@@ -458,14 +458,14 @@ SSBA_API size_t ssba_cache_attend_workspace_bytes(const ssba_cache_desc* desc);
  *   q           device, [T][heads][head_dim] of desc->dtype.
  *   idx, cnt    NULL: all pages of the row's sequence. Else the lists of ssba_cache_select ([T][kv_heads][keep]
  *               and [T][kv_heads]): the pages listed, in any order; one listed twice counts twice.
- *   O, lse      device out, [T][heads][head_dim] of desc->dtype and fp32 [T][heads], the natural log of the row's
- *               sum of exp(scale * q.k). A row that sees no token: O = 0, lse = -inf.
+ *   O, lse      device out, [T][heads][head_dim] of desc->dtype (32-byte aligned) and fp32 [T][heads], the natural
+ *               log of the row's sum of exp(scale * q.k). A row that sees no token: O = 0, lse = -inf.
  *   workspace   device scratch of at least ssba_cache_attend_workspace_bytes(desc), 16-byte aligned.
  *               Its first SSBA_CACHE_TICKET_BYTES are zero-filled once; a call leaves them zero (after
  *               SSBA_ERR_TIMEOUT they have to be zeroed again). Calls that may overlap on the GPU need
  *               workspaces of their own.
  * Tokens that a row does not see have no part in it, whatever their K and V hold. Products and sums are
- * fp32 (bf16 calls form products of 8-bit values exactly and round the weights to 8 bits of significand
+ * fp32 (bf16 calls form products of 8-bit values exactly and round the weights to 8 bits of significand or more
  * before they meet V). */
 SSBA_API int ssba_cache_attend(const ssba_cache_desc* desc, const ssba_cache* cache, const void* q, int32_t T,
                                const int32_t* table, int32_t width, const int32_t* lens, const int32_t* cu,

@@ -109,8 +109,8 @@ int attend(const char* who, const ssba_cache_desc* desc, const ssba_cache* cache
         return SSBA_ERR_INVALID;
     }
     if (T == 0 || B == 0) return SSBA_OK;
-    if (!q || !O || !lse || !aligned(q, 16) || !aligned(O, 16) || !aligned(lse, 4)) {
-        set_error("%s: q, O and lse must be non-null, q and O 16-byte aligned", who);
+    if (!q || !O || !lse || !aligned(q, 16) || !aligned(O, 32) || !aligned(lse, 4)) {
+        set_error("%s: q, O and lse must be non-null, q 16-byte and O 32-byte aligned", who);
         return SSBA_ERR_INVALID;
     }
     const size_t need = ssba_cache_attend_workspace_bytes(desc);
@@ -124,11 +124,12 @@ int attend(const char* who, const ssba_cache_desc* desc, const ssba_cache* cache
     const cache::Batch bt{table, lens, cu, B, width, T};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (desc->dtype == SSBA_BF16) {
-        // Rows that share a K/V head's tokens, on average over the batch's sequences: up to 16 as columns of products
-        // over the bytes, bound by HBM; more as rows of fp16 products. (16 sequences of up to 8000 tokens, 8 K/V
-        // heads: 16 rows 62 us against 113, 32 rows 129 against 115, 64 rows 198 against 118.)
+        // Rows that share a K/V head's tokens, on average over the batch's sequences: up to 16, which are the columns of one
+        // item, as columns of products over the bytes, bound by HBM; more as rows of fp16 products. (16 sequences of
+        // up to 8000 tokens, 8 K/V heads of 128: 16 rows 61 us as columns, 90 as rows; 32 rows 91, 91; 64 rows 143, 92;
+        // 128 rows 258, 125. One of 30000 tokens: 32 rows 35, 40; 64 rows 52, 42. 24 heads of 64, two of 2000: 32 rows 27, 21.)
         const long long rows = ((long long)T + B - 1) / B * (desc->heads / desc->kv_heads);
-        if (!idx && rows > 16) 
+        if (!idx && rows > 16)
             return launch_cache_attend_rows(p, bt, desc->head_dim, scale, q, O, lse, workspace, st, budget_ns, withhold);
         return launch_cache_attend_tc(p, bt, desc->head_dim, scale, q, idx, cnt, keep, O, lse, workspace, st, budget_ns, withhold);
     }

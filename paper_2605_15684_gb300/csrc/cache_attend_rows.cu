@@ -13,14 +13,21 @@
 // 11 bits; m begins 8 below the largest exponent, so P's smallest step is 2^-32 of the largest weight.
 //
 // One CTA an SM, 16 warps: a producer (TMA of the pages' bytes), an issuer, four converters (half a page each: bytes to
-// fp16 in the swizzled layout of the products), one that walks the items for the softmax, and a softmax warpgroup for each row tile (a thread is a row).
+// fp16 in the swizzled layout of the products), one that walks the items for the softmax, one that counts off a part
+// while the next items run, and a softmax warpgroup for each row tile (a thread is a row).
 // P overwrites the lower half of its S, so of one row tile PV_g comes before QK_{g + 1}; while one row tile
 // is with the tensor cores the other is with its softmax. A tile's maximum is taken first, but the row's reference is
 // raised (and O rescaled in tensor memory) only where P would pass 2^14. The softmax's code is loops over 32 scores: it
-// has to stay in the SM's instruction cache beside the other roles' (unrolled, a tile takes 2.5 us instead of 2.3).
-// What bounds it: of one row tile, S to P takes 1.2 us (one warp a scheduler, so latencies show) and PV and QK
-// of 128 x 128 x 128 another 1.1 beside the other tile's; the tensor pipe is busy 1.35 of a tile's 2.3 us.
-// Work is shared out and joined as in cache_attend_tc.cu.
+// has to stay in the SM's instruction cache beside the other roles' (unrolled, a tile takes 2.5 us instead of 2.2).
+//
+// Work is shared out and joined as in cache_attend_tc.cu, but a part is 130 KB: CTA c ends with the item that CTA c + 1
+// began with, finds that one's part there and keeps its own in shared memory. (4 sequences of 4000 tokens, 1000 rows in
+// all, 8 K/V heads of 128: 84 us; 90 with every part written, 110 with parts laid out by row, whose 16 bytes a thread
+// fill half a sector.) Results are written 32 bytes a thread for that reason too: 82 us against 85.
+// What bounds it, at that size: a tile of 256 rows takes 2.2 us, of which the four products have the tensor cores
+// for 1.35 (the loop without softmax and conversion takes 1.6); of one row tile S to P takes 1.2 us (one warp a
+// scheduler, so latencies show). Some 24 tiles a CTA are 52 us; 10 us pass before the first S (dependent loads of table, scales
+// and Q, cold instructions), 7 in the join, the rest in changes of items (2.7 us each) and shares of unequal cost.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -120,6 +127,19 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi)
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&b);
+}
+
+__device__ __forceinline__ void store32(void* to, const uint32_t (&y)[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]),
+                 "r"(y[4]), "r"(y[5]), "r"(y[6]), "r"(y[7])
+                 : "memory");
+}
+
 // A part of a shared item: O as [D / 4][256 rows] of four channels, so that a warp, whose threads are rows, writes and reads
 // 512 bytes in a row; behind it the rows' references and sums.
 template <int D>
@@ -128,74 +148,86 @@ struct Part {
     float2 ml[kItemRows];
 };
 
-// Joins the np parts of an item that begins in CTA c0, in order, and writes its rows: two threads a row, half of the
-// channels each, 32 at a time. The first part may be the CTA's own, in shared memory: an SM gets some 36 bytes a
-// nanosecond from L2, so a part of 256 rows of 128 channels that has to be read takes 3.5 us.
-template <int D>
+// Joins the np parts of an item that begins in CTA c0, in order, and writes its rows: a warp takes 32 rows and 4 kC
+// channels at a time, kP parts in flight. The first part may be the CTA's own, in shared memory.
+template <int D, int kC, int kP>
 __device__ __noinline__ void join(const Params& p, const Rows rows, float base, int c0, int np, const Part<D>* own)
 {
-    constexpr int kN = 8;
-    const int r = threadIdx.x % kItemRows, half = threadIdx.x / kItemRows;
-    int head;
-    const int row = rows.of(p, r, head);
-    if (row < 0) return;
+    constexpr int kChunks = D / 4 / kC;
+    const int lane = threadIdx.x & 31, tasks = (rows.n * p.gc + 31) / 32 * kChunks, first = own ? 1 : 0;
     // part 0 is slot 1 of CTA c0, part k slot 0 of CTA c0 + k
     auto part = [&](int k) { return reinterpret_cast<const Part<D>*>(p.parts) + (size_t)(c0 + k) * 2 + (k == 0); };
-    const int first = own ? 1 : 0;
-    const float2 mine = own ? own->ml[r] : make_float2(-INFINITY, 0.f);
-    float m = mine.x, l = mine.y;
-#pragma unroll 2
-    for (int k = first; k < np; ++k) {
-        const float2 ml = __ldcg(&part(k)->ml[r]);
-        const float top = fmaxf(m, ml.x), at0 = top == -INFINITY ? 0.f : top;
-        l = fmaf(ml.y, fast_exp2(ml.x - at0), l * fast_exp2(m - at0));
-        m = top;
-    }
-    const float at0 = m == -INFINITY ? 0.f : m, inv = l != 0.f ? exp2f(base) / l : 0.f;
-    const size_t at = (size_t)row * p.pl.heads + head;
 #pragma unroll 1
-    for (int c = half * (D / 8); c < (half + 1) * (D / 8); c += kN) {
-        float4 o[kN];
-        auto load = [&](int k, float4 (&v)[kN]) {  // part k's factor and channels
+    for (int task = threadIdx.x >> 5; task < tasks; task += kThreads / 32) {
+        const int r = task / kChunks * 32 + lane, c = task % kChunks * kC;
+        int head;
+        const int row = rows.of(p, r, head);
+        const float2 mine = own ? own->ml[r] : make_float2(-INFINITY, 0.f);
+        float m = mine.x, l = mine.y;
+#pragma unroll 1
+        for (int k0 = first; k0 < np; k0 += kP) {
+            float2 ml[kP];
 #pragma unroll
-            for (int i = 0; i < kN; ++i) v[i] = k < np ? __ldcg(&part(k)->o[c + i][r]) : make_float4(0.f, 0.f, 0.f, 0.f);
-            return k < np ? fast_exp2(__ldcg(&part(k)->ml[r]).x - at0) : 0.f;
-        };
-        float4 v[2][kN];
-        float f[2];
-        f[0] = load(first, v[0]);
-        f[1] = load(first + 1, v[1]);
-        const float f_own = fast_exp2(mine.x - at0);
+            for (int k = 0; k < kP; ++k) ml[k] = k0 + k < np ? __ldcg(&part(k0 + k)->ml[r]) : make_float2(-INFINITY, 0.f);
 #pragma unroll
-        for (int i = 0; i < kN; ++i) {
+            for (int k = 0; k < kP; ++k) {
+                const float top = fmaxf(m, ml[k].x), at0 = top == -INFINITY ? 0.f : top;
+                l = fmaf(ml[k].y, fast_exp2(ml[k].x - at0), l * fast_exp2(m - at0));
+                m = top;
+            }
+        }
+        const float at0 = m == -INFINITY ? 0.f : m, inv = l != 0.f ? exp2f(base) / l : 0.f, f_own = fast_exp2(mine.x - at0);
+        const size_t at = (size_t)max(row, 0) * p.pl.heads + head;
+        float4 o[kC];
+#pragma unroll
+        for (int i = 0; i < kC; ++i) {
             o[i] = own ? own->o[c + i][r] : make_float4(0.f, 0.f, 0.f, 0.f);
             o[i] = make_float4(fmaf(o[i].x, f_own, 0.f), fmaf(o[i].y, f_own, 0.f), fmaf(o[i].z, f_own, 0.f), fmaf(o[i].w, f_own, 0.f));
         }
 #pragma unroll 1
-        for (int k = first;;) {
+        for (int k0 = first; k0 < np; k0 += kP) {
+            float4 v[kP][kC];
+            float f[kP];
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int k = 0; k < kP; ++k) {
+                const bool real = k0 + k < np;
 #pragma unroll
-                for (int i = 0; i < kN; ++i) {
-                    o[i].x = fmaf(v[j][i].x, f[j], o[i].x);
-                    o[i].y = fmaf(v[j][i].y, f[j], o[i].y);
-                    o[i].z = fmaf(v[j][i].z, f[j], o[i].z);
-                    o[i].w = fmaf(v[j][i].w, f[j], o[i].w);
+                for (int i = 0; i < kC; ++i) v[k][i] = real ? __ldcg(&part(k0 + k)->o[c + i][r]) : make_float4(0.f, 0.f, 0.f, 0.f);
+                f[k] = real ? fast_exp2(__ldcg(&part(k0 + k)->ml[r]).x - at0) : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < kP; ++k)
+#pragma unroll
+                for (int i = 0; i < kC; ++i) {
+                    o[i].x = fmaf(v[k][i].x, f[k], o[i].x);
+                    o[i].y = fmaf(v[k][i].y, f[k], o[i].y);
+                    o[i].z = fmaf(v[k][i].z, f[k], o[i].z);
+                    o[i].w = fmaf(v[k][i].w, f[k], o[i].w);
                 }
-            k += 2;
-            if (k >= np) break;
-            f[0] = load(k, v[0]);
-            f[1] = load(k + 1, v[1]);
         }
+        if (row < 0) continue;
 #pragma unroll
-        for (int i = 0; i < kN; i += 2) {
-            const __nv_bfloat162 y[4] = {__floats2bfloat162_rn(o[i].x * inv, o[i].y * inv), __floats2bfloat162_rn(o[i].z * inv, o[i].w * inv),
-                                         __floats2bfloat162_rn(o[i + 1].x * inv, o[i + 1].y * inv),
-                                         __floats2bfloat162_rn(o[i + 1].z * inv, o[i + 1].w * inv)};
-            *reinterpret_cast<uint4*>(p.O + at * D + (c + i) * 4) = *reinterpret_cast<const uint4*>(y);
+        for (int i = 0; i < kC; i += 4) {
+            uint32_t y[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                y[2 * e] = pack_bf16(o[i + e].x * inv, o[i + e].y * inv);
+                y[2 * e + 1] = pack_bf16(o[i + e].z * inv, o[i + e].w * inv);
+            }
+            store32(p.O + at * D + (c + i) * 4, y);
         }
+        if (c == 0) p.lse[at] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
     }
-    if (half == 0) p.lse[at] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+}
+
+// Many rows of two or three parts, or few rows of many parts: the way that takes fewer round trips to L2.
+template <int D>
+__device__ __forceinline__ void join(const Params& p, const Rows& rows, float base, int c0, int np, const Part<D>* own)
+{
+    const int blocks = (rows.n * p.gc + 31) / 32, others = np - (own ? 1 : 0);
+    const int wide = (blocks * (D / 32) + 15) / 16 * others, deep = (blocks * (D / 16) + 15) / 16 * ((others + 3) / 4);
+    if (wide <= deep) join<D, 8, 1>(p, rows, base, c0, np, own);
+    else join<D, 4, 4>(p, rows, base, c0, np, own);
 }
 
 template <int D>
@@ -777,14 +809,14 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                     }
                     if (whole && row0 >= 0) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8) {
-                            uint32_t y[4];
+                        for (int e = 0; e < 32; e += 16) {
+                            uint32_t y[8];
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
+                            for (int k = 0; k < 8; ++k) {
                                 const __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
                                 y[k] = *reinterpret_cast<const uint32_t*>(&b);
                             }
-                            *reinterpret_cast<uint4*>(p.O + at * D + c + e) = make_uint4(y[0], y[1], y[2], y[3]);
+                            store32(p.O + at * D + c + e, y);
                         }
                     } else if (!whole) {
 #pragma unroll

@@ -98,6 +98,16 @@ def test_outputs_lists_and_workspaces(lib):
     assert lib.ssba_cache_copy(d, c, FAKE, FAKE, -1, None) == api.SSBA_ERR_INVALID
 
 
+@pytest.mark.parametrize("dtype", [api.SSBA_BF16, api.SSBA_FP32])
+def test_the_output_has_to_be_aligned_to_what_a_thread_writes_at_once(lib, dtype):
+    d = desc(dtype=dtype)
+    need = lib.ssba_cache_attend_workspace_bytes(d)
+    for off in (4, 8, 16):
+        assert lib.ssba_cache_attend(d, pool(), FAKE, 3, *BATCH, None, None, 0, FAKE + off, FAKE, FAKE, need,
+                                     None) == api.SSBA_ERR_INVALID
+        assert b"O 32-byte aligned" in lib.ssba_last_error()
+
+
 def test_binding_refuses_before_it_calls(lib):
     d = pc.CacheDesc(8, 2, 128, 4)
     q, t = torch.zeros(3, 8, 128, dtype=torch.bfloat16), torch.zeros(1, 4, dtype=torch.int32)

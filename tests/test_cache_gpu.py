@@ -393,3 +393,18 @@ def test_bad_values_are_flagged_and_reach_nothing():
     after = bt.pool()
     for name in ("K", "V", "k_scale", "v_scale", "k_mean"):
         assert np.array_equal(getattr(after, name), getattr(before, name), equal_nan=True)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,n,heads,kv", [([9000], [9], 8, 2), ([9000], [70], 8, 2), ([6000, 130, 2500], [300, 130, 77], 6, 3)])
+def test_attend_rows_joined_from_parts(lens, n, heads, kv, d):
+    # few rows of many parts and many rows of few: each item is shared out over several CTAs
+    bt = Batch(lens, kv, d, seed=21)
+    check_attend(bt, n, heads, seed=22)
+    # which CTA joins an item depends on who is last; the result does not
+    q, cu = queries(sum(n), heads, d, BF16, 23), ints(shares(n))
+    first = pc.cache_attend(bt.desc(heads), bt.cache, q, bt.gpu_table(), ints(lens), cu)
+    for _ in range(30):
+        again = pc.cache_attend(bt.desc(heads), bt.cache, q, bt.gpu_table(), ints(lens), cu)
+        for a, b in zip(first, again):
+            assert torch.equal(a.view(torch.int16 if a.dtype == BF16 else torch.int32), b.view(torch.int16 if b.dtype == BF16 else torch.int32))
