@@ -204,6 +204,25 @@ def test_attend_nan_behind_a_row(d, dtype):
     hold(lse, wl, bl, "lse")
 
 
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attend_pages_of_zeros_and_far_scales(d, dtype, n):
+    """Pages whose K or V is all zero (scale 0), the first one too, beside V scales from 2^-60 to 2^30."""
+    bt = Batch([700, 64, 300], 2, d, seed=31)
+    c = bt.cache
+    for b, zero_k, zero_v in ((0, (1, 4, 10), (0, 4, 7)), (1, (0,), (0,)), (2, (), (1, 4))):
+        for j in zero_k:
+            c.K.view(torch.uint8)[bt.table[b][j]] = 0
+            c.k_scale[bt.table[b][j]] = 0
+        for j in zero_v:
+            c.V.view(torch.uint8)[bt.table[b][j]] = 0
+            c.v_scale[bt.table[b][j]] = 0
+    for j, e in ((1, -60), (2, 30), (5, -3), (9, 29)):
+        c.v_scale[bt.table[0][j]] = 2.0 ** e
+    check_attend(bt, [n, 1, min(n, 9)], 4, dtype, seed=32)
+
+
 # ----------------------------------------------------------------------------- select
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("d", [64, 128])
@@ -235,6 +254,17 @@ def test_select_long(pages):
         idx, cnt = pc.cache_select(bt.desc(4), bt.cache, q, bt.gpu_table(), ints(bt.lens), ints([0, 1]), keep)
         want = ref.select(bt.pool(), q.double().cpu().numpy(), bt.table, bt.lens, [0, 1], keep, 1)
         assert np.array_equal(idx.cpu().numpy(), want[0]) and np.array_equal(cnt.cpu().numpy(), want[1])
+
+
+@pytest.mark.parametrize("keep,first", [(300, 128), (300, 129), (400, 399), (900, 517), (650, 0)])
+def test_select_many_first_pages(keep, first):
+    """More pages that are always kept than a CTA has threads."""
+    bt = Batch([64 * 700, 64 * 401 + 1, 64 * 130], 1, 64, spare=1)
+    q = queries(3, 2, 64, BF16, 5)
+    idx, cnt = torch.full((3, 1, keep), -9, dtype=torch.int32, device="cuda"), torch.full((3, 1), -9, dtype=torch.int32, device="cuda")
+    pc.cache_select(bt.desc(2), bt.cache, q, bt.gpu_table(), ints(bt.lens), ints([0, 1, 2, 3]), keep, first, idx, cnt)
+    want = ref.select(bt.pool(), q.double().cpu().numpy(), bt.table, bt.lens, [0, 1, 2, 3], keep, first)
+    assert np.array_equal(idx.cpu().numpy(), want[0]) and np.array_equal(cnt.cpu().numpy(), want[1])
 
 
 def test_select_all_equal():
