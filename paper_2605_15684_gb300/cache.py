@@ -473,7 +473,8 @@ class PageTable:
 @dataclass
 class CacheStep:
     """The new tokens of some sequences, as the calls of every layer take them: table [B, width], held [B] tokens before
-    the step, lens [B] with it, cu [B + 1] rows; int32 on the device."""
+    the step, lens [B] with it, cu [B + 1] rows; int32 on the device. It names pages: good until one of its sequences is
+    freed, truncated or takes another step, or the pools are compacted."""
     table: torch.Tensor
     held: torch.Tensor
     lens: torch.Tensor

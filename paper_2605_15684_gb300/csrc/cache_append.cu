@@ -7,6 +7,12 @@
 // exponent range, and a change of scale rounds again only what falls below the smallest normal e4m3.
 // A page that becomes full gets its mean key, s * (sum of the 64 bytes' values) / 64: at most 64 * 448 in
 // steps of 2^-9 are 24 bits, so that sum is exact in any order.
+//
+// Bound by HBM where there is much to append: every value is read once, kept in shared memory between its maximum
+// and its rounding, and written as a byte. 16384 tokens of 8 prompts, 8 heads of 128: 101 MB, 24 us, of which 15 are
+// those bytes at the copy rate; the rest is the start (cu and lens, table, scale: three loads in a row) and the last of
+// some five units a CTA. (One unit at a time 45 us; the next one's inputs under way 33; consecutive units a CTA and whole
+// pages without checks 24.) One token of each of 32 sequences: 4.7 us, all latencies of that chain.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -311,7 +317,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 5 : 2) ssba_cache_a
     }
 }
 
-// Pages src[i] -> dst[i]; the kv_heads * 64 * D bytes of a page are contiguous in K and in V.
+// Pages src[i] -> dst[i]; the kv_heads * 64 * D bytes of a page are contiguous in K and in V. A CTA a page and head, all of
+// its loads under way at once. Bound by HBM: 2048 pages of 8 heads of 128 (554 MB both ways) take 90.5 us, 6.1 TB/s.
 constexpr int kCopyThreads = 256;
 
 __global__ void __launch_bounds__(kCopyThreads) ssba_cache_copy_kernel(const Pool pl, int D, const int32_t* src,

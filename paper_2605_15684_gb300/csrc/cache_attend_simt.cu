@@ -2,6 +2,11 @@
 //
 //   s = scale * k_scale * (q . byte values of k),  O = sum softmax(s) * v_scale * byte values of v
 // over the tokens that a row sees, in all pages of its sequence or in listed ones.
+//
+// fp32 queries serve to check a model, so the kernel is kept simple: products on the CUDA cores, a row at a time, K and V
+// from L2 where rows share them. Shares of a row's pages are joined by a second launch. Eight rows of three sequences of
+// up to 1500 tokens, 24 heads of 64: 12.5 us, of which 1.4 are the bytes: latencies of the page's chain (table, scale, K,
+// softmax, V) and the second launch. (Eight heads a CTA whatever the group's size: 30 us.)
 #include <algorithm>
 #include <cmath>
 
