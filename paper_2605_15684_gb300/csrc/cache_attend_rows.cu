@@ -24,10 +24,13 @@
 // began with, finds that one's part there and keeps its own in shared memory. (4 sequences of 4000 tokens, 1000 rows in
 // all, 8 K/V heads of 128: 84 us; 90 with every part written, 110 with parts laid out by row, whose 16 bytes a thread
 // fill half a sector.) Results are written 32 bytes a thread for that reason too: 82 us against 85.
-// What bounds it, at that size: a tile of 256 rows takes 2.2 us, of which the four products have the tensor cores
-// for 1.35 (the loop without softmax and conversion takes 1.6); of one row tile S to P takes 1.2 us (one warp a
-// scheduler, so latencies show). Some 24 tiles a CTA are 52 us; 10 us pass before the first S (dependent loads of table, scales
-// and Q, cold instructions), 7 in the join, the rest in changes of items (2.7 us each) and shares of unequal cost.
+// What bounds it, at that size: a tile of 256 rows takes 2.2 us, a chain of QK, softmax (1.2 us a row tile, one warp a
+// scheduler, so latencies show) and PV in two pipelines. The four products alone would take 1.1 at the full rate, shared
+// memory 1.3 (Q, K and V for the products 192 KB a tile, the conversion 128). Two S of 64 tokens a pipeline, so that softmax
+// never waits, were slower (89 us): products of 64 columns read Q twice as often. PV of a tile's first half while the
+// second is in the softmax changed nothing (84). Some 24 tiles a CTA are 52 us; 10 us pass before the first S (dependent
+// loads of table, scales and Q, cold instructions), 7 in the join, the rest in changes of items (2.7 us each) and
+// shares of unequal cost.
 #include <algorithm>
 #include <climits>
 #include <cmath>
