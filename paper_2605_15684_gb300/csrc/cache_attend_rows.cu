@@ -87,6 +87,7 @@ struct __align__(1024) Smem {
     uint64_t q_full[2], s_full[2], p_full[2], o_full[2], n_full[2], n_empty[2], x_full, x_empty, drain;
     long long w0, w1, total;
     int first_b, ctas;
+    Seq first_s;
     long long first_at;
     uint32_t tmem_base;
     Item item[kItemRing];  // te = 0: no more

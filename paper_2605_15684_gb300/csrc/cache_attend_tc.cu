@@ -82,6 +82,7 @@ struct __align__(1024) Smem {
     uint64_t s_full[2], p_full[2], o_full[2], q_full[2], q_empty[2], m_full[2], m_empty[2], drain;
     long long w0, w1, total;
     int first_b, ctas;
+    Seq first_s;
     long long first_at;
     uint32_t tmem_base;
     Rows rows[2];          // of the items that are shared with other CTAs
@@ -114,7 +115,7 @@ __device__ __forceinline__ bool soft_any(bool x)
     return r != 0;
 }
 
-// Joins the np parts of an item that begins in CTA c0, in order, and writes its rows: a softmax warp takes every
+// Joins the np parts of an item that begins in CTA c0, in order, and writes its rows: four warps an item, a warp takes every
 // fourth row, two at a time, a lane four channels, with eight parts' loads in flight.
 template <int R, int D>
 __device__ __noinline__ void join(const Params& p, const Rows rows, int c0, int np, int quad, int lane)
@@ -192,7 +193,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
                                                     ~static_cast<uintptr_t>(1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        sm.abort_flag = 0;
+        sm.abort_flag = sm.last[0] = sm.last[1] = 0;
         for (int i = 0; i < C::kSlots; ++i) {
             mbar_init(smem_u32(&sm.full[i]), 1);
             mbar_init(smem_u32(&sm.empty[i]), 1);
@@ -661,9 +662,6 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
                 sm.last_c0[tok] = c0;
                 sm.last[tok] = np;
             }
-            soft_sync();
-            for (int i = 0; i < 2; ++i)
-                if (sm.last[i]) join<R, D>(p, sm.rows[i], sm.last_c0[i], sm.last[i], quad, lane);
         }
         dead = *abortf != 0;
     }
@@ -677,6 +675,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
             wait_raw(smem_u32(&sm.drain), 0, p.budget_ns);
         }
         if (threadIdx.x == 0) atomicExch(p.pl.status, SSBA_ERR_TIMEOUT);
+    } else if (sm.last[warp / 4]) {
+        join<R, D>(p, sm.rows[warp / 4], sm.last_c0[warp / 4], sm.last[warp / 4], warp & 3, lane);
     }
     tc_fence_before();
     __syncthreads();

@@ -160,7 +160,7 @@ struct Walk {
             locate();
         } else {
             b = sm.first_b;
-            s = load_seq(p.bt, b, p.pl.status);
+            s = sm.first_s;
             const Blocks bl(s, p.tq);
             const long long one = max(bl.sum(), 1LL);
             long long at = sm.first_at;
@@ -273,8 +273,11 @@ __device__ void make_share(const Params& p, S& sm)
         }
         return sum;
     };
+    Seq seq{0, 0, 0};  // the thread's of the last scan
     auto tiles_of = [&](int b) {
-        return b < p.bt.B ? Blocks(load_seq(p.bt, b, p.pl.status), p.tq).sum() * heads : 0LL;
+        if (b >= p.bt.B) return 0LL;
+        seq = load_seq(p.bt, b, p.pl.status);
+        return Blocks(seq, p.tq).sum() * heads;
     };
     long long W = 0, mine = 0, front = 0;
     if (kList) {
@@ -311,6 +314,7 @@ __device__ void make_share(const Params& p, S& sm)
             const long long at = base + front;
             if (w0 >= at && w0 < at + mine) {
                 sm.first_b = b0 + tid;
+                sm.first_s = seq;
                 sm.first_at = w0 - at;
             }
             base += sum;
