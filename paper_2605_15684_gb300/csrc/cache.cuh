@@ -46,9 +46,9 @@ __device__ __forceinline__ T ld(const T* p)
 
 __device__ __forceinline__ void flag(int* status) { *status = SSBA_ERR_CHECK; }
 
-__device__ __forceinline__ Seq load_seq(const Batch& bt, int b, int* status)
+// A sequence from its entries in cu and lens, clamped.
+__device__ __forceinline__ Seq make_seq(const Batch& bt, int c0, int c1, int l, int* status)
 {
-    const int c0 = ld(bt.cu + b), c1 = ld(bt.cu + b + 1), l = ld(bt.lens + b);
     Seq s;
     s.row = min(max(c0, 0), bt.T);
     const int end = min(max(c1, s.row), bt.T);
@@ -56,6 +56,11 @@ __device__ __forceinline__ Seq load_seq(const Batch& bt, int b, int* status)
     s.len = min(max(l, 0), bt.width * kPage);
     if (s.row != c0 || end != c1 || s.len != l) flag(status);
     return s;
+}
+
+__device__ __forceinline__ Seq load_seq(const Batch& bt, int b, int* status)
+{
+    return make_seq(bt, ld(bt.cu + b), ld(bt.cu + b + 1), ld(bt.lens + b), status);
 }
 
 // Tokens that row t sees: those up to its own, the new tokens of a sequence being its last.
@@ -84,6 +89,21 @@ __device__ __forceinline__ int find_seq(const Batch& bt, int t, int lane)
         lo += k * step;
     }
     return lo;
+}
+
+// find_seq, and the sequence itself (of no tokens where there is none): where each has one row, all of it in one round trip.
+__device__ __forceinline__ int seq_of(const Batch& bt, const Pool& pl, int t, int lane, Seq& s)
+{
+    if (t < bt.B) {
+        const int c0 = ld(bt.cu + t), c1 = ld(bt.cu + t + 1), l = ld(bt.lens + t);
+        if (c0 <= t && t < c1) {
+            s = make_seq(bt, c0, c1, l, pl.status);
+            return t;
+        }
+    }
+    const int b = find_seq(bt, t, lane);
+    s = b >= 0 ? load_seq(bt, b, pl.status) : Seq{0, 0, 0};
+    return b;
 }
 
 // Page of label j of sequence b, or -1 (flagged) when the table holds none of the pool's.

@@ -41,11 +41,11 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
     ptx::grid_dep_launch();
     const int t = blockIdx.x, part = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int h = blockIdx.y / chunks, chunk = blockIdx.y % chunks;
-    const int b = find_seq(bt, t, lane);
+    Seq s;
+    const int b = seq_of(bt, pl, t, lane, s);
     if (b < 0) return;
     const int G = pl.heads / pl.kv_heads, g0 = chunk * H, ng = min(H, G - g0);
     const size_t head0 = (size_t)t * pl.heads + h * G + g0;
-    const Seq s = load_seq(bt, b, pl.status);
     const int L = visible(s, t, pl.status);
     const int P = (L + kPage - 1) / kPage;
     const size_t row = (size_t)t * pl.kv_heads + h;

@@ -180,8 +180,7 @@ struct Walk {
     }
     __device__ __forceinline__ void locate()  // (lists) the sequence of row t
     {
-        b = find_seq(p.bt, t, threadIdx.x & 31);
-        s = b >= 0 ? load_seq(p.bt, b, p.pl.status) : Seq{0, 0, 0};
+        b = seq_of(p.bt, p.pl, t, threadIdx.x & 31, s);
     }
     __device__ __forceinline__ void share()
     {

@@ -236,9 +236,9 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_select_kernel(const Pool 
     const int t = blockIdx.x / ranks, h = blockIdx.y;
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
-    const int b = find_seq(bt, t, lane);
+    Seq s;
+    const int b = seq_of(bt, pl, t, lane, s);
     if (b < 0) return;  // (the whole cluster)
-    const Seq s = load_seq(bt, b, pl.status);
     const size_t row = (size_t)t * pl.kv_heads + h;
     int32_t* out = idx + row * keep;
     const int L = visible(s, t, pl.status);
