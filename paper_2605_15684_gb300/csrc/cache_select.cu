@@ -8,10 +8,10 @@
 // are, ties going to the lower label and NaN lowest, until min(keep, P) are. The scores are fp32 sums.
 //
 // Bound by the means, which are read once, where sequences are long: 32 rows of up to 65000 tokens, 8 heads of 128
-// (84 MB): 24.9 us, 12.4 at the copy rate. What is left over: three dependent loads before the first mean, eight pages a warp
-// in flight, and about 6 us of histogram, ranks and lists of each row's first CTA, which nothing overlaps at the end.
-// (One CTA of 1024 threads a row 51 us, clusters 28, 128-thread CTAs of one wave 25.) One row each of four sequences
-// of up to 8000 tokens: 6.2 us, latencies.
+// (84 MB): 24.6 us, 12.4 at the copy rate. What is left over: 2 us of dependent loads before the first mean, rows of unequal
+// length (the median CTA has scored after 12 us, the last one after 18), and 3.5 us of histogram, ranks and lists in a row's
+// first CTA. (One CTA of 1024 threads a row 51 us, clusters 28, 128-thread CTAs of one wave 25.) One row each of
+// four sequences of up to 8000 tokens: 5.3 us, latencies.
 #include <algorithm>
 #include <cmath>
 
@@ -220,8 +220,8 @@ __device__ __forceinline__ uint32_t cluster_size()
 }
 
 // A cluster of 1 to 8 CTAs per row: each scores its share of the pages, into the first CTA's shared memory; that
-// one then selects.
-template <typename T, int D>
+// one then selects. kU: pages that eight lanes have in flight.
+template <typename T, int D, int kU>
 __global__ void __launch_bounds__(kThreads) ssba_cache_select_kernel(const Pool pl, const Batch bt, const T* q, int keep,
                                                                      int first, int32_t* idx, int32_t* cnt)
 {
@@ -257,8 +257,8 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_select_kernel(const Pool 
     asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     uint32_t score_at;  // of the first CTA's scores
     asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(score_at) : "r"(ptx::smem_u32(score)));
-    // eight lanes a page, each with every eighth chunk of four channels; eight pages of a warp in flight
-    constexpr int kC = D / 32, kU = 2;
+    // eight lanes a page, each with every eighth chunk of four channels; 4 kU pages of a warp in flight
+    constexpr int kC = D / 32;
     const int sub = lane & 7;
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     for (int s0 = rank * share; s0 < i_end; s0 += kSlice) {
@@ -323,19 +323,15 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_select_kernel(const Pool 
     }
 }
 
-template <typename T, int D>
-int select_as(const Pool& pl, const Batch& bt, const void* q, int keep, int first, int32_t* idx, int32_t* cnt,
-              cudaStream_t st)
+template <typename T, int D, int kU>
+cudaError_t select_with(const Pool& pl, const Batch& bt, const void* q, int keep, int first, int32_t* idx, int32_t* cnt,
+                        int ranks, cudaStream_t st)
 {
     const size_t smem = ((size_t)(pl.heads / pl.kv_heads) * D + bt.width + (bt.width + 31) / 32) * 4;
     static PerDeviceOnce once;
     once.run([&] {
-        cudaFuncSetAttribute(ssba_cache_select_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSelectSmem);
+        cudaFuncSetAttribute(ssba_cache_select_kernel<T, D, kU>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSelectSmem);
     });
-    // CTAs a row: as many as run at once (eight an SM), and no share of fewer than 32 pages
-    const long long rows = (long long)bt.T * pl.kv_heads;
-    int ranks = 1;
-    while (ranks < 8 && 2 * rows * ranks <= 8LL * device_sm_count() && bt.width > 64 * ranks) ranks *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(bt.T * ranks, pl.kv_heads, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
@@ -350,9 +346,24 @@ int select_as(const Pool& pl, const Batch& bt, const void* q, int keep, int firs
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, ssba_cache_select_kernel<T, D>, pl, bt, static_cast<const T*>(q), keep, first,
-                                       idx, cnt);
-    if (e == cudaSuccess) e = cudaGetLastError();
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, ssba_cache_select_kernel<T, D, kU>, pl, bt, static_cast<const T*>(q), keep,
+                                             first, idx, cnt);
+    return e == cudaSuccess ? cudaGetLastError() : e;
+}
+
+template <typename T, int D>
+int select_as(const Pool& pl, const Batch& bt, const void* q, int keep, int first, int32_t* idx, int32_t* cnt,
+              cudaStream_t st)
+{
+    // CTAs a row: as many as run at once (eight an SM), and no share of fewer than 32 pages
+    const long long rows = (long long)bt.T * pl.kv_heads;
+    int ranks = 1;
+    while (ranks < 8 && 2 * rows * ranks <= 8LL * device_sm_count() && bt.width > 64 * ranks) ranks *= 2;
+    // Twice the pages in flight takes registers for four or five CTAs an SM: where no more are to run. (8 heads of 128, up
+    // to 8000 tokens: 4 rows 6.3 us with two, 5.3 with four, 16 rows 6.6, 5.7; up to 65000: 8 rows 10.5, 9.1, 12 rows
+    // 14.3, 14.2, 16 rows, where more run, 16.2, 18.0, 32 rows 24.6, 25.9.)
+    const cudaError_t e = rows * ranks <= 5LL * device_sm_count() ? select_with<T, D, 4>(pl, bt, q, keep, first, idx, cnt, ranks, st)
+                                                                  : select_with<T, D, 2>(pl, bt, q, keep, first, idx, cnt, ranks, st);
     if (e == cudaSuccess) return SSBA_OK;
     set_error("ssba_cache_select: %s", cudaGetErrorString(e));
     return SSBA_ERR_CUDA;
