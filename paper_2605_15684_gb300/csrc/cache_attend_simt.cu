@@ -4,9 +4,9 @@
 // over the tokens that a row sees, in all pages of its sequence or in listed ones.
 //
 // fp32 queries serve to check a model, so the kernel is kept simple: products on the CUDA cores, a row at a time, K and V
-// from L2 where rows share them. Shares of a row's pages are joined by a second launch. Eight rows of three sequences of
-// up to 1500 tokens, 24 heads of 64: 12.5 us, of which 1.4 are the bytes: latencies of the page's chain (table, scale, K,
-// softmax, V) and the second launch. (Eight heads a CTA whatever the group's size: 30 us.)
+// from L2 where rows share them. Shares of a row's pages are joined by the last of their CTAs. Eight rows of three sequences
+// of up to 1500 tokens, 24 heads of 64: 11.6 us, of which 1.4 are the bytes: latencies of the page's chain (table, scale, K,
+// softmax, V) and of the join. (K 16 channels and V four tokens at a time 12.9 us, eight heads a CTA whatever the group's size 30.)
 #include <algorithm>
 #include <cmath>
 
@@ -31,9 +31,10 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 template <int D, int H>
 __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
     const Pool pl, const Batch bt, const float* q, const int32_t* idx, const int32_t* cnt, int keep, float scale_log2,
-    float* O, float* lse, float* ws, int parts, int chunks)
+    float* O, float* lse, float* ws, unsigned* tickets, int parts, int chunks)
 {
     constexpr int kC = D / 32;  // channels of a lane
+    constexpr int kV = 16;      // tokens whose V is under way at a time (32: no faster)
     __shared__ __align__(16) float qs[H][D];
     __shared__ __align__(16) float ps[kWarps][kPage][H];
     __shared__ float ms[kWarps][H], ls[kWarps][H];
@@ -85,24 +86,29 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
         const uint8_t* K = pl.K + unit * kPage * D;
         const uint8_t* V = pl.V + unit * kPage * D;
         float a[2][H] = {};
+        // 64 channels of the lane's two tokens under way at a time
 #pragma unroll 1
-        for (int c = 0; c < D; c += 16) {
-            uint4 kk[2];
-            kk[0] = ld(reinterpret_cast<const uint4*>(K + lane * D + c));
-            kk[1] = ld(reinterpret_cast<const uint4*>(K + (lane + 32) * D + c));
+        for (int c = 0; c < D; c += 64) {
+            uint4 kk[4][2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float f[2][4];
-                from_e4m3x4((&kk[0].x)[e], f[0]);
-                from_e4m3x4((&kk[1].x)[e], f[1]);
+            for (int x = 0; x < 4; ++x)
 #pragma unroll
-                for (int g = 0; g < H; ++g) {
-                    const float4 x = *reinterpret_cast<const float4*>(&qs[g][c + 4 * e]);
+                for (int u = 0; u < 2; ++u) kk[x][u] = ld(reinterpret_cast<const uint4*>(K + (lane + 32 * u) * D + c + 16 * x));
 #pragma unroll
-                    for (int u = 0; u < 2; ++u)
-                        a[u][g] = fmaf(x.w, f[u][3], fmaf(x.z, f[u][2], fmaf(x.y, f[u][1], fmaf(x.x, f[u][0], a[u][g]))));
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float f[2][4];
+                    from_e4m3x4((&kk[x][0].x)[e], f[0]);
+                    from_e4m3x4((&kk[x][1].x)[e], f[1]);
+#pragma unroll
+                    for (int g = 0; g < H; ++g) {
+                        const float4 q4 = *reinterpret_cast<const float4*>(&qs[g][c + 16 * x + 4 * e]);
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+                            a[u][g] = fmaf(q4.w, f[u][3], fmaf(q4.z, f[u][2], fmaf(q4.y, f[u][1], fmaf(q4.x, f[u][0], a[u][g]))));
+                    }
                 }
-            }
         }
         __syncwarp();
 #pragma unroll
@@ -122,21 +128,24 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
             ps[warp][lane + 32][g] = p1 * vs;
         }
         __syncwarp();
-#pragma unroll 4
-        for (int r = 0; r < nt; ++r) {
-            float f[4];
-            if (kC == 4) {
-                from_e4m3x4(ld(reinterpret_cast<const uint32_t*>(V + r * D) + lane), f);
-            } else {
-                const float2 y = from_e4m3x2(ld(reinterpret_cast<const uint16_t*>(V + r * D) + lane));
-                f[0] = y.x;
-                f[1] = y.y;
+#pragma unroll 1
+        for (int r0 = 0; r0 < nt; r0 += kV) {
+            uint32_t raw[kV];
+#pragma unroll
+            for (int r = 0; r < kV; ++r) {
+                const uint8_t* at = V + (r0 + r) * D + lane * kC;
+                raw[r] = r0 + r >= nt ? 0u : kC == 4 ? ld(reinterpret_cast<const uint32_t*>(at)) : ld(reinterpret_cast<const uint16_t*>(at));
             }
 #pragma unroll
-            for (int g = 0; g < H; ++g) {
-                const float x = ps[warp][r][g];
+            for (int r = 0; r < kV; ++r) {
+                float f[4];
+                from_e4m3x4(raw[r], f);
 #pragma unroll
-                for (int c = 0; c < kC; ++c) o[g][c] = fmaf(x, f[c], o[g][c]);
+                for (int g = 0; g < H; ++g) {
+                    const float x = ps[warp][r0 + r][g];
+#pragma unroll
+                    for (int c = 0; c < kC; ++c) o[g][c] = fmaf(x, f[c], o[g][c]);
+                }
             }
         }
     }
@@ -187,31 +196,35 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
         }
         __syncthreads();
     }
-}
-
-// Joins the shares of one head of one row, in order.
-template <int D>
-__global__ void __launch_bounds__(D) ssba_cache_join_kernel(const Pool pl, const Batch bt, const float* ws, float* O,
-                                                            float* lse, int parts, int chunks, int H)
-{
-    ptx::grid_dep_wait();
-    ptx::grid_dep_launch();
-    const int t = blockIdx.x, h = blockIdx.y / chunks, chunk = blockIdx.y % chunks, g = blockIdx.z, c = threadIdx.x;
-    const int G = pl.heads / pl.kv_heads, gg = chunk * H + g;
-    if (gg >= G || find_seq(bt, t, c & 31) < 0) return;
-    const float* w = ws + ((size_t)blockIdx.x * gridDim.y + blockIdx.y) * parts * H * (D + 2) + g * (D + 2);
-    const size_t step = (size_t)H * (D + 2);
-    float top = -INFINITY, l = 0.f, o = 0.f;
-    for (int i = 0; i < parts; ++i) top = fmaxf(top, w[i * step + D]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    for (int i = 0; i < parts; ++i) {
-        const float f = exp2f(w[i * step + D] - ref);
-        l += w[i * step + D + 1] * f;
-        o += w[i * step + c] * f;
+    if (parts == 1) return;
+    // the CTA that comes last joins the row's shares, in order
+    __shared__ bool last;
+    const unsigned item = blockIdx.x * gridDim.y + blockIdx.y;
+    if (tid == 0) {  // (everyone's stores lie before the last barrier)
+        unsigned seen;
+        asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(seen) : "l"(tickets + item) : "memory");
+        last = seen == (unsigned)(parts - 1);
+        if (last) tickets[item] = 0;
     }
-    const size_t head = (size_t)t * pl.heads + h * G + gg;
-    O[head * D + c] = l != 0.f ? o / l : 0.f;
-    if (c == 0) lse[head] = (ref + log2f(l)) * kLn2;
+    __syncthreads();
+    if (!last) return;
+    const size_t step = (size_t)H * (D + 2);
+    for (int i = tid; i < ng * D; i += kThreads) {
+        const int g = i / D, c = i % D;
+        const float* w = ws + (size_t)item * parts * step + g * (D + 2);
+        float top = -INFINITY, lt = 0.f, ot = 0.f;
+#pragma unroll 4
+        for (int k = 0; k < parts; ++k) top = fmaxf(top, __ldcg(w + k * step + D));
+        const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll 4
+        for (int k = 0; k < parts; ++k) {
+            const float f = exp2f(__ldcg(w + k * step + D) - ref);
+            lt += __ldcg(w + k * step + D + 1) * f;
+            ot += __ldcg(w + k * step + c) * f;
+        }
+        O[(head0 + g) * D + c] = lt != 0.f ? ot / lt : 0.f;
+        if (c == 0) lse[head0 + g] = (ref + log2f(lt)) * kLn2;
+    }
 }
 
 template <int D, int H>
@@ -225,11 +238,9 @@ int attend_as(const Pool& pl, const Batch& bt, float scale, const void* q, const
     // shares: as many as give the SMs work, none of fewer than a page a warp
     const int parts = (int)std::max<long long>(1, std::min<long long>(kMaxParts / std::max<long long>(items, 1), (pages + kWarps - 1) / kWarps));
     const dim3 grid(bt.T, pl.kv_heads * chunks, parts);
-    cudaError_t e = launch_dependent(ssba_cache_attend_simt_kernel<D, H>, grid, kThreads, 0, st, pl, bt, static_cast<const float*>(q),
-                                     idx, cnt, keep, scale * kLog2e, static_cast<float*>(O), lse, parts_at, parts, chunks);
-    if (e == cudaSuccess && parts > 1)
-        e = launch_dependent(ssba_cache_join_kernel<D>, dim3(bt.T, pl.kv_heads * chunks, H), D, 0, st, pl, bt, parts_at,
-                             static_cast<float*>(O), lse, parts, chunks, H);
+    const cudaError_t e = launch_dependent(ssba_cache_attend_simt_kernel<D, H>, grid, kThreads, 0, st, pl, bt, static_cast<const float*>(q),
+                                     idx, cnt, keep, scale * kLog2e, static_cast<float*>(O), lse, parts_at,
+                                     static_cast<unsigned*>(ws), parts, chunks);
     if (e == cudaSuccess) return SSBA_OK;
     set_error("ssba_cache_attend: %s", cudaGetErrorString(e));
     return SSBA_ERR_CUDA;

@@ -267,6 +267,17 @@ def test_select_many_first_pages(keep, first):
     assert np.array_equal(idx.cpu().numpy(), want[0]) and np.array_equal(cnt.cpu().numpy(), want[1])
 
 
+@pytest.mark.parametrize("d,dtype", [(64, BF16), (128, FP32)])
+def test_select_many_rows(d, dtype):
+    """More rows than run at once."""
+    lens = [(97 * b) % 700 + 1 for b in range(110)]
+    bt = Batch(lens, 8, d, seed=8)
+    q = queries(110, 16, d, dtype, 6)
+    idx, cnt = pc.cache_select(bt.desc(16, dtype), bt.cache, q, bt.gpu_table(), ints(lens), ints(list(range(111))), 5, 1)
+    want = ref.select(bt.pool(), q.double().cpu().numpy(), bt.table, lens, list(range(111)), 5, 1)
+    assert np.array_equal(idx.cpu().numpy(), want[0]) and np.array_equal(cnt.cpu().numpy(), want[1])
+
+
 def test_select_all_equal():
     bt = Batch([64 * 40], 1, 128)
     bt.cache.k_mean.fill_(0.5)
