@@ -28,9 +28,9 @@
 // last joins them in order, so that the result does not depend on which it was.
 //
 // Bound by HBM where sequences are long: 64 of up to 16000 tokens, 8 K/V heads of 128 for 64 query heads (1.33 GB):
-// 210 us, 0.93 of the copy rate (a first version on the CUDA cores took 996). Some 13 us
+// 210 us, 0.93 of the copy rate (a first version on the CUDA cores took 996). Some 10 us
 // do not depend on the size: shares, table, scales and first tiles at the start, the last tile's chain and the join at
-// the end; they are most of 16 sequences of up to 8000 tokens (37 us, 24 at the copy rate) and nearly all of one
+// the end; they are what 16 sequences of up to 8000 tokens (35.7 us) take beyond the 24 at the copy rate, and nearly all of one
 // of 700 tokens (9.1 us). The tensor pipe is busy for 3 % of the time: N = 2R columns of 128 rows.
 #include <algorithm>
 #include <climits>
