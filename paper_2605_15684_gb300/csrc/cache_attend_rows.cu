@@ -486,7 +486,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                         const bool v = x > 0;
                         const uint32_t rs = use % kRaw, cs = use % kCv;
                         wait_phase(rfull0 + 8 * rs, (use / kRaw) & 1, abort_at, p.budget_ns);
-                        const int first = (two || x != 1 || head ? pos : last_pos) + (w & 1) * 32;  // token of the half page's first row
+                        const int first = (two || x != 1 || head ? pos : last_pos) + (w & 1) * 32;  // token of the first row
                         if (v && first + 31 >= lo_lim) {
                             // tokens that no row sees: their V is whatever the page holds, and 0 * NaN would reach
                             // every row; tokens that some rows see: a NaN is taken out and kept for those rows
@@ -517,8 +517,10 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
 #pragma unroll
                         for (int k = 0; k < kIts; ++k) {
                             const int row = row0 + k * kRows;
-                            uint32_t y[8] = {half2_of(in[k].x & 0xffff), half2_of(in[k].x >> 16), half2_of(in[k].y & 0xffff), half2_of(in[k].y >> 16),
-                                             half2_of(in[k].z & 0xffff), half2_of(in[k].z >> 16), half2_of(in[k].w & 0xffff), half2_of(in[k].w >> 16)};
+                            const uint32_t x4[4] = {in[k].x, in[k].y, in[k].z, in[k].w};
+                            uint32_t y[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) y[e] = half2_of(e & 1 ? x4[e / 2] >> 16 : x4[e / 2] & 0xffff);
                             const uint4 a = make_uint4(y[0], y[1], y[2], y[3]), b = make_uint4(y[4], y[5], y[6], y[7]);
                             uint8_t* to = &sm.cv[cs][c / 4][row][0];
                             const int q = (c % 4) * 2;
@@ -613,7 +615,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                     const uint32_t v[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
                     uint32_t y[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {  // (an infinity times 0 is NaN: it makes its row's scores NaN, as it would a softmax's)
+                    for (int e = 0; e < 4; ++e) {  // (an infinity times 0 is NaN: it makes its row's scores NaN, as in any softmax)
                         const float a = __uint_as_float(v[e] << 16), b = __uint_as_float(v[e] & 0xffff0000u);
                         y[e] = pack_half(fmaf(a, 0.f, a * inv), fmaf(b, 0.f, b * inv));
                     }
@@ -816,16 +818,15 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                         for (int e = 0; e < 32; e += 16) {
                             uint32_t y[8];
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                const __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
-                                y[k] = *reinterpret_cast<const uint32_t*>(&b);
-                            }
+                            for (int k = 0; k < 8; ++k)
+                                y[k] = pack_bf16(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
                             store32(p.O + at * D + c + e, y);
                         }
                     } else if (!whole) {
 #pragma unroll
                         for (int e = 0; e < 32; e += 4)
-                            *reinterpret_cast<uint4*>(&part->o[(c + e) / 4][u * kRowTile + r]) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                            *reinterpret_cast<uint4*>(&part->o[(c + e) / 4][u * kRowTile + r]) =
+                                make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                     }
                 }
                 if (whole && row0 >= 0) p.lse[at] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
@@ -891,7 +892,8 @@ int launch(const Maps& maps, const Params& p, cudaStream_t st)
     once.run([smem] {
         cudaFuncSetAttribute(ssba_cache_attend_rows_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     });
-    const cudaError_t e = launch_dependent(ssba_cache_attend_rows_kernel<D>, dim3(std::min(device_sm_count(), kMaxGrid)), kThreads, smem, st, maps, p);
+    const cudaError_t e = launch_dependent(ssba_cache_attend_rows_kernel<D>, dim3(std::min(device_sm_count(), kMaxGrid)),
+                                           kThreads, smem, st, maps, p);
     if (e == cudaSuccess) return SSBA_OK;
     set_error("ssba_cache_attend: %s", cudaGetErrorString(e));
     return SSBA_ERR_CUDA;

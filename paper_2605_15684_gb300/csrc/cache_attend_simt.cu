@@ -134,7 +134,8 @@ __global__ void __launch_bounds__(kThreads) ssba_cache_attend_simt_kernel(
 #pragma unroll
             for (int r = 0; r < kV; ++r) {
                 const uint8_t* at = V + (r0 + r) * D + lane * kC;
-                raw[r] = r0 + r >= nt ? 0u : kC == 4 ? ld(reinterpret_cast<const uint32_t*>(at)) : ld(reinterpret_cast<const uint16_t*>(at));
+                if (r0 + r >= nt) raw[r] = 0;
+                else raw[r] = kC == 4 ? ld(reinterpret_cast<const uint32_t*>(at)) : ld(reinterpret_cast<const uint16_t*>(at));
             }
 #pragma unroll
             for (int r = 0; r < kV; ++r) {
@@ -236,11 +237,12 @@ int attend_as(const Pool& pl, const Batch& bt, float scale, const void* q, const
     const long long items = (long long)bt.T * pl.kv_heads * chunks;
     const int pages = idx ? keep : bt.width;
     // shares: as many as give the SMs work, none of fewer than a page a warp
-    const int parts = (int)std::max<long long>(1, std::min<long long>(kMaxParts / std::max<long long>(items, 1), (pages + kWarps - 1) / kWarps));
+    const long long most = std::min<long long>(kMaxParts / std::max<long long>(items, 1), (pages + kWarps - 1) / kWarps);
+    const int parts = (int)std::max<long long>(1, most);
     const dim3 grid(bt.T, pl.kv_heads * chunks, parts);
-    const cudaError_t e = launch_dependent(ssba_cache_attend_simt_kernel<D, H>, grid, kThreads, 0, st, pl, bt, static_cast<const float*>(q),
-                                     idx, cnt, keep, scale * kLog2e, static_cast<float*>(O), lse, parts_at,
-                                     static_cast<unsigned*>(ws), parts, chunks);
+    const cudaError_t e = launch_dependent(ssba_cache_attend_simt_kernel<D, H>, grid, kThreads, 0, st, pl, bt,
+                                           static_cast<const float*>(q), idx, cnt, keep, scale * kLog2e, static_cast<float*>(O),
+                                           lse, parts_at, static_cast<unsigned*>(ws), parts, chunks);
     if (e == cudaSuccess) return SSBA_OK;
     set_error("ssba_cache_attend: %s", cudaGetErrorString(e));
     return SSBA_ERR_CUDA;

@@ -611,7 +611,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<R, D>::kCtas) ssba_cache_attend_
                 int head;
                 const int row = it.row_of(lane, head);
                 const long long at = row >= 0 ? (long long)row * p.pl.heads + head : -1;
-                sm.row[quad][0][lane] = make_float4(sum != 0.f ? 1.f / sum : 0.f, 0.f, __int_as_float((int)at), __int_as_float((int)(at >> 32)));
+                sm.row[quad][0][lane] =
+                    make_float4(sum != 0.f ? 1.f / sum : 0.f, 0.f, __int_as_float((int)at), __int_as_float((int)(at >> 32)));
                 if (quad == 0) {
                     if (!whole) reinterpret_cast<float2*>(part + R * D)[lane] = make_float2(ref, sum);
                     else if (row >= 0) p.lse[at] = sum != 0.f ? (ref + log2f(sum)) * kLn2 : -INFINITY;
@@ -694,7 +695,8 @@ int launch(const Maps& maps, const Params& p, cudaStream_t st)
     once.run([smem] {
         cudaFuncSetAttribute(ssba_cache_attend_tc_kernel<R, D, kList>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     });
-    const cudaError_t e = launch_dependent(ssba_cache_attend_tc_kernel<R, D, kList>, dim3(std::min(device_sm_count() * C::kCtas, kMaxGrid)), kThreads, smem, st, maps, p);
+    const cudaError_t e = launch_dependent(ssba_cache_attend_tc_kernel<R, D, kList>,
+                                           dim3(std::min(device_sm_count() * C::kCtas, kMaxGrid)), kThreads, smem, st, maps, p);
     if (e == cudaSuccess) return SSBA_OK;
     set_error("ssba_cache_attend: %s", cudaGetErrorString(e));
     return SSBA_ERR_CUDA;

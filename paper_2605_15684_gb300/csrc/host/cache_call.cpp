@@ -141,7 +141,8 @@ PyObject* select(PyObject*, PyObject* const* a, Py_ssize_t n)
         const at::Tensor* q = rows(a[1], *c, c->desc.heads);
         if (elsewhere(*c) || !q || !batch(a + 2, *c, b) || first < 0 || keep <= first || keep > SSBA_CACHE_MAX_WIDTH)
             return none();
-        at::Tensor idx = make(*c, {q->size(0), c->desc.kv_heads, keep}, at::kInt), cnt = make(*c, {q->size(0), c->desc.kv_heads}, at::kInt);
+        at::Tensor idx = make(*c, {q->size(0), c->desc.kv_heads, keep}, at::kInt);
+        at::Tensor cnt = make(*c, {q->size(0), c->desc.kv_heads}, at::kInt);
         const int rc = c->select(&c->desc, &c->pool, q->const_data_ptr(), (int32_t)q->size(0), b.table, b.width, b.lens, b.cu,
                                  b.B, (int32_t)keep, (int32_t)first, idx.mutable_data_ptr<int32_t>(),
                                  cnt.mutable_data_ptr<int32_t>(), stream(*c));
