@@ -3,18 +3,21 @@
 //
 // An item is up to 256 rows (tokens times the group's heads) of one sequence and K/V head, in two tiles of 128
 // rows; it visits its sequence's tiles of 128 tokens (two pages):
-//   S_u = Q_u K^T   tcgen05.mma kind::f16, M = 128, N = 128, K = D   (fp16, K-major)
-//   O_u += P_u V    M = 128, N = D, K = 128                          (fp16, P from tensor memory, V MN-major)
-// An e4m3 value is an fp16 value, so K and V are converted without rounding, once for both row tiles, and their
-// page's scale stays out of the products: K's multiplies the scores, V's is added to their exponent,
+//   S_u = Q_u K^T   tcgen05.mma kind::f8f6f4, M = 128, N = 128, K = D, twice (K's bytes as they are)
+//   O_u += P_u V    tcgen05.mma kind::f16, M = 128, N = D, K = 128 (fp16, P from tensor memory, V MN-major)
+// Q is the sum of two e4m3 numbers, whose products go into one sum: a row is brought below 448 by a power of two, and
+// x = hi + lo with hi = e4m3(x), lo = e4m3(x - hi): exact for bf16 values down to 2^-10 of the row's largest, below that off
+// by 2^-19 of it at most, where a bf16 value's own rounding is 2^-9 of the value.
+// An e4m3 value is an fp16 value, so V is converted without rounding, once for both row tiles, and the
+// pages' scales stay out of the products: K's multiplies the scores, V's is added to their exponent,
 //   P = 2^(s + log2 v_scale - m),   l = sum P / v_scale,   O = sum P (bytes of V) / l,
-// v_scale relative to the sequence's first page (within 2^+-100 of it). Rows of Q are brought below 448 by a
-// power of two; their 8 bits of significand are exact in fp16 down to 2^-25 of the row's largest. P is rounded to fp16's
+// v_scale relative to the sequence's first page (within 2^+-100 of it). P is rounded to fp16's
 // 11 bits; m begins 8 below the largest exponent, so P's smallest step is 2^-32 of the largest weight.
 //
-// One CTA an SM, 16 warps: a producer (TMA of the pages' bytes), an issuer, four converters (half a page each: bytes to
+// One CTA an SM, 16 warps: a producer (TMA of the pages' bytes), an issuer, four converters (half a page of V each: bytes to
 // fp16 in the swizzled layout of the products), one that walks the items for the softmax, one that counts off a part
-// while the next items run, and a softmax warpgroup for each row tile (a thread is a row).
+// while the next items run, and a softmax warpgroup for each row tile (a thread is a row). An item of up to 128
+// rows has one row tile: both pipelines take its rows, and its tiles in turn.
 // P overwrites the lower half of its S, so of one row tile PV_g comes before QK_{g + 1}; while one row tile
 // is with the tensor cores the other is with its softmax. A tile's maximum is taken first, but the row's reference is
 // raised (and O rescaled in tensor memory) only where P would pass 2^14. The softmax's code is loops over 32 scores: it
@@ -25,12 +28,12 @@
 // all, 8 K/V heads of 128: 84 us; 90 with every part written, 110 with parts laid out by row, whose 16 bytes a thread
 // fill half a sector.) Results are written 32 bytes a thread for that reason too: 82 us against 85.
 // What bounds it, at that size: a tile of 256 rows takes 2.2 us, a chain of QK, softmax (1.2 us a row tile, one warp a
-// scheduler, so latencies show) and PV in two pipelines. The four products alone would take 1.1 at the full rate, shared
-// memory 1.3 (Q, K and V for the products 192 KB a tile, the conversion 128). Two S of 64 tokens a pipeline, so that softmax
-// never waits, were slower (89 us): products of 64 columns read Q twice as often. PV of a tile's first half while the
-// second is in the softmax changed nothing (84). Some 24 tiles a CTA are 52 us; 10 us pass before the first S (dependent
-// loads of table, scales and Q, cold instructions), 7 in the join, the rest in changes of items (2.7 us each) and
-// shares of unequal cost.
+// scheduler, so latencies show) and PV in two pipelines; the four products alone would take 1.1 at the full rate. Two S of
+// 64 tokens a pipeline, so that softmax never waits, were slower (89 us): products of 64 columns read Q twice as often.
+// PV of a tile's first half while the second is in the softmax changed nothing (84). Some 24 tiles a CTA are 52 us; 10 us
+// pass before the first S (dependent loads of table, scales and Q, cold instructions), 7 in the join, the rest in
+// changes of items (2.7 us each) and shares of unequal cost. 64 rows of 16 sequences of up to 8000 tokens, one row tile
+// each: 85 us (92 with K converted to fp16 as V is, 89 with unrolled products in the issuer).
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -46,7 +49,7 @@ namespace {
 constexpr int kThreads = 512;
 constexpr int kRowTile = 128;
 constexpr int kItemRows = 2 * kRowTile;
-constexpr int kCv = 3, kRaw = 3, kMetas = 8;
+constexpr int kK = 3, kCv = 2, kRaw = 2, kMetas = 8;  // tiles of K; of V, converted and as bytes
 constexpr float kTop = 8.f;         // log2 of the largest P against a new reference
 constexpr float kMost = 14.f;       // log2 of the largest P that is let stand (fp16 ends at 65504)
 constexpr int kConverters = 4;
@@ -73,9 +76,10 @@ struct Meta {
 
 template <int D>
 struct __align__(1024) Smem {
-    uint8_t q[2][D / 64][kRowTile][128];   // fp16, 64 channels a 128-byte row, 128-byte swizzle
-    uint8_t cv[kCv][D / 64][kTile][128];
-    uint8_t raw[kRaw][kTile * D];
+    uint8_t q[2][2][kRowTile][D];          // e4m3: a row tile's high and low parts, swizzled as K is
+    uint8_t cv[kCv][D / 64][kTile][128];   // fp16 V, 64 channels a 128-byte row, 128-byte swizzle
+    uint8_t kraw[kK][kTile * D];           // K's bytes (rows of 128 or 64 bytes, that swizzle)
+    uint8_t raw[kRaw][kTile * D];          // V's bytes
     // by item parity and converter: first token whose V is NaN, of those that not every row sees
     int nan_at[2][kConverters][D];
     int nan_any[2][kConverters];
@@ -83,7 +87,7 @@ struct __align__(1024) Smem {
     float2 ml[kRowTile];    // (tiles in turn) reference and sum of the second pipeline's rows
     float first_lv[2];      // by item parity: log2 of the V scale that the item's are relative to
     Meta meta[kMetas][2];
-    uint64_t raw_full[kRaw], raw_empty[kRaw], cv_full[kCv], cv_empty[kCv], m_full[kMetas];
+    uint64_t k_full[kK], k_empty[kK], raw_full[kRaw], raw_empty[kRaw], cv_full[kCv], cv_empty[kCv], m_full[kMetas];
     uint64_t q_full[2], s_full[2], p_full[2], o_full[2], n_full[2], n_empty[2], x_full, x_empty, drain;
     long long w0, w1, total;
     int first_b, ctas;
@@ -247,6 +251,10 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
             mbar_init(smem_u32(&sm.i_full[i]), 1);
             mbar_init(smem_u32(&sm.i_empty[i]), 8);
         }
+        for (int i = 0; i < kK; ++i) {
+            mbar_init(smem_u32(&sm.k_full[i]), 1);
+            mbar_init(smem_u32(&sm.k_empty[i]), 1);
+        }
         for (int i = 0; i < kRaw; ++i) {
             mbar_init(smem_u32(&sm.raw_full[i]), 1);
             mbar_init(smem_u32(&sm.raw_empty[i]), kConverters);
@@ -291,32 +299,41 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
     const uint32_t rfull0 = smem_u32(&sm.raw_full[0]), rempty0 = smem_u32(&sm.raw_empty[0]);
     const uint32_t cfull0 = smem_u32(&sm.cv_full[0]), cempty0 = smem_u32(&sm.cv_empty[0]);
     bool dead = false;
-    uint32_t loads = 0;  // of the producer
+    const uint32_t kfull0 = smem_u32(&sm.k_full[0]), kempty0 = smem_u32(&sm.k_empty[0]);
+    constexpr uint32_t kSwizzle = D == 128 ? 2 : 4;  // of Q's and K's rows (see sdesc)
+    uint32_t kloads = 0, vloads = 0;  // of the producer
     // an item of up to 128 rows has no second row tile: both pipelines take its rows, and its tiles in turn
     auto both = [&](const Walk<false>& w) { return w.rows().n * p.gc > kRowTile; };
 
     if (warp == kLoad) {
         // ------------------------------------------------------------ producer
         Walk<false> it(p, sm);
-        auto copy = [&](const CUtensorMap* map, int p0, int p1) {
-            const uint32_t slot = loads % kRaw;
-            if (!mbar_wait(rempty0 + 8 * slot, ((loads / kRaw) & 1) ^ 1, abortf, p.budget_ns)) {
+        auto copy = [&](const CUtensorMap* map, uint32_t empty, uint32_t full, uint32_t to, uint32_t turn, int p0, int p1) {
+            if (!mbar_wait(empty, (turn & 1) ^ 1, abortf, p.budget_ns)) {
                 dead = true;
                 return;
             }
-            const uint32_t bar = rfull0 + 8 * slot, to = smem_u32(&sm.raw[slot][0]);
-            mbar_arrive_expect_tx(bar, ((p0 >= 0) + (p1 >= 0)) * (uint32_t)(kPage * D));
+            mbar_arrive_expect_tx(full, ((p0 >= 0) + (p1 >= 0)) * (uint32_t)(kPage * D));
             if (p.withhold && blockIdx.x == 0) {
                 dead = true;
                 return;
             }
-            if (p0 >= 0) tma_load_3d(to, map, bar, 0, 0, p0);
-            if (p1 >= 0) tma_load_3d(to + kPage * D, map, bar, 0, 0, p1);
-            ++loads;
+            if (p0 >= 0) tma_load_3d(to, map, full, 0, 0, p0);
+            if (p1 >= 0) tma_load_3d(to + kPage * D, map, full, 0, 0, p1);
         };
+        auto copy_k = [&](int p0, int p1) {
+            const uint32_t x = kloads % kK;
+            copy(&maps.k, kempty0 + 8 * x, kfull0 + 8 * x, smem_u32(&sm.kraw[x][0]), kloads / kK, p0, p1);
+            if (!dead) ++kloads;
+        };
+        auto copy_v = [&](int p0, int p1) {
+            const uint32_t x = vloads % kRaw;
+            copy(&maps.v, rempty0 + 8 * x, rfull0 + 8 * x, smem_u32(&sm.raw[x][0]), vloads / kRaw, p0, p1);
+            if (!dead) ++vloads;
+        };
+        // K_0, then K_{i + 1} and V_i
         for (; it.more() && !dead; it.next()) {
             const int h = it.hv / p.chunks;
-            const bool two = both(it);
             int v0 = -1, v1 = -1;  // the last tile's pages
             for (int c0 = 2 * it.tb; c0 < 2 * it.te && !dead; c0 += 32) {  // 32 pages at a time
                 int j, page = -1;
@@ -326,17 +343,16 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 for (int i = 0; i < n && !dead; ++i) {
                     const int p0 = __shfl_sync(0xffffffffu, unit, 2 * i), p1 = __shfl_sync(0xffffffffu, unit, 2 * i + 1);
                     if (lane == 0) {
-                        copy(&maps.k, p0, p1);
-                        if (two && !dead) copy(&maps.v, p0, p1);
-                        if (!two && !dead && c0 / 2 + i > it.tb) copy(&maps.v, v0, v1);
+                        copy_k(p0, p1);
+                        if (!dead && c0 / 2 + i > it.tb) copy_v(v0, v1);
                     }
                     v0 = p0;
                     v1 = p1;
                     dead = __shfl_sync(0xffffffffu, (int)dead, 0) != 0;
                 }
             }
-            if (!two && !dead) {
-                if (lane == 0) copy(&maps.v, v0, v1);
+            if (!dead) {
+                if (lane == 0) copy_v(v0, v1);
                 dead = __shfl_sync(0xffffffffu, (int)dead, 0) != 0;
             }
         }
@@ -344,62 +360,62 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
     } else if (warp == kIssue) {
         // ------------------------------------------------------------ issuer
         Walk<false> it(p, sm);
-        uint32_t cnt[2] = {0, 0}, q0 = 0, q1 = 0, base = 0;  // tiles and items of each pipeline; ring slots used before the item
-        auto slot_full = [&](uint32_t x) { wait_phase(cfull0 + 8 * (x % kCv), (x / kCv) & 1, abort_at, p.budget_ns); };
-        auto qk = [&](int u, uint32_t slot, bool release) {
-            slot_full(slot);
-            tc_fence_after();
-            if (elect_one_sync()) {
-                const uint64_t a = sdesc_sw128(smem_u32(&sm.q[u][0][0][0]), 16, 1024);
-                const uint64_t b = sdesc_sw128(smem_u32(&sm.cv[slot % kCv][0][0][0]), 16, 1024);
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint64_t at = (uint64_t)((k / 4) * (kTile * 128 / 16) + (k % 4) * 2);
-                    mma_ss(tbase + u * 128, a + at, b + at, idesc_f16_f32(128, 128, false), k > 0 ? 1u : 0u);
-                }
-                mma_commit(smem_u32(&sm.s_full[u]));
-                if (release) mma_commit(cempty0 + 8 * (slot % kCv));
-            }
-            __syncwarp();
-            ++cnt[u];
-        };
-        auto pv = [&](int u, uint32_t slot, bool first, bool last, bool release) {
-            wait_phase(smem_u32(&sm.p_full[u]), (cnt[u] - 1) & 1, abort_at, p.budget_ns);
-            slot_full(slot);
-            tc_fence_after();
-            if (elect_one_sync()) {
-                const uint64_t b = sdesc_sw128(smem_u32(&sm.cv[slot % kCv][0][0][0]), kTile * 128, 1024);
-#pragma unroll
-                for (int k = 0; k < kTile / 16; ++k)
-                    mma_ts(tbase + 256 + u * D, tbase + u * 128 + k * 8, b + (uint64_t)(k * 128), idesc_f16_f32(128, D, true),
-                           (!first || k > 0) ? 1u : 0u);
-                if (last) mma_commit(smem_u32(&sm.o_full[u]));
-                if (release) mma_commit(cempty0 + 8 * (slot % kCv));
-            }
-            __syncwarp();
-        };
+        // One loop, one copy of each product's code and no unrolling, so that it stays in the instruction cache beside the other
+        // roles' (with a copy for each way through it, a jump back waited 0.5 us for its code).
+        uint32_t done0 = 0, done1 = 0, q0 = 0, q1 = 0, base = 0;  // QKs and items of each pipeline; tiles before the item
         for (; it.more(); it.next()) {
             const int n = it.te - it.tb;
             const bool two = both(it);
-            // steps i = 0 .. n; a pipeline's PV of a tile before its next QK. One loop, one copy of the products' code.
+            wait_phase(smem_u32(&sm.q_full[0]), q0++ & 1, abort_at, p.budget_ns);
+            if (two || n > 1) wait_phase(smem_u32(&sm.q_full[1]), q1++ & 1, abort_at, p.budget_ns);
+            // A step is PV of a tile and QK of a later one in one pipeline, which take the steps in turn. Two row tiles: PV_{i-1} and
+            // QK_i in both; tiles in turn: PV_{i-2} and QK_i.
+            const int steps = two ? 2 * (n + 1) : n + 2;
 #pragma unroll 1
-            for (int i = 0; i <= n; ++i) {
-                if (i == 0) {
-                    wait_phase(smem_u32(&sm.q_full[0]), q0++ & 1, abort_at, p.budget_ns);
-                    if (two || n > 1) wait_phase(smem_u32(&sm.q_full[1]), q1++ & 1, abort_at, p.budget_ns);
-                }
+            for (int s = 0; s < steps; ++s) {
+                const int u = s & 1, i = two ? s >> 1 : s, t = two ? i - 1 : i - 2;
+                const bool release = !two || u == 1;  // (the last to read the tile)
+                if (t >= 0) {
+                    const uint32_t tile = base + t, slot = tile % kCv;
+                    wait_phase(smem_u32(&sm.p_full[u]), ((u ? done1 : done0) - 1) & 1, abort_at, p.budget_ns);
+                    wait_phase(cfull0 + 8 * slot, (tile / kCv) & 1, abort_at, p.budget_ns);
+                    tc_fence_after();
+                    if (elect_one_sync()) {
+                        uint64_t b = sdesc_sw128(smem_u32(&sm.cv[slot][0][0][0]), kTile * 128, 1024);
+                        uint32_t more = two ? t > 0 : t > 1;
 #pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
-                    if (two) {  // K_0 V_0 K_1 V_1 ...; both row tiles at every step
-                        if (i > 0) pv(h, base + 2 * i - 1, i == 1, i == n, h == 1);
-                        if (i < n) qk(h, base + 2 * i, h == 1);
-                    } else {  // K_0 K_1 V_0 K_2 V_1 ... V_{n - 1}; tiles in turn
-                        if (h == 0 && i < n) qk(i & 1, base + max(2 * i - 1, 0), true);
-                        if (h == 1 && i > 0) pv((i - 1) & 1, base + (i < n ? 2 * i : 2 * n - 1), i <= 2, i >= n - 1, true);
+                        for (int k = 0; k < kTile / 16; ++k) {
+                            mma_ts(tbase + 256 + u * D, tbase + u * 128 + k * 8, b, idesc_f16_f32(128, D, true), more);
+                            b += 128;
+                            more = 1;
+                        }
+                        if (t >= (two ? n - 1 : n - 2)) mma_commit(smem_u32(&sm.o_full[u]));
+                        if (release) mma_commit(cempty0 + 8 * slot);
                     }
+                    __syncwarp();
+                }
+                if (i < n) {
+                    const uint32_t tile = base + i, slot = tile % kK;
+                    wait_phase(kfull0 + 8 * slot, (tile / kK) & 1, abort_at, p.budget_ns);
+                    tc_fence_after();
+                    if (elect_one_sync()) {
+                        uint64_t a = sdesc(smem_u32(&sm.q[u][0][0][0]), 16, 8 * D, kSwizzle);
+                        const uint64_t b = sdesc(smem_u32(&sm.kraw[slot][0]), 16, 8 * D, kSwizzle);
+#pragma unroll 1
+                        for (int k = 0; k < 2 * (D / 32); ++k) {  // the high parts, then the low ones
+                            mma_f8_ss(tbase + u * 128, a, b + (uint64_t)(2 * (k & (D / 32 - 1))), idesc_e4m3_f32(128, 128, false, false),
+                                      k > 0 ? 1u : 0u);
+                            a += k == D / 32 - 1 ? kRowTile * D / 16 - 2 * (D / 32 - 1) : 2;
+                        }
+                        mma_commit(smem_u32(&sm.s_full[u]));
+                        if (release) mma_commit(kempty0 + 8 * slot);
+                    }
+                    __syncwarp();
+                    done0 += u == 0;
+                    done1 += u;
                 }
             }
-            base += 2 * n;
+            base += n;
         }
         dead = *abortf != 0;
     } else if (warp >= kItems && warp < kSoftmax) {
@@ -435,17 +451,15 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
         }
         dead = *abortf != 0;
     } else if (warp < kSoftmax) {
-        // ------------------------------------------------------------ converters: half a page of every tile
+        // ------------------------------------------------------------ converters: half a page of every tile of V
         constexpr int kLanes = D / 16, kRows = 32 / kLanes, kIts = 32 / kRows;  // lanes of a row (16 bytes each), rows at a time
         const int w = warp - kConvert, c = lane % kLanes, row0 = w * 32 + lane / kLanes;
-        uint32_t use = 0, g = 0;
+        uint32_t g = 0;  // tiles
         int seg = 0;
         Walk<false> it(p, sm);
         for (; it.more(); it.next(), ++seg) {
             const int h = it.hv / p.chunks;
             const Rows rows = it.rows();
-            const bool two = both(it);
-            int last_pos = kNowhere;  // of the last tile's page
             const int lo_lim = it.limit(rows.row), hi_lim = it.limit(rows.row + max(rows.n, 1) - 1);
             float base = 0.f;
             for (int c0 = it.tb; c0 < it.te; c0 += 32) {  // 32 tiles' pages at a time
@@ -478,16 +492,15 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 for (int i = 0; i < n; ++i, ++g) {
                     const int pos = __shfl_sync(0xffffffffu, my_pos, i);
                     const float ks = __shfl_sync(0xffffffffu, my_ks, i), lv = __shfl_sync(0xffffffffu, my_lv, i);
-                    // K of the tile, and V of it (two row tiles) or of the one before (tiles in turn; the last tile's own too)
-                    const bool head = c0 + i == it.tb, tail = c0 + i == it.te - 1;
-                    const int steps = two ? 2 : 1 + !head + tail;
-#pragma unroll 1
-                    for (int x = 0; x < steps; ++x, ++use) {
-                        const bool v = x > 0;
-                        const uint32_t rs = use % kRaw, cs = use % kCv;
-                        wait_phase(rfull0 + 8 * rs, (use / kRaw) & 1, abort_at, p.budget_ns);
-                        const int first = (two || x != 1 || head ? pos : last_pos) + (w & 1) * 32;  // token of the first row
-                        if (v && first + 31 >= lo_lim) {
+                    if ((w & 1) == 0 && lane == 0) {  // (what the softmax needs to know of the tile)
+                        sm.meta[g % kMetas][w / 2] = Meta{ks, lv, exp2f(-lv), pos};
+                        mbar_arrive(smem_u32(&sm.m_full[g % kMetas]));
+                    }
+                    {
+                        const uint32_t rs = g % kRaw, cs = g % kCv;
+                        wait_phase(rfull0 + 8 * rs, (g / kRaw) & 1, abort_at, p.budget_ns);
+                        const int first = pos + (w & 1) * 32;  // token of the first row
+                        if (first + 31 >= lo_lim) {
                             // tokens that no row sees: their V is whatever the page holds, and 0 * NaN would reach
                             // every row; tokens that some rows see: a NaN is taken out and kept for those rows
 #pragma unroll 1
@@ -513,7 +526,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
 #pragma unroll
                         for (int k = 0; k < kIts; ++k)
                             in[k] = *reinterpret_cast<const uint4*>(&sm.raw[rs][(row0 + k * kRows) * D + c * 16]);
-                        wait_phase(cempty0 + 8 * cs, ((use / kCv) & 1) ^ 1, abort_at, p.budget_ns);
+                        wait_phase(cempty0 + 8 * cs, ((g / kCv) & 1) ^ 1, abort_at, p.budget_ns);
 #pragma unroll
                         for (int k = 0; k < kIts; ++k) {
                             const int row = row0 + k * kRows;
@@ -529,17 +542,13 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                             *reinterpret_cast<uint4*>(to + ((q + turn) ^ (row & 7)) * 16) = turn ? b : a;
                             *reinterpret_cast<uint4*>(to + ((q + !turn) ^ (row & 7)) * 16) = turn ? a : b;
                         }
-                        const bool meta = !v && (w & 1) == 0 && lane == 0;
-                        if (meta) sm.meta[g % kMetas][w / 2] = Meta{ks, lv, exp2f(-lv), pos};
                         fence_proxy_async_smem();
                         __syncwarp();
                         if (lane == 0) {
                             mbar_arrive(rempty0 + 8 * rs);
                             mbar_arrive(cfull0 + 8 * cs);
-                            if (meta) mbar_arrive(smem_u32(&sm.m_full[g % kMetas]));
                         }
                     }
-                    last_pos = pos;
                 }
             }
             if (lane == 0) mbar_arrive(smem_u32(&sm.n_full[seg & 1]));
@@ -564,19 +573,19 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
             constexpr int kLanes = D / 8, kRows = 32 / kLanes;  // lanes of a row (8 values each), rows at a time
             const int c = lane % kLanes, top = w.two ? u * kRowTile : 0;
             const Rows rows = w.rows;
+            // where the lane's 16 bytes of a row wait to be split: the row's own two parts
+            auto staged = [&](int row) { return &sm.q[u][c / (kLanes / 2)][row][(c % (kLanes / 2) ^ (row & (kLanes / 2 - 1))) * 16]; };
 #pragma unroll 2
             for (int k = 0; k < 32 / kRows; ++k) {
                 const int at = quad * 32 + k * kRows + lane / kLanes;
                 int hd;
                 const int rr = rows.of(p, top + at, hd);
                 const __nv_bfloat16* src = p.q + ((size_t)max(rr, 0) * p.pl.heads + (rr >= 0 ? hd : 0)) * D + c * 8;
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                                 smem_u32(&sm.q[u][c / 8][at][((c % 8) ^ (at & 7)) * 16])),
-                             "l"(src), "r"(rr >= 0 ? 16 : 0)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(staged(at))), "l"(src), "r"(rr >= 0 ? 16 : 0)
                              : "memory");
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
-            // each lane what it has copied itself: 8 values of a row, which is scaled by a power of two
+            // each lane what it has copied itself: 8 values of a row, which is scaled by a power of two and split
             // (four rows at a time, their shuffles side by side)
             constexpr int kB = 4;
 #pragma unroll 1
@@ -584,9 +593,8 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 uint4 w[kB];
                 uint32_t big[kB];
                 auto at = [&](int k) { return quad * 32 + (k0 + k) * kRows + lane / kLanes; };
-                auto mine = [&](int k) { return reinterpret_cast<uint4*>(&sm.q[u][c / 8][at(k)][((c % 8) ^ (at(k) & 7)) * 16]); };
 #pragma unroll
-                for (int k = 0; k < kB; ++k) w[k] = *mine(k);
+                for (int k = 0; k < kB; ++k) w[k] = *reinterpret_cast<const uint4*>(staged(at(k)));
 #pragma unroll
                 for (int k = 0; k < kB; ++k) {
                     const uint32_t a = 0x7fff7fffu;
@@ -607,20 +615,26 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
 #pragma unroll
                     for (int k = 0; k < kB; ++k) big[k] = max(big[k], __shfl_xor_sync(0xffffffffu, big[k], o));
                 }
+                __syncwarp();  // (a row's parts take the place of its values)
 #pragma unroll
                 for (int k = 0; k < kB; ++k) {
                     const float scale = scale_for(__uint_as_float(big[k] << 16));
                     // (a power of two from 2^-126 to 2^120: its inverse by its exponent)
                     const float inv = scale > 0.f ? __uint_as_float(0x7f000000u - __float_as_uint(scale)) : 1.f;
                     const uint32_t v[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
-                    uint32_t y[4];
+                    uint32_t hi[4], lo[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {  // (an infinity times 0 is NaN: it makes its row's scores NaN, as in any softmax)
                         const float a = __uint_as_float(v[e] << 16), b = __uint_as_float(v[e] & 0xffff0000u);
-                        y[e] = pack_half(fmaf(a, 0.f, a * inv), fmaf(b, 0.f, b * inv));
+                        const float x = fmaf(a, 0.f, a * inv), y = fmaf(b, 0.f, b * inv);
+                        hi[e] = to_e4m3x2(x, y);
+                        const float2 back = from_e4m3x2(hi[e]);
+                        lo[e] = to_e4m3x2(x - back.x, y - back.y);
                     }
-                    *mine(k) = make_uint4(y[0], y[1], y[2], y[3]);
-                    if (c == 0) sm.qf[u][at(k)] = scale * p.scale_log2;
+                    const int row = at(k), chunk = D == 128 ? (c / 2) ^ (row & 7) : (c / 2) ^ ((row >> 1) & 3);
+                    *reinterpret_cast<uint2*>(&sm.q[u][0][row][chunk * 16 + (c & 1) * 8]) = make_uint2(hi[0] | (hi[1] << 16), hi[2] | (hi[3] << 16));
+                    *reinterpret_cast<uint2*>(&sm.q[u][1][row][chunk * 16 + (c & 1) * 8]) = make_uint2(lo[0] | (lo[1] << 16), lo[2] | (lo[3] << 16));
+                    if (c == 0) sm.qf[u][row] = scale * p.scale_log2;
                 }
             }
             fence_proxy_async_smem();
@@ -862,9 +876,11 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
     }
     if (__syncthreads_or(dead)) {
         // a wait ran out: nothing more is issued, but copies and products may be in flight
-        if (warp == kLoad && lane == 0)
-            for (uint32_t x = loads > kRaw ? loads - kRaw : 0; x < loads; ++x)
+        if (warp == kLoad && lane == 0) {
+            for (uint32_t x = kloads > kK ? kloads - kK : 0; x < kloads; ++x) wait_raw(kfull0 + 8 * (x % kK), (x / kK) & 1, p.budget_ns);
+            for (uint32_t x = vloads > kRaw ? vloads - kRaw : 0; x < vloads; ++x)
                 wait_raw(rfull0 + 8 * (x % kRaw), (x / kRaw) & 1, p.budget_ns);
+        }
         if (warp == kIssue && elect_one_sync()) {
             mma_commit(smem_u32(&sm.drain));
             wait_raw(smem_u32(&sm.drain), 0, p.budget_ns);
@@ -915,7 +931,7 @@ int launch_cache_attend_rows(const cache::Pool& pl, const cache::Batch& bt, int 
     Maps maps;
     memset(&maps, 0, sizeof(maps));
     const long long tiles = (long long)pl.pages * pl.kv_heads;
-    if (!encode_page_map(&maps.k, pl.K, tiles, head_dim, CU_TENSOR_MAP_SWIZZLE_NONE) ||
+    if (!encode_page_map(&maps.k, pl.K, tiles, head_dim, head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B) ||
         !encode_page_map(&maps.v, pl.V, tiles, head_dim, CU_TENSOR_MAP_SWIZZLE_NONE)) {
         set_error("ssba_cache_attend: cuTensorMapEncodeTiled failed");
         return SSBA_ERR_CUDA;
