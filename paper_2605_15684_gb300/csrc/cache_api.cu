@@ -126,8 +126,8 @@ int attend(const char* who, const ssba_cache_desc* desc, const ssba_cache* cache
     if (desc->dtype == SSBA_BF16) {
         // Rows that share a K/V head's tokens, on average over the batch's sequences: up to 16, which are the columns of one
         // item, as columns of products over the bytes, bound by HBM; more as rows of fp16 products. (16 sequences of
-        // up to 8000 tokens, 8 K/V heads of 128: 16 rows 61 us as columns, 90 as rows; 32 rows 91, 91; 64 rows 143, 92;
-        // 128 rows 258, 125. One of 30000 tokens: 32 rows 35, 40; 64 rows 52, 42. 24 heads of 64, two of 2000: 32 rows 27, 21.)
+        // up to 8000 tokens, 8 K/V heads of 128: 16 rows 57 us as columns, 72 as rows; 32 rows 86, 73; 64 rows 137, 74;
+        // 128 rows 250, 106. One of 30000 tokens: 32 rows 34, 35; 64 rows 46, 39. 24 heads of 64, two of 2000: 32 rows 24, 19.)
         const long long rows = ((long long)T + B - 1) / B * (desc->heads / desc->kv_heads);
         if (!idx && rows > 16)
             return launch_cache_attend_rows(p, bt, desc->head_dim, scale, q, O, lse, workspace, st, budget_ns, withhold);

@@ -25,7 +25,7 @@
 //
 // Work is shared out and joined as in cache_attend_tc.cu, but a part is 130 KB: CTA c ends with the item that CTA c + 1
 // began with, finds that one's part there and keeps its own in shared memory. (4 sequences of 4000 tokens, 1000 rows in
-// all, 8 K/V heads of 128: 84 us; 90 with every part written, 110 with parts laid out by row, whose 16 bytes a thread
+// all, 8 K/V heads of 128: 81 us; 90 with every part written, 110 with parts laid out by row, whose 16 bytes a thread
 // fill half a sector.) Results are written 32 bytes a thread for that reason too: 82 us against 85.
 // What bounds it, at that size: a tile of 256 rows takes 2.2 us, a chain of QK, softmax (1.2 us a row tile, one warp a
 // scheduler, so latencies show) and PV in two pipelines; the four products alone would take 1.1 at the full rate. Two S of
@@ -33,7 +33,8 @@
 // PV of a tile's first half while the second is in the softmax changed nothing (84). Some 24 tiles a CTA are 52 us; 10 us
 // pass before the first S (dependent loads of table, scales and Q, cold instructions), 7 in the join, the rest in
 // changes of items (2.7 us each) and shares of unequal cost. 64 rows of 16 sequences of up to 8000 tokens, one row tile
-// each: 85 us (92 with K converted to fp16 as V is, 89 with unrolled products in the issuer).
+// each: 74 us (92 with K converted to fp16 as V is, 89 with unrolled products in the issuer, 85 where lanes and warps without
+// a row were masked like rows that see nothing).
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -641,7 +642,11 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sm.q_full[u]));
             int head;
-            lim = limit(w, rows.of(p, top + r, head));
+            const int row = rows.of(p, top + r, head);
+            lim = limit(w, row);
+            // a lane without a row sees what the warp's rows see, so that it makes no tile one to be masked (0.7 us each)
+            const int most = __reduce_max_sync(0xffffffffu, lim);
+            if (row < 0) lim = most;
             qf = sm.qf[u][r];
             __syncwarp();
         };
@@ -673,63 +678,70 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                 const bool cut = __any_sync(0xffffffffu, la < kPage || lb < kPage);
                 wait_phase(smem_u32(&sm.s_full[u]), cnt & 1, abort_at, p.budget_ns);
                 tc_fence_after();
-                uint32_t x[32];
-                auto get = [&](int ch) {  // chunk ch of the scores, what the row does not see at -inf
-                    tmem_ld_32x32b_x32(scol + 32 * ch, x);
-                    tmem_wait_ld();
-                    if (cut) {
-                        const int left = (ch < 2 ? la : lb) - (ch & 1) * 32;
+                if (!__any_sync(0xffffffffu, la + lb > 0)) {
+                    // none of the warp's rows sees any of it (in an item of few rows most warps have none): its weights are zero
+                    const uint32_t zero[16] = {};
+#pragma unroll 1
+                    for (int ch = 0; ch < 4; ++ch) tmem_st_32x32b_x16(scol + 16 * ch, zero);
+                } else {
+                    uint32_t x[32];
+                    auto get = [&](int ch) {  // chunk ch of the scores, what the row does not see at -inf
+                        tmem_ld_32x32b_x32(scol + 32 * ch, x);
+                        tmem_wait_ld();
+                        if (cut) {
+                            const int left = (ch < 2 ? la : lb) - (ch & 1) * 32;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (e >= left) x[e] = 0xff800000u;
+                            for (int e = 0; e < 32; ++e)
+                                if (e >= left) x[e] = 0xff800000u;
+                        }
+                    };
+                    // the tile's largest exponent: factors of scores are not negative
+                    float mx = -INFINITY;
+#pragma unroll 1
+                    for (int ch = 0; ch < 4; ++ch) {
+                        get(ch);
+                        float top = __uint_as_float(x[0]);
+#pragma unroll
+                        for (int e = 1; e < 31; e += 2) top = max3(top, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+                        top = fmaxf(top, __uint_as_float(x[31]));
+                        mx = fmaxf(mx, fmaf(top, ch < 2 ? ca : cb, ch < 2 ? ma.lv : mb.lv));
                     }
-                };
-                // the tile's largest exponent: factors of scores are not negative
-                float mx = -INFINITY;
+                    const bool up = m == -INFINITY ? mx > -INFINITY : mx > m + kMost;
+                    if (__any_sync(0xffffffffu, up)) {
+                        const float now = up ? mx - kTop : m, f = up ? fast_exp2(m - now) : 1.f;
+                        l *= f;
+                        m = now;
+                        if (i > own) {  // O holds the tiles so far: QK of this one was issued behind their PV
 #pragma unroll 1
-                for (int ch = 0; ch < 4; ++ch) {
-                    get(ch);
-                    float top = __uint_as_float(x[0]);
+                            for (int c = 0; c < D; c += 16) {
+                                uint32_t o[16];
+                                tmem_ld_32x32b_x16(ocol + c, o);
+                                tmem_wait_ld();
 #pragma unroll
-                    for (int e = 1; e < 31; e += 2) top = max3(top, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
-                    top = fmaxf(top, __uint_as_float(x[31]));
-                    mx = fmaxf(mx, fmaf(top, ch < 2 ? ca : cb, ch < 2 ? ma.lv : mb.lv));
-                }
-                const bool up = m == -INFINITY ? mx > -INFINITY : mx > m + kMost;
-                if (__any_sync(0xffffffffu, up)) {
-                    const float now = up ? mx - kTop : m, f = up ? fast_exp2(m - now) : 1.f;
-                    l *= f;
-                    m = now;
-                    if (i > own) {  // O holds the tiles so far: QK of this one was issued behind their PV
-#pragma unroll 1
-                        for (int c = 0; c < D; c += 16) {
-                            uint32_t o[16];
-                            tmem_ld_32x32b_x16(ocol + c, o);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                            tmem_st_32x32b_x16(ocol + c, o);
+                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                tmem_st_32x32b_x16(ocol + c, o);
+                            }
                         }
                     }
-                }
-                const float ref = m == -INFINITY ? 0.f : m;
-                // P of a chunk goes over scores that have been read
+                    const float ref = m == -INFINITY ? 0.f : m;
+                    // P of a chunk goes over scores that have been read
 #pragma unroll 1
-                for (int ch = 0; ch < 4; ++ch) {
-                    get(ch);
-                    const float cc = ch < 2 ? ca : cb, off = (ch < 2 ? ma.lv : mb.lv) - ref;
-                    const float2 c2 = make_float2(cc, cc), o2 = make_float2(off, off);
-                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                    uint32_t pk[16];
+                    for (int ch = 0; ch < 4; ++ch) {
+                        get(ch);
+                        const float cc = ch < 2 ? ca : cb, off = (ch < 2 ? ma.lv : mb.lv) - ref;
+                        const float2 c2 = make_float2(cc, cc), o2 = make_float2(off, off);
+                        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                        uint32_t pk[16];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float2 y = __ffma2_rn(make_float2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), c2, o2);
-                        y = make_float2(fast_exp2(y.x), fast_exp2(y.y));
-                        sum[e & 1] = __fadd2_rn(sum[e & 1], y);
-                        pk[e] = pack_half(y.x, y.y);
+                        for (int e = 0; e < 16; ++e) {
+                            float2 y = __ffma2_rn(make_float2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), c2, o2);
+                            y = make_float2(fast_exp2(y.x), fast_exp2(y.y));
+                            sum[e & 1] = __fadd2_rn(sum[e & 1], y);
+                            pk[e] = pack_half(y.x, y.y);
+                        }
+                        tmem_st_32x32b_x16(scol + 16 * ch, pk);
+                        l = fmaf((sum[0].x + sum[1].x) + (sum[0].y + sum[1].y), ch < 2 ? ma.inv : mb.inv, l);
                     }
-                    tmem_st_32x32b_x16(scol + 16 * ch, pk);
-                    l = fmaf((sum[0].x + sum[1].x) + (sum[0].y + sum[1].y), ch < 2 ? ma.inv : mb.inv, l);
                 }
                 tmem_wait_st();
                 tc_fence_before();
