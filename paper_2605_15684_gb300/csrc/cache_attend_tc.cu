@@ -8,8 +8,8 @@
 //   O^T = V^T P^T M = 128 channels, N = 2R, K = 128 tokens                  (A = V tile, MN-major)
 // Q and P are not 8-bit values: each is the sum of two e4m3 numbers, x = hi + lo / 16 with hi = e4m3(x) and
 // lo = e4m3(16 (x - hi)), 4 + 4 bits of significand, in two columns whose products are added in fp32. A row
-// of Q is first brought below 448 by a power of two; its 8-bit significands then split without rounding,
-// but for what lies 2^-22 below the row's largest. P is rounded to 8 bits as a bf16 P would be.
+// of Q is first brought below 448 by a power of two; its 8-bit significands then split without rounding
+// down to 2^-13 of the row's largest, and to within 2^-21 of it below. P is rounded to 8 bits as a bf16 P would be.
 //
 // A CTA takes an equal share of the batch's tiles, whole items (one sequence, one K/V head, R rows) and
 // parts of them, in order. Warps of a CTA (all walk the same items):

@@ -436,6 +436,30 @@ def test_bad_values_are_flagged_and_reach_nothing():
         assert np.array_equal(getattr(after, name), getattr(before, name), equal_nan=True)
 
 
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attend_queries_with_one_large_channel(d, n):
+    """A channel of Q a thousand times the others', where K is zero: the others make the scores. 1000 is held
+    as 250 * 4 in steps of 2^-9, so a row's small values are off by 2^-10 * 4 at most, which a score has d times over,
+    times |k|; a weight is off by twice that, an output by A times that."""
+    bt = Batch([900, 130], 2, d, seed=41)
+    K = bt.cache.K.view(torch.uint8)
+    K[..., 3] = 0
+    g = torch.Generator().manual_seed(42)
+    T = n + 1
+    q = torch.randn((T, 8, d), generator=g)
+    q[:, :, 3] = 1000 * torch.sign(q[:, :, 3])
+    q = q.bfloat16().cuda()
+    O, lse = pc.cache_attend(bt.desc(8), bt.cache, q, bt.gpu_table(), ints([900, 130]), ints([0, n, T]))
+    torch.cuda.synchronize()
+    want, wl, A, S = ref.attend(bt.pool(), q.double().cpu().numpy(), bt.table, [900, 130], [0, n, T], d ** -0.5)
+    bO, bl = ref.bounds(want, A, S, d, 900, True)
+    k = torch.nan_to_num(bt.cache.K.float() * bt.cache.k_scale[:, :, None, None]).abs().sum(-1).max().item()
+    off = d ** -0.5 * k * 2.0 ** -10 * 4
+    hold(O, want, bO + 2 * off * A, "O")
+    hold(lse, wl, bl + off, "lse")
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("lens,n,heads,kv", [([9000], [9], 8, 2), ([9000], [70], 8, 2), ([6000, 130, 2500], [300, 130, 77], 6, 3)])
 def test_attend_rows_joined_from_parts(lens, n, heads, kv, d):
