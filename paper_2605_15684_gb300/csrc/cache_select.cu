@@ -171,6 +171,7 @@ __device__ void select_top(const float* score, uint32_t* kept, int n, int want, 
     __syncthreads();
     const int cut = sc.pick[0], left = sc.pick[1], nc = sc.hist[cut];
     if (nc > kCand) {
+        __syncthreads();  // everyone has read its step's count: the walk clears the histogram for its own
         select_radix(score, n, want, first, out, sc);
         return;
     }

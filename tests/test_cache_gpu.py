@@ -278,6 +278,28 @@ def test_select_many_rows(d, dtype):
     assert np.array_equal(idx.cpu().numpy(), want[0]) and np.array_equal(cnt.cpu().numpy(), want[1])
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("keep", [3, 65, 700])
+def test_select_few_high_scores_above_many_close_ones(keep, d):
+    """Finite scores, a handful of which lie so far above that all others fall into the lowest steps between the extremes, where
+    the cut then is: more of them than are ranked by counting. Sums of eighths and 64ths are exact in fp32."""
+    pages, rows = 2200, 24
+    bt = Batch([64 * pages - 7], 1, d, spare=1)
+    g = torch.Generator().manual_seed(51)
+    q = queries(rows, 4, d, BF16, 52)
+    km = torch.randint(-2, 3, (pages, d), generator=g).float() / 64
+    for i, j in enumerate((70, 700, 1500, 2100)):
+        km[j] = q[i, i].float().cpu() * 256
+    bt.cache.k_mean[torch.from_numpy(bt.table[0][:pages].copy()).cuda(), 0] = km.cuda()
+    table = np.repeat(bt.table, rows, axis=0)
+    lens, cu = [64 * pages - 7 - 64 * i for i in range(rows)], list(range(rows + 1))
+    want = ref.select(bt.pool(), q.double().cpu().numpy(), table, lens, cu, keep, 1)
+    for _ in range(20):
+        idx, cnt = pc.cache_select(bt.desc(4), bt.cache, q, ints(table), ints(lens), ints(cu), keep)
+        assert np.array_equal(idx.cpu().numpy(), want[0]) and np.array_equal(cnt.cpu().numpy(), want[1])
+    assert api.get_status() == api.SSBA_OK
+
+
 def test_select_all_equal():
     bt = Batch([64 * 40], 1, 128)
     bt.cache.k_mean.fill_(0.5)
