@@ -493,7 +493,8 @@ SSBA_API int ssba_cache_copy(const ssba_cache_desc* desc, const ssba_cache* cach
                              const int32_t* dst, int32_t n, void* stream);
 
 /* Reads and clears the device status word of the current device (SSBA_OK,
- * SSBA_ERR_TIMEOUT or SSBA_ERR_CHECK). Synchronous: call after the caller's stream sync. Returns
+ * SSBA_ERR_TIMEOUT or SSBA_ERR_CHECK; of both since the last read, the timeout, whose
+ * workspaces have to be zeroed). Synchronous: call after the caller's stream sync. Returns
  * SSBA_OK, or SSBA_ERR_CUDA if the read failed. */
 SSBA_API int ssba_get_status(int32_t* device_status_out);
 

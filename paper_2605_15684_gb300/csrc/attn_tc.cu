@@ -779,7 +779,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_attn_tc_kernel(const __grid_
                         bad |= c < 0 || c > p.keep;
                     }
                 }
-                if (__any_sync(0xffffffffu, bad) && lane == 0) atomicExch(p.status, SSBA_ERR_CHECK);
+                if (__any_sync(0xffffffffu, bad) && lane == 0) atomicCAS(p.status, SSBA_OK, SSBA_ERR_CHECK);  // (an unread timeout stays)
                 __syncwarp();
             }
             // the round's Q pair, once the last round's final QK has read its own

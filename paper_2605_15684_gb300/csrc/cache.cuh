@@ -44,7 +44,8 @@ __device__ __forceinline__ T ld(const T* p)
     return *p;
 }
 
-__device__ __forceinline__ void flag(int* status) { *status = SSBA_ERR_CHECK; }
+// A timeout that nobody has read yet stays: whoever reads it drops the workspaces whose counters it has left set.
+__device__ __forceinline__ void flag(int* status) { atomicCAS(status, SSBA_OK, SSBA_ERR_CHECK); }
 
 // A sequence from its entries in cu and lens, clamped.
 __device__ __forceinline__ Seq make_seq(const Batch& bt, int c0, int c1, int l, int* status)

@@ -251,6 +251,27 @@ def test_a_wait_that_runs_out(lens, n, d):
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+def test_a_timeout_is_not_hidden_by_a_later_check():
+    """A wait that ran out, and behind it, before anyone has read the status, a call with a page outside the pool: what is
+    read is the timeout, whose counters the binding has to forget."""
+    for lens, n in (([3000, 100], [1, 1]), ([900, 300], [60, 50])):
+        bt = Batch(lens, 2, 128)
+        a = args(bt, n, 8)
+        want = pc.cache_attend(*a)
+        (kept,) = [w for (dev, st), w in pc._ws.items() if st == torch.cuda.current_stream().cuda_stream]
+        pc.test_cache_timeout(*a, torch.empty_like(want[0]), torch.empty_like(want[1]), kept)
+        table = bt.gpu_table()
+        table[1, 0] = bt.pages
+        other = torch.zeros(pc.cache_attend_workspace_bytes(a[0]), dtype=torch.uint8, device="cuda")
+        pc.cache_attend(a[0], a[1], a[2], table, a[4], a[5], workspace=other)
+        torch.cuda.synchronize()
+        assert api.get_status() == api.SSBA_ERR_TIMEOUT
+        got = pc.cache_attend(*a)
+        torch.cuda.synchronize()
+        assert api.get_status() == api.SSBA_OK
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_a_workspace_is_left_as_it_was_found():
     """The counters are zero after a call, so that a caller's workspace serves call after call of any shape."""
     ws = torch.zeros(pc.cache_attend_workspace_bytes(Batch([64], 1, 64).desc(1)), dtype=torch.uint8, device="cuda")
