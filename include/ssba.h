@@ -464,9 +464,9 @@ SSBA_API size_t ssba_cache_attend_workspace_bytes(const ssba_cache_desc* desc);
  *               Its first SSBA_CACHE_TICKET_BYTES are zero-filled once; a call leaves them zero (after
  *               SSBA_ERR_TIMEOUT they have to be zeroed again). Calls that may overlap on the GPU need
  *               workspaces of their own.
- * bf16 calls without lists of more than 16 rows a K/V head and sequence, on average, hold a row's query values to within
- * 2^-17 of its largest (the others to 2^-21), and take V scales of a sequence's pages as no more than 2^100 apart from its first
- * page's (or from 1, where that one's is 0).
+ * bf16 calls hold a row's query values to within 2^-21 of its largest. Those without lists of more than 16 rows a K/V head
+ * and sequence, on average, take V scales of a sequence's pages as no more than 2^100 apart from its first page's (or from 1,
+ * where that one's is 0).
  * Tokens that a row does not see have no part in it, whatever their K and V hold. Products and sums are
  * fp32 (bf16 calls form products of 8-bit values exactly and round the weights to 8 bits of significand or more
  * before they meet V). */

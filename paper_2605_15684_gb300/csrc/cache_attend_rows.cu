@@ -5,10 +5,12 @@
 // rows; it visits its sequence's tiles of 128 tokens (two pages):
 //   S_u = Q_u K^T   tcgen05.mma kind::f8f6f4, M = 128, N = 128, K = D, twice (K's bytes as they are)
 //   O_u += P_u V    tcgen05.mma kind::f16, M = 128, N = D, K = 128 (fp16, P from tensor memory, V MN-major)
-// Q is the sum of two e4m3 numbers, whose products go into one sum: a row is brought below 448 by a power of two, and
-// x = hi + lo with hi = e4m3(x), lo = e4m3(x - hi). A bf16 value of 2^-2 or more is held exactly, a smaller one to half a
-// step of 2^-9; the row's largest being above 224, that is down to 2^-9 of it, and to within 2^-17 of it below. (fp16
-// would go on to 2^-25, but K would have to be converted too: 92 us against 89 in the last case below.)
+// Q is the sum of two 8-bit numbers, whose products go into one sum: a row is brought below 448 by a power of two, and
+// x = hi + lo with hi = e4m3(x), lo = e5m2(x - hi). Of a bf16 value's 8 bits hi takes four, and what it leaves is at most 8
+// steps of the value's last bit, a number of three bits: exact from 2^-6 on, where hi is normal. Below, lo's steps end at
+// 2^-16 and half of one of 2^-13 is the most that is lost: 2^-14, the row's largest being above 224. So a value is exact
+// down to 2^-13 of that and within 2^-21 of it below, as with few rows. (A lo in e4m3, whose steps end at 2^-9, costs
+// the same and loses up to 2^-10, 3 % of a value of 2^-5; fp16 needs K converted too, 92 us against 89 in the last case below.)
 // An e4m3 value is an fp16 value, so V is converted without rounding, once for both row tiles, and the
 // pages' scales stay out of the products: K's multiplies the scores, V's is added to their exponent,
 //   P = 2^(s + log2 v_scale - m),   l = sum P / v_scale,   O = sum P (bytes of V) / l,
@@ -61,6 +63,8 @@ constexpr uint32_t kTmemCols = 512;
 
 constexpr uint32_t idesc_f16_f32(int M, int N, bool b_mn_major) { return idesc_e4m3_f32(M, N, false, b_mn_major); }  // formats 0: fp16
 
+constexpr uint32_t kAE5m2 = 1u << 7;  // of an instruction descriptor of kind::f8f6f4: A is e5m2 (B's type is its own)
+
 constexpr int kItemRing = 4;
 
 // An item's share as the softmax warps get it, which have no registers for the walk.
@@ -78,7 +82,7 @@ struct Meta {
 
 template <int D>
 struct __align__(1024) Smem {
-    uint8_t q[2][2][kRowTile][D];          // e4m3: a row tile's high and low parts, swizzled as K is
+    uint8_t q[2][2][kRowTile][D];          // a row tile's high (e4m3) and low (e5m2) parts, swizzled as K is
     uint8_t cv[kCv][D / 64][kTile][128];   // fp16 V, 64 channels a 128-byte row, 128-byte swizzle
     uint8_t kraw[kK][kTile * D];           // K's bytes (rows of 128 or 64 bytes, that swizzle)
     uint8_t raw[kRaw][kTile * D];          // V's bytes
@@ -129,6 +133,14 @@ __device__ __forceinline__ uint32_t half2_of(uint32_t e4m3x2)
     uint32_t h;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(e4m3x2)));
     return h;
+}
+
+// Two floats to two e5m2 bytes, as to_e4m3x2.
+__device__ __forceinline__ uint32_t to_e5m2x2(float lo, float hi)
+{
+    uint16_t r;
+    asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
 }
 
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi)
@@ -405,8 +417,8 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                         const uint64_t b = sdesc(smem_u32(&sm.kraw[slot][0]), 16, 8 * D, kSwizzle);
 #pragma unroll 1
                         for (int k = 0; k < 2 * (D / 32); ++k) {  // the high parts, then the low ones
-                            mma_f8_ss(tbase + u * 128, a, b + (uint64_t)(2 * (k & (D / 32 - 1))), idesc_e4m3_f32(128, 128, false, false),
-                                      k > 0 ? 1u : 0u);
+                            mma_f8_ss(tbase + u * 128, a, b + (uint64_t)(2 * (k & (D / 32 - 1))),
+                                      idesc_e4m3_f32(128, 128, false, false) | (k < D / 32 ? 0u : kAE5m2), k > 0 ? 1u : 0u);
                             a += k == D / 32 - 1 ? kRowTile * D / 16 - 2 * (D / 32 - 1) : 2;
                         }
                         mma_commit(smem_u32(&sm.s_full[u]));
@@ -631,7 +643,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                         const float x = fmaf(a, 0.f, a * inv), y = fmaf(b, 0.f, b * inv);
                         hi[e] = to_e4m3x2(x, y);
                         const float2 back = from_e4m3x2(hi[e]);
-                        lo[e] = to_e4m3x2(x - back.x, y - back.y);
+                        lo[e] = to_e5m2x2(x - back.x, y - back.y);
                     }
                     const int row = at(k), chunk = D == 128 ? (c / 2) ^ (row & 7) : (c / 2) ^ ((row >> 1) & 3);
                     *reinterpret_cast<uint2*>(&sm.q[u][0][row][chunk * 16 + (c & 1) * 8]) = make_uint2(hi[0] | (hi[1] << 16), hi[2] | (hi[3] << 16));

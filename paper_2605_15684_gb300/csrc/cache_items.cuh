@@ -18,7 +18,8 @@ __device__ __forceinline__ uint64_t sdesc(uint32_t saddr, uint32_t lbo_bytes, ui
     return (sdesc_sw128(saddr, lbo_bytes, sbo_bytes) & ~(7ull << 61)) | (static_cast<uint64_t>(layout) << 61);
 }
 
-// Instruction descriptor for kind::f8f6f4 with e4m3 A and B (formats 0), and for kind::f16 with fp16 ones (also 0),
+// Instruction descriptor for kind::f8f6f4 with e4m3 A and B (formats 0; each operand has its own field), and for kind::f16
+// with fp16 ones (also 0, and the same for both),
 // with an fp32 accumulator; the other fields as in idesc_bf16_f32.
 __host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N, bool a_mn_major, bool b_mn_major)
 {

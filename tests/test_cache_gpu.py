@@ -482,6 +482,34 @@ def test_attend_queries_with_one_large_channel(d, n):
     hold(lse, wl, bl + off, "lse")
 
 
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attend_queries_hold_small_values_beside_a_large_one(d, n):
+    """One channel of Q far above the others, where K is zero, for few rows and for many. The others are 4 (2^-5 + 2^-10),
+    and 1000 is held as 250 * 4: what a value's first part leaves is 2^-10, the same in every channel, and keys have the
+    queries' signs, so that nothing cancels. The two parts are off by 2^-14 * 4 at most, which a score has d times over,
+    times |k|; a weight is off by twice that, an output by A times that."""
+    bt = Batch([900, 130], 2, d, seed=41)
+    c, T = bt.cache, n + 1
+    g = torch.Generator().manual_seed(43)
+    sign = torch.randint(0, 2, (d,), generator=g) * 2.0 - 1
+    key = sign[None] * (32 + 4 * torch.randint(0, 8, (64, 1), generator=g).float())  # whole steps of e4m3
+    key[:, 3] = 0
+    c.K.view(torch.uint8)[:] = key.to(ref.E4M3).view(torch.uint8).cuda()
+    c.k_scale.fill_(2.0 ** -4)
+    q = (sign * 4 * (2.0 ** -5 + 2.0 ** -10)).repeat(T, 8, 1)
+    q[:, :, 3] = 1000
+    q = q.bfloat16().cuda()
+    assert (q[:, :, 4].abs() == 4 * (2.0 ** -5 + 2.0 ** -10)).all()
+    O, lse = pc.cache_attend(bt.desc(8), c, q, bt.gpu_table(), ints([900, 130]), ints([0, n, T]))
+    torch.cuda.synchronize()
+    want, wl, A, S = ref.attend(bt.pool(), q.double().cpu().numpy(), bt.table, [900, 130], [0, n, T], d ** -0.5)
+    bO, bl = ref.bounds(want, A, S, d, 900, True)
+    off = d ** -0.5 * d * 60 * 2.0 ** -4 * 2.0 ** -14 * 4
+    hold(O, want, bO + 2 * off * A, "O")
+    hold(lse, wl, bl + off, "lse")
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("lens,n,heads,kv", [([9000], [9], 8, 2), ([9000], [70], 8, 2), ([6000, 130, 2500], [300, 130, 77], 6, 3)])
 def test_attend_rows_joined_from_parts(lens, n, heads, kv, d):
