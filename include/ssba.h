@@ -466,7 +466,7 @@ SSBA_API size_t ssba_cache_attend_workspace_bytes(const ssba_cache_desc* desc);
  *               workspaces of their own.
  * bf16 calls hold a row's query values to within 2^-21 of its largest. Those without lists of more than 16 rows a K/V head
  * and sequence, on average, take V scales of a sequence's pages as no more than 2^100 apart from its first page's (or from 1,
- * where that one's is 0).
+ * where that one's is 0), and beside pages where it is 0 as from 2^-60 to 2^30 times that one's (or 1).
  * Tokens that a row does not see have no part in it, whatever their K and V hold. Products and sums are
  * fp32 (bf16 calls form products of 8-bit values exactly and round the weights to 8 bits of significand or more
  * before they meet V). */

@@ -58,6 +58,11 @@ constexpr float kTop = 8.f;         // log2 of the largest P against a new refer
 constexpr float kMost = 14.f;       // log2 of the largest P that is let stand (fp16 ends at 65504)
 constexpr int kConverters = 4;
 constexpr float kSpan = 100.f;      // log2 of V scales, relative to the first page's
+// The same for a page whose V is all zero. Its P meet zeros, so they count in the sum of weights alone: low enough not to raise the
+// row's reference above what the other pages' values need (with 0, V scales of 2^-30 behind a first page of zeros left P
+// two bits), and not so low that 2^(s + it - m) vanishes where the weight counts: for other pages from 2^-60 to 2^30, weights down
+// to 2^-36 of the largest.
+constexpr float kNoV = -60.f;
 enum Role { kLoad = 0, kIssue = 1, kConvert = 2, kItems = 6, kSoftmax = 8 };
 constexpr uint32_t kTmemCols = 512;
 
@@ -499,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
                     __syncwarp();
                 }
                 if (page >= 0) {
-                    my_lv = vs > 0.f ? fminf(fmaxf(log2f(vs) - base, -kSpan), kSpan) : isnan(vs) ? vs : 0.f;
+                    my_lv = vs > 0.f ? fminf(fmaxf(log2f(vs) - base, -kSpan), kSpan) : isnan(vs) ? vs : kNoV;
                 }
                 const int my_pos = page >= 0 ? j * kPage : kNowhere;
                 const int n = min(32, it.te - c0);

@@ -223,6 +223,22 @@ def test_attend_pages_of_zeros_and_far_scales(d, dtype, n):
     check_attend(bt, [n, 1, min(n, 9)], 4, dtype, seed=32)
 
 
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("zero,others", [((0,), -34), ((0, 5, 9), -44), ((0, 2), 28)])
+def test_attend_pages_of_zero_values_beside_small_ones(zero, others, d, n):
+    """Pages whose V is all zero, the first one among them, have a part in the weights' sum alone: the other pages' values,
+    however small, keep their bits."""
+    bt = Batch([700, 300], 2, d, seed=61)
+    c = bt.cache
+    for b in range(2):
+        for j, p in enumerate(int(p) for p in bt.table[b] if p >= 0):
+            c.v_scale[p] = 0.0 if j in zero else 2.0 ** others
+            if j in zero:
+                c.V.view(torch.uint8)[p] = 0
+    check_attend(bt, [n, min(n, 33)], 4, seed=62)
+
+
 # ----------------------------------------------------------------------------- select
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("d", [64, 128])
