@@ -5,6 +5,10 @@
 // A call that is not plainly in order (a wrong shape, type or device, results that are not to be allocated on the
 // current stream, no memory) returns None, and cache.py goes the long way, which names what is wrong. A status other than SSBA_OK comes
 // back as a number. Nothing is kept between calls.
+//
+// The interpreter's lock is held while arguments are looked at, and not while results are allocated or kernels launched: either
+// may wait for the GPU, and what the GPU waits for (a host callback, another thread's copy) may need the lock. The caller's
+// references keep the arguments' tensors meanwhile.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -87,6 +91,15 @@ const Call* call_of(PyObject* const* a, Py_ssize_t n, Py_ssize_t want)
     return static_cast<Call*>(PyCapsule_GetPointer(a[0], kName));
 }
 
+// Without the interpreter's lock, to the end of the scope (also by an exception).
+struct Unlocked {
+    PyThreadState* state = PyEval_SaveThread();
+    Unlocked() = default;
+    Unlocked(const Unlocked&) = delete;
+    Unlocked& operator=(const Unlocked&) = delete;
+    ~Unlocked() { PyEval_RestoreThread(state); }
+};
+
 bool elsewhere(const Call& c) { return c10::cuda::current_device() != c.device; }
 
 void* stream(const Call& c) { return c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(c.device)).stream(); }
@@ -119,8 +132,13 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n)
         Batch b;
         const at::Tensor *k = rows(a[1], *c, c->desc.kv_heads), *v = rows(a[2], *c, c->desc.kv_heads);
         if (elsewhere(*c) || !k || !v || v->size(0) != k->size(0) || !batch(a + 3, *c, b)) return none();
-        return PyLong_FromLong(c->append(&c->desc, &c->pool, k->const_data_ptr(), v->const_data_ptr(), (int32_t)k->size(0),
-                                         b.table, b.width, b.lens, b.cu, b.B, stream(*c)));
+        int rc;
+        {
+            Unlocked scope;
+            rc = c->append(&c->desc, &c->pool, k->const_data_ptr(), v->const_data_ptr(), (int32_t)k->size(0), b.table, b.width,
+                           b.lens, b.cu, b.B, stream(*c));
+        }
+        return PyLong_FromLong(rc);
     } catch (...) {
         return none();
     }
@@ -141,11 +159,16 @@ PyObject* select(PyObject*, PyObject* const* a, Py_ssize_t n)
         const at::Tensor* q = rows(a[1], *c, c->desc.heads);
         if (elsewhere(*c) || !q || !batch(a + 2, *c, b) || first < 0 || keep <= first || keep > SSBA_CACHE_MAX_WIDTH)
             return none();
-        at::Tensor idx = make(*c, {q->size(0), c->desc.kv_heads, keep}, at::kInt);
-        at::Tensor cnt = make(*c, {q->size(0), c->desc.kv_heads}, at::kInt);
-        const int rc = c->select(&c->desc, &c->pool, q->const_data_ptr(), (int32_t)q->size(0), b.table, b.width, b.lens, b.cu,
-                                 b.B, (int32_t)keep, (int32_t)first, idx.mutable_data_ptr<int32_t>(),
-                                 cnt.mutable_data_ptr<int32_t>(), stream(*c));
+        at::Tensor idx, cnt;
+        int rc;
+        {
+            Unlocked scope;
+            idx = make(*c, {q->size(0), c->desc.kv_heads, keep}, at::kInt);
+            cnt = make(*c, {q->size(0), c->desc.kv_heads}, at::kInt);
+            rc = c->select(&c->desc, &c->pool, q->const_data_ptr(), (int32_t)q->size(0), b.table, b.width, b.lens, b.cu, b.B,
+                           (int32_t)keep, (int32_t)first, idx.mutable_data_ptr<int32_t>(), cnt.mutable_data_ptr<int32_t>(),
+                           stream(*c));
+        }
         if (rc != SSBA_OK) return PyLong_FromLong(rc);
         PyObject *x = THPVariable_Wrap(std::move(idx)), *y = THPVariable_Wrap(std::move(cnt));
         return Py_BuildValue("NN", x, y);
@@ -171,12 +194,17 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n)
                 idx->size(1) != c->desc.kv_heads || cnt->size(1) != c->desc.kv_heads || idx->size(2) > SSBA_CACHE_MAX_WIDTH)
                 return none();
         }
-        at::Tensor O = make(*c, q->sizes(), c->type), lse = make(*c, {q->size(0), q->size(1)}, at::kFloat);
-        const int rc = c->attend(&c->desc, &c->pool, q->const_data_ptr(), (int32_t)q->size(0), b.table, b.width, b.lens, b.cu,
-                                 b.B, idx ? idx->const_data_ptr<int32_t>() : nullptr,
-                                 cnt ? cnt->const_data_ptr<int32_t>() : nullptr, idx ? (int32_t)idx->size(2) : 0,
-                                 O.mutable_data_ptr(), lse.mutable_data_ptr<float>(), ws->mutable_data_ptr(),
-                                 (size_t)ws->numel(), stream(*c));
+        at::Tensor O, lse;
+        int rc;
+        {
+            Unlocked scope;
+            O = make(*c, q->sizes(), c->type);
+            lse = make(*c, {q->size(0), q->size(1)}, at::kFloat);
+            rc = c->attend(&c->desc, &c->pool, q->const_data_ptr(), (int32_t)q->size(0), b.table, b.width, b.lens, b.cu, b.B,
+                           idx ? idx->const_data_ptr<int32_t>() : nullptr, cnt ? cnt->const_data_ptr<int32_t>() : nullptr,
+                           idx ? (int32_t)idx->size(2) : 0, O.mutable_data_ptr(), lse.mutable_data_ptr<float>(),
+                           ws->mutable_data_ptr(), (size_t)ws->numel(), stream(*c));
+        }
         if (rc != SSBA_OK) return PyLong_FromLong(rc);
         PyObject *x = THPVariable_Wrap(std::move(O)), *y = THPVariable_Wrap(std::move(lse));
         return Py_BuildValue("NN", x, y);
@@ -194,8 +222,13 @@ PyObject* copy(PyObject*, PyObject* const* a, Py_ssize_t n)
         const at::Tensor *s = tensor(a[1], *c, at::kInt), *d = tensor(a[2], *c, at::kInt);
         if (elsewhere(*c) || !s || !d || s->dim() != 1 || d->dim() != 1 || s->size(0) != d->size(0) || s->size(0) > INT32_MAX)
             return none();
-        return PyLong_FromLong(c->copy(&c->desc, &c->pool, s->const_data_ptr<int32_t>(), d->const_data_ptr<int32_t>(),
-                                       (int32_t)s->size(0), stream(*c)));
+        int rc;
+        {
+            Unlocked scope;
+            rc = c->copy(&c->desc, &c->pool, s->const_data_ptr<int32_t>(), d->const_data_ptr<int32_t>(), (int32_t)s->size(0),
+                         stream(*c));
+        }
+        return PyLong_FromLong(rc);
     } catch (...) {
         return none();
     }

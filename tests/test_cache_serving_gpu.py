@@ -1,6 +1,8 @@
 """The cache's calls together, as a server makes them: growing, forked, truncated and compacted sequences over several layers,
 on other streams, in graphs, and with a wait that runs out."""
+import ctypes
 import math
+import threading
 
 import numpy as np
 import pytest
@@ -370,6 +372,53 @@ def test_short_and_long_way_into_a_call():
     assert O.shape == (0, 8, 128) and lse.shape == (0, 8) and idx.shape == (0, 2, 4) and cnt.shape == (0, 2)
     torch.cuda.synchronize()
     assert api.get_status() == api.SSBA_OK
+
+
+def test_calls_let_other_threads_run():
+    """The native calls hold Python's lock neither while they allocate nor while they launch: entry points that are asked
+    for it (a stand-in returns 1 where its thread holds it, 0, which is SSBA_OK, where not) say so."""
+    bt = Batch([700, 90], 2, 128)
+    desc, cache, q, table, lens, cu = args(bt, [1, 1], 8)
+    held = ctypes.cast(ctypes.pythonapi.PyGILState_Check, ctypes.c_void_p).value
+    assert ctypes.pythonapi.PyGILState_Check() == 1
+    c, ext = desc.c(), pc._extension()
+    call = ext.bind(held, held, held, held, ctypes.addressof(c), ctypes.addressof(cache._c), q.device.index, True)
+    k = torch.zeros((2, 2, 128), dtype=BF16, device="cuda")
+    ws = torch.zeros(256, dtype=torch.uint8, device="cuda")
+    assert ext.append(call, k, k, table, lens, cu) == 0
+    assert ext.copy(call, lens, lens) == 0
+    assert isinstance(ext.select(call, q, table, lens, cu, 4, 1), tuple)
+    assert isinstance(ext.attend(call, q, table, lens, cu, None, None, ws), tuple)
+
+
+def test_threads_with_streams_of_their_own():
+    """Threads that serve sequences of their own side by side, each on its stream: what each would get alone."""
+    def work(i, out):
+        torch.cuda.set_device(0)
+        with torch.cuda.stream(torch.cuda.Stream()):
+            desc, cache, q, table, lens, cu = a = calls[i]
+            for _ in range(25):
+                O, lse = pc.cache_attend(*a)
+                idx, cnt = pc.cache_select(*a, 4)
+                O2, lse2 = pc.cache_attend(*a, idx, cnt)
+            out[i] = (O, lse, idx, cnt, O2, lse2)
+            torch.cuda.current_stream().synchronize()
+
+    batches = [Batch([3000 - 500 * i, 90 + i], 2, 128 if i % 2 else 64, i) for i in range(4)]
+    calls = [args(bt, [1, 1] if i < 2 else [50, 9], 8) for i, bt in enumerate(batches)]
+    torch.cuda.synchronize()
+    alone, together = {}, {}
+    for i in range(4):
+        work(i, alone)
+    threads = [threading.Thread(target=work, args=(i, together)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert api.get_status() == api.SSBA_OK
+    for i in range(4):
+        assert all(torch.equal(x, y) for x, y in zip(alone[i], together[i]))
 
 
 @pytest.mark.parametrize("B", [129, 1500])
