@@ -525,9 +525,10 @@ class PagedCache:
 
     def _copy(self, pairs) -> None:
         if pairs:
-            src, dst = (self._ints(x) for x in zip(*pairs))
-            for pool in self.pools:
-                cache_copy(self.desc, pool, src, dst)
+            with torch.cuda.device(self.device):  # (the page table has them already: no refusal for the current device's sake)
+                src, dst = (self._ints(x) for x in zip(*pairs))
+                for pool in self.pools:
+                    cache_copy(self.desc, pool, src, dst)
 
     def compact(self) -> int:
         """Moves the live pages to the front of the pools; returns how many moved."""

@@ -267,3 +267,37 @@ def test_native_calls_leave_what_is_not_in_order_to_the_long_way(lib):
         ext.attend(call, q)
     with pytest.raises(ValueError):
         ext.append(None, q, q, t, t, t)
+
+
+def test_copies_of_a_step_are_made_on_the_caches_device(monkeypatch):
+    """The page table says that a step's pages were copied before they are: so that is done wherever the caller's current
+    device is (calls on a pool refuse any but its own)."""
+    current, made = ["another"], []
+
+    class On:
+        def __init__(self, dev):
+            self.dev = dev
+
+        def __enter__(self):
+            self.was, current[0] = current[0], self.dev
+
+        def __exit__(self, *_):
+            current[0] = self.was
+
+    def copy(d, pool, src, dst, stream=None):
+        if current[0] != cache.device:
+            raise api.SsbaError(api.SSBA_ERR_INVALID, "the current device is another")
+        made.append((pool, src.tolist(), dst.tolist()))
+
+    monkeypatch.setattr(torch.cuda, "device", On)
+    monkeypatch.setattr(pc, "cache_copy", copy)
+    cache = object.__new__(pc.PagedCache)
+    cache.desc, cache.table, cache.pools, cache.device = None, pc.PageTable(6), ["a", "b"], torch.device("cpu")
+    a = cache.new()
+    cache.step([a], [70])
+    b = cache.fork(a)
+    cache.step([b], [3])
+    assert made == [("a", [1], [2]), ("b", [1], [2])] and cache.length(b) == 73
+    cache.free(a)
+    assert cache.compact() == 1 and made[2:] == [("a", [2], [1]), ("b", [2], [1])]
+    assert current == ["another"]
