@@ -175,6 +175,44 @@ def test_attend_lists(dtype):
     check_attend(bt, n, 8, dtype, lists, q)
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("heads,kv,d", [(17, 1, 64), (40, 1, 128), (72, 2, 64), (12, 1, 128)])
+def test_attend_lists_of_large_groups(heads, kv, d, dtype):
+    """Groups that take several items of a few-row call, or several CTAs of an fp32 one, with lists."""
+    bt = Batch([1000, 64, 130], kv, d, seed=71)
+    n = [2, 1, 3]
+    q = queries(6, heads, d, dtype, 72)
+    lists = pc.cache_select(bt.desc(heads, dtype), bt.cache, q, bt.gpu_table(), ints(bt.lens), ints(shares(n)), 4)
+    check_attend(bt, n, heads, dtype, lists, q)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_attend_lists_with_a_page_twice(dtype):
+    """A page listed twice counts twice, the last one, which is not full, too."""
+    bt = Batch([500, 290], 2, 128, seed=73)
+    idx = ints([[[3, 7, 3, 0, 7], [1, -1, -1, -1, -1]], [[4, 4, 2, 2, 2], [0, 4, 0, 9, 9]]])
+    check_attend(bt, [1, 1], 4, dtype, (idx, ints([[5, 1], [5, 3]])), seed=74)
+
+
+@pytest.mark.parametrize("heads,kv", [(12, 1), (40, 1), (18, 2)])
+def test_attend_fp32_large_groups(heads, kv):
+    check_attend(Batch([200, 90, 1], kv, 128), [1, 1, 1], heads, FP32)
+    check_attend(Batch([2500, 90, 1], kv, 64), [2, 1, 1], heads, FP32)
+
+
+@pytest.mark.parametrize("heads,kv,d", [(130, 1, 64), (130, 1, 128), (256, 1, 64), (300, 1, 128), (600, 2, 64)])
+def test_attend_groups_of_more_than_a_row_tile(heads, kv, d):
+    """Groups past 128 rows of one token (two row tiles) and past 256 (several items), alone and joined from parts."""
+    check_attend(Batch([200, 90, 1], kv, d, seed=75), [3, 1, 1], heads)
+    check_attend(Batch([3000], kv, d, seed=76), [2], heads)
+
+
+@pytest.mark.parametrize("n", [[0, 40, 0, 0, 1, 0], [0, 0, 0, 0, 0, 100]])
+def test_attend_sequences_without_rows(n):
+    """A padded batch: sequences that have tokens and no rows, in front, between and behind."""
+    check_attend(Batch([300, 500, 0, 64, 70, 900], 2, 128, seed=77), n, 8, T_more=5, seed=78)
+
+
 def test_attend_lists_of_nothing():
     """Empty lists, and lists of labels in any order."""
     bt = Batch([500, 500], 1, 64)
