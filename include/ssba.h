@@ -55,7 +55,8 @@ typedef enum {
                                  row range or list of the paged cache was out of range       */
 } ssba_status;
 
-typedef enum { SSBA_BF16 = 0, SSBA_FP32 = 1 } ssba_dtype;
+/* SSBA_E4M3 is a type of the products of ssba_linear alone. */
+typedef enum { SSBA_BF16 = 0, SSBA_FP32 = 1, SSBA_E4M3 = 2 } ssba_dtype;
 
 /* One SSBA layer's geometry and sparsity rule.
  *   B, heads, head_dim   tensor sizes; head_dim = C of Sec. 2.2 (per head).
@@ -491,6 +492,108 @@ SSBA_API int ssba_test_cache_timeout(const ssba_cache_desc* desc, const ssba_cac
  * keys. No page may be among dst twice, or both among src and dst. */
 SSBA_API int ssba_cache_copy(const ssba_cache_desc* desc, const ssba_cache* cache, const int32_t* src,
                              const int32_t* dst, int32_t n, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * A layer around its attention: the root-mean-square norm, products with weights and what follows them, and
+ * rotary positions with several axes. (The paper's layer has these around Sec. 2.2's attention without naming
+ * their form; the definitions here are the usual ones.)
+ *
+ * Conventions shared by these calls
+ *   Layout     rows are tokens, contiguous, 16-byte aligned; weights are [outputs][inputs].
+ *   Sums       fp32 throughout; a 16-bit output is rounded once, from fp32. Deterministic (no atomics).
+ *   8 bits     e4m3 values with one fp32 scale a row: a value stands for itself times its row's scale.
+ *   Errors     as above; T = 0 is no work and succeeds (a sum over no rows is 0). */
+
+/* The norm in front of a product, with the residual's addition:
+ *   h = round(x + r),  rstd = 1 / sqrt(mean_i h_i^2 + eps),  y_i = h_i rstd w_i       (h is x without r)
+ *   x, r        device, [T][D] of dtype (SSBA_BF16 or SSBA_FP32); r may be NULL.
+ *   w           device, fp32 [D].
+ *   h           device out, [T][D] of dtype; NULL exactly where r is. It may be x or r.
+ *   y           device out: [T][D] of dtype, or e4m3 [T][D] where scale is given: then scale[t] becomes the least power
+ *               of two (at least 2^-126; 1 for a row of zeros) under which no finite value of the row passes 448, and
+ *               y holds e4m3(y / scale), rounded to nearest. y of dtype may be x.
+ *   scale       device out, fp32 [T], or NULL.
+ *   rstd        device out, fp32 [T] (for the backward pass).
+ * D a multiple of 8, at most SSBA_NORM_MAX_WIDTH; eps finite and >= 0. */
+#define SSBA_NORM_MAX_WIDTH 16384
+SSBA_API int ssba_rms_norm(const void* x, const void* r, const float* w, int32_t T, int32_t D, int32_t dtype, float eps,
+                           void* h, void* y, float* scale, float* rstd, void* stream);
+
+/* Its gradient. With xh = h rstd and g = dy w:  dx = rstd (g - xh mean_i(g xh)) + dh,  dw = sum_t dy xh.
+ *   dy, h, dh   device, [T][D] of dtype: the gradient of y, the h (or x) and rstd of the forward call, and the
+ *               gradient that reaches h from elsewhere (NULL: none). dx is the gradient of x and of r alike.
+ *   dx, dw      device out, [T][D] of dtype and fp32 [D]. dx may be dy or dh.
+ *   workspace   device scratch of at least ssba_rms_norm_backward_workspace_bytes, 16-byte aligned; no fill needed.
+ *               The size holds for the current device. */
+SSBA_API size_t ssba_rms_norm_backward_workspace_bytes(int32_t T, int32_t D, int32_t dtype);
+SSBA_API int ssba_rms_norm_backward(const void* dy, const void* h, const float* w, const float* rstd, const void* dh,
+                                    int32_t T, int32_t D, int32_t dtype, void* dx, float* dw, void* workspace,
+                                    size_t ws_bytes, void* stream);
+
+/* relu(z) = max(z, 0) (its slope at 0 is 0), silu(z) = z s(z), gelu(z) = z s(2 sqrt(2/pi) (z + 0.044715 z^3)) (its tanh form), with
+ * s(t) = 1 / (1 + e^-t). */
+typedef enum { SSBA_ACT_NONE = 0, SSBA_ACT_RELU = 1, SSBA_ACT_GELU = 2, SSBA_ACT_SILU = 3 } ssba_act;
+
+/* T rows of K inputs and N outputs. dtype: SSBA_BF16, or SSBA_E4M3 (x, W and their scales; the outputs are bf16).
+ * gated: W holds the N gate rows, then the N up rows, and act is not SSBA_ACT_NONE.
+ * N and K are multiples of 8 (K of 16 for SSBA_E4M3), at most SSBA_LINEAR_MAX_WIDTH; T at most SSBA_CACHE_MAX_ROWS. */
+#define SSBA_LINEAR_MAX_WIDTH (1 << 17)
+typedef struct {
+    int32_t T, N, K;
+    int32_t dtype, act, gated;
+} ssba_linear_desc;
+
+/* One product with what follows it:
+ *   plain:  z = (x W^T) x_scale w_scale + bias,  y = act(z) + r
+ *   gated:  g, u = (x Wg^T, x Wu^T) x_scale w_scale,  y = act(g) u
+ *   x, W        device, [T][K] and [N][K] ([2 N][K] gated) of desc->dtype.
+ *   x_scale, w_scale  device fp32 [T] and [N] ([2 N]): both for SSBA_E4M3, else NULL.
+ *   bias        device fp32 [N], or NULL. NULL when gated.
+ *   r           device bf16 [T][N], or NULL. NULL when gated. It may be y.
+ *   y           device out, bf16 [T][N].
+ *   z           device out, bf16 [T][N] ([T][2 N]: g, then u), or NULL: kept for the backward pass. */
+SSBA_API int ssba_linear(const ssba_linear_desc* desc, const void* x, const void* W, const float* x_scale,
+                         const float* w_scale, const float* bias, const void* r, void* y, void* z, void* stream);
+
+/* Its gradients, SSBA_BF16 alone. dz = dy act'(z) (gated: dg = dy u act'(g), du = dy act(g)), rounded to bf16, then
+ * dx = dz W and dW = dz^T x; db = sum_t dz before that rounding.
+ *   dy          device, bf16 [T][N]: the gradient of y (and, as it is, of r).
+ *   x, W        those of the forward call. W may be NULL without dx, x without dW.
+ *   z           the z of the forward call; NULL with SSBA_ACT_NONE.
+ *   dx, dW, db  device out, bf16 [T][K], bf16 [N][K] ([2 N][K]), fp32 [N]; each may be NULL (db is, when gated).
+ *   workspace   device scratch of at least ssba_linear_backward_workspace_bytes(desc), 16-byte aligned (may be 0 bytes
+ *               and NULL only if that is 0); no fill needed. The size holds for the current device. */
+SSBA_API size_t ssba_linear_backward_workspace_bytes(const ssba_linear_desc* desc);
+SSBA_API int ssba_linear_backward(const ssba_linear_desc* desc, const void* dy, const void* x, const void* W,
+                                  const void* z, void* dx, void* dW, float* db, void* workspace, size_t ws_bytes,
+                                  void* stream);
+
+/* Rotary positions with several axes. The first 2P dimensions of a head are P = sum(sections) pairs, the first
+ * sections[0] of axis 0, the next of axis 1 and so on; pair j of axis a turns by pos[a] theta_j:
+ *   (u, v) -> (u cos - v sin, u sin + v cos), with inverse (which is the gradient) by the negative angle.
+ *   shared = 0  theta of an axis's i-th pair is base^(-i / sections[a]): every axis has the whole range of rates;
+ *   shared = 1  theta of pair j is base^(-j / P): the axes share one range.
+ *   layout      SSBA_ROPE_PAIRS: pair j is dimensions 2j, 2j + 1; SSBA_ROPE_HALVES: j, j + P.
+ * Dimensions from 2P on are copied. Angles are exact to 2^-32 of a turn, beside theta's own rounding to 53 bits, at any position. */
+#define SSBA_ROPE_MAX_AXES 4
+#define SSBA_ROPE_MAX_HEAD_DIM 256
+enum { SSBA_ROPE_PAIRS = 0, SSBA_ROPE_HALVES = 1 };
+typedef struct {
+    int32_t B, T, heads, head_dim;
+    int32_t axes, sections[SSBA_ROPE_MAX_AXES];
+    int32_t layout, shared, inverse;
+    int32_t dtype; /* SSBA_BF16 or SSBA_FP32 */
+    double base;   /* finite, > 1 */
+} ssba_rope_desc;
+
+/*   x, out      device; head h of token t of sequence b starts at b s[0] + t s[1] + h s[2] elements (x_stride, out_stride,
+ *               host arrays of three), its dimensions side by side. Aligned to their element; the more of base, strides,
+ *               head_dim (and, in halves, P) is in multiples of 16 bytes, the wider the accesses. Strides >= 0. out may be
+ *               x with the same strides; else they may not overlap, and no two heads of out.
+ *   pos         device, int32, any sign: axis a of token t of sequence b at b pos_batch + t axes + a (pos_batch 0:
+ *               the same positions for all sequences). */
+SSBA_API int ssba_rope_axes(const ssba_rope_desc* desc, const void* x, const int64_t* x_stride, const int32_t* pos,
+                            int64_t pos_batch, void* out, const int64_t* out_stride, void* stream);
 
 /* Reads and clears the device status word of the current device (SSBA_OK,
  * SSBA_ERR_TIMEOUT or SSBA_ERR_CHECK; of both since the last read, the timeout, whose

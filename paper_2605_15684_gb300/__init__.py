@@ -16,6 +16,10 @@ from .cache import (  # noqa: F401
     Cache, CacheDesc, CacheStep, PagedCache, PageTable, cache_alloc, cache_append, cache_attend,
     cache_attend_workspace_bytes, cache_copy, cache_select,
 )
+from .layer import (  # noqa: F401
+    gated_linear, gated_linear_backward, linear, linear_backward, linear_backward_workspace_bytes, rms_norm,
+    rms_norm_backward, rms_norm_backward_workspace_bytes, rope_axes,
+)
 
 __all__ = [
     "SsbaDesc", "SsbaError", "BoundLayer", "BoundSelectLayer", "backward", "backward_workspace_bytes",
@@ -25,4 +29,6 @@ __all__ = [
     "pool_blocks", "qkv_rope_pool", "realized_sparsity", "select_mask",
     "Cache", "CacheDesc", "CacheStep", "PagedCache", "PageTable", "cache_alloc", "cache_append", "cache_attend", "cache_attend_workspace_bytes",
     "cache_copy", "cache_select",
+    "gated_linear", "gated_linear_backward", "linear", "linear_backward", "linear_backward_workspace_bytes", "rms_norm",
+    "rms_norm_backward", "rms_norm_backward_workspace_bytes", "rope_axes",
 ]

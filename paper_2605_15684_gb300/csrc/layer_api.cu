@@ -1,0 +1,260 @@
+// layer_api.cu -- the entry points of a layer around its attention (include/ssba.h): argument validation on the host and
+// kernel launches on the caller's stream.
+#include <cmath>
+
+#include "layer.cuh"
+
+namespace ssba {
+namespace layer {
+namespace {
+
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+int invalid(const char* who, const char* what)
+{
+    set_error("%s: %s", who, what);
+    return SSBA_ERR_INVALID;
+}
+
+int check_norm(const char* who, int32_t T, int32_t D, int32_t dtype)
+{
+    if (T < 0 || D <= 0) {
+        set_error("%s: T=%d must be >= 0 and D=%d positive", who, T, D);
+        return SSBA_ERR_INVALID;
+    }
+    if (dtype != SSBA_BF16 && dtype != SSBA_FP32) {
+        set_error("%s: dtype %d: SSBA_BF16 and SSBA_FP32 are supported", who, dtype);
+        return SSBA_ERR_INVALID;
+    }
+    if (D % 8 || D > SSBA_NORM_MAX_WIDTH) {
+        set_error("%s: D=%d must be a multiple of 8 and at most %d", who, D, SSBA_NORM_MAX_WIDTH);
+        return SSBA_ERR_UNSUPPORTED;
+    }
+    return SSBA_OK;
+}
+
+int check_linear(const char* who, const ssba_linear_desc* d)
+{
+    if (!d) return invalid(who, "null descriptor");
+    if (d->T < 0 || d->N <= 0 || d->K <= 0) {
+        set_error("%s: T=%d must be >= 0, N=%d and K=%d positive", who, d->T, d->N, d->K);
+        return SSBA_ERR_INVALID;
+    }
+    if (d->dtype != SSBA_BF16 && d->dtype != SSBA_E4M3) {
+        set_error("%s: dtype %d: SSBA_BF16 and SSBA_E4M3 are supported", who, d->dtype);
+        return SSBA_ERR_INVALID;
+    }
+    if (d->act < SSBA_ACT_NONE || d->act > SSBA_ACT_SILU || (d->gated && d->act == SSBA_ACT_NONE)) {
+        set_error("%s: unknown activation %d, or none of a gated product", who, d->act);
+        return SSBA_ERR_INVALID;
+    }
+    if (d->N % 8 || d->K % (d->dtype == SSBA_E4M3 ? 16 : 8) || d->N > SSBA_LINEAR_MAX_WIDTH || d->K > SSBA_LINEAR_MAX_WIDTH ||
+        d->T > SSBA_CACHE_MAX_ROWS) {
+        set_error("%s: N=%d and K=%d must be multiples of 8 (K of 16 in e4m3) and at most %d, T=%d at most %d", who, d->N, d->K,
+                  SSBA_LINEAR_MAX_WIDTH, d->T, SSBA_CACHE_MAX_ROWS);
+        return SSBA_ERR_UNSUPPORTED;
+    }
+    return SSBA_OK;
+}
+
+}  // namespace
+}  // namespace layer
+}  // namespace ssba
+
+using namespace ssba;
+using namespace ssba::layer;
+
+extern "C" {
+
+int ssba_rms_norm(const void* x, const void* r, const float* w, int32_t T, int32_t D, int32_t dtype, float eps, void* h,
+                  void* y, float* scale, float* rstd, void* stream)
+{
+    static const char who[] = "ssba_rms_norm";
+    SSBA_NVTX_RANGE(who);
+    const int rc = check_norm(who, T, D, dtype);
+    if (rc != SSBA_OK) return rc;
+    if (!(eps >= 0.f) || std::isinf(eps)) return invalid(who, "eps must be finite and >= 0");
+    if ((r != nullptr) != (h != nullptr)) return invalid(who, "r and h come together");
+    if (T == 0) return SSBA_OK;
+    if (!x || !w || !y || !rstd) return invalid(who, "x, w, y and rstd must be non-null");
+    if (!aligned(x, 16) || !aligned(r, 16) || !aligned(w, 16) || !aligned(h, 16) || !aligned(y, 16) || !aligned(scale, 4) ||
+        !aligned(rstd, 4))
+        return invalid(who, "x, r, w, h and y must be 16-byte aligned, scale and rstd 4-byte");
+    return launch_rms_norm(x, r, w, T, D, dtype, eps, h, y, scale != nullptr, scale, rstd, static_cast<cudaStream_t>(stream));
+}
+
+size_t ssba_rms_norm_backward_workspace_bytes(int32_t T, int32_t D, int32_t dtype)
+{
+    if (check_norm("ssba_rms_norm_backward_workspace_bytes", T, D, dtype) != SSBA_OK) return 0;
+    return round256(sizeof(float) * D * (size_t)rms_norm_backward_parts(T, D, dtype));
+}
+
+int ssba_rms_norm_backward(const void* dy, const void* h, const float* w, const float* rstd, const void* dh, int32_t T,
+                           int32_t D, int32_t dtype, void* dx, float* dw, void* workspace, size_t ws_bytes, void* stream)
+{
+    static const char who[] = "ssba_rms_norm_backward";
+    SSBA_NVTX_RANGE(who);
+    const int rc = check_norm(who, T, D, dtype);
+    if (rc != SSBA_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (!dw || !aligned(dw, 4)) return invalid(who, "dw must be non-null and 4-byte aligned");
+    if (T == 0) {
+        const cudaError_t e = cudaMemsetAsync(dw, 0, sizeof(float) * D, st);
+        if (e == cudaSuccess) return SSBA_OK;
+        cudaGetLastError();
+        set_error("%s: %s", who, cudaGetErrorString(e));
+        return SSBA_ERR_CUDA;
+    }
+    if (!dy || !h || !w || !rstd || !dx) return invalid(who, "dy, h, w, rstd and dx must be non-null");
+    if (!aligned(dy, 16) || !aligned(h, 16) || !aligned(w, 16) || !aligned(dh, 16) || !aligned(dx, 16) || !aligned(rstd, 4))
+        return invalid(who, "dy, h, w, dh and dx must be 16-byte aligned, rstd 4-byte");
+    const size_t need = ssba_rms_norm_backward_workspace_bytes(T, D, dtype);
+    if (!workspace || ws_bytes < need || !aligned(workspace, 16)) {
+        set_error("%s: workspace of %zu bytes (16-byte aligned) required, got %zu", who, need, ws_bytes);
+        return SSBA_ERR_WORKSPACE;
+    }
+    return launch_rms_norm_backward(dy, h, w, rstd, dh, T, D, dtype, dx, dw, static_cast<float*>(workspace), st);
+}
+
+int ssba_linear(const ssba_linear_desc* desc, const void* x, const void* W, const float* x_scale, const float* w_scale,
+                const float* bias, const void* r, void* y, void* z, void* stream)
+{
+    static const char who[] = "ssba_linear";
+    SSBA_NVTX_RANGE(who);
+    const int rc = check_linear(who, desc);
+    if (rc != SSBA_OK) return rc;
+    const bool f8 = desc->dtype == SSBA_E4M3;
+    if ((x_scale != nullptr) != f8 || (w_scale != nullptr) != f8)
+        return invalid(who, "x_scale and w_scale are given for e4m3 and for nothing else");
+    if (desc->gated && (bias || r)) return invalid(who, "a gated product has no bias and no residual");
+    if (desc->T == 0) return SSBA_OK;
+    if (!x || !W || !y) return invalid(who, "x, W and y must be non-null");
+    if (!aligned(x, 16) || !aligned(W, 16) || !aligned(w_scale, 16) || !aligned(bias, 16) || !aligned(r, 16) ||
+        !aligned(y, 16) || !aligned(z, 16) || !aligned(x_scale, 4))
+        return invalid(who, "x, W, w_scale, bias, r, y and z must be 16-byte aligned, x_scale 4-byte");
+    const Product p{x, W, y, z, r, x_scale, w_scale, bias, desc->T, desc->N, desc->K, desc->act, f8, false, false, desc->gated != 0};
+    return launch_product(p, who, static_cast<cudaStream_t>(stream));
+}
+
+size_t ssba_linear_backward_workspace_bytes(const ssba_linear_desc* desc)
+{
+    if (check_linear("ssba_linear_backward_workspace_bytes", desc) != SSBA_OK) return 0;
+    const size_t dz = desc->act == SSBA_ACT_NONE ? 0 : round256((size_t)desc->T * desc->N * (desc->gated ? 4 : 2));
+    const size_t part = desc->gated || !desc->T ? 0 : round256(sizeof(float) * desc->N * (size_t)act_backward_parts(desc->T, desc->N));
+    return dz + part;
+}
+
+int ssba_linear_backward(const ssba_linear_desc* desc, const void* dy, const void* x, const void* W, const void* z, void* dx,
+                         void* dW, float* db, void* workspace, size_t ws_bytes, void* stream)
+{
+    static const char who[] = "ssba_linear_backward";
+    SSBA_NVTX_RANGE(who);
+    int rc = check_linear(who, desc);
+    if (rc != SSBA_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool gated = desc->gated != 0, act = desc->act != SSBA_ACT_NONE;
+    const int T = desc->T, N = desc->N, K = desc->K, rows = gated ? 2 * N : N;
+    if (desc->dtype != SSBA_BF16) return invalid(who, "the gradients are those of bf16 products");
+    if (gated && db) return invalid(who, "a gated product has no bias");
+    if ((dx && !W) || (dW && !x && T)) return invalid(who, "dx needs W, and dW needs x");
+    if (!aligned(dy, 16) || !aligned(x, 16) || !aligned(W, 16) || !aligned(z, 16) || !aligned(dx, 16) || !aligned(dW, 16) || !aligned(db, 4))
+        return invalid(who, "dy, x, W, z, dx and dW must be 16-byte aligned, db 4-byte");
+    if (T == 0) {
+        cudaError_t e = dW ? cudaMemsetAsync(dW, 0, (size_t)rows * K * 2, st) : cudaSuccess;
+        if (e == cudaSuccess && db) e = cudaMemsetAsync(db, 0, sizeof(float) * N, st);
+        if (e == cudaSuccess) return SSBA_OK;
+        cudaGetLastError();
+        set_error("%s: %s", who, cudaGetErrorString(e));
+        return SSBA_ERR_CUDA;
+    }
+    if (!dy || (act && !z)) return invalid(who, "dy, and z with an activation, must be non-null");
+    const size_t need = ssba_linear_backward_workspace_bytes(desc);
+    if (need && (!workspace || ws_bytes < need || !aligned(workspace, 16))) {
+        set_error("%s: workspace of %zu bytes (16-byte aligned) required, got %zu", who, need, ws_bytes);
+        return SSBA_ERR_WORKSPACE;
+    }
+    const void* dz = dy;
+    if (act || db) {
+        const size_t dzb = act ? round256((size_t)T * rows * 2) : 0;
+        if (act) dz = workspace;
+        rc = launch_act_backward(dy, z, act ? workspace : nullptr, db, db ? reinterpret_cast<float*>(static_cast<char*>(workspace) + dzb) : nullptr,
+                                 T, N, desc->act, gated, who, st);
+        if (rc != SSBA_OK) return rc;
+    }
+    if (dx) {
+        Product p{};
+        p.a = dz;
+        p.b = W;
+        p.y = dx;
+        p.M = T;
+        p.N = K;
+        p.K = rows;
+        p.b_mn = true;
+        rc = launch_product(p, who, st);
+        if (rc != SSBA_OK) return rc;
+    }
+    if (dW) {
+        Product p{};
+        p.a = dz;
+        p.b = x;
+        p.y = dW;
+        p.M = rows;
+        p.N = K;
+        p.K = T;
+        p.a_mn = p.b_mn = true;
+        rc = launch_product(p, who, st);
+    }
+    return rc;
+}
+
+int ssba_rope_axes(const ssba_rope_desc* desc, const void* x, const int64_t* x_stride, const int32_t* pos, int64_t pos_batch,
+                   void* out, const int64_t* out_stride, void* stream)
+{
+    static const char who[] = "ssba_rope_axes";
+    SSBA_NVTX_RANGE(who);
+    if (!desc) return invalid(who, "null descriptor");
+    const ssba_rope_desc& d = *desc;
+    if (d.B < 0 || d.T < 0 || d.heads <= 0 || d.head_dim <= 0) {
+        set_error("%s: B=%d and T=%d must be >= 0, heads=%d and head_dim=%d positive", who, d.B, d.T, d.heads, d.head_dim);
+        return SSBA_ERR_INVALID;
+    }
+    if (d.dtype != SSBA_BF16 && d.dtype != SSBA_FP32) return invalid(who, "dtype must be SSBA_BF16 or SSBA_FP32");
+    if (d.axes < 1 || d.axes > SSBA_ROPE_MAX_AXES) {
+        set_error("%s: axes=%d must be 1..%d", who, d.axes, SSBA_ROPE_MAX_AXES);
+        return SSBA_ERR_INVALID;
+    }
+    long long P = 0;
+    for (int a = 0; a < d.axes; ++a) {
+        if (d.sections[a] <= 0) return invalid(who, "every axis has at least one pair");
+        P += d.sections[a];
+    }
+    if (2 * P > d.head_dim) {
+        set_error("%s: the sections' %lld pairs do not fit head_dim=%d", who, P, d.head_dim);
+        return SSBA_ERR_INVALID;
+    }
+    if (d.layout != SSBA_ROPE_PAIRS && d.layout != SSBA_ROPE_HALVES) return invalid(who, "unknown layout");
+    if (!(d.base > 1.0) || std::isinf(d.base)) return invalid(who, "base must be finite and > 1");
+    if (d.head_dim > SSBA_ROPE_MAX_HEAD_DIM || d.head_dim % 2 || (long long)d.B * d.T > (1ll << 30)) {
+        set_error("%s: head_dim=%d must be even and at most %d, and B * T at most 2^30", who, d.head_dim, SSBA_ROPE_MAX_HEAD_DIM);
+        return SSBA_ERR_UNSUPPORTED;
+    }
+    if (!x_stride || !out_stride) return invalid(who, "the strides must be non-null");
+    const int64_t es = d.dtype == SSBA_BF16 ? 2 : 4;
+    for (int i = 0; i < 3; ++i)
+        if (x_stride[i] < 0 || out_stride[i] < 0 || x_stride[i] > (1ll << 42) || out_stride[i] > (1ll << 42))
+            return invalid(who, "strides must be >= 0 and at most 2^42 elements");
+    if (pos_batch < 0) return invalid(who, "pos_batch must be >= 0");
+    if (d.B == 0 || d.T == 0) return SSBA_OK;
+    if (!x || !pos || !out) return invalid(who, "x, pos and out must be non-null");
+    // adjacent pairs are read together
+    const int64_t unit = d.layout == SSBA_ROPE_PAIRS ? 2 * es : es;
+    bool fits = aligned(x, unit) && aligned(out, unit) && aligned(pos, 4);
+    if (d.layout == SSBA_ROPE_PAIRS)
+        for (int i = 0; i < 3; ++i) fits = fits && x_stride[i] % 2 == 0 && out_stride[i] % 2 == 0;
+    if (!fits) return invalid(who, "x and out must be aligned to an element (adjacent pairs: to a pair, strides too), pos to 4 bytes");
+    return launch_rope(d, x, x_stride, pos, pos_batch, out, out_stride, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

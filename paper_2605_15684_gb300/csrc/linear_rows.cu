@@ -1,0 +1,332 @@
+// linear_rows.cu -- the products of linear_pair.cu where rows are few: the weights are the tensor cores' rows.
+//
+// With few tokens a product is the reading of its weights, and the tiles of many tokens would leave most SMs without
+// work. So the weights take the 128 rows of a tile, kNT tokens its columns, and K is split over the CTAs of a cluster:
+//   D[128 weight rows][kNT] = sum over this CTA's share of K,   then   y[t][n] = act(sum of the CTAs' D ...) + r
+// Gated, a tile is 64 gate rows over the 64 matching up rows. For dx = dz W the weights come along their rows ("mn").
+// The partial tiles stay in shared memory (fp32, where the operands were) and each CTA of the cluster adds up and
+// finishes a share of the outputs through distributed shared memory: no workspace, no atomics, one order.
+// Bound by HBM (the weights once; tokens come from L2): about 100 KB of operands are under way in each of two CTAs an SM.
+// 192 threads: warp 0 TMA, warp 1 tcgen05.mma M = 128, N = kNT, warps 2-5 take D out of TMEM, and all finish.
+// Every wait is bounded; a timeout is written to the device status word.
+#include <algorithm>
+#include <cstddef>
+#include <cstring>
+
+#include "layer.cuh"
+
+namespace ssba {
+namespace layer {
+namespace {
+
+using namespace ptx;
+
+constexpr int kThreads = 192;
+constexpr uint32_t kABytes = 128 * 128;
+constexpr int kPitch = 132;  // floats of a column of D: 128 and a shift of banks
+constexpr int kMaxSplit = 8;
+
+template <int kNT>
+struct RowsCfg {
+    static constexpr uint32_t kBBytes = kNT * 128;
+    static constexpr int kStages = kNT <= 16 ? 6 : kNT == 32 ? 5 : kNT == 64 ? 4 : 3;
+};
+
+template <int kNT>
+struct __align__(1024) RowsSmem {
+    using C = RowsCfg<kNT>;
+    union {
+        struct {
+            uint8_t a[C::kStages][kABytes];
+            uint8_t b[C::kStages][C::kBBytes];
+        };
+        float part[kNT][kPitch];  // [token][weight row], when the products are done
+    };
+    uint64_t full[C::kStages], empty[C::kStages];
+    uint64_t done;
+    uint32_t tmem_base;
+    int abort_flag;
+};
+
+struct RowsMaps {
+    CUtensorMap w, x;
+};
+
+struct RowsParams {
+    __nv_bfloat16 *y, *z;
+    const __nv_bfloat16* r;
+    const float *xs, *ws, *bias;
+    int T, N;  // tokens; outputs a token (gated: of either half)
+    int ksteps, split, act;
+    int* status;
+    uint64_t budget_ns;
+};
+
+template <int kAct>
+__device__ __forceinline__ float4 act4(float4 v)
+{
+    return make_float4(act_fn<kAct>(v.x), act_fn<kAct>(v.y), act_fn<kAct>(v.z), act_fn<kAct>(v.w));
+}
+
+__device__ __forceinline__ float4 activate4(float4 v, int act)
+{
+    if (act == SSBA_ACT_SILU) return act4<SSBA_ACT_SILU>(v);
+    if (act == SSBA_ACT_GELU) return act4<SSBA_ACT_GELU>(v);
+    if (act == SSBA_ACT_RELU) return act4<SSBA_ACT_RELU>(v);
+    return v;
+}
+
+__device__ __forceinline__ void put4(__nv_bfloat16* to, float4 v)
+{
+    *reinterpret_cast<uint2*>(to) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
+}
+
+// Four rows of D of a token: the cluster's partial sums in the order of its CTAs.
+__device__ __forceinline__ float4 joined(uint32_t at, int split)
+{
+    float4 s = ld_cluster4(at_rank(at, 0));
+    for (int c = 1; c < split; ++c) {
+        const float4 v = ld_cluster4(at_rank(at, c));
+        s.x += v.x;
+        s.y += v.y;
+        s.z += v.z;
+        s.w += v.w;
+    }
+    return s;
+}
+
+__device__ __forceinline__ float4 scaled(float4 v, const RowsParams& p, int t, const float* ws)
+{
+    if (!p.xs) return v;
+    const float x = p.xs[t];
+    const float4 w = __ldg(reinterpret_cast<const float4*>(ws));
+    return make_float4(v.x * (x * w.x), v.y * (x * w.y), v.z * (x * w.z), v.w * (x * w.w));
+}
+
+template <int kNT, bool kF8, bool kWmn, bool kGated>
+__global__ void __launch_bounds__(kThreads) ssba_product_rows_kernel(const __grid_constant__ RowsMaps maps, const RowsParams p)
+{
+    using C = RowsCfg<kNT>;
+    constexpr int kStages = C::kStages, kBK = kF8 ? 128 : 64;
+    constexpr int kOut = kGated ? 64 : 128;  // outputs a token of a tile
+    constexpr uint32_t kIdesc = idesc_of(kF8, 128, kNT, kWmn, false);
+    constexpr uint32_t kTmem = kNT < 32 ? 32 : kNT;
+    extern __shared__ uint8_t smem_raw[];
+    RowsSmem<kNT>& sm = *reinterpret_cast<RowsSmem<kNT>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                                          ~static_cast<uintptr_t>(1023));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)cluster_rank();
+    const int n0 = (int)(blockIdx.x / p.split) * kOut, t0 = (int)blockIdx.y * kNT;
+    const int k0 = (int)((long long)p.ksteps * rank / p.split), k1 = (int)((long long)p.ksteps * (rank + 1) / p.split);
+    volatile int* abortf = &sm.abort_flag;
+
+    if (threadIdx.x == 0) {
+        sm.abort_flag = 0;
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(smem_u32(&sm.full[s]), 1);
+            mbar_init(smem_u32(&sm.empty[s]), 1);
+        }
+        mbar_init(smem_u32(&sm.done), 1);
+        fence_mbar_init();
+        tma_prefetch_desc(&maps.w);
+        tma_prefetch_desc(&maps.x);
+    }
+    if (warp == 1) {
+        tmem_alloc(smem_u32(&sm.tmem_base), kTmem);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tbase = sm.tmem_base;
+    bool dead = false;
+    grid_dep_wait();
+    grid_dep_launch();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int g = 0;
+            for (int k = k0; k < k1; ++k, ++g) {
+                const int s = g % kStages;
+                if (!mbar_wait(smem_u32(&sm.empty[s]), ((g / kStages) & 1) ^ 1, abortf, p.budget_ns)) {
+                    dead = true;
+                    break;
+                }
+                const uint32_t bar = smem_u32(&sm.full[s]), a = smem_u32(&sm.a[s][0]);
+                mbar_arrive_expect_tx(bar, kABytes + C::kBBytes);
+                if constexpr (kWmn) {
+                    tma_load_3d(a, &maps.w, bar, n0, k * kBK, 0);
+                    tma_load_3d(a + 8192, &maps.w, bar, n0 + 64, k * kBK, 0);
+                } else if constexpr (kGated) {
+                    tma_load_3d(a, &maps.w, bar, k * kBK, n0, 0);
+                    tma_load_3d(a + 8192, &maps.w, bar, k * kBK, n0, 1);
+                } else {
+                    tma_load_3d(a, &maps.w, bar, k * kBK, n0, 0);
+                }
+                tma_load_3d(smem_u32(&sm.b[s][0]), &maps.x, bar, k * kBK, t0, 0);
+            }
+            if (dead) {
+                for (int x = g > kStages ? g - kStages : 0; x < g; ++x)
+                    wait_raw(smem_u32(&sm.full[x % kStages]), (x / kStages) & 1, p.budget_ns);
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (elect_one_sync()) {
+            const uint32_t a0 = smem_u32(&sm.a[0][0]), b0 = smem_u32(&sm.b[0][0]);
+            int g = 0;
+            for (int k = k0; k < k1; ++k, ++g) {
+                const int s = g % kStages;
+                if (!mbar_wait(smem_u32(&sm.full[s]), (g / kStages) & 1, abortf, p.budget_ns)) {
+                    dead = true;
+                    break;
+                }
+                tc_fence_after();
+                const uint64_t ad = sdesc_sw128(a0 + s * kABytes, kWmn ? 8192 : 16, 1024);
+                const uint64_t bd = sdesc_sw128(b0 + s * C::kBBytes, 16, 1024);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    mma<kF8, false>(tbase, ad + (uint64_t)(i * (kWmn ? 128 : 2)), bd + (uint64_t)(i * 2), kIdesc, (g | i) != 0 ? 1u : 0u);
+                mma_commit(smem_u32(&sm.empty[s]));
+            }
+            mma_commit(smem_u32(&sm.done));  // given up or not: nothing of this CTA's products is under way after it
+        }
+        __syncwarp();
+    }
+    // all: the products are done, so the operands' memory is free for D
+    {
+        const bool ok = wait_raw(smem_u32(&sm.done), 0, 2 * p.budget_ns);
+        tc_fence_after();
+        if (!__all_sync(0xffffffffu, ok)) dead = true;
+    }
+    if (warp >= 2) {
+        const int quad = warp & 3;
+        const uint32_t at = tbase + ((uint32_t)(32 * quad) << 16);
+#pragma unroll
+        for (int c = 0; c < kNT; c += 16) {
+            uint32_t v[16];
+            tmem_ld_32x32b_x16(at + c, v);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sm.part[c + i][32 * quad + lane] = __uint_as_float(v[i]);
+        }
+        tc_fence_before();
+    }
+    __syncwarp();
+    cluster_sync_all();
+
+    // outputs of the tile in fours, those of a token in a row, dealt out over the cluster's threads
+    const int tokens = min(kNT, p.T - t0);
+    for (int e = rank * kThreads + (int)threadIdx.x; e < tokens * (kOut / 4); e += p.split * kThreads) {
+        const int t = e / (kOut / 4), i = (e - t * (kOut / 4)) * 4, n = n0 + i;
+        if (n >= p.N) continue;
+        const size_t o = (size_t)(t0 + t) * p.N + n;
+        const uint32_t at = smem_u32(&sm.part[t][i]);
+        float4 v = joined(at, p.split);
+        if constexpr (kGated) {
+            float4 u = joined(at + 64 * 4, p.split);
+            v = scaled(v, p, t0 + t, p.ws + n);
+            u = scaled(u, p, t0 + t, p.ws + p.N + n);
+            if (p.z) {
+                put4(p.z + (size_t)(t0 + t) * 2 * p.N + n, v);
+                put4(p.z + (size_t)(t0 + t) * 2 * p.N + p.N + n, u);
+            }
+            v = activate4(v, p.act);
+            v = make_float4(v.x * u.x, v.y * u.y, v.z * u.z, v.w * u.w);
+        } else {
+            v = scaled(v, p, t0 + t, p.ws + n);
+            if (p.bias) {
+                const float4 w = __ldg(reinterpret_cast<const float4*>(p.bias + n));
+                v = make_float4(v.x + w.x, v.y + w.y, v.z + w.z, v.w + w.w);
+            }
+            if (p.z) put4(p.z + o, v);
+            v = activate4(v, p.act);
+            if (p.r) {
+                const uint2 w = *reinterpret_cast<const uint2*>(p.r + o);
+                const float2 a = unpack2(w.x), b = unpack2(w.y);
+                v = make_float4(v.x + a.x, v.y + a.y, v.z + b.x, v.w + b.y);
+            }
+        }
+        put4(p.y + o, v);
+    }
+    if (dead) atomicExch(p.status, SSBA_ERR_TIMEOUT);
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();  // the others have read this CTA's part
+    tc_fence_after();
+    if (warp == 1) tmem_dealloc(tbase, kTmem);
+}
+
+template <int kNT, bool kF8, bool kWmn, bool kGated>
+int launch_as(const Product& q, const char* who, cudaStream_t st)
+{
+    constexpr int kBK = kF8 ? 128 : 64, kOut = kGated ? 64 : 128;
+    auto kernel = ssba_product_rows_kernel<kNT, kF8, kWmn, kGated>;
+    const size_t smem = sizeof(RowsSmem<kNT>) + 1024;
+    static PerDeviceOnce attr;
+    attr.run([=] { cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
+    const int e = kF8 ? 1 : 2;
+    const uint64_t T = q.M, N = q.N, K = q.K;
+    RowsMaps maps;
+    memset(&maps, 0, sizeof(maps));
+    bool ok = kWmn ? encode_map(&maps.w, q.b, kF8, N, K, 1, N * e, N * K * e, 64, 64)
+                   : encode_map(&maps.w, q.b, kF8, K, N, kGated ? 2 : 1, K * e, N * K * e, kBK, kOut);
+    ok = ok && encode_map(&maps.x, q.a, kF8, K, T, 1, K * e, T * K * e, kBK, kNT);
+    if (!ok) {
+        set_error("%s: cuTensorMapEncodeTiled failed", who);
+        return SSBA_ERR_CUDA;
+    }
+    RowsParams p = {};
+    p.y = static_cast<__nv_bfloat16*>(q.y);
+    p.z = static_cast<__nv_bfloat16*>(q.z);
+    p.r = static_cast<const __nv_bfloat16*>(q.r);
+    p.xs = q.xs;
+    p.ws = q.ws;
+    p.bias = q.bias;
+    p.T = q.M;
+    p.N = q.N;
+    p.ksteps = (q.K + kBK - 1) / kBK;
+    p.act = q.act;
+    p.budget_ns = kWaitBudgetNs;
+    p.status = device_status_word();
+    if (!p.status) {
+        set_error("%s: could not resolve the device status word", who);
+        return SSBA_ERR_CUDA;
+    }
+    const long long tiles = (q.N + kOut - 1) / kOut, cols = (q.M + kNT - 1) / kNT;
+    // K over as many CTAs as two an SM hold, with two steps each at least
+    int split = 1;
+    while (split < kMaxSplit && tiles * cols * split * 2 <= 2ll * device_sm_count() && p.ksteps >= split * 4) split *= 2;
+    p.split = split;
+    const cudaError_t err = launch_early(kernel, dim3((unsigned)(tiles * split), (unsigned)cols), kThreads, smem, st, split, maps, p);
+    if (err == cudaSuccess) return SSBA_OK;
+    set_error("%s: ssba_product_rows_kernel launch: %s", who, cudaGetErrorString(err));
+    return SSBA_ERR_CUDA;
+}
+
+template <int kNT>
+int launch_tokens(const Product& q, const char* who, cudaStream_t st)
+{
+    if (q.b_mn) return launch_as<kNT, false, true, false>(q, who, st);
+    if (q.gated) return q.f8 ? launch_as<kNT, true, false, true>(q, who, st) : launch_as<kNT, false, false, true>(q, who, st);
+    return q.f8 ? launch_as<kNT, true, false, false>(q, who, st) : launch_as<kNT, false, false, false>(q, who, st);
+}
+
+}  // namespace
+
+int launch_product_rows(const Product& q, const char* who, cudaStream_t st)
+{
+    if (q.M <= 16) return launch_tokens<16>(q, who, st);
+    if (q.M <= 32) return launch_tokens<32>(q, who, st);
+    if (q.M <= 64) return launch_tokens<64>(q, who, st);
+    return launch_tokens<128>(q, who, st);
+}
+
+int launch_product(const Product& q, const char* who, cudaStream_t st)
+{
+    if (q.a_mn) return launch_product_pair(q, who, st);
+    return q.M <= 256 ? launch_product_rows(q, who, st) : launch_product_pair(q, who, st);
+}
+
+}  // namespace layer
+}  // namespace ssba

@@ -1,0 +1,419 @@
+// norm.cu -- the root-mean-square norm in front of a layer's products, with the residual's addition, and backward.
+//
+//   h = round(x + r)                    (x itself without a residual)
+//   rstd = 1 / sqrt(mean_i h_i^2 + eps),   y_i = h_i rstd w_i
+//   8-bit rows: s = the least power of two with max_i |y_i| / s <= 448, q_i = e4m3(y_i / s)
+//   backward, with xh = h rstd and g = dy w:   dx = rstd (g - xh mean(g xh)) (+ dh),   dw = sum_t dy xh
+//
+// y is the norm of the rounded h, which is what the backward pass reads. Both kernels are bound by HBM: every tensor
+// passes once, a row stays in registers (as the packed bits that were read) between its sum and its output. A row is
+// one warp's or one CTA's, 16 bytes a thread and step; the 8-bit rows' maximum of |h w| goes through the same
+// reduction as the sum of squares (max |y| = rstd max |h w|, so one barrier serves both).
+// Backward: CTAs walk over rows and keep dw of their columns in registers (fp32); the partial sums of all
+// CTAs meet in a second launch, in one order.
+#include "layer.cuh"
+
+namespace ssba {
+namespace layer {
+namespace {
+
+using namespace ptx;
+
+template <class T>
+struct Vec;  // 16 bytes of T
+template <>
+struct Vec<__nv_bfloat16> {
+    static constexpr int n = 8;
+    static __device__ __forceinline__ void get(const uint4& v, float* f)
+    {
+        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 p = unpack2(u[i]);
+            f[2 * i] = p.x;
+            f[2 * i + 1] = p.y;
+        }
+    }
+    static __device__ __forceinline__ uint4 put(const float* f)
+    {
+        return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
+    }
+};
+template <>
+struct Vec<float> {
+    static constexpr int n = 4;
+    static __device__ __forceinline__ void get(const uint4& v, float* f)
+    {
+        f[0] = __uint_as_float(v.x);
+        f[1] = __uint_as_float(v.y);
+        f[2] = __uint_as_float(v.z);
+        f[3] = __uint_as_float(v.w);
+    }
+    static __device__ __forceinline__ uint4 put(const float* f)
+    {
+        return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    }
+};
+
+template <int n>
+__device__ __forceinline__ void load_w(const float* w, float* f)
+{
+#pragma unroll
+    for (int i = 0; i < n; i += 4) {
+        const float4 v = __ldg(reinterpret_cast<const float4*>(w + i));
+        f[i] = v.x;
+        f[i + 1] = v.y;
+        f[i + 2] = v.z;
+        f[i + 3] = v.w;
+    }
+}
+
+// The sum of s and the maximum of m over the row's kTPR threads (a warp, or the whole CTA; `at` alternates
+// between two halves of the exchange area, so that one barrier a row is enough).
+template <int kTPR, bool kMax>
+__device__ __forceinline__ void row_reduce(float& s, float& m, float2 (*area)[32], int at)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (kMax) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    }
+    if constexpr (kTPR > 32) {
+        constexpr int kWarps = kTPR / 32;
+        const int lane = threadIdx.x & 31;
+        if (lane == 0) area[at][threadIdx.x >> 5] = make_float2(s, m);
+        __syncthreads();
+        const float2 v = area[at][lane % kWarps];
+        s = v.x;
+        m = v.y;
+#pragma unroll
+        for (int o = kWarps / 2; o > 0; o >>= 1) {
+            s += __shfl_xor_sync(0xffffffffu, s, o);
+            if (kMax) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        }
+    }
+}
+
+// The least power of two s with a / s <= 448 = 1.75 * 2^8 (at least 2^-126; 1 for a row of zeros), and its reciprocal.
+__device__ __forceinline__ float row_scale(float a, float& inverse)
+{
+    const uint32_t bits = __float_as_uint(a);
+    int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+    if (a == 0.f) e = 0;
+    e = min(max(e, -126), 126);
+    inverse = __uint_as_float((uint32_t)(127 - e) << 23);
+    return __uint_as_float((uint32_t)(127 + e) << 23);
+}
+
+__device__ __forceinline__ uint32_t pack_e4m3(const float* f)
+{
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[0], f[1]), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[2], f[3]), __NV_SATFINITE, __NV_E4M3);
+    return lo | (hi << 16);
+}
+
+struct NormArgs {
+    const uint4 *x, *r;
+    const float* w;
+    uint4 *h, *y;
+    uint8_t* q;
+    float *scale, *rstd;
+    int T, D;
+    float eps;
+};
+
+constexpr int kWarpCta = 128;  // threads of a CTA whose warps take a row each
+
+template <class T, int kTPR, int kNV, bool kRes, bool kF8>
+__global__ void __launch_bounds__(kTPR == 32 ? kWarpCta : kTPR) ssba_rms_norm_kernel(const NormArgs p)
+{
+    constexpr int n = Vec<T>::n, kRows = kTPR == 32 ? kWarpCta / 32 : 1;
+    __shared__ float2 area[2][32];
+    const int nv = p.D / n, tid = threadIdx.x % kTPR;
+    grid_dep_wait();
+    grid_dep_launch();
+    int at = 0;
+    for (long long t = (long long)blockIdx.x * kRows + threadIdx.x / kTPR; t < p.T; t += (long long)gridDim.x * kRows, at ^= 1) {
+        uint4 v[kNV], u[kRes ? kNV : 1];
+#pragma unroll
+        for (int j = 0; j < kNV; ++j) {
+            const int i = tid + j * kTPR;
+            v[j] = i < nv ? p.x[t * nv + i] : make_uint4(0, 0, 0, 0);
+            if (kRes) u[j] = i < nv ? p.r[t * nv + i] : make_uint4(0, 0, 0, 0);
+        }
+        float s = 0.f, m = 0.f;
+#pragma unroll
+        for (int j = 0; j < kNV; ++j) {
+            const int i = tid + j * kTPR;
+            float f[n];
+            Vec<T>::get(v[j], f);
+            if (kRes) {
+                float g[n];
+                Vec<T>::get(u[j], g);
+#pragma unroll
+                for (int e = 0; e < n; ++e) f[e] += g[e];
+                v[j] = Vec<T>::put(f);
+                if (i < nv) p.h[t * nv + i] = v[j];
+                Vec<T>::get(v[j], f);
+            }
+#pragma unroll
+            for (int e = 0; e < n; ++e) s = fmaf(f[e], f[e], s);
+            if (kF8 && i < nv) {
+                float w[n];
+                load_w<n>(p.w + (size_t)i * n, w);
+#pragma unroll
+                for (int e = 0; e < n; ++e) m = fmaxf(m, fabsf(f[e] * w[e]));
+            }
+        }
+        row_reduce<kTPR, kF8>(s, m, area, at);
+        const float rstd = 1.f / sqrtf(s / (float)p.D + p.eps);
+        float inverse = 1.f;
+        if (kF8) {
+            const float scale = row_scale(m * rstd, inverse);
+            if (tid == 0) p.scale[t] = scale;
+        }
+        if (tid == 0) p.rstd[t] = rstd;
+#pragma unroll
+        for (int j = 0; j < kNV; ++j) {
+            const int i = tid + j * kTPR;
+            if (i >= nv) continue;
+            float f[n], w[n];
+            Vec<T>::get(v[j], f);
+            load_w<n>(p.w + (size_t)i * n, w);
+#pragma unroll
+            for (int e = 0; e < n; ++e) f[e] = f[e] * rstd * w[e];
+            if (kF8) {
+#pragma unroll
+                for (int e = 0; e < n; ++e) f[e] *= inverse;
+                uint32_t b[n / 4];
+#pragma unroll
+                for (int e = 0; e < n; e += 4) b[e / 4] = pack_e4m3(f + e);
+                if constexpr (n == 8)
+                    reinterpret_cast<uint2*>(p.q)[t * nv + i] = make_uint2(b[0], b[1]);
+                else
+                    reinterpret_cast<uint32_t*>(p.q)[t * nv + i] = b[0];
+            } else {
+                p.y[t * nv + i] = Vec<T>::put(f);
+            }
+        }
+    }
+}
+
+struct NormBwdArgs {
+    const uint4 *dy, *h, *dh;
+    const float *w, *rstd;
+    uint4* dx;
+    float* part;
+    int T, D;
+};
+
+constexpr int kBwdWarps = 8;  // warps of a CTA whose warps take a row each
+
+template <class T, int kTPR, int kNV, bool kDh>
+__global__ void __launch_bounds__(kTPR == 32 ? kBwdWarps * 32 : kTPR) ssba_rms_norm_bwd_kernel(const NormBwdArgs p)
+{
+    constexpr int n = Vec<T>::n, kRows = kTPR == 32 ? kBwdWarps : 1;
+    __shared__ float2 area[2][32];
+    extern __shared__ float cols[];  // [D], where a CTA's warps add up
+    const int nv = p.D / n, tid = threadIdx.x % kTPR;
+    float dw[kNV][n] = {};
+    grid_dep_wait();
+    grid_dep_launch();
+    int at = 0;
+    for (long long t = (long long)blockIdx.x * kRows + threadIdx.x / kTPR; t < p.T; t += (long long)gridDim.x * kRows, at ^= 1) {
+        uint4 a[kNV], b[kNV], c[kDh ? kNV : 1];
+#pragma unroll
+        for (int j = 0; j < kNV; ++j) {
+            const int i = tid + j * kTPR;
+            const bool in = i < nv;
+            a[j] = in ? p.dy[t * nv + i] : make_uint4(0, 0, 0, 0);
+            b[j] = in ? p.h[t * nv + i] : make_uint4(0, 0, 0, 0);
+            if (kDh) c[j] = in ? p.dh[t * nv + i] : make_uint4(0, 0, 0, 0);
+        }
+        const float rstd = p.rstd[t];
+        float s = 0.f, none = 0.f;
+#pragma unroll
+        for (int j = 0; j < kNV; ++j) {
+            const int i = tid + j * kTPR;
+            if (i >= nv) continue;
+            float d[n], h[n], w[n];
+            Vec<T>::get(a[j], d);
+            Vec<T>::get(b[j], h);
+            load_w<n>(p.w + (size_t)i * n, w);
+#pragma unroll
+            for (int e = 0; e < n; ++e) {
+                const float k = d[e] * (h[e] * rstd);
+                s = fmaf(k, w[e], s);
+                dw[j][e] += k;
+            }
+        }
+        row_reduce<kTPR, false>(s, none, area, at);
+        const float along = s / (float)p.D;
+#pragma unroll
+        for (int j = 0; j < kNV; ++j) {
+            const int i = tid + j * kTPR;
+            if (i >= nv) continue;
+            float d[n], h[n], w[n], g[n];
+            Vec<T>::get(a[j], d);
+            Vec<T>::get(b[j], h);
+            load_w<n>(p.w + (size_t)i * n, w);
+            if (kDh) Vec<T>::get(c[j], g);
+#pragma unroll
+            for (int e = 0; e < n; ++e) {
+                const float o = rstd * (d[e] * w[e] - h[e] * rstd * along);
+                d[e] = kDh ? o + g[e] : o;
+            }
+            p.dx[t * nv + i] = Vec<T>::put(d);
+        }
+    }
+    float* out = p.part + (size_t)blockIdx.x * p.D;
+    if constexpr (kTPR == 32) {
+        // the warps' sums, in the order of the warps
+        for (int k = 0; k < kBwdWarps; ++k) {
+            if ((int)(threadIdx.x >> 5) == k) {
+#pragma unroll
+                for (int j = 0; j < kNV; ++j) {
+                    const int i = tid + j * kTPR;
+                    if (i >= nv) continue;
+#pragma unroll
+                    for (int e = 0; e < n; ++e) {
+                        const float v = k ? cols[i * n + e] + dw[j][e] : dw[j][e];
+                        cols[i * n + e] = v;
+                        if (k == kBwdWarps - 1) out[i * n + e] = v;
+                    }
+                }
+            }
+            __syncthreads();
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < kNV; ++j) {
+            const int i = tid + j * kTPR;
+            if (i >= nv) continue;
+#pragma unroll
+            for (int e = 0; e < n; e += 4)
+                *reinterpret_cast<float4*>(out + (size_t)i * n + e) =
+                    make_float4(dw[j][e], dw[j][e + 1], dw[j][e + 2], dw[j][e + 3]);
+        }
+    }
+}
+
+// out[c] = sum_p part[p][c]: a CTA takes 32 columns, its 32 warps every 32nd part each, then the warps in order.
+__global__ void __launch_bounds__(1024) ssba_column_sum_kernel(const float* part, int parts, int N, float* out)
+{
+    __shared__ float sums[32][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    grid_dep_wait();
+    grid_dep_launch();
+    float s = 0.f;
+    if (c < N) {
+#pragma unroll 4
+        for (int p = warp; p < parts; p += 32) s += part[(size_t)p * N + c];
+    }
+    sums[warp][lane] = s;
+    __syncthreads();
+    s = sums[lane][warp];  // column `warp` of the 32, its parts over the lanes
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane == 0 && blockIdx.x * 32 + warp < N) out[blockIdx.x * 32 + warp] = s;
+}
+
+// Threads a row and 16-byte steps a thread. Rows of up to 4 KB are a warp's (no barrier; all its loads under way at
+// once), longer ones a CTA's.
+template <class T, class F>
+int by_width(int nv, F&& f)
+{
+    using std::integral_constant;
+#define SSBA_ROW(tpr, steps) return f(integral_constant<int, tpr>(), integral_constant<int, steps>())
+    if (nv <= 32) SSBA_ROW(32, 1);
+    if (nv <= 64) SSBA_ROW(32, 2);
+    if (nv <= 128) SSBA_ROW(32, 4);
+    if (nv <= 192) SSBA_ROW(32, 6);
+    if (nv <= 256) SSBA_ROW(128, 2);
+    if (nv <= 512) SSBA_ROW(256, 2);
+    if (nv <= 1024) SSBA_ROW(256, 4);
+    if constexpr (sizeof(T) == 4) {
+        if (nv > 2048) SSBA_ROW(1024, 4);
+    }
+    SSBA_ROW(512, 4);
+#undef SSBA_ROW
+}
+
+int launched(cudaError_t e, const char* what)
+{
+    if (e == cudaSuccess) return SSBA_OK;
+    set_error("%s launch: %s", what, cudaGetErrorString(e));
+    return SSBA_ERR_CUDA;
+}
+
+template <class T, bool kRes, bool kF8>
+int norm_as(const NormArgs& p, cudaStream_t st)
+{
+    return by_width<T>(p.D / Vec<T>::n, [&](auto tpr, auto steps) {
+        constexpr int kTPR = decltype(tpr)::value, kRows = kTPR == 32 ? kWarpCta / 32 : 1;
+        const long long ctas = ((long long)p.T + kRows - 1) / kRows, most = 64ll * device_sm_count();
+        return launched(launch_early(ssba_rms_norm_kernel<T, kTPR, decltype(steps)::value, kRes, kF8>,
+                                     dim3((unsigned)(ctas < most ? ctas : most)), kTPR == 32 ? kWarpCta : kTPR, 0, st, 1, p),
+                        "ssba_rms_norm_kernel");
+    });
+}
+
+// CTAs of the backward pass: as many as run at once, each with rows enough to make its column sums worth writing.
+int bwd_ctas(int T, int D, int dtype)
+{
+    const int nv = D / (dtype == SSBA_BF16 ? 8 : 4);
+    const bool warps = nv <= 192;
+    const int rows = warps ? kBwdWarps : 1;
+    const long long need = ((long long)T + rows - 1) / rows, most = (long long)device_sm_count() * (warps ? 3 : nv <= 256 ? 8 : nv <= 1024 ? 4 : 2);
+    return (int)(need < most ? need : most);
+}
+
+template <class T, bool kDh>
+int norm_bwd_as(const NormBwdArgs& p, int ctas, cudaStream_t st)
+{
+    return by_width<T>(p.D / Vec<T>::n, [&](auto tpr, auto steps) {
+        constexpr int kTPR = decltype(tpr)::value;
+        return launched(launch_early(ssba_rms_norm_bwd_kernel<T, kTPR, decltype(steps)::value, kDh>, dim3(ctas),
+                                     kTPR == 32 ? kBwdWarps * 32 : kTPR, kTPR == 32 ? sizeof(float) * p.D : 0, st, 1, p),
+                        "ssba_rms_norm_bwd_kernel");
+    });
+}
+
+}  // namespace
+
+int launch_column_sum(const float* part, int parts, int N, float* out, const char* who, cudaStream_t st)
+{
+    return launched(launch_early(ssba_column_sum_kernel, dim3((N + 31) / 32), 1024, 0, st, 1, part, parts, N, out), who);
+}
+
+int launch_rms_norm(const void* x, const void* r, const float* w, int T, int D, int dtype, float eps, void* h, void* y,
+                    bool e4m3, float* scale, float* rstd, cudaStream_t st)
+{
+    const NormArgs p{static_cast<const uint4*>(x), static_cast<const uint4*>(r), w, static_cast<uint4*>(h),
+                     static_cast<uint4*>(y), static_cast<uint8_t*>(y), scale, rstd, T, D, eps};
+    auto go = [&](auto t) {
+        using E = decltype(t);
+        if (r) return e4m3 ? norm_as<E, true, true>(p, st) : norm_as<E, true, false>(p, st);
+        return e4m3 ? norm_as<E, false, true>(p, st) : norm_as<E, false, false>(p, st);
+    };
+    return dtype == SSBA_BF16 ? go(__nv_bfloat16()) : go(float());
+}
+
+int rms_norm_backward_parts(int T, int D, int dtype) { return bwd_ctas(T, D, dtype); }
+
+int launch_rms_norm_backward(const void* dy, const void* h, const float* w, const float* rstd, const void* dh, int T, int D,
+                             int dtype, void* dx, float* dw, float* part, cudaStream_t st)
+{
+    const NormBwdArgs p{static_cast<const uint4*>(dy), static_cast<const uint4*>(h), static_cast<const uint4*>(dh), w, rstd,
+                        static_cast<uint4*>(dx), part, T, D};
+    const int ctas = bwd_ctas(T, D, dtype);
+    auto go = [&](auto t) {
+        using E = decltype(t);
+        return dh ? norm_bwd_as<E, true>(p, ctas, st) : norm_bwd_as<E, false>(p, ctas, st);
+    };
+    const int rc = dtype == SSBA_BF16 ? go(__nv_bfloat16()) : go(float());
+    return rc == SSBA_OK ? launch_column_sum(part, ctas, D, dw, "ssba_rms_norm_backward", st) : rc;
+}
+
+}  // namespace layer
+}  // namespace ssba

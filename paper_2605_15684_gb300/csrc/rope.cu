@@ -1,0 +1,217 @@
+// rope.cu -- rotary positions with several axes (time, height, width, ...), on heads at any strides.
+//
+// A head's first 2P dimensions are P pairs, cut into one run of pairs for each axis. Pair j of axis a turns by the
+// angle pos_a theta_j: (u, v) -> (u cos - v sin, u sin + v cos); the inverse, which is the gradient, by its negative.
+// Pairs are adjacent dimensions (2j, 2j + 1) or halves (j, j + P); dimensions from 2P on stay.
+//
+// Angles: theta_j / (2 pi) is held as a 64-bit fraction of a turn, whose product with an integer position modulo 2^64 is
+// the angle modulo whole turns, without a rounding: at any position the angle is off by 2^-32 of a turn and by what
+// theta's own 53 bits leave (a product in fp32 is off by a tenth of a radian at a million). The top 32 bits, signed,
+// are the angle in units of 2^-31 pi, which sincospif takes.
+//
+// Bound by HBM: x is read once and written once, 16 bytes a thread and step where the strides and the cut allow it (else
+// 8, 4 or 2). A thread forms the sines of its pairs of one token once and applies them to the heads of its share.
+#include <cmath>
+
+#include "layer.cuh"
+
+namespace ssba {
+namespace layer {
+namespace {
+
+using namespace ptx;
+
+constexpr int kMaxPairs = SSBA_ROPE_MAX_HEAD_DIM / 2;
+
+struct RopeArgs {
+    const char* x;
+    char* out;
+    const int32_t* pos;
+    int64_t xs[3], os[3], pos_batch;  // strides of batch, token, head in bytes; of pos's batch in elements
+    long long work;                   // threads with something to do
+    int T, heads, axes, P, D;
+    int units, turned;                // units a token and head; of them those that turn
+    int share, shares;                // heads a thread, threads a token's unit
+    int inverse;
+    uint8_t axis[kMaxPairs];
+    uint64_t theta[kMaxPairs];        // turns of 2^64 a position
+};
+
+template <int kBytes>
+struct Word;
+template <>
+struct Word<16> { using type = uint4; };
+template <>
+struct Word<8> { using type = uint2; };
+template <>
+struct Word<4> { using type = uint32_t; };
+template <>
+struct Word<2> { using type = uint16_t; };
+
+// n elements of E in 16, 8, 4 or 2 bytes
+template <class E, int n>
+struct Pack {
+    using W = typename Word<n * (int)sizeof(E)>::type;
+    union U {
+        W w;
+        E e[n];
+        __device__ U() {}
+    };
+    static __device__ __forceinline__ void load(const char* p, float* f)
+    {
+        U u;
+        u.w = *reinterpret_cast<const W*>(p);
+#pragma unroll
+        for (int i = 0; i < n; ++i) f[i] = (float)u.e[i];
+    }
+    static __device__ __forceinline__ void store(char* p, const float* f)
+    {
+        U u;
+#pragma unroll
+        for (int i = 0; i < n; ++i) u.e[i] = (E)f[i];
+        *reinterpret_cast<W*>(p) = u.w;
+    }
+};
+
+// (u, v) turned, with the same roundings in every instantiation: widths and layouts give the same bits.
+__device__ __forceinline__ void turn(float u, float v, float c, float s, float& a, float& b)
+{
+    a = fmaf(u, c, -__fmul_rn(v, s));
+    b = fmaf(u, s, __fmul_rn(v, c));
+}
+
+// kN: elements of a piece. Halves: a unit is a piece of either half; adjacent pairs: one piece.
+template <class E, int kN, bool kHalves>
+__global__ void __launch_bounds__(256) ssba_rope_kernel(const __grid_constant__ RopeArgs p)
+{
+    constexpr int kPairs = kHalves ? kN : kN / 2;
+    grid_dep_wait();
+    grid_dep_launch();
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (id >= p.work) return;
+    const int unit = (int)(id % p.units);
+    const long long rest = id / p.units;
+    const long long token = rest % ((long long)p.work / p.units / p.shares);
+    const int sh = (int)(rest / ((long long)p.work / p.units / p.shares));
+    const long long b = token / p.T, t = token - b * p.T;
+    const int h0 = sh * p.share, h1 = min(h0 + p.share, p.heads);
+    const char* x = p.x + b * p.xs[0] + t * p.xs[1] + h0 * p.xs[2];
+    char* o = p.out + b * p.os[0] + t * p.os[1] + h0 * p.os[2];
+    if (unit >= p.turned) {  // dimensions that stay (halves only: adjacent pairs past P turn by nothing)
+        const int at = (2 * p.P + (unit - p.turned) * kN) * (int)sizeof(E);
+        for (int h = h0; h < h1; ++h, x += p.xs[2], o += p.os[2]) {
+            float f[kN];
+            Pack<E, kN>::load(x + at, f);
+            Pack<E, kN>::store(o + at, f);
+        }
+        return;
+    }
+    const int32_t* pos = p.pos + b * p.pos_batch + t * p.axes;
+    float c[kPairs], s[kPairs];
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+        const int j = unit * kPairs + i;
+        if (!kHalves && j >= p.P) {
+            c[i] = 1.f;
+            s[i] = 0.f;
+            continue;
+        }
+        const uint64_t turns = (uint64_t)(int64_t)pos[p.axis[j]] * p.theta[j];
+        sincospif((float)(int32_t)(turns >> 32) * 4.656612873077393e-10f, &s[i], &c[i]);
+        if (p.inverse) s[i] = -s[i];
+    }
+    const int at = unit * kN * (int)sizeof(E), half = p.P * (int)sizeof(E);
+#pragma unroll 4
+    for (int h = h0; h < h1; ++h, x += p.xs[2], o += p.os[2]) {
+        if constexpr (kHalves) {
+            float u[kN], v[kN], a[kN], d[kN];
+            Pack<E, kN>::load(x + at, u);
+            Pack<E, kN>::load(x + at + half, v);
+#pragma unroll
+            for (int i = 0; i < kN; ++i) turn(u[i], v[i], c[i], s[i], a[i], d[i]);
+            Pack<E, kN>::store(o + at, a);
+            Pack<E, kN>::store(o + at + half, d);
+        } else {
+            float u[kN], a[kN];
+            Pack<E, kN>::load(x + at, u);
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) turn(u[2 * i], u[2 * i + 1], c[i], s[i], a[2 * i], a[2 * i + 1]);
+            Pack<E, kN>::store(o + at, a);
+        }
+    }
+}
+
+template <class E, bool kHalves>
+int rope_as(RopeArgs& p, int bytes, long long tokens, cudaStream_t st)
+{
+    auto go = [&](auto n_) {
+        constexpr int n = decltype(n_)::value;
+        p.units = kHalves ? p.P / n + (p.D - 2 * p.P) / n : p.D / n;
+        p.turned = kHalves ? p.P / n : p.units;
+        // Heads a thread: as many as leave some eight warps a scheduler; a thread's sines then serve them all.
+        const long long lanes = tokens * p.units, full = (long long)device_sm_count() * 1024;
+        int shares = (int)(full / lanes > p.heads ? p.heads : full / lanes);
+        if (shares < 1) shares = 1;
+        p.share = (p.heads + shares - 1) / shares;
+        p.shares = (p.heads + p.share - 1) / p.share;
+        p.work = lanes * p.shares;
+        const cudaError_t e = launch_early(ssba_rope_kernel<E, n, kHalves>, dim3((unsigned)((p.work + 255) / 256)), 256, 0, st, 1, p);
+        if (e == cudaSuccess) return (int)SSBA_OK;
+        set_error("ssba_rope_kernel launch: %s", cudaGetErrorString(e));
+        return (int)SSBA_ERR_CUDA;
+    };
+    using std::integral_constant;
+    constexpr int s = sizeof(E);
+    if (bytes == 16) return go(integral_constant<int, 16 / s>());
+    if (bytes == 8) return go(integral_constant<int, 8 / s>());
+    if constexpr (kHalves || s == 2) {
+        if (bytes == 4) return go(integral_constant<int, 4 / s>());
+    }
+    if constexpr (kHalves && s == 2) return go(integral_constant<int, 1>());
+    return SSBA_ERR_INVALID;  // not reached: the caller's bytes hold a pair, or an element of halves
+}
+
+}  // namespace
+
+int launch_rope(const ssba_rope_desc& d, const void* x, const int64_t* xs, const int32_t* pos, int64_t pos_batch, void* out,
+                const int64_t* os, cudaStream_t st)
+{
+    RopeArgs p = {};
+    const int es = d.dtype == SSBA_BF16 ? 2 : 4;
+    p.x = static_cast<const char*>(x);
+    p.out = static_cast<char*>(out);
+    p.pos = pos;
+    p.pos_batch = pos_batch;
+    uint64_t all = reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(out);
+    for (int i = 0; i < 3; ++i) {
+        p.xs[i] = xs[i] * es;
+        p.os[i] = os[i] * es;
+        all |= (uint64_t)p.xs[i] | (uint64_t)p.os[i];
+    }
+    p.T = d.T;
+    p.heads = d.heads;
+    p.axes = d.axes;
+    p.D = d.head_dim;
+    for (int a = 0; a < d.axes; ++a) p.P += d.sections[a];
+    const double two64 = 18446744073709551616.0, turn = 6.283185307179586476925286766559;
+    for (int a = 0, j = 0; a < d.axes; ++a)
+        for (int i = 0; i < d.sections[a]; ++i, ++j) {
+            p.axis[j] = (uint8_t)a;
+            const double e = d.shared ? (double)j / p.P : (double)i / d.sections[a];
+            p.theta[j] = (uint64_t)(std::pow(d.base, -e) / turn * two64 + 0.5);
+        }
+    p.inverse = d.inverse;
+    // the widest piece that every row's start, and the cuts of halves, are multiples of
+    const bool halves = d.layout == SSBA_ROPE_HALVES;
+    all |= (uint64_t)p.D * es;
+    if (halves) all |= (uint64_t)p.P * es;
+    int bytes = 16;
+    while (all & (bytes - 1)) bytes >>= 1;
+    const long long tokens = (long long)d.B * d.T;
+    if (d.dtype == SSBA_BF16)
+        return halves ? rope_as<__nv_bfloat16, true>(p, bytes, tokens, st) : rope_as<__nv_bfloat16, false>(p, bytes, tokens, st);
+    return halves ? rope_as<float, true>(p, bytes, tokens, st) : rope_as<float, false>(p, bytes, tokens, st);
+}
+
+}  // namespace layer
+}  // namespace ssba

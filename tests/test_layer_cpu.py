@@ -1,0 +1,142 @@
+"""Refusals of a layer's operators: every bad call is an error on the host, before any device work."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2605_15684_gb300 import api, build, layer
+
+FAKE = 0x100000  # a 16-byte aligned, never dereferenced address
+ODD = FAKE + 4
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return api.load_library()
+
+
+def linear_desc(**kw):
+    d = dict(T=4, N=64, K=64, dtype=api.SSBA_BF16, act=0, gated=0)
+    d.update(kw)
+    return ctypes.byref(layer._LinearDesc(**d))
+
+
+def rope_desc(**kw):
+    d = dict(B=1, T=4, heads=2, head_dim=64, axes=2, sections=(16, 16, 0, 0), layout=0, shared=0, inverse=0,
+             dtype=api.SSBA_BF16, base=10000.0)
+    d.update(kw)
+    d["sections"] = (ctypes.c_int32 * 4)(*d["sections"])
+    return ctypes.byref(layer._RopeDesc(**d))
+
+
+def S(*v):
+    return (ctypes.c_int64 * 3)(*v)
+
+
+INV, UNS, WS = api.SSBA_ERR_INVALID, api.SSBA_ERR_UNSUPPORTED, api.SSBA_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("args,code", [
+    (dict(T=-1), INV), (dict(D=0), INV), (dict(dtype=2), INV), (dict(dtype=7), INV), (dict(D=60), UNS), (dict(D=16392), UNS),
+    (dict(eps=-1.0), INV), (dict(eps=float("inf")), INV), (dict(eps=float("nan")), INV), (dict(r=FAKE), INV), (dict(h=FAKE), INV),
+    (dict(x=None), INV), (dict(w=None), INV), (dict(y=None), INV), (dict(rstd=None), INV), (dict(x=ODD), INV), (dict(w=ODD), INV),
+    (dict(y=ODD), INV), (dict(scale=FAKE + 2), INV),
+])
+def test_norm_refusals(lib, args, code):
+    a = dict(x=FAKE, r=None, w=FAKE, T=4, D=64, dtype=0, eps=1e-6, h=None, y=FAKE, scale=None, rstd=FAKE)
+    a.update(args)
+    assert lib.ssba_rms_norm(*a.values(), None) == code
+    assert b"ssba_rms_norm" in lib.ssba_last_error()
+
+
+@pytest.mark.parametrize("args,code", [
+    (dict(T=-1), INV), (dict(D=60), UNS), (dict(dtype=2), INV), (dict(dy=None), INV), (dict(h=None), INV), (dict(w=None), INV),
+    (dict(rstd=None), INV), (dict(dx=None), INV), (dict(dw=None), INV), (dict(dh=ODD), INV), (dict(ws=None), WS), (dict(n=16), WS),
+    (dict(ws=ODD), WS),
+])
+def test_norm_backward_refusals(lib, args, code):
+    a = dict(dy=FAKE, h=FAKE, w=FAKE, rstd=FAKE, dh=None, T=400, D=64, dtype=0, dx=FAKE, dw=FAKE, ws=FAKE, n=1 << 30)
+    a.update(args)
+    assert lib.ssba_rms_norm_backward(*a.values(), None) == code
+
+
+@pytest.mark.parametrize("desc,args,code", [
+    (dict(T=-1), {}, INV), (dict(N=0), {}, INV), (dict(K=0), {}, INV), (dict(dtype=1), {}, INV), (dict(dtype=3), {}, INV), (dict(act=4), {}, INV),
+    (dict(act=-1), {}, INV), (dict(gated=1), {}, INV), (dict(N=60), {}, UNS), (dict(K=60), {}, UNS), (dict(N=1 << 18), {}, UNS),
+    (dict(K=1 << 18), {}, UNS), (dict(T=(1 << 24) + 1), {}, UNS),
+    (dict(dtype=2, K=72), dict(xs=FAKE, ws=FAKE), UNS), (dict(dtype=2), {}, INV), (dict(dtype=2), dict(xs=FAKE), INV), ({}, dict(ws=FAKE), INV),
+    (dict(gated=1, act=3), dict(bias=FAKE), INV), (dict(gated=1, act=3), dict(r=FAKE), INV),
+    ({}, dict(x=None), INV), ({}, dict(W=None), INV), ({}, dict(y=None), INV), ({}, dict(x=ODD), INV), ({}, dict(z=ODD), INV), ({}, dict(bias=ODD), INV),
+])
+def test_linear_refusals(lib, desc, args, code):
+    a = dict(x=FAKE, W=FAKE, xs=None, ws=None, bias=None, r=None, y=FAKE, z=None)
+    a.update(args)
+    assert lib.ssba_linear(linear_desc(**desc), *a.values(), None) == code
+
+
+@pytest.mark.parametrize("desc,args,code", [
+    (dict(dtype=2), {}, INV), (dict(N=60), {}, UNS), (dict(gated=1, act=3), dict(db=FAKE), INV), ({}, dict(W=None), INV), ({}, dict(x=None), INV),
+    ({}, dict(dy=None), INV), (dict(act=2), {}, INV), (dict(act=2), dict(z=FAKE, ws=None), WS), (dict(act=2), dict(z=FAKE, n=16), WS),
+    ({}, dict(dx=ODD), INV), ({}, dict(db=FAKE + 2), INV),
+])
+def test_linear_backward_refusals(lib, desc, args, code):
+    a = dict(dy=FAKE, x=FAKE, W=FAKE, z=None, dx=FAKE, dW=FAKE, db=None, ws=FAKE, n=1 << 30)
+    a.update(args)
+    assert lib.ssba_linear_backward(linear_desc(**desc), *a.values(), None) == code
+    assert lib.ssba_linear_backward(None, *a.values(), None) == INV
+
+
+@pytest.mark.parametrize("desc,args,code", [
+    (dict(B=-1), {}, INV), (dict(T=-1), {}, INV), (dict(heads=0), {}, INV), (dict(head_dim=0), {}, INV), (dict(axes=0), {}, INV), (dict(axes=5), {}, INV),
+    (dict(sections=(16, 0, 0, 0)), {}, INV), (dict(sections=(16, 17, 0, 0)), {}, INV), (dict(sections=(2 ** 31 - 1, 2 ** 31 - 1, 0, 0)), {}, INV),
+    (dict(layout=2), {}, INV), (dict(base=1.0), {}, INV), (dict(base=float("nan")), {}, INV), (dict(base=float("inf")), {}, INV), (dict(dtype=2), {}, INV),
+    (dict(head_dim=65), {}, UNS), (dict(head_dim=258), {}, UNS), (dict(B=1 << 20, T=1 << 20), {}, UNS),
+    ({}, dict(x=None), INV), ({}, dict(pos=None), INV), ({}, dict(out=None), INV), ({}, dict(xs=None), INV), ({}, dict(os=S(0, -64, 64)), INV),
+    ({}, dict(x=FAKE + 2), INV), (dict(layout=1), dict(x=FAKE + 1), INV), ({}, dict(xs=S(0, 65, 64)), INV), ({}, dict(pos=FAKE + 2), INV), ({}, dict(pb=-1), INV),
+])
+def test_rope_refusals(lib, desc, args, code):
+    a = dict(x=FAKE, xs=S(512, 128, 64), pos=FAKE, pb=0, out=FAKE, os=S(512, 128, 64))
+    a.update(args)
+    assert lib.ssba_rope_axes(rope_desc(**desc), *a.values(), None) == code
+
+
+def test_no_rows_is_no_work(lib):
+    assert lib.ssba_rms_norm(None, None, None, 0, 64, 0, 1e-6, None, None, None, None, None) == api.SSBA_OK
+    assert lib.ssba_linear(linear_desc(T=0), *[None] * 8, None) == api.SSBA_OK
+    assert lib.ssba_rope_axes(rope_desc(T=0), None, S(0, 0, 0), None, 0, None, S(0, 0, 0), None) == api.SSBA_OK
+
+
+def test_workspace_sizes(lib):
+    assert lib.ssba_linear_backward_workspace_bytes(linear_desc(T=100, N=64, act=2)) >= 100 * 64 * 2 + 64 * 4
+    assert lib.ssba_linear_backward_workspace_bytes(linear_desc(T=100, N=64, act=3, gated=1)) == 100 * 128 * 2
+    assert lib.ssba_linear_backward_workspace_bytes(linear_desc(N=60)) == 0
+    assert lib.ssba_rms_norm_backward_workspace_bytes(100, 64, 0) >= 64 * 4
+    assert lib.ssba_rms_norm_backward_workspace_bytes(100, 63, 0) == 0
+
+
+def test_python_refuses_what_is_not_on_the_gpu(lib):
+    x, w = torch.zeros(4, 64, dtype=torch.bfloat16), torch.ones(64)
+    for call in (lambda: layer.rms_norm(x, w), lambda: layer.rms_norm_backward(x, x, w, w[:4]), lambda: layer.linear(x, x),
+                 lambda: layer.gated_linear(x, x), lambda: layer.linear_backward(x, x, x), lambda: layer.rms_norm(w, w),
+                 lambda: layer.gated_linear_backward(x, x, x, x), lambda: layer.rms_norm(x.half(), w), lambda: layer.linear(None, x),
+                 lambda: layer.rope_axes(x.view(1, 2, 2, 64), torch.zeros(2, 2, dtype=torch.int32), (16, 16)),
+                 lambda: layer.rope_axes(x, None, (16,))):
+        with pytest.raises(api.SsbaError):
+            call()
+
+
+def test_rope_descriptor_refusals():
+    ok = (1, 4, 2, 64, (16, 16), "pairs", False, False, torch.bfloat16, 10000.0)
+    layer._rope_desc(ok)
+    for i, v in ((4, ()), (4, (1,) * 5), (4, (16, 0)), (4, (2 ** 33, 1)), (5, "interleaved"), (1, 2 ** 31)):
+        with pytest.raises(api.SsbaError):
+            layer._rope_desc((*ok[:i], v, *ok[i + 1:]))
+
+
+@pytest.mark.parametrize("shape,strides,dense", [
+    ((2, 3, 4, 64), (768, 256, 64, 1), True), ((2, 3, 4, 64), (768, 64, 192, 1), True), ((2, 3, 4, 64), (0, 256, 64, 1), False),
+    ((1, 3, 4, 64), (0, 256, 64, 1), True), ((2, 3, 4, 64), (768, 256, 32, 1), False), ((1, 3, 1, 64), (0, 63, 7, 1), False),
+])
+def test_overlapping_outputs_are_seen(shape, strides, dense):
+    assert layer._dense_heads(shape, strides) is dense
