@@ -211,9 +211,9 @@ int launch_column_sum(const float* part, int parts, int N, float* out, const cha
 int launch_rope(const ssba_rope_desc& d, const void* x, const int64_t* xs, const int32_t* pos, int64_t pos_batch, void* out,
                 const int64_t* os, cudaStream_t st);
 
-// A launch on st that may begin before the grid in front has ended (the kernels wait for it themselves).
+// A launch on st. early: it may begin before the grid in front has ended (the kernel waits for that itself).
 template <class... P, class... A>
-cudaError_t launch_early(void (*k)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster, A... a)
+cudaError_t launch_on(bool early, void (*k)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster, A... a)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
@@ -221,20 +221,26 @@ cudaError_t launch_early(void (*k)(P...), dim3 grid, int threads, size_t smem, c
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute la[2];
-    la[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    la[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.numAttrs = 1;
+    if (early) {
+        la[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        la[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+    }
     if (cluster > 1) {
-        la[1].id = cudaLaunchAttributeClusterDimension;
-        la[1].val.clusterDim.x = (unsigned)cluster;
-        la[1].val.clusterDim.y = 1;
-        la[1].val.clusterDim.z = 1;
-        cfg.numAttrs = 2;
+        la[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+        la[cfg.numAttrs].val.clusterDim.x = (unsigned)cluster;
+        la[cfg.numAttrs].val.clusterDim.y = 1;
+        la[cfg.numAttrs++].val.clusterDim.z = 1;
     }
     cfg.attrs = la;
     cudaError_t e = cudaLaunchKernelEx(&cfg, k, a...);
     const cudaError_t last = cudaGetLastError();
     return e == cudaSuccess ? last : e;
+}
+
+template <class... P, class... A>
+cudaError_t launch_early(void (*k)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster, A... a)
+{
+    return launch_on(true, k, grid, threads, smem, st, cluster, a...);
 }
 
 // A tensor of `depth` planes of rows, its boxes box_rows rows of `box_cols` elements.

@@ -192,8 +192,6 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_product_pair_kernel(const __
     tc_fence_after();
     const uint32_t tbase = sm.tmem_base;
     bool dead = false;
-    grid_dep_wait();
-    grid_dep_launch();
 
     if (warp == 0) {
         // ------------------------------------------------------------ this CTA's operands
@@ -471,7 +469,10 @@ int launch_as(const Product& q, const char* who, cudaStream_t st)
     }
     const int most = pairs_at_once(kernel, smem);
     const int pairs = p.tiles < most ? p.tiles : most;
-    const cudaError_t err = launch_early(kernel, dim3(2 * pairs), kThreads, smem, st, 2, maps, p);
+    // In stream order, neither beginning before the grid in front has ended nor letting the next one begin. Pairs that
+    // were set up beside the last waves of another grid (a gated block's backward pass, many calls queued)
+    // did not end; a launch of its own costs about 2 us.
+    const cudaError_t err = launch_on(false, kernel, dim3(2 * pairs), kThreads, smem, st, 2, maps, p);
     if (err == cudaSuccess) return SSBA_OK;
     set_error("%s: ssba_product_pair_kernel launch: %s", who, cudaGetErrorString(err));
     return SSBA_ERR_CUDA;
