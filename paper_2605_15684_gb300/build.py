@@ -3,8 +3,8 @@
 Each .cu file under csrc/ is compiled by nvcc in parallel and linked into one shared
 object with the CUDA runtime linked statically, so the library loads on a machine
 without a GPU driver (the driver is only needed once a call reaches the device).
-csrc/host/cache_call.cpp becomes _cache_call.so, the Python extension through which cache.py
-makes its calls (g++, against the installed torch).
+csrc/host/cache_call.cpp and layer_call.cpp become _cache_call.so and _layer_call.so, the Python extensions
+through which cache.py and layer.py make their calls (g++, against the installed torch).
 
 Variants (built only on request, each in a folder and a library of its own, so that the
 default libssba.so is never affected):
@@ -38,15 +38,15 @@ def library_file(variant: str = "") -> str:
     return LIB if not variant else os.path.join(HERE, f"libssba_{variant}.so")
 
 
-def call_file() -> str:
-    return os.path.join(HERE, "_cache_call.so")
+def call_file(name: str = "cache_call") -> str:
+    return os.path.join(HERE, f"_{name}.so")
 
 
-def build_call(force: bool = False) -> str:
-    """Compiles the Python extension of the cache's calls; returns its path."""
+def build_call(force: bool = False, name: str = "cache_call") -> str:
+    """Compiles a Python extension of csrc/host (the cache's calls, or the layer's); returns its path."""
     import torch
 
-    src, out = os.path.join(CSRC, "host", "cache_call.cpp"), call_file()
+    src, out = os.path.join(CSRC, "host", f"{name}.cpp"), call_file(name)
     home = os.path.dirname(torch.__file__)
     if force or _stale(out, [src, os.path.join(INCLUDE, "ssba.h"), os.path.join(home, "version.py")]):
         cuda = os.path.dirname(os.path.dirname(os.path.realpath(_nvcc())))
@@ -115,12 +115,13 @@ def build(force: bool = False, verbose: bool = False, extra_flags=(), variant: s
         os.replace(obj + ".tmp", obj)
         return r.stderr
 
-    with cf.ThreadPoolExecutor(max_workers=max(1, min(len(jobs) + 1, os.cpu_count() or 4))) as ex:
-        call = ex.submit(build_call, force)
+    with cf.ThreadPoolExecutor(max_workers=max(1, min(len(jobs) + 2, os.cpu_count() or 4))) as ex:
+        calls = [ex.submit(build_call, force, name) for name in ("cache_call", "layer_call")]
         for out in ex.map(compile_one, jobs):
             if verbose and out:
                 print(out, file=sys.stderr)
-        call.result()
+        for call in calls:
+            call.result()
     objs = [os.path.join(objdir, os.path.basename(s)[:-3] + ".o") for s in sources()]
     if force or jobs or _stale(lib, objs):
         tmp = lib + f".tmp{os.getpid()}"

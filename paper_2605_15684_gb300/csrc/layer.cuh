@@ -10,22 +10,39 @@ namespace ssba {
 namespace layer {
 
 // ------------------------------------------------------------------ activations
-// silu(z) = z sigma(z); gelu(z) = z sigma(2 sqrt(2/pi) (z + 0.044715 z^3)), which is its tanh form.
-constexpr float kGelu = 1.5957691216057308f, kGelu3 = 0.044715f;
+// silu(z) = z sigma(z); gelu(z) = z sigma(2 sqrt(2/pi) (z + 0.044715 z^3)), which is its tanh form. sigma(t) is formed as
+// 1 / (1 + 2^u), u = -log2(e) t: two units of the special function pipe, whose rate (16 a cycle and SM) bounds
+// an epilogue that can hide behind short products, and three to five of the others.
+constexpr float kLog2e = 1.4426950408889634f, kGelu = 1.5957691216057308f, kGelu3 = 0.044715f;
 
-template <int kAct>
-__device__ __forceinline__ float act_inner(float z)
+__device__ __forceinline__ float ex2(float x)
 {
-    return kAct == SSBA_ACT_GELU ? kGelu * (z + kGelu3 * z * z * z) : z;
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
-// The quotient of z and 1 + e^-t: 0 where the exponential overflows, which is z sigma(t) to fp32's least numbers.
+__device__ __forceinline__ float rcp(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// sigma(t(z)): 0 where the power overflows, which is z sigma to fp32's least numbers.
+template <int kAct>
+__device__ __forceinline__ float sigma(float z)
+{
+    const float u = kAct == SSBA_ACT_GELU ? z * fmaf(z * z, -kLog2e * kGelu * kGelu3, -kLog2e * kGelu) : z * -kLog2e;
+    return rcp(1.f + ex2(u));
+}
+
 template <int kAct>
 __device__ __forceinline__ float act_fn(float z)
 {
     if (kAct == SSBA_ACT_NONE) return z;
     if (kAct == SSBA_ACT_RELU) return z < 0.f ? 0.f : z;  // a NaN stays one
-    return __fdividef(z, 1.f + __expf(-act_inner<kAct>(z)));
+    return z * sigma<kAct>(z);
 }
 
 // act'(z) and act(z). With p = sigma(t(z)): act' = p + z p (1 - p) t'(z); the second term is 0 where p (1 - p) is,
@@ -37,7 +54,7 @@ __device__ __forceinline__ float act_slope(float z, float& value)
         value = z < 0.f ? 0.f : z;
         return z > 0.f ? 1.f : (z == z ? 0.f : z);  // a NaN stays one
     }
-    const float p = __fdividef(1.f, 1.f + __expf(-act_inner<kAct>(z)));
+    const float p = sigma<kAct>(z);
     value = z * p;
     const float q = p * (1.f - p);
     if (q == 0.f) return p;
@@ -177,8 +194,8 @@ __device__ __forceinline__ void store_wait_all() { asm volatile("cp.async.bulk.w
 // What a product and its epilogue work on: y[t][n] = act(sum_k a b xs[t] ws[n] + bias[n]) + r[t][n], or, gated,
 // act(g) u of the products with b's first and last N rows.
 struct Product {
-    const void* a;      // rows [M][K], or [K][M] (a_mn)
-    const void* b;      // weights [N][K] ([2][N][K] gated), or [K][N] (b_mn)
+    const void* a;      // rows [M][K]
+    const void* b;      // weights [N][K] ([2][N][K] gated), or [K][N] (b_mn: linear_rows.cu alone)
     void* y;            // [M][N] bf16
     void* z;            // [M][N] ([M][2 N] gated) bf16, or null
     const void* r;      // [M][N] bf16, or null
@@ -187,13 +204,16 @@ struct Product {
     const float* bias;  // [N], or null
     int M, N, K;
     int act;
-    bool f8, a_mn, b_mn, gated;
+    bool f8, b_mn, gated;
 };
 
 // Rows as CTA pairs' 256-row tiles / weights as rows and tokens as columns, K split over a cluster.
 int launch_product_pair(const Product& p, const char* who, cudaStream_t st);
 int launch_product_rows(const Product& p, const char* who, cudaStream_t st);
 int launch_product(const Product& p, const char* who, cudaStream_t st);
+// dx = dz W and dW = dz^T x in one launch; either may be null.
+int launch_gradients(const void* dz, const void* x, const void* W, void* dx, void* dW, int T, int N, int K, const char* who,
+                     cudaStream_t st);
 
 // dz = dy act'(z) ([T][N]; gated: dy [T][N], z and dz [T][2 N]), and with db its column sums by way of part.
 int launch_act_backward(const void* dy, const void* z, void* dz, float* db, float* part, int T, int N, int act, bool gated,

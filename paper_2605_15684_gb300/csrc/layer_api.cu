@@ -134,7 +134,7 @@ int ssba_linear(const ssba_linear_desc* desc, const void* x, const void* W, cons
     if (!aligned(x, 16) || !aligned(W, 16) || !aligned(w_scale, 16) || !aligned(bias, 16) || !aligned(r, 16) ||
         !aligned(y, 16) || !aligned(z, 16) || !aligned(x_scale, 4))
         return invalid(who, "x, W, w_scale, bias, r, y and z must be 16-byte aligned, x_scale 4-byte");
-    const Product p{x, W, y, z, r, x_scale, w_scale, bias, desc->T, desc->N, desc->K, desc->act, f8, false, false, desc->gated != 0};
+    const Product p{x, W, y, z, r, x_scale, w_scale, bias, desc->T, desc->N, desc->K, desc->act, f8, false, desc->gated != 0};
     return launch_product(p, who, static_cast<cudaStream_t>(stream));
 }
 
@@ -183,29 +183,7 @@ int ssba_linear_backward(const ssba_linear_desc* desc, const void* dy, const voi
                                  T, N, desc->act, gated, who, st);
         if (rc != SSBA_OK) return rc;
     }
-    if (dx) {
-        Product p{};
-        p.a = dz;
-        p.b = W;
-        p.y = dx;
-        p.M = T;
-        p.N = K;
-        p.K = rows;
-        p.b_mn = true;
-        rc = launch_product(p, who, st);
-        if (rc != SSBA_OK) return rc;
-    }
-    if (dW) {
-        Product p{};
-        p.a = dz;
-        p.b = x;
-        p.y = dW;
-        p.M = rows;
-        p.N = K;
-        p.K = T;
-        p.a_mn = p.b_mn = true;
-        rc = launch_product(p, who, st);
-    }
+    if (dx || dW) rc = launch_gradients(dz, x, W, dx, dW, T, rows, K, who, st);
     return rc;
 }
 

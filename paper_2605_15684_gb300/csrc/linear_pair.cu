@@ -2,14 +2,14 @@
 //
 //   y = act(a b^T xs ws + bias) + r          a [M][K], b [N][K], bf16 or e4m3 with row scales xs, ws
 //   gated: y = act(g) u,  g = a b_0^T xs ws_0,  u = a b_1^T xs ws_1
-//   backward: dx = dz W (b along its rows, "b_mn"), dW = dz^T x (both along their rows)
+//   backward, in one launch: dx = dz W, dW = dz^T x
 //
 // A tile is 256 rows x kBN columns (gated: 128 columns of g beside 128 of u) of a pair of CTAs, cta_group::2: each CTA
 // holds 128 rows of a and half of b's rows, so that a k step of 128 bytes brings 32 KB into an SM for 512 tensor
 // cycles of bf16 (one CTA alone would take 48 KB; shared memory moves 128 bytes a cycle and products read it too).
 // Gated, the first CTA holds gate rows and the second the matching up rows, so that a row's g and u meet in one
-// thread of the epilogue. Operands along K are 128-byte rows; operands along their rows ("mn") come as boxes of 64
-// columns x 64 k. e4m3 takes the same bytes: a step has 128 values of K in place of 64.
+// thread of the epilogue. Operands along K are 128-byte rows; operands along their rows ("mn": dW's both, dx's b) come as
+// boxes of 64 columns x 64 k. e4m3 takes the same bytes: a step has 128 values of K in place of 64.
 // Persistent, one CTA an SM, 320 threads:
 //   warp 0     TMA of this CTA's operands, counted on the first CTA's barriers
 //   warp 1     (first CTA) tcgen05.mma M = 256, N = kBN into one of two accumulators; commits reach both CTAs
@@ -58,12 +58,23 @@ struct __align__(1024) PairSmem {
 };
 
 struct PairMaps {
-    CUtensorMap a, b, y, z, r;
+    CUtensorMap a, b, y, z, r;  // kBare: a, b, y of dx; dW's below
+    CUtensorMap a2, b2, y2;
 };
 
-struct PairParams {
-    int M, N, K;
+struct Tiles {
     int m_tiles, n_tiles, tiles, ksteps;
+};
+
+// A launch has one set of tiles, or (kBare) two, dx's and dW's: set `first`, then the other. Pair q of P takes
+// tiles q, q + P ... of the first set; those of the second are dealt out so that the pairs with a tile more of the
+// first (q < over) take fewer: n_over each, the others n_rest.
+struct PairParams {
+    int M, N;
+    int M2, N2;
+    Tiles set[2];
+    int first, pairs, over, n_over, n_rest;
+    int first_tiles, other_tiles, rounds;  // rounds: whole ones of the first set
     int act;
     int has_r;
     const float *xs, *ws, *bias;
@@ -71,12 +82,31 @@ struct PairParams {
     uint64_t budget_ns;
 };
 
-__device__ __forceinline__ void tile_at(const PairParams& p, int t, int& m, int& n)
+// The k-th tile of pair q: which set, and the tile's row and column of tiles. Within a set, tiles go through the rows in
+// bands of kBand.
+struct Item {
+    int set, m, n, ksteps;
+};
+
+__device__ __forceinline__ bool item_at(const PairParams& p, int q, int k, Item& o)
 {
-    const int band = t / (kBand * p.n_tiles), in = t - band * kBand * p.n_tiles;
-    const int rows = min(kBand, p.m_tiles - band * kBand);
-    n = in / rows;
-    m = band * kBand + in - n * rows;
+    o.set = p.first;
+    int t = q + k * p.pairs;
+    if (t >= p.first_tiles) {
+        const bool over = q < p.over;
+        const int j = k - p.rounds - (over ? 1 : 0);
+        if (j >= (over ? p.n_over : p.n_rest)) return false;
+        o.set = 1 - p.first;
+        t = over ? p.n_rest * (p.pairs - p.over) + j * p.over + q : j * (p.pairs - p.over) + q - p.over;
+        if (t >= p.other_tiles) return false;
+    }
+    const int n_tiles = o.set ? p.set[1].n_tiles : p.set[0].n_tiles, m_tiles = o.set ? p.set[1].m_tiles : p.set[0].m_tiles;
+    o.ksteps = o.set ? p.set[1].ksteps : p.set[0].ksteps;
+    const int band = t / (kBand * n_tiles), in = t - band * kBand * n_tiles;
+    const int rows = min(kBand, m_tiles - band * kBand);
+    o.n = in / rows;
+    o.m = band * kBand + in - o.n * rows;
+    return true;
 }
 
 // 32 values of z to act(z), with the branch on the activation outside the loop.
@@ -123,26 +153,30 @@ __device__ __forceinline__ void add_half(const uint8_t* box, int row, int half, 
     }
 }
 
-// v *= xs ws[c ..], v += bias[c ..]; N, a multiple of 8, bounds the columns.
-__device__ __forceinline__ void scale_bias(float (&v)[32], float xs, const float* ws, const float* bias, int c, int N)
+// v *= xs ws[c ..] and v += bias[c ..] over 32 columns; N, a multiple of 8, bounds them.
+__device__ __forceinline__ void scale32(float (&v)[32], float xs, const float* ws, int c, int N)
 {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         if (c + 4 * j >= N) break;
-        if (ws) {
-            const float4 w = __ldg(reinterpret_cast<const float4*>(ws + c) + j);
-            v[4 * j] *= xs * w.x;
-            v[4 * j + 1] *= xs * w.y;
-            v[4 * j + 2] *= xs * w.z;
-            v[4 * j + 3] *= xs * w.w;
-        }
-        if (bias) {
-            const float4 w = __ldg(reinterpret_cast<const float4*>(bias + c) + j);
-            v[4 * j] += w.x;
-            v[4 * j + 1] += w.y;
-            v[4 * j + 2] += w.z;
-            v[4 * j + 3] += w.w;
-        }
+        const float4 w = __ldg(reinterpret_cast<const float4*>(ws + c) + j);
+        v[4 * j] *= xs * w.x;
+        v[4 * j + 1] *= xs * w.y;
+        v[4 * j + 2] *= xs * w.z;
+        v[4 * j + 3] *= xs * w.w;
+    }
+}
+
+__device__ __forceinline__ void bias32(float (&v)[32], const float* bias, int c, int N)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if (c + 4 * j >= N) break;
+        const float4 w = __ldg(reinterpret_cast<const float4*>(bias + c) + j);
+        v[4 * j] += w.x;
+        v[4 * j + 1] += w.y;
+        v[4 * j + 2] += w.z;
+        v[4 * j + 3] += w.w;
     }
 }
 
@@ -151,21 +185,20 @@ __device__ __forceinline__ void tmem_get(float (&v)[32], uint32_t at)
     tmem_ld_32x32b_x32(at, reinterpret_cast<uint32_t*>(v));
 }
 
-template <int kBN, bool kF8, bool kAmn, bool kBmn, int kEpi, bool kZ>
+template <int kBN, bool kF8, int kEpi, bool kZ>
 __global__ void __launch_bounds__(kThreads, 1) ssba_product_pair_kernel(const __grid_constant__ PairMaps maps, const PairParams p)
 {
     using C = PairCfg<kBN, kZ>;
     constexpr int kStages = C::kStages;
-    constexpr int kBK = kF8 ? 128 : 64;               // values of K a step
+    constexpr int kBK = kF8 ? 128 : 64;                    // values of K a step
     constexpr int kCols = kEpi == kGated ? kBN / 2 : kBN;  // output columns of a tile
     constexpr uint32_t kStep = kABytes + C::kBBytes;
-    constexpr uint32_t kIdesc = idesc_of(kF8, 256, kBN, kAmn, kBmn);
     extern __shared__ uint8_t smem_raw[];
     PairSmem<kBN, kZ>& sm = *reinterpret_cast<PairSmem<kBN, kZ>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                                                   ~static_cast<uintptr_t>(1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
-    const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
+    const int pair = blockIdx.x >> 1;
     volatile int* abortf = &sm.abort_flag;
 
     if (threadIdx.x == 0) {
@@ -192,18 +225,20 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_product_pair_kernel(const __
     tc_fence_after();
     const uint32_t tbase = sm.tmem_base;
     bool dead = false;
+    Item o;
 
     if (warp == 0) {
         // ------------------------------------------------------------ this CTA's operands
         uint32_t g = 0;
         if (lane == 0) {
-            for (int t = first; t < p.tiles && !dead; t += step) {
-                int m, n;
-                tile_at(p, t, m, n);
-                const int m0 = m * 256 + (int)rank * 128;
-                const int n0 = kEpi == kGated ? n * kCols : n * kBN + (int)rank * (kBN / 2);
+            for (int it = 0; !dead && item_at(p, pair, it, o); ++it) {
+                const int m0 = o.m * 256 + (int)rank * 128;
+                const int n0 = kEpi == kGated ? o.n * kCols : o.n * kBN + (int)rank * (kBN / 2);
                 const int plane = kEpi == kGated ? (int)rank : 0;
-                for (int k = 0; k < p.ksteps; ++k, ++g) {
+                const bool second = kEpi == kBare && o.set == 1;
+                const CUtensorMap *ma = second ? &maps.a2 : &maps.a, *mb = second ? &maps.b2 : &maps.b;
+                const int ksteps = o.ksteps;
+                for (int k = 0; k < ksteps; ++k, ++g) {
                     const uint32_t s = g % kStages;
                     if (!mbar_wait(smem_u32(&sm.empty[s]), ((g / kStages) & 1) ^ 1, abortf, p.budget_ns)) {
                         dead = true;
@@ -213,18 +248,18 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_product_pair_kernel(const __
                     const uint32_t bar = at_rank(smem_u32(&sm.full[s]), 0);
                     if (rank == 0) mbar_arrive_expect_tx(smem_u32(&sm.full[s]), 2 * kStep);
                     const uint32_t a = smem_u32(&sm.a[s][0]), b = smem_u32(&sm.b[s][0]);
-                    if constexpr (kAmn) {
-                        tma_load_pair(a, &maps.a, bar, m0, k * kBK, 0);
-                        tma_load_pair(a + 8192, &maps.a, bar, m0 + 64, k * kBK, 0);
+                    if (second) {
+                        tma_load_pair(a, ma, bar, m0, k * kBK, 0);
+                        tma_load_pair(a + 8192, ma, bar, m0 + 64, k * kBK, 0);
                     } else {
-                        tma_load_pair(a, &maps.a, bar, k * kBK, m0, 0);
+                        tma_load_pair(a, ma, bar, k * kBK, m0, 0);
                     }
-                    if constexpr (kBmn) {
+                    if constexpr (kEpi == kBare) {
 #pragma unroll
                         for (int i = 0; i < kBN / 128; ++i)
-                            tma_load_pair(b + 8192 * i, &maps.b, bar, n0 + 64 * i, k * kBK, 0);
+                            tma_load_pair(b + 8192 * i, mb, bar, n0 + 64 * i, k * kBK, 0);
                     } else {
-                        tma_load_pair(b, &maps.b, bar, k * kBK, n0, plane);
+                        tma_load_pair(b, mb, bar, k * kBK, n0, plane);
                     }
                 }
             }
@@ -238,9 +273,10 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_product_pair_kernel(const __
     } else if (warp == 1) {
         // ------------------------------------------------------------ products, by the first CTA
         if (rank == 0 && elect_one_sync()) {
-            uint32_t g = 0, it = 0;
+            constexpr bool kBmn = kEpi == kBare;
+            uint32_t g = 0;
             const uint32_t a0 = smem_u32(&sm.a[0][0]), b0 = smem_u32(&sm.b[0][0]);
-            for (int t = first; t < p.tiles && !dead; t += step, ++it) {
+            for (uint32_t it = 0; !dead && item_at(p, pair, (int)it, o); ++it) {
                 const uint32_t acc = it & 1;
                 if (!mbar_wait(smem_u32(&sm.acc_empty[acc]), ((it >> 1) & 1) ^ 1, abortf, p.budget_ns)) {
                     dead = true;
@@ -248,21 +284,26 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_product_pair_kernel(const __
                 }
                 tc_fence_after();
                 const uint32_t d = tbase + acc * kBN;
-                for (int k = 0; k < p.ksteps; ++k, ++g) {
+                // 16 k are 2 KB of an operand along its rows, 32 bytes of one along K
+                const bool amn = kEpi == kBare && o.set == 1;
+                const uint32_t idesc = amn ? idesc_of(kF8, 256, kBN, true, kBmn) : idesc_of(kF8, 256, kBN, false, kBmn);
+                const uint32_t a_lbo = amn ? 8192 : 16;
+                const uint64_t a_step = amn ? 128 : 2;
+                const int ksteps = o.ksteps;
+                for (int k = 0; k < ksteps; ++k, ++g) {
                     const uint32_t s = g % kStages;
                     if (!mbar_wait(smem_u32(&sm.full[s]), (g / kStages) & 1, abortf, p.budget_ns)) {
                         dead = true;
                         break;
                     }
                     tc_fence_after();
-                    const uint64_t ad = sdesc_sw128(a0 + s * kABytes, kAmn ? 8192 : 16, 1024);
+                    const uint64_t ad = sdesc_sw128(a0 + s * kABytes, a_lbo, 1024);
                     const uint64_t bd = sdesc_sw128(b0 + s * C::kBBytes, kBmn ? 8192 : 16, 1024);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)  // 16 k along rows are 2 KB, along K 32 bytes
-                        mma<kF8, true>(d, ad + (uint64_t)(i * (kAmn ? 128 : 2)), bd + (uint64_t)(i * (kBmn ? 128 : 2)),
-                                       kIdesc, (k | i) != 0 ? 1u : 0u);
+                    for (int i = 0; i < 4; ++i)
+                        mma<kF8, true>(d, ad + i * a_step, bd + (uint64_t)(i * (kBmn ? 128 : 2)), idesc, (k | i) != 0 ? 1u : 0u);
                     commit_pair(smem_u32(&sm.empty[s]));
-                    if (k == p.ksteps - 1) commit_pair(smem_u32(&sm.acc_full[acc]));
+                    if (k == ksteps - 1) commit_pair(smem_u32(&sm.acc_full[acc]));
                 }
             }
             if (dead) {
@@ -277,20 +318,21 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_product_pair_kernel(const __
         constexpr int kChunks = kEpi == kGated ? 1 : kBN / 128;  // of 64 columns a warp
         uint8_t(*box)[kBoxBytes] = sm.box[w];
         const uint32_t empty0 = at_rank(smem_u32(&sm.acc_empty[0]), 0), empty1 = at_rank(smem_u32(&sm.acc_empty[1]), 0);
-        uint32_t it = 0, nres = 0, nbox = 0;
-        for (int t = first; t < p.tiles && !dead; t += step, ++it) {
-            int m, n;
-            tile_at(p, t, m, n);
-            const int row0 = m * 256 + (int)rank * 128 + 32 * quad, row = row0 + lane;
-            const int col0 = n * kCols + half * (kCols / 2);
+        uint32_t nres = 0, nbox = 0;
+        for (uint32_t it = 0; item_at(p, pair, (int)it, o); ++it) {
+            const bool second = kEpi == kBare && o.set == 1;
+            const int M = second ? p.M2 : p.M, N = second ? p.N2 : p.N;
+            const CUtensorMap* my = second ? &maps.y2 : &maps.y;
+            const int row0 = o.m * 256 + (int)rank * 128 + 32 * quad, row = row0 + lane;
+            const int col0 = o.n * kCols + half * (kCols / 2);
             const uint32_t acc = it & 1;
             bool res = false;
             if constexpr (kEpi == kPlain) {
-                res = p.has_r && row0 < p.M && col0 < p.N;
+                res = p.has_r && row0 < M && col0 < N;
                 if (res) {
                     if (lane == 0) {
                         store_wait_read<0>();
-                        const int boxes = kChunks == 2 && col0 + 64 < p.N ? 2 : 1;
+                        const int boxes = kChunks == 2 && col0 + 64 < N ? 2 : 1;
                         mbar_arrive_expect_tx(smem_u32(&sm.res[w]), boxes * kBoxBytes);
                         for (int c = 0; c < boxes; ++c)
                             tma_load_3d(smem_u32(box[c]), &maps.r, smem_u32(&sm.res[w]), col0 + 64 * c, row0, 0);
@@ -298,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_product_pair_kernel(const __
                     __syncwarp();
                 }
             }
-            const float xs = kEpi != kBare && p.xs && row < p.M ? p.xs[row] : 1.f;
+            const float xs = kEpi != kBare && p.xs && row < M ? p.xs[row] : 1.f;
             bool ok = mbar_wait(smem_u32(&sm.acc_full[acc]), (it >> 1) & 1, abortf, p.budget_ns);
             tc_fence_after();
             if constexpr (kEpi == kPlain) {
@@ -311,71 +353,73 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_product_pair_kernel(const __
                 dead = true;
                 break;
             }
-            const uint32_t taddr = tbase + ((uint32_t)(32 * quad) << 16) + acc * kBN;
+            const uint32_t taddr = tbase + ((uint32_t)(32 * quad) << 16) + acc * kBN + half * (kCols / 2);
+            // pieces of 32 columns; the next one's values are on their way while one is worked on (gated: there are two a piece)
+            constexpr int kPieces = 2 * kChunks;
+            float v[kEpi == kGated ? 1 : 2][32], u[32];
+            if constexpr (kEpi != kGated) tmem_get(v[0], taddr);
+            uint8_t *by = nullptr, *bz = nullptr, *bu = nullptr;
 #pragma unroll
-            for (int c = 0; c < kChunks; ++c) {
-                const int col = col0 + 64 * c;
-                const bool live = row0 < p.M && col < p.N;
-                // the chunk's boxes: with a residual, or with z, by chunk; else in turn
-                uint8_t *by, *bz, *bu;
-                if (kZ) {
-                    by = box[kEpi == kGated ? 0 : c];
-                    bz = box[kEpi == kGated ? 1 : 2];
-                    bu = box[2];
-                    if (live) {
-                        if (lane == 0) store_wait_read<0>();
-                        __syncwarp();
-                    }
-                } else {
-                    by = box[kEpi == kPlain && p.has_r ? c : (nbox & 1)];
-                    bz = bu = nullptr;
-                    if (live && !(kEpi == kPlain && p.has_r)) {
-                        ++nbox;
-                        if (lane == 0) store_wait_read<1>();
-                        __syncwarp();
-                    }
-                }
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    float v[32];
-                    if constexpr (kEpi == kGated) {
-                        float u[32];
-                        tmem_get(v, taddr + half * 64 + 32 * q);
-                        tmem_get(u, taddr + kBN / 2 + half * 64 + 32 * q);
-                        tmem_wait_ld();
-                        if (p.ws) {
-                            scale_bias(v, xs, p.ws, nullptr, col + 32 * q, p.N);
-                            scale_bias(u, xs, p.ws + p.N, nullptr, col + 32 * q, p.N);
+            for (int i = 0; i < kPieces; ++i) {
+                const int c = i >> 1, q = i & 1, col = col0 + 64 * c;
+                const bool live = row0 < M && col < N;
+                float(&x)[32] = v[kEpi == kGated ? 0 : i & 1];
+                if (q == 0) {
+                    // the chunk's boxes: with a residual, or with z, by chunk; else in turn
+                    if (kZ) {
+                        by = box[kEpi == kGated ? 0 : c];
+                        bz = box[kEpi == kGated ? 1 : 2];
+                        bu = box[2];
+                        if (live) {
+                            if (lane == 0) store_wait_read<0>();
+                            __syncwarp();
                         }
-                        if (kZ && live) {
-                            put_half(bz, lane, q, v);
-                            put_half(bu, lane, q, u);
-                        }
-                        activate(v, p.act);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] *= u[i];
                     } else {
-                        tmem_get(v, taddr + half * (kBN / 2) + 64 * c + 32 * q);
-                        tmem_wait_ld();
-                        if constexpr (kEpi == kPlain) {
-                            scale_bias(v, xs, p.ws, p.bias, col + 32 * q, p.N);
-                            if (kZ && live) put_half(bz, lane, q, v);
-                            activate(v, p.act);
-                            if (res && live) add_half(by, lane, q, v);
+                        by = box[kEpi == kPlain && p.has_r ? c : (nbox & 1)];
+                        if (live && !(kEpi == kPlain && p.has_r)) {
+                            ++nbox;
+                            if (lane == 0) store_wait_read<1>();
+                            __syncwarp();
                         }
                     }
-                    if (c == kChunks - 1 && q == 1) {  // the accumulator has been read
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) arrive_cluster(acc ? empty1 : empty0);
-                    }
-                    if (live) put_half(by, lane, q, v);
                 }
-                if (live) {
+                if constexpr (kEpi == kGated) {
+                    tmem_get(x, taddr + 32 * i);
+                    tmem_get(u, taddr + kBN / 2 + 32 * i);
+                }
+                tmem_wait_ld();
+                if (i + 1 < kPieces) {
+                    if constexpr (kEpi != kGated) tmem_get(v[(i + 1) & 1], taddr + 32 * (i + 1));
+                } else {  // the accumulator has been read
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive_cluster(acc ? empty1 : empty0);
+                }
+                if constexpr (kEpi == kGated) {
+                    if (p.ws) {
+                        scale32(x, xs, p.ws, col + 32 * q, N);
+                        scale32(u, xs, p.ws + N, col + 32 * q, N);
+                    }
+                    if (kZ && live) {
+                        put_half(bz, lane, q, x);
+                        put_half(bu, lane, q, u);
+                    }
+                    activate(x, p.act);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) x[e] *= u[e];
+                } else if constexpr (kEpi == kPlain) {
+                    if (p.ws) scale32(x, xs, p.ws, col + 32 * q, N);
+                    if (p.bias) bias32(x, p.bias, col + 32 * q, N);
+                    if (kZ && live) put_half(bz, lane, q, x);
+                    activate(x, p.act);
+                    if (res && live) add_half(by, lane, q, x);
+                }
+                if (live) put_half(by, lane, q, x);
+                if (q == 1 && live) {
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) {
-                        tma_store(&maps.y, smem_u32(by), col, row0, 0);
+                        tma_store(my, smem_u32(by), col, row0, 0);
                         if (kZ) {
                             tma_store(&maps.z, smem_u32(bz), col, row0, 0);
                             if (kEpi == kGated) tma_store(&maps.z, smem_u32(bu), col, row0, 1);
@@ -425,57 +469,95 @@ int pairs_at_once(Kernel k, size_t smem)
     return n;
 }
 
-template <int kBN, bool kF8, bool kAmn, bool kBmn, int kEpi, bool kZ>
-int launch_as(const Product& q, const char* who, cudaStream_t st)
+template <int kBN, bool kF8, int kEpi, bool kZ>
+int launch_pairs(PairMaps& maps, PairParams& p, const char* who, cudaStream_t st)
 {
-    constexpr int kBK = kF8 ? 128 : 64, kCols = kEpi == kGated ? kBN / 2 : kBN;
-    auto kernel = ssba_product_pair_kernel<kBN, kF8, kAmn, kBmn, kEpi, kZ>;
+    auto kernel = ssba_product_pair_kernel<kBN, kF8, kEpi, kZ>;
     const size_t smem = sizeof(PairSmem<kBN, kZ>) + 1024;
     static PerDeviceOnce attr;
     attr.run([=] { cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
-    const int e = kF8 ? 1 : 2;
-    PairMaps maps;
-    memset(&maps, 0, sizeof(maps));
-    const uint64_t M = q.M, N = q.N, K = q.K, planes = kEpi == kGated ? 2 : 1;
-    bool ok = kAmn ? encode_map(&maps.a, q.a, kF8, M, K, 1, M * e, M * K * e, 64, 64)
-                   : encode_map(&maps.a, q.a, kF8, K, M, 1, K * e, M * K * e, kBK, 128);
-    ok = ok && (kBmn ? encode_map(&maps.b, q.b, kF8, N, K, 1, N * e, N * K * e, 64, 64)
-                     : encode_map(&maps.b, q.b, kF8, K, N, planes, K * e, N * K * e, kBK, kBN / 2));
-    ok = ok && encode_map(&maps.y, q.y, false, N, M, 1, N * 2, M * N * 2, 64, 32);
-    if (kZ) ok = ok && encode_map(&maps.z, q.z, false, N, M, planes, planes * N * 2, N * 2, 64, 32);
-    if (q.r) ok = ok && encode_map(&maps.r, q.r, false, N, M, 1, N * 2, M * N * 2, 64, 32);
-    if (!ok) {
-        set_error("%s: cuTensorMapEncodeTiled failed", who);
-        return SSBA_ERR_CUDA;
-    }
-    PairParams p = {};
-    p.M = q.M;
-    p.N = q.N;
-    p.K = q.K;
-    p.m_tiles = (q.M + 255) / 256;
-    p.n_tiles = (q.N + kCols - 1) / kCols;
-    p.tiles = p.m_tiles * p.n_tiles;
-    p.ksteps = (q.K + kBK - 1) / kBK;
-    p.act = q.act;
-    p.has_r = q.r != nullptr;
-    p.xs = q.xs;
-    p.ws = q.ws;
-    p.bias = q.bias;
     p.budget_ns = kWaitBudgetNs;
     p.status = device_status_word();
     if (!p.status) {
         set_error("%s: could not resolve the device status word", who);
         return SSBA_ERR_CUDA;
     }
+    // Pairs, and how the second set's tiles go to them: the last pair to end ends as early as it can.
+    const long long all = (long long)p.set[0].tiles + p.set[1].tiles;
     const int most = pairs_at_once(kernel, smem);
-    const int pairs = p.tiles < most ? p.tiles : most;
+    const int P = p.pairs = (int)(all < most ? all : most);
+    long long best = -1;
+    for (int f = 0; f < 2; ++f) {
+        const Tiles &a = p.set[f], &b = p.set[1 - f];
+        if (!a.tiles) continue;
+        const int over = a.tiles % P, c = a.tiles / P;
+        const int top = over ? (b.tiles + P - 1) / P : 0;
+        for (int n = 0; n <= top; ++n) {
+            const long long left = (long long)b.tiles - (long long)n * over;
+            const int rest = left > 0 ? (int)((left + P - over - 1) / (P - over)) : 0;
+            const long long t0 = over ? (c + 1ll) * a.ksteps + (long long)n * b.ksteps : 0, t1 = (long long)c * a.ksteps + (long long)rest * b.ksteps;
+            const long long end = t0 > t1 ? t0 : t1;
+            if (best < 0 || end < best) {
+                best = end;
+                p.first = f;
+                p.over = over;
+                p.n_over = n;
+                p.n_rest = rest;
+            }
+        }
+    }
+    p.first_tiles = p.set[p.first].tiles;
+    p.other_tiles = p.set[1 - p.first].tiles;
+    p.rounds = p.first_tiles / P;
     // In stream order, neither beginning before the grid in front has ended nor letting the next one begin. Pairs that
     // were set up beside the last waves of another grid (a gated block's backward pass, many calls queued)
     // did not end; a launch of its own costs about 2 us.
-    const cudaError_t err = launch_on(false, kernel, dim3(2 * pairs), kThreads, smem, st, 2, maps, p);
+    const cudaError_t err = launch_on(false, kernel, dim3(2 * P), kThreads, smem, st, 2, maps, p);
     if (err == cudaSuccess) return SSBA_OK;
     set_error("%s: ssba_product_pair_kernel launch: %s", who, cudaGetErrorString(err));
     return SSBA_ERR_CUDA;
+}
+
+Tiles tiles_of(long long M, long long N, long long K, int cols, int bk)
+{
+    Tiles t;
+    t.m_tiles = (int)((M + 255) / 256);
+    t.n_tiles = (int)((N + cols - 1) / cols);
+    t.tiles = t.m_tiles * t.n_tiles;
+    t.ksteps = (int)((K + bk - 1) / bk);
+    return t;
+}
+
+int no_maps(const char* who)
+{
+    set_error("%s: cuTensorMapEncodeTiled failed", who);
+    return SSBA_ERR_CUDA;
+}
+
+template <int kBN, bool kF8, int kEpi, bool kZ>
+int launch_as(const Product& q, const char* who, cudaStream_t st)
+{
+    constexpr int kBK = kF8 ? 128 : 64, kCols = kEpi == kGated ? kBN / 2 : kBN;
+    const int e = kF8 ? 1 : 2;
+    PairMaps maps;
+    memset(&maps, 0, sizeof(maps));
+    const uint64_t M = q.M, N = q.N, K = q.K, planes = kEpi == kGated ? 2 : 1;
+    bool ok = encode_map(&maps.a, q.a, kF8, K, M, 1, K * e, 0, kBK, 128) &&
+              encode_map(&maps.b, q.b, kF8, K, N, planes, K * e, N * K * e, kBK, kBN / 2) &&
+              encode_map(&maps.y, q.y, false, N, M, 1, N * 2, 0, 64, 32);
+    if (kZ) ok = ok && encode_map(&maps.z, q.z, false, N, M, planes, planes * N * 2, N * 2, 64, 32);
+    if (q.r) ok = ok && encode_map(&maps.r, q.r, false, N, M, 1, N * 2, 0, 64, 32);
+    if (!ok) return no_maps(who);
+    PairParams p = {};
+    p.M = q.M;
+    p.N = q.N;
+    p.set[0] = tiles_of(q.M, q.N, q.K, kCols, kBK);
+    p.act = q.act;
+    p.has_r = q.r != nullptr;
+    p.xs = q.xs;
+    p.ws = q.ws;
+    p.bias = q.bias;
+    return launch_pairs<kBN, kF8, kEpi, kZ>(maps, p, who, st);
 }
 
 }  // namespace
@@ -483,22 +565,55 @@ int launch_as(const Product& q, const char* who, cudaStream_t st)
 int launch_product_pair(const Product& q, const char* who, cudaStream_t st)
 {
     if (q.gated) {
-        if (q.f8) return q.z ? launch_as<256, true, false, false, kGated, true>(q, who, st) : launch_as<256, true, false, false, kGated, false>(q, who, st);
-        return q.z ? launch_as<256, false, false, false, kGated, true>(q, who, st) : launch_as<256, false, false, false, kGated, false>(q, who, st);
+        if (q.f8) return q.z ? launch_as<256, true, kGated, true>(q, who, st) : launch_as<256, true, kGated, false>(q, who, st);
+        return q.z ? launch_as<256, false, kGated, true>(q, who, st) : launch_as<256, false, kGated, false>(q, who, st);
     }
-    // 256 columns a tile, or 128 where their rounds over the SMs are shorter in all (a 128-column step takes the
-    // same bytes of a for half the products)
+    if (q.z) return q.f8 ? launch_as<256, true, kPlain, true>(q, who, st) : launch_as<256, false, kPlain, true>(q, who, st);
+    // 256 columns a tile, or 128 where that needs no more rounds over the SMs: a 128-column step brings three quarters of
+    // the bytes for half the products, and takes 0.9 of the time (dx of 5001 rows, 2048 columns, K 11264)
     const long long pairs = device_sm_count() / 2 > 0 ? device_sm_count() / 2 : 1, mt = (q.M + 255) / 256;
     const long long wide = (mt * ((q.N + 255) / 256) + pairs - 1) / pairs, narrow = (mt * ((q.N + 127) / 128) + pairs - 1) / pairs;
-    const bool half = 11 * narrow < 20 * wide;
-    if (q.a_mn) return half ? launch_as<128, false, true, true, kBare, false>(q, who, st) : launch_as<256, false, true, true, kBare, false>(q, who, st);
-    if (q.b_mn) return half ? launch_as<128, false, false, true, kBare, false>(q, who, st) : launch_as<256, false, false, true, kBare, false>(q, who, st);
-    if (q.f8) {
-        if (q.z) return launch_as<256, true, false, false, kPlain, true>(q, who, st);
-        return half ? launch_as<128, true, false, false, kPlain, false>(q, who, st) : launch_as<256, true, false, false, kPlain, false>(q, who, st);
+    const bool half = 9 * narrow < 10 * wide;
+    if (q.f8) return half ? launch_as<128, true, kPlain, false>(q, who, st) : launch_as<256, true, kPlain, false>(q, who, st);
+    return half ? launch_as<128, false, kPlain, false>(q, who, st) : launch_as<256, false, kPlain, false>(q, who, st);
+}
+
+int launch_gradients(const void* dz, const void* x, const void* W, void* dx, void* dW, int T, int N, int K, const char* who,
+                     cudaStream_t st)
+{
+    if (dx && T <= 256) {  // few rows: the weights as the tensor cores' rows
+        Product q{};
+        q.a = dz;
+        q.b = W;
+        q.y = dx;
+        q.M = T;
+        q.N = K;
+        q.K = N;
+        q.b_mn = true;
+        const int rc = launch_product_rows(q, who, st);
+        if (rc != SSBA_OK || !dW) return rc;
+        dx = nullptr;
     }
-    if (q.z) return launch_as<256, false, false, false, kPlain, true>(q, who, st);
-    return half ? launch_as<128, false, false, false, kPlain, false>(q, who, st) : launch_as<256, false, false, false, kPlain, false>(q, who, st);
+    PairMaps maps;
+    memset(&maps, 0, sizeof(maps));
+    PairParams p = {};
+    const uint64_t t = T, n = N, k = K;
+    bool ok = true;
+    if (dx) {
+        ok = encode_map(&maps.a, dz, false, n, t, 1, n * 2, 0, 64, 128) && encode_map(&maps.b, W, false, k, n, 1, k * 2, 0, 64, 64) &&
+             encode_map(&maps.y, dx, false, k, t, 1, k * 2, 0, 64, 32);
+        p.M = T;
+        p.N = K;
+        p.set[0] = tiles_of(T, K, N, 256, 64);
+    }
+    if (dW) {
+        ok = ok && encode_map(&maps.a2, dz, false, n, t, 1, n * 2, 0, 64, 64) && encode_map(&maps.b2, x, false, k, t, 1, k * 2, 0, 64, 64) &&
+             encode_map(&maps.y2, dW, false, k, n, 1, k * 2, 0, 64, 32);
+        p.M2 = N;
+        p.N2 = K;
+        p.set[1] = tiles_of(N, K, T, 256, 64);
+    }
+    return ok ? launch_pairs<256, false, kBare, false>(maps, p, who, st) : no_maps(who);
 }
 
 }  // namespace layer

@@ -324,7 +324,6 @@ int launch_product_rows(const Product& q, const char* who, cudaStream_t st)
 
 int launch_product(const Product& q, const char* who, cudaStream_t st)
 {
-    if (q.a_mn) return launch_product_pair(q, who, st);
     return q.M <= 256 ? launch_product_rows(q, who, st) : launch_product_pair(q, who, st);
 }
 

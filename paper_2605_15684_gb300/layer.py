@@ -3,7 +3,8 @@ and what follows them, the gated half of a feed-forward block, rotary positions 
 the gradients of each.
 
 Argument marshalling only, as in api.py: tensors are checked, outputs and workspaces allocated on the call's
-stream, and every step runs in the library's kernels on the current device.
+stream, and every step runs in the library's kernels on the current device. Calls on the current stream that leave
+their outputs to be allocated take a native short way (csrc/host/layer_call.cpp).
 
     y, h, rstd = rms_norm(x, w, residual=r)            # h = x + r, y = its norm
     q, s, h, rstd = rms_norm(x, w, residual=r, e4m3=True)
@@ -15,12 +16,14 @@ stream, and every step runs in the library's kernels on the current device.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
+import os
 
 import torch
 
-from . import api
+from . import api, build
 from .api import (SSBA_BF16, SSBA_ERR_INVALID, SSBA_FP32, SsbaError, _check, _empty, _out, _raise_on, _side,
-                  _stream_ptr, load_library)
+                  _lock, _stream_ptr, load_library)
 
 SSBA_E4M3 = 2
 E4M3 = torch.float8_e4m3fn
@@ -39,6 +42,28 @@ class _RopeDesc(ctypes.Structure):
                 ("axes", ctypes.c_int32), ("sections", ctypes.c_int32 * ROPE_MAX_AXES), ("layout", ctypes.c_int32),
                 ("shared", ctypes.c_int32), ("inverse", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("base", ctypes.c_double)]
+
+
+_ext = None
+
+
+def _extension():
+    """The native short way into the calls (csrc/host/layer_call.cpp), made by build() beside the library."""
+    global _ext
+    lib = load_library()
+    with _lock:
+        if _ext is None:
+            path = build.call_file("layer_call")
+            if not os.path.exists(path):
+                raise SsbaError(api.SSBA_ERR_CUDA, f"{path} is missing: run paper_2605_15684_gb300.build.build()")
+            spec = importlib.util.spec_from_file_location("_layer_call", path)
+            ext = importlib.util.module_from_spec(spec)
+            spec.loader.exec_module(ext)
+            ext.bind(*(ctypes.cast(getattr(lib, "ssba_" + n), ctypes.c_void_p).value
+                       for n in ("rms_norm", "rms_norm_backward", "rms_norm_backward_workspace_bytes", "linear", "linear_backward",
+                                 "linear_backward_workspace_bytes", "rope_axes")))
+            _ext = ext
+    return _ext
 
 
 def _invalid(msg: str):
@@ -103,6 +128,12 @@ def rms_norm(x, w, residual=None, eps: float = 1e-6, e4m3: bool = False, y=None,
     """ssba_rms_norm: x [T, D] bf16 or fp32, w [D] fp32 -> (y, h, rstd), or with e4m3 (y, scale, h, rstd): h = x +
     residual (x itself without one), y its norm times w (e4m3: values whose rows stand for themselves times scale [T], a power
     of two), rstd [T] fp32 for rms_norm_backward. ``h`` may be x or residual, ``y`` (not e4m3) may be x."""
+    if stream is None and y is None and h is None and rstd is None and scale is None:
+        out = (_ext or _extension()).rms_norm(x, w, residual, eps, e4m3)
+        if out.__class__ is tuple:
+            return out
+        if out is not None:
+            _raise_on(out)
     lib = load_library()
     T, D = _matrix(x, "x", _NORM_TYPES)
     dt, dev = x.dtype, x.device
@@ -137,6 +168,12 @@ def rms_norm_backward_workspace_bytes(T: int, D: int, dtype=torch.bfloat16) -> i
 def rms_norm_backward(dy, h, w, rstd, dh=None, dx=None, dw=None, workspace=None, stream=None):
     """ssba_rms_norm_backward: dy, and the h (or x) and rstd of the forward call -> (dx [T, D], dw [D] fp32); dx is the
     gradient of x and of the residual alike, with ``dh``, which reaches h from elsewhere, added. ``dx`` may be dy or dh."""
+    if stream is None and dx is None and dw is None and workspace is None:
+        out = (_ext or _extension()).rms_norm_backward(dy, h, w, rstd, dh)
+        if out.__class__ is tuple:
+            return out
+        if out is not None:
+            _raise_on(out)
     lib = load_library()
     T, D = _matrix(h, "h", _NORM_TYPES)
     dt, dev = h.dtype, h.device
@@ -158,6 +195,12 @@ def rms_norm_backward(dy, h, w, rstd, dh=None, dx=None, dw=None, workspace=None,
 
 
 def _product(x, W, bias, residual, act, x_scale, w_scale, pre, y, z, stream, gated):
+    if stream is None and y is None and z is None:
+        out = (_ext or _extension()).linear(x, W, bias, residual, x_scale, w_scale, _act(act, gated), pre, gated)
+        if out.__class__ is int:
+            _raise_on(out)
+        if out is not None:
+            return out
     lib = load_library()
     T, K = _matrix(x, "x", (torch.bfloat16, E4M3))
     rows, k = _matrix(W, "W", (x.dtype,))
@@ -209,6 +252,12 @@ def linear_backward_workspace_bytes(T: int, N: int, K: int, act=None, gated: boo
 
 
 def _product_backward(dy, x, W, z, act, db, dx, dW, workspace, stream, gated, bias):
+    if stream is None and dx is None and dW is None and db is None and workspace is None:
+        out = (_ext or _extension()).linear_backward(dy, x, W, z if act is not None else None, _act(act, gated), gated, bias)
+        if out.__class__ is tuple:
+            return out
+        if out is not None:
+            _raise_on(out)
     lib = load_library()
     bf = torch.bfloat16
     T, N = _matrix(dy, "dy", (bf,))
@@ -311,6 +360,12 @@ def rope_axes(x, positions, axes, base: float = 10000.0, layout: str = "pairs", 
     behind them as they were. layout "pairs" (2j, 2j + 1) or "halves" (j, j + sum(axes)); shared False: each axis has the whole range
     of rates, True: the pairs share one. inverse: by the negative angles, which gives the gradient. ``out``: of
     x's shape at any strides; x itself for in place. Returns out."""
+    if stream is None and layout in ROPE_LAYOUTS:
+        got = (_ext or _extension()).rope(x, positions, axes, base, ROPE_LAYOUTS[layout], shared, inverse, out)
+        if got.__class__ is int:
+            _raise_on(got)
+        if got is not None:
+            return got
     lib = load_library()
     shape, xs = _heads(x, "x", _NORM_TYPES)
     B, T, H, D = shape
