@@ -153,30 +153,33 @@ __device__ __forceinline__ void add_half(const uint8_t* box, int row, int half, 
     }
 }
 
-// v *= xs ws[c ..] and v += bias[c ..] over 32 columns; N, a multiple of 8, bounds them.
-__device__ __forceinline__ void scale32(float (&v)[32], float xs, const float* ws, int c, int N)
+// Columns c .. c + 31 of a row of N values of fp32 (N a multiple of 8), all under way at once: a load behind a branch of its
+// own would wait for each, some 250 cycles where L1 is left 28 KB. Past N they repeat the last; nothing reads those.
+__device__ __forceinline__ void row32(float4 (&w)[8], const float* from, int c, int N)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = __ldg(reinterpret_cast<const float4*>(from + min(c + 4 * j, N - 4)));
+}
+
+__device__ __forceinline__ void scale32(float (&v)[32], float xs, const float4 (&w)[8])
 {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        if (c + 4 * j >= N) break;
-        const float4 w = __ldg(reinterpret_cast<const float4*>(ws + c) + j);
-        v[4 * j] *= xs * w.x;
-        v[4 * j + 1] *= xs * w.y;
-        v[4 * j + 2] *= xs * w.z;
-        v[4 * j + 3] *= xs * w.w;
+        v[4 * j] *= xs * w[j].x;
+        v[4 * j + 1] *= xs * w[j].y;
+        v[4 * j + 2] *= xs * w[j].z;
+        v[4 * j + 3] *= xs * w[j].w;
     }
 }
 
-__device__ __forceinline__ void bias32(float (&v)[32], const float* bias, int c, int N)
+__device__ __forceinline__ void bias32(float (&v)[32], const float4 (&w)[8])
 {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        if (c + 4 * j >= N) break;
-        const float4 w = __ldg(reinterpret_cast<const float4*>(bias + c) + j);
-        v[4 * j] += w.x;
-        v[4 * j + 1] += w.y;
-        v[4 * j + 2] += w.z;
-        v[4 * j + 3] += w.w;
+        v[4 * j] += w[j].x;
+        v[4 * j + 1] += w[j].y;
+        v[4 * j + 2] += w[j].z;
+        v[4 * j + 3] += w[j].w;
     }
 }
 
@@ -340,7 +343,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_product_pair_kernel(const __
                     __syncwarp();
                 }
             }
-            const float xs = kEpi != kBare && p.xs && row < M ? p.xs[row] : 1.f;
+            const float xs = kF8 && row < M ? p.xs[row] : 1.f;
             bool ok = mbar_wait(smem_u32(&sm.acc_full[acc]), (it >> 1) & 1, abortf, p.budget_ns);
             tc_fence_after();
             if constexpr (kEpi == kPlain) {
@@ -383,9 +386,15 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_product_pair_kernel(const __
                         }
                     }
                 }
+                float4 sw[8], sb[8];
                 if constexpr (kEpi == kGated) {
                     tmem_get(x, taddr + 32 * i);
                     tmem_get(u, taddr + kBN / 2 + 32 * i);
+                    if (kF8) row32(sw, p.ws, col + 32 * q, N);
+                    if (kF8) row32(sb, p.ws + p.N, col + 32 * q, N);
+                } else if constexpr (kEpi == kPlain) {
+                    if (kF8) row32(sw, p.ws, col + 32 * q, N);
+                    if (p.bias) row32(sb, p.bias, col + 32 * q, N);
                 }
                 tmem_wait_ld();
                 if (i + 1 < kPieces) {
@@ -396,9 +405,9 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_product_pair_kernel(const __
                     if (lane == 0) arrive_cluster(acc ? empty1 : empty0);
                 }
                 if constexpr (kEpi == kGated) {
-                    if (p.ws) {
-                        scale32(x, xs, p.ws, col + 32 * q, N);
-                        scale32(u, xs, p.ws + N, col + 32 * q, N);
+                    if (kF8) {
+                        scale32(x, xs, sw);
+                        scale32(u, xs, sb);
                     }
                     if (kZ && live) {
                         put_half(bz, lane, q, x);
@@ -408,8 +417,8 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_product_pair_kernel(const __
 #pragma unroll
                     for (int e = 0; e < 32; ++e) x[e] *= u[e];
                 } else if constexpr (kEpi == kPlain) {
-                    if (p.ws) scale32(x, xs, p.ws, col + 32 * q, N);
-                    if (p.bias) bias32(x, p.bias, col + 32 * q, N);
+                    if (kF8) scale32(x, xs, sw);
+                    if (p.bias) bias32(x, sb);
                     if (kZ && live) put_half(bz, lane, q, x);
                     activate(x, p.act);
                     if (res && live) add_half(by, lane, q, x);
