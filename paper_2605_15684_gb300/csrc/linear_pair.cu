@@ -10,13 +10,16 @@
 // Gated, the first CTA holds gate rows and the second the matching up rows, so that a row's g and u meet in one
 // thread of the epilogue. Operands along K are 128-byte rows; operands along their rows ("mn": dW's both, dx's b) come as
 // boxes of 64 columns x 64 k. e4m3 takes the same bytes: a step has 128 values of K in place of 64.
-// Persistent, one CTA an SM, 320 threads:
-//   warp 0     TMA of this CTA's operands, counted on the first CTA's barriers
-//   warp 1     (first CTA) tcgen05.mma M = 256, N = kBN into one of two accumulators; commits reach both CTAs
-//   warps 2-9  epilogue of this CTA's 128 rows, two warps a quadrant of TMEM lanes, 64 columns at a time: a lane has a
-//              row; results go to 32 x 64 boxes in shared memory (128-byte swizzle, so that neither the
-//              rows' stores nor the copy out conflict) and out by TMA, which also clips ragged edges. The residual
-//              comes the same way, before the products are done.
+// Persistent, one CTA an SM:
+//   warp 0   TMA of this CTA's operands, counted on the first CTA's barriers
+//   warp 1   (first CTA) tcgen05.mma M = 256, N = kBN into one of two accumulators; commits reach both CTAs
+//   the rest epilogue of this CTA's 128 rows, a warp a quadrant of TMEM lanes and 64 columns (16 warps at 256 columns; gated 8
+//            warps with 64 columns of g and of u): a lane has a row; results go to 32 x 64 boxes in shared memory
+//            (128-byte swizzle, so that neither the rows' stores nor the copy out conflict) and out by TMA, which
+//            also clips ragged edges. The residual comes the same way, before the products are done.
+// What bounds a tile: the products, whose operands take nearly all that shared memory moves (64 KB in and out a step
+// of 512 cycles; 600 measured). An epilogue of eight warps took longer than 12 steps of it, waiting for its loads
+// and for the special function units in turn.
 // Sums are fp32 in TMEM; z and y are rounded once each. Tiles go through the rows in bands of eight tiles, so that the
 // CTAs at work share operands in L2. Every wait is bounded; a timeout is written to the device status word.
 #include <cstddef>
@@ -30,29 +33,30 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kEpiWarps = 8, kThreads = (2 + kEpiWarps) * 32;
 constexpr uint32_t kABytes = 128 * 128, kBoxBytes = 32 * 128;
 constexpr int kBand = 8;
 
 enum { kPlain = 0, kGated = 1, kBare = 2 };  // kBare: y alone, nothing but the rounding
 
-template <int kBN, bool kZ>
+template <int kBN, int kEpi, bool kZ>
 struct PairCfg {
     static constexpr uint32_t kBBytes = kBN / 2 * 128;
-    static constexpr int kBoxes = kZ ? 3 : 2;
-    static constexpr int kStages = kZ ? (kBN == 256 ? 4 : 5) : (kBN == 256 ? 5 : 6);
+    static constexpr int kEpiWarps = kEpi == kGated ? 8 : kBN / 16;
+    static constexpr int kThreads = (2 + kEpiWarps) * 32;
+    static constexpr int kBoxes = kEpi == kGated && kZ ? 3 : 1;  // a warp
+    static constexpr int kStages = kEpi == kGated ? (kZ ? 4 : 6) : kBN == 256 ? 5 : 6;
 };
 
-template <int kBN, bool kZ>
+template <int kBN, int kEpi, bool kZ>
 struct __align__(1024) PairSmem {
-    using C = PairCfg<kBN, kZ>;
+    using C = PairCfg<kBN, kEpi, kZ>;
     uint8_t a[C::kStages][kABytes];
     uint8_t b[C::kStages][C::kBBytes];
-    uint8_t box[kEpiWarps][C::kBoxes][kBoxBytes];
+    uint8_t box[C::kEpiWarps][C::kBoxes][kBoxBytes];
     uint64_t full[C::kStages], empty[C::kStages];
     uint64_t acc_full[2], acc_empty[2];
     uint64_t drain;
-    uint64_t res[kEpiWarps];
+    uint64_t res[C::kEpiWarps];
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -109,62 +113,71 @@ __device__ __forceinline__ bool item_at(const PairParams& p, int q, int k, Item&
     return true;
 }
 
-// 32 values of z to act(z), with the branch on the activation outside the loop.
-template <int kAct>
-__device__ __forceinline__ void apply32(float (&v)[32])
+// Values of z to act(z), with the branch on the activation outside the loop.
+template <int kAct, int n>
+__device__ __forceinline__ void apply(float (&v)[n])
 {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = act_fn<kAct>(v[i]);
+    for (int i = 0; i < n; ++i) v[i] = act_fn<kAct>(v[i]);
 }
 
-__device__ __forceinline__ void activate(float (&v)[32], int act)
+template <int n>
+__device__ __forceinline__ void activate(float (&v)[n], int act)
 {
     if (act == SSBA_ACT_SILU)
-        apply32<SSBA_ACT_SILU>(v);
+        apply<SSBA_ACT_SILU>(v);
     else if (act == SSBA_ACT_GELU)
-        apply32<SSBA_ACT_GELU>(v);
+        apply<SSBA_ACT_GELU>(v);
     else if (act == SSBA_ACT_RELU)
-        apply32<SSBA_ACT_RELU>(v);
+        apply<SSBA_ACT_RELU>(v);
 }
 
-// Half a row (32 values, 64 bytes) of a 32 x 64 box, 128-byte swizzle.
-__device__ __forceinline__ void put_half(uint8_t* box, int row, int half, const float (&v)[32])
+// Unit j (16 bytes, eight columns) of a row of a 32 x 64 box, 128-byte swizzle.
+__device__ __forceinline__ uint4* unit(uint8_t* box, int row, int j)
 {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint4 w = make_uint4(pack2(v[8 * j], v[8 * j + 1]), pack2(v[8 * j + 2], v[8 * j + 3]),
-                                   pack2(v[8 * j + 4], v[8 * j + 5]), pack2(v[8 * j + 6], v[8 * j + 7]));
-        *reinterpret_cast<uint4*>(box + row * 128 + (((4 * half + j) ^ (row & 7)) << 4)) = w;
-    }
+    return reinterpret_cast<uint4*>(box + row * 128 + ((j ^ (row & 7)) << 4));
 }
 
-__device__ __forceinline__ void add_half(const uint8_t* box, int row, int half, float (&v)[32])
+// n values (a multiple of 8) from unit j on, rounded.
+template <int n>
+__device__ __forceinline__ void put(uint8_t* box, int row, int j, const float (&v)[n])
 {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint4 w = *reinterpret_cast<const uint4*>(box + row * 128 + (((4 * half + j) ^ (row & 7)) << 4));
+    for (int i = 0; i < n / 8; ++i)
+        *unit(box, row, j + i) = make_uint4(pack2(v[8 * i], v[8 * i + 1]), pack2(v[8 * i + 2], v[8 * i + 3]),
+                                            pack2(v[8 * i + 4], v[8 * i + 5]), pack2(v[8 * i + 6], v[8 * i + 7]));
+}
+
+template <int n>
+__device__ __forceinline__ void add(uint8_t* box, int row, int j, float (&v)[n])
+{
+#pragma unroll
+    for (int i = 0; i < n / 8; ++i) {
+        const uint4 w = *unit(box, row, j + i);
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 f = unpack2(u[i]);
-            v[8 * j + 2 * i] += f.x;
-            v[8 * j + 2 * i + 1] += f.y;
+        for (int e = 0; e < 4; ++e) {
+            const float2 f = unpack2(u[e]);
+            v[8 * i + 2 * e] += f.x;
+            v[8 * i + 2 * e + 1] += f.y;
         }
     }
 }
 
-// Columns c .. c + 31 of a row of N values of fp32 (N a multiple of 8), all under way at once: a load behind a branch of its
+// Columns from c on of a row of N values of fp32 (N a multiple of 8), all under way at once: a load behind a branch of its
 // own would wait for each, some 250 cycles where L1 is left 28 KB. Past N they repeat the last; nothing reads those.
-__device__ __forceinline__ void row32(float4 (&w)[8], const float* from, int c, int N)
+template <int n4>
+__device__ __forceinline__ void cols(float4 (&w)[n4], const float* from, int c, int N)
 {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = __ldg(reinterpret_cast<const float4*>(from + min(c + 4 * j, N - 4)));
+    for (int j = 0; j < n4; ++j) w[j] = __ldg(reinterpret_cast<const float4*>(from + min(c + 4 * j, N - 4)));
 }
 
-__device__ __forceinline__ void scale32(float (&v)[32], float xs, const float4 (&w)[8])
+template <int n4>
+__device__ __forceinline__ void scale(float (&v)[4 * n4], float xs, const float4 (&w)[n4])
 {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < n4; ++j) {
         v[4 * j] *= xs * w[j].x;
         v[4 * j + 1] *= xs * w[j].y;
         v[4 * j + 2] *= xs * w[j].z;
@@ -172,10 +185,11 @@ __device__ __forceinline__ void scale32(float (&v)[32], float xs, const float4 (
     }
 }
 
-__device__ __forceinline__ void bias32(float (&v)[32], const float4 (&w)[8])
+template <int n4>
+__device__ __forceinline__ void plus(float (&v)[4 * n4], const float4 (&w)[n4])
 {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < n4; ++j) {
         v[4 * j] += w[j].x;
         v[4 * j + 1] += w[j].y;
         v[4 * j + 2] += w[j].z;
@@ -188,17 +202,23 @@ __device__ __forceinline__ void tmem_get(float (&v)[32], uint32_t at)
     tmem_ld_32x32b_x32(at, reinterpret_cast<uint32_t*>(v));
 }
 
-template <int kBN, bool kF8, int kEpi, bool kZ>
-__global__ void __launch_bounds__(kThreads, 1) ssba_product_pair_kernel(const __grid_constant__ PairMaps maps, const PairParams p)
+__device__ __forceinline__ void tmem_get(float (&v)[16], uint32_t at)
 {
-    using C = PairCfg<kBN, kZ>;
-    constexpr int kStages = C::kStages;
+    tmem_ld_32x32b_x16(at, reinterpret_cast<uint32_t(&)[16]>(v));
+}
+
+template <int kBN, bool kF8, int kEpi, bool kZ>
+__global__ void __launch_bounds__(PairCfg<kBN, kEpi, kZ>::kThreads, 1)
+    ssba_product_pair_kernel(const __grid_constant__ PairMaps maps, const PairParams p)
+{
+    using C = PairCfg<kBN, kEpi, kZ>;
+    constexpr int kStages = C::kStages, kEpiWarps = C::kEpiWarps;
     constexpr int kBK = kF8 ? 128 : 64;                    // values of K a step
     constexpr int kCols = kEpi == kGated ? kBN / 2 : kBN;  // output columns of a tile
     constexpr uint32_t kStep = kABytes + C::kBBytes;
     extern __shared__ uint8_t smem_raw[];
-    PairSmem<kBN, kZ>& sm = *reinterpret_cast<PairSmem<kBN, kZ>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
-                                                                  ~static_cast<uintptr_t>(1023));
+    using Smem = PairSmem<kBN, kEpi, kZ>;
+    Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const int pair = blockIdx.x >> 1;
@@ -317,124 +337,122 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_product_pair_kernel(const __
         __syncwarp();
     } else {
         // ------------------------------------------------------------ epilogue
-        const int w = warp - 2, quad = warp & 3, half = w >> 2;
-        constexpr int kChunks = kEpi == kGated ? 1 : kBN / 128;  // of 64 columns a warp
+        const int w = warp - 2, quad = warp & 3, part = w >> 2;  // part: which 64 columns of the tile (gated: of g and of u)
         uint8_t(*box)[kBoxBytes] = sm.box[w];
         const uint32_t empty0 = at_rank(smem_u32(&sm.acc_empty[0]), 0), empty1 = at_rank(smem_u32(&sm.acc_empty[1]), 0);
-        uint32_t nres = 0, nbox = 0;
+        uint32_t nres = 0;
         for (uint32_t it = 0; item_at(p, pair, (int)it, o); ++it) {
             const bool second = kEpi == kBare && o.set == 1;
             const int M = second ? p.M2 : p.M, N = second ? p.N2 : p.N;
             const CUtensorMap* my = second ? &maps.y2 : &maps.y;
-            const int row0 = o.m * 256 + (int)rank * 128 + 32 * quad, row = row0 + lane;
-            const int col0 = o.n * kCols + half * (kCols / 2);
+            const int row0 = o.m * 256 + (int)rank * 128 + 32 * quad, row = row0 + lane, col = o.n * kCols + part * 64;
             const uint32_t acc = it & 1;
-            bool res = false;
-            if constexpr (kEpi == kPlain) {
-                res = p.has_r && row0 < M && col0 < N;
-                if (res) {
-                    if (lane == 0) {
-                        store_wait_read<0>();
-                        const int boxes = kChunks == 2 && col0 + 64 < N ? 2 : 1;
-                        mbar_arrive_expect_tx(smem_u32(&sm.res[w]), boxes * kBoxBytes);
-                        for (int c = 0; c < boxes; ++c)
-                            tma_load_3d(smem_u32(box[c]), &maps.r, smem_u32(&sm.res[w]), col0 + 64 * c, row0, 0);
+            const bool live = row0 < M && col < N;
+            const bool res = kEpi == kPlain && p.has_r && live;
+            if (live) {  // the boxes are free once the last tile's have been read
+                if (lane == 0) {
+                    store_wait_read<0>();
+                    if (res) {
+                        mbar_arrive_expect_tx(smem_u32(&sm.res[w]), kBoxBytes);
+                        tma_load_3d(smem_u32(box[0]), &maps.r, smem_u32(&sm.res[w]), col, row0, 0);
                     }
-                    __syncwarp();
                 }
+                __syncwarp();
             }
             const float xs = kF8 && row < M ? p.xs[row] : 1.f;
             bool ok = mbar_wait(smem_u32(&sm.acc_full[acc]), (it >> 1) & 1, abortf, p.budget_ns);
             tc_fence_after();
-            if constexpr (kEpi == kPlain) {
-                if (res) {  // waited for in any case: the copy must not outlive the CTA
-                    ok = wait_raw(smem_u32(&sm.res[w]), nres & 1, p.budget_ns) && ok;
-                    ++nres;
-                }
+            if (res) {  // waited for in any case: the copy must not outlive the CTA
+                ok = wait_raw(smem_u32(&sm.res[w]), nres & 1, p.budget_ns) && ok;
+                ++nres;
             }
             if (!__all_sync(0xffffffffu, ok)) {
                 dead = true;
                 break;
             }
-            const uint32_t taddr = tbase + ((uint32_t)(32 * quad) << 16) + acc * kBN + half * (kCols / 2);
-            // pieces of 32 columns; the next one's values are on their way while one is worked on (gated: there are two a piece)
-            constexpr int kPieces = 2 * kChunks;
-            float v[kEpi == kGated ? 1 : 2][32], u[32];
-            if constexpr (kEpi != kGated) tmem_get(v[0], taddr);
-            uint8_t *by = nullptr, *bz = nullptr, *bu = nullptr;
+            const uint32_t taddr = tbase + ((uint32_t)(32 * quad) << 16) + acc * kBN + part * 64;
+            auto read = [&] {  // the accumulator has been read
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive_cluster(acc ? empty1 : empty0);
+            };
+            if constexpr (kEpi == kGated) {
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                const int c = i >> 1, q = i & 1, col = col0 + 64 * c;
-                const bool live = row0 < M && col < N;
-                float(&x)[32] = v[kEpi == kGated ? 0 : i & 1];
-                if (q == 0) {
-                    // the chunk's boxes: with a residual, or with z, by chunk; else in turn
-                    if (kZ) {
-                        by = box[kEpi == kGated ? 0 : c];
-                        bz = box[kEpi == kGated ? 1 : 2];
-                        bu = box[2];
-                        if (live) {
-                            if (lane == 0) store_wait_read<0>();
-                            __syncwarp();
-                        }
-                    } else {
-                        by = box[kEpi == kPlain && p.has_r ? c : (nbox & 1)];
-                        if (live && !(kEpi == kPlain && p.has_r)) {
-                            ++nbox;
-                            if (lane == 0) store_wait_read<1>();
-                            __syncwarp();
-                        }
-                    }
-                }
-                float4 sw[8], sb[8];
-                if constexpr (kEpi == kGated) {
-                    tmem_get(x, taddr + 32 * i);
+                for (int i = 0; i < 2; ++i) {
+                    float v[32], u[32];
+                    float4 sv[8], su[8];
+                    tmem_get(v, taddr + 32 * i);
                     tmem_get(u, taddr + kBN / 2 + 32 * i);
-                    if (kF8) row32(sw, p.ws, col + 32 * q, N);
-                    if (kF8) row32(sb, p.ws + p.N, col + 32 * q, N);
-                } else if constexpr (kEpi == kPlain) {
-                    if (kF8) row32(sw, p.ws, col + 32 * q, N);
-                    if (p.bias) row32(sb, p.bias, col + 32 * q, N);
-                }
-                tmem_wait_ld();
-                if (i + 1 < kPieces) {
-                    if constexpr (kEpi != kGated) tmem_get(v[(i + 1) & 1], taddr + 32 * (i + 1));
-                } else {  // the accumulator has been read
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) arrive_cluster(acc ? empty1 : empty0);
-                }
-                if constexpr (kEpi == kGated) {
+                    if (kF8) cols(sv, p.ws, col + 32 * i, N);
+                    if (kF8) cols(su, p.ws + N, col + 32 * i, N);
+                    tmem_wait_ld();
+                    if (i == 1) read();
                     if (kF8) {
-                        scale32(x, xs, sw);
-                        scale32(u, xs, sb);
+                        scale(v, xs, sv);
+                        scale(u, xs, su);
                     }
                     if (kZ && live) {
-                        put_half(bz, lane, q, x);
-                        put_half(bu, lane, q, u);
+                        put(box[1], lane, 4 * i, v);
+                        put(box[2], lane, 4 * i, u);
                     }
-                    activate(x, p.act);
+                    activate(v, p.act);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) x[e] *= u[e];
-                } else if constexpr (kEpi == kPlain) {
-                    if (kF8) scale32(x, xs, sw);
-                    if (p.bias) bias32(x, sb);
-                    if (kZ && live) put_half(bz, lane, q, x);
-                    activate(x, p.act);
-                    if (res && live) add_half(by, lane, q, x);
+                    for (int e = 0; e < 32; ++e) v[e] *= u[e];
+                    if (live) put(box[0], lane, 4 * i, v);
                 }
-                if (live) put_half(by, lane, q, x);
-                if (q == 1 && live) {
+            } else {
+                uint32_t late[kZ ? 32 : 1];  // with z: y's bits, until z has left the box
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float v[16];
+                    float4 sw[4], sb[4];
+                    tmem_get(v, taddr + 16 * i);
+                    if (kEpi == kPlain && kF8) cols(sw, p.ws, col + 16 * i, N);
+                    if (kEpi == kPlain && p.bias) cols(sb, p.bias, col + 16 * i, N);
+                    tmem_wait_ld();
+                    if (i == 3) read();
+                    if constexpr (kEpi == kPlain) {
+                        if (kF8) scale(v, xs, sw);
+                        if (p.bias) plus(v, sb);
+                        if constexpr (kZ) {
+                            float z[16];
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) z[e] = v[e];
+                            activate(v, p.act);
+                            if (res) add(box[0], lane, 2 * i, v);
+                            if (live) put(box[0], lane, 2 * i, z);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) late[8 * i + e] = pack2(v[2 * e], v[2 * e + 1]);
+                        } else {
+                            activate(v, p.act);
+                            if (res) add(box[0], lane, 2 * i, v);
+                        }
+                    }
+                    if (!kZ && live) put(box[0], lane, 2 * i, v);
+                }
+                if (kZ && live) {
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) {
-                        tma_store(my, smem_u32(by), col, row0, 0);
-                        if (kZ) {
-                            tma_store(&maps.z, smem_u32(bz), col, row0, 0);
-                            if (kEpi == kGated) tma_store(&maps.z, smem_u32(bu), col, row0, 1);
-                        }
+                        tma_store(&maps.z, smem_u32(box[0]), col, row0, 0);
                         store_commit();
+                        store_wait_read<0>();
                     }
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) *unit(box[0], lane, j) = make_uint4(late[4 * j], late[4 * j + 1], late[4 * j + 2], late[4 * j + 3]);
+                }
+            }
+            if (live) {
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    tma_store(my, smem_u32(box[0]), col, row0, 0);
+                    if (kZ && kEpi == kGated) {
+                        tma_store(&maps.z, smem_u32(box[1]), col, row0, 0);
+                        tma_store(&maps.z, smem_u32(box[2]), col, row0, 1);
+                    }
+                    store_commit();
                 }
             }
         }
@@ -452,7 +470,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_product_pair_kernel(const __
 
 // Pairs of CTAs that run at once on the current device.
 template <class Kernel>
-int pairs_at_once(Kernel k, size_t smem)
+int pairs_at_once(Kernel k, int threads, size_t smem)
 {
     static int cache[kMaxDevices] = {};
     static std::mutex m;
@@ -461,7 +479,7 @@ int pairs_at_once(Kernel k, size_t smem)
     if (dev >= 0 && dev < kMaxDevices && cache[dev] > 0) return cache[dev];
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * (device_sm_count() / 2), 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.blockDim = dim3(threads, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cudaLaunchAttribute la[1];
     la[0].id = cudaLaunchAttributeClusterDimension;
@@ -482,7 +500,8 @@ template <int kBN, bool kF8, int kEpi, bool kZ>
 int launch_pairs(PairMaps& maps, PairParams& p, const char* who, cudaStream_t st)
 {
     auto kernel = ssba_product_pair_kernel<kBN, kF8, kEpi, kZ>;
-    const size_t smem = sizeof(PairSmem<kBN, kZ>) + 1024;
+    constexpr int kThreads = PairCfg<kBN, kEpi, kZ>::kThreads;
+    const size_t smem = sizeof(PairSmem<kBN, kEpi, kZ>) + 1024;
     static PerDeviceOnce attr;
     attr.run([=] { cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
     p.budget_ns = kWaitBudgetNs;
@@ -493,7 +512,7 @@ int launch_pairs(PairMaps& maps, PairParams& p, const char* who, cudaStream_t st
     }
     // Pairs, and how the second set's tiles go to them: the last pair to end ends as early as it can.
     const long long all = (long long)p.set[0].tiles + p.set[1].tiles;
-    const int most = pairs_at_once(kernel, smem);
+    const int most = pairs_at_once(kernel, kThreads, smem);
     const int P = p.pairs = (int)(all < most ? all : most);
     long long best = -1;
     for (int f = 0; f < 2; ++f) {
