@@ -246,19 +246,20 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
-// (dy, x, W, z or None, act, gated, bias) -> (dx, dW, db or None)
+// (dy, x or None, W or None, z or None, act, gated, bias, whether dx and dW are wanted) -> (dx, dW, db, each or None)
 PyObject* linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
-    return guarded(n, 7, [&]() -> PyObject* {
+    return guarded(n, 9, [&]() -> PyObject* {
         const int dev = here();
         const at::Tensor* dy = dense(a[0], dev, at::kBFloat16);
-        const at::Tensor* W = dense(a[2], dev, at::kBFloat16);
-        const bool gated = truth(a[5]), bias = truth(a[6]);
-        if (dy->dim() != 2 || W->dim() != 2) throw Long();
-        const int32_t T = narrow(dy->size(0)), N = narrow(dy->size(1)), K = narrow(W->size(1));
-        const int32_t rows = narrow((int64_t)N * (gated ? 2 : 1));
-        const at::Tensor* x = matrix(a[1], dev, at::kBFloat16, T, K);
-        if (W->size(0) != rows) throw Long();
+        const bool gated = truth(a[5]), bias = truth(a[6]), want_dx = truth(a[7]), want_dW = truth(a[8]);
+        if (dy->dim() != 2 || (!want_dx && !want_dW)) throw Long();
+        const int32_t T = narrow(dy->size(0)), N = narrow(dy->size(1)), rows = narrow((int64_t)N * (gated ? 2 : 1));
+        const at::Tensor* one = dense(want_dx ? a[2] : a[1], dev, at::kBFloat16);
+        if (one->dim() != 2) throw Long();
+        const int32_t K = narrow(one->size(1));
+        const at::Tensor* W = want_dx ? matrix(a[2], dev, at::kBFloat16, rows, K) : nullptr;
+        const at::Tensor* x = want_dW ? matrix(a[1], dev, at::kBFloat16, T, K) : nullptr;
         const int32_t act = (int32_t)number(a[4]);
         if ((act != 0) != (a[3] != Py_None)) throw Long();
         const at::Tensor* z = act ? matrix(a[3], dev, at::kBFloat16, T, rows) : nullptr;
@@ -268,8 +269,8 @@ PyObject* linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
         {
             Unlocked scope;
             const size_t need = g.linear_bytes(&d);
-            dx = make(dev, {T, K}, at::kBFloat16);
-            dW = make(dev, {rows, K}, at::kBFloat16);
+            if (want_dx) dx = make(dev, {T, K}, at::kBFloat16);
+            if (want_dW) dW = make(dev, {rows, K}, at::kBFloat16);
             if (bias) db = make(dev, {N}, at::kFloat);
             if (need) ws = make(dev, {(int64_t)need}, at::kByte);
             rc = g.linear_backward(&d, data(dy), data(x), data(W), data(z), out(dx), out(dW), out_floats(db), out(ws), need, stream(dev));

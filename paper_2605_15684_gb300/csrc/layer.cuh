@@ -181,6 +181,14 @@ __device__ __forceinline__ void tma_store(const void* map, uint32_t src, int c0,
                  : "memory");
 }
 
+// A tile to L2 alone.
+__device__ __forceinline__ void tma_prefetch_3d(const void* map, int c0, int c1, int c2)
+{
+    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global [%0, {%1, %2, %3}];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c0),
+                 "r"(c1), "r"(c2)
+                 : "memory");
+}
+
 __device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 // At most n of this thread's groups of stores still read shared memory / are still under way.
 template <int n>
@@ -211,6 +219,9 @@ struct Product {
 int launch_product_pair(const Product& p, const char* who, cudaStream_t st);
 int launch_product_rows(const Product& p, const char* who, cudaStream_t st);
 int launch_product(const Product& p, const char* who, cudaStream_t st);
+// What either is expected to take, in microseconds.
+double product_pair_us(long long M, long long N, long long K, bool f8, bool gated);
+double product_rows_us(long long M, long long N, long long K, bool f8, bool gated);
 // dx = dz W and dW = dz^T x in one launch; either may be null.
 int launch_gradients(const void* dz, const void* x, const void* W, void* dx, void* dW, int T, int N, int K, const char* who,
                      cudaStream_t st);

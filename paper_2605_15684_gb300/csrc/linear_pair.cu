@@ -496,23 +496,10 @@ int pairs_at_once(Kernel k, int threads, size_t smem)
     return n;
 }
 
-template <int kBN, bool kF8, int kEpi, bool kZ>
-int launch_pairs(PairMaps& maps, PairParams& p, const char* who, cudaStream_t st)
+// Pairs, and how the second set's tiles go to them: the last pair to end ends as early as it can. Returns its steps of K.
+long long plan(PairParams& p, int most)
 {
-    auto kernel = ssba_product_pair_kernel<kBN, kF8, kEpi, kZ>;
-    constexpr int kThreads = PairCfg<kBN, kEpi, kZ>::kThreads;
-    const size_t smem = sizeof(PairSmem<kBN, kEpi, kZ>) + 1024;
-    static PerDeviceOnce attr;
-    attr.run([=] { cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
-    p.budget_ns = kWaitBudgetNs;
-    p.status = device_status_word();
-    if (!p.status) {
-        set_error("%s: could not resolve the device status word", who);
-        return SSBA_ERR_CUDA;
-    }
-    // Pairs, and how the second set's tiles go to them: the last pair to end ends as early as it can.
     const long long all = (long long)p.set[0].tiles + p.set[1].tiles;
-    const int most = pairs_at_once(kernel, kThreads, smem);
     const int P = p.pairs = (int)(all < most ? all : most);
     long long best = -1;
     for (int f = 0; f < 2; ++f) {
@@ -537,6 +524,25 @@ int launch_pairs(PairMaps& maps, PairParams& p, const char* who, cudaStream_t st
     p.first_tiles = p.set[p.first].tiles;
     p.other_tiles = p.set[1 - p.first].tiles;
     p.rounds = p.first_tiles / P;
+    return best;
+}
+
+template <int kBN, bool kF8, int kEpi, bool kZ>
+int launch_pairs(PairMaps& maps, PairParams& p, const char* who, cudaStream_t st)
+{
+    auto kernel = ssba_product_pair_kernel<kBN, kF8, kEpi, kZ>;
+    constexpr int kThreads = PairCfg<kBN, kEpi, kZ>::kThreads;
+    const size_t smem = sizeof(PairSmem<kBN, kEpi, kZ>) + 1024;
+    static PerDeviceOnce attr;
+    attr.run([=] { cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
+    p.budget_ns = kWaitBudgetNs;
+    p.status = device_status_word();
+    if (!p.status) {
+        set_error("%s: could not resolve the device status word", who);
+        return SSBA_ERR_CUDA;
+    }
+    plan(p, pairs_at_once(kernel, kThreads, smem));
+    const int P = p.pairs;
     // In stream order, neither beginning before the grid in front has ended nor letting the next one begin. Pairs that
     // were set up beside the last waves of another grid (a gated block's backward pass, many calls queued)
     // did not end; a launch of its own costs about 2 us.
@@ -590,6 +596,20 @@ int launch_as(const Product& q, const char* who, cudaStream_t st)
 
 }  // namespace
 
+namespace {
+
+long long rounds(long long M, long long N, long long cols)
+{
+    const long long pairs = device_sm_count() / 2 > 0 ? device_sm_count() / 2 : 1;
+    return (((M + 255) / 256) * ((N + cols - 1) / cols) + pairs - 1) / pairs;
+}
+
+// 256 columns a tile, or 128 where that needs no more rounds over the SMs: a 128-column step brings three quarters of
+// the bytes for half the products, and takes 0.9 of the time (dx of 5001 rows, 2048 columns, K 11264).
+bool narrow(long long M, long long N) { return 9 * rounds(M, N, 128) < 10 * rounds(M, N, 256); }
+
+}  // namespace
+
 int launch_product_pair(const Product& q, const char* who, cudaStream_t st)
 {
     if (q.gated) {
@@ -597,19 +617,33 @@ int launch_product_pair(const Product& q, const char* who, cudaStream_t st)
         return q.z ? launch_as<256, false, kGated, true>(q, who, st) : launch_as<256, false, kGated, false>(q, who, st);
     }
     if (q.z) return q.f8 ? launch_as<256, true, kPlain, true>(q, who, st) : launch_as<256, false, kPlain, true>(q, who, st);
-    // 256 columns a tile, or 128 where that needs no more rounds over the SMs: a 128-column step brings three quarters of
-    // the bytes for half the products, and takes 0.9 of the time (dx of 5001 rows, 2048 columns, K 11264)
-    const long long pairs = device_sm_count() / 2 > 0 ? device_sm_count() / 2 : 1, mt = (q.M + 255) / 256;
-    const long long wide = (mt * ((q.N + 255) / 256) + pairs - 1) / pairs, narrow = (mt * ((q.N + 127) / 128) + pairs - 1) / pairs;
-    const bool half = 9 * narrow < 10 * wide;
+    const bool half = narrow(q.M, q.N);
     if (q.f8) return half ? launch_as<128, true, kPlain, false>(q, who, st) : launch_as<256, true, kPlain, false>(q, who, st);
     return half ? launch_as<128, false, kPlain, false>(q, who, st) : launch_as<256, false, kPlain, false>(q, who, st);
+}
+
+// A start and an end of 5.6 us in all and 0.25 a step of K and round of tiles (measured 7 to 45 us within a tenth).
+double product_pair_us(long long M, long long N, long long K, bool f8, bool gated)
+{
+    const long long ksteps = (K + (f8 ? 127 : 63)) / (f8 ? 128 : 64), wide = gated ? 128 : 256;
+    return 5.6 + 0.25 * ksteps * rounds(M, N, wide);
 }
 
 int launch_gradients(const void* dz, const void* x, const void* W, void* dx, void* dW, int T, int N, int K, const char* who,
                      cudaStream_t st)
 {
-    if (dx && T <= 256) {  // few rows: the weights as the tensor cores' rows
+    // dx of few rows takes the weights as the tensor cores' rows where that, and dW's launch of its own, ends sooner (also
+    // where dW is not wanted, so that dx is the same either way). A step of operands along their rows takes 0.33 us
+    // where few pairs have work.
+    const int most = device_sm_count() / 2 > 0 ? device_sm_count() / 2 : 1;
+    const Tiles of_dx = tiles_of(T, K, N, 256, 64), of_dW = tiles_of(N, K, T, 256, 64);
+    auto pair_us = [&](bool with_dx) {
+        PairParams p = {};
+        if (with_dx) p.set[0] = of_dx;
+        p.set[1] = of_dW;
+        return 5.6 + 0.33 * plan(p, most);
+    };
+    if (dx && (T <= 64 || product_rows_us(T, K, N, false, false) + pair_us(false) < pair_us(true))) {
         Product q{};
         q.a = dz;
         q.b = W;
@@ -632,14 +666,14 @@ int launch_gradients(const void* dz, const void* x, const void* W, void* dx, voi
              encode_map(&maps.y, dx, false, k, t, 1, k * 2, 0, 64, 32);
         p.M = T;
         p.N = K;
-        p.set[0] = tiles_of(T, K, N, 256, 64);
+        p.set[0] = of_dx;
     }
     if (dW) {
         ok = ok && encode_map(&maps.a2, dz, false, n, t, 1, n * 2, 0, 64, 64) && encode_map(&maps.b2, x, false, k, t, 1, k * 2, 0, 64, 64) &&
              encode_map(&maps.y2, dW, false, k, n, 1, k * 2, 0, 64, 32);
         p.M2 = N;
         p.N2 = K;
-        p.set[1] = tiles_of(N, K, T, 256, 64);
+        p.set[1] = of_dW;
     }
     return ok ? launch_pairs<256, false, kBare, false>(maps, p, who, st) : no_maps(who);
 }

@@ -11,6 +11,7 @@
 //
 // Bound by HBM: x is read once and written once, 16 bytes a thread and step where the strides and the cut allow it (else
 // 8, 4 or 2). A thread forms the sines of its pairs of one token once and applies them to the heads of its share.
+#include <algorithm>
 #include <cmath>
 
 #include "layer.cuh"
@@ -28,10 +29,10 @@ struct RopeArgs {
     char* out;
     const int32_t* pos;
     int64_t xs[3], os[3], pos_batch;  // strides of batch, token, head in bytes; of pos's batch in elements
-    long long work;                   // threads with something to do
+    long long lanes;                  // units of all tokens
     int T, heads, axes, P, D;
     int units, turned;                // units a token and head; of them those that turn
-    int share, shares;                // heads a thread, threads a token's unit
+    int share;                        // heads a thread; the grid's y has the shares
     int inverse;
     uint8_t axis[kMaxPairs];
     uint64_t theta[kMaxPairs];        // turns of 2^64 a position
@@ -88,13 +89,21 @@ __global__ void __launch_bounds__(256) ssba_rope_kernel(const __grid_constant__ 
     grid_dep_wait();
     grid_dep_launch();
     const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (id >= p.work) return;
-    const int unit = (int)(id % p.units);
-    const long long rest = id / p.units;
-    const long long token = rest % ((long long)p.work / p.units / p.shares);
-    const int sh = (int)(rest / ((long long)p.work / p.units / p.shares));
-    const long long b = token / p.T, t = token - b * p.T;
-    const int h0 = sh * p.share, h1 = min(h0 + p.share, p.heads);
+    if (id >= p.lanes) return;
+    int unit;
+    long long b, t;
+    if (p.lanes <= 0xffffffffll) {  // 32-bit divisions where they do (a fifth of the instructions)
+        const uint32_t i = (uint32_t)id, token = i / (uint32_t)p.units, seq = token / (uint32_t)p.T;
+        unit = (int)(i - token * (uint32_t)p.units);
+        b = seq;
+        t = token - seq * (uint32_t)p.T;
+    } else {
+        const long long token = id / p.units;
+        unit = (int)(id - token * p.units);
+        b = token / p.T;
+        t = token - b * p.T;
+    }
+    const int h0 = (int)blockIdx.y * p.share, h1 = min(h0 + p.share, p.heads);
     const char* x = p.x + b * p.xs[0] + t * p.xs[1] + h0 * p.xs[2];
     char* o = p.out + b * p.os[0] + t * p.os[1] + h0 * p.os[2];
     if (unit >= p.turned) {  // dimensions that stay (halves only: adjacent pairs past P turn by nothing)
@@ -149,13 +158,12 @@ int rope_as(RopeArgs& p, int bytes, long long tokens, cudaStream_t st)
         p.units = kHalves ? p.P / n + (p.D - 2 * p.P) / n : p.D / n;
         p.turned = kHalves ? p.P / n : p.units;
         // Heads a thread: as many as leave some eight warps a scheduler; a thread's sines then serve them all.
-        const long long lanes = tokens * p.units, full = (long long)device_sm_count() * 1024;
-        int shares = (int)(full / lanes > p.heads ? p.heads : full / lanes);
-        if (shares < 1) shares = 1;
+        const long long full = (long long)device_sm_count() * 1024;
+        p.lanes = tokens * p.units;
+        const int shares = (int)std::min<long long>(std::max<long long>(full / p.lanes, 1), std::min(p.heads, 65535));
         p.share = (p.heads + shares - 1) / shares;
-        p.shares = (p.heads + p.share - 1) / p.share;
-        p.work = lanes * p.shares;
-        const cudaError_t e = launch_early(ssba_rope_kernel<E, n, kHalves>, dim3((unsigned)((p.work + 255) / 256)), 256, 0, st, 1, p);
+        const dim3 grid((unsigned)((p.lanes + 255) / 256), (unsigned)((p.heads + p.share - 1) / p.share));
+        const cudaError_t e = launch_early(ssba_rope_kernel<E, n, kHalves>, grid, 256, 0, st, 1, p);
         if (e == cudaSuccess) return (int)SSBA_OK;
         set_error("ssba_rope_kernel launch: %s", cudaGetErrorString(e));
         return (int)SSBA_ERR_CUDA;

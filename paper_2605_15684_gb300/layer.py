@@ -252,8 +252,9 @@ def linear_backward_workspace_bytes(T: int, N: int, K: int, act=None, gated: boo
 
 
 def _product_backward(dy, x, W, z, act, db, dx, dW, workspace, stream, gated, bias):
-    if stream is None and dx is None and dW is None and db is None and workspace is None:
-        out = (_ext or _extension()).linear_backward(dy, x, W, z if act is not None else None, _act(act, gated), gated, bias)
+    if stream is None and db is None and workspace is None and (dx is None or dx is False) and (dW is None or dW is False):
+        out = (_ext or _extension()).linear_backward(dy, x, W, z if act is not None else None, _act(act, gated), gated, bias,
+                                                     dx is None, dW is None)
         if out.__class__ is tuple:
             return out
         if out is not None:

@@ -273,3 +273,234 @@ def test_rope_is_the_projections():
         # one rounding more here: of the projection, a pair's two
         near(got, want.double(), 2.0 ** -7 * want.double().abs() + 2.0 ** -7 * 6)
     assert float((qkv[:, :, 2].transpose(1, 2).double() - V.double()).abs().max()) <= 2.0 ** -7 * float(V.abs().max())
+
+
+# ----------------------------------------------------------------------------- as they are used
+def test_rows_behind_the_last_stay():
+    """Outputs that are the first rows of larger buffers: nothing behind them is written."""
+    for T, K, N in ((5, 256, 136), (70, 256, 136), (300, 1536, 392), (2500, 64, 264)):
+        randn, x, W, _, _ = operands(T, K, N, False, 3)
+        dy, z = randn(T, N).to(BF), randn(T, N).to(BF)
+        big = {n: torch.full((T + 9, c), 7.0, device="cuda", dtype=BF) for n, c in (("y", N), ("z", N), ("dx", K), ("h", K), ("g", N))}
+        gb.linear(x, W, act="silu", y=big["y"][:T], z=big["z"][:T])
+        gb.linear_backward(dy, x, W, z=z, act="silu", dx=big["dx"][:T])
+        gb.rms_norm(x, torch.ones(K, device="cuda"), residual=x, h=big["h"][:T])
+        gb.gated_linear(x, torch.cat((W, W)), y=big["g"][:T])
+        for n, t in big.items():
+            assert bool((t[T:] == 7).all()) and not bool((t[:T] == 7).all(1).any()), (n, T)
+
+
+def test_no_rows():
+    x, W, w = torch.zeros(0, 64, device="cuda", dtype=BF), torch.ones(16, 64, device="cuda", dtype=BF), torch.ones(64, device="cuda")
+    y, h, rstd = gb.rms_norm(x, w, residual=x)
+    assert y.shape == (0, 64) and rstd.shape == (0,)
+    assert gb.linear(x, W).shape == (0, 16) and gb.gated_linear(x, W).shape == (0, 8)
+    dy = torch.zeros(0, 16, device="cuda", dtype=BF)
+    dx, dW, db = gb.linear_backward(dy, x, W, z=dy, act="gelu", bias=True)
+    assert dx.shape == (0, 64) and not dW.any() and not db.any()
+    dx, dw = gb.rms_norm_backward(x, x, w, rstd)
+    assert not dw.any()
+    pos = torch.zeros(0, 1, device="cuda", dtype=torch.int32)
+    assert gb.rope_axes(x.view(0, 1, 64), pos, (32,)).shape == (0, 1, 64)
+
+
+def test_python_refusals_on_the_gpu():
+    randn, x, W, _, _ = operands(8, 64, 32, False, 1)
+    w = torch.ones(64, device="cuda")
+    x8, s8 = ref.e4m3_rows(x)
+    pos = torch.zeros(8, 1, device="cuda", dtype=torch.int32)
+    h = x.view(8, 1, 64)
+    for call in (lambda: gb.rms_norm(x, w.double()), lambda: gb.rms_norm(x, w[:32]), lambda: gb.rms_norm(x.T, w), lambda: gb.rms_norm(x, None),
+                 lambda: gb.rms_norm(x, w, residual=x[:4]), lambda: gb.rms_norm(x, w, eps=-1.0), lambda: gb.rms_norm(x, w, h=x),
+                 lambda: gb.rms_norm(x[:, :60].contiguous(), w[:60]),
+                 lambda: gb.linear(x, W.T), lambda: gb.linear(x, W.float()), lambda: gb.linear(x8, W), lambda: gb.linear(x8, W.to(E4M3)),
+                 lambda: gb.linear(x, W, x_scale=s8, w_scale=s8), lambda: gb.linear(x, W, act="tanh"), lambda: gb.linear(x, W, bias=w),
+                 lambda: gb.linear(x, W, residual=x), lambda: gb.linear(x, W, y=x), lambda: gb.gated_linear(x, W, act=None),
+                 lambda: gb.gated_linear(x, W[:31]), lambda: gb.linear_backward(x, x, W), lambda: gb.linear_backward(x[:, :32].contiguous(), x, W, act="silu"),
+                 lambda: gb.linear_backward(x[:, :32].contiguous(), x, W, dx=False, dW=False), lambda: gb.linear_backward(x[:, :32].contiguous(), None, W),
+                 lambda: gb.rope_axes(h, pos, (33,)), lambda: gb.rope_axes(h, pos, (16, 16)), lambda: gb.rope_axes(h, pos.long(), (32,)),
+                 lambda: gb.rope_axes(h, pos, (32,), layout="x"), lambda: gb.rope_axes(h, pos, (32,), base=1.0), lambda: gb.rope_axes(h, pos[:4], (32,)),
+                 lambda: gb.rope_axes(h, pos, (32,), out=h[:1].expand(8, 1, 64)), lambda: gb.rope_axes(h.transpose(0, 2), pos, (32,))):
+        with pytest.raises(api.SsbaError):
+            call()
+
+
+def test_short_and_long_way_are_one():
+    """Calls that take the native way and calls with their outputs given, on the current and on another stream."""
+    randn, x, W, _, _ = operands(70, 256, 144, False, 5)
+    w, r, b = 1 + randn(256, std=0.1), randn(70, 256).to(BF), randn(144)
+    dy, z = randn(70, 144).to(BF), randn(70, 144).to(BF)
+    pos = torch.randint(0, 99, (70, 2), device="cuda", dtype=torch.int32)
+    st = torch.cuda.Stream()
+
+    def run(**kw):
+        out = [*gb.rms_norm(x, w, residual=r, **kw), *gb.rms_norm(x, w, e4m3=True, **kw)[:2]]
+        out += gb.rms_norm_backward(r, x, w, out[2], dh=r, **kw)
+        out += [gb.linear(x, W, bias=b, act="gelu", **kw), *gb.linear(x, W, pre=True, **kw), *gb.gated_linear(x, W, pre=True, **kw)]
+        out += gb.linear_backward(dy, x, W, z=z, act="silu", bias=True, **kw)
+        out += gb.gated_linear_backward(dy[:, :72].contiguous(), x, W, z, **kw)
+        out.append(gb.rope_axes(x.view(70, 4, 64), pos, (16, 16), **kw))
+        return out
+
+    a, b_ = run(), run(stream=torch.cuda.current_stream())
+    st.wait_stream(torch.cuda.current_stream())
+    c = run(stream=st)
+    with torch.cuda.stream(st):
+        d = run()
+    torch.cuda.synchronize()
+    for i, (p, q, s, t) in enumerate(zip(a, b_, c, d)):
+        assert torch.equal(p.float(), q.float()) and torch.equal(p.float(), s.float()) and torch.equal(p.float(), t.float()), i
+
+
+def layer_forward(desc, p, x, pos, lists=None):
+    """One pre-norm layer: norm, projection, rotary positions, sparse attention, projection with residual, norm, gated block.
+    Returns every stage."""
+    B, N, H = desc.B, desc.N, desc.heads
+    s = {}
+    s["y1"], _, s["k1"] = gb.rms_norm(x, p["n1"])
+    qkv = s["qkv"] = gb.linear(s["y1"], p["Wqkv"], bias=p["b"])
+    v5 = qkv.view(B, N, 3, H, 64)
+    s["Q"], s["K"], s["V"] = (torch.empty(B, H, N, 64, device="cuda", dtype=BF) for _ in range(3))
+    gb.rope_axes(v5[:, :, 0], pos, (16, 16), out=s["Q"].transpose(1, 2))
+    gb.rope_axes(v5[:, :, 1], pos, (16, 16), out=s["K"].transpose(1, 2))
+    s["V"].copy_(v5[:, :, 2].transpose(1, 2))
+    s["O"], s["lse"], s["idx"], s["cnt"] = gb.forward_fused(desc, s["Q"], s["K"], s["V"])[:4]
+    s["o"] = s["O"].transpose(1, 2).reshape(B * N, H * 64)
+    s["a"] = gb.linear(s["o"], p["Wo"])
+    s["y2"], s["h"], s["k2"] = gb.rms_norm(s["a"], p["n2"], residual=x)
+    s["g"], s["z"] = gb.gated_linear(s["y2"], p["Wgu"], pre=True)
+    s["out"] = gb.linear(s["g"], p["Wd"], residual=s["h"])
+    return s
+
+
+def layer_backward(desc, p, x, pos, s, dout):
+    B, N, H = desc.B, desc.N, desc.heads
+    g = {}
+    dg, g["Wd"], _ = gb.linear_backward(dout, s["g"], p["Wd"])
+    dy2, g["Wgu"] = gb.gated_linear_backward(dg, s["y2"], p["Wgu"], s["z"])
+    da, g["n2"] = gb.rms_norm_backward(dy2, s["h"], p["n2"], s["k2"], dh=dout)  # of a and, as it is, of x
+    do, g["Wo"], _ = gb.linear_backward(da, s["o"], p["Wo"])
+    dO = do.view(B, N, H, 64).transpose(1, 2).contiguous()
+    dQ, dK, dV = gb.backward(desc, s["Q"], s["K"], s["V"], s["O"], s["lse"], dO, s["idx"], s["cnt"])
+    dqkv = torch.empty(B, N, 3, H, 64, device="cuda", dtype=BF)
+    gb.rope_axes(dQ.to(BF).transpose(1, 2), pos, (16, 16), inverse=True, out=dqkv[:, :, 0])
+    gb.rope_axes(dK.to(BF).transpose(1, 2), pos, (16, 16), inverse=True, out=dqkv[:, :, 1])
+    dqkv[:, :, 2].copy_(dV.transpose(1, 2))
+    dy1, g["Wqkv"], g["b"] = gb.linear_backward(dqkv.view(B * N, -1), s["y1"], p["Wqkv"], bias=True)
+    g["x"], g["n1"] = gb.rms_norm_backward(dy1, x, p["n1"], s["k1"], dh=da)
+    return g
+
+
+def layer_inputs(seed=0, H=2, side=16, F=192):
+    randn = rng(seed)
+    D = H * 64
+    desc = api.SsbaDesc(1, H, side, side, rho=0.5)
+    mat = lambda n, k: (randn(n, k) / k ** 0.5).to(BF)  # noqa: E731
+    p = dict(n1=1 + randn(D, std=0.1), Wqkv=mat(3 * D, D), b=randn(3 * D, std=0.1), Wo=mat(D, D), n2=1 + randn(D, std=0.1), Wgu=mat(2 * F, D), Wd=mat(D, F))
+    n = torch.arange(side * side, device="cuda", dtype=torch.int32)
+    return desc, p, randn(side * side, D).to(BF), torch.stack((n // side, n % side), 1), randn(side * side, D, std=0.1).to(BF)
+
+
+def test_a_layer_forward_and_backward():
+    """A layer and its gradients against the whole layer in 64 bits with autograd, on the kernel's lists. Every stage rounds
+    to bf16 (2^-9 of its values, on average over sqrt(3)); some twenty of them in a row, each with a gain of about one,
+    stay below 20 * 2^-9 = 2^-4.7 of the results' norm."""
+    desc, p, x, pos, dout = layer_inputs()
+    s = layer_forward(desc, p, x, pos)
+    g = layer_backward(desc, p, x, pos, s, dout)
+    N, H = desc.N, desc.heads
+    d = {k: v.double().requires_grad_(True) for k, v in {**p, "x": x}.items()}
+    norm = lambda h, w: h * (h.square().mean(1, keepdim=True) + 1e-6).rsqrt() * w  # noqa: E731
+    qkv = (norm(d["x"], d["n1"]) @ d["Wqkv"].T + d["b"]).view(1, N, 3, H, 64)
+    th = 10000.0 ** (-torch.arange(16, device="cuda", dtype=torch.float64) / 16)
+    ang = torch.cat((pos[:, :1].double() * th, pos[:, 1:].double() * th), 1)[None, :, None]
+    def turn(t):
+        u, v = t[..., 0::2], t[..., 1::2]
+        return torch.stack((u * ang.cos() - v * ang.sin(), u * ang.sin() + v * ang.cos()), -1).flatten(-2)
+    Q, K, V = turn(qkv[:, :, 0]).transpose(1, 2), turn(qkv[:, :, 1]).transpose(1, 2), qkv[:, :, 2].transpose(1, 2)
+    label = (torch.arange(N, device="cuda") // 16 // 8) * 2 + (torch.arange(N, device="cuda") % 16) // 8
+    kept = torch.zeros(1, H, 4, 4, device="cuda").scatter_(3, s["idx"].long(), 1.0) > 0
+    mask = kept[:, :, label][:, :, :, label]
+    a = (Q @ K.transpose(2, 3) / 8).masked_fill(~mask, float("-inf")).softmax(3) @ V
+    h = a.transpose(1, 2).reshape(N, H * 64) @ d["Wo"].T + d["x"]
+    z = norm(h, d["n2"]) @ d["Wgu"].T
+    F = z.shape[1] // 2
+    out = (torch.nn.functional.silu(z[:, :F]) * z[:, F:]) @ d["Wd"].T + h
+    grads = torch.autograd.grad(out, list(d.values()), dout.double())
+    far = lambda got, want: float((got.double() - want).norm() / want.norm())  # noqa: E731
+    assert far(s["out"], out) < 2.0 ** -4.7
+    for name, want in zip(d, grads):
+        assert far(g[name], want) < 2.0 ** -4.7, name
+
+
+def test_a_layer_in_two_graphs():
+    """Forward and backward of a layer captured twice, replayed in turn on new inputs, with eager calls between."""
+    desc, p, x, pos, dout = layer_inputs(1)
+    st = torch.cuda.Stream()
+    state = []
+    for seed in (1, 2):
+        _, _, xi, _, di = layer_inputs(seed)
+        st.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(st):
+            layer_backward(desc, p, xi, pos, layer_forward(desc, p, xi, pos), di)
+        torch.cuda.current_stream().wait_stream(st)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            s = layer_forward(desc, p, xi, pos)
+            g = layer_backward(desc, p, xi, pos, s, di)
+        state.append((graph, xi, di, s, g))
+    for round_ in range(3):
+        for i, (graph, xi, di, s, g) in enumerate(state):
+            _, _, nx, _, nd = layer_inputs(10 + 2 * round_ + i)
+            xi.copy_(nx)
+            di.copy_(nd)
+        for graph, *_ in state:
+            graph.replay()
+        for graph, xi, di, s, g in state:
+            e = layer_forward(desc, p, xi, pos)
+            eg = layer_backward(desc, p, xi, pos, e, di)
+            torch.cuda.synchronize()
+            assert torch.equal(s["out"], e["out"])
+            for n in eg:
+                assert torch.equal(g[n], eg[n]), n
+
+
+def test_many_calls_queued():
+    """Backward passes queued far ahead of the GPU, as a training loop leaves them, and chains of few-token calls."""
+    randn, x, W, _, _ = operands(1500, 512, 1024, False, 9, 2048)
+    dy, z = randn(1500, 1024).to(BF), randn(1500, 2048).to(BF)
+    want = gb.gated_linear_backward(dy, x, W, z)
+    few = x[:8].contiguous()
+    first = gb.linear(gb.gated_linear(few, W), W[:512, :].reshape(256, 1024))
+    for i in range(300):
+        dx, dW = gb.gated_linear_backward(dy, x, W, z)
+        y, _, _ = gb.rms_norm(dx, torch.ones(512, device="cuda"))
+        a = gb.linear(gb.gated_linear(few, W), W[:512, :].reshape(256, 1024))
+    torch.cuda.synchronize()
+    assert torch.equal(dx, want[0]) and torch.equal(dW, want[1]) and torch.equal(a, first)
+
+
+def test_past_32_bits():
+    """Rows whose offsets pass 2^31 elements, and 2^32 bytes."""
+    T, D = 540000, 4096
+    x = torch.zeros(T, D, device="cuda", dtype=BF)
+    x[-40:] = torch.randn(40, D, device="cuda").to(BF)
+    w = torch.ones(D, device="cuda")
+    y, _, k = gb.rms_norm(x, w)
+    yr, kr = ref.norm(x[-40:], w, 1e-6)
+    near(y[-40:], yr, yr.abs() * (2.0 ** -8 + 2.0 ** -10))
+    assert not y[:-40].any()
+    dx, dw = gb.rms_norm_backward(x, x, w, k)
+    want, _ = ref.norm_backward(x[-40:], x[-40:], w, k[-40:], None)
+    near(dx[-40:], want, want.abs() * 2.0 ** -8 + 2.0 ** -10)
+    del y, dx
+    W = (torch.randn(D, 64, device="cuda") / 8).to(BF)
+    r = x[:, :64].contiguous()
+    out = gb.linear(r, W)  # [T, 4096]
+    yr, _, ty, _ = ref.linear(r[-40:], W)
+    near(out[-40:], yr, ty)
+    assert not out[:-40].any()
+    pos = torch.zeros(T, 1, device="cuda", dtype=torch.int32)
+    pos[-40:] = 5
+    turned = gb.rope_axes(x.view(T, 64, 64), pos, (32,), layout="halves", out=out.view(T, 64, 64))
+    near(turned[-40:], ref.rope(x[-40:].view(1, 40, 64, 64), pos[-40:], (32,), layout="halves")[0], 0.05 + 0 * turned[-40:].double())
