@@ -45,8 +45,8 @@ __device__ __forceinline__ float act_fn(float z)
     return z * sigma<kAct>(z);
 }
 
-// act'(z) and act(z). With p = sigma(t(z)): act' = p + z p (1 - p) t'(z); the second term is 0 where p (1 - p) is,
-// also where z^2 would overflow.
+// act'(z) and act(z). With p = sigma(t(z)): act' = p + z p (1 - p) t'(z) = p (1 + z t' (1 - p)). z is held within 10^6 in the
+// second term, where 1 - p or p is 0 long before, so that no infinity meets a 0.
 template <int kAct>
 __device__ __forceinline__ float act_slope(float z, float& value)
 {
@@ -54,11 +54,10 @@ __device__ __forceinline__ float act_slope(float z, float& value)
         value = z < 0.f ? 0.f : z;
         return z > 0.f ? 1.f : (z == z ? 0.f : z);  // a NaN stays one
     }
-    const float p = sigma<kAct>(z);
+    const float p = sigma<kAct>(z), c = fminf(fmaxf(z, -1e6f), 1e6f);
     value = z * p;
-    const float q = p * (1.f - p);
-    if (q == 0.f) return p;
-    return p + z * q * (kAct == SSBA_ACT_GELU ? kGelu * (1.f + 3.f * kGelu3 * z * z) : 1.f);
+    const float t = kAct == SSBA_ACT_GELU ? c * fmaf(c * c, 3.f * kGelu * kGelu3, kGelu) : c;
+    return p * fmaf(t, 1.f - p, 1.f);
 }
 
 // ------------------------------------------------------------------ small pieces

@@ -13,6 +13,7 @@
 // 8, 4 or 2). A thread forms the sines of its pairs of one token once and applies them to the heads of its share.
 #include <algorithm>
 #include <cmath>
+#include <cstring>
 
 #include "layer.cuh"
 
@@ -179,12 +180,41 @@ int rope_as(RopeArgs& p, int bytes, long long tokens, cudaStream_t st)
     return SSBA_ERR_INVALID;  // not reached: the caller's bytes hold a pair, or an element of halves
 }
 
+// The rates of a call's pairs and their axes follow from the rule alone. A thread keeps those of its last rule: a model's
+// calls share one, and 64 powers in 64 bits take longer than a few tokens' kernel.
+struct Rates {
+    int32_t axes = 0, sections[SSBA_ROPE_MAX_AXES] = {}, shared = 0;
+    double base = 0;
+    int P = 0;
+    uint8_t axis[kMaxPairs];
+    uint64_t theta[kMaxPairs];
+
+    void set(const ssba_rope_desc& d)
+    {
+        bool same = axes == d.axes && (shared != 0) == (d.shared != 0) && base == d.base;
+        for (int a = 0; same && a < axes; ++a) same = sections[a] == d.sections[a];
+        if (same) return;
+        axes = d.axes;
+        shared = d.shared;
+        base = d.base;
+        P = 0;
+        for (int a = 0; a < axes; ++a) P += sections[a] = d.sections[a];
+        const double two64 = 18446744073709551616.0, turn = 6.283185307179586476925286766559;
+        for (int a = 0, j = 0; a < axes; ++a)
+            for (int i = 0; i < sections[a]; ++i, ++j) {
+                axis[j] = (uint8_t)a;
+                const double e = shared ? (double)j / P : (double)i / sections[a];
+                theta[j] = (uint64_t)(std::pow(base, -e) / turn * two64 + 0.5);
+            }
+    }
+};
+
 }  // namespace
 
 int launch_rope(const ssba_rope_desc& d, const void* x, const int64_t* xs, const int32_t* pos, int64_t pos_batch, void* out,
                 const int64_t* os, cudaStream_t st)
 {
-    RopeArgs p = {};
+    RopeArgs p;
     const int es = d.dtype == SSBA_BF16 ? 2 : 4;
     p.x = static_cast<const char*>(x);
     p.out = static_cast<char*>(out);
@@ -200,15 +230,12 @@ int launch_rope(const ssba_rope_desc& d, const void* x, const int64_t* xs, const
     p.heads = d.heads;
     p.axes = d.axes;
     p.D = d.head_dim;
-    for (int a = 0; a < d.axes; ++a) p.P += d.sections[a];
-    const double two64 = 18446744073709551616.0, turn = 6.283185307179586476925286766559;
-    for (int a = 0, j = 0; a < d.axes; ++a)
-        for (int i = 0; i < d.sections[a]; ++i, ++j) {
-            p.axis[j] = (uint8_t)a;
-            const double e = d.shared ? (double)j / p.P : (double)i / d.sections[a];
-            p.theta[j] = (uint64_t)(std::pow(d.base, -e) / turn * two64 + 0.5);
-        }
-    p.inverse = d.inverse;
+    static thread_local Rates rates;
+    rates.set(d);
+    p.P = rates.P;
+    memcpy(p.axis, rates.axis, p.P);
+    memcpy(p.theta, rates.theta, sizeof(uint64_t) * p.P);
+    p.inverse = d.inverse != 0;
     // the widest piece that every row's start, and the cuts of halves, are multiples of
     const bool halves = d.layout == SSBA_ROPE_HALVES;
     all |= (uint64_t)p.D * es;
