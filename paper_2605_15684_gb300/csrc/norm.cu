@@ -9,6 +9,9 @@
 // passes once, a row stays in registers (as the packed bits that were read) between its sum and its output. A row is
 // one warp's or one CTA's, 16 bytes a thread and step; the 8-bit rows' maximum of |h w| goes through the same
 // reduction as the sum of squares (max |y| = rstd max |h w|, so one barrier serves both).
+// Under the 8-bit rows, y is the fp32 number nearest to the exact product: the sum of squares, rstd and the products carry
+// their rounding errors along in a second fp32 (the pass is bound by HBM; the extra eight instructions a value are
+// free). A plain fp32 product puts one value in a million on the other side of a tie, and so off by an eighth.
 // Backward: CTAs walk over rows and keep dw of their columns in registers (fp32); the partial sums of all
 // CTAs meet in a second launch, in one order.
 #include "layer.cuh"
@@ -68,30 +71,65 @@ __device__ __forceinline__ void load_w(const float* w, float* f)
     }
 }
 
-// The sum of s and the maximum of m over the row's kTPR threads (a warp, or the whole CTA; `at` alternates
-// between two halves of the exchange area, so that one barrier a row is enough).
-template <int kTPR, bool kMax>
-__device__ __forceinline__ void row_reduce(float& s, float& m, float2 (*area)[32], int at)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (kMax) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+// A sum and the error of its roundings.
+struct Sum {
+    float hi, lo;
+    __device__ __forceinline__ void add(float x, float err)
+    {
+        const float t = hi + x, z = t - hi;
+        lo += ((hi - (t - z)) + (x - z)) + err;
+        hi = t;
     }
+};
+
+// The sum of s and the maximum of m over the row's kTPR threads (a warp, or the whole CTA; `at` alternates between two
+// halves of the exchange area, so that one barrier a row is enough). kExact: with the sums' errors.
+template <int kTPR, bool kMax, bool kExact>
+__device__ __forceinline__ void row_reduce(Sum& s, float& m, float4 (*area)[32], int at)
+{
+    auto step = [&](int o) {
+        const float x = __shfl_xor_sync(0xffffffffu, s.hi, o);
+        if (kExact)
+            s.add(x, __shfl_xor_sync(0xffffffffu, s.lo, o));
+        else
+            s.hi += x;
+        if (kMax) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    };
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) step(o);
     if constexpr (kTPR > 32) {
         constexpr int kWarps = kTPR / 32;
         const int lane = threadIdx.x & 31;
-        if (lane == 0) area[at][threadIdx.x >> 5] = make_float2(s, m);
+        if (lane == 0) area[at][threadIdx.x >> 5] = make_float4(s.hi, s.lo, m, 0.f);
         __syncthreads();
-        const float2 v = area[at][lane % kWarps];
-        s = v.x;
-        m = v.y;
+        const float4 v = area[at][lane % kWarps];
+        s.hi = v.x;
+        s.lo = v.y;
+        m = v.z;
 #pragma unroll
-        for (int o = kWarps / 2; o > 0; o >>= 1) {
-            s += __shfl_xor_sync(0xffffffffu, s, o);
-            if (kMax) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        }
+        for (int o = kWarps / 2; o > 0; o >>= 1) step(o);
     }
+}
+
+// 1 / sqrt(sum / D + eps) as a pair of fp32: the hardware's value and one step of Newton's iteration on its error.
+__device__ __forceinline__ Sum exact_rstd(const Sum& s, float D, float eps)
+{
+    Sum m{s.hi / D, 0.f};
+    m.lo = (fmaf(-m.hi, D, s.hi) + s.lo) / D;
+    m.add(eps, 0.f);
+    const float r = rsqrtf(m.hi);
+    if (!(r > 0.f && r < __int_as_float(0x7f800000))) return Sum{r, 0.f};
+    const float t = m.hi * r, off = fmaf(m.hi, r, -t) + m.lo * r;  // (m.hi + m.lo) r = t + off
+    const float low = 0.5f * r * (fmaf(-t, r, 1.f) - off * r);
+    const float hi = r + low;
+    return Sum{hi, (r - hi) + low};
+}
+
+// f k w, rounded once.
+__device__ __forceinline__ float product(float f, const Sum& k, float w)
+{
+    const float p = f * k.hi, pe = fmaf(f, k.lo, fmaf(f, k.hi, -p)), y = p * w;
+    return y + fmaf(pe, w, fmaf(p, w, -y));
 }
 
 // The least power of two s with a / s <= 448 = 1.75 * 2^8 (at least 2^-126; 1 for a row of zeros), and its reciprocal.
@@ -128,7 +166,7 @@ template <class T, int kTPR, int kNV, bool kRes, bool kF8>
 __global__ void __launch_bounds__(kTPR == 32 ? kWarpCta : kTPR) ssba_rms_norm_kernel(const NormArgs p)
 {
     constexpr int n = Vec<T>::n, kRows = kTPR == 32 ? kWarpCta / 32 : 1;
-    __shared__ float2 area[2][32];
+    __shared__ float4 area[2][32];
     const int nv = p.D / n, tid = threadIdx.x % kTPR;
     grid_dep_wait();
     grid_dep_launch();
@@ -141,7 +179,8 @@ __global__ void __launch_bounds__(kTPR == 32 ? kWarpCta : kTPR) ssba_rms_norm_ke
             v[j] = i < nv ? p.x[t * nv + i] : make_uint4(0, 0, 0, 0);
             if (kRes) u[j] = i < nv ? p.r[t * nv + i] : make_uint4(0, 0, 0, 0);
         }
-        float s = 0.f, m = 0.f;
+        Sum s{0.f, 0.f};
+        float m = 0.f;
 #pragma unroll
         for (int j = 0; j < kNV; ++j) {
             const int i = tid + j * kTPR;
@@ -157,7 +196,14 @@ __global__ void __launch_bounds__(kTPR == 32 ? kWarpCta : kTPR) ssba_rms_norm_ke
                 Vec<T>::get(v[j], f);
             }
 #pragma unroll
-            for (int e = 0; e < n; ++e) s = fmaf(f[e], f[e], s);
+            for (int e = 0; e < n; ++e) {
+                if (kF8) {
+                    const float q = f[e] * f[e];  // exact for bf16
+                    s.add(q, n == 8 ? 0.f : fmaf(f[e], f[e], -q));
+                } else {
+                    s.hi = fmaf(f[e], f[e], s.hi);
+                }
+            }
             if (kF8 && i < nv) {
                 float w[n];
                 load_w<n>(p.w + (size_t)i * n, w);
@@ -165,14 +211,18 @@ __global__ void __launch_bounds__(kTPR == 32 ? kWarpCta : kTPR) ssba_rms_norm_ke
                 for (int e = 0; e < n; ++e) m = fmaxf(m, fabsf(f[e] * w[e]));
             }
         }
-        row_reduce<kTPR, kF8>(s, m, area, at);
-        const float rstd = 1.f / sqrtf(s / (float)p.D + p.eps);
+        row_reduce<kTPR, kF8, kF8>(s, m, area, at);
+        Sum rstd{0.f, 0.f};
+        if (kF8)
+            rstd = exact_rstd(s, (float)p.D, p.eps);
+        else
+            rstd.hi = 1.f / sqrtf(s.hi / (float)p.D + p.eps);
         float inverse = 1.f;
         if (kF8) {
-            const float scale = row_scale(m * rstd, inverse);
+            const float scale = row_scale(m * rstd.hi, inverse);
             if (tid == 0) p.scale[t] = scale;
         }
-        if (tid == 0) p.rstd[t] = rstd;
+        if (tid == 0) p.rstd[t] = rstd.hi;
 #pragma unroll
         for (int j = 0; j < kNV; ++j) {
             const int i = tid + j * kTPR;
@@ -181,10 +231,8 @@ __global__ void __launch_bounds__(kTPR == 32 ? kWarpCta : kTPR) ssba_rms_norm_ke
             Vec<T>::get(v[j], f);
             load_w<n>(p.w + (size_t)i * n, w);
 #pragma unroll
-            for (int e = 0; e < n; ++e) f[e] = f[e] * rstd * w[e];
+            for (int e = 0; e < n; ++e) f[e] = kF8 ? product(f[e], rstd, w[e]) * inverse : f[e] * rstd.hi * w[e];
             if (kF8) {
-#pragma unroll
-                for (int e = 0; e < n; ++e) f[e] *= inverse;
                 uint32_t b[n / 4];
 #pragma unroll
                 for (int e = 0; e < n; e += 4) b[e / 4] = pack_e4m3(f + e);
@@ -213,7 +261,7 @@ template <class T, int kTPR, int kNV, bool kDh>
 __global__ void __launch_bounds__(kTPR == 32 ? kBwdWarps * 32 : kTPR) ssba_rms_norm_bwd_kernel(const NormBwdArgs p)
 {
     constexpr int n = Vec<T>::n, kRows = kTPR == 32 ? kBwdWarps : 1;
-    __shared__ float2 area[2][32];
+    __shared__ float4 area[2][32];
     extern __shared__ float cols[];  // [D], where a CTA's warps add up
     const int nv = p.D / n, tid = threadIdx.x % kTPR;
     float dw[kNV][n] = {};
@@ -231,7 +279,8 @@ __global__ void __launch_bounds__(kTPR == 32 ? kBwdWarps * 32 : kTPR) ssba_rms_n
             if (kDh) c[j] = in ? p.dh[t * nv + i] : make_uint4(0, 0, 0, 0);
         }
         const float rstd = p.rstd[t];
-        float s = 0.f, none = 0.f;
+        Sum s{0.f, 0.f};
+        float none = 0.f;
 #pragma unroll
         for (int j = 0; j < kNV; ++j) {
             const int i = tid + j * kTPR;
@@ -243,12 +292,12 @@ __global__ void __launch_bounds__(kTPR == 32 ? kBwdWarps * 32 : kTPR) ssba_rms_n
 #pragma unroll
             for (int e = 0; e < n; ++e) {
                 const float k = d[e] * (h[e] * rstd);
-                s = fmaf(k, w[e], s);
+                s.hi = fmaf(k, w[e], s.hi);
                 dw[j][e] += k;
             }
         }
-        row_reduce<kTPR, false>(s, none, area, at);
-        const float along = s / (float)p.D;
+        row_reduce<kTPR, false, false>(s, none, area, at);
+        const float along = s.hi / (float)p.D;
 #pragma unroll
         for (int j = 0; j < kNV; ++j) {
             const int i = tid + j * kTPR;

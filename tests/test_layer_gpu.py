@@ -427,7 +427,7 @@ def test_a_layer_forward_and_backward():
     F = z.shape[1] // 2
     out = (torch.nn.functional.silu(z[:, :F]) * z[:, F:]) @ d["Wd"].T + h
     grads = torch.autograd.grad(out, list(d.values()), dout.double())
-    far = lambda got, want: float((got.double() - want).norm() / want.norm())  # noqa: E731
+    far = lambda got, want: float((got.double() - want.detach()).norm() / want.detach().norm())  # noqa: E731
     assert far(s["out"], out) < 2.0 ** -4.7
     for name, want in zip(d, grads):
         assert far(g[name], want) < 2.0 ** -4.7, name
