@@ -221,6 +221,7 @@ int launch_product(const Product& p, const char* who, cudaStream_t st);
 // What either is expected to take, in microseconds.
 double product_pair_us(long long M, long long N, long long K, bool f8, bool gated);
 double product_rows_us(long long M, long long N, long long K, bool f8, bool gated);
+bool product_rows_fit(long long M);
 // dx = dz W and dW = dz^T x in one launch; either may be null.
 int launch_gradients(const void* dz, const void* x, const void* W, void* dx, void* dW, int T, int N, int K, const char* who,
                      cudaStream_t st);

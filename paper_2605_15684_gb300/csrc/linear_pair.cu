@@ -643,7 +643,7 @@ int launch_gradients(const void* dz, const void* x, const void* W, void* dx, voi
         p.set[1] = of_dW;
         return 5.6 + 0.33 * plan(p, most);
     };
-    if (dx && (T <= 64 || product_rows_us(T, K, N, false, false) + pair_us(false) < pair_us(true))) {
+    if (dx && (T <= 64 || (product_rows_fit(T) && product_rows_us(T, K, N, false, false) + pair_us(false) < pair_us(true)))) {
         Product q{};
         q.a = dz;
         q.b = W;

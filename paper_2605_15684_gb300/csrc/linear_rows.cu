@@ -81,25 +81,28 @@ __device__ __forceinline__ void put4(__nv_bfloat16* to, float4 v)
     *reinterpret_cast<uint2*>(to) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
 }
 
-// Four rows of D of a token: the cluster's partial sums in the order of its CTAs.
+// Four rows of D of a token: the cluster's partial sums in the order of its CTAs. All loads are under way before the
+// first is needed (one after the other they took 2 us of a join of eight).
 __device__ __forceinline__ float4 joined(uint32_t at, int split)
 {
-    float4 s = ld_cluster4(at_rank(at, 0));
-    for (int c = 1; c < split; ++c) {
-        const float4 v = ld_cluster4(at_rank(at, c));
-        s.x += v.x;
-        s.y += v.y;
-        s.z += v.z;
-        s.w += v.w;
+    float4 v[kMaxSplit];
+#pragma unroll
+    for (int c = 0; c < kMaxSplit; ++c) v[c] = c < split ? ld_cluster4(at_rank(at, c)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int c = 1; c < kMaxSplit; ++c) {
+        v[0].x += v[c].x;
+        v[0].y += v[c].y;
+        v[0].z += v[c].z;
+        v[0].w += v[c].w;
     }
-    return s;
+    return v[0];
 }
 
 __device__ __forceinline__ float4 scaled(float4 v, const RowsParams& p, int t, const float* ws)
 {
     if (!p.xs) return v;
     const float x = p.xs[t];
-    const float4 w = __ldg(reinterpret_cast<const float4*>(ws));
+    const float4 w = *reinterpret_cast<const float4*>(ws);  // plain loads: the grid in front may have written these
     return make_float4(v.x * (x * w.x), v.y * (x * w.y), v.z * (x * w.z), v.w * (x * w.w));
 }
 
@@ -249,7 +252,7 @@ __global__ void __launch_bounds__(kThreads) ssba_product_rows_kernel(const __gri
         } else {
             v = scaled(v, p, t0 + t, p.ws + n);
             if (p.bias) {
-                const float4 w = __ldg(reinterpret_cast<const float4*>(p.bias + n));
+                const float4 w = *reinterpret_cast<const float4*>(p.bias + n);
                 v = make_float4(v.x + w.x, v.y + w.y, v.z + w.z, v.w + w.w);
             }
             if (p.z) put4(p.z + o, v);
@@ -349,10 +352,13 @@ double product_rows_us(long long M, long long N, long long K, bool f8, bool gate
     return 8.4 + 0.37 * ((ksteps + split - 1) / split) * ((tiles * split + slots - 1) / slots);
 }
 
+bool product_rows_fit(long long M) { return (M + 127) / 128 <= 65535; }  // tiles of tokens are the grid's y
+
 int launch_product(const Product& q, const char* who, cudaStream_t st)
 {
     // Up to 64 tokens the weights are the rows; above, whichever is expected to end first.
-    const bool rows = q.M <= 64 || product_rows_us(q.M, q.N, q.K, q.f8, q.gated) < product_pair_us(q.M, q.N, q.K, q.f8, q.gated);
+    const bool rows = q.M <= 64 || (product_rows_fit(q.M) && product_rows_us(q.M, q.N, q.K, q.f8, q.gated) <
+                                                                product_pair_us(q.M, q.N, q.K, q.f8, q.gated));
     return rows ? launch_product_rows(q, who, st) : launch_product_pair(q, who, st);
 }
 

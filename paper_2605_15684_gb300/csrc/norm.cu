@@ -63,7 +63,7 @@ __device__ __forceinline__ void load_w(const float* w, float* f)
 {
 #pragma unroll
     for (int i = 0; i < n; i += 4) {
-        const float4 v = __ldg(reinterpret_cast<const float4*>(w + i));
+        const float4 v = *reinterpret_cast<const float4*>(w + i);  // plain: the grid in front may have written it
         f[i] = v.x;
         f[i + 1] = v.y;
         f[i + 2] = v.z;

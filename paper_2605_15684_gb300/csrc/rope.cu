@@ -59,19 +59,19 @@ struct Pack {
         E e[n];
         __device__ U() {}
     };
-    static __device__ __forceinline__ void load(const char* p, float* f)
+    static __device__ __forceinline__ void get(const W& w, float* f)
     {
         U u;
-        u.w = *reinterpret_cast<const W*>(p);
+        u.w = w;
 #pragma unroll
         for (int i = 0; i < n; ++i) f[i] = (float)u.e[i];
     }
-    static __device__ __forceinline__ void store(char* p, const float* f)
+    static __device__ __forceinline__ W put(const float* f)
     {
         U u;
 #pragma unroll
         for (int i = 0; i < n; ++i) u.e[i] = (E)f[i];
-        *reinterpret_cast<W*>(p) = u.w;
+        return u.w;
     }
 };
 
@@ -86,7 +86,8 @@ __device__ __forceinline__ void turn(float u, float v, float c, float s, float& 
 template <class E, int kN, bool kHalves>
 __global__ void __launch_bounds__(256) ssba_rope_kernel(const __grid_constant__ RopeArgs p)
 {
-    constexpr int kPairs = kHalves ? kN : kN / 2;
+    constexpr int kPairs = kHalves ? kN : kN / 2, kBatch = kHalves ? 3 : 6;
+    using W = typename Pack<E, kN>::W;
     grid_dep_wait();
     grid_dep_launch();
     const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -107,15 +108,23 @@ __global__ void __launch_bounds__(256) ssba_rope_kernel(const __grid_constant__ 
     const int h0 = (int)blockIdx.y * p.share, h1 = min(h0 + p.share, p.heads);
     const char* x = p.x + b * p.xs[0] + t * p.xs[1] + h0 * p.xs[2];
     char* o = p.out + b * p.os[0] + t * p.os[1] + h0 * p.os[2];
+    const int at = unit * kN * (int)sizeof(E), half = p.P * (int)sizeof(E);
     if (unit >= p.turned) {  // dimensions that stay (halves only: adjacent pairs past P turn by nothing)
-        const int at = (2 * p.P + (unit - p.turned) * kN) * (int)sizeof(E);
-        for (int h = h0; h < h1; ++h, x += p.xs[2], o += p.os[2]) {
-            float f[kN];
-            Pack<E, kN>::load(x + at, f);
-            Pack<E, kN>::store(o + at, f);
-        }
+        const int stay = (2 * p.P + (unit - p.turned) * kN) * (int)sizeof(E);
+        for (int h = h0; h < h1; ++h, x += p.xs[2], o += p.os[2]) *reinterpret_cast<W*>(o + stay) = *reinterpret_cast<const W*>(x + stay);
         return;
     }
+    // a batch of heads is loaded at once, the first before the sines are formed
+    W u[kBatch], v[kHalves ? kBatch : 1];
+    auto load = [&](int left) {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+            if (k < left) {
+                u[k] = *reinterpret_cast<const W*>(x + k * p.xs[2] + at);
+                if (kHalves) v[k] = *reinterpret_cast<const W*>(x + k * p.xs[2] + at + half);
+            }
+    };
+    load(h1 - h0);
     const int32_t* pos = p.pos + b * p.pos_batch + t * p.axes;
     float c[kPairs], s[kPairs];
 #pragma unroll
@@ -130,24 +139,30 @@ __global__ void __launch_bounds__(256) ssba_rope_kernel(const __grid_constant__ 
         sincospif((float)(int32_t)(turns >> 32) * 4.656612873077393e-10f, &s[i], &c[i]);
         if (p.inverse) s[i] = -s[i];
     }
-    const int at = unit * kN * (int)sizeof(E), half = p.P * (int)sizeof(E);
-#pragma unroll 4
-    for (int h = h0; h < h1; ++h, x += p.xs[2], o += p.os[2]) {
-        if constexpr (kHalves) {
-            float u[kN], v[kN], a[kN], d[kN];
-            Pack<E, kN>::load(x + at, u);
-            Pack<E, kN>::load(x + at + half, v);
+    for (int h = h0;;) {
 #pragma unroll
-            for (int i = 0; i < kN; ++i) turn(u[i], v[i], c[i], s[i], a[i], d[i]);
-            Pack<E, kN>::store(o + at, a);
-            Pack<E, kN>::store(o + at + half, d);
-        } else {
-            float u[kN], a[kN];
-            Pack<E, kN>::load(x + at, u);
+        for (int k = 0; k < kBatch; ++k) {
+            if (h + k >= h1) break;
+            char* to = o + k * p.os[2] + at;
+            float f[kN], a[kN];
+            Pack<E, kN>::get(u[k], f);
+            if constexpr (kHalves) {
+                float g[kN], d[kN];
+                Pack<E, kN>::get(v[k], g);
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) turn(u[2 * i], u[2 * i + 1], c[i], s[i], a[2 * i], a[2 * i + 1]);
-            Pack<E, kN>::store(o + at, a);
+                for (int i = 0; i < kN; ++i) turn(f[i], g[i], c[i], s[i], a[i], d[i]);
+                *reinterpret_cast<W*>(to + half) = Pack<E, kN>::put(d);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kPairs; ++i) turn(f[2 * i], f[2 * i + 1], c[i], s[i], a[2 * i], a[2 * i + 1]);
+            }
+            *reinterpret_cast<W*>(to) = Pack<E, kN>::put(a);
         }
+        h += kBatch;
+        if (h >= h1) return;
+        x += kBatch * p.xs[2];
+        o += kBatch * p.os[2];
+        load(h1 - h);
     }
 }
 

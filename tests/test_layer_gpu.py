@@ -504,3 +504,19 @@ def test_past_32_bits():
     pos[-40:] = 5
     turned = gb.rope_axes(x.view(T, 64, 64), pos, (32,), layout="halves", out=out.view(T, 64, 64))
     near(turned[-40:], ref.rope(x[-40:].view(1, 40, 64, 64), pos[-40:], (32,), layout="halves")[0], 0.05 + 0 * turned[-40:].double())
+
+
+def test_more_rows_than_a_grid_has():
+    """Narrow products of nine million rows: the few-row kernel's grid would not hold them."""
+    T = 9 * 2 ** 20
+    x = torch.zeros(T, 8, device="cuda", dtype=BF)
+    x[-5:] = torch.randn(5, 8, device="cuda").to(BF)
+    W = torch.randn(8, 8, device="cuda").to(BF)
+    y = gb.linear(x, W)
+    yr, _, ty, _ = ref.linear(x[-5:], W)
+    near(y[-5:], yr, ty)
+    assert not y[:-5].any()
+    dx, dW, _ = gb.linear_backward(x, x, W)
+    want = ref.linear_backward(x[-5:], x[-5:], W, None, None)
+    near(dx[-5:], *want[0])
+    near(dW, *want[1])
