@@ -222,9 +222,10 @@ int launch_product(const Product& p, const char* who, cudaStream_t st);
 double product_pair_us(long long M, long long N, long long K, bool f8, bool gated);
 double product_rows_us(long long M, long long N, long long K, bool f8, bool gated);
 bool product_rows_fit(long long M);
-// dx = dz W and dW = dz^T x in one launch; either may be null.
-int launch_gradients(const void* dz, const void* x, const void* W, void* dx, void* dW, int T, int N, int K, const char* who,
-                     cudaStream_t st);
+// dx = dz W and dW = dz^T x; either may be null. parts: gradients_workspace_bytes (only dW needs them).
+size_t gradients_workspace_bytes(int T, int N, int K);
+int launch_gradients(const void* dz, const void* x, const void* W, void* dx, void* dW, float* parts, int T, int N, int K,
+                     const char* who, cudaStream_t st);
 
 // dz = dy act'(z) ([T][N]; gated: dy [T][N], z and dz [T][2 N]), and with db its column sums by way of part.
 int launch_act_backward(const void* dy, const void* z, void* dz, float* db, float* part, int T, int N, int act, bool gated,
@@ -275,14 +276,16 @@ cudaError_t launch_early(void (*k)(P...), dim3 grid, int threads, size_t smem, c
 }
 
 // A tensor of `depth` planes of rows, its boxes box_rows rows of `box_cols` elements.
-inline bool encode_map(CUtensorMap* m, const void* base, bool f8, uint64_t cols, uint64_t rows, uint64_t depth,
+enum Element { kBf16, kE4m3, kF32 };
+
+inline bool encode_map(CUtensorMap* m, const void* base, Element type, uint64_t cols, uint64_t rows, uint64_t depth,
                        uint64_t row_bytes, uint64_t plane_bytes, uint32_t box_cols, uint32_t box_rows)
 {
     EncodeTiledFn fn = tensor_map_encoder();
     if (!fn) return false;
     cuuint64_t dims[3] = {cols, rows, depth}, strides[2] = {row_bytes, depth > 1 ? plane_bytes : row_bytes};
     cuuint32_t box[3] = {box_cols, box_rows, 1}, es[3] = {1, 1, 1};
-    return fn(m, f8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims,
+    return fn(m, type == kE4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : type == kF32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims,
               strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

@@ -143,7 +143,8 @@ size_t ssba_linear_backward_workspace_bytes(const ssba_linear_desc* desc)
     if (check_linear("ssba_linear_backward_workspace_bytes", desc) != SSBA_OK) return 0;
     const size_t dz = desc->act == SSBA_ACT_NONE ? 0 : round256((size_t)desc->T * desc->N * (desc->gated ? 4 : 2));
     const size_t part = desc->gated || !desc->T ? 0 : round256(sizeof(float) * desc->N * (size_t)act_backward_parts(desc->T, desc->N));
-    return dz + part;
+    const size_t sums = desc->T && desc->dtype == SSBA_BF16 ? round256(gradients_workspace_bytes(desc->T, desc->gated ? 2 * desc->N : desc->N, desc->K)) : 0;
+    return dz + part + sums;
 }
 
 int ssba_linear_backward(const ssba_linear_desc* desc, const void* dy, const void* x, const void* W, const void* z, void* dx,
@@ -176,14 +177,15 @@ int ssba_linear_backward(const ssba_linear_desc* desc, const void* dy, const voi
         return SSBA_ERR_WORKSPACE;
     }
     const void* dz = dy;
+    const size_t dzb = act ? round256((size_t)T * rows * 2) : 0;
+    const size_t part = gated ? 0 : round256(sizeof(float) * N * (size_t)act_backward_parts(T, N));
     if (act || db) {
-        const size_t dzb = act ? round256((size_t)T * rows * 2) : 0;
         if (act) dz = workspace;
         rc = launch_act_backward(dy, z, act ? workspace : nullptr, db, db ? reinterpret_cast<float*>(static_cast<char*>(workspace) + dzb) : nullptr,
                                  T, N, desc->act, gated, who, st);
         if (rc != SSBA_OK) return rc;
     }
-    if (dx || dW) rc = launch_gradients(dz, x, W, dx, dW, T, rows, K, who, st);
+    if (dx || dW) rc = launch_gradients(dz, x, W, dx, dW, reinterpret_cast<float*>(static_cast<char*>(workspace) + dzb + part), T, rows, K, who, st);
     return rc;
 }
 

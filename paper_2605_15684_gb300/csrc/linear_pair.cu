@@ -66,8 +66,9 @@ struct PairMaps {
     CUtensorMap a2, b2, y2;
 };
 
+// Tiles of a product; with split, each is cut along K into `split` (tiles counts them all).
 struct Tiles {
-    int m_tiles, n_tiles, tiles, ksteps;
+    int m_tiles, n_tiles, tiles, ksteps, split;
 };
 
 // A launch has one set of tiles, or (kBare) two, dx's and dW's: set `first`, then the other. Pair q of P takes
@@ -86,10 +87,10 @@ struct PairParams {
     uint64_t budget_ns;
 };
 
-// The k-th tile of pair q: which set, and the tile's row and column of tiles. Within a set, tiles go through the rows in
-// bands of kBand.
+// The k-th tile of pair q: which set, the tile's row and column of tiles, and its steps of K. Within a set (and part of K),
+// tiles go through the rows in bands of kBand.
 struct Item {
-    int set, m, n, ksteps;
+    int set, m, n, part, k0, k1;
 };
 
 __device__ __forceinline__ bool item_at(const PairParams& p, int q, int k, Item& o)
@@ -105,7 +106,14 @@ __device__ __forceinline__ bool item_at(const PairParams& p, int q, int k, Item&
         if (t >= p.other_tiles) return false;
     }
     const int n_tiles = o.set ? p.set[1].n_tiles : p.set[0].n_tiles, m_tiles = o.set ? p.set[1].m_tiles : p.set[0].m_tiles;
-    o.ksteps = o.set ? p.set[1].ksteps : p.set[0].ksteps;
+    const int ksteps = o.set ? p.set[1].ksteps : p.set[0].ksteps, split = o.set ? p.set[1].split : 1;
+    o.part = 0;
+    if (split > 1) {
+        o.part = t / (m_tiles * n_tiles);
+        t -= o.part * m_tiles * n_tiles;
+    }
+    o.k0 = (int)((long long)ksteps * o.part / split);
+    o.k1 = (int)((long long)ksteps * (o.part + 1) / split);
     const int band = t / (kBand * n_tiles), in = t - band * kBand * n_tiles;
     const int rows = min(kBand, m_tiles - band * kBand);
     o.n = in / rows;
@@ -260,8 +268,7 @@ __global__ void __launch_bounds__(PairCfg<kBN, kEpi, kZ>::kThreads, 1)
                 const int plane = kEpi == kGated ? (int)rank : 0;
                 const bool second = kEpi == kBare && o.set == 1;
                 const CUtensorMap *ma = second ? &maps.a2 : &maps.a, *mb = second ? &maps.b2 : &maps.b;
-                const int ksteps = o.ksteps;
-                for (int k = 0; k < ksteps; ++k, ++g) {
+                for (int k = o.k0; k < o.k1; ++k, ++g) {
                     const uint32_t s = g % kStages;
                     if (!mbar_wait(smem_u32(&sm.empty[s]), ((g / kStages) & 1) ^ 1, abortf, p.budget_ns)) {
                         dead = true;
@@ -312,8 +319,7 @@ __global__ void __launch_bounds__(PairCfg<kBN, kEpi, kZ>::kThreads, 1)
                 const uint32_t idesc = amn ? idesc_of(kF8, 256, kBN, true, kBmn) : idesc_of(kF8, 256, kBN, false, kBmn);
                 const uint32_t a_lbo = amn ? 8192 : 16;
                 const uint64_t a_step = amn ? 128 : 2;
-                const int ksteps = o.ksteps;
-                for (int k = 0; k < ksteps; ++k, ++g) {
+                for (int k = o.k0; k < o.k1; ++k, ++g) {
                     const uint32_t s = g % kStages;
                     if (!mbar_wait(smem_u32(&sm.full[s]), (g / kStages) & 1, abortf, p.budget_ns)) {
                         dead = true;
@@ -324,9 +330,9 @@ __global__ void __launch_bounds__(PairCfg<kBN, kEpi, kZ>::kThreads, 1)
                     const uint64_t bd = sdesc_sw128(b0 + s * C::kBBytes, kBmn ? 8192 : 16, 1024);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        mma<kF8, true>(d, ad + i * a_step, bd + (uint64_t)(i * (kBmn ? 128 : 2)), idesc, (k | i) != 0 ? 1u : 0u);
+                        mma<kF8, true>(d, ad + i * a_step, bd + (uint64_t)(i * (kBmn ? 128 : 2)), idesc, k > o.k0 || i > 0 ? 1u : 0u);
                     commit_pair(smem_u32(&sm.empty[s]));
-                    if (k == ksteps - 1) commit_pair(smem_u32(&sm.acc_full[acc]));
+                    if (k == o.k1 - 1) commit_pair(smem_u32(&sm.acc_full[acc]));
                 }
             }
             if (dead) {
@@ -345,6 +351,7 @@ __global__ void __launch_bounds__(PairCfg<kBN, kEpi, kZ>::kThreads, 1)
             const bool second = kEpi == kBare && o.set == 1;
             const int M = second ? p.M2 : p.M, N = second ? p.N2 : p.N;
             const CUtensorMap* my = second ? &maps.y2 : &maps.y;
+            const bool parts = second && p.set[1].split > 1;
             const int row0 = o.m * 256 + (int)rank * 128 + 32 * quad, row = row0 + lane, col = o.n * kCols + part * 64;
             const uint32_t acc = it & 1;
             const bool live = row0 < M && col < N;
@@ -428,7 +435,25 @@ __global__ void __launch_bounds__(PairCfg<kBN, kEpi, kZ>::kThreads, 1)
                             if (res) add(box[0], lane, 2 * i, v);
                         }
                     }
-                    if (!kZ && live) put(box[0], lane, 2 * i, v);
+                    if (kEpi == kBare && parts) {  // a part of K: fp32, 32 columns a box
+                        if (live) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                *reinterpret_cast<float4*>(unit(box[0], lane, 4 * (i & 1) + j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                            if (i == 1) {
+                                fence_proxy_async_smem();
+                                __syncwarp();
+                                if (lane == 0) {
+                                    tma_store(my, smem_u32(box[0]), col, row0, o.part);
+                                    store_commit();
+                                    store_wait_read<0>();
+                                }
+                                __syncwarp();
+                            }
+                        }
+                    } else if (!kZ && live) {
+                        put(box[0], lane, 2 * i, v);
+                    }
                 }
                 if (kZ && live) {
                     fence_proxy_async_smem();
@@ -447,7 +472,10 @@ __global__ void __launch_bounds__(PairCfg<kBN, kEpi, kZ>::kThreads, 1)
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    tma_store(my, smem_u32(box[0]), col, row0, 0);
+                    if (!(kEpi == kBare && parts))
+                        tma_store(my, smem_u32(box[0]), col, row0, 0);
+                    else if (col + 32 < N)
+                        tma_store(my, smem_u32(box[0]), col + 32, row0, o.part);
                     if (kZ && kEpi == kGated) {
                         tma_store(&maps.z, smem_u32(box[1]), col, row0, 0);
                         tma_store(&maps.z, smem_u32(box[2]), col, row0, 1);
@@ -510,7 +538,8 @@ long long plan(PairParams& p, int most)
         for (int n = 0; n <= top; ++n) {
             const long long left = (long long)b.tiles - (long long)n * over;
             const int rest = left > 0 ? (int)((left + P - over - 1) / (P - over)) : 0;
-            const long long t0 = over ? (c + 1ll) * a.ksteps + (long long)n * b.ksteps : 0, t1 = (long long)c * a.ksteps + (long long)rest * b.ksteps;
+            const long long sa = (a.ksteps + a.split - 1) / a.split, sb = b.tiles ? (b.ksteps + b.split - 1) / b.split : 0;
+            const long long t0 = over ? (c + 1ll) * sa + n * sb : 0, t1 = c * sa + rest * sb;
             const long long end = t0 > t1 ? t0 : t1;
             if (best < 0 || end < best) {
                 best = end;
@@ -555,6 +584,7 @@ int launch_pairs(PairMaps& maps, PairParams& p, const char* who, cudaStream_t st
 Tiles tiles_of(long long M, long long N, long long K, int cols, int bk)
 {
     Tiles t;
+    t.split = 1;
     t.m_tiles = (int)((M + 255) / 256);
     t.n_tiles = (int)((N + cols - 1) / cols);
     t.tiles = t.m_tiles * t.n_tiles;
@@ -576,11 +606,11 @@ int launch_as(const Product& q, const char* who, cudaStream_t st)
     PairMaps maps;
     memset(&maps, 0, sizeof(maps));
     const uint64_t M = q.M, N = q.N, K = q.K, planes = kEpi == kGated ? 2 : 1;
-    bool ok = encode_map(&maps.a, q.a, kF8, K, M, 1, K * e, 0, kBK, 128) &&
-              encode_map(&maps.b, q.b, kF8, K, N, planes, K * e, N * K * e, kBK, kBN / 2) &&
-              encode_map(&maps.y, q.y, false, N, M, 1, N * 2, 0, 64, 32);
-    if (kZ) ok = ok && encode_map(&maps.z, q.z, false, N, M, planes, planes * N * 2, N * 2, 64, 32);
-    if (q.r) ok = ok && encode_map(&maps.r, q.r, false, N, M, 1, N * 2, 0, 64, 32);
+    bool ok = encode_map(&maps.a, q.a, kF8 ? kE4m3 : kBf16, K, M, 1, K * e, 0, kBK, 128) &&
+              encode_map(&maps.b, q.b, kF8 ? kE4m3 : kBf16, K, N, planes, K * e, N * K * e, kBK, kBN / 2) &&
+              encode_map(&maps.y, q.y, kBf16, N, M, 1, N * 2, 0, 64, 32);
+    if (kZ) ok = ok && encode_map(&maps.z, q.z, kBf16, N, M, planes, planes * N * 2, N * 2, 64, 32);
+    if (q.r) ok = ok && encode_map(&maps.r, q.r, kBf16, N, M, 1, N * 2, 0, 64, 32);
     if (!ok) return no_maps(who);
     PairParams p = {};
     p.M = q.M;
@@ -629,21 +659,77 @@ double product_pair_us(long long M, long long N, long long K, bool f8, bool gate
     return 5.6 + 0.25 * ksteps * rounds(M, N, wide);
 }
 
-int launch_gradients(const void* dz, const void* x, const void* W, void* dx, void* dW, int T, int N, int K, const char* who,
-                     cudaStream_t st)
+namespace {
+
+constexpr int kMaxParts = 32;
+
+// dx and dW of a backward pass: dx with the weights as rows or in dW's launch, and the parts that dW's sum over the tokens is
+// cut into (where its tiles are too few for the SMs). By the sizes alone, whether or not both are wanted, so that
+// neither changes with the other.
+struct GradientPlan {
+    bool rows;
+    int parts;
+};
+
+// Steps of 0.33 us (operands along their rows, few pairs at work); parts add a join, some 3 us and their bytes.
+GradientPlan gradient_plan(int T, int N, int K)
 {
-    // dx of few rows takes the weights as the tensor cores' rows where that, and dW's launch of its own, ends sooner (also
-    // where dW is not wanted, so that dx is the same either way). A step of operands along their rows takes 0.33 us
-    // where few pairs have work.
     const int most = device_sm_count() / 2 > 0 ? device_sm_count() / 2 : 1;
     const Tiles of_dx = tiles_of(T, K, N, 256, 64), of_dW = tiles_of(N, K, T, 256, 64);
-    auto pair_us = [&](bool with_dx) {
-        PairParams p = {};
-        if (with_dx) p.set[0] = of_dx;
-        p.set[1] = of_dW;
-        return 5.6 + 0.33 * plan(p, most);
-    };
-    if (dx && (T <= 64 || (product_rows_fit(T) && product_rows_us(T, K, N, false, false) + pair_us(false) < pair_us(true)))) {
+    const bool fit = product_rows_fit(T);
+    const double rows_us = fit ? product_rows_us(T, K, N, false, false) : 0.;
+    GradientPlan best = {T <= 64, 1};
+    double best_us = -1.;
+    for (int parts = 1; parts <= kMaxParts; parts *= 2) {
+        if (parts > 1 && (of_dW.ksteps < 8 * parts || (long long)of_dW.tiles * parts > 2 * most)) break;
+        for (int rows = T <= 64 ? 1 : 0; rows < (fit ? 2 : 1); ++rows) {
+            PairParams p = {};
+            if (!rows) p.set[0] = of_dx;
+            p.set[1] = of_dW;
+            p.set[1].split = parts;
+            p.set[1].tiles *= parts;
+            const double us = 0.33 * plan(p, most) + (rows ? rows_us : 0.) + (parts > 1 ? 3. + 2e-6 * parts * N * K : 0.);
+            if (best_us < 0. || us < best_us) {
+                best_us = us;
+                best = {rows != 0, parts};
+            }
+        }
+    }
+    return best;
+}
+
+// dW = the parts' sum, in their order, rounded. n4: fours of a part.
+__global__ void __launch_bounds__(256) ssba_join_parts_kernel(const float4* part, int parts, long long n4, uint2* dW)
+{
+    grid_dep_wait();
+    grid_dep_launch();
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n4; i += (long long)gridDim.x * 256) {
+        float4 s = part[i];
+#pragma unroll 4
+        for (int k = 1; k < parts; ++k) {
+            const float4 v = part[k * n4 + i];
+            s.x += v.x;
+            s.y += v.y;
+            s.z += v.z;
+            s.w += v.w;
+        }
+        dW[i] = make_uint2(pack2(s.x, s.y), pack2(s.z, s.w));
+    }
+}
+
+}  // namespace
+
+size_t gradients_workspace_bytes(int T, int N, int K)
+{
+    const int parts = gradient_plan(T, N, K).parts;
+    return parts > 1 ? sizeof(float) * parts * (size_t)N * K : 0;
+}
+
+int launch_gradients(const void* dz, const void* x, const void* W, void* dx, void* dW, float* parts, int T, int N, int K,
+                     const char* who, cudaStream_t st)
+{
+    const GradientPlan g = gradient_plan(T, N, K);
+    if (dx && g.rows) {
         Product q{};
         q.a = dz;
         q.b = W;
@@ -662,20 +748,31 @@ int launch_gradients(const void* dz, const void* x, const void* W, void* dx, voi
     const uint64_t t = T, n = N, k = K;
     bool ok = true;
     if (dx) {
-        ok = encode_map(&maps.a, dz, false, n, t, 1, n * 2, 0, 64, 128) && encode_map(&maps.b, W, false, k, n, 1, k * 2, 0, 64, 64) &&
-             encode_map(&maps.y, dx, false, k, t, 1, k * 2, 0, 64, 32);
+        ok = encode_map(&maps.a, dz, kBf16, n, t, 1, n * 2, 0, 64, 128) && encode_map(&maps.b, W, kBf16, k, n, 1, k * 2, 0, 64, 64) &&
+             encode_map(&maps.y, dx, kBf16, k, t, 1, k * 2, 0, 64, 32);
         p.M = T;
         p.N = K;
-        p.set[0] = of_dx;
+        p.set[0] = tiles_of(T, K, N, 256, 64);
     }
     if (dW) {
-        ok = ok && encode_map(&maps.a2, dz, false, n, t, 1, n * 2, 0, 64, 64) && encode_map(&maps.b2, x, false, k, t, 1, k * 2, 0, 64, 64) &&
-             encode_map(&maps.y2, dW, false, k, n, 1, k * 2, 0, 64, 32);
+        ok = ok && encode_map(&maps.a2, dz, kBf16, n, t, 1, n * 2, 0, 64, 64) && encode_map(&maps.b2, x, kBf16, k, t, 1, k * 2, 0, 64, 64) &&
+             (g.parts > 1 ? encode_map(&maps.y2, parts, kF32, k, n, g.parts, k * 4, n * k * 4, 32, 32)
+                          : encode_map(&maps.y2, dW, kBf16, k, n, 1, k * 2, 0, 64, 32));
         p.M2 = N;
         p.N2 = K;
-        p.set[1] = of_dW;
+        p.set[1] = tiles_of(N, K, T, 256, 64);
+        p.set[1].split = g.parts;
+        p.set[1].tiles *= g.parts;
     }
-    return ok ? launch_pairs<256, false, kBare, false>(maps, p, who, st) : no_maps(who);
+    if (!ok) return no_maps(who);
+    const int rc = launch_pairs<256, false, kBare, false>(maps, p, who, st);
+    if (rc != SSBA_OK || !dW || g.parts == 1) return rc;
+    const long long n4 = (long long)N * K / 4, ctas = (n4 + 255) / 256, most = 16ll * device_sm_count();
+    const cudaError_t e = launch_early(ssba_join_parts_kernel, dim3((unsigned)(ctas < most ? ctas : most)), 256, 0, st, 1,
+                                       reinterpret_cast<const float4*>(parts), g.parts, n4, static_cast<uint2*>(dW));
+    if (e == cudaSuccess) return SSBA_OK;
+    set_error("%s: ssba_join_parts_kernel launch: %s", who, cudaGetErrorString(e));
+    return SSBA_ERR_CUDA;
 }
 
 }  // namespace layer

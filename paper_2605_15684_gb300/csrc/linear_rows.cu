@@ -293,9 +293,9 @@ int launch_as(const Product& q, const char* who, cudaStream_t st)
     const uint64_t T = q.M, N = q.N, K = q.K;
     RowsMaps maps;
     memset(&maps, 0, sizeof(maps));
-    bool ok = kWmn ? encode_map(&maps.w, q.b, kF8, N, K, 1, N * e, N * K * e, 64, 64)
-                   : encode_map(&maps.w, q.b, kF8, K, N, kGated ? 2 : 1, K * e, N * K * e, kBK, kOut);
-    ok = ok && encode_map(&maps.x, q.a, kF8, K, T, 1, K * e, T * K * e, kBK, kNT);
+    bool ok = kWmn ? encode_map(&maps.w, q.b, kF8 ? kE4m3 : kBf16, N, K, 1, N * e, N * K * e, 64, 64)
+                   : encode_map(&maps.w, q.b, kF8 ? kE4m3 : kBf16, K, N, kGated ? 2 : 1, K * e, N * K * e, kBK, kOut);
+    ok = ok && encode_map(&maps.x, q.a, kF8 ? kE4m3 : kBf16, K, T, 1, K * e, T * K * e, kBK, kNT);
     if (!ok) {
         set_error("%s: cuTensorMapEncodeTiled failed", who);
         return SSBA_ERR_CUDA;

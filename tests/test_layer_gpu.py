@@ -520,3 +520,20 @@ def test_more_rows_than_a_grid_has():
     want = ref.linear_backward(x[-5:], x[-5:], W, None, None)
     near(dx[-5:], *want[0])
     near(dW, *want[1])
+
+
+@pytest.mark.parametrize("T,K,N", [(5000, 72, 64), (9000, 520, 264), (20000, 1536, 392)])
+def test_weights_gradient_of_many_tokens(T, K, N):
+    """Few tiles and a long sum: dW is summed in parts. Alone and beside dx it is the same."""
+    randn, x, W, _, _ = operands(T, K, N, False, T)
+    dy, z = randn(T, N).to(BF), randn(T, N, std=2).to(BF)
+    for act in (None, "silu"):
+        zz = z if act else None
+        got = gb.linear_backward(dy, x, W, z=zz, act=act, bias=True)
+        for g, (want, tol), what in zip(got, ref.linear_backward(dy, x, W, zz, act), ("dx", "dW", "db")):
+            near(g, want, tol, what)
+        assert torch.equal(gb.linear_backward(dy, x, None, z=zz, act=act, dx=False)[1], got[1])
+        into = torch.zeros_like(got[1])
+        ws = torch.zeros(gb.linear_backward_workspace_bytes(T, N, K, act), dtype=torch.uint8, device="cuda")
+        gb.linear_backward(dy, x, W, z=zz, act=act, dW=into, workspace=ws)
+        assert torch.equal(into, got[1])
