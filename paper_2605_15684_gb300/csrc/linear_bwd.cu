@@ -14,7 +14,7 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kWarps = 8, kCols = 256;
+constexpr int kWarps = 8, kCols = 256, kCtas = 4;  // kCtas: of an SM
 
 struct ActArgs {
     const uint4 *dy, *z;
@@ -41,7 +41,7 @@ __device__ __forceinline__ uint4 put8(const float* f)
 }
 
 template <int kAct, bool kSum>
-__global__ void __launch_bounds__(kWarps * 32) ssba_act_bwd_kernel(const ActArgs p)
+__global__ void __launch_bounds__(kWarps * 32, kCtas) ssba_act_bwd_kernel(const ActArgs p)
 {
     __shared__ float sums[kSum ? kWarps : 1][kCols];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x * kCols + lane * 8;
@@ -50,24 +50,34 @@ __global__ void __launch_bounds__(kWarps * 32) ssba_act_bwd_kernel(const ActArgs
     const long long t1 = min((long long)p.T, ((long long)blockIdx.y + 1) * p.rows);
     float s[8] = {};
     if (c < p.N) {
-#pragma unroll 4
-        for (long long t = (long long)blockIdx.y * p.rows + warp; t < t1; t += kWarps) {
-            const size_t i = ((size_t)t * p.N + c) / 8;
-            float d[8];
-            get8(p.dy[i], d);
-            if (kAct != SSBA_ACT_NONE) {
-                float z[8];
-                get8(p.z[i], z);
+        // four rows a round, all loads under way at once
+        for (long long t = (long long)blockIdx.y * p.rows + warp; t < t1; t += 4 * kWarps) {
+            uint4 dy[4], z[4];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float v;
-                    d[e] *= act_slope<kAct>(z[e], v);
-                }
-                p.dz[i] = put8(d);
+            for (int r = 0; r < 4; ++r) {
+                const bool in = t + r * kWarps < t1;
+                const size_t i = ((size_t)(t + r * kWarps) * p.N + c) / 8;
+                dy[r] = in ? p.dy[i] : make_uint4(0, 0, 0, 0);
+                if (kAct != SSBA_ACT_NONE) z[r] = in ? p.z[i] : make_uint4(0, 0, 0, 0);
             }
-            if (kSum) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s[e] += d[e];
+            for (int r = 0; r < 4; ++r) {
+                float d[8];
+                get8(dy[r], d);
+                if (kAct != SSBA_ACT_NONE) {
+                    float f[8];
+                    get8(z[r], f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        float v;
+                        d[e] *= act_slope<kAct>(f[e], v);
+                    }
+                    if (t + r * kWarps < t1) p.dz[((size_t)(t + r * kWarps) * p.N + c) / 8] = put8(d);
+                }
+                if (kSum) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[e] += d[e];
+                }
             }
         }
     }
@@ -112,8 +122,8 @@ __global__ void __launch_bounds__(256) ssba_gated_bwd_kernel(const ActArgs p)
 
 int rows_of(int T, int N)
 {
-    // runs of rows, as many as give eight CTAs an SM, of 32 rows at least
-    const long long wide = (N + kCols - 1) / kCols, most = 8ll * device_sm_count();
+    // runs of rows, as many as run at once, of 32 rows at least
+    const long long wide = (N + kCols - 1) / kCols, most = (long long)kCtas * device_sm_count();
     long long runs = most / wide;
     if (runs < 1) runs = 1;
     long long rows = (T + runs - 1) / runs;

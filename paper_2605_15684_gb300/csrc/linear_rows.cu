@@ -6,7 +6,7 @@
 // Gated, a tile is 64 gate rows over the 64 matching up rows. For dx = dz W the weights come along their rows ("mn").
 // The partial tiles stay in shared memory (fp32, where the operands were) and each CTA of the cluster adds up and
 // finishes a share of the outputs through distributed shared memory: no workspace, no atomics, one order.
-// Bound by HBM (the weights once; tokens come from L2): about 100 KB of operands are under way in each of two CTAs an SM.
+// Bound by HBM (the weights once; tokens come from L2): some 200 KB of operands are under way in an SM, of two or three CTAs.
 // 192 threads: warp 0 TMA, warp 1 tcgen05.mma M = 128, N = kNT, warps 2-5 take D out of TMEM, and all finish.
 // Every wait is bounded; a timeout is written to the device status word.
 #include <algorithm>
@@ -26,15 +26,16 @@ constexpr uint32_t kABytes = 128 * 128;
 constexpr int kPitch = 132;  // floats of a column of D: 128 and a shift of banks
 constexpr int kMaxSplit = 8;
 
-template <int kNT>
+// kMany: three CTAs an SM with shorter rings, in place of two.
+template <int kNT, bool kMany>
 struct RowsCfg {
     static constexpr uint32_t kBBytes = kNT * 128;
-    static constexpr int kStages = kNT <= 16 ? 6 : kNT == 32 ? 5 : kNT == 64 ? 4 : 3;
+    static constexpr int kStages = kNT == 16 ? (kMany ? 4 : 6) : kNT == 32 ? (kMany ? 3 : 5) : kNT == 64 ? 4 : 3;
 };
 
-template <int kNT>
+template <int kNT, bool kMany>
 struct __align__(1024) RowsSmem {
-    using C = RowsCfg<kNT>;
+    using C = RowsCfg<kNT, kMany>;
     union {
         struct {
             uint8_t a[C::kStages][kABytes];
@@ -106,17 +107,17 @@ __device__ __forceinline__ float4 scaled(float4 v, const RowsParams& p, int t, c
     return make_float4(v.x * (x * w.x), v.y * (x * w.y), v.z * (x * w.z), v.w * (x * w.w));
 }
 
-template <int kNT, bool kF8, bool kWmn, bool kGated>
+template <int kNT, bool kMany, bool kF8, bool kWmn, bool kGated>
 __global__ void __launch_bounds__(kThreads) ssba_product_rows_kernel(const __grid_constant__ RowsMaps maps, const RowsParams p)
 {
-    using C = RowsCfg<kNT>;
+    using C = RowsCfg<kNT, kMany>;
+    using Smem = RowsSmem<kNT, kMany>;
     constexpr int kStages = C::kStages, kBK = kF8 ? 128 : 64;
     constexpr int kOut = kGated ? 64 : 128;  // outputs a token of a tile
     constexpr uint32_t kIdesc = idesc_of(kF8, 128, kNT, kWmn, false);
     constexpr uint32_t kTmem = kNT < 32 ? 32 : kNT;
     extern __shared__ uint8_t smem_raw[];
-    RowsSmem<kNT>& sm = *reinterpret_cast<RowsSmem<kNT>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
-                                                          ~static_cast<uintptr_t>(1023));
+    Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)cluster_rank();
     const int n0 = (int)(blockIdx.x / p.split) * kOut, t0 = (int)blockIdx.y * kNT;
@@ -273,20 +274,20 @@ __global__ void __launch_bounds__(kThreads) ssba_product_rows_kernel(const __gri
     if (warp == 1) tmem_dealloc(tbase, kTmem);
 }
 
-// CTAs that share a tile's K: as many as two an SM hold, with two steps each at least.
-int split_of(long long tiles, int ksteps)
+// CTAs that share a tile's K: as many as the SMs hold (ctas each), with two steps each at least.
+int split_of(long long tiles, int ksteps, int ctas)
 {
     int split = 1;
-    while (split < kMaxSplit && tiles * split * 2 <= 2ll * device_sm_count() && ksteps >= split * 4) split *= 2;
+    while (split < kMaxSplit && tiles * split * 2 <= (long long)ctas * device_sm_count() && ksteps >= split * 4) split *= 2;
     return split;
 }
 
-template <int kNT, bool kF8, bool kWmn, bool kGated>
+template <int kNT, bool kMany, bool kF8, bool kWmn, bool kGated>
 int launch_as(const Product& q, const char* who, cudaStream_t st)
 {
     constexpr int kBK = kF8 ? 128 : 64, kOut = kGated ? 64 : 128;
-    auto kernel = ssba_product_rows_kernel<kNT, kF8, kWmn, kGated>;
-    const size_t smem = sizeof(RowsSmem<kNT>) + 1024;
+    auto kernel = ssba_product_rows_kernel<kNT, kMany, kF8, kWmn, kGated>;
+    const size_t smem = sizeof(RowsSmem<kNT, kMany>) + 1024;
     static PerDeviceOnce attr;
     attr.run([=] { cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
     const int e = kF8 ? 1 : 2;
@@ -318,29 +319,40 @@ int launch_as(const Product& q, const char* who, cudaStream_t st)
         return SSBA_ERR_CUDA;
     }
     const long long tiles = (q.N + kOut - 1) / kOut, cols = (q.M + kNT - 1) / kNT;
-    const int split = p.split = split_of(tiles * cols, p.ksteps);
+    const int split = p.split = split_of(tiles * cols, p.ksteps, kMany ? 3 : 2);
     const cudaError_t err = launch_early(kernel, dim3((unsigned)(tiles * split), (unsigned)cols), kThreads, smem, st, split, maps, p);
     if (err == cudaSuccess) return SSBA_OK;
     set_error("%s: ssba_product_rows_kernel launch: %s", who, cudaGetErrorString(err));
     return SSBA_ERR_CUDA;
 }
 
-template <int kNT>
+template <int kNT, bool kMany>
 int launch_tokens(const Product& q, const char* who, cudaStream_t st)
 {
-    if (q.b_mn) return launch_as<kNT, false, true, false>(q, who, st);
-    if (q.gated) return q.f8 ? launch_as<kNT, true, false, true>(q, who, st) : launch_as<kNT, false, false, true>(q, who, st);
-    return q.f8 ? launch_as<kNT, true, false, false>(q, who, st) : launch_as<kNT, false, false, false>(q, who, st);
+    if (q.b_mn) return launch_as<kNT, kMany, false, true, false>(q, who, st);
+    if (q.gated) return q.f8 ? launch_as<kNT, kMany, true, false, true>(q, who, st) : launch_as<kNT, kMany, false, false, true>(q, who, st);
+    return q.f8 ? launch_as<kNT, kMany, true, false, false>(q, who, st) : launch_as<kNT, kMany, false, false, false>(q, who, st);
+}
+
+// Three CTAs an SM where that lets K be cut once more than two do, so that the SMs have more alike to read: one token,
+// K 4096, gated N 11008 33.4 -> 31.1 us; 16 tokens, 1536 x 6144 7.3 -> 6.8. Elsewhere the longer rings win: 7 tokens, 4096 x
+// 4096 8.6 us against 10.5; 16 tokens, gated 1536 x 4096 7.6 against 9.4.
+template <int kNT>
+int launch_few(const Product& q, const char* who, cudaStream_t st)
+{
+    const long long tiles = (q.N + (q.gated ? 63 : 127)) / (q.gated ? 64 : 128);
+    const int ksteps = (q.K + (q.f8 ? 127 : 63)) / (q.f8 ? 128 : 64);
+    return split_of(tiles, ksteps, 3) > split_of(tiles, ksteps, 2) ? launch_tokens<kNT, true>(q, who, st) : launch_tokens<kNT, false>(q, who, st);
 }
 
 }  // namespace
 
 int launch_product_rows(const Product& q, const char* who, cudaStream_t st)
 {
-    if (q.M <= 16) return launch_tokens<16>(q, who, st);
-    if (q.M <= 32) return launch_tokens<32>(q, who, st);
-    if (q.M <= 64) return launch_tokens<64>(q, who, st);
-    return launch_tokens<128>(q, who, st);
+    if (q.M <= 16) return launch_few<16>(q, who, st);
+    if (q.M <= 32) return launch_few<32>(q, who, st);
+    if (q.M <= 64) return launch_tokens<64, false>(q, who, st);
+    return launch_tokens<128, false>(q, who, st);
 }
 
 // Microseconds of a call with weights as rows and 128 tokens a tile: a start and an end of 8.4 in all (the join of the parts
@@ -348,7 +360,7 @@ int launch_product_rows(const Product& q, const char* who, cudaStream_t st)
 double product_rows_us(long long M, long long N, long long K, bool f8, bool gated)
 {
     const long long tiles = ((N + (gated ? 63 : 127)) / (gated ? 64 : 128)) * ((M + 127) / 128), slots = 2ll * device_sm_count();
-    const int ksteps = (int)((K + (f8 ? 127 : 63)) / (f8 ? 128 : 64)), split = split_of(tiles, ksteps);
+    const int ksteps = (int)((K + (f8 ? 127 : 63)) / (f8 ? 128 : 64)), split = split_of(tiles, ksteps, 2);
     return 8.4 + 0.37 * ((ksteps + split - 1) / split) * ((tiles * split + slots - 1) / slots);
 }
 
