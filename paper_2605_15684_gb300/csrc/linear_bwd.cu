@@ -14,7 +14,7 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kWarps = 8, kCols = 256, kCtas = 4;  // kCtas: of an SM
+constexpr int kWarps = 8, kCols = 256, kCtas = 3;  // kCtas: of an SM
 
 struct ActArgs {
     const uint4 *dy, *z;
