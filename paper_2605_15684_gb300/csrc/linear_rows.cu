@@ -30,7 +30,7 @@ constexpr int kMaxSplit = 8;
 template <int kNT, bool kMany>
 struct RowsCfg {
     static constexpr uint32_t kBBytes = kNT * 128;
-    static constexpr int kStages = kNT == 16 ? (kMany ? 4 : 6) : kNT == 32 ? 5 : kNT == 64 ? 4 : 3;
+    static constexpr int kStages = kNT == 16 ? (kMany ? 4 : 6) : kNT == 32 ? (kMany ? 3 : 5) : kNT == 64 ? 4 : 3;
 };
 
 template <int kNT, bool kMany>
@@ -337,20 +337,21 @@ int launch_tokens(const Product& q, const char* who, cudaStream_t st)
 
 // Three CTAs an SM where that lets K be cut once more than two do, so that the SMs have more alike to read: one token,
 // K 4096, gated N 11008 33.4 -> 31.1 us; 16 tokens, 1536 x 6144 7.3 -> 6.8. Elsewhere the longer rings win: 7 tokens, 4096 x
-// 4096 8.6 us against 10.5; 16 tokens, gated 1536 x 4096 7.6 against 9.4; 32 tokens, 8-bit gated 4096 x 12288 22.4 against 24.0 (cold).
-int launch_16(const Product& q, const char* who, cudaStream_t st)
+// 4096 8.6 us against 10.5; 16 tokens, gated 1536 x 4096 7.6 against 9.4. 32 tokens, 8-bit gated 4096 x 12288: three 19.2 us, two 20.6.
+template <int kNT>
+int launch_few(const Product& q, const char* who, cudaStream_t st)
 {
     const long long tiles = (q.N + (q.gated ? 63 : 127)) / (q.gated ? 64 : 128);
     const int ksteps = (q.K + (q.f8 ? 127 : 63)) / (q.f8 ? 128 : 64);
-    return split_of(tiles, ksteps, 3) > split_of(tiles, ksteps, 2) ? launch_tokens<16, true>(q, who, st) : launch_tokens<16, false>(q, who, st);
+    return split_of(tiles, ksteps, 3) > split_of(tiles, ksteps, 2) ? launch_tokens<kNT, true>(q, who, st) : launch_tokens<kNT, false>(q, who, st);
 }
 
 }  // namespace
 
 int launch_product_rows(const Product& q, const char* who, cudaStream_t st)
 {
-    if (q.M <= 16) return launch_16(q, who, st);
-    if (q.M <= 32) return launch_tokens<32, false>(q, who, st);
+    if (q.M <= 16) return launch_few<16>(q, who, st);
+    if (q.M <= 32) return launch_few<32>(q, who, st);
     if (q.M <= 64) return launch_tokens<64, false>(q, who, st);
     return launch_tokens<128, false>(q, who, st);
 }
