@@ -502,7 +502,8 @@ SSBA_API int ssba_cache_copy(const ssba_cache_desc* desc, const ssba_cache* cach
  *   Layout     rows are tokens, contiguous, 16-byte aligned; weights are [outputs][inputs].
  *   Sums       fp32 throughout; a 16-bit output is rounded once, from fp32. Deterministic (no atomics).
  *   8 bits     e4m3 values with one fp32 scale a row: a value stands for itself times its row's scale.
- *   Errors     as above; T = 0 is no work and succeeds (a sum over no rows is 0). */
+ *   Errors     as above; T = 0 is no work and succeeds (a sum over no rows is 0). An output or workspace that lies on another
+ *              tensor of the call is refused, but for those that are said to be allowed (the very same tensor). */
 
 /* The norm in front of a product, with the residual's addition:
  *   h = round(x + r),  rstd = 1 / sqrt(mean_i h_i^2 + eps),  y_i = h_i rstd w_i       (h is x without r)
@@ -589,7 +590,8 @@ typedef struct {
 /*   x, out      device; head h of token t of sequence b starts at b s[0] + t s[1] + h s[2] elements (x_stride, out_stride,
  *               host arrays of three), its dimensions side by side. Aligned to their element; the more of base, strides,
  *               head_dim (and, in halves, P) is in multiples of 16 bytes, the wider the accesses. Strides >= 0. out may be
- *               x with the same strides; else they may not overlap, and no two heads of out.
+ *               x with the same strides; else they may not share an element (other parts of one tensor may be interleaved, at the
+ *               same strides), nor may two heads of out.
  *   pos         device, int32, any sign: axis a of token t of sequence b at b pos_batch + t axes + a (pos_batch 0:
  *               the same positions for all sequences). */
 SSBA_API int ssba_rope_axes(const ssba_rope_desc* desc, const void* x, const int64_t* x_stride, const int32_t* pos,

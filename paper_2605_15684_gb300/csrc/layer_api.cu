@@ -1,6 +1,7 @@
 // layer_api.cu -- the entry points of a layer around its attention (include/ssba.h): argument validation on the host and
 // kernel launches on the caller's stream.
 #include <cmath>
+#include <utility>
 
 #include "layer.cuh"
 
@@ -16,6 +17,62 @@ int invalid(const char* who, const char* what)
 {
     set_error("%s: %s", who, what);
     return SSBA_ERR_INVALID;
+}
+
+// A range of device memory that a call reads or writes.
+struct Range {
+    const void* at;
+    size_t bytes;
+    bool meets(const Range& o) const
+    {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(at), b = reinterpret_cast<uintptr_t>(o.at);
+        return at && o.at && a < b + o.bytes && b < a + bytes;
+    }
+};
+
+// Whether `out` lies on any of the others. (Where it may be one of them, the caller leaves that one out if they are the same.)
+template <size_t n>
+bool lies_on(const Range& out, const Range (&others)[n])
+{
+    for (const Range& o : others)
+        if (out.meets(o)) return true;
+    return false;
+}
+
+Range unless_same(const Range& r, const void* out) { return r.at == out ? Range{nullptr, 0} : r; }
+
+// Whether two sets of heads that lie alike, `apart` elements from one another, have an element in common: apart is then a sum
+// of c[i] * stride[i], |c[i]| < size[i]. Each stride steps past the dimensions inside it (given largest first), so the
+// coefficients are the quotients or next to them.
+bool lie_on_each_other(int64_t apart, const int64_t* size, const int64_t* stride, int dims)
+{
+    if (dims == 0) return apart == 0;
+    if (size[0] <= 1 || stride[0] == 0) return lie_on_each_other(apart, size + 1, stride + 1, dims - 1);
+    const int64_t q = apart / stride[0];
+    for (int64_t c = q - 1; c <= q + 1; ++c)
+        if (c < size[0] && -c < size[0] && lie_on_each_other(apart - c * stride[0], size + 1, stride + 1, dims - 1)) return true;
+    return false;
+}
+
+// Whether writing `out` may change an x that is still to be read: not where out is x, nor where they share nothing.
+bool rope_overlaps(const ssba_rope_desc& d, const void* x, const int64_t* xs, const void* out, const int64_t* os, int64_t es)
+{
+    auto extent = [&](const void* at, const int64_t* s) {
+        return Range{at, (size_t)(((d.B - 1) * s[0] + (d.T - 1) * s[1] + (d.heads - 1) * s[2] + d.head_dim) * es)};
+    };
+    if (!extent(x, xs).meets(extent(out, os))) return false;
+    int64_t size[4] = {d.B, d.T, d.heads, d.head_dim}, stride[4] = {os[0], os[1], os[2], 1};
+    for (int i = 0; i < 3; ++i)
+        if (xs[i] != os[i] && size[i] > 1) return true;
+    if (x == out) return false;
+    const int64_t bytes = (int64_t)(reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(x));
+    if (bytes % es) return true;
+    for (int i = 1; i < 4; ++i)
+        for (int j = i; j > 0 && stride[j] > stride[j - 1]; --j) {
+            std::swap(stride[j], stride[j - 1]);
+            std::swap(size[j], size[j - 1]);
+        }
+    return lie_on_each_other(bytes / es, size, stride, 4);
 }
 
 int check_norm(const char* who, int32_t T, int32_t D, int32_t dtype)
@@ -82,6 +139,11 @@ int ssba_rms_norm(const void* x, const void* r, const float* w, int32_t T, int32
     if (!aligned(x, 16) || !aligned(r, 16) || !aligned(w, 16) || !aligned(h, 16) || !aligned(y, 16) || !aligned(scale, 4) ||
         !aligned(rstd, 4))
         return invalid(who, "x, r, w, h and y must be 16-byte aligned, scale and rstd 4-byte");
+    const size_t rows = (size_t)T * D * (dtype == SSBA_BF16 ? 2 : 4), out = scale ? (size_t)T * D : rows, each = sizeof(float) * T;
+    const Range X{x, rows}, R{r, rows}, W{w, sizeof(float) * D}, H{h, rows}, Y{y, out};
+    if (lies_on(H, {unless_same(X, h), unless_same(R, h), W}) || lies_on(Y, {scale ? X : unless_same(X, y), R, W, H}) ||
+        lies_on(Range{rstd, each}, {X, R, W, H, Y}) || lies_on(Range{scale, scale ? each : 0}, {X, R, W, H, Y, Range{rstd, each}}))
+        return invalid(who, "an output lies on another tensor of the call (h may be x or r, and y of dtype x)");
     return launch_rms_norm(x, r, w, T, D, dtype, eps, h, y, scale != nullptr, scale, rstd, static_cast<cudaStream_t>(stream));
 }
 
@@ -115,6 +177,11 @@ int ssba_rms_norm_backward(const void* dy, const void* h, const float* w, const 
         set_error("%s: workspace of %zu bytes (16-byte aligned) required, got %zu", who, need, ws_bytes);
         return SSBA_ERR_WORKSPACE;
     }
+    const size_t rows = (size_t)T * D * (dtype == SSBA_BF16 ? 2 : 4);
+    const Range DY{dy, rows}, H{h, rows}, DH{dh, rows}, W{w, sizeof(float) * D}, K{rstd, sizeof(float) * T}, DX{dx, rows}, S{workspace, need};
+    if (lies_on(DX, {unless_same(DY, dx), H, unless_same(DH, dx), W, K, S}) || lies_on(Range{dw, sizeof(float) * D}, {DY, H, DH, W, K, DX, S}) ||
+        lies_on(S, {DY, H, DH, W, K}))
+        return invalid(who, "an output or the workspace lies on another tensor of the call (dx may be dy or dh)");
     return launch_rms_norm_backward(dy, h, w, rstd, dh, T, D, dtype, dx, dw, static_cast<float*>(workspace), st);
 }
 
@@ -134,6 +201,10 @@ int ssba_linear(const ssba_linear_desc* desc, const void* x, const void* W, cons
     if (!aligned(x, 16) || !aligned(W, 16) || !aligned(w_scale, 16) || !aligned(bias, 16) || !aligned(r, 16) ||
         !aligned(y, 16) || !aligned(z, 16) || !aligned(x_scale, 4))
         return invalid(who, "x, W, w_scale, bias, r, y and z must be 16-byte aligned, x_scale 4-byte");
+    const size_t T = desc->T, N = desc->N, K = desc->K, rows = desc->gated ? 2 * N : N, e = f8 ? 1 : 2;
+    const Range X{x, T * K * e}, M{W, rows * K * e}, XS{x_scale, 4 * T}, WS{w_scale, 4 * rows}, B{bias, 4 * N}, R{r, T * N * 2}, Y{y, T * N * 2};
+    if (lies_on(Y, {X, M, XS, WS, B, unless_same(R, y)}) || lies_on(Range{z, T * rows * 2}, {X, M, XS, WS, B, R, Y}))
+        return invalid(who, "an output lies on another tensor of the call (y may be r)");
     const Product p{x, W, y, z, r, x_scale, w_scale, bias, desc->T, desc->N, desc->K, desc->act, f8, false, desc->gated != 0};
     return launch_product(p, who, static_cast<cudaStream_t>(stream));
 }
@@ -175,6 +246,14 @@ int ssba_linear_backward(const ssba_linear_desc* desc, const void* dy, const voi
     if (need && (!workspace || ws_bytes < need || !aligned(workspace, 16))) {
         set_error("%s: workspace of %zu bytes (16-byte aligned) required, got %zu", who, need, ws_bytes);
         return SSBA_ERR_WORKSPACE;
+    }
+    {
+        const size_t t = T, n = N, k = K;
+        const Range DY{dy, t * n * 2}, X{dW ? x : nullptr, t * k * 2}, M{dx ? W : nullptr, rows * k * 2}, Z{act ? z : nullptr, t * rows * 2};
+        const Range DX{dx, t * k * 2}, DW{dW, rows * k * 2}, DB{db, 4 * n}, S{workspace, need};
+        if (lies_on(DX, {DY, X, M, Z}) || lies_on(DW, {DY, X, M, Z, DX}) || lies_on(DB, {DY, X, M, Z, DX, DW}) ||
+            lies_on(S, {DY, X, M, Z, DX, DW, DB}))
+            return invalid(who, "an output or the workspace lies on another tensor of the call");
     }
     const void* dz = dy;
     const size_t dzb = act ? round256((size_t)T * rows * 2) : 0;
@@ -234,6 +313,7 @@ int ssba_rope_axes(const ssba_rope_desc* desc, const void* x, const int64_t* x_s
     if (d.layout == SSBA_ROPE_PAIRS)
         for (int i = 0; i < 3; ++i) fits = fits && x_stride[i] % 2 == 0 && out_stride[i] % 2 == 0;
     if (!fits) return invalid(who, "x and out must be aligned to an element (adjacent pairs: to a pair, strides too), pos to 4 bytes");
+    if (rope_overlaps(d, x, x_stride, out, out_stride, es)) return invalid(who, "out lies on x (it may be x with the same strides)");
     return launch_rope(d, x, x_stride, pos, pos_batch, out, out_stride, static_cast<cudaStream_t>(stream));
 }
 

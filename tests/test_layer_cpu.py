@@ -140,3 +140,38 @@ def test_rope_descriptor_refusals():
 ])
 def test_overlapping_outputs_are_seen(shape, strides, dense):
     assert layer._dense_heads(shape, strides) is dense
+
+
+def test_outputs_on_other_tensors_are_refused(lib):
+    """Addresses far apart, but for one output that overlaps one other tensor of its call."""
+    at = [0x100000000 * (i + 1) for i in range(12)]
+    x, r, w, h, y, sc, k = at[:7]
+    norm = lambda **a: lib.ssba_rms_norm(*{**dict(x=x, r=r, w=w, T=4, D=64, dtype=0, eps=1e-6, h=h, y=y, s=sc, k=k), **a}.values(), None)  # noqa: E731
+    for bad in (dict(h=x + 16), dict(h=w), dict(y=x), dict(y=h + 16), dict(y=r), dict(k=y + 4), dict(s=h), dict(s=k), dict(s=None, y=x + 16)):
+        assert norm(**bad) == INV, bad
+        assert b"lies on" in lib.ssba_last_error()
+    dy, hh, dh, dx, dw, ws = at[:6]
+    back = lambda **a: lib.ssba_rms_norm_backward(*{**dict(dy=dy, h=hh, w=at[6], k=at[7], dh=dh, T=400, D=64, dtype=0, dx=dx, dw=dw, ws=ws, n=1 << 28), **a}.values(), None)  # noqa: E731
+    for bad in (dict(dx=hh), dict(dx=dy + 16), dict(dw=dx), dict(ws=hh), dict(dx=ws)):
+        assert back(**bad) == INV, bad
+    X, W, xs, wsc, b, res, Y, Z = at[:8]
+    lin = lambda d, **a: lib.ssba_linear(linear_desc(**d), *{**dict(x=X, W=W, xs=None, ws=None, b=b, r=res, y=Y, z=Z), **a}.values(), None)  # noqa: E731
+    for bad in (dict(y=X), dict(y=W + 16), dict(y=res + 16), dict(z=Y), dict(z=res), dict(y=b), dict(z=X)):
+        assert lin({}, **bad) == INV, bad
+    assert lin(dict(gated=1, act=3), b=None, r=None, z=Y + 4 * 64 * 2 - 16) == INV
+    bwd = lambda **a: lib.ssba_linear_backward(linear_desc(act=2), *{**dict(dy=at[0], x=at[1], W=at[2], z=at[3], dx=at[4], dW=at[5], db=at[6], ws=at[7], n=1 << 28), **a}.values(), None)  # noqa: E731
+    for bad in (dict(dx=at[0]), dict(dx=at[1]), dict(dW=at[2]), dict(dW=at[4] + 16), dict(db=at[3]), dict(ws=at[0]), dict(ws=at[5]), dict(dx=at[7])):
+        assert bwd(**bad) == INV, bad
+
+
+@pytest.mark.parametrize("apart,xs,os", [
+    (64, (768, 192, 64), (768, 192, 64)),     # a head further on in the same tensor
+    (2, (768, 192, 64), (768, 192, 64)),      # two dimensions further on
+    (192 * 3, (768, 192, 64), (768, 192, 64)),
+    (0, (768, 192, 64), (768, 64, 256)),      # the same tensor in another order
+    (1536, (768, 192, 64), (1536, 192, 64)),
+])
+def test_rope_refuses_an_output_on_its_input(lib, apart, xs, os):
+    x = 0x100000000
+    rc = lib.ssba_rope_axes(rope_desc(B=4, heads=3), x, S(*xs), 0x900000000, 0, x + 2 * apart, S(*os), None)
+    assert rc == INV and b"lies on" in lib.ssba_last_error()

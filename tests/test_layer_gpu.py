@@ -110,8 +110,8 @@ def operands(T, K, N, f8, seed, rows=None):
     return randn, x.to(BF), W.to(BF), None, None
 
 
-SIZES = [(1, 16, 8), (1, 1536, 1536), (7, 4096, 264), (16, 80, 136), (17, 528, 512), (40, 1040, 1000), (64, 64, 64), (100, 512, 640),
-         (129, 208, 1536), (256, 1536, 320), (257, 128, 256), (300, 1536, 392), (515, 80, 1544), (2500, 336, 776), (700, 144, 4104)]
+SIZES = [(1, 16, 8), (1, 1536, 1528), (7, 4096, 264), (16, 80, 136), (17, 528, 512), (40, 1040, 1000), (64, 64, 64), (100, 512, 640),
+         (129, 208, 1528), (256, 1536, 320), (257, 128, 256), (300, 1536, 392), (515, 80, 1544), (2500, 336, 776), (700, 144, 4104)]
 
 
 @pytest.mark.parametrize("T,K,N", SIZES)
