@@ -556,6 +556,15 @@ typedef struct {
 SSBA_API int ssba_linear(const ssba_linear_desc* desc, const void* x, const void* W, const float* x_scale,
                          const float* w_scale, const float* bias, const void* r, void* y, void* z, void* stream);
 
+/* Test hook for failure detection in the products: runs ssba_linear (bf16, without scales, bias, residual and z) with every
+ * wait limited to budget_ns of wall time (clamped to [1 ms, 2 s]) and CTA 0 announcing its first copies without
+ * issuing them, so that the waits on them run out. Its roles stop, wait (bounded) for their own copies and products in flight,
+ * free the tensor memory and return; other tiles are finished. The device status word reads SSBA_ERR_TIMEOUT
+ * (ssba_get_status, after a synchronize), y is undefined, and the context stays usable. No fault, trap or endless wait is
+ * involved. */
+SSBA_API int ssba_test_linear_timeout(const ssba_linear_desc* desc, const void* x, const void* W, void* y,
+                                      uint64_t budget_ns, void* stream);
+
 /* Its gradients, SSBA_BF16 alone. dz = dy act'(z) (gated: dg = dy u act'(g), du = dy act(g)), rounded to bf16, then
  * dx = dz W and dW = dz^T x; db = sum_t dz before that rounding.
  *   dy          device, bf16 [T][N]: the gradient of y (and, as it is, of r).

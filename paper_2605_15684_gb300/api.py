@@ -36,7 +36,7 @@ EXPORTED = ("ssba_keep_count", "ssba_mask_workspace_bytes", "ssba_build_mask", "
             "ssba_cache_append", "ssba_cache_select", "ssba_cache_attend_workspace_bytes", "ssba_cache_attend",
             "ssba_cache_copy", "ssba_test_cache_timeout", "ssba_rms_norm", "ssba_rms_norm_backward",
             "ssba_rms_norm_backward_workspace_bytes", "ssba_linear", "ssba_linear_backward",
-            "ssba_linear_backward_workspace_bytes", "ssba_rope_axes", "ssba_get_status", "ssba_last_error", "ssba_timeline_read")
+            "ssba_linear_backward_workspace_bytes", "ssba_test_linear_timeout", "ssba_rope_axes", "ssba_get_status", "ssba_last_error", "ssba_timeline_read")
 
 
 class SsbaError(RuntimeError):
@@ -179,8 +179,9 @@ def load_library(path: str | None = None):
         lib.ssba_rms_norm_backward.argtypes = [P, P, P, P, P, I, I, I, P, P, P, ctypes.c_size_t, P]
         lib.ssba_linear.argtypes = [P] * 10
         lib.ssba_linear_backward.argtypes = [P] * 9 + [ctypes.c_size_t, P]
+        lib.ssba_test_linear_timeout.argtypes = [P, P, P, P, ctypes.c_uint64, P]
         lib.ssba_rope_axes.argtypes = [P, P, P, P, ctypes.c_int64, P, P, P]
-        for fn in ("rms_norm", "rms_norm_backward", "linear", "linear_backward", "rope_axes"):
+        for fn in ("rms_norm", "rms_norm_backward", "linear", "linear_backward", "test_linear_timeout", "rope_axes"):
             getattr(lib, "ssba_" + fn).restype = ctypes.c_int
         lib.ssba_rms_norm_backward_workspace_bytes.argtypes = [I, I, I]
         lib.ssba_rms_norm_backward_workspace_bytes.restype = ctypes.c_size_t

@@ -212,6 +212,8 @@ struct Product {
     int M, N, K;
     int act;
     bool f8, b_mn, gated;
+    uint64_t budget_ns = kWaitBudgetNs;  // of each wait
+    int withhold = 0;                    // the failure-detection test hook: CTA 0 announces its first copies and leaves them
 };
 
 // Rows as CTA pairs' 256-row tiles / weights as rows and tokens as columns, K split over a cluster.

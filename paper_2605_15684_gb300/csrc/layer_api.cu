@@ -116,6 +116,29 @@ int check_linear(const char* who, const ssba_linear_desc* d)
     return SSBA_OK;
 }
 
+// ssba_linear, and its test hook with a limit of its own and copies that never come.
+int linear(const char* who, const ssba_linear_desc* desc, const void* x, const void* W, const float* x_scale,
+           const float* w_scale, const float* bias, const void* r, void* y, void* z, void* stream, uint64_t budget_ns, int withhold)
+{
+    const int rc = check_linear(who, desc);
+    if (rc != SSBA_OK) return rc;
+    const bool f8 = desc->dtype == SSBA_E4M3;
+    if ((x_scale != nullptr) != f8 || (w_scale != nullptr) != f8)
+        return invalid(who, "x_scale and w_scale are given for e4m3 and for nothing else");
+    if (desc->gated && (bias || r)) return invalid(who, "a gated product has no bias and no residual");
+    if (desc->T == 0) return SSBA_OK;
+    if (!x || !W || !y) return invalid(who, "x, W and y must be non-null");
+    if (!aligned(x, 16) || !aligned(W, 16) || !aligned(w_scale, 16) || !aligned(bias, 16) || !aligned(r, 16) ||
+        !aligned(y, 16) || !aligned(z, 16) || !aligned(x_scale, 4))
+        return invalid(who, "x, W, w_scale, bias, r, y and z must be 16-byte aligned, x_scale 4-byte");
+    const size_t T = desc->T, N = desc->N, K = desc->K, rows = desc->gated ? 2 * N : N, e = f8 ? 1 : 2;
+    const Range X{x, T * K * e}, M{W, rows * K * e}, XS{x_scale, 4 * T}, WS{w_scale, 4 * rows}, B{bias, 4 * N}, R{r, T * N * 2}, Y{y, T * N * 2};
+    if (lies_on(Y, {X, M, XS, WS, B, unless_same(R, y)}) || lies_on(Range{z, T * rows * 2}, {X, M, XS, WS, B, R, Y}))
+        return invalid(who, "an output lies on another tensor of the call (y may be r)");
+    const Product p{x, W, y, z, r, x_scale, w_scale, bias, desc->T, desc->N, desc->K, desc->act, f8, false, desc->gated != 0, budget_ns, withhold};
+    return launch_product(p, who, static_cast<cudaStream_t>(stream));
+}
+
 }  // namespace
 }  // namespace layer
 }  // namespace ssba
@@ -188,25 +211,17 @@ int ssba_rms_norm_backward(const void* dy, const void* h, const float* w, const 
 int ssba_linear(const ssba_linear_desc* desc, const void* x, const void* W, const float* x_scale, const float* w_scale,
                 const float* bias, const void* r, void* y, void* z, void* stream)
 {
-    static const char who[] = "ssba_linear";
-    SSBA_NVTX_RANGE(who);
-    const int rc = check_linear(who, desc);
-    if (rc != SSBA_OK) return rc;
-    const bool f8 = desc->dtype == SSBA_E4M3;
-    if ((x_scale != nullptr) != f8 || (w_scale != nullptr) != f8)
-        return invalid(who, "x_scale and w_scale are given for e4m3 and for nothing else");
-    if (desc->gated && (bias || r)) return invalid(who, "a gated product has no bias and no residual");
-    if (desc->T == 0) return SSBA_OK;
-    if (!x || !W || !y) return invalid(who, "x, W and y must be non-null");
-    if (!aligned(x, 16) || !aligned(W, 16) || !aligned(w_scale, 16) || !aligned(bias, 16) || !aligned(r, 16) ||
-        !aligned(y, 16) || !aligned(z, 16) || !aligned(x_scale, 4))
-        return invalid(who, "x, W, w_scale, bias, r, y and z must be 16-byte aligned, x_scale 4-byte");
-    const size_t T = desc->T, N = desc->N, K = desc->K, rows = desc->gated ? 2 * N : N, e = f8 ? 1 : 2;
-    const Range X{x, T * K * e}, M{W, rows * K * e}, XS{x_scale, 4 * T}, WS{w_scale, 4 * rows}, B{bias, 4 * N}, R{r, T * N * 2}, Y{y, T * N * 2};
-    if (lies_on(Y, {X, M, XS, WS, B, unless_same(R, y)}) || lies_on(Range{z, T * rows * 2}, {X, M, XS, WS, B, R, Y}))
-        return invalid(who, "an output lies on another tensor of the call (y may be r)");
-    const Product p{x, W, y, z, r, x_scale, w_scale, bias, desc->T, desc->N, desc->K, desc->act, f8, false, desc->gated != 0};
-    return launch_product(p, who, static_cast<cudaStream_t>(stream));
+    SSBA_NVTX_RANGE("ssba_linear");
+    return linear("ssba_linear", desc, x, W, x_scale, w_scale, bias, r, y, z, stream, kWaitBudgetNs, 0);
+}
+
+int ssba_test_linear_timeout(const ssba_linear_desc* desc, const void* x, const void* W, void* y, uint64_t budget_ns,
+                             void* stream)
+{
+    SSBA_NVTX_RANGE("ssba_test_linear_timeout");
+    if (!desc || desc->T <= 0 || desc->dtype != SSBA_BF16) return invalid("ssba_test_linear_timeout", "needs bf16 and at least one row");
+    const uint64_t ns = budget_ns < 1000000ull ? 1000000ull : budget_ns > kWaitBudgetNs ? kWaitBudgetNs : budget_ns;
+    return linear("ssba_test_linear_timeout", desc, x, W, nullptr, nullptr, nullptr, nullptr, y, nullptr, stream, ns, 1);
 }
 
 size_t ssba_linear_backward_workspace_bytes(const ssba_linear_desc* desc)

@@ -85,6 +85,7 @@ struct PairParams {
     const float *xs, *ws, *bias;
     int* status;
     uint64_t budget_ns;
+    int withhold;
 };
 
 // The k-th tile of pair q: which set, the tile's row and column of tiles, and its steps of K. Within a set (and part of K),
@@ -277,6 +278,7 @@ __global__ void __launch_bounds__(PairCfg<kBN, kEpi, kZ>::kThreads, 1)
                     // the first CTA's barrier counts the copies of both
                     const uint32_t bar = at_rank(smem_u32(&sm.full[s]), 0);
                     if (rank == 0) mbar_arrive_expect_tx(smem_u32(&sm.full[s]), 2 * kStep);
+                    if (p.withhold && blockIdx.x == 0 && g == 0) continue;
                     const uint32_t a = smem_u32(&sm.a[s][0]), b = smem_u32(&sm.b[s][0]);
                     if (second) {
                         tma_load_pair(a, ma, bar, m0, k * kBK, 0);
@@ -564,7 +566,6 @@ int launch_pairs(PairMaps& maps, PairParams& p, const char* who, cudaStream_t st
     const size_t smem = sizeof(PairSmem<kBN, kEpi, kZ>) + 1024;
     static PerDeviceOnce attr;
     attr.run([=] { cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
-    p.budget_ns = kWaitBudgetNs;
     p.status = device_status_word();
     if (!p.status) {
         set_error("%s: could not resolve the device status word", who);
@@ -621,6 +622,8 @@ int launch_as(const Product& q, const char* who, cudaStream_t st)
     p.xs = q.xs;
     p.ws = q.ws;
     p.bias = q.bias;
+    p.budget_ns = q.budget_ns;
+    p.withhold = q.withhold;
     return launch_pairs<kBN, kF8, kEpi, kZ>(maps, p, who, st);
 }
 
@@ -745,6 +748,7 @@ int launch_gradients(const void* dz, const void* x, const void* W, void* dx, voi
     PairMaps maps;
     memset(&maps, 0, sizeof(maps));
     PairParams p = {};
+    p.budget_ns = kWaitBudgetNs;
     const uint64_t t = T, n = N, k = K;
     bool ok = true;
     if (dx) {

@@ -61,6 +61,7 @@ struct RowsParams {
     int ksteps, split, act;
     int* status;
     uint64_t budget_ns;
+    int withhold;
 };
 
 template <int kAct>
@@ -171,6 +172,7 @@ __global__ void __launch_bounds__(kThreads) ssba_product_rows_kernel(const __gri
                 }
                 const uint32_t bar = smem_u32(&sm.full[s]), a = smem_u32(&sm.a[s][0]);
                 mbar_arrive_expect_tx(bar, kABytes + C::kBBytes);
+                if (p.withhold && blockIdx.x == 0 && blockIdx.y == 0 && g == 0) continue;
                 if constexpr (kWmn) {
                     tma_load_3d(a, &maps.w, bar, n0, k * kBK, 0);
                     tma_load_3d(a + 8192, &maps.w, bar, n0 + 64, k * kBK, 0);
@@ -313,7 +315,8 @@ int launch_as(const Product& q, const char* who, cudaStream_t st)
     p.N = q.N;
     p.ksteps = (q.K + kBK - 1) / kBK;
     p.act = q.act;
-    p.budget_ns = kWaitBudgetNs;
+    p.budget_ns = q.budget_ns;
+    p.withhold = q.withhold;
     p.status = device_status_word();
     if (!p.status) {
         set_error("%s: could not resolve the device status word", who);

@@ -242,6 +242,19 @@ def gated_linear(x, W, act="silu", x_scale=None, w_scale=None, pre: bool = False
     return _product(x, W, None, None, act, x_scale, w_scale, pre, y, z, stream, 1)
 
 
+def test_linear_timeout(x, W, y, gated: bool = False, budget_ns: int = 2_000_000, stream=None) -> None:
+    """ssba_test_linear_timeout: the products' failure-detection test hook (include/ssba.h)."""
+    lib = load_library()
+    T, K = _matrix(x, "x", (torch.bfloat16,))
+    rows, _ = _matrix(W, "W", (torch.bfloat16,))
+    N = rows // 2 if gated else rows
+    _check(W, "W", (rows, K), torch.bfloat16)
+    _check(y, "y", (T, N), torch.bfloat16)
+    d = _LinearDesc(T, N, K, SSBA_BF16, _act("silu" if gated else None), int(gated))
+    _raise_on(lib.ssba_test_linear_timeout(ctypes.byref(d), x.data_ptr(), W.data_ptr(), y.data_ptr(), int(budget_ns),
+                                           _stream_ptr(stream)))
+
+
 def _linear_desc_of(T, N, K, act, gated):
     return _LinearDesc(_sized(T, "T"), _sized(N, "N"), _sized(K, "K"), SSBA_BF16, _act(act, gated), gated)
 

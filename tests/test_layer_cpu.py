@@ -175,3 +175,9 @@ def test_rope_refuses_an_output_on_its_input(lib, apart, xs, os):
     x = 0x100000000
     rc = lib.ssba_rope_axes(rope_desc(B=4, heads=3), x, S(*xs), 0x900000000, 0, x + 2 * apart, S(*os), None)
     assert rc == INV and b"lies on" in lib.ssba_last_error()
+
+
+def test_timeout_hook_refusals(lib):
+    for d in (dict(T=0), dict(dtype=2), dict(N=60)):
+        assert lib.ssba_test_linear_timeout(linear_desc(**d), FAKE, FAKE, FAKE, 1000000, None) in (INV, UNS)
+    assert lib.ssba_test_linear_timeout(None, FAKE, FAKE, FAKE, 1000000, None) == INV

@@ -537,3 +537,21 @@ def test_weights_gradient_of_many_tokens(T, K, N):
         ws = torch.zeros(gb.linear_backward_workspace_bytes(T, N, K, act), dtype=torch.uint8, device="cuda")
         gb.linear_backward(dy, x, W, z=zz, act=act, dW=into, workspace=ws)
         assert torch.equal(into, got[1])
+
+
+@pytest.mark.parametrize("T,K,N", [(5, 4096, 256), (40, 64, 136), (100, 512, 640), (2500, 336, 776), (9000, 512, 1536)])
+@pytest.mark.parametrize("is_gated", [False, True])
+def test_a_wait_that_runs_out(T, K, N, is_gated):
+    """Copies that never come: every kernel gives up, says so, and the next call is right."""
+    from paper_2605_15684_gb300 import layer
+    _, x, W, _, _ = operands(T, K, N, False, 4, 2 * N if is_gated else N)
+    call = gb.gated_linear if is_gated else gb.linear
+    want = call(x, W)
+    torch.cuda.synchronize()
+    assert api.get_status() == api.SSBA_OK
+    layer.test_linear_timeout(x, W, torch.empty_like(want), gated=is_gated, budget_ns=3_000_000)
+    torch.cuda.synchronize()
+    assert api.get_status() == api.SSBA_ERR_TIMEOUT
+    assert torch.equal(call(x, W), want)
+    torch.cuda.synchronize()
+    assert api.get_status() == api.SSBA_OK
