@@ -5,7 +5,8 @@
 //
 // Bound by HBM: z and dy are read once, 16 bytes a thread, and dz is written once, rounded to bf16 for the products. The
 // bias's gradient sums dz in fp32 before that rounding: a CTA takes 256 columns of a run of rows (a warp a
-// row, a lane 8 columns), its warps meet in shared memory, and the runs' sums in a second launch, in one order.
+// row, a lane 8 columns), its warps meet in shared memory, and the runs' sums (if more than one) in a second launch, in
+// one order.
 #include "layer.cuh"
 
 namespace ssba {
@@ -122,7 +123,8 @@ __global__ void __launch_bounds__(256) ssba_gated_bwd_kernel(const ActArgs p)
 
 int rows_of(int T, int N)
 {
-    // runs of rows, as many as run at once, of 32 rows at least
+    // runs of rows, as many as run at once, of 32 rows at least; up to 128 rows one, whose sums need no join
+    if (T <= 128) return T > 0 ? T : 1;
     const long long wide = (N + kCols - 1) / kCols, most = (long long)kCtas * device_sm_count();
     long long runs = most / wide;
     if (runs < 1) runs = 1;
@@ -144,7 +146,8 @@ int act_backward_parts(int T, int N) { return (T + rows_of(T, N) - 1) / rows_of(
 int launch_act_backward(const void* dy, const void* z, void* dz, float* db, float* part, int T, int N, int act, bool gated,
                         const char* who, cudaStream_t st)
 {
-    const ActArgs p{static_cast<const uint4*>(dy), static_cast<const uint4*>(z), static_cast<uint4*>(dz), part, T, N, rows_of(T, N), act};
+    const int parts = act_backward_parts(T, N);
+    const ActArgs p{static_cast<const uint4*>(dy), static_cast<const uint4*>(z), static_cast<uint4*>(dz), parts == 1 ? db : part, T, N, rows_of(T, N), act};
     if (gated) {
         const long long ctas = ((long long)T * (N / 8) + 255) / 256, most = 32ll * device_sm_count();
         const dim3 grid((unsigned)(ctas < most ? ctas : most));
@@ -152,7 +155,6 @@ int launch_act_backward(const void* dy, const void* z, void* dz, float* db, floa
         if (act == SSBA_ACT_SILU) return go(ssba_gated_bwd_kernel<SSBA_ACT_SILU>);
         return act == SSBA_ACT_GELU ? go(ssba_gated_bwd_kernel<SSBA_ACT_GELU>) : go(ssba_gated_bwd_kernel<SSBA_ACT_RELU>);
     }
-    const int parts = act_backward_parts(T, N);
     const dim3 grid((N + kCols - 1) / kCols, parts);
     auto go = [&](auto k) { return launched(launch_early(k, grid, kWarps * 32, 0, st, 1, p), who); };
     int rc;
@@ -164,7 +166,7 @@ int launch_act_backward(const void* dy, const void* z, void* dz, float* db, floa
         rc = db ? go(ssba_act_bwd_kernel<SSBA_ACT_GELU, true>) : go(ssba_act_bwd_kernel<SSBA_ACT_GELU, false>);
     else
         rc = db ? go(ssba_act_bwd_kernel<SSBA_ACT_SILU, true>) : go(ssba_act_bwd_kernel<SSBA_ACT_SILU, false>);
-    return rc == SSBA_OK && db ? launch_column_sum(part, parts, N, db, who, st) : rc;
+    return rc == SSBA_OK && db && parts > 1 ? launch_column_sum(part, parts, N, db, who, st) : rc;
 }
 
 }  // namespace layer

@@ -453,15 +453,16 @@ int rms_norm_backward_parts(int T, int D, int dtype) { return bwd_ctas(T, D, dty
 int launch_rms_norm_backward(const void* dy, const void* h, const float* w, const float* rstd, const void* dh, int T, int D,
                              int dtype, void* dx, float* dw, float* part, cudaStream_t st)
 {
-    const NormBwdArgs p{static_cast<const uint4*>(dy), static_cast<const uint4*>(h), static_cast<const uint4*>(dh), w, rstd,
-                        static_cast<uint4*>(dx), part, T, D};
     const int ctas = bwd_ctas(T, D, dtype);
+    const bool one = ctas == 1 && reinterpret_cast<uintptr_t>(dw) % 16 == 0;  // its sums are dw
+    const NormBwdArgs p{static_cast<const uint4*>(dy), static_cast<const uint4*>(h), static_cast<const uint4*>(dh), w, rstd,
+                        static_cast<uint4*>(dx), one ? dw : part, T, D};
     auto go = [&](auto t) {
         using E = decltype(t);
         return dh ? norm_bwd_as<E, true>(p, ctas, st) : norm_bwd_as<E, false>(p, ctas, st);
     };
     const int rc = dtype == SSBA_BF16 ? go(__nv_bfloat16()) : go(float());
-    return rc == SSBA_OK ? launch_column_sum(part, ctas, D, dw, "ssba_rms_norm_backward", st) : rc;
+    return rc == SSBA_OK && !one ? launch_column_sum(part, ctas, D, dw, "ssba_rms_norm_backward", st) : rc;
 }
 
 }  // namespace layer

@@ -555,3 +555,17 @@ def test_a_wait_that_runs_out(T, K, N, is_gated):
     assert torch.equal(call(x, W), want)
     torch.cuda.synchronize()
     assert api.get_status() == api.SSBA_OK
+
+
+def test_sums_at_odd_addresses():
+    """dw and db that are 4-byte aligned only, of few rows (whose sums are written without a join) and of many."""
+    for T in (3, 100, 700):
+        randn, x, W, _, _ = operands(T, 64, 72, False, T)
+        dy, z, w = randn(T, 72).to(BF), randn(T, 72).to(BF), 1 + randn(64, std=0.1)
+        _, _, rstd = gb.rms_norm(x, w)
+        dx, dw = gb.rms_norm_backward(x, x, w, rstd)
+        db = gb.linear_backward(dy, x, W, z=z, act="gelu", bias=True)[2]
+        odd = torch.zeros(138, device="cuda")
+        gb.rms_norm_backward(x, x, w, rstd, dw=odd[1:65])
+        gb.linear_backward(dy, x, W, z=z, act="gelu", db=odd[65:137])
+        assert torch.equal(odd[1:65], dw) and torch.equal(odd[65:137], db) and not odd[0] and not odd[137]
