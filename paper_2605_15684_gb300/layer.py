@@ -231,7 +231,8 @@ def _product(x, W, bias, residual, act, x_scale, w_scale, pre, y, z, stream, gat
 def linear(x, W, bias=None, residual=None, act=None, x_scale=None, w_scale=None, pre: bool = False, y=None, z=None,
            stream=None):
     """ssba_linear: y = act(z) + residual with z = x W^T (x_scale w_scale) + bias; x [T, K], W [N, K] bf16, or both e4m3
-    with fp32 scales [T] and [N]; bias [N] fp32, residual [T, N] bf16 (may be ``y``); act None, "relu", "gelu" or "silu".
+    with fp32 scales [T] and [N] (rms_norm makes such rows; of weights once: s = 2 ** ceil(log2(max |W_n| / 448)), W / s
+    rounded); bias [N] fp32, residual [T, N] bf16 (may be ``y``); act None, "relu", "gelu" or "silu".
     Returns y [T, N] bf16, or with ``pre`` (y, z): z is what linear_backward needs of an activation."""
     return _product(x, W, bias, residual, act, x_scale, w_scale, pre, y, z, stream, 0)
 
