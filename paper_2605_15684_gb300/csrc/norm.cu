@@ -255,14 +255,21 @@ struct NormBwdArgs {
     int T, D;
 };
 
-constexpr int kBwdWarps = 8;  // warps of a CTA whose warps take a row each
+constexpr int kBwdWarps = 4;  // warps of a CTA whose warps take a row each
+
+// CTAs of an SM, all of which run at once: 12 warps of 48 columns a lane (up to 168 registers with what is under way), more of fewer, or 1024
+// threads of 16 columns (64 registers).
+constexpr int bwd_ctas_of(int tpr, int steps)
+{
+    return tpr == 32 ? (steps == 1 ? 8 : steps == 2 ? 6 : steps == 4 ? 4 : 3) : 1024 / tpr;
+}
 
 template <class T, int kTPR, int kNV, bool kDh>
-__global__ void __launch_bounds__(kTPR == 32 ? kBwdWarps * 32 : kTPR) ssba_rms_norm_bwd_kernel(const NormBwdArgs p)
+__global__ void __launch_bounds__(kTPR == 32 ? kBwdWarps * 32 : kTPR, bwd_ctas_of(kTPR, kNV)) ssba_rms_norm_bwd_kernel(const NormBwdArgs p)
 {
     constexpr int n = Vec<T>::n, kRows = kTPR == 32 ? kBwdWarps : 1;
     __shared__ float4 area[2][32];
-    extern __shared__ float cols[];  // [D], where a CTA's warps add up
+    extern __shared__ float cols[];  // [warps][D], where a CTA's warps add up
     const int nv = p.D / n, tid = threadIdx.x % kTPR;
     float dw[kNV][n] = {};
     grid_dep_wait();
@@ -318,21 +325,21 @@ __global__ void __launch_bounds__(kTPR == 32 ? kBwdWarps * 32 : kTPR) ssba_rms_n
     float* out = p.part + (size_t)blockIdx.x * p.D;
     if constexpr (kTPR == 32) {
         // the warps' sums, in the order of the warps
-        for (int k = 0; k < kBwdWarps; ++k) {
-            if ((int)(threadIdx.x >> 5) == k) {
+        float* mine = cols + (threadIdx.x >> 5) * p.D;
 #pragma unroll
-                for (int j = 0; j < kNV; ++j) {
-                    const int i = tid + j * kTPR;
-                    if (i >= nv) continue;
+        for (int j = 0; j < kNV; ++j) {
+            const int i = tid + j * kTPR;
+            if (i >= nv) continue;
 #pragma unroll
-                    for (int e = 0; e < n; ++e) {
-                        const float v = k ? cols[i * n + e] + dw[j][e] : dw[j][e];
-                        cols[i * n + e] = v;
-                        if (k == kBwdWarps - 1) out[i * n + e] = v;
-                    }
-                }
-            }
-            __syncthreads();
+            for (int e = 0; e < n; e += 4)
+                *reinterpret_cast<float4*>(mine + i * n + e) = make_float4(dw[j][e], dw[j][e + 1], dw[j][e + 2], dw[j][e + 3]);
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < p.D; c += kBwdWarps * 32) {
+            float v = cols[c];
+#pragma unroll
+            for (int k = 1; k < kBwdWarps; ++k) v += cols[k * p.D + c];
+            out[c] = v;
         }
     } else {
 #pragma unroll
@@ -407,23 +414,47 @@ int norm_as(const NormArgs& p, cudaStream_t st)
     });
 }
 
-// CTAs of the backward pass: as many as run at once, each with rows enough to make its column sums worth writing.
-int bwd_ctas(int T, int D, int dtype)
+// The backward pass: threads a row and steps a thread. Its registers hold dw of the columns as well, so long rows take more
+// threads of two steps (one wave of CTAs; in two, with four steps, 4096 rows of 8192 took 51 us).
+template <class T, class F>
+int by_width_bwd(int nv, F&& f)
 {
-    const int nv = D / (dtype == SSBA_BF16 ? 8 : 4);
-    const bool warps = nv <= 192;
-    const int rows = warps ? kBwdWarps : 1;
-    const long long need = ((long long)T + rows - 1) / rows, most = (long long)device_sm_count() * (warps ? 3 : nv <= 256 ? 8 : nv <= 1024 ? 4 : 2);
-    return (int)(need < most ? need : most);
+    using std::integral_constant;
+#define SSBA_ROW(tpr, steps) return f(integral_constant<int, tpr>(), integral_constant<int, steps>())
+    if (nv <= 32) SSBA_ROW(32, 1);
+    if (nv <= 64) SSBA_ROW(32, 2);
+    if (nv <= 128) SSBA_ROW(32, 4);
+    if (nv <= 192) SSBA_ROW(32, 6);
+    if (nv <= 256) SSBA_ROW(128, 2);
+    if (nv <= 512) SSBA_ROW(256, 2);
+    if (nv <= 1024) SSBA_ROW(512, 2);
+    if constexpr (sizeof(T) == 4) {
+        if (nv > 2048) SSBA_ROW(1024, 4);
+    }
+    SSBA_ROW(1024, 2);
+#undef SSBA_ROW
 }
+
+// CTAs of the backward pass: as many as run at once.
+template <class T>
+int bwd_ctas_as(int rows, int D)
+{
+    return by_width_bwd<T>(D / Vec<T>::n, [&](auto tpr, auto steps) {
+        constexpr int kTPR = decltype(tpr)::value, kRows = kTPR == 32 ? kBwdWarps : 1;
+        const long long need = ((long long)rows + kRows - 1) / kRows, most = (long long)device_sm_count() * bwd_ctas_of(kTPR, decltype(steps)::value);
+        return (int)(need < most ? need : most);
+    });
+}
+
+int bwd_ctas(int T, int D, int dtype) { return dtype == SSBA_BF16 ? bwd_ctas_as<__nv_bfloat16>(T, D) : bwd_ctas_as<float>(T, D); }
 
 template <class T, bool kDh>
 int norm_bwd_as(const NormBwdArgs& p, int ctas, cudaStream_t st)
 {
-    return by_width<T>(p.D / Vec<T>::n, [&](auto tpr, auto steps) {
+    return by_width_bwd<T>(p.D / Vec<T>::n, [&](auto tpr, auto steps) {
         constexpr int kTPR = decltype(tpr)::value;
         return launched(launch_early(ssba_rms_norm_bwd_kernel<T, kTPR, decltype(steps)::value, kDh>, dim3(ctas),
-                                     kTPR == 32 ? kBwdWarps * 32 : kTPR, kTPR == 32 ? sizeof(float) * p.D : 0, st, 1, p),
+                                     kTPR == 32 ? kBwdWarps * 32 : kTPR, kTPR == 32 ? sizeof(float) * kBwdWarps * p.D : 0, st, 1, p),
                         "ssba_rms_norm_bwd_kernel");
     });
 }
