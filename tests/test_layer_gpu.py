@@ -569,3 +569,20 @@ def test_sums_at_odd_addresses():
         gb.rms_norm_backward(x, x, w, rstd, dw=odd[1:65])
         gb.linear_backward(dy, x, W, z=z, act="gelu", db=odd[65:137])
         assert torch.equal(odd[1:65], dw) and torch.equal(odd[65:137], db) and not odd[0] and not odd[137]
+
+
+def test_norm_of_tiny_rows_without_eps():
+    """eps 0 and rows of 1e-15 (rstd 1e15) and of 1e15: the gradient neither overflows nor vanishes on the way."""
+    randn = rng(8)
+    h = randn(6, 264) * torch.tensor([1e-15, 1e15, 1.0, 1e-12, 1e10, 3.0], device="cuda")[:, None]
+    w, dy = 1 + randn(264, std=0.1), randn(6, 264)
+    for dt in (BF, F32):
+        hh, dd = h.to(dt), dy.to(dt)
+        y, _, rstd = gb.rms_norm(hh, w, eps=0.0)
+        yr, k = ref.norm(hh, w, 0.0)
+        near(y, yr, yr.abs() * (ref.half_step(dt) + 2.0 ** -14))
+        dx, dw = gb.rms_norm_backward(dd, hh, w, rstd)
+        want, wdw = ref.norm_backward(dd, hh, w, k, None)
+        size = (dd.double() * w.double()).abs().amax(1, keepdim=True) * k[:, None]
+        near(dx, want, want.abs() * ref.half_step(dt) + size * 2.0 ** -14, "dx")
+        near(dw, wdw, (dd.double().abs() * (hh.double() * k[:, None]).abs()).sum(0) * 2.0 ** -14, "dw")
