@@ -586,3 +586,29 @@ def test_norm_of_tiny_rows_without_eps():
         size = (dd.double() * w.double()).abs().amax(1, keepdim=True) * k[:, None]
         near(dx, want, want.abs() * ref.half_step(dt) + size * 2.0 ** -14, "dx")
         near(dw, wdw, (dd.double().abs() * (hh.double() * k[:, None]).abs()).sum(0) * 2.0 ** -14, "dw")
+
+
+def test_two_streams_at_once():
+    """Products of both kernels on one stream while rows of many waves of CTAs, and other products, run on another."""
+    randn, x, W, _, _ = operands(3000, 512, 1024, False, 9, 2048)
+    dy, z, w = randn(3000, 1024).to(BF), randn(3000, 2048).to(BF), torch.ones(512, device="cuda")
+    rows = randn(60000, 512).to(BF)
+    few = x[:9].contiguous()
+
+    def a():
+        return [*gb.gated_linear_backward(dy, x, W, z), gb.linear(x, W), gb.gated_linear(few, W)]
+
+    def b():
+        return [gb.rms_norm(rows, w)[0], gb.linear(few, W), gb.linear(rows, W[:256].contiguous()), gb.gated_linear(x, W)]
+
+    want_a, want_b = a(), b()
+    torch.cuda.synchronize()
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(30):
+        with torch.cuda.stream(s):
+            got_a = a()
+        with torch.cuda.stream(t):
+            got_b = b()
+    torch.cuda.synchronize()
+    for got, want in zip(got_a + got_b, want_a + want_b):
+        assert torch.equal(got, want)
