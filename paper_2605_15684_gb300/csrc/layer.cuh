@@ -223,7 +223,6 @@ int launch_product(const Product& p, const char* who, cudaStream_t st);
 // What either is expected to take, in microseconds.
 double product_pair_us(long long M, long long N, long long K, bool f8, bool gated);
 double product_rows_us(long long M, long long N, long long K, bool f8, bool gated);
-bool product_rows_fit(long long M);
 // dx = dz W and dW = dz^T x; either may be null. parts: gradients_workspace_bytes (only dW needs them).
 size_t gradients_workspace_bytes(int T, int N, int K);
 int launch_gradients(const void* dz, const void* x, const void* W, void* dx, void* dW, float* parts, int T, int N, int K,

@@ -679,13 +679,12 @@ GradientPlan gradient_plan(int T, int N, int K)
 {
     const int most = device_sm_count() / 2 > 0 ? device_sm_count() / 2 : 1;
     const Tiles of_dx = tiles_of(T, K, N, 256, 64), of_dW = tiles_of(N, K, T, 256, 64);
-    const bool fit = product_rows_fit(T);
-    const double rows_us = fit ? product_rows_us(T, K, N, false, false) : 0.;
+    const double rows_us = product_rows_us(T, K, N, false, false);
     GradientPlan best = {T <= 64, 1};
     double best_us = -1.;
     for (int parts = 1; parts <= kMaxParts; parts *= 2) {
         if (parts > 1 && (of_dW.ksteps < 8 * parts || (long long)of_dW.tiles * parts > 2 * most)) break;
-        for (int rows = T <= 64 ? 1 : 0; rows < (fit ? 2 : 1); ++rows) {
+        for (int rows = T <= 64 ? 1 : 0; rows < 2; ++rows) {
             PairParams p = {};
             if (!rows) p.set[0] = of_dx;
             p.set[1] = of_dW;

@@ -351,30 +351,39 @@ int launch_few(const Product& q, const char* who, cudaStream_t st)
 
 }  // namespace
 
+namespace {
+
+// Microseconds of a call of more than 64 tokens: a start and an end (the join of the parts among them), and a step of K, with
+// two CTAs an SM. 64 tokens a tile cost less of either and have twice the tiles, which read the weights from L2 the
+// second time: 128 tokens, 4096 x 4096 11.8 us (16 steps) against 13.8 (8); 256, 1536 x 1536 7.7 against 10.4; but 128, gated
+// 4096 x 4096 19.6 (32) against 17.9 (16). Within a fifth of 7 to 32 us measured of 100 to 1024 tokens.
+double rows_us(int nt, long long M, long long N, long long K, bool f8, bool gated)
+{
+    const long long cols = (M + nt - 1) / nt, tiles = ((N + (gated ? 63 : 127)) / (gated ? 64 : 128)) * cols, slots = 2ll * device_sm_count();
+    if (cols > 65535) return 1e30;  // tiles of tokens are the grid's y
+    const int ksteps = (int)((K + (f8 ? 127 : 63)) / (f8 ? 128 : 64)), split = split_of(tiles, ksteps, 2);
+    return (nt == 64 ? 6.4 : 8.4) + (nt == 64 ? 0.30 : 0.37) * ((ksteps + split - 1) / split) * ((tiles * split + slots - 1) / slots);
+}
+
+}  // namespace
+
+double product_rows_us(long long M, long long N, long long K, bool f8, bool gated)
+{
+    return std::min(rows_us(64, M, N, K, f8, gated), rows_us(128, M, N, K, f8, gated));
+}
+
 int launch_product_rows(const Product& q, const char* who, cudaStream_t st)
 {
     if (q.M <= 16) return launch_few<16>(q, who, st);
     if (q.M <= 32) return launch_few<32>(q, who, st);
-    if (q.M <= 64) return launch_tokens<64, false>(q, who, st);
-    return launch_tokens<128, false>(q, who, st);
+    const bool narrow = q.M <= 64 || rows_us(64, q.M, q.N, q.K, q.f8, q.gated) <= rows_us(128, q.M, q.N, q.K, q.f8, q.gated);
+    return narrow ? launch_tokens<64, false>(q, who, st) : launch_tokens<128, false>(q, who, st);
 }
-
-// Microseconds of a call with weights as rows and 128 tokens a tile: a start and an end of 8.4 in all (the join of the parts
-// among them), 0.37 a step of K. Within a tenth of 7.6 to 32 us measured of 100 to 1024 tokens, K 1536 to 6144, N 512 to 6144.
-double product_rows_us(long long M, long long N, long long K, bool f8, bool gated)
-{
-    const long long tiles = ((N + (gated ? 63 : 127)) / (gated ? 64 : 128)) * ((M + 127) / 128), slots = 2ll * device_sm_count();
-    const int ksteps = (int)((K + (f8 ? 127 : 63)) / (f8 ? 128 : 64)), split = split_of(tiles, ksteps, 2);
-    return 8.4 + 0.37 * ((ksteps + split - 1) / split) * ((tiles * split + slots - 1) / slots);
-}
-
-bool product_rows_fit(long long M) { return (M + 127) / 128 <= 65535; }  // tiles of tokens are the grid's y
 
 int launch_product(const Product& q, const char* who, cudaStream_t st)
 {
     // Up to 64 tokens the weights are the rows; above, whichever is expected to end first.
-    const bool rows = q.M <= 64 || (product_rows_fit(q.M) && product_rows_us(q.M, q.N, q.K, q.f8, q.gated) <
-                                                                product_pair_us(q.M, q.N, q.K, q.f8, q.gated));
+    const bool rows = q.M <= 64 || product_rows_us(q.M, q.N, q.K, q.f8, q.gated) < product_pair_us(q.M, q.N, q.K, q.f8, q.gated);
     return rows ? launch_product_rows(q, who, st) : launch_product_pair(q, who, st);
 }
 
