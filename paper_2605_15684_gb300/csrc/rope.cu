@@ -75,6 +75,17 @@ struct Pack {
     }
 };
 
+// w with its 32-bit words from `first` on as they are in x
+template <class W>
+__device__ __forceinline__ W kept(W w, const W& x, int first)
+{
+    uint32_t* to = reinterpret_cast<uint32_t*>(&w);
+    const uint32_t* from = reinterpret_cast<const uint32_t*>(&x);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(W) / 4; ++i) to[i] = i >= first ? from[i] : to[i];
+    return w;
+}
+
 // (u, v) turned, with the same roundings in every instantiation: widths and layouts give the same bits.
 __device__ __forceinline__ void turn(float u, float v, float c, float s, float& a, float& b)
 {
@@ -109,11 +120,14 @@ __global__ void __launch_bounds__(256) ssba_rope_kernel(const __grid_constant__ 
     const char* x = p.x + b * p.xs[0] + t * p.xs[1] + h0 * p.xs[2];
     char* o = p.out + b * p.os[0] + t * p.os[1] + h0 * p.os[2];
     const int at = unit * kN * (int)sizeof(E), half = p.P * (int)sizeof(E);
-    if (unit >= p.turned) {  // dimensions that stay (halves only: adjacent pairs past P turn by nothing)
+    if (unit >= p.turned) {  // dimensions that stay (halves only)
         const int stay = (2 * p.P + (unit - p.turned) * kN) * (int)sizeof(E);
         for (int h = h0; h < h1; ++h, x += p.xs[2], o += p.os[2]) *reinterpret_cast<W*>(o + stay) = *reinterpret_cast<const W*>(x + stay);
         return;
     }
+    // Adjacent pairs: of a unit's 32-bit words, the first that stays. The bits that were read are written there (a turn by nothing would
+    // spread an infinity or a NaN over its pair); a loop of its own, without the batches below, took half as long again.
+    const int first = (2 * p.P - unit * kN) * (int)sizeof(E) / 4;
     // a batch of heads is loaded at once, the first before the sines are formed
     W u[kBatch], v[kHalves ? kBatch : 1];
     auto load = [&](int left) {
@@ -156,7 +170,9 @@ __global__ void __launch_bounds__(256) ssba_rope_kernel(const __grid_constant__ 
 #pragma unroll
                 for (int i = 0; i < kPairs; ++i) turn(f[2 * i], f[2 * i + 1], c[i], s[i], a[2 * i], a[2 * i + 1]);
             }
-            *reinterpret_cast<W*>(to) = Pack<E, kN>::put(a);
+            W w = Pack<E, kN>::put(a);
+            if constexpr (!kHalves) w = kept(w, u[k], first);
+            *reinterpret_cast<W*>(to) = w;
         }
         h += kBatch;
         if (h >= h1) return;
