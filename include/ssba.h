@@ -511,8 +511,8 @@ SSBA_API int ssba_cache_copy(const ssba_cache_desc* desc, const ssba_cache* cach
  *   w           device, fp32 [D].
  *   h           device out, [T][D] of dtype; NULL exactly where r is. It may be x or r.
  *   y           device out: [T][D] of dtype, or e4m3 [T][D] where scale is given: then scale[t] becomes the least power
- *               of two (at least 2^-126; 1 for a row of zeros) under which no finite value of the row passes 448, and
- *               y holds e4m3(y / scale), rounded to nearest. y of dtype may be x.
+ *               of two (at least 2^-126; 1 where no h_i w_i is finite and, in fp32, other than 0) under which no finite y of the row
+ *               passes 448, and y holds e4m3(y / scale), rounded to nearest. y of dtype may be x.
  *   scale       device out, fp32 [T], or NULL.
  *   rstd        device out, fp32 [T] (for the backward pass).
  * D a multiple of 8, at most SSBA_NORM_MAX_WIDTH; eps finite and >= 0. */

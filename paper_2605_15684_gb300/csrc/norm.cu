@@ -8,7 +8,8 @@
 // y is the norm of the rounded h, which is what the backward pass reads. Both kernels are bound by HBM: every tensor
 // passes once, a row stays in registers (as the packed bits that were read) between its sum and its output. A row is
 // one warp's or one CTA's, 16 bytes a thread and step; the 8-bit rows' maximum of |h w| goes through the same
-// reduction as the sum of squares (max |y| = rstd max |h w|, so one barrier serves both).
+// reduction as the sum of squares (max |y| = rstd max |h w|, so one barrier serves both). In fp32 that product is off by three
+// roundings: where it lies next to a power of two times 448, the row is taken again, by the largest y as it is rounded.
 // Under the 8-bit rows, y is the fp32 number nearest to the exact product: the sum of squares, rstd and the products carry
 // their rounding errors along in a second fp32 (the pass is bound by HBM; the extra eight instructions a value are
 // free). A plain fp32 product puts one value in a million on the other side of a tie, and so off by an eighth.
@@ -71,19 +72,25 @@ __device__ __forceinline__ void load_w(const float* w, float* f)
     }
 }
 
-// A sum and the error of its roundings.
+// A sum and the error of its roundings. a.add(b) and b.add(a) are one to the bit: the error of hi + x is exact in either order.
 struct Sum {
     float hi, lo;
     __device__ __forceinline__ void add(float x, float err)
     {
         const float t = hi + x, z = t - hi;
-        lo += ((hi - (t - z)) + (x - z)) + err;
+        lo = ((hi - (t - z)) + (x - z)) + (lo + err);
         hi = t;
+    }
+    __device__ __forceinline__ void add_square(float x, bool bf16)
+    {
+        const float q = x * x;  // exact for bf16
+        add(q, bf16 ? 0.f : fmaf(x, x, -q));
     }
 };
 
 // The sum of s and the maximum of m over the row's kTPR threads (a warp, or the whole CTA; `at` alternates between two
-// halves of the exchange area, so that one barrier a row is enough). kExact: with the sums' errors.
+// halves of the exchange area, so that one barrier a row is enough). kExact: with the sums' errors. All of the row's threads
+// end with the same bits, since each step adds the same two numbers in either lane.
 template <int kTPR, bool kMax, bool kExact>
 __device__ __forceinline__ void row_reduce(Sum& s, float& m, float4 (*area)[32], int at)
 {
@@ -132,7 +139,16 @@ __device__ __forceinline__ float product(float f, const Sum& k, float w)
     return y + fmaf(pe, w, fmaf(p, w, -y));
 }
 
-// The least power of two s with a / s <= 448 = 1.75 * 2^8 (at least 2^-126; 1 for a row of zeros), and its reciprocal.
+// Whether the scale that a row's largest |y| asks for is not certain from a = max |h w| rstd in fp32, which is off by three
+// roundings: a within eight units of the last place of a border (448 times a power of two), or a or m = max |h w| where fp32
+// has lost bits, or all of them (below 2^-100; NaN and infinities). A row of zeros, m = 0, is certain.
+__device__ __forceinline__ bool scale_is_open(float a, float m)
+{
+    const uint32_t bits = __float_as_uint(a), least = (127u - 100u) << 23;
+    return (((bits - (0x600000u - 8u)) & 0x7fffffu) <= 16u || bits - least >= 0x7f800000u - least || m < 0x1p-100f) && bits != 0;
+}
+
+// The least power of two s with a / s <= 448 = 1.75 * 2^8 (at least 2^-126; 1 for a = 0), and its reciprocal.
 __device__ __forceinline__ float row_scale(float a, float& inverse)
 {
     const uint32_t bits = __float_as_uint(a);
@@ -148,6 +164,16 @@ __device__ __forceinline__ uint32_t pack_e4m3(const float* f)
     const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[0], f[1]), __NV_SATFINITE, __NV_E4M3);
     const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[2], f[3]), __NV_SATFINITE, __NV_E4M3);
     return lo | (hi << 16);
+}
+
+// Eight-bit values of n of y: 8 or 4 bytes.
+template <int n>
+__device__ __forceinline__ void put_e4m3(uint8_t* q, long long i, const float* f)
+{
+    if constexpr (n == 8)
+        reinterpret_cast<uint2*>(q)[i] = make_uint2(pack_e4m3(f), pack_e4m3(f + 4));
+    else
+        reinterpret_cast<uint32_t*>(q)[i] = pack_e4m3(f);
 }
 
 struct NormArgs {
@@ -171,6 +197,7 @@ __global__ void __launch_bounds__(kTPR == 32 ? kWarpCta : kTPR) ssba_rms_norm_ke
     grid_dep_wait();
     grid_dep_launch();
     int at = 0;
+    bool again = false;
     for (long long t = (long long)blockIdx.x * kRows + threadIdx.x / kTPR; t < p.T; t += (long long)gridDim.x * kRows, at ^= 1) {
         uint4 v[kNV], u[kRes ? kNV : 1];
 #pragma unroll
@@ -197,12 +224,10 @@ __global__ void __launch_bounds__(kTPR == 32 ? kWarpCta : kTPR) ssba_rms_norm_ke
             }
 #pragma unroll
             for (int e = 0; e < n; ++e) {
-                if (kF8) {
-                    const float q = f[e] * f[e];  // exact for bf16
-                    s.add(q, n == 8 ? 0.f : fmaf(f[e], f[e], -q));
-                } else {
+                if (kF8)
+                    s.add_square(f[e], n == 8);
+                else
                     s.hi = fmaf(f[e], f[e], s.hi);
-                }
             }
             if (kF8 && i < nv) {
                 float w[n];
@@ -219,8 +244,10 @@ __global__ void __launch_bounds__(kTPR == 32 ? kWarpCta : kTPR) ssba_rms_norm_ke
             rstd.hi = 1.f / sqrtf(s.hi / (float)p.D + p.eps);
         float inverse = 1.f;
         if (kF8) {
-            const float scale = row_scale(m * rstd.hi, inverse);
-            if (tid == 0) p.scale[t] = scale;
+            const float a = m * rstd.hi, scale = row_scale(a, inverse);
+            const bool open = scale_is_open(a, m);
+            if (tid == 0) p.scale[t] = open ? 0.f : scale;
+            again = again || open;
         }
         if (tid == 0) p.rstd[t] = rstd.hi;
 #pragma unroll
@@ -232,16 +259,57 @@ __global__ void __launch_bounds__(kTPR == 32 ? kWarpCta : kTPR) ssba_rms_norm_ke
             load_w<n>(p.w + (size_t)i * n, w);
 #pragma unroll
             for (int e = 0; e < n; ++e) f[e] = kF8 ? product(f[e], rstd, w[e]) * inverse : f[e] * rstd.hi * w[e];
-            if (kF8) {
-                uint32_t b[n / 4];
-#pragma unroll
-                for (int e = 0; e < n; e += 4) b[e / 4] = pack_e4m3(f + e);
-                if constexpr (n == 8)
-                    reinterpret_cast<uint2*>(p.q)[t * nv + i] = make_uint2(b[0], b[1]);
-                else
-                    reinterpret_cast<uint32_t*>(p.q)[t * nv + i] = b[0];
-            } else {
+            if (kF8)
+                put_e4m3<n>(p.q, t * nv + i, f);
+            else
                 p.y[t * nv + i] = Vec<T>::put(f);
+        }
+    }
+    if constexpr (kF8) {
+        const bool mine = kTPR == 32 ? __any_sync(0xffffffffu, again) : __syncthreads_or(again);
+        if (!mine) return;
+        __syncwarp();
+        // The rows left open, behind the loop (in it they took 4 % of the others' time): the scale of the largest finite y as it is
+        // rounded, and the row's values. A thread reads the h that it wrote, and where all read scale[t] a barrier of
+        // the sum's lies in front of its writing.
+#pragma unroll 1
+        for (long long t = (long long)blockIdx.x * kRows + threadIdx.x / kTPR; t < p.T; t += (long long)gridDim.x * kRows) {
+            if (p.scale[t] != 0.f) continue;
+            const uint4* row = (kRes ? p.h : p.x) + t * nv;
+            float f[n], w[n], a = 0.f;
+            Sum s{0.f, 0.f};
+#pragma unroll 1
+            for (int i = tid; i < nv; i += kTPR) {
+                Vec<T>::get(row[i], f);
+#pragma unroll
+                for (int e = 0; e < n; ++e) s.add_square(f[e], n == 8);
+            }
+            row_reduce<kTPR, false, true>(s, a, area, at);
+            at ^= 1;
+            const Sum rstd = exact_rstd(s, (float)p.D, p.eps);
+#pragma unroll 1
+            for (int i = tid; i < nv; i += kTPR) {
+                Vec<T>::get(row[i], f);
+                load_w<n>(p.w + (size_t)i * n, w);
+#pragma unroll
+                for (int e = 0; e < n; ++e) {
+                    const float y = fabsf(product(f[e], rstd, w[e]));
+                    a = fmaxf(a, y < __int_as_float(0x7f800000) ? y : 0.f);
+                }
+            }
+            Sum none{0.f, 0.f};
+            row_reduce<kTPR, true, false>(none, a, area, at);
+            at ^= 1;
+            float inverse;
+            const float scale = row_scale(a, inverse);
+            if (tid == 0) p.scale[t] = scale;
+#pragma unroll 1
+            for (int i = tid; i < nv; i += kTPR) {
+                Vec<T>::get(row[i], f);
+                load_w<n>(p.w + (size_t)i * n, w);
+#pragma unroll
+                for (int e = 0; e < n; ++e) f[e] = product(f[e], rstd, w[e]) * inverse;
+                put_e4m3<n>(p.q, t * nv + i, f);
             }
         }
     }

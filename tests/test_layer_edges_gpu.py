@@ -4,9 +4,10 @@ import torch
 
 import paper_2605_15684_gb300 as gb
 from paper_2605_15684_gb300 import api, build
+from tests import layer_ref as ref
 
 pytestmark = pytest.mark.gpu
-BF, F32 = torch.bfloat16, torch.float32
+BF, F32, E4M3 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -49,3 +50,93 @@ def test_rope_copies_the_dimensions_behind_its_pairs(D, axes, layout, dt):
         y = gb.rope_axes(src, pos, axes, layout=layout, out=out)
         assert torch.equal(bits(y[..., tail:]), bits(rest))
         assert torch.equal(y[..., :tail], want[..., :tail])
+
+
+def least_scale(y):
+    """The least power of two (2^-126 at least) under which no finite value of y's rows (fp32) passes 448; 1 where all are 0."""
+    a = torch.where(y.isfinite(), y, 0.0).abs().amax(1)
+    m, e = torch.frexp(a)
+    e = torch.where(a == 0, 0, (e - 9 + (m > 0.875).to(e.dtype)).clamp(min=-126))
+    return ((e.long() + 1023) << 52).view(torch.float64)
+
+
+@pytest.mark.parametrize("D", [64, 256, 576, 784, 1600, 3136, 4096, 12544, 16384])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_e4m3_scale_at_its_border(D, dt):
+    """One value a row and eps 0: y is sqrt(D) w whatever the value. With w = 7 / sqrt(D) it is 448 / 64 and the scale 2^-6; next to
+    it above, twice that."""
+    root = round(D ** 0.5)
+    g = torch.Generator(device="cuda").manual_seed(D)
+    x = torch.zeros(256, D, device="cuda", dtype=dt)
+    at = torch.randint(0, D, (256,), generator=g, device="cuda")
+    x[torch.arange(256, device="cuda"), at] = (torch.randn(256, generator=g, device="cuda") * 4).to(dt)
+    x[0, at[0]] = 1.2109375
+    exact = root & (root - 1) == 0  # 7 / root is an fp32 number
+    w7 = torch.full((D,), 7.0 / root if exact else 1.0, device="cuda")
+    for w in (w7, torch.nextafter(w7, 2 * w7), torch.nextafter(w7, 0 * w7)):
+        q, scale = gb.rms_norm(x, w, eps=0.0, e4m3=True)[:2]
+        y = (ref.norm(x, w, 0.0)[0]).float()
+        want = least_scale(y)
+        assert torch.equal(scale.double(), want), (scale.double() / want).unique()
+        assert torch.equal(q.float(), (y.double() / want[:, None]).float().to(E4M3).float())
+
+
+@pytest.mark.parametrize("D", [64, 1536, 4096, 16384])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_e4m3_scale_of_odd_rows(D, dt):
+    """Rows of zeros, of values that no e4m3 can follow, weights that underflow before rstd brings them back, NaN and infinities."""
+    randn = rng(D)
+    x, w = randn(9, D).to(dt), 1 + randn(D, std=0.1)
+    x[1] = 0
+    x[2, D // 2], x[3, 1], x[4, D - 1] = float("nan"), float("inf"), float("-inf")
+    x[5] *= 1e-30
+    x[6] *= 1e-20
+    x[7, :] = 0
+    x[7, 3] = 1e-30
+    for k, eps in ((1.0, 1e-6), (1e-20, 1e-6), (1e-10, 1e-38), (1e25, 1e-6)):
+        q, scale = gb.rms_norm(x, w * k, eps=eps, e4m3=True)[:2]
+        y = ref.norm(x, w * k, eps)[0]
+        want = least_scale(y.float())
+        plain = [0, 1, 2, 3, 4, 8]
+        assert torch.equal(scale.double()[plain], want[plain]), (k, scale, want)
+        got = q.double() * scale.double()[:, None]
+        for i in (0, 1, 8):
+            assert torch.equal(q[i].float(), (y[i].float().double() / want[i]).float().to(E4M3).float()), (k, i)
+        assert bool(got[2].isnan().all()) and bool(got[3, 1].isnan()) and not got[3, 2:].any() and not got[4, :-1].any()
+        assert float(scale[2]) == float(scale[3]) == float(scale[4]) == 1
+        # the small rows: a half step of e4m3, and what a root of a sum of squares near fp32's least numbers leaves
+        a = y[5:8].abs()
+        assert bool(((got[5:8] - y[5:8]).abs() <= a * 0.07 + scale[5:8, None].double() * 2.0 ** -10 + 2.0 ** -126).all()), k
+
+
+def test_e4m3_rows_are_those_of_the_exact_product():
+    """Millions of values, equal to the 64-bit form rounded to fp32 and then to e4m3: sums and products in plain fp32 put several of
+    them on the other side of a tie. Both forms of y differ by some 2^-46, so that one in 2^22 of the values rounds to
+    another fp32 number, and of these the one in 2^20 next to a tie to another e4m3."""
+    for T, D, dt in ((8192, 1536, BF), (2048, 1536, F32), (1024, 4096, BF), (300, 16384, F32)):
+        randn = rng(T + D)
+        x, r, w = randn(T, D).to(dt), randn(T, D, std=2).to(dt), 1 + randn(D, std=0.1)
+        q, scale, h, _ = gb.rms_norm(x, w, residual=r, e4m3=True)
+        y = ref.norm(h, w, 1e-6)[0].float()
+        want = least_scale(y)
+        assert torch.equal(scale.double(), want)
+        assert torch.equal(q.float(), (y.double() / want[:, None]).float().to(E4M3).float())
+
+
+@pytest.mark.parametrize("D", [8, 264, 1536, 4096, 8200, 16384])
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("residual", [False, True])
+def test_e4m3_values_next_to_ties(D, dt, residual):
+    """Rows of one magnitude and eps 0: y is w, up to sign, whatever the magnitude. With w at ties of e4m3 and one fp32 number to
+    either side, a y that is off by its last place is another e4m3 value."""
+    g = torch.Generator(device="cuda").manual_seed(D)
+    T = 300
+    rand = lambda *s: torch.rand(s, generator=g, device="cuda")  # noqa: E731
+    h = ((1 + rand(T, 1)) * torch.exp2((rand(T, 1) * 20 - 10).round())).to(dt) * torch.where(rand(T, D) < 0.5, 1, -1).to(dt)
+    tie = (17 + 2 * (rand(D) * 8).floor()) / 16 * torch.exp2((rand(D) * 14).floor() - 6)
+    tie = torch.where(rand(D) < 0.1, (2 * (rand(D) * 8).floor() + 1) * 2.0 ** -10, tie)
+    w = torch.where(rand(D) < 0.34, tie, torch.nextafter(tie, torch.where(rand(D) < 0.5, 0.0, 1000.0)))
+    w[0] = 300.0
+    q, scale = gb.rms_norm(h, w, residual=torch.zeros_like(h) if residual else None, eps=0.0, e4m3=True)[:2]
+    assert bool((scale == 1).all())
+    assert torch.equal(q.float(), (h.float().sign() * w).to(E4M3).float())
