@@ -584,7 +584,8 @@ SSBA_API int ssba_linear_backward(const ssba_linear_desc* desc, const void* dy, 
  *   shared = 0  theta of an axis's i-th pair is base^(-i / sections[a]): every axis has the whole range of rates;
  *   shared = 1  theta of pair j is base^(-j / P): the axes share one range.
  *   layout      SSBA_ROPE_PAIRS: pair j is dimensions 2j, 2j + 1; SSBA_ROPE_HALVES: j, j + P.
- * Dimensions from 2P on are copied. Angles are exact to 2^-32 of a turn, beside theta's own rounding to 53 bits, at any position. */
+ * Dimensions from 2P on are copied, bit for bit. At any position, sines and cosines are fp32 and within 1.5 * 2^-24 of those of
+ * the product of the position and theta, theta's own rounding to 53 bits apart. */
 #define SSBA_ROPE_MAX_AXES 4
 #define SSBA_ROPE_MAX_HEAD_DIM 256
 enum { SSBA_ROPE_PAIRS = 0, SSBA_ROPE_HALVES = 1 };

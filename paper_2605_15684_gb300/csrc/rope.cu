@@ -5,9 +5,10 @@
 // Pairs are adjacent dimensions (2j, 2j + 1) or halves (j, j + P); dimensions from 2P on stay.
 //
 // Angles: theta_j / (2 pi) is held as a 64-bit fraction of a turn, whose product with an integer position modulo 2^64 is
-// the angle modulo whole turns, without a rounding: at any position the angle is off by 2^-32 of a turn and by what
-// theta's own 53 bits leave (a product in fp32 is off by a tenth of a radian at a million). The top 32 bits, signed,
-// are the angle in units of 2^-31 pi, which sincospif takes.
+// the angle modulo whole turns, without a rounding (a product in fp32 is off by a tenth of a radian at a million). Its top 24
+// bits, signed, are an fp32 number of units of pi, which sincospif takes; the next 32 turn that sine and cosine on by an angle l
+// below 2^-24 of a turn, sin + l cos and cos - l sin (l^2 is 2^-43). So the angle is used to 2^-48 of a turn, beside
+// theta's own 53 bits, and what is left is sincospif's error, a unit of the last place, and a rounding.
 //
 // Bound by HBM: x is read once and written once, 16 bytes a thread and step where the strides and the cut allow it (else
 // 8, 4 or 2). A thread forms the sines of its pairs of one token once and applies them to the heads of its share.
@@ -150,7 +151,11 @@ __global__ void __launch_bounds__(256) ssba_rope_kernel(const __grid_constant__ 
             continue;
         }
         const uint64_t turns = (uint64_t)(int64_t)pos[p.axis[j]] * p.theta[j];
-        sincospif((float)(int32_t)(turns >> 32) * 4.656612873077393e-10f, &s[i], &c[i]);
+        const float l = (float)(uint32_t)(turns >> 8) * 8.719671245021580e-17f;  // 2 pi 2^-56
+        float sn, cs;
+        sincospif((float)((int32_t)(turns >> 32) & ~0xff) * 4.656612873077393e-10f, &sn, &cs);
+        s[i] = fmaf(l, cs, sn);
+        c[i] = fmaf(-l, sn, cs);
         if (p.inverse) s[i] = -s[i];
     }
     for (int h = h0;;) {

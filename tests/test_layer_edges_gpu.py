@@ -5,6 +5,7 @@ import torch
 import paper_2605_15684_gb300 as gb
 from paper_2605_15684_gb300 import api, build
 from tests import layer_ref as ref
+from tests.layer_ref import near
 
 pytestmark = pytest.mark.gpu
 BF, F32, E4M3 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
@@ -140,3 +141,19 @@ def test_e4m3_values_next_to_ties(D, dt, residual):
     q, scale = gb.rms_norm(h, w, residual=torch.zeros_like(h) if residual else None, eps=0.0, e4m3=True)[:2]
     assert bool((scale == 1).all())
     assert torch.equal(q.float(), (h.float().sign() * w).to(E4M3).float())
+
+
+@pytest.mark.parametrize("layout", ["pairs", "halves"])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_rope_angles_in_fp32(layout, inverse):
+    """Pairs (1, 0) become a cosine and a sine. sincospif is within one unit of its last place, 2^-24 below 1; the rest of the angle
+    adds a rounding, 2^-25; the angle's own error at positions up to 2^20 (theta's 53 bits, and the reference's angle) is below
+    2^20 2^-51. Angles of 24 bits alone would be off by up to 2^-26 of a turn, 2^-23.3."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    T, axes, P = 20000, (32, 96), 128
+    pos = torch.randint(-2 ** 20, 2 ** 20, (T, 2), generator=g, device="cuda", dtype=torch.int32)
+    x = torch.zeros(1, T, 1, 2 * P, device="cuda")
+    x[..., 0::2 if layout == "pairs" else 1][..., :P] = 1
+    y = gb.rope_axes(x, pos, axes, layout=layout, inverse=inverse)
+    want = ref.rope(x, pos, axes, 10000.0, layout, False, inverse)
+    near(y, want, torch.full_like(want, 2.0 ** -24 + 2.0 ** -25 + 2.0 ** -30), "angles")
