@@ -603,7 +603,7 @@ typedef struct {
  *               x with the same strides; else they may not share an element (other parts of one tensor may be interleaved, at the
  *               same strides), nor may two heads of out.
  *   pos         device, int32, any sign: axis a of token t of sequence b at b pos_batch + t axes + a (pos_batch 0:
- *               the same positions for all sequences). */
+ *               the same positions for all sequences). It may not lie between out's first element and its last. */
 SSBA_API int ssba_rope_axes(const ssba_rope_desc* desc, const void* x, const int64_t* x_stride, const int32_t* pos,
                             int64_t pos_batch, void* out, const int64_t* out_stride, void* stream);
 

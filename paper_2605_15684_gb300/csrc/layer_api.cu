@@ -54,13 +54,16 @@ bool lie_on_each_other(int64_t apart, const int64_t* size, const int64_t* stride
     return false;
 }
 
+// From the first element of heads at these strides to behind the last.
+Range rope_extent(const ssba_rope_desc& d, const void* at, const int64_t* s, int64_t es)
+{
+    return Range{at, (size_t)(((d.B - 1) * s[0] + (d.T - 1) * s[1] + (d.heads - 1) * s[2] + d.head_dim) * es)};
+}
+
 // Whether writing `out` may change an x that is still to be read: not where out is x, nor where they share nothing.
 bool rope_overlaps(const ssba_rope_desc& d, const void* x, const int64_t* xs, const void* out, const int64_t* os, int64_t es)
 {
-    auto extent = [&](const void* at, const int64_t* s) {
-        return Range{at, (size_t)(((d.B - 1) * s[0] + (d.T - 1) * s[1] + (d.heads - 1) * s[2] + d.head_dim) * es)};
-    };
-    if (!extent(x, xs).meets(extent(out, os))) return false;
+    if (!rope_extent(d, x, xs, es).meets(rope_extent(d, out, os, es))) return false;
     int64_t size[4] = {d.B, d.T, d.heads, d.head_dim}, stride[4] = {os[0], os[1], os[2], 1};
     for (int i = 0; i < 3; ++i)
         if (xs[i] != os[i] && size[i] > 1) return true;
@@ -329,6 +332,8 @@ int ssba_rope_axes(const ssba_rope_desc* desc, const void* x, const int64_t* x_s
         for (int i = 0; i < 3; ++i) fits = fits && x_stride[i] % 2 == 0 && out_stride[i] % 2 == 0;
     if (!fits) return invalid(who, "x and out must be aligned to an element (adjacent pairs: to a pair, strides too), pos to 4 bytes");
     if (rope_overlaps(d, x, x_stride, out, out_stride, es)) return invalid(who, "out lies on x (it may be x with the same strides)");
+    const Range positions{pos, sizeof(int32_t) * ((size_t)(d.B - 1) * (size_t)pos_batch + (size_t)d.T * d.axes)};
+    if (rope_extent(d, out, out_stride, es).meets(positions)) return invalid(who, "out lies on pos");
     return launch_rope(d, x, x_stride, pos, pos_batch, out, out_stride, static_cast<cudaStream_t>(stream));
 }
 

@@ -177,6 +177,13 @@ def test_rope_refuses_an_output_on_its_input(lib, apart, xs, os):
     assert rc == INV and b"lies on" in lib.ssba_last_error()
 
 
+@pytest.mark.parametrize("pb,at", [(0, -4 * 2 * 4 + 4), (0, 0), (0, 4 * (768 * 3 + 192 * 3 + 64 * 2 + 64) - 4), (8, -4 * (3 * 8 + 4 * 2) + 4), (8, -4 * 3 * 8)])
+def test_rope_refuses_an_output_on_its_positions(lib, pb, at):
+    out = 0x100000000
+    rc = lib.ssba_rope_axes(rope_desc(B=4, heads=3, dtype=api.SSBA_FP32), 0x900000000, S(768, 192, 64), out + at, pb, out, S(768, 192, 64), None)
+    assert rc == INV and b"lies on pos" in lib.ssba_last_error()
+
+
 def test_timeout_hook_refusals(lib):
     for d in (dict(T=0), dict(dtype=2), dict(N=60)):
         assert lib.ssba_test_linear_timeout(linear_desc(**d), FAKE, FAKE, FAKE, 1000000, None) in (INV, UNS)
