@@ -21,7 +21,8 @@
 // of 512 cycles; 600 measured). An epilogue of eight warps took longer than 12 steps of it, waiting for its loads
 // and for the special function units in turn.
 // Sums are fp32 in TMEM; z and y are rounded once each. Tiles go through the rows in bands of eight tiles, so that the
-// CTAs at work share operands in L2. Every wait is bounded; a timeout is written to the device status word.
+// CTAs at work share operands in L2. Waits on barriers in shared memory are bounded; a timeout is written to the device status word. The
+// allocation of tensor memory and the cluster's barriers have no limit of their own: each ends as the CTAs that it waits for do.
 #include <cstddef>
 #include <cstring>
 
@@ -575,7 +576,7 @@ int launch_pairs(PairMaps& maps, PairParams& p, const char* who, cudaStream_t st
     const int P = p.pairs;
     // In stream order, neither beginning before the grid in front has ended nor letting the next one begin. Pairs that
     // were set up beside the last waves of another grid (a gated block's backward pass, many calls queued)
-    // did not end; a launch of its own costs about 2 us.
+    // did not end; the cause is not known. A launch of its own costs about 2 us.
     const cudaError_t err = launch_on(false, kernel, dim3(2 * P), kThreads, smem, st, 2, maps, p);
     if (err == cudaSuccess) return SSBA_OK;
     set_error("%s: ssba_product_pair_kernel launch: %s", who, cudaGetErrorString(err));

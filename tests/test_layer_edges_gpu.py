@@ -157,3 +157,20 @@ def test_rope_angles_in_fp32(layout, inverse):
     y = gb.rope_axes(x, pos, axes, layout=layout, inverse=inverse)
     want = ref.rope(x, pos, axes, 10000.0, layout, False, inverse)
     near(y, want, torch.full_like(want, 2.0 ** -24 + 2.0 ** -25 + 2.0 ** -30), "angles")
+
+
+@pytest.mark.parametrize("T,K,N", [(3, 256, 8192), (40, 1536, 6144), (64, 512, 16384), (256, 1536, 1536)])
+def test_few_rows_backward_queued(T, K, N):
+    """Backward passes of few rows queued far ahead of the GPU: each launches the few-row product early, behind the grid of the
+    slopes, and the next slopes behind it."""
+    randn = rng(T)
+    x, W = randn(T, K).to(BF), randn(N, K, std=K ** -0.5).to(BF)
+    Wg = torch.cat((W, W))
+    dy, z, zg = randn(T, N).to(BF), randn(T, N).to(BF), randn(T, 2 * N).to(BF)
+    want = [gb.linear_backward(dy, x, W, z=z, act="gelu", bias=True), gb.gated_linear_backward(dy, x, Wg, zg), (gb.gated_linear(x, Wg),)]
+    for _ in range(150):
+        got = [gb.linear_backward(dy, x, W, z=z, act="gelu", bias=True), gb.gated_linear_backward(dy, x, Wg, zg), (gb.gated_linear(x, Wg),)]
+    torch.cuda.synchronize()
+    assert api.get_status() == api.SSBA_OK
+    for a, b in zip(sum(map(list, got), []), sum(map(list, want), [])):
+        assert torch.equal(a, b)
