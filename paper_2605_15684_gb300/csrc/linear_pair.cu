@@ -501,9 +501,9 @@ __global__ void __launch_bounds__(PairCfg<kBN, kEpi, kZ>::kThreads, 1)
     if (warp == 1) tmem_free_pair(tbase, 2 * kBN);
 }
 
-// Pairs of CTAs that run at once on the current device.
-template <class Kernel>
-int pairs_at_once(Kernel k, int threads, size_t smem)
+// Pairs of CTAs of a kernel that run at once on the current device, kept for each kernel by itself (they are one type).
+template <auto kernel>
+int pairs_at_once(int threads, size_t smem)
 {
     static int cache[kMaxDevices] = {};
     static std::mutex m;
@@ -521,7 +521,7 @@ int pairs_at_once(Kernel k, int threads, size_t smem)
     cfg.attrs = la;
     cfg.numAttrs = 1;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, k, &cfg) != cudaSuccess || n < 1) {
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
         cudaGetLastError();
         return device_sm_count() / 2 > 0 ? device_sm_count() / 2 : 1;
     }
@@ -564,7 +564,7 @@ long long plan(PairParams& p, int most)
 template <int kBN, bool kF8, int kEpi, bool kZ>
 int launch_pairs(PairMaps& maps, PairParams& p, const char* who, cudaStream_t st)
 {
-    auto kernel = ssba_product_pair_kernel<kBN, kF8, kEpi, kZ>;
+    constexpr auto kernel = ssba_product_pair_kernel<kBN, kF8, kEpi, kZ>;
     constexpr int kThreads = PairCfg<kBN, kEpi, kZ>::kThreads;
     const size_t smem = sizeof(PairSmem<kBN, kEpi, kZ>) + 1024;
     static PerDeviceOnce attr;
@@ -574,7 +574,7 @@ int launch_pairs(PairMaps& maps, PairParams& p, const char* who, cudaStream_t st
         set_error("%s: could not resolve the device status word", who);
         return SSBA_ERR_CUDA;
     }
-    plan(p, pairs_at_once(kernel, kThreads, smem));
+    plan(p, pairs_at_once<kernel>(kThreads, smem));
     const int P = p.pairs;
     // In stream order, neither beginning before the grid in front has ended nor letting the next one begin. Pairs that
     // were set up beside the last waves of another grid (a gated block's backward pass, many calls queued)
