@@ -599,9 +599,9 @@ typedef struct {
 
 /*   x, out      device; head h of token t of sequence b starts at b s[0] + t s[1] + h s[2] elements (x_stride, out_stride,
  *               host arrays of three), its dimensions side by side. Aligned to their element; the more of base, strides,
- *               head_dim (and, in halves, P) is in multiples of 16 bytes, the wider the accesses. Strides >= 0. out may be
- *               x with the same strides; else they may not share an element (other parts of one tensor may be interleaved, at the
- *               same strides), nor may two heads of out.
+ *               head_dim (and, in halves, P) is in multiples of 16 bytes, the wider the accesses. Strides >= 0; that of a
+ *               dimension of one is not looked at. out may be x with the same strides; else they may not share an element (other
+ *               parts of one tensor may be interleaved, at the same strides), nor may two heads of out.
  *   pos         device, int32, any sign: axis a of token t of sequence b at b pos_batch + t axes + a (pos_batch 0:
  *               the same positions for all sequences). It may not lie between out's first element and its last. */
 SSBA_API int ssba_rope_axes(const ssba_rope_desc* desc, const void* x, const int64_t* x_stride, const int32_t* pos,

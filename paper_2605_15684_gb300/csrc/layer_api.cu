@@ -319,9 +319,13 @@ int ssba_rope_axes(const ssba_rope_desc* desc, const void* x, const int64_t* x_s
     }
     if (!x_stride || !out_stride) return invalid(who, "the strides must be non-null");
     const int64_t es = d.dtype == SSBA_BF16 ? 2 : 4;
-    for (int i = 0; i < 3; ++i)
-        if (x_stride[i] < 0 || out_stride[i] < 0 || x_stride[i] > (1ll << 42) || out_stride[i] > (1ll << 42))
-            return invalid(who, "strides must be >= 0 and at most 2^42 elements");
+    int64_t xs[3], os[3];  // a dimension of one has no stride
+    const int32_t sizes[3] = {d.B, d.T, d.heads};
+    for (int i = 0; i < 3; ++i) {
+        xs[i] = sizes[i] > 1 ? x_stride[i] : 0;
+        os[i] = sizes[i] > 1 ? out_stride[i] : 0;
+        if (xs[i] < 0 || os[i] < 0 || xs[i] > (1ll << 42) || os[i] > (1ll << 42)) return invalid(who, "strides must be >= 0 and at most 2^42 elements");
+    }
     if (pos_batch < 0) return invalid(who, "pos_batch must be >= 0");
     if (d.B == 0 || d.T == 0) return SSBA_OK;
     if (!x || !pos || !out) return invalid(who, "x, pos and out must be non-null");
@@ -329,12 +333,12 @@ int ssba_rope_axes(const ssba_rope_desc* desc, const void* x, const int64_t* x_s
     const int64_t unit = d.layout == SSBA_ROPE_PAIRS ? 2 * es : es;
     bool fits = aligned(x, unit) && aligned(out, unit) && aligned(pos, 4);
     if (d.layout == SSBA_ROPE_PAIRS)
-        for (int i = 0; i < 3; ++i) fits = fits && x_stride[i] % 2 == 0 && out_stride[i] % 2 == 0;
+        for (int i = 0; i < 3; ++i) fits = fits && xs[i] % 2 == 0 && os[i] % 2 == 0;
     if (!fits) return invalid(who, "x and out must be aligned to an element (adjacent pairs: to a pair, strides too), pos to 4 bytes");
-    if (rope_overlaps(d, x, x_stride, out, out_stride, es)) return invalid(who, "out lies on x (it may be x with the same strides)");
+    if (rope_overlaps(d, x, xs, out, os, es)) return invalid(who, "out lies on x (it may be x with the same strides)");
     const Range positions{pos, sizeof(int32_t) * ((size_t)(d.B - 1) * (size_t)pos_batch + (size_t)d.T * d.axes)};
-    if (rope_extent(d, out, out_stride, es).meets(positions)) return invalid(who, "out lies on pos");
-    return launch_rope(d, x, x_stride, pos, pos_batch, out, out_stride, static_cast<cudaStream_t>(stream));
+    if (rope_extent(d, out, os, es).meets(positions)) return invalid(who, "out lies on pos");
+    return launch_rope(d, x, xs, pos, pos_batch, out, os, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -174,3 +174,20 @@ def test_few_rows_backward_queued(T, K, N):
     assert api.get_status() == api.SSBA_OK
     for a, b in zip(sum(map(list, got), []), sum(map(list, want), [])):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("layout", ["pairs", "halves"])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_rope_strides_of_single_rows(layout, dt):
+    """A dimension of one has no stride: odd and huge ones there are nothing to a call."""
+    randn = rng(7)
+    row = randn(2, 193).to(dt)[:1, :192]
+    x = row.as_strided((1, 1, 3, 64), (193, 193, 64, 1))
+    pos = torch.tensor([[17, 5]], device="cuda", dtype=torch.int32)
+    want = gb.rope_axes(x.clone(memory_format=torch.contiguous_format), pos, (16, 16), layout=layout)
+    assert torch.equal(gb.rope_axes(x, pos, (16, 16), layout=layout), want)
+    for st in ((2 ** 50 + 1, 193, 64, 1), (1, 2 ** 43, 64, 1)):
+        z = torch.zeros(192, device="cuda", dtype=dt).as_strided((1, 1, 3, 64), st)
+        assert torch.equal(gb.rope_axes(x, pos, (16, 16), layout=layout, out=z), want)
+        assert torch.equal(gb.rope_axes(z, pos, (16, 16), layout=layout, inverse=True, out=z, stream=torch.cuda.current_stream()),
+                           gb.rope_axes(want, pos, (16, 16), layout=layout, inverse=True))
