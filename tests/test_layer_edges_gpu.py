@@ -1,4 +1,6 @@
 """GPU tests of a layer's operators at their edges: values and layouts that are allowed and seldom met."""
+import threading
+
 import pytest
 import torch
 
@@ -191,3 +193,92 @@ def test_rope_strides_of_single_rows(layout, dt):
         assert torch.equal(gb.rope_axes(x, pos, (16, 16), layout=layout, out=z), want)
         assert torch.equal(gb.rope_axes(z, pos, (16, 16), layout=layout, inverse=True, out=z, stream=torch.cuda.current_stream()),
                            gb.rope_axes(want, pos, (16, 16), layout=layout, inverse=True))
+
+
+@pytest.mark.parametrize("T,D", [(40, 1536), (9, 4096), (5, 8200), (3, 16384), (64, 264)])
+def test_norm_sums_in_fp32(T, D):
+    """fp32 rows to what the kernel's tree of sums allows. A thread adds at most 24 squares, then up to ten sums of threads: 34
+    roundings of 2^-24, halved by the root; mean, eps, root and quotient add two, the products of y two more."""
+    randn = rng(D)
+    x, w = randn(T, D), 1 + randn(D, std=0.2)
+    y, _, rstd = gb.rms_norm(x, w)
+    yr, k = ref.norm(x, w, 1e-6)
+    off = (34 / 2 + 2) * 2.0 ** -24
+    near(rstd, k, k * off, "rstd")
+    near(y, yr, yr.abs() * (off + 2 * 2.0 ** -24), "y")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("D", [264, 1536, 4096])
+def test_norm_of_rows_that_are_not_finite(D, dt):
+    """NaN and infinities stay in their rows, forward; backward too, but for dw, which sums over the rows."""
+    randn = rng(D)
+    x, r, w, dy = randn(40, D).to(dt), randn(40, D).to(dt), 1 + randn(D, std=0.1), randn(40, D).to(dt)
+    good = gb.rms_norm(x, w, residual=r)
+    back = gb.rms_norm_backward(dy, x, w, good[2])
+    x[3, 5], r[17, 0], x[30, D - 1] = float("nan"), float("inf"), float("-inf")
+    bad = gb.rms_norm(x, w, residual=r)
+    rows = torch.ones(40, dtype=torch.bool, device="cuda")
+    rows[[3, 17, 30]] = False
+    for a, b in zip(bad, good):
+        assert torch.equal(a[rows], b[rows])
+    assert bool(bad[0][3].isnan().all()) and bool(bad[0][17, 0].isnan()) and not bad[0][17, 1:].any()
+    assert float(bad[2][17]) == float(bad[2][30]) == 0 and bool(bad[2][3].isnan())
+    dx, dw = gb.rms_norm_backward(dy, x, w, good[2])
+    assert torch.equal(dx[rows], back[0][rows]) and bool(dx[3].isnan().all())
+
+
+@pytest.mark.parametrize("layout", ["pairs", "halves"])
+def test_rope_of_values_that_are_not_finite(layout):
+    """A NaN or an infinity reaches its own pair alone."""
+    x = rng(4)(1, 6, 5, 64).to(BF)
+    pos = torch.arange(12, device="cuda", dtype=torch.int32).view(6, 2) + 1
+    good = gb.rope_axes(x, pos, (16, 16), layout=layout)
+    x[0, 2, 1, 10], x[0, 4, 3, 63], x[0, 5, 0, 0] = float("nan"), float("inf"), float("-inf")
+    bad = gb.rope_axes(x, pos, (16, 16), layout=layout)
+    where = torch.zeros_like(x, dtype=torch.bool)
+    for t, h, i in ((2, 1, 10), (4, 3, 63), (5, 0, 0)):
+        where[0, t, h, i] = where[0, t, h, i ^ 1 if layout == "pairs" else (i + 32) % 64] = True
+    assert torch.equal(bad[~where], good[~where]) and not bool(bad[where].isfinite().any())
+
+
+def test_threads_through_the_native_calls():
+    """Layer calls from four threads, each on a stream of its own: the extension lets the interpreter's lock go."""
+    work, bad, start = [], [], threading.Barrier(4)
+    for i in range(4):
+        randn = rng(i)
+        T, K, N = (5, 70, 300, 1100)[i], 256 + 64 * i, 144 + 8 * i
+        x, r, W, w, b = randn(T, K).to(BF), randn(T, K).to(BF), randn(N, K, std=K ** -0.5).to(BF), 1 + randn(K, std=0.1), randn(N)
+        pos = torch.randint(0, 99, (T, 2), device="cuda", dtype=torch.int32)
+        dy, axes = randn(T, N).to(BF), (8 + 2 * i, 16)
+
+        def run(x=x, r=r, W=W, w=w, b=b, pos=pos, dy=dy, axes=axes, T=T, K=K):
+            y, h, rstd = gb.rms_norm(x, w, residual=r)
+            z, pre = gb.linear(y, W, bias=b, act="gelu", pre=True)
+            dx, dW, db = gb.linear_backward(dy, y, W, z=pre, act="gelu", bias=True)
+            dn, dw = gb.rms_norm_backward(dx, h, w, rstd, dh=r)
+            q, s = gb.rms_norm(x, w, e4m3=True)[:2]
+            return [y, h, rstd, z, pre, dx, dW, db, dn, dw, q.float(), s, gb.rope_axes(x.view(T, K // 64, 64), pos, axes)]
+
+        work.append((run, run()))
+    torch.cuda.synchronize()
+
+    def thread(run, want):
+        try:
+            s = torch.cuda.Stream()
+            with torch.cuda.stream(s):
+                start.wait()
+                for _ in range(200):
+                    got = run()
+            s.synchronize()
+            if not all(torch.equal(a, b) for a, b in zip(got, want)):
+                bad.append("results differ")
+        except Exception as e:
+            bad.append(repr(e))
+
+    threads = [threading.Thread(target=thread, args=w) for w in work]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
