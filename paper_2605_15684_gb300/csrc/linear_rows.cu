@@ -6,7 +6,7 @@
 // Gated, a tile is 64 gate rows over the 64 matching up rows. For dx = dz W the weights come along their rows ("mn").
 // The partial tiles stay in shared memory (fp32, where the operands were) and each CTA of the cluster adds up and
 // finishes a share of the outputs through distributed shared memory: no workspace, no atomics, one order.
-// Bound by HBM (the weights once; tokens come from L2): some 200 KB of operands are under way in an SM, of two or three CTAs.
+// Bound by HBM (the weights once; tokens come from L2): some 200 KB of operands are under way in an SM, of two CTAs.
 // 192 threads: warp 0 TMA, warp 1 tcgen05.mma M = 128, N = kNT, warps 2-5 take D out of TMEM, and all finish.
 // Waits on barriers in shared memory are bounded; a timeout is written to the device status word. The allocation of tensor memory, the
 // cluster's barrier and the wait for the grid in front have no limit of their own: each ends as the CTAs that it
@@ -28,16 +28,18 @@ constexpr uint32_t kABytes = 128 * 128;
 constexpr int kPitch = 132;  // floats of a column of D: 128 and a shift of banks
 constexpr int kMaxSplit = 8;
 
-// kMany: three CTAs an SM with shorter rings, in place of two.
-template <int kNT, bool kMany>
+// Two CTAs an SM. (Three with shorter rings, where that let K be cut once more, took 1 to 12 % longer with tensor memory taken behind
+// the wait, and half as long again where clusters of eight then needed a second round: 12 tokens, K 4096: gated N 11008 28.1 us
+// against 29.3, N 7168 11.2 against 15.6; 16 tokens, 1536 x 6144 6.1 against 7.1; 32, 8-bit gated 4096 x 12288 19.4 against 20.)
+template <int kNT>
 struct RowsCfg {
     static constexpr uint32_t kBBytes = kNT * 128;
-    static constexpr int kStages = kNT == 16 ? (kMany ? 4 : 6) : kNT == 32 ? (kMany ? 3 : 5) : kNT == 64 ? 4 : 3;
+    static constexpr int kStages = kNT == 16 ? 6 : kNT == 32 ? 5 : kNT == 64 ? 4 : 3;
 };
 
-template <int kNT, bool kMany>
+template <int kNT>
 struct __align__(1024) RowsSmem {
-    using C = RowsCfg<kNT, kMany>;
+    using C = RowsCfg<kNT>;
     union {
         struct {
             uint8_t a[C::kStages][kABytes];
@@ -110,11 +112,11 @@ __device__ __forceinline__ float4 scaled(float4 v, const RowsParams& p, int t, c
     return make_float4(v.x * (x * w.x), v.y * (x * w.y), v.z * (x * w.z), v.w * (x * w.w));
 }
 
-template <int kNT, bool kMany, bool kF8, bool kWmn, bool kGated>
+template <int kNT, bool kF8, bool kWmn, bool kGated>
 __global__ void __launch_bounds__(kThreads) ssba_product_rows_kernel(const __grid_constant__ RowsMaps maps, const RowsParams p)
 {
-    using C = RowsCfg<kNT, kMany>;
-    using Smem = RowsSmem<kNT, kMany>;
+    using C = RowsCfg<kNT>;
+    using Smem = RowsSmem<kNT>;
     constexpr int kStages = C::kStages, kBK = kF8 ? 128 : 64;
     constexpr int kOut = kGated ? 64 : 128;  // outputs a token of a tile
     constexpr uint32_t kIdesc = idesc_of(kF8, 128, kNT, kWmn, false);
@@ -288,20 +290,20 @@ __global__ void __launch_bounds__(kThreads) ssba_product_rows_kernel(const __gri
     if (warp == 1) tmem_dealloc(tbase, kTmem);
 }
 
-// CTAs that share a tile's K: as many as the SMs hold (ctas each), with two steps each at least.
-int split_of(long long tiles, int ksteps, int ctas)
+// CTAs that share a tile's K: as many as the SMs hold (two each), with two steps each at least.
+int split_of(long long tiles, int ksteps)
 {
     int split = 1;
-    while (split < kMaxSplit && tiles * split * 2 <= (long long)ctas * device_sm_count() && ksteps >= split * 4) split *= 2;
+    while (split < kMaxSplit && tiles * split * 2 <= 2ll * device_sm_count() && ksteps >= split * 4) split *= 2;
     return split;
 }
 
-template <int kNT, bool kMany, bool kF8, bool kWmn, bool kGated>
+template <int kNT, bool kF8, bool kWmn, bool kGated>
 int launch_as(const Product& q, const char* who, cudaStream_t st)
 {
     constexpr int kBK = kF8 ? 128 : 64, kOut = kGated ? 64 : 128;
-    auto kernel = ssba_product_rows_kernel<kNT, kMany, kF8, kWmn, kGated>;
-    const size_t smem = sizeof(RowsSmem<kNT, kMany>) + 1024;
+    auto kernel = ssba_product_rows_kernel<kNT, kF8, kWmn, kGated>;
+    const size_t smem = sizeof(RowsSmem<kNT>) + 1024;
     static PerDeviceOnce attr;
     attr.run([=] { cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
     const int e = kF8 ? 1 : 2;
@@ -334,30 +336,19 @@ int launch_as(const Product& q, const char* who, cudaStream_t st)
         return SSBA_ERR_CUDA;
     }
     const long long tiles = (q.N + kOut - 1) / kOut, cols = (q.M + kNT - 1) / kNT;
-    const int split = p.split = split_of(tiles * cols, p.ksteps, kMany ? 3 : 2);
+    const int split = p.split = split_of(tiles * cols, p.ksteps);
     const cudaError_t err = launch_early(kernel, dim3((unsigned)(tiles * split), (unsigned)cols), kThreads, smem, st, split, maps, p);
     if (err == cudaSuccess) return SSBA_OK;
     set_error("%s: ssba_product_rows_kernel launch: %s", who, cudaGetErrorString(err));
     return SSBA_ERR_CUDA;
 }
 
-template <int kNT, bool kMany>
+template <int kNT>
 int launch_tokens(const Product& q, const char* who, cudaStream_t st)
 {
-    if (q.b_mn) return launch_as<kNT, kMany, false, true, false>(q, who, st);
-    if (q.gated) return q.f8 ? launch_as<kNT, kMany, true, false, true>(q, who, st) : launch_as<kNT, kMany, false, false, true>(q, who, st);
-    return q.f8 ? launch_as<kNT, kMany, true, false, false>(q, who, st) : launch_as<kNT, kMany, false, false, false>(q, who, st);
-}
-
-// Three CTAs an SM where that lets K be cut once more than two do, so that the SMs have more alike to read: one token,
-// K 4096, gated N 11008 33.4 -> 31.1 us; 16 tokens, 1536 x 6144 7.3 -> 6.8. Elsewhere the longer rings win: 7 tokens, 4096 x
-// 4096 8.6 us against 10.5; 16 tokens, gated 1536 x 4096 7.6 against 9.4. 32 tokens, 8-bit gated 4096 x 12288: three 19.2 us, two 20.6.
-template <int kNT>
-int launch_few(const Product& q, const char* who, cudaStream_t st)
-{
-    const long long tiles = (q.N + (q.gated ? 63 : 127)) / (q.gated ? 64 : 128);
-    const int ksteps = (q.K + (q.f8 ? 127 : 63)) / (q.f8 ? 128 : 64);
-    return split_of(tiles, ksteps, 3) > split_of(tiles, ksteps, 2) ? launch_tokens<kNT, true>(q, who, st) : launch_tokens<kNT, false>(q, who, st);
+    if (q.b_mn) return launch_as<kNT, false, true, false>(q, who, st);
+    if (q.gated) return q.f8 ? launch_as<kNT, true, false, true>(q, who, st) : launch_as<kNT, false, false, true>(q, who, st);
+    return q.f8 ? launch_as<kNT, true, false, false>(q, who, st) : launch_as<kNT, false, false, false>(q, who, st);
 }
 
 }  // namespace
@@ -372,7 +363,7 @@ double rows_us(int nt, long long M, long long N, long long K, bool f8, bool gate
 {
     const long long cols = (M + nt - 1) / nt, tiles = ((N + (gated ? 63 : 127)) / (gated ? 64 : 128)) * cols, slots = 2ll * device_sm_count();
     if (cols > 65535) return 1e30;  // tiles of tokens are the grid's y
-    const int ksteps = (int)((K + (f8 ? 127 : 63)) / (f8 ? 128 : 64)), split = split_of(tiles, ksteps, 2);
+    const int ksteps = (int)((K + (f8 ? 127 : 63)) / (f8 ? 128 : 64)), split = split_of(tiles, ksteps);
     return (nt == 64 ? 6.4 : 8.4) + (nt == 64 ? 0.30 : 0.37) * ((ksteps + split - 1) / split) * ((tiles * split + slots - 1) / slots);
 }
 
@@ -385,10 +376,10 @@ double product_rows_us(long long M, long long N, long long K, bool f8, bool gate
 
 int launch_product_rows(const Product& q, const char* who, cudaStream_t st)
 {
-    if (q.M <= 16) return launch_few<16>(q, who, st);
-    if (q.M <= 32) return launch_few<32>(q, who, st);
+    if (q.M <= 16) return launch_tokens<16>(q, who, st);
+    if (q.M <= 32) return launch_tokens<32>(q, who, st);
     const bool narrow = q.M <= 64 || rows_us(64, q.M, q.N, q.K, q.f8, q.gated) <= rows_us(128, q.M, q.N, q.K, q.f8, q.gated);
-    return narrow ? launch_tokens<64, false>(q, who, st) : launch_tokens<128, false>(q, who, st);
+    return narrow ? launch_tokens<64>(q, who, st) : launch_tokens<128>(q, who, st);
 }
 
 int launch_product(const Product& q, const char* who, cudaStream_t st)
