@@ -232,13 +232,14 @@ def linear(x, W, bias=None, residual=None, act=None, x_scale=None, w_scale=None,
            stream=None):
     """ssba_linear: y = act(z) + residual with z = x W^T (x_scale w_scale) + bias; x [T, K], W [N, K] bf16, or both e4m3
     with fp32 scales [T] and [N] (rms_norm makes such rows; of weights once: s = 2 ** ceil(log2(max |W_n| / 448)), W / s
-    rounded); bias [N] fp32, residual [T, N] bf16 (may be ``y``); act None, "relu", "gelu" or "silu".
+    rounded); bias [N] fp32, residual [T, N] bf16 (may be ``y``); act None, "relu", "gelu" (its tanh form, which is not torch's default) or "silu".
     Returns y [T, N] bf16, or with ``pre`` (y, z): z is what linear_backward needs of an activation."""
     return _product(x, W, bias, residual, act, x_scale, w_scale, pre, y, z, stream, 0)
 
 
 def gated_linear(x, W, act="silu", x_scale=None, w_scale=None, pre: bool = False, y=None, z=None, stream=None):
-    """ssba_linear, gated: y = act(x Wg^T) * (x Wu^T), W [2 F, K] the rows of Wg, then those of Wu; types as linear.
+    """ssba_linear, gated: y = act(x Wg^T) * (x Wu^T), W [2 F, K] the rows of Wg, then those of Wu; types and act ("gelu" is its
+    tanh form) as linear.
     Returns y [T, F] bf16, or with ``pre`` (y, z [T, 2 F]): both products, which gated_linear_backward needs."""
     return _product(x, W, None, None, act, x_scale, w_scale, pre, y, z, stream, 1)
 
