@@ -297,12 +297,12 @@ __global__ void __launch_bounds__(PairCfg<kBN, kEpi, kZ>::kThreads, 1)
                 }
             }
             const uint32_t last = g > kStages ? g - kStages : 0;
+            // the products' arrivals on this CTA's barriers come from the first CTA: none may be under way when this one ends
+            for (uint32_t x = last; !dead && x < g; ++x) dead = !mbar_wait(smem_u32(&sm.empty[x % kStages]), (x / kStages) & 1, abortf, p.budget_ns);
             if (dead && rank == 0) {
                 // drain: the copies of the last stages issued may still be under way
                 for (uint32_t x = last; x < g; ++x) wait_raw(smem_u32(&sm.full[x % kStages]), (x / kStages) & 1, p.budget_ns);
             }
-            // the products' arrivals on this CTA's barriers come from the first CTA: none may be under way when this one ends
-            for (uint32_t x = last; !dead && x < g; ++x) dead = !mbar_wait(smem_u32(&sm.empty[x % kStages]), (x / kStages) & 1, abortf, p.budget_ns);
         }
         __syncwarp();
     } else if (warp == 1) {
