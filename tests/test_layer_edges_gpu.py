@@ -282,3 +282,23 @@ def test_threads_through_the_native_calls():
     for t in threads:
         t.join()
     assert not bad
+
+
+@pytest.mark.parametrize("T,D", [(50000, 64), (20000, 2304), (12000, 4608)])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_e4m3_scale_of_more_rows_than_ctas(T, D, dt):
+    """A third of the rows at a scale's border (one magnitude a row, so y is w, and the largest w is 448 / 64), some of NaN, and rows of
+    zeros between them, where a CTA has several rows."""
+    randn = rng(D)
+    g = torch.Generator(device="cuda").manual_seed(T)
+    w = torch.rand(D, generator=g, device="cuda") * 6
+    w[D // 3] = 7.0
+    x = randn(T, D).to(dt)
+    x[::3] = torch.where(x[::3] < 0, -1, 1) * (1.5 * torch.exp2(torch.arange(0, T, 3, device="cuda") % 20 - 10.0))[:, None].to(dt)
+    x[1::7] = 0
+    x[5::1001, D - 1] = float("nan")
+    q, scale = gb.rms_norm(x, w, eps=1e-30, e4m3=True)[:2]
+    y = ref.norm(x, w, 1e-30)[0].float()
+    want = least_scale(y)
+    assert torch.equal(scale.double(), want)
+    assert torch.equal(q.float().nan_to_num(-1.0), (y.double() / want[:, None]).float().to(E4M3).float().nan_to_num(-1.0))
