@@ -641,7 +641,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_attn_tc_kernel(const __grid_
             }
         }
     }
-    grid_dep_launch();
+    if (gwarp == 1) grid_dep_launch();  // by the warp that has taken tensor memory: the next grid's CTAs may then take theirs
     // which pipeline of this CTA, and the role within it: the softmax warps first, so that a
     // pipeline's four are one per TMEM lane quadrant (and two softmax warps share a scheduler)
     const bool soft = gwarp < kSlots * kSoftWarps;

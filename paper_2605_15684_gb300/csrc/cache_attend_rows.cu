@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(kThreads, 1) ssba_cache_attend_rows_kernel(con
     tc_fence_before();
     // everything above reads no input (programmatic dependent launch: it may run beside the last grid's end)
     grid_dep_wait();
-    grid_dep_launch();
+    if (warp == kIssue) grid_dep_launch();  // by the warp that has taken tensor memory: the next grid's CTAs may then take theirs
     make_share<false, kThreads>(p, sm);  // ends in a barrier
     tc_fence_after();
     const uint32_t tbase = sm.tmem_base;
